@@ -1,0 +1,87 @@
+/*
+ * Operators of libdit that need no context: the block-scaled e4m3 product with the quantisers of its
+ * operands, and attention over selected key blocks with the selector of its lists.  They are the two
+ * heavy parts of a DiT block in reduced arithmetic: the step runs them for contexts created with
+ * DIT_FLAG_FP8_BLOCK128 or DIT_FLAG_SPARSE_ATTENTION (dit.h), and a caller with a model of its own can
+ * call them directly.
+ *
+ * Conventions: those of dit.h (C ABI, dit_status, device pointers of the current device, `stream` a
+ * cudaStream_t), and
+ *   - every call is asynchronous on `stream`, allocates nothing, keeps nothing from one call to the next
+ *     and may be captured into a CUDA graph (the first call on a device sets kernel attributes: make it
+ *     outside a capture).  Argument errors are found on the host before any launch.
+ *   - rows, columns and leading dimensions are in elements unless stated otherwise; a leading dimension
+ *     is the distance between the starts of two rows.  Element offsets may exceed 32 bits.
+ *   - outputs are written exactly where they are defined: padding columns between a row's last element
+ *     and the next row, and rows behind the last one, stay as they were.
+ *   - results do not depend on timing: every sum is taken in an order fixed by the shapes, without
+ *     atomics.
+ *   - kernels bound their waits; one that gave up leaves its output undefined and sets a status word of
+ *     the device, which dit_ops_poll_status reads.
+ */
+#ifndef DIT_OPS_H_
+#define DIT_OPS_H_
+
+#include "dit.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+typedef enum { DIT_TYPE_F16 = 0, DIT_TYPE_BF16 = 1, DIT_TYPE_F32 = 2 } dit_type;
+
+#define DIT_BLOCK 128 /* columns per scale; rows per query block and per key block */
+
+/* Quantises a matrix x [rows, cols] row by row in groups of 128 columns (the last group may be short):
+ *   top[m, g]    = max(largest |x| of the group, 2^-100)
+ *   scale[g, m]  = top / 448                               (fp32, round to nearest)
+ *   code[m, c]   = e4m3 nearest to x[m, c] * (448 / top)   (ties to even, |code| <= 448)
+ * so that x ~ code * scale.  The scales lie group-major: scales[g * ld_scales + m], g < ceil(cols / 128).
+ * A group that holds a NaN gets a NaN scale and NaN codes; one that holds an infinity an infinite scale,
+ * so that its products are NaN.
+ *   x       device, type f16, bf16 or f32, element-aligned, ld >= cols
+ *   codes   device bytes, 16-byte aligned, ld_codes >= cols and a multiple of 16 (what dit_gemm_block128
+ *           wants of its operands)
+ *   scales  device fp32, ld_scales >= rows
+ * rows == 0 is a no-op.  DIT_ERR_INVALID_ARG for NULL pointers, bad types, leading dimensions or
+ * alignment; DIT_ERR_SHAPE for cols < 1 or rows or cols above 2^31 - 1024. */
+dit_status dit_quantize_block128(const void *x, dit_type type, int64_t ld, int64_t rows, int64_t cols, void *codes,
+                                 int64_t ld_codes, float *scales, int64_t ld_scales, void *stream);
+
+/* The same for a weight w [in, out] (y = x w, as everywhere in this library): one scale for each block of
+ * 128 x 128 elements, the codes transposed:
+ *   codes [out, ld_codes], ld_codes >= in and a multiple of 16;  scales [ceil(out / 128), ceil(in / 128)] */
+dit_status dit_quantize_weight_block128(const void *w, dit_type type, int64_t ld, int64_t in_dim, int64_t out_dim,
+                                        void *codes, int64_t ld_codes, float *scales, void *stream);
+
+/* Product of two quantised operands, both with k contiguous in a row:
+ *   out[m, n] = sum_g a_scales[g, m] * b_scales[n / 128, g] * (sum over the group's k of a[m, k] b[n, k]) + bias[n]
+ * Each group's inner sum is a tensor-core sum of exact products in fp32; the scaled sum over the groups is
+ * held in fp32 and rounded once into out.  16-bit outputs clamp to the largest finite value.
+ *   a        device e4m3 codes [m, lda], 16-byte aligned, lda >= k and a multiple of 16; columns k.. are not used
+ *   a_scales device fp32 [ceil(k / 128), ld_a_scales], ld_a_scales >= m   (dit_quantize_block128)
+ *   b        device e4m3 codes [n, ldb], likewise;  b_scales device fp32 [ceil(n / 128), ceil(k / 128)]
+ *   bias     device fp32 [n] or NULL
+ *   out      device [m, ld_out] of out_type, element-aligned, ld_out >= n; must not overlap the operands
+ * m == 0 is a no-op; DIT_ERR_SHAPE for n or k < 1 or a size above 2^31 - 1024. */
+typedef struct {
+  const void *a;
+  const float *a_scales;
+  const void *b;
+  const float *b_scales;
+  const float *bias;
+  void *out;
+  int64_t lda, ld_a_scales, ldb, ld_out;
+  int64_t m, n, k;
+  dit_type out_type;
+} dit_gemm_block128_args;
+dit_status dit_gemm_block128(const dit_gemm_block128_args *args, void *stream);
+
+/* Reads and clears (with a synchronisation of the current device) the status word that a kernel of this
+ * header sets when a bounded wait ran out: DIT_OK or DIT_ERR_TIMEOUT. */
+dit_status dit_ops_poll_status(void);
+
+#ifdef __cplusplus
+}
+#endif
+#endif /* DIT_OPS_H_ */

@@ -58,7 +58,14 @@ class DitShellWeights(C.Structure):
                                           "w_out", "b_out")]
 
 
+class DitGemmBlock128Args(C.Structure):
+    _fields_ = ([(n, C.c_void_p) for n in ("a", "a_scales", "b", "b_scales", "bias", "out")]
+                + [(n, C.c_int64) for n in ("lda", "ld_a_scales", "ldb", "ld_out", "m", "n", "k")] + [("out_type", C.c_int)])
+
+
 SCHED_EXPORTS = ["dit_sched_allocate", "dit_sched_round"]
+OPS_EXPORTS = ["dit_quantize_block128", "dit_quantize_weight_block128", "dit_gemm_block128", "dit_ops_poll_status"]
+BLOCK = 128      # columns per scale; rows per query block and per key block
 
 
 class DitSchedOption(C.Structure):
@@ -157,6 +164,14 @@ def load_library() -> C.CDLL:
     lib.dit_sched_round.restype = C.c_int
     lib.dit_sched_round.argtypes = [C.POINTER(DitSchedRequest), i32, i32, C.c_double, C.c_double, C.POINTER(i32),
                                     C.POINTER(i32), C.POINTER(i32), C.POINTER(i32)]
+    lib.dit_quantize_block128.restype = C.c_int
+    lib.dit_quantize_block128.argtypes = [vp, C.c_int, i64, i64, i64, vp, i64, vp, i64, vp]
+    lib.dit_quantize_weight_block128.restype = C.c_int
+    lib.dit_quantize_weight_block128.argtypes = [vp, C.c_int, i64, i64, i64, vp, i64, vp, vp]
+    lib.dit_gemm_block128.restype = C.c_int
+    lib.dit_gemm_block128.argtypes = [C.POINTER(DitGemmBlock128Args), vp]
+    lib.dit_ops_poll_status.restype = C.c_int
+    lib.dit_ops_poll_status.argtypes = []
     lib.dit_last_launch_count.restype = i64
     lib.dit_last_launch_count.argtypes = [vp]
     lib.dit_status_string.restype = C.c_char_p
@@ -568,6 +583,134 @@ def dit_modulation_noalloc(cond, w_ada, b_ada, mod_out, stream=None):
     if st != DIT_OK:
         raise DitError(st, lib.dit_status_string(st).decode())
     return mod_out
+
+
+# ---------------------------------------------------------------------- operators without a context (dit_ops.h)
+def _need(ok: bool, what: str):
+    if not ok:
+        raise DitError(1, what)
+
+
+def _type_code(dtype) -> int:
+    import torch
+    codes = {torch.float16: 0, torch.bfloat16: 1, torch.float32: 2}
+    _need(dtype in codes, f"{dtype} is not one of float16, bfloat16, float32")
+    return codes[dtype]
+
+
+def _matrix(t, what: str):
+    """A CUDA matrix whose rows are contiguous (rows themselves may lie apart): the row stride in elements."""
+    _need(t.is_cuda and t.dim() == 2, f"{what} must be a CUDA matrix")
+    _need(t.shape[1] <= 1 or t.stride(1) == 1, f"{what} must be contiguous along its columns")
+    return max(t.stride(0), t.shape[1]) if t.shape[0] <= 1 else t.stride(0)
+
+
+class _on_device:
+    """Makes the tensors' device current (they must share one) and hands out the stream to use there."""
+
+    def __init__(self, stream, first, *others):
+        import torch
+        for t in others:
+            _need(t is None or t.device == first.device, "tensors lie on different devices")
+        self.guard, self.torch, self.stream, self.device = torch.cuda.device(first.device), torch, stream, first.device
+
+    def __enter__(self):
+        self.guard.__enter__()
+        s = self.torch.cuda.current_stream(self.device) if self.stream is None else self.stream
+        _need(s.device == self.device, "the stream belongs to another device than the tensors")
+        return C.c_void_p(s.cuda_stream)
+
+    def __exit__(self, *exc):
+        return self.guard.__exit__(*exc)
+
+
+def _ops_check(st: int):
+    if st != DIT_OK:
+        raise DitError(st, load_library().dit_status_string(st).decode())
+
+
+def _data(t):
+    return None if t is None else t.data_ptr()
+
+
+def _codes_for(rows: int, cols: int, device):
+    """Uninitialised e4m3 codes [rows, cols] whose rows start on 16-byte boundaries."""
+    import torch
+    return torch.empty((rows, (cols + 15) // 16 * 16), dtype=torch.float8_e4m3fn, device=device)[:, :cols]
+
+
+def dit_quantize_block128(x, codes=None, scales=None, stream=None):
+    """x [rows, cols] fp16 / bf16 / fp32 -> (codes [rows, cols] float8_e4m3fn, scales [ceil(cols / 128), rows] fp32)."""
+    import torch
+    lib, ld = load_library(), _matrix(x, "x")
+    rows, cols = x.shape
+    groups = (cols + BLOCK - 1) // BLOCK
+    if codes is None:
+        codes = _codes_for(rows, cols, x.device)
+    if scales is None:
+        scales = torch.empty((groups, rows), dtype=torch.float32, device=x.device)
+    _need(codes.dtype == torch.float8_e4m3fn and codes.shape == x.shape, "codes must be float8_e4m3fn, shaped like x")
+    _need(scales.dtype == torch.float32 and scales.shape == (groups, rows), "scales must be fp32 [ceil(cols / 128), rows]")
+    ld_codes, ld_scales = _matrix(codes, "codes"), _matrix(scales, "scales")
+    if rows <= 1:
+        ld_codes = (ld_codes + 15) // 16 * 16
+    with _on_device(stream, x, codes, scales) as s:
+        _ops_check(lib.dit_quantize_block128(_data(x), _type_code(x.dtype), ld, rows, cols, _data(codes), ld_codes, _data(scales), ld_scales, s))
+    return codes, scales
+
+
+def dit_quantize_weight_block128(w, codes=None, scales=None, stream=None):
+    """w [in, out] -> (codes [out, in] float8_e4m3fn, scales [ceil(out / 128), ceil(in / 128)] fp32)."""
+    import torch
+    lib, ld = load_library(), _matrix(w, "w")
+    n_in, n_out = w.shape
+    shape = ((n_out + BLOCK - 1) // BLOCK, (n_in + BLOCK - 1) // BLOCK)
+    if codes is None:
+        codes = _codes_for(n_out, n_in, w.device)
+    if scales is None:
+        scales = torch.empty(shape, dtype=torch.float32, device=w.device)
+    _need(codes.dtype == torch.float8_e4m3fn and codes.shape == (n_out, n_in), "codes must be float8_e4m3fn [out, in]")
+    _need(scales.dtype == torch.float32 and scales.shape == shape and scales.is_contiguous(),
+          "scales must be contiguous fp32 [ceil(out / 128), ceil(in / 128)]")
+    ld_codes = _matrix(codes, "codes")
+    if n_out <= 1:
+        ld_codes = (ld_codes + 15) // 16 * 16
+    with _on_device(stream, w, codes, scales) as s:
+        _ops_check(lib.dit_quantize_weight_block128(_data(w), _type_code(w.dtype), ld, n_in, n_out, _data(codes), ld_codes, _data(scales), s))
+    return codes, scales
+
+
+def dit_gemm_block128(a, a_scales, b, b_scales, bias=None, out=None, out_dtype=None, stream=None):
+    """a [m, k], b [n, k] float8_e4m3fn codes with their scales -> a b^T [m, n] (+ bias) in out_dtype (default fp16)."""
+    import torch
+    lib = load_library()
+    lda, ldb, ld_sa = _matrix(a, "a"), _matrix(b, "b"), _matrix(a_scales, "a_scales")
+    m, k = a.shape
+    n = b.shape[0]
+    groups = (k + BLOCK - 1) // BLOCK
+    _need(a.dtype == torch.float8_e4m3fn and b.dtype == torch.float8_e4m3fn, "a and b must be float8_e4m3fn codes")
+    _need(b.shape[1] == k, "a and b differ in k")
+    _need(a_scales.dtype == torch.float32 and a_scales.shape == (groups, m), "a_scales must be fp32 [ceil(k / 128), m]")
+    _need(b_scales.dtype == torch.float32 and b_scales.is_contiguous() and b_scales.shape == ((n + BLOCK - 1) // BLOCK, groups),
+          "b_scales must be contiguous fp32 [ceil(n / 128), ceil(k / 128)]")
+    _need(bias is None or (bias.is_cuda and bias.dtype == torch.float32 and bias.is_contiguous() and bias.shape == (n,)), "bias must be contiguous fp32 [n]")
+    if out is None:
+        out = torch.empty((m, n), dtype=out_dtype or torch.float16, device=a.device)
+    _need(out.shape == (m, n) and (out_dtype is None or out.dtype == out_dtype), "out must be [m, n] of out_dtype")
+    if m <= 1:
+        lda = (lda + 15) // 16 * 16
+    if n <= 1:
+        ldb = (ldb + 15) // 16 * 16
+    args = DitGemmBlock128Args(_data(a), _data(a_scales), _data(b), _data(b_scales), _data(bias), _data(out), lda, ld_sa, ldb,
+                               _matrix(out, "out"), m, n, k, _type_code(out.dtype))
+    with _on_device(stream, a, a_scales, b, b_scales, bias, out) as s:
+        _ops_check(lib.dit_gemm_block128(C.byref(args), s))
+    return out
+
+
+def dit_ops_poll_status():
+    """Raises DIT_ERR_TIMEOUT when a wait of one of these operators has run out on the current device since the last call."""
+    _ops_check(load_library().dit_ops_poll_status())
 
 
 def context_for(dims, max_blocks: int, max_total_tokens: int, max_requests: int = 8, flags: int = 0) -> DitContext:

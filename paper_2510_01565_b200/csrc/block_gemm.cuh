@@ -1,0 +1,467 @@
+// Product of two e4m3 operands with block scales for sm_100a:
+//   C[m, n] = sum_g sa[g, m] * sb[n / 128, g] * (sum over the 128 k of group g of A[m, k] B[n, k])   (+ fused epilogue)
+// Both operands are K-major.  The scales are general fp32 numbers, so the tensor cores cannot apply them:
+// every group's partial tile is taken out of tensor memory and added to accumulators in registers with
+// one packed multiply-add per pair.  That costs the epilogue warps 128 x 256 values per 128 k of a
+// CTA's half of a 256 x 256 tile, 512 cycles of the tensor pipe, against about 256 cycles of
+// tensor-memory reads and 256 of multiply-adds that run beside each other: tensor memory holds two
+// partial tiles, so the next group's MMAs run while the last one's sums are added.
+//
+// Two kernels.  gemm_block128_pair_kernel: persistent, one 256 x 256 tile per CTA pair, for shapes with
+// enough tiles.  gemm_block128_split_kernel: 128 output columns x up to 128 rows per CTA, k split over a
+// cluster and joined through distributed shared memory in rank order, for few rows, where reading B once is
+// the bound.
+#pragma once
+#include "common.cuh"
+#include "gemm.cuh"
+#include "ptx.cuh"
+
+namespace dit {
+
+// kBlkF16 / kBlkBF16 / kBlkF32: out = acc + bias in that type.
+// kBlkGeluF16: out = gelu_tanh(acc + bias) as fp16.  kBlkGateResidF32: out = resid + gate[request(row)] * (acc + bias).
+enum BlockGemmEpilogue : int { kBlkF16 = 0, kBlkBF16 = 1, kBlkF32 = 2, kBlkGeluF16 = 3, kBlkGateResidF32 = 4 };
+
+struct BlockGemmParams {
+  int M, N, K;
+  int band;                  // tile order, see tile_coords
+  const float* sa;           // [groups, ld_sa]
+  const float* sb;           // [ceil(N / 128), groups]
+  const float* bias;         // [N] or NULL
+  void* out;                 // row stride ld_out elements
+  long long ld_sa, ld_out;
+  int vec_out;               // rows of out start on 16-byte boundaries
+  int* status;
+  // kBlkGateResidF32 only (row strides of resid and out are ld_out)
+  const float* resid;
+  const float* gate;         // gate vector of request 0; request r at gate + r * gate_stride
+  long long gate_stride;
+};
+
+namespace bgemm {
+constexpr int BM = 128, BN = 256, STAGES = 6;
+constexpr int A_BYTES = BM * 128, B_BYTES = (BN / 2) * 128;
+constexpr int STAGE_BYTES = A_BYTES + B_BYTES;
+constexpr int EPI_WARPS = 8;
+constexpr int THREADS = 128 + 32 * EPI_WARPS;
+constexpr int REGS_ISSUE = 56, REGS_EPILOGUE = 224;   // (56 + 2 * 224) * 32 <= 16384 per scheduler
+constexpr int STAGE_OUT_BYTES = 2560;                 // per epilogue warp: 32 rows x 80 bytes, or 16 rows x 144 bytes
+constexpr int SMEM_BYTES = STAGES * STAGE_BYTES + 1024 + 256 + EPI_WARPS * STAGE_OUT_BYTES;
+}  // namespace bgemm
+
+// Writes 32 columns x 32 rows of a warp (this lane's row in v) through `stage`, so that a store instruction covers
+// whole sectors of a few rows.  `rows_ok`: bit r set when row r of the warp's 32 exists.  16-bit outputs: rows
+// padded to 80 bytes; fp32: two halves of 16 rows padded to 144 bytes.
+template <int EPI>
+__device__ __forceinline__ void block_store_chunk(const BlockGemmParams& p, const SeqInfo& seq, uint8_t* stage, float (&v)[32],
+                                                  int lane, long long row0, int col0, unsigned rows_ok) {
+  const bool whole = p.vec_out && col0 + 32 <= p.N;                   // warp-uniform
+  if constexpr (EPI == kBlkF32 || EPI == kBlkGateResidF32) {
+    float* st = reinterpret_cast<float*>(stage);
+    float* out = static_cast<float*>(p.out);
+#pragma unroll
+    for (int hf = 0; hf < 2; ++hf) {
+      if ((lane >> 4) == hf) {
+#pragma unroll
+        for (int i = 0; i < 32; i += 4) *reinterpret_cast<float4*>(st + (lane & 15) * 36 + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+      }
+      __syncwarp();
+      if (whole) {
+        const int cg = (lane & 7) * 4;
+#pragma unroll
+        for (int it = 0; it < 4; ++it) {
+          const int rr = hf * 16 + it * 4 + (lane >> 3);
+          if ((rows_ok >> rr) & 1u) {
+            float4 a = *reinterpret_cast<const float4*>(st + (rr & 15) * 36 + cg);
+            const long long at = (row0 + rr) * p.ld_out + col0 + cg;
+            if (EPI == kBlkGateResidF32) {
+              const int req = find_request(seq, static_cast<int>(row0) + rr);
+              const float4 g = __ldg(reinterpret_cast<const float4*>(p.gate + req * p.gate_stride + col0 + cg));
+              const float4 x = *reinterpret_cast<const float4*>(p.resid + at);
+              const float2 o0 = ffma2(make_float2(g.x, g.y), make_float2(a.x, a.y), make_float2(x.x, x.y));
+              const float2 o1 = ffma2(make_float2(g.z, g.w), make_float2(a.z, a.w), make_float2(x.z, x.w));
+              a = make_float4(o0.x, o0.y, o1.x, o1.y);
+            }
+            *reinterpret_cast<float4*>(out + at) = a;
+          }
+        }
+      } else if (col0 + lane < p.N) {
+        for (int r = 0; r < 16; ++r) {
+          const int rr = hf * 16 + r;
+          if ((rows_ok >> rr) & 1u) out[(row0 + rr) * p.ld_out + col0 + lane] = st[r * 36 + lane];
+        }
+      }
+      __syncwarp();
+    }
+  } else {
+    constexpr bool kBf = EPI == kBlkBF16;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      uint32_t w[4];
+#pragma unroll
+      for (int h = 0; h < 4; ++h) {
+        float2 ab = make_float2(v[8 * q + 2 * h], v[8 * q + 2 * h + 1]);
+        if (EPI == kBlkGeluF16) ab = gelu_tanh_f32x2(ab);
+        w[h] = pack16x2<kBf>(ab.x, ab.y);
+      }
+      *reinterpret_cast<uint4*>(stage + lane * 80 + q * 16) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    __syncwarp();
+    uint16_t* out = static_cast<uint16_t*>(p.out);
+    if (whole) {
+#pragma unroll
+      for (int it = 0; it < 4; ++it) {
+        const int rr = it * 8 + (lane >> 2), part = lane & 3;
+        if ((rows_ok >> rr) & 1u)
+          *reinterpret_cast<uint4*>(out + (row0 + rr) * p.ld_out + col0 + part * 8) = *reinterpret_cast<const uint4*>(stage + rr * 80 + part * 16);
+      }
+    } else if (col0 + lane < p.N) {
+      for (int rr = 0; rr < 32; ++rr)
+        if ((rows_ok >> rr) & 1u) out[(row0 + rr) * p.ld_out + col0 + lane] = *reinterpret_cast<const uint16_t*>(stage + rr * 80 + lane * 2);
+    }
+    __syncwarp();
+  }
+}
+
+// Roles as in gemm_tcgen05_kernel: warp 0 TMA producer, warp 1 MMA issuer (leader CTA) and owner of tensor memory, warps 4..11
+// accumulate and write: two per quarter of the tile's rows, one for each 128 columns (so a warp's columns share one
+// scale of B per group, and a lane's row one scale of A).
+template <int EPI>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(bgemm::THREADS, 1)
+gemm_block128_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const BlockGemmParams p,
+                          const __grid_constant__ SeqInfo seq) {
+  using namespace bgemm;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t raw = smem_u32(smem_raw);
+  const uint32_t base = (raw + 1023u) & ~1023u;
+  uint8_t* aligned = smem_raw + (base - raw);
+  const uint32_t bar0 = base + STAGES * STAGE_BYTES;
+  auto full_bar = [&](int s) { return bar0 + 8u * s; };
+  auto empty_bar = [&](int s) { return bar0 + 8u * (STAGES + s); };
+  auto tfull_bar = [&](int a) { return bar0 + 8u * (2 * STAGES + a); };
+  auto tempty_bar = [&](int a) { return bar0 + 8u * (2 * STAGES + 2 + a); };
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(aligned + STAGES * STAGE_BYTES + 8 * (2 * STAGES + 4));
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  uint8_t* out_stage = aligned + STAGES * STAGE_BYTES + 256;
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = cluster_ctarank();
+  const int pair = blockIdx.x >> 1, num_pairs = gridDim.x >> 1;
+  const int num_m = (p.M + 2 * BM - 1) / (2 * BM), num_n = (p.N + BN - 1) / BN;
+  const int num_tiles = num_m * num_n;
+  const int groups = (p.K + 127) / 128;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < STAGES; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
+    for (int a = 0; a < 2; ++a) { mbar_init(tfull_bar(a), 1); mbar_init(tempty_bar(a), 2 * EPI_WARPS); }
+    *abort_flag = 0;
+    fence_mbar_init();
+  }
+  if (warp == 0 && lane == 0) { prefetch_tmap(&tmA); prefetch_tmap(&tmB); }
+  if (warp == 1) { tmem_alloc_pair(smem_u32(tmem_slot), 512); tmem_relinquish_pair(); }
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync_all();
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+
+  if (warp < 4) {
+    DIT_SETMAXNREG_DEC(REGS_ISSUE);
+    if (warp == 0) {
+      if (lane == 0) {
+        int stage = 0; uint32_t phase = 0;
+        for (int t = pair; t < num_tiles; t += num_pairs) {
+          int mb, nb;
+          tile_coords(t, num_m, num_n, p.band, mb, nb);
+          const int m0 = mb * (2 * BM) + rank * BM, n0 = nb * BN + rank * (BN / 2);
+          for (int g = 0; g < groups; ++g) {
+            if (!mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag)) goto done;
+            const uint32_t full_leader = map_to_cta(full_bar(stage), 0);
+            if (rank == 0) mbar_arrive_expect_tx(full_bar(stage), 2 * STAGE_BYTES);
+            const uint32_t sa = base + stage * STAGE_BYTES;
+            tma_load_2d_pair(sa, &tmA, g * 128, m0, full_leader);
+            tma_load_2d_pair(sa + A_BYTES, &tmB, g * 128, n0, full_leader);
+            if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+          }
+        }
+      }
+    } else if (warp == 1) {
+      if (lane == 0 && rank == 0) {
+        constexpr uint32_t idesc = idesc_e4m3(2 * BM, BN);
+        int stage = 0; uint32_t phase = 0; int use = 0;                // use: partial tiles issued so far
+        for (int t = pair; t < num_tiles; t += num_pairs) {
+          for (int g = 0; g < groups; ++g, ++use) {
+            const int buf = use & 1;
+            if (!mbar_wait(tempty_bar(buf), ((use >> 1) & 1u) ^ 1u, abort_flag)) goto done;
+            if (!mbar_wait(full_bar(stage), phase, abort_flag)) goto done;
+            tc_fence_after();
+            const uint32_t sa = base + stage * STAGE_BYTES;
+            const uint64_t adesc = smem_desc_sw128(sa, 16, 1024), bdesc = smem_desc_sw128(sa + A_BYTES, 16, 1024);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) umma_f8_pair(tmem_base + buf * BN, adesc + 2 * k, bdesc + 2 * k, idesc, k != 0);
+            umma_commit_pair(empty_bar(stage), 3);
+            umma_commit_pair(tfull_bar(buf), 3);
+            if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+          }
+        }
+      }
+    }
+  } else {
+    DIT_SETMAXNREG_INC(REGS_EPILOGUE);
+    const int quarter = warp & 3, chalf = (warp - 4) >> 2;
+    const uint32_t t_row = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) + chalf * 128;
+    const uint32_t tempty_leader[2] = {map_to_cta(tempty_bar(0), 0), map_to_cta(tempty_bar(1), 0)};
+    uint8_t* stage = out_stage + (warp - 4) * STAGE_OUT_BYTES;
+    int use = 0;
+    for (int t = pair; t < num_tiles; t += num_pairs) {
+      int mb, nb;
+      tile_coords(t, num_m, num_n, p.band, mb, nb);
+      const int row0 = mb * (2 * BM) + rank * BM + quarter * 32, n0 = nb * BN + chalf * 128;
+      const bool row_in = row0 + lane < p.M, cols_in = n0 < p.N;       // columns past N: nothing to add or write
+      const float* sa = p.sa + (row_in ? row0 + lane : 0);
+      const float* sb = p.sb + static_cast<long long>(cols_in ? n0 >> 7 : 0) * groups;
+      float2 acc[64];
+#pragma unroll
+      for (int i = 0; i < 64; ++i) acc[i] = make_float2(0.f, 0.f);
+      if (p.bias && cols_in) {
+#pragma unroll
+        for (int i = 0; i < 64; ++i) {
+          if (n0 + 2 * i < p.N) acc[i].x = __ldg(p.bias + n0 + 2 * i);
+          if (n0 + 2 * i + 1 < p.N) acc[i].y = __ldg(p.bias + n0 + 2 * i + 1);
+        }
+      }
+      float f_next = __ldg(sa) * __ldg(sb);
+      for (int g = 0; g < groups; ++g, ++use) {
+        const int buf = use & 1;
+        const float2 f = make_float2(f_next, f_next);
+        if (g + 1 < groups) f_next = __ldg(sa + (g + 1) * p.ld_sa) * __ldg(sb + g + 1);
+        if (!__all_sync(0xffffffffu, mbar_wait(tfull_bar(buf), (use >> 1) & 1u, abort_flag))) goto done;
+        tc_fence_after();
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          uint32_t r[64];
+          __syncwarp();
+          tmem_ld32p(t_row + buf * BN + h * 64, r);
+          tmem_ld32p(t_row + buf * BN + h * 64 + 32, r + 32);
+          tmem_ld_wait();
+          if (h == 1) {                                                // everything is in registers: hand the buffer back
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_cluster_light(tempty_leader[buf]);
+          }
+#pragma unroll
+          for (int i = 0; i < 32; ++i)
+            acc[h * 32 + i] = ffma2(make_float2(__uint_as_float(r[2 * i]), __uint_as_float(r[2 * i + 1])), f, acc[h * 32 + i]);
+        }
+      }
+      if (!cols_in) continue;
+      const unsigned rows_ok = __ballot_sync(0xffffffffu, row_in);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        if (n0 + c * 32 >= p.N) break;                                 // warp-uniform
+        float v[32];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) { v[2 * i] = acc[c * 16 + i].x; v[2 * i + 1] = acc[c * 16 + i].y; }
+        block_store_chunk<EPI>(p, seq, stage, v, lane, row0, n0 + c * 32, rows_ok);
+      }
+    }
+  }
+
+done:
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync_all();
+  if (warp == 1) { tc_fence_after(); tmem_dealloc_pair(tmem_base, 512); }
+  if (threadIdx.x == 0 && *abort_flag) atomicMax(p.status, kStatusGemmTimeout);
+}
+
+// ------------------------------------------------------------------------------------------------
+// Few rows.  The roles of the operands are swapped: 128 rows of B (output columns) are the MMA's M, up to BT rows of A its
+// N, so that a lane owns one output column and the MMA wastes nothing on absent rows beyond the rounding to 16.
+// Reading B once is the bound (1 byte per 2 M flops): the k groups are split over the CTAs of a cluster until the
+// launch fills the device, each CTA streams its part through a ring of TMA boxes, and the partial
+// accumulators meet in distributed shared memory, where rank r sums its share of the rows in rank order.
+// Two CTAs fit on an SM (shared memory and tensor memory alike), so one CTA's set-up and join run under the
+// other's stream.
+// ------------------------------------------------------------------------------------------------
+template <int BT>
+struct SplitCfg {
+  static constexpr int A_BYTES = 128 * 128, T_BYTES = BT * 128, STAGE_BYTES = A_BYTES + T_BYTES;
+  static constexpr int STAGES = BT <= 32 ? 5 : (BT == 64 ? 4 : 3);
+  static constexpr int BUFS = BT <= 64 ? 4 : 2;                        // partial tiles in tensor memory
+  static constexpr int COLS = BUFS * BT < 32 ? 32 : BUFS * BT;         // 64, 128, 256, 256
+  static constexpr int SCALE_GROUPS = 8;                               // groups of row scales staged at a time
+  static constexpr int OFF_SCALE = STAGES * STAGE_BYTES;
+  static constexpr int OFF_BAR = OFF_SCALE + 2 * SCALE_GROUPS * BT * 4;
+  static constexpr int SMEM_BYTES = OFF_BAR + 256 + 1024;
+  static constexpr int THREADS = 192;
+  static_assert(BT * 128 * 4 <= STAGES * STAGE_BYTES, "the partial accumulators reuse the ring");
+  static_assert(3 * SMEM_BYTES > 227 * 1024 || 3 * COLS <= 512, "CTAs that fit an SM's shared memory must fit its tensor memory");
+  static_assert(2 * COLS <= 512 && 4 * SMEM_BYTES > 227 * 1024, "at most three CTAs per SM");
+};
+
+template <int EPI>
+__device__ __forceinline__ void block_store_one(const BlockGemmParams& p, const SeqInfo& seq, int row, int col, float v) {
+  const long long at = row * p.ld_out + col;
+  if constexpr (EPI == kBlkF16) static_cast<uint16_t*>(p.out)[at] = pack16<false>(v);
+  else if constexpr (EPI == kBlkBF16) static_cast<uint16_t*>(p.out)[at] = pack16<true>(v);
+  else if constexpr (EPI == kBlkGeluF16) static_cast<uint16_t*>(p.out)[at] = pack16<false>(gelu_tanh_f32(v));
+  else if constexpr (EPI == kBlkF32) static_cast<float*>(p.out)[at] = v;
+  else static_cast<float*>(p.out)[at] = fmaf(p.gate[find_request(seq, row) * p.gate_stride + col], v, p.resid[at]);
+}
+
+template <int EPI, int BT>
+__global__ void __launch_bounds__(SplitCfg<BT>::THREADS)
+gemm_block128_split_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const BlockGemmParams p,
+                           const __grid_constant__ SeqInfo seq, const int splits) {
+  using C = SplitCfg<BT>;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t raw = smem_u32(smem_raw);
+  const uint32_t base = (raw + 1023u) & ~1023u;
+  uint8_t* aligned = smem_raw + (base - raw);
+  const uint32_t bar0 = base + C::OFF_BAR;
+  auto full_bar = [&](int s) { return bar0 + 8u * s; };
+  auto empty_bar = [&](int s) { return bar0 + 8u * (C::STAGES + s); };
+  auto tfull_bar = [&](int b) { return bar0 + 8u * (2 * C::STAGES + b); };
+  auto tempty_bar = [&](int b) { return bar0 + 8u * (2 * C::STAGES + C::BUFS + b); };
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(aligned + C::OFF_BAR + 8 * (2 * C::STAGES + 2 * C::BUFS));
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rank = splits > 1 ? static_cast<int>(cluster_ctarank()) : 0;
+  const int tile = blockIdx.x / splits;
+  const int num_n = (p.N + 127) >> 7;
+  const int n0 = (tile % num_n) * 128, m0 = (tile / num_n) * BT;
+  const int groups = (p.K + 127) / 128;
+  const int g0 = static_cast<int>(static_cast<long long>(groups) * rank / splits), g1 = static_cast<int>(static_cast<long long>(groups) * (rank + 1) / splits);
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < C::STAGES; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
+    for (int b = 0; b < C::BUFS; ++b) { mbar_init(tfull_bar(b), 1); mbar_init(tempty_bar(b), 4); }
+    *abort_flag = 0;
+    fence_mbar_init();
+  }
+  if (warp == 0 && lane == 0) { prefetch_tmap(&tmA); prefetch_tmap(&tmB); }
+  if (warp == 1) { tmem_alloc(smem_u32(tmem_slot), C::COLS); tmem_relinquish(); }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+  float acc[BT];
+  const int quarter = warp & 3;                                        // warps 2..5 -> quarters 2, 3, 0, 1
+  const int col = n0 + quarter * 32 + lane;                            // this lane's output column (warps 2..5)
+#pragma unroll
+  for (int i = 0; i < BT; ++i) acc[i] = 0.f;
+
+  if (warp == 0) {
+    if (lane == 0) {
+      int stage = 0; uint32_t phase = 0;
+      for (int g = g0; g < g1; ++g) {
+        if (!mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag)) break;
+        const uint32_t s = base + stage * C::STAGE_BYTES;
+        mbar_arrive_expect_tx(full_bar(stage), C::STAGE_BYTES);
+        tma_load_2d(s, &tmB, g * 128, n0, full_bar(stage));
+        tma_load_2d(s + C::A_BYTES, &tmA, g * 128, m0, full_bar(stage));
+        if (++stage == C::STAGES) { stage = 0; phase ^= 1u; }
+      }
+    }
+  } else if (warp == 1) {
+    if (lane == 0) {
+      constexpr uint32_t idesc = idesc_e4m3(128, BT);
+      int stage = 0; uint32_t phase = 0;
+      for (int g = g0; g < g1; ++g) {
+        const int use = g - g0, buf = use % C::BUFS;
+        if (!mbar_wait(tempty_bar(buf), ((use / C::BUFS) & 1u) ^ 1u, abort_flag)) break;
+        if (!mbar_wait(full_bar(stage), phase, abort_flag)) break;
+        tc_fence_after();
+        const uint32_t s = base + stage * C::STAGE_BYTES;
+        const uint64_t wdesc = smem_desc_sw128(s, 16, 1024), tdesc = smem_desc_sw128(s + C::A_BYTES, 16, 1024);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) umma_f8(tmem_base + buf * BT, wdesc + 2 * k, tdesc + 2 * k, idesc, k != 0);
+        umma_commit(empty_bar(stage));
+        umma_commit(tfull_bar(buf));
+        if (++stage == C::STAGES) { stage = 0; phase ^= 1u; }
+      }
+    }
+  } else {
+    const float* sb = p.sb + static_cast<long long>(n0 >> 7) * groups;
+    float* scales = reinterpret_cast<float*>(aligned + C::OFF_SCALE);  // [2][SCALE_GROUPS][BT]: sa * sb of the coming groups
+    const int et = threadIdx.x - 64;
+    auto stage_scales = [&](int first) {                               // groups first .. first + 7 into their half
+      float* dst = scales + (((first - g0) / C::SCALE_GROUPS) & 1) * C::SCALE_GROUPS * BT;
+      for (int i = et; i < C::SCALE_GROUPS * BT; i += 128) {
+        const int g = first + i / BT, m = m0 + i % BT;
+        dst[i] = (g < g1 && m < p.M) ? __ldg(p.sa + g * p.ld_sa + m) * __ldg(sb + g) : 0.f;
+      }
+    };
+    stage_scales(g0);
+    bool ok = true;
+    for (int g = g0; g < g1; ++g) {                                    // after a failed wait the warps still meet at their barrier
+      const int use = g - g0, buf = use % C::BUFS, in = use % C::SCALE_GROUPS;
+      if (in == 0) {
+        asm volatile("bar.sync 1, 128;" ::: "memory");                 // this half is written, the other one read
+        if (g + C::SCALE_GROUPS < g1) stage_scales(g + C::SCALE_GROUPS);
+      }
+      const float* sc = scales + ((use / C::SCALE_GROUPS) & 1) * C::SCALE_GROUPS * BT + in * BT;
+      ok = ok && __all_sync(0xffffffffu, mbar_wait(tfull_bar(buf), (use / C::BUFS) & 1u, abort_flag));
+      if (!ok) continue;
+      tc_fence_after();
+      const uint32_t t_row = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) + buf * BT;
+      constexpr int CH = BT < 32 ? BT : 32;
+#pragma unroll
+      for (int c = 0; c < BT / CH; ++c) {
+        uint32_t r[CH];
+        __syncwarp();
+        if constexpr (CH == 16) tmem_ld16p(t_row + c * CH, r); else tmem_ld32p(t_row + c * CH, r);
+        tmem_ld_wait();
+        if (c == BT / CH - 1) {
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(tempty_bar(buf));
+        }
+#pragma unroll
+        for (int i = 0; i < CH; i += 4) {
+          const float4 s = *reinterpret_cast<const float4*>(sc + c * CH + i);
+          acc[c * CH + i] = fmaf(__uint_as_float(r[i]), s.x, acc[c * CH + i]);
+          acc[c * CH + i + 1] = fmaf(__uint_as_float(r[i + 1]), s.y, acc[c * CH + i + 1]);
+          acc[c * CH + i + 2] = fmaf(__uint_as_float(r[i + 2]), s.z, acc[c * CH + i + 2]);
+          acc[c * CH + i + 3] = fmaf(__uint_as_float(r[i + 3]), s.w, acc[c * CH + i + 3]);
+        }
+      }
+    }
+    const float bias = (p.bias && col < p.N) ? __ldg(p.bias + col) : 0.f;
+    if (splits == 1) {
+      if (ok && col < p.N) {
+#pragma unroll
+        for (int i = 0; i < BT; ++i)
+          if (m0 + i < p.M) block_store_one<EPI>(p, seq, m0 + i, col, acc[i] + bias);
+      }
+    } else if (ok) {
+      // every MMA of this CTA has completed and with it every read of the ring: the partials may take its place
+      float* part = reinterpret_cast<float*>(aligned);
+#pragma unroll
+      for (int i = 0; i < BT; ++i) part[i * 128 + quarter * 32 + lane] = acc[i];
+    }
+  }
+  if (splits > 1) {
+    __syncwarp();
+    cluster_sync_all();
+    if (warp >= 2 && col < p.N) {
+      const float bias = p.bias ? __ldg(p.bias + col) : 0.f;
+      const int rows = min(BT, p.M - m0);
+      for (int i = rank; i < rows; i += splits) {
+        float v = bias;
+        for (int r = 0; r < splits; ++r) v += ld_cluster_f32(map_to_cta(base + (i * 128 + quarter * 32 + lane) * 4, r));
+        block_store_one<EPI>(p, seq, m0 + i, col, v);
+      }
+    }
+    __syncwarp();
+    cluster_sync_all();                                                // peers may still read this CTA's partials until here
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) { tc_fence_after(); tmem_dealloc(tmem_base, C::COLS); }
+  if (threadIdx.x == 0 && *abort_flag) atomicMax(p.status, kStatusGemmTimeout);
+}
+
+}  // namespace dit

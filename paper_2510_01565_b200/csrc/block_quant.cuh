@@ -1,0 +1,218 @@
+// Quantisation to e4m3 codes with one fp32 scale per 128 columns of a row (activations) or per
+// 128 x 128 block (weights, transposed on the way):
+//   top = max(max|x|, 2^-100),  scale = top / 448,  code = e4m3(x * (448 / top))
+// Both divisions and the product are single IEEE fp32 operations, so the codes are a function of the
+// inputs alone that any fp32 implementation reproduces bit for bit.  The floor keeps 448 / top finite
+// for groups of zeros and of tiny numbers.  The maximum is taken on the absolute values' bit patterns,
+// whose integer order is the numbers' order with infinity above every number and NaN above infinity.
+#pragma once
+#include "common.cuh"
+#include "ptx.cuh"
+
+namespace dit {
+
+constexpr uint32_t kQuantFloorBits = 0x0D800000u;   // 2^-100
+
+__device__ __forceinline__ void quant_factors(uint32_t top_bits, float& inv, float& scale) {
+  const float top = __uint_as_float(max(top_bits, kQuantFloorBits));
+  inv = __fdiv_rn(448.0f, top);
+  scale = __fdiv_rn(top, 448.0f);
+}
+
+// Two values -> two e4m3 codes (low byte first), nearest even, clamped to +-448.
+__device__ __forceinline__ uint32_t e4m3x2(float lo, float hi) {
+  return __nv_cvt_float2_to_fp8x2(make_float2(lo, hi), __NV_SATFINITE, __NV_E4M3);
+}
+
+// kType: 0 = fp16, 1 = bf16, 2 = fp32.  Elements per 16-byte load and the widening of one load.
+template <int kType>
+struct QuantIn {
+  static constexpr int EPL = kType == 2 ? 4 : 8;
+  using Elem = typename std::conditional<kType == 2, float, uint16_t>::type;
+  static __device__ __forceinline__ float widen(Elem e) {
+    if constexpr (kType == 2) return e;
+    else if constexpr (kType == 1) return __uint_as_float(static_cast<uint32_t>(e) << 16);
+    else return __half2float(__ushort_as_half(e));
+  }
+  static __device__ __forceinline__ void widen16(const uint4& r, float (&v)[EPL]) {
+    const uint32_t u[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (kType == 2) v[i] = __uint_as_float(u[i]);
+      else if constexpr (kType == 1) { v[2 * i] = __uint_as_float(u[i] << 16); v[2 * i + 1] = __uint_as_float(u[i] & 0xFFFF0000u); }
+      else { const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&u[i])); v[2 * i] = f.x; v[2 * i + 1] = f.y; }
+    }
+  }
+};
+
+struct QuantParams {
+  const void* x;
+  uint8_t* codes;
+  float* scales;
+  long long ld, ld_codes, ld_scales;
+  int rows, cols, groups;      // groups of 128 columns
+  int rows_per_task;           // 8 or 32
+};
+
+// One warp per (group of 128 columns, run of rows): a 16-byte load per lane covers the group in two rows
+// (16-bit inputs) or one (fp32), the maximum is a shuffle reduction over the lanes of a row, and the
+// run's scales leave as one coalesced store (they lie group-major).  Neighbouring warps take
+// neighbouring groups, so a CTA reads runs of 2 KB.  Bound by HBM: 3 bytes per 16-bit element; four loads
+// per lane are requested ahead of use.
+// kVec: rows start on 16-byte boundaries; otherwise elements are loaded one by one.
+constexpr int kQuantBlockWarps = 8;
+
+template <int kType, bool kVec>
+__global__ void __launch_bounds__(kQuantBlockWarps * 32)
+quantize_block128_kernel(const QuantParams p) {
+  using In = QuantIn<kType>;
+  constexpr int EPL = In::EPL, LPR = 128 / EPL, RPI = 32 / LPR;   // lanes per row, rows per iteration
+  constexpr int BATCH = 4;
+  const int lane = threadIdx.x & 31;
+  const long long task = static_cast<long long>(blockIdx.x) * kQuantBlockWarps + (threadIdx.x >> 5);
+  const int group = static_cast<int>(task % p.groups);
+  const long long row0 = task / p.groups * p.rows_per_task;
+  if (row0 >= p.rows) return;
+  const int n_rows = static_cast<int>(min(static_cast<long long>(p.rows_per_task), p.rows - row0));
+  const int sub = lane / LPR, c0 = group * 128 + (lane % LPR) * EPL;
+  const int n_in = min(EPL, p.cols - c0);                         // this lane's columns inside the matrix (may be <= 0)
+  const typename In::Elem* src = static_cast<const typename In::Elem*>(p.x) + row0 * p.ld + c0;
+  uint8_t* dst = p.codes + row0 * p.ld_codes + c0;
+  float my_scale = 0.f;
+  for (int b = 0; b < n_rows; b += BATCH * RPI) {
+    float v[BATCH][EPL];
+    if (kVec && n_in == EPL) {
+      uint4 raw[BATCH];
+#pragma unroll
+      for (int i = 0; i < BATCH; ++i) {
+        const int r = b + i * RPI + sub;
+        raw[i] = r < n_rows ? __ldg(reinterpret_cast<const uint4*>(src + r * p.ld)) : make_uint4(0, 0, 0, 0);
+      }
+#pragma unroll
+      for (int i = 0; i < BATCH; ++i) In::widen16(raw[i], v[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < BATCH; ++i) {
+        const int r = b + i * RPI + sub;
+#pragma unroll
+        for (int e = 0; e < EPL; ++e) v[i][e] = (r < n_rows && e < n_in) ? In::widen(src[r * p.ld + e]) : 0.f;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < BATCH; ++i) {
+      uint32_t top = 0;
+#pragma unroll
+      for (int e = 0; e < EPL; ++e) top = max(top, __float_as_uint(v[i][e]) & 0x7FFFFFFFu);
+#pragma unroll
+      for (int o = LPR / 2; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+      float inv, scale;
+      quant_factors(top, inv, scale);
+      const int r = b + i * RPI + sub;
+#pragma unroll
+      for (int s = 0; s < RPI; ++s) {                             // lane k of the warp keeps the scale of row k of the run
+        const float sc = __shfl_sync(0xffffffffu, scale, s * LPR);
+        if (lane == b + i * RPI + s) my_scale = sc;
+      }
+      if (r < n_rows && n_in > 0) {
+        uint8_t* d = dst + r * p.ld_codes;
+        uint32_t w[EPL / 4];
+#pragma unroll
+        for (int q = 0; q < EPL / 4; ++q)
+          w[q] = e4m3x2(v[i][4 * q] * inv, v[i][4 * q + 1] * inv) | (e4m3x2(v[i][4 * q + 2] * inv, v[i][4 * q + 3] * inv) << 16);
+        if (n_in == EPL) {                                        // rows of codes start on 16-byte boundaries
+          if constexpr (EPL == 8) *reinterpret_cast<uint2*>(d) = make_uint2(w[0], w[1]);
+          else *reinterpret_cast<uint32_t*>(d) = w[0];
+        } else {
+#pragma unroll
+          for (int e = 0; e < EPL; ++e)
+            if (e < n_in) d[e] = static_cast<uint8_t>(w[e / 4] >> (8 * (e % 4)));
+        }
+      }
+    }
+  }
+  if (lane < n_rows) p.scales[group * p.ld_scales + row0 + lane] = my_scale;
+}
+
+// Weights w [in, out] -> codes [out, in] with one scale per 128 x 128 block: a CTA holds its block in
+// registers (8 vectors of 16 bytes of 16-bit input per thread), reduces the maximum, and turns the block
+// through shared memory as packed quadruples of codes along `in`.  A thread's vectors are four
+// consecutive `in` rows at the same eight columns, so each of its 16 words holds four consecutive
+// codes of one output row; word kq of row n lies at kq ^ 2 (n / 8), which keeps both phases free of
+// bank conflicts.  Bound by HBM: 3 bytes per element.
+struct QuantWeightParams {
+  const void* w;
+  uint8_t* codes;
+  float* scales;
+  long long ld, ld_codes;
+  int in_dim, out_dim, in_groups;
+};
+
+template <int kType, bool kVec>
+__global__ void __launch_bounds__(256)
+quantize_weight_block128_kernel(const QuantWeightParams p) {
+  using In = QuantIn<kType>;
+  constexpr int COLS = 8, VECS = COLS / In::EPL;                  // 16-byte loads per eight columns: 1 (16-bit) or 2 (fp32)
+  __shared__ uint32_t turned[128 * 32];
+  __shared__ uint32_t warp_top[8];
+  const int gk = blockIdx.x % p.in_groups, gn = blockIdx.x / p.in_groups;
+  const int k0 = gk * 128, n0 = gn * 128;
+  const int c = threadIdx.x & 15, rq = threadIdx.x >> 4;          // columns n0 + 8c .., rows k0 + 4 rq + 64 i + j
+  const typename In::Elem* src = static_cast<const typename In::Elem*>(p.w);
+  float v[2][4][COLS];
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int k = k0 + 4 * rq + 64 * i + j, n = n0 + 8 * c;
+      const typename In::Elem* at = src + static_cast<long long>(k) * p.ld + n;
+      if (kVec && k < p.in_dim && n + COLS <= p.out_dim) {
+#pragma unroll
+        for (int q = 0; q < VECS; ++q) {
+          float t[In::EPL];
+          In::widen16(__ldg(reinterpret_cast<const uint4*>(at) + q), t);
+#pragma unroll
+          for (int e = 0; e < In::EPL; ++e) v[i][j][q * In::EPL + e] = t[e];
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < COLS; ++e) v[i][j][e] = (k < p.in_dim && n + e < p.out_dim) ? In::widen(at[e]) : 0.f;
+      }
+    }
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int e = 0; e < COLS; ++e) top = max(top, __float_as_uint(v[i][j][e]) & 0x7FFFFFFFu);
+  top = __reduce_max_sync(0xffffffffu, top);
+  if ((threadIdx.x & 31) == 0) warp_top[threadIdx.x >> 5] = top;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 8; ++i) top = max(top, warp_top[i]);
+  float inv, scale;
+  quant_factors(top, inv, scale);
+  if (threadIdx.x == 0) p.scales[static_cast<long long>(gn) * p.in_groups + gk] = scale;
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int e = 0; e < COLS; ++e) {
+      const int n = 8 * c + e, kq = rq + 16 * i;
+      turned[n * 32 + (kq ^ (2 * c))] = e4m3x2(v[i][0][e] * inv, v[i][1][e] * inv) | (e4m3x2(v[i][2][e] * inv, v[i][3][e] * inv) << 16);
+    }
+  __syncthreads();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int n_in = min(4, p.in_dim - (k0 + 4 * lane));
+#pragma unroll 4
+  for (int r = 0; r < 16; ++r) {
+    const int n = warp * 16 + r;
+    if (n0 + n >= p.out_dim || n_in <= 0) continue;
+    const uint32_t word = turned[n * 32 + (lane ^ (2 * (n >> 3)))];
+    uint8_t* d = p.codes + static_cast<long long>(n0 + n) * p.ld_codes + k0 + 4 * lane;
+    if (n_in == 4) *reinterpret_cast<uint32_t*>(d) = word;
+    else
+      for (int e = 0; e < n_in; ++e) d[e] = static_cast<uint8_t>(word >> (8 * e));
+  }
+}
+
+}  // namespace dit

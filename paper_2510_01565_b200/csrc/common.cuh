@@ -8,6 +8,7 @@
 #include <stdint.h>
 
 #include "../../include/dit.h"
+#include "../../include/dit_ops.h"
 
 namespace dit {
 

@@ -1,0 +1,308 @@
+// The context-free operators of include/dit_ops.h: argument checks, tensor maps, launch rules.
+#include <algorithm>
+#include <cstdint>
+#include <mutex>
+#include <type_traits>
+
+#include "block_gemm.cuh"
+#include "block_quant.cuh"
+#include "common.cuh"
+#include "ops_launch.h"
+
+using namespace dit;
+
+namespace {
+
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                  const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+constexpr int kMaxDevices = 64;
+constexpr int64_t kMaxSize = INT32_MAX - 1024;
+
+// One status word per device, for waits that ran out.  In host code its name is a handle; the device
+// address is looked up once per device, with that device current.
+static __device__ int g_ops_status;
+
+struct DeviceState {
+  bool ready;
+  int num_sms, pairs;                  // pairs: CTA pairs of the pair kernel that are resident at once
+  int* status;
+};
+std::mutex g_mutex;
+DeviceState g_device[kMaxDevices];
+EncodeTiledFn g_encode = nullptr;
+
+template <class Kernel>
+cudaError_t allow_smem(Kernel kernel, int bytes) {
+  return cudaFuncSetAttribute(reinterpret_cast<const void*>(kernel), cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+}
+template <int EPI>
+cudaError_t allow_gemm() {
+  cudaError_t e = allow_smem(&gemm_block128_pair_kernel<EPI>, bgemm::SMEM_BYTES);
+  if (e == cudaSuccess) e = allow_smem(&gemm_block128_split_kernel<EPI, 16>, SplitCfg<16>::SMEM_BYTES);
+  if (e == cudaSuccess) e = allow_smem(&gemm_block128_split_kernel<EPI, 32>, SplitCfg<32>::SMEM_BYTES);
+  if (e == cudaSuccess) e = allow_smem(&gemm_block128_split_kernel<EPI, 64>, SplitCfg<64>::SMEM_BYTES);
+  if (e == cudaSuccess) e = allow_smem(&gemm_block128_split_kernel<EPI, 128>, SplitCfg<128>::SMEM_BYTES);
+  return e;
+}
+
+// The current device's state, prepared on its first use.  *unsupported is set on anything but compute capability 10.x.
+cudaError_t device_state(const DeviceState** out, bool* unsupported) {
+  *unsupported = false;
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev < 0 || dev >= kMaxDevices) return cudaErrorInvalidDevice;
+  std::lock_guard<std::mutex> lock(g_mutex);
+  DeviceState& s = g_device[dev];
+  if (!s.ready) {
+    int major = 0;
+    if ((e = cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev)) != cudaSuccess) return e;
+    if (major != 10) { *unsupported = true; return cudaErrorNotSupported; }
+    if ((e = cudaDeviceGetAttribute(&s.num_sms, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess) return e;
+    if (!g_encode) {
+      void* fn = nullptr;
+      cudaDriverEntryPointQueryResult found;
+      if ((e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &found)) != cudaSuccess) return e;
+      if (!fn || found != cudaDriverEntryPointSuccess) return cudaErrorNotSupported;
+      g_encode = reinterpret_cast<EncodeTiledFn>(fn);
+    }
+    void* p = nullptr;
+    if ((e = cudaGetSymbolAddress(&p, g_ops_status)) != cudaSuccess) return e;
+    s.status = static_cast<int*>(p);
+    if ((e = allow_gemm<kBlkF16>()) != cudaSuccess || (e = allow_gemm<kBlkBF16>()) != cudaSuccess || (e = allow_gemm<kBlkF32>()) != cudaSuccess ||
+        (e = allow_gemm<kBlkGeluF16>()) != cudaSuccess || (e = allow_gemm<kBlkGateResidF32>()) != cudaSuccess)
+      return e;
+    cudaLaunchConfig_t lc = {};
+    lc.gridDim = dim3(s.num_sms & ~1); lc.blockDim = dim3(bgemm::THREADS); lc.dynamicSmemBytes = bgemm::SMEM_BYTES;
+    cudaLaunchAttribute at;
+    at.id = cudaLaunchAttributeClusterDimension;
+    at.val.clusterDim.x = 2; at.val.clusterDim.y = 1; at.val.clusterDim.z = 1;
+    lc.attrs = &at; lc.numAttrs = 1;
+    int clusters = 0;
+    if ((e = cudaOccupancyMaxActiveClusters(&clusters, reinterpret_cast<const void*>(&gemm_block128_pair_kernel<kBlkF16>), &lc)) != cudaSuccess) return e;
+    s.pairs = std::max(1, std::min(clusters, s.num_sms / 2));
+    s.ready = true;
+  }
+  *out = &s;
+  return cudaSuccess;
+}
+
+dit_status ready(const DeviceState** s) {
+  bool unsupported = false;
+  const cudaError_t e = device_state(s, &unsupported);
+  if (unsupported) return DIT_ERR_UNSUPPORTED_ARCH;
+  return e == cudaSuccess ? DIT_OK : DIT_ERR_CUDA;
+}
+
+// Byte matrix [rows, inner] with `pitch` bytes between rows: boxes of 128 bytes x box_rows, 128-byte swizzle, zeros outside.
+bool byte_map(CUtensorMap* m, const void* ptr, uint64_t inner, uint64_t rows, uint64_t pitch, uint32_t box_rows) {
+  const cuuint64_t dims[2] = {inner, rows};
+  const cuuint64_t strides[1] = {pitch};
+  const cuuint32_t box[2] = {128, box_rows};
+  const cuuint32_t estr[2] = {1, 1};
+  return g_encode(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+const SeqInfo kNoSeq{};
+
+template <int EPI, int BT>
+cudaError_t launch_split(const CUtensorMap& tmA, const CUtensorMap& tmB, const BlockGemmParams& p, const SeqInfo& seq, int splits, cudaStream_t st) {
+  const long long tiles = static_cast<long long>((p.N + 127) / 128) * ((p.M + BT - 1) / BT);
+  cudaLaunchConfig_t lc = {};
+  lc.gridDim = dim3(static_cast<unsigned>(tiles * splits)); lc.blockDim = dim3(SplitCfg<BT>::THREADS);
+  lc.dynamicSmemBytes = SplitCfg<BT>::SMEM_BYTES; lc.stream = st;
+  cudaLaunchAttribute at;
+  at.id = cudaLaunchAttributeClusterDimension;
+  at.val.clusterDim.x = splits; at.val.clusterDim.y = 1; at.val.clusterDim.z = 1;
+  lc.attrs = &at; lc.numAttrs = splits > 1 ? 1 : 0;
+  return cudaLaunchKernelEx(&lc, &gemm_block128_split_kernel<EPI, BT>, tmA, tmB, p, seq, splits);
+}
+
+template <int EPI>
+cudaError_t launch_product(const DeviceState& d, const BlockProduct& b, BlockGemmParams p, const SeqInfo& seq, cudaStream_t st) {
+  CUtensorMap tmA, tmB;
+  const long long tiles_n = (p.N + 127) / 128;
+  const int groups = (p.K + 127) / 128;
+  const long long pair_tiles = static_cast<long long>((p.M + 255) / 256) * ((p.N + 255) / 256);
+  // Few rows, or too few 256 x 256 tiles to fill the device: the split kernel.
+  if (p.M <= 128 || pair_tiles < d.pairs / 2) {
+    const int bt = p.M <= 16 ? 16 : (p.M <= 32 ? 32 : (p.M <= 64 ? 64 : 128));
+    const long long tiles = tiles_n * ((p.M + bt - 1) / bt);
+    int splits = 1;
+    while (splits < 8 && 2 * splits <= groups && tiles * splits < d.num_sms) splits *= 2;
+    if (!byte_map(&tmA, b.a, p.K, p.M, b.lda, bt) || !byte_map(&tmB, b.b, p.K, p.N, b.ldb, 128)) return cudaErrorInvalidValue;
+    if (bt == 16) return launch_split<EPI, 16>(tmA, tmB, p, seq, splits, st);
+    if (bt == 32) return launch_split<EPI, 32>(tmA, tmB, p, seq, splits, st);
+    if (bt == 64) return launch_split<EPI, 64>(tmA, tmB, p, seq, splits, st);
+    return launch_split<EPI, 128>(tmA, tmB, p, seq, splits, st);
+  }
+  if (!byte_map(&tmA, b.a, p.K, p.M, b.lda, 128) || !byte_map(&tmB, b.b, p.K, p.N, b.ldb, 128)) return cudaErrorInvalidValue;
+  {  // tile order: hold the panels of whichever operand costs fewer DRAM reads in L2 (as launch_gemm of the step does)
+    const long long panel = 256ll * p.K, num_m = (p.M + 255) / 256, num_n = (p.N + 255) / 256;
+    const long long fit = std::max(1ll, (38ll << 20) / panel);
+    const long long rb = std::min(fit, num_m), cb = std::min(fit, num_n);
+    const long long cost_rows = num_m * panel + num_n * panel * ((num_m + rb - 1) / rb);
+    const long long cost_cols = num_n * panel + num_m * panel * ((num_n + cb - 1) / cb);
+    p.band = cost_cols < cost_rows ? -static_cast<int>(cb) : static_cast<int>(rb);
+  }
+  const int grid = 2 * static_cast<int>(std::min<long long>(pair_tiles, d.pairs));
+  gemm_block128_pair_kernel<EPI><<<grid, bgemm::THREADS, bgemm::SMEM_BYTES, st>>>(tmA, tmB, p, seq);
+  return cudaGetLastError();
+}
+
+template <int kType>
+cudaError_t launch_quant(const QuantParams& p, long long tasks, bool vec, cudaStream_t st) {
+  const unsigned grid = static_cast<unsigned>((tasks + kQuantBlockWarps - 1) / kQuantBlockWarps);
+  if (vec) quantize_block128_kernel<kType, true><<<grid, kQuantBlockWarps * 32, 0, st>>>(p);
+  else quantize_block128_kernel<kType, false><<<grid, kQuantBlockWarps * 32, 0, st>>>(p);
+  return cudaGetLastError();
+}
+template <int kType>
+cudaError_t launch_quant_weight(const QuantWeightParams& p, bool vec, cudaStream_t st) {
+  const unsigned grid = static_cast<unsigned>(static_cast<long long>(p.in_groups) * ((p.out_dim + 127) / 128));
+  if (vec) quantize_weight_block128_kernel<kType, true><<<grid, 256, 0, st>>>(p);
+  else quantize_weight_block128_kernel<kType, false><<<grid, 256, 0, st>>>(p);
+  return cudaGetLastError();
+}
+
+int type_bytes(dit_type t) { return t == DIT_TYPE_F32 ? 4 : 2; }
+bool type_ok(dit_type t) { return t == DIT_TYPE_F16 || t == DIT_TYPE_BF16 || t == DIT_TYPE_F32; }
+bool aligned(const void* p, uintptr_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
+
+}  // namespace
+
+namespace dit {
+
+cudaError_t ops_prepare_device() {
+  const DeviceState* d;
+  bool unsupported;
+  return device_state(&d, &unsupported);
+}
+
+cudaError_t launch_block_product(const BlockProduct& b, const SeqInfo& seq, cudaStream_t st) {
+  const DeviceState* d;
+  bool unsupported;
+  const cudaError_t e = device_state(&d, &unsupported);
+  if (e != cudaSuccess) return e;
+  BlockGemmParams p{};
+  p.M = b.m; p.N = b.n; p.K = b.k;
+  p.sa = b.a_scales; p.sb = b.b_scales; p.bias = b.bias; p.out = b.out;
+  p.ld_sa = b.ld_a_scales; p.ld_out = b.ld_out;
+  const int elem = (b.epilogue == kBlkF32 || b.epilogue == kBlkGateResidF32) ? 4 : 2;
+  p.vec_out = aligned(b.out, 16) && b.ld_out * elem % 16 == 0;
+  p.status = d->status;
+  p.resid = b.resid; p.gate = b.gate; p.gate_stride = b.gate_stride;
+  switch (b.epilogue) {
+    case kBlkF16: return launch_product<kBlkF16>(*d, b, p, seq, st);
+    case kBlkBF16: return launch_product<kBlkBF16>(*d, b, p, seq, st);
+    case kBlkF32: return launch_product<kBlkF32>(*d, b, p, seq, st);
+    case kBlkGeluF16: return launch_product<kBlkGeluF16>(*d, b, p, seq, st);
+    case kBlkGateResidF32: return launch_product<kBlkGateResidF32>(*d, b, p, seq, st);
+  }
+  return cudaErrorInvalidValue;
+}
+
+cudaError_t launch_quantize_rows(const void* x, dit_type type, long long ld, long long rows, long long cols, void* codes,
+                                 long long ld_codes, float* scales, long long ld_scales, cudaStream_t st) {
+  const DeviceState* d;
+  bool unsupported;
+  const cudaError_t e = device_state(&d, &unsupported);
+  if (e != cudaSuccess) return e;
+  QuantParams p{};
+  p.x = x; p.codes = static_cast<uint8_t*>(codes); p.scales = scales;
+  p.ld = ld; p.ld_codes = ld_codes; p.ld_scales = ld_scales;
+  p.rows = static_cast<int>(rows); p.cols = static_cast<int>(cols); p.groups = static_cast<int>((cols + 127) / 128);
+  // runs of 32 rows per warp once that fills the device, of 8 below
+  p.rows_per_task = (rows + 31) / 32 * p.groups >= 16ll * d->num_sms ? 32 : 8;
+  const long long tasks = (rows + p.rows_per_task - 1) / p.rows_per_task * p.groups;
+  if (tasks > 8ll * INT32_MAX - 8) return cudaErrorInvalidValue;
+  const bool vec = aligned(x, 16) && ld * type_bytes(type) % 16 == 0;
+  if (type == DIT_TYPE_F16) return launch_quant<0>(p, tasks, vec, st);
+  if (type == DIT_TYPE_BF16) return launch_quant<1>(p, tasks, vec, st);
+  return launch_quant<2>(p, tasks, vec, st);
+}
+
+cudaError_t launch_quantize_weight(const void* w, dit_type type, long long ld, int in_dim, int out_dim, void* codes, long long ld_codes,
+                                   float* scales, cudaStream_t st) {
+  QuantWeightParams p{};
+  p.w = w; p.codes = static_cast<uint8_t*>(codes); p.scales = scales; p.ld = ld; p.ld_codes = ld_codes;
+  p.in_dim = in_dim; p.out_dim = out_dim; p.in_groups = (in_dim + 127) / 128;
+  const bool vec = aligned(w, 16) && ld * type_bytes(type) % 16 == 0;
+  if (type == DIT_TYPE_F16) return launch_quant_weight<0>(p, vec, st);
+  if (type == DIT_TYPE_BF16) return launch_quant_weight<1>(p, vec, st);
+  return launch_quant_weight<2>(p, vec, st);
+}
+
+}  // namespace dit
+
+// =============================================================================================== C ABI
+extern "C" {
+
+dit_status dit_quantize_block128(const void* x, dit_type type, int64_t ld, int64_t rows, int64_t cols, void* codes,
+                                 int64_t ld_codes, float* scales, int64_t ld_scales, void* stream) {
+  if (rows < 0 || !type_ok(type)) return DIT_ERR_INVALID_ARG;
+  if (cols < 1 || cols > kMaxSize || rows > kMaxSize) return DIT_ERR_SHAPE;
+  if (rows == 0) return DIT_OK;
+  if (!x || !codes || !scales) return DIT_ERR_INVALID_ARG;
+  if (ld < cols || ld_codes < cols || ld_codes % 16 || ld_scales < rows) return DIT_ERR_INVALID_ARG;
+  if (!aligned(x, type_bytes(type)) || !aligned(codes, 16) || !aligned(scales, 4)) return DIT_ERR_INVALID_ARG;
+  const DeviceState* d;
+  const dit_status s = ready(&d);
+  if (s != DIT_OK) return s;
+  return launch_quantize_rows(x, type, ld, rows, cols, codes, ld_codes, scales, ld_scales, static_cast<cudaStream_t>(stream)) == cudaSuccess
+             ? DIT_OK : DIT_ERR_CUDA;
+}
+
+dit_status dit_quantize_weight_block128(const void* w, dit_type type, int64_t ld, int64_t in_dim, int64_t out_dim, void* codes,
+                                        int64_t ld_codes, float* scales, void* stream) {
+  if (!type_ok(type)) return DIT_ERR_INVALID_ARG;
+  if (in_dim < 1 || out_dim < 1 || in_dim > kMaxSize || out_dim > kMaxSize) return DIT_ERR_SHAPE;
+  if (((in_dim + 127) / 128) * ((out_dim + 127) / 128) > INT32_MAX) return DIT_ERR_SHAPE;
+  if (!w || !codes || !scales) return DIT_ERR_INVALID_ARG;
+  if (ld < out_dim || ld_codes < in_dim || ld_codes % 16) return DIT_ERR_INVALID_ARG;
+  if (!aligned(w, type_bytes(type)) || !aligned(codes, 16) || !aligned(scales, 4)) return DIT_ERR_INVALID_ARG;
+  const DeviceState* d;
+  const dit_status s = ready(&d);
+  if (s != DIT_OK) return s;
+  return launch_quantize_weight(w, type, ld, static_cast<int>(in_dim), static_cast<int>(out_dim), codes, ld_codes, scales,
+                                static_cast<cudaStream_t>(stream)) == cudaSuccess ? DIT_OK : DIT_ERR_CUDA;
+}
+
+dit_status dit_gemm_block128(const dit_gemm_block128_args* a, void* stream) {
+  if (!a || a->m < 0 || !type_ok(a->out_type)) return DIT_ERR_INVALID_ARG;
+  if (a->n < 1 || a->k < 1 || a->m > kMaxSize || a->n > kMaxSize || a->k > kMaxSize) return DIT_ERR_SHAPE;
+  if (a->m == 0) return DIT_OK;
+  if (!a->a || !a->a_scales || !a->b || !a->b_scales || !a->out) return DIT_ERR_INVALID_ARG;
+  if (a->lda < a->k || a->ldb < a->k || a->lda % 16 || a->ldb % 16 || a->ld_a_scales < a->m || a->ld_out < a->n) return DIT_ERR_INVALID_ARG;
+  if (!aligned(a->a, 16) || !aligned(a->b, 16) || !aligned(a->a_scales, 4) || !aligned(a->b_scales, 4) || !aligned(a->bias, 4) ||
+      !aligned(a->out, type_bytes(a->out_type)))
+    return DIT_ERR_INVALID_ARG;
+  // tiles are counted in 32 bits: with the split kernel's smallest tile, 128 x 128
+  if (((a->m + 127) / 128) * ((a->n + 127) / 128) > INT32_MAX / 16) return DIT_ERR_SHAPE;
+  const DeviceState* d;
+  const dit_status s = ready(&d);
+  if (s != DIT_OK) return s;
+  BlockProduct b{};
+  b.a = a->a; b.a_scales = a->a_scales; b.b = a->b; b.b_scales = a->b_scales; b.bias = a->bias; b.out = a->out;
+  b.lda = a->lda; b.ld_a_scales = a->ld_a_scales; b.ldb = a->ldb; b.ld_out = a->ld_out;
+  b.m = static_cast<int>(a->m); b.n = static_cast<int>(a->n); b.k = static_cast<int>(a->k);
+  b.epilogue = a->out_type == DIT_TYPE_F16 ? kBlkF16 : (a->out_type == DIT_TYPE_BF16 ? kBlkBF16 : kBlkF32);
+  return launch_block_product(b, kNoSeq, static_cast<cudaStream_t>(stream)) == cudaSuccess ? DIT_OK : DIT_ERR_CUDA;
+}
+
+dit_status dit_ops_poll_status(void) {
+  const DeviceState* d;
+  const dit_status s = ready(&d);
+  if (s != DIT_OK) return s;
+  int value = 0;
+  if (cudaDeviceSynchronize() != cudaSuccess) return DIT_ERR_CUDA;
+  if (cudaMemcpy(&value, d->status, sizeof(value), cudaMemcpyDeviceToHost) != cudaSuccess) return DIT_ERR_CUDA;
+  if (value == kStatusOk) return DIT_OK;
+  if (cudaMemset(d->status, 0, sizeof(int)) != cudaSuccess) return DIT_ERR_CUDA;
+  return DIT_ERR_TIMEOUT;
+}
+
+}  // extern "C"

@@ -1,0 +1,34 @@
+// Launchers of the context-free operators for the step (dit_api.cu).  The kernels and their per-device
+// preparation live in ops_api.cu.
+#pragma once
+#include <cuda.h>
+#include <cuda_runtime.h>
+
+#include "common.cuh"
+
+namespace dit {
+
+// Epilogues of the block-scaled product that the step uses beside the plain ones.
+struct BlockProduct {
+  const void* a;             // e4m3 [m, lda]
+  const float* a_scales;     // [groups, ld_a_scales]
+  const void* b;             // e4m3 [n, ldb]
+  const float* b_scales;     // [ceil(n / 128), groups]
+  const float* bias;
+  void* out;
+  long long lda, ld_a_scales, ldb, ld_out;
+  int m, n, k;
+  int epilogue;              // BlockGemmEpilogue
+  const float* resid;        // gated residual only
+  const float* gate;
+  long long gate_stride;
+};
+
+cudaError_t ops_prepare_device();                      // sets kernel attributes once per device
+cudaError_t launch_block_product(const BlockProduct& b, const SeqInfo& seq, cudaStream_t st);
+cudaError_t launch_quantize_rows(const void* x, dit_type type, long long ld, long long rows, long long cols, void* codes,
+                                 long long ld_codes, float* scales, long long ld_scales, cudaStream_t st);
+cudaError_t launch_quantize_weight(const void* w, dit_type type, long long ld, int in_dim, int out_dim, void* codes, long long ld_codes,
+                                   float* scales, cudaStream_t st);
+
+}  // namespace dit
