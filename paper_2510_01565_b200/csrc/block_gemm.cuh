@@ -39,14 +39,16 @@ struct BlockGemmParams {
 };
 
 namespace bgemm {
-constexpr int BM = 128, BN = 256, STAGES = 6;
+constexpr int BM = 128, BN = 256, STAGES = 4;
 constexpr int A_BYTES = BM * 128, B_BYTES = (BN / 2) * 128;
 constexpr int STAGE_BYTES = A_BYTES + B_BYTES;
 constexpr int EPI_WARPS = 8;
 constexpr int THREADS = 128 + 32 * EPI_WARPS;
 constexpr int REGS_ISSUE = 56, REGS_EPILOGUE = 224;   // (56 + 2 * 224) * 32 <= 16384 per scheduler
-constexpr int STAGE_OUT_BYTES = 2560;                 // per epilogue warp: 32 rows x 80 bytes, or 16 rows x 144 bytes
-constexpr int SMEM_BYTES = STAGES * STAGE_BYTES + 1024 + 256 + EPI_WARPS * STAGE_OUT_BYTES;
+constexpr int STAGE_OUT_BYTES = 8192;                 // per epilogue warp: 32 rows x 256 bytes, as two swizzled boxes of 128 bytes x 32 rows
+constexpr int BIAS_BYTES = 512;                       // per epilogue warp: the bias of its 128 columns
+constexpr int OFF_OUT = STAGES * STAGE_BYTES, OFF_BAR = OFF_OUT + EPI_WARPS * (STAGE_OUT_BYTES + BIAS_BYTES);
+constexpr int SMEM_BYTES = OFF_BAR + 256 + 1024;
 }  // namespace bgemm
 
 // Writes 32 columns x 32 rows of a warp (this lane's row in v) through `stage`, so that a store instruction covers
@@ -123,26 +125,31 @@ __device__ __forceinline__ void block_store_chunk(const BlockGemmParams& p, cons
   }
 }
 
-// Roles as in gemm_tcgen05_kernel: warp 0 TMA producer, warp 1 MMA issuer (leader CTA) and owner of tensor memory, warps 4..11
-// accumulate and write: two per quarter of the tile's rows, one for each 128 columns (so a warp's columns share one
-// scale of B per group, and a lane's row one scale of A).
+// Roles: warp 0 TMA producer, warps 1 and 2 MMA issuers (leader CTA; warp 1 owns tensor memory), warps 4..11 accumulate and
+// write: two per quarter of the tile's rows, one for each 128 columns (so a warp's columns share one scale of B per
+// group, and a lane's row one scale of A).
+// A group's partial tile is made and taken out in two halves: half h multiplies rows 64 h .. 64 h + 63 of each CTA's
+// B box, i.e. columns 64 h.. of both scale blocks.  Tensor memory holds two groups x two halves: a half's round
+// trip (MMAs, commit, wake-up, read-out, arrival at the leader: about 1100 cycles, of which 256 are MMAs) then fits
+// under the other three, which it did not with two whole partial tiles (900 cycles per group measured).  Issuer h owns half h;
+// its commit reports both that its part of the stage has been read and that the half is complete: producer and
+// accumulating warps wait on the same barrier.
 template <int EPI>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(bgemm::THREADS, 1)
-gemm_block128_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const BlockGemmParams p,
+gemm_block128_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
+                          const __grid_constant__ CUtensorMap tmOut, const BlockGemmParams p,
                           const __grid_constant__ SeqInfo seq) {
   using namespace bgemm;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw);
   const uint32_t base = (raw + 1023u) & ~1023u;
   uint8_t* aligned = smem_raw + (base - raw);
-  const uint32_t bar0 = base + STAGES * STAGE_BYTES;
+  const uint32_t bar0 = base + OFF_BAR;
   auto full_bar = [&](int s) { return bar0 + 8u * s; };
-  auto empty_bar = [&](int s) { return bar0 + 8u * (STAGES + s); };
-  auto tfull_bar = [&](int a) { return bar0 + 8u * (2 * STAGES + a); };
-  auto tempty_bar = [&](int a) { return bar0 + 8u * (2 * STAGES + 2 + a); };
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(aligned + STAGES * STAGE_BYTES + 8 * (2 * STAGES + 4));
+  auto done_bar = [&](int s, int h) { return bar0 + 8u * (STAGES + 2 * s + h); };      // half h's MMAs of stage s have completed
+  auto tempty_bar = [&](int buf, int h) { return bar0 + 8u * (3 * STAGES + 2 * buf + h); };
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(aligned + OFF_BAR + 8 * (3 * STAGES + 4));
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-  uint8_t* out_stage = aligned + STAGES * STAGE_BYTES + 256;
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = cluster_ctarank();
@@ -152,8 +159,8 @@ gemm_block128_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_
   const int groups = (p.K + 127) / 128;
 
   if (threadIdx.x == 0) {
-    for (int s = 0; s < STAGES; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
-    for (int a = 0; a < 2; ++a) { mbar_init(tfull_bar(a), 1); mbar_init(tempty_bar(a), 2 * EPI_WARPS); }
+    for (int s = 0; s < STAGES; ++s) { mbar_init(full_bar(s), 1); mbar_init(done_bar(s, 0), 1); mbar_init(done_bar(s, 1), 1); }
+    for (int a = 0; a < 4; ++a) mbar_init(tempty_bar(a >> 1, a & 1), 2 * EPI_WARPS);
     *abort_flag = 0;
     fence_mbar_init();
   }
@@ -175,7 +182,7 @@ gemm_block128_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_
           tile_coords(t, num_m, num_n, p.band, mb, nb);
           const int m0 = mb * (2 * BM) + rank * BM, n0 = nb * BN + rank * (BN / 2);
           for (int g = 0; g < groups; ++g) {
-            if (!mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag)) goto done;
+            if (!mbar_wait(done_bar(stage, 0), phase ^ 1u, abort_flag) || !mbar_wait(done_bar(stage, 1), phase ^ 1u, abort_flag)) goto done;
             const uint32_t full_leader = map_to_cta(full_bar(stage), 0);
             if (rank == 0) mbar_arrive_expect_tx(full_bar(stage), 2 * STAGE_BYTES);
             const uint32_t sa = base + stage * STAGE_BYTES;
@@ -185,89 +192,157 @@ gemm_block128_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_
           }
         }
       }
-    } else if (warp == 1) {
-      if (lane == 0 && rank == 0) {
-        constexpr uint32_t idesc = idesc_e4m3(2 * BM, BN);
-        int stage = 0; uint32_t phase = 0; int use = 0;                // use: partial tiles issued so far
-        for (int t = pair; t < num_tiles; t += num_pairs) {
-          for (int g = 0; g < groups; ++g, ++use) {
-            const int buf = use & 1;
-            if (!mbar_wait(tempty_bar(buf), ((use >> 1) & 1u) ^ 1u, abort_flag)) goto done;
-            if (!mbar_wait(full_bar(stage), phase, abort_flag)) goto done;
-            tc_fence_after();
-            const uint32_t sa = base + stage * STAGE_BYTES;
-            const uint64_t adesc = smem_desc_sw128(sa, 16, 1024), bdesc = smem_desc_sw128(sa + A_BYTES, 16, 1024);
+    } else if (warp < 3 && rank == 0) {
+      // the whole warp runs the loop, so that descriptors and addresses live in uniform registers; one thread issues
+      constexpr uint32_t idesc = idesc_e4m3(2 * BM, BN / 2);
+      const int h = warp - 1;
+      const bool issuer = elect_one();
+      const int uses = groups * ((num_tiles - pair + num_pairs - 1) / num_pairs);
+      int stage = 0; uint32_t phase = 0;
+      for (int use = 0; use < uses; ++use) {                           // partial tiles of this pair, in order
+        const int buf = use & 1;
+        if (!__all_sync(0xffffffffu, mbar_wait(tempty_bar(buf, h), ((use >> 1) & 1u) ^ 1u, abort_flag) && mbar_wait(full_bar(stage), phase, abort_flag))) goto done;
+        tc_fence_after();
+        const uint32_t sa = base + stage * STAGE_BYTES;
+        const uint64_t adesc = smem_desc_sw128(sa, 16, 1024), bdesc = smem_desc_sw128(sa + A_BYTES + h * (B_BYTES / 2), 16, 1024);
+        if (issuer) {
 #pragma unroll
-            for (int k = 0; k < 4; ++k) umma_f8_pair(tmem_base + buf * BN, adesc + 2 * k, bdesc + 2 * k, idesc, k != 0);
-            umma_commit_pair(empty_bar(stage), 3);
-            umma_commit_pair(tfull_bar(buf), 3);
-            if (++stage == STAGES) { stage = 0; phase ^= 1u; }
-          }
+          for (int k = 0; k < 4; ++k) umma_f8_pair(tmem_base + buf * BN + h * (BN / 2), adesc + 2 * k, bdesc + 2 * k, idesc, k != 0);
+          umma_commit_pair(done_bar(stage, h), 3);                     // in both CTAs
         }
+        if (++stage == STAGES) { stage = 0; phase ^= 1u; }
       }
     }
   } else {
     DIT_SETMAXNREG_INC(REGS_EPILOGUE);
     const int quarter = warp & 3, chalf = (warp - 4) >> 2;
-    const uint32_t t_row = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) + chalf * 128;
-    const uint32_t tempty_leader[2] = {map_to_cta(tempty_bar(0), 0), map_to_cta(tempty_bar(1), 0)};
-    uint8_t* stage = out_stage + (warp - 4) * STAGE_OUT_BYTES;
-    int use = 0;
-    for (int t = pair; t < num_tiles; t += num_pairs) {
+    const uint32_t t_row = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) + chalf * 64;
+    const uint32_t tempty_leader = map_to_cta(tempty_bar(0, 0), 0);
+    uint8_t* stage = aligned + OFF_OUT + (warp - 4) * STAGE_OUT_BYTES;
+    float* bias_of = reinterpret_cast<float*>(aligned + OFF_OUT + EPI_WARPS * STAGE_OUT_BYTES + (warp - 4) * BIAS_BYTES);
+    // What a tile needs from memory before its first group: requested for the next tile before the current one is
+    // written.  Lane l holds the bias of columns l, 32 + l, 64 + l, 96 + l; scales run two groups ahead of their use.
+    struct Ahead { int row0, n0; const float *sa, *sb; float bias[4], sa_at[3], sb_at[3]; } next;
+    auto request = [&](int t) {
       int mb, nb;
       tile_coords(t, num_m, num_n, p.band, mb, nb);
-      const int row0 = mb * (2 * BM) + rank * BM + quarter * 32, n0 = nb * BN + chalf * 128;
-      const bool row_in = row0 + lane < p.M, cols_in = n0 < p.N;       // columns past N: nothing to add or write
-      const float* sa = p.sa + (row_in ? row0 + lane : 0);
-      const float* sb = p.sb + static_cast<long long>(cols_in ? n0 >> 7 : 0) * groups;
+      next.row0 = mb * (2 * BM) + rank * BM + quarter * 32; next.n0 = nb * BN + chalf * 128;
+      next.sa = p.sa + (next.row0 + lane < p.M ? next.row0 + lane : 0);
+      next.sb = p.sb + static_cast<long long>(next.n0 < p.N ? next.n0 >> 7 : 0) * groups;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) next.bias[c] = (p.bias && next.n0 + c * 32 + lane < p.N) ? __ldg(p.bias + next.n0 + c * 32 + lane) : 0.f;
+#pragma unroll
+      for (int d = 0; d < 2; ++d) {
+        const int at = min(d, groups - 1);
+        next.sa_at[d] = __ldg(next.sa + at * p.ld_sa); next.sb_at[d] = __ldg(next.sb + at);
+      }
+    };
+    int stage_of = 0; uint32_t phase = 0; int buf = 0;                 // of the next group
+    bool ready = false;                                                // its first half is known to be complete
+    if (pair < num_tiles) request(pair);
+    for (int t = pair; t < num_tiles; t += num_pairs) {
+      const int row0 = next.row0, n0 = next.n0;
+      const float *sa = next.sa, *sb = next.sb;
+      float sa_at[3] = {next.sa_at[0], next.sa_at[1], 0.f}, sb_at[3] = {next.sb_at[0], next.sb_at[1], 0.f};
+#pragma unroll
+      for (int c = 0; c < 4; ++c) bias_of[c * 32 + lane] = next.bias[c];
       float2 acc[64];
 #pragma unroll
       for (int i = 0; i < 64; ++i) acc[i] = make_float2(0.f, 0.f);
-      if (p.bias && cols_in) {
-#pragma unroll
-        for (int i = 0; i < 64; ++i) {
-          if (n0 + 2 * i < p.N) acc[i].x = __ldg(p.bias + n0 + 2 * i);
-          if (n0 + 2 * i + 1 < p.N) acc[i].y = __ldg(p.bias + n0 + 2 * i + 1);
+      for (int g = 0; g < groups; ++g) {
+        {
+          const int at = min(g + 2, groups - 1);
+          sa_at[2] = __ldg(sa + at * p.ld_sa); sb_at[2] = __ldg(sb + at);
         }
-      }
-      float f_next = __ldg(sa) * __ldg(sb);
-      for (int g = 0; g < groups; ++g, ++use) {
-        const int buf = use & 1;
-        const float2 f = make_float2(f_next, f_next);
-        if (g + 1 < groups) f_next = __ldg(sa + (g + 1) * p.ld_sa) * __ldg(sb + g + 1);
-        if (!__all_sync(0xffffffffu, mbar_wait(tfull_bar(buf), (use >> 1) & 1u, abort_flag))) goto done;
-        tc_fence_after();
+        const float fs = sa_at[0] * sb_at[0];
+        const float2 f = make_float2(fs, fs);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
+          if (!__all_sync(0xffffffffu, ready || mbar_wait(done_bar(stage_of, h), phase, abort_flag))) goto done;
+          tc_fence_after();
           uint32_t r[64];
           __syncwarp();
-          tmem_ld32p(t_row + buf * BN + h * 64, r);
-          tmem_ld32p(t_row + buf * BN + h * 64 + 32, r + 32);
+          tmem_ld32p(t_row + buf * BN + h * 128, r);
+          tmem_ld32p(t_row + buf * BN + h * 128 + 32, r + 32);
           tmem_ld_wait();
-          if (h == 1) {                                                // everything is in registers: hand the buffer back
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive_cluster_light(tempty_leader[buf]);
-          }
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive_cluster_light(tempty_leader + 8u * (2 * buf + h));
+          if (h == 1 && ++stage_of == STAGES) { stage_of = 0; phase ^= 1u; }
+          ready = mbar_test_wait(done_bar(stage_of, h ^ 1), phase);    // the answer arrives under the multiply-adds
 #pragma unroll
           for (int i = 0; i < 32; ++i)
             acc[h * 32 + i] = ffma2(make_float2(__uint_as_float(r[2 * i]), __uint_as_float(r[2 * i + 1])), f, acc[h * 32 + i]);
         }
+#pragma unroll
+        for (int d = 0; d < 2; ++d) { sa_at[d] = sa_at[d + 1]; sb_at[d] = sb_at[d + 1]; }
+        buf ^= 1;
       }
-      if (!cols_in) continue;
-      const unsigned rows_ok = __ballot_sync(0xffffffffu, row_in);
+      if (t + num_pairs < num_tiles) request(t + num_pairs);
+      if (n0 >= p.N || row0 >= p.M) continue;                          // nothing of this warp's part exists (warp-uniform)
+      __syncwarp();                                                    // bias_of is complete
+      auto finished = [&](int i) {                                     // columns 2i .. 2i + 3 of the warp's 128, i even
+        const float4 b4 = *reinterpret_cast<const float4*>(bias_of + 2 * i);
+        const float2 lo = fadd2(acc[i], make_float2(b4.x, b4.y)), hi = fadd2(acc[i + 1], make_float2(b4.z, b4.w));
+        return make_float4(lo.x, lo.y, hi.x, hi.y);
+      };
+      if (EPI != kBlkGateResidF32 && p.vec_out) {
+        // Through shared memory and out by TMA: the warp is free again as soon as its rows lie there, and what lies
+        // outside the matrix is dropped.  A box is 128 bytes x 32 rows, 16-byte units XOR-swizzled by the row.
+        constexpr bool kWide = EPI == kBlkF32;
+        constexpr int COLS = kWide ? 32 : 64;                          // columns per box; two boxes per round
+#pragma unroll
+        for (int round = 0; round < (kWide ? 2 : 1); ++round) {
+          if (lane == 0) bulk_store_read_done();                       // the previous boxes have left
+          __syncwarp();
+#pragma unroll
+          for (int q = 0; q < 16; ++q) {
+            uint4 w;
+            if constexpr (kWide) {
+              const float4 v = finished(round * 32 + 2 * q);
+              w = make_uint4(__float_as_uint(v.x), __float_as_uint(v.y), __float_as_uint(v.z), __float_as_uint(v.w));
+            } else {
+              float4 a = finished(4 * q), b = finished(4 * q + 2);
+              if (EPI == kBlkGeluF16) {
+                float2 t0 = gelu_tanh_f32x2(make_float2(a.x, a.y)), t1 = gelu_tanh_f32x2(make_float2(a.z, a.w));
+                a = make_float4(t0.x, t0.y, t1.x, t1.y);
+                t0 = gelu_tanh_f32x2(make_float2(b.x, b.y)); t1 = gelu_tanh_f32x2(make_float2(b.z, b.w));
+                b = make_float4(t0.x, t0.y, t1.x, t1.y);
+              }
+              constexpr bool kBf = EPI == kBlkBF16;
+              w = make_uint4(pack16x2<kBf>(a.x, a.y), pack16x2<kBf>(a.z, a.w), pack16x2<kBf>(b.x, b.y), pack16x2<kBf>(b.z, b.w));
+            }
+            *reinterpret_cast<uint4*>(stage + (q >> 3) * 4096 + lane * 128 + (((q & 7) ^ (lane & 7)) << 4)) = w;
+          }
+          fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0) {
+            const int x = n0 + round * 2 * COLS;
+            if (x < p.N) tma_store_2d(&tmOut, smem_u32(stage), x, row0);
+            if (x + COLS < p.N) tma_store_2d(&tmOut, smem_u32(stage) + 4096, x + COLS, row0);
+            bulk_store_commit();
+          }
+        }
+        __syncwarp();
+        continue;
+      }
+      const unsigned rows_ok = __ballot_sync(0xffffffffu, row0 + lane < p.M);
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
         if (n0 + c * 32 >= p.N) break;                                 // warp-uniform
         float v[32];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) { v[2 * i] = acc[c * 16 + i].x; v[2 * i + 1] = acc[c * 16 + i].y; }
+        for (int i = 0; i < 16; i += 2) {
+          const float4 v4 = finished(c * 16 + i);
+          v[2 * i] = v4.x; v[2 * i + 1] = v4.y; v[2 * i + 2] = v4.z; v[2 * i + 3] = v4.w;
+        }
         block_store_chunk<EPI>(p, seq, stage, v, lane, row0, n0 + c * 32, rows_ok);
       }
     }
   }
 
 done:
+  bulk_store_done();                                                   // (threads that stored nothing pass at once)
   tc_fence_before();
   __syncthreads();
   cluster_sync_all();

@@ -106,6 +106,18 @@ bool byte_map(CUtensorMap* m, const void* ptr, uint64_t inner, uint64_t rows, ui
                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// Output matrix: boxes of 128 bytes x 32 rows, 128-byte swizzle.
+bool out_map(CUtensorMap* m, const BlockProduct& b) {
+  const bool wide = b.epilogue == kBlkF32;
+  const cuuint64_t dims[2] = {static_cast<cuuint64_t>(b.n), static_cast<cuuint64_t>(b.m)};
+  const cuuint64_t strides[1] = {static_cast<cuuint64_t>(b.ld_out) * (wide ? 4 : 2)};
+  const cuuint32_t box[2] = {wide ? 32u : 64u, 32u};
+  const cuuint32_t estr[2] = {1, 1};
+  const CUtensorMapDataType type = wide ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : (b.epilogue == kBlkBF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16);
+  return g_encode(m, type, 2, b.out, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                  CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 const SeqInfo kNoSeq{};
 
 template <int EPI, int BT>
@@ -149,7 +161,9 @@ cudaError_t launch_product(const DeviceState& d, const BlockProduct& b, BlockGem
     p.band = cost_cols < cost_rows ? -static_cast<int>(cb) : static_cast<int>(rb);
   }
   const int grid = 2 * static_cast<int>(std::min<long long>(pair_tiles, d.pairs));
-  gemm_block128_pair_kernel<EPI><<<grid, bgemm::THREADS, bgemm::SMEM_BYTES, st>>>(tmA, tmB, p, seq);
+  CUtensorMap tmOut = tmA;                       // unused where the output is written directly
+  if (p.vec_out && EPI != kBlkGateResidF32 && !out_map(&tmOut, b)) return cudaErrorInvalidValue;
+  gemm_block128_pair_kernel<EPI><<<grid, bgemm::THREADS, bgemm::SMEM_BYTES, st>>>(tmA, tmB, tmOut, p, seq);
   return cudaGetLastError();
 }
 
