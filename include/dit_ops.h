@@ -77,6 +77,55 @@ typedef struct {
 } dit_gemm_block128_args;
 dit_status dit_gemm_block128(const dit_gemm_block128_args *args, void *stream);
 
+/* A batch of attention problems over packed rows, as the step packs its requests: request r owns q_lens[r] rows of q
+ * (and of the output) and kv_lens[r] rows of k and v, one request after the other.  Head h is columns
+ * h * head_dim .. of each.  The lengths are HOST arrays, read before the call returns; they differ for a few new rows that
+ * read a longer stored context, and are equal in a denoising step.  A request may have no rows of q, or none of k.
+ *   Query block i of a request is its rows 128 i .. 128 i + 127, key block j likewise (the last one may be short);
+ *   blocks are counted from each request's own first row.  Query blocks are numbered through the batch,
+ *   request after request: n_query_blocks = sum of ceil(q_lens[r] / 128).
+ *   q, k, v   device, type f16 or bf16, 16-byte aligned, leading dimensions multiples of 8 and >= n_heads * head_dim
+ *             (three column ranges of one packed [rows, 3 * width] buffer are fine)
+ *   head_dim  64 or 128; n_requests <= DIT_MAX_REQUESTS */
+typedef struct {
+  const void *q, *k, *v;
+  int64_t ld_q, ld_k, ld_v;
+  dit_type type;
+  int32_t n_heads, head_dim, n_requests;
+  const int32_t *q_lens, *kv_lens;
+} dit_attention_batch;
+
+/* Selects key blocks by a cheap score: the product of the mean of the query block's rows with the mean of the key
+ * block's rows, taken in 64-bit arithmetic.  Each query block of each head keeps the
+ * min(keep[r], key blocks of its request) key blocks with the largest scores; of equal scores the lower block
+ * wins; a NaN counts as less than any number.  Key blocks that hold one of the request's last tail_rows[r] rows (its text
+ * tokens) come before every score; where there are more of them than keep[r], the lowest of them.  v is not read.
+ *   keep, tail_rows  HOST [n_requests], keep >= 1, tail_rows >= 0 or NULL (no tail)
+ *   block_index      device int32 [n_heads, n_query_blocks, ld_index], ld_index >= the largest keep: the selected key
+ *                    blocks in ascending order, then -1 up to the largest keep of the batch
+ *   block_count      device int32 [n_heads, n_query_blocks]
+ *   workspace        device, 16-byte aligned, dit_select_blocks_workspace(batch) bytes; its contents need not be
+ *                    kept between calls, and calls that may run at the same time need workspaces of their own
+ * DIT_ERR_SHAPE for lengths whose sum leaves int32, head_dim other than 64 or 128, or more than 16384 key blocks in a
+ * request; DIT_ERR_CAPACITY for too many requests or too small a workspace. */
+size_t dit_select_blocks_workspace(const dit_attention_batch *batch);
+dit_status dit_select_blocks(const dit_attention_batch *batch, const int32_t *keep, const int32_t *tail_rows,
+                             int32_t *block_index, int32_t *block_count, int64_t ld_index, void *workspace,
+                             size_t workspace_bytes, void *stream);
+
+/* Softmax attention of every query row over the keys of its query block's listed key blocks:
+ *   out[i] = sum_j softmax_j(scale * q_i . k_j) v_j,   j over the rows of the listed blocks of row i's request
+ * The lists are those of dit_select_blocks or the caller's own: the first block_count entries of each list count, clamped
+ * to [0, ld_index]; their order does not matter, an entry listed twice counts once, and entries outside the
+ * request's key blocks are ignored.  A row without any key gets zeros.  Rows of other requests are never
+ * part of a result, whatever they hold.  Scores, the softmax and the sums are held in fp32; probabilities are rounded
+ * to the inputs' type for the second product, as the step's attention does.
+ *   scale   0 for 1 / sqrt(head_dim)
+ *   out     device, the inputs' type, rows as q's, 16-byte aligned, ld_out a multiple of 8 and >= n_heads * head_dim;
+ *           must not overlap the inputs */
+dit_status dit_block_attention(const dit_attention_batch *batch, const int32_t *block_index, const int32_t *block_count,
+                               int64_t ld_index, float scale, void *out, int64_t ld_out, void *stream);
+
 /* Reads and clears (with a synchronisation of the current device) the status word that a kernel of this
  * header sets when a bounded wait ran out: DIT_OK or DIT_ERR_TIMEOUT. */
 dit_status dit_ops_poll_status(void);

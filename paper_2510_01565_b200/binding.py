@@ -63,8 +63,14 @@ class DitGemmBlock128Args(C.Structure):
                 + [(n, C.c_int64) for n in ("lda", "ld_a_scales", "ldb", "ld_out", "m", "n", "k")] + [("out_type", C.c_int)])
 
 
+class DitAttentionBatch(C.Structure):
+    _fields_ = ([(n, C.c_void_p) for n in ("q", "k", "v")] + [(n, C.c_int64) for n in ("ld_q", "ld_k", "ld_v")] + [("type", C.c_int)]
+                + [(n, C.c_int32) for n in ("n_heads", "head_dim", "n_requests")] + [("q_lens", C.POINTER(C.c_int32)), ("kv_lens", C.POINTER(C.c_int32))])
+
+
 SCHED_EXPORTS = ["dit_sched_allocate", "dit_sched_round"]
-OPS_EXPORTS = ["dit_quantize_block128", "dit_quantize_weight_block128", "dit_gemm_block128", "dit_ops_poll_status"]
+OPS_EXPORTS = ["dit_quantize_block128", "dit_quantize_weight_block128", "dit_gemm_block128", "dit_select_blocks_workspace", "dit_select_blocks",
+               "dit_block_attention", "dit_ops_poll_status"]
 BLOCK = 128      # columns per scale; rows per query block and per key block
 
 
@@ -170,6 +176,13 @@ def load_library() -> C.CDLL:
     lib.dit_quantize_weight_block128.argtypes = [vp, C.c_int, i64, i64, i64, vp, i64, vp, vp]
     lib.dit_gemm_block128.restype = C.c_int
     lib.dit_gemm_block128.argtypes = [C.POINTER(DitGemmBlock128Args), vp]
+    bp = C.POINTER(DitAttentionBatch)
+    lib.dit_select_blocks_workspace.restype = C.c_size_t
+    lib.dit_select_blocks_workspace.argtypes = [bp]
+    lib.dit_select_blocks.restype = C.c_int
+    lib.dit_select_blocks.argtypes = [bp, C.POINTER(i32), C.POINTER(i32), vp, vp, i64, vp, C.c_size_t, vp]
+    lib.dit_block_attention.restype = C.c_int
+    lib.dit_block_attention.argtypes = [bp, vp, vp, i64, C.c_float, vp, i64, vp]
     lib.dit_ops_poll_status.restype = C.c_int
     lib.dit_ops_poll_status.argtypes = []
     lib.dit_last_launch_count.restype = i64
@@ -602,7 +615,7 @@ def _matrix(t, what: str):
     """A CUDA matrix whose rows are contiguous (rows themselves may lie apart): the row stride in elements."""
     _need(t.is_cuda and t.dim() == 2, f"{what} must be a CUDA matrix")
     _need(t.shape[1] <= 1 or t.stride(1) == 1, f"{what} must be contiguous along its columns")
-    return max(t.stride(0), t.shape[1]) if t.shape[0] <= 1 else t.stride(0)
+    return t.shape[1] if t.shape[0] <= 1 else t.stride(0)
 
 
 class _on_device:
@@ -705,6 +718,70 @@ def dit_gemm_block128(a, a_scales, b, b_scales, bias=None, out=None, out_dtype=N
                                _matrix(out, "out"), m, n, k, _type_code(out.dtype))
     with _on_device(stream, a, a_scales, b, b_scales, bias, out) as s:
         _ops_check(lib.dit_gemm_block128(C.byref(args), s))
+    return out
+
+
+def _attention_batch(q, k, v, q_lens, kv_lens, n_heads):
+    """(struct, number of query blocks); v may be None.  The arrays of lengths live as long as the struct does."""
+    n = len(q_lens)
+    _need(len(kv_lens) == n, "q_lens and kv_lens differ in length")
+    rows = {"q": sum(q_lens), "k": sum(kv_lens), "v": sum(kv_lens)}
+    width = q.shape[-1]
+    _need(n_heads >= 1 and width % n_heads == 0, "the columns of q do not divide into n_heads")
+    for t, what in ((q, "q"), (k, "k"), (v, "v")):
+        if t is not None:
+            _need(t.dim() == 2 and t.shape == (rows[what], width), f"{what} must be [{rows[what]}, {width}]")
+            _need(t.dtype == q.dtype, "q, k and v differ in type")
+    lds = [0 if t is None else _matrix(t, what) for t, what in ((q, "q"), (k, "k"), (v, "v"))]
+    lens = C.c_int32 * max(n, 1)
+    batch = DitAttentionBatch(_data(q), _data(k), _data(v), *lds, _type_code(q.dtype), n_heads, width // n_heads, n, lens(*q_lens), lens(*kv_lens))
+    return batch, sum((l + BLOCK - 1) // BLOCK for l in q_lens)
+
+
+def dit_select_blocks(q, k, q_lens, kv_lens, n_heads: int, keep, tail_rows=None, index=None, count=None, workspace=None, stream=None):
+    """q [sum q_lens, width], k [sum kv_lens, width] fp16 or bf16; keep, tail_rows: one whole number per request.
+    -> (block_index [n_heads, query blocks, max keep] int32, block_count [n_heads, query blocks] int32)."""
+    import torch
+    lib = load_library()
+    batch, q_blocks = _attention_batch(q, k, None, q_lens, kv_lens, n_heads)
+    n = len(q_lens)
+    _need(len(keep) == n and (tail_rows is None or len(tail_rows) == n), "keep and tail_rows need one number per request")
+    widest = max(keep, default=1)
+    if index is None:
+        _need(widest >= 1, "keep must be at least 1")
+        index = torch.empty((n_heads, q_blocks, widest), dtype=torch.int32, device=q.device)
+    if count is None:
+        count = torch.empty((n_heads, q_blocks), dtype=torch.int32, device=q.device)
+    _check_lists(index, count, n_heads, q_blocks)
+    size = lib.dit_select_blocks_workspace(C.byref(batch))
+    if workspace is None:
+        workspace = torch.empty(max(size, 16), dtype=torch.uint8, device=q.device)
+    ints = C.c_int32 * max(n, 1)
+    with _on_device(stream, q, k, index, count, workspace) as s:
+        _ops_check(lib.dit_select_blocks(C.byref(batch), ints(*keep), None if tail_rows is None else ints(*tail_rows), _data(index), _data(count),
+                                         index.shape[2], _data(workspace), workspace.numel() * workspace.element_size(), s))
+    return index, count
+
+
+def _check_lists(index, count, n_heads, q_blocks):
+    import torch
+    _need(index.is_cuda and index.dtype == torch.int32 and index.is_contiguous() and index.dim() == 3 and index.shape[:2] == (n_heads, q_blocks),
+          "block_index must be contiguous int32 [n_heads, query blocks, entries]")
+    _need(count.is_cuda and count.dtype == torch.int32 and count.is_contiguous() and count.shape == (n_heads, q_blocks),
+          "block_count must be contiguous int32 [n_heads, query blocks]")
+
+
+def dit_block_attention(q, k, v, q_lens, kv_lens, n_heads: int, index, count, scale: float = 0.0, out=None, stream=None):
+    """Attention of every query block over its listed key blocks -> out, shaped and typed like q."""
+    import torch
+    lib = load_library()
+    batch, q_blocks = _attention_batch(q, k, v, q_lens, kv_lens, n_heads)
+    _check_lists(index, count, n_heads, q_blocks)
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    _need(out.shape == q.shape and out.dtype == q.dtype, "out must be shaped and typed like q")
+    with _on_device(stream, q, k, v, index, count, out) as s:
+        _ops_check(lib.dit_block_attention(C.byref(batch), _data(index), _data(count), max(index.shape[2], 1), scale, _data(out), _matrix(out, "out"), s))
     return out
 
 

@@ -1,9 +1,11 @@
 // The context-free operators of include/dit_ops.h: argument checks, tensor maps, launch rules.
 #include <algorithm>
+#include <cmath>
 #include <cstdint>
 #include <mutex>
 #include <type_traits>
 
+#include "block_attention.cuh"
 #include "block_gemm.cuh"
 #include "block_quant.cuh"
 #include "common.cuh"
@@ -19,6 +21,9 @@ typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t,
 
 constexpr int kMaxDevices = 64;
 constexpr int64_t kMaxSize = INT32_MAX - 1024;
+// selecting kernel: means of four query blocks, then the scores of one to four rows
+constexpr int kSelectFixedSmem = 128 * kSelectRows * 8;
+constexpr int kSelectSmemMax = kSelectFixedSmem + kMaxKeyBlocks * 8 + 32 * 1024;
 
 // One status word per device, for waits that ran out.  In host code its name is a handle; the device
 // address is looked up once per device, with that device current.
@@ -44,6 +49,15 @@ cudaError_t allow_gemm() {
   if (e == cudaSuccess) e = allow_smem(&gemm_block128_split_kernel<EPI, 32>, SplitCfg<32>::SMEM_BYTES);
   if (e == cudaSuccess) e = allow_smem(&gemm_block128_split_kernel<EPI, 64>, SplitCfg<64>::SMEM_BYTES);
   if (e == cudaSuccess) e = allow_smem(&gemm_block128_split_kernel<EPI, 128>, SplitCfg<128>::SMEM_BYTES);
+  return e;
+}
+
+template <int D, bool BF16>
+cudaError_t allow_attention() {
+  cudaError_t e = allow_smem(&block_attention_kernel<D, BF16>, BlockAttnCfg<D>::SMEM_BYTES);
+  if (e == cudaSuccess) e = allow_smem(&block_rows_kernel<D, BF16, 1>, BlockRowsCfg<D>::SMEM_BYTES);
+  if (e == cudaSuccess) e = allow_smem(&block_rows_kernel<D, BF16, 2>, BlockRowsCfg<D>::SMEM_BYTES);
+  if (e == cudaSuccess) e = allow_smem(&block_rows_kernel<D, BF16, 4>, BlockRowsCfg<D>::SMEM_BYTES);
   return e;
 }
 
@@ -74,6 +88,10 @@ cudaError_t device_state(const DeviceState** out, bool* unsupported) {
     if ((e = allow_gemm<kBlkF16>()) != cudaSuccess || (e = allow_gemm<kBlkBF16>()) != cudaSuccess || (e = allow_gemm<kBlkF32>()) != cudaSuccess ||
         (e = allow_gemm<kBlkGeluF16>()) != cudaSuccess || (e = allow_gemm<kBlkGateResidF32>()) != cudaSuccess)
       return e;
+    if ((e = allow_attention<64, false>()) != cudaSuccess || (e = allow_attention<64, true>()) != cudaSuccess ||
+        (e = allow_attention<128, false>()) != cudaSuccess || (e = allow_attention<128, true>()) != cudaSuccess ||
+        (e = allow_smem(&block_select_kernel, kSelectSmemMax)) != cudaSuccess)
+      return e;
     cudaLaunchConfig_t lc = {};
     lc.gridDim = dim3(s.num_sms & ~1); lc.blockDim = dim3(bgemm::THREADS); lc.dynamicSmemBytes = bgemm::SMEM_BYTES;
     cudaLaunchAttribute at;
@@ -96,6 +114,10 @@ dit_status ready(const DeviceState** s) {
   return e == cudaSuccess ? DIT_OK : DIT_ERR_CUDA;
 }
 
+int type_bytes(dit_type t) { return t == DIT_TYPE_F32 ? 4 : 2; }
+bool type_ok(dit_type t) { return t == DIT_TYPE_F16 || t == DIT_TYPE_BF16 || t == DIT_TYPE_F32; }
+bool aligned(const void* p, uintptr_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
+
 // Byte matrix [rows, inner] with `pitch` bytes between rows: boxes of 128 bytes x box_rows, 128-byte swizzle, zeros outside.
 bool byte_map(CUtensorMap* m, const void* ptr, uint64_t inner, uint64_t rows, uint64_t pitch, uint32_t box_rows) {
   const cuuint64_t dims[2] = {inner, rows};
@@ -116,6 +138,91 @@ bool out_map(CUtensorMap* m, const BlockProduct& b) {
   const CUtensorMapDataType type = wide ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : (b.epilogue == kBlkBF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16);
   return g_encode(m, type, 2, b.out, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                   CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// 16-bit matrix [rows, cols] with row stride ld: boxes of 64 columns x 128 rows, 128-byte swizzle, zeros outside.
+bool half_map(CUtensorMap* m, const void* ptr, uint64_t cols, uint64_t rows, uint64_t ld) {
+  const cuuint64_t dims[2] = {cols, rows};
+  const cuuint64_t strides[1] = {ld * 2};
+  const cuuint32_t box[2] = {64, 128};
+  const cuuint32_t estr[2] = {1, 1};
+  return g_encode(m, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, const_cast<void*>(ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Checks what the selector and the attention share and lays the batch out.  `values`: v is needed as well.
+dit_status plan_batch(const dit_attention_batch* a, bool values, BlockBatch* b) {
+  if (!a || a->n_requests < 0 || a->n_heads < 1 || (a->type != DIT_TYPE_F16 && a->type != DIT_TYPE_BF16)) return DIT_ERR_INVALID_ARG;
+  if (a->head_dim != 64 && a->head_dim != 128) return DIT_ERR_SHAPE;
+  if (a->n_requests > DIT_MAX_REQUESTS) return DIT_ERR_CAPACITY;
+  if (a->n_requests > 0 && (!a->q_lens || !a->kv_lens)) return DIT_ERR_INVALID_ARG;
+  if (static_cast<int64_t>(a->n_heads) * a->head_dim > (1 << 20)) return DIT_ERR_SHAPE;
+  int64_t q = 0, kv = 0, qb = 0, kb = 0;
+  b->n = a->n_requests;
+  for (int r = 0; r <= a->n_requests; ++r) {
+    b->cu_q[r] = static_cast<int>(q); b->cu_kv[r] = static_cast<int>(kv);
+    b->first_qblock[r] = static_cast<int>(qb); b->first_kblock[r] = static_cast<int>(kb);
+    if (r == a->n_requests) break;
+    if (a->q_lens[r] < 0 || a->kv_lens[r] < 0) return DIT_ERR_INVALID_ARG;
+    const int64_t kblocks = (static_cast<int64_t>(a->kv_lens[r]) + 127) / 128;
+    if (kblocks > kMaxKeyBlocks) return DIT_ERR_SHAPE;
+    q += a->q_lens[r]; kv += a->kv_lens[r];
+    qb += (static_cast<int64_t>(a->q_lens[r]) + 127) / 128; kb += kblocks;
+    if (q > kMaxSize || kv > kMaxSize) return DIT_ERR_SHAPE;
+    b->order[r] = r;
+  }
+  for (int i = 1; i < b->n; ++i)                 // requests with the most query rows first (insertion sort: stable, at most 64)
+    for (int j = i; j > 0 && a->q_lens[b->order[j]] > a->q_lens[b->order[j - 1]]; --j) std::swap(b->order[j], b->order[j - 1]);
+  const int64_t width = static_cast<int64_t>(a->n_heads) * a->head_dim;
+  auto matrix = [&](const void* p, int64_t ld, int64_t rows) { return rows == 0 || (p && aligned(p, 16) && ld >= width && ld % 8 == 0); };
+  if (!matrix(a->q, a->ld_q, q) || !matrix(a->k, a->ld_k, kv) || (values && !matrix(a->v, a->ld_v, kv))) return DIT_ERR_INVALID_ARG;
+  // grids are counted in 32 bits
+  if ((qb + kb) * a->n_heads > INT32_MAX / 16) return DIT_ERR_SHAPE;
+  return DIT_OK;
+}
+
+template <int D, bool BF16, int R>
+cudaError_t launch_rows(const CUtensorMap& tmK, const CUtensorMap& tmV, const BlockAttnParams& p, const dit_attention_batch& a, const BlockBatch& b,
+                        int splits, cudaStream_t st) {
+  cudaLaunchConfig_t lc = {};
+  lc.gridDim = dim3(static_cast<unsigned>(b.n) * a.n_heads * splits); lc.blockDim = dim3(BlockRowsCfg<D>::THREADS);
+  lc.dynamicSmemBytes = BlockRowsCfg<D>::SMEM_BYTES; lc.stream = st;
+  cudaLaunchAttribute at;
+  at.id = cudaLaunchAttributeClusterDimension;
+  at.val.clusterDim.x = splits; at.val.clusterDim.y = 1; at.val.clusterDim.z = 1;
+  lc.attrs = &at; lc.numAttrs = splits > 1 ? 1 : 0;
+  return cudaLaunchKernelEx(&lc, &block_rows_kernel<D, BF16, R>, tmK, tmV, p, static_cast<const uint16_t*>(a.q), static_cast<long long>(a.ld_q), b, splits);
+}
+
+template <int D, bool BF16>
+cudaError_t launch_attend(const DeviceState& d, const dit_attention_batch& a, const BlockBatch& b, const BlockAttnParams& p, cudaStream_t st) {
+  const uint64_t width = static_cast<uint64_t>(a.n_heads) * D;
+  const int q_rows = b.cu_q[b.n], kv_rows = b.cu_kv[b.n];
+  int most = 0, qblocks = 0, longest = 0;
+  for (int r = 0; r < b.n; ++r) {
+    const int rows = b.cu_q[r + 1] - b.cu_q[r];
+    most = std::max(most, rows);
+    longest = std::max(longest, b.first_kblock[r + 1] - b.first_kblock[r]);
+    qblocks += (rows + BlockAttnCfg<D>::Q_ROWS - 1) / BlockAttnCfg<D>::Q_ROWS;
+  }
+  CUtensorMap tmQ, tmK, tmV;
+  // without keys nothing is loaded; the maps still have to describe some memory
+  const void* k = kv_rows > 0 ? a.k : a.q;
+  const void* v = kv_rows > 0 ? a.v : a.q;
+  if (!half_map(&tmQ, a.q, width, q_rows, a.ld_q) || !half_map(&tmK, k, width, std::max(kv_rows, 1), kv_rows > 0 ? a.ld_k : a.ld_q) ||
+      !half_map(&tmV, v, width, std::max(kv_rows, 1), kv_rows > 0 ? a.ld_v : a.ld_q))
+    return cudaErrorInvalidValue;
+  if (most <= 4) {
+    // a cluster of CTAs per (request, head): as many as two CTAs per SM hold, no more than there are blocks to share
+    const int items = b.n * a.n_heads;
+    const long long listed = std::min<long long>(longest, p.ld_index);
+    const int splits = static_cast<int>(std::max<long long>(1, std::min<long long>({8, 2ll * d.num_sms / items, listed})));
+    if (most <= 1) return launch_rows<D, BF16, 1>(tmK, tmV, p, a, b, splits, st);
+    if (most <= 2) return launch_rows<D, BF16, 2>(tmK, tmV, p, a, b, splits, st);
+    return launch_rows<D, BF16, 4>(tmK, tmV, p, a, b, splits, st);
+  }
+  block_attention_kernel<D, BF16><<<static_cast<unsigned>(qblocks) * a.n_heads, BlockAttnCfg<D>::THREADS, BlockAttnCfg<D>::SMEM_BYTES, st>>>(tmQ, tmK, tmV, p, b);
+  return cudaGetLastError();
 }
 
 const SeqInfo kNoSeq{};
@@ -182,9 +289,38 @@ cudaError_t launch_quant_weight(const QuantWeightParams& p, bool vec, cudaStream
   return cudaGetLastError();
 }
 
-int type_bytes(dit_type t) { return t == DIT_TYPE_F32 ? 4 : 2; }
-bool type_ok(dit_type t) { return t == DIT_TYPE_F16 || t == DIT_TYPE_BF16 || t == DIT_TYPE_F32; }
-bool aligned(const void* p, uintptr_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
+cudaError_t launch_select(const dit_attention_batch& a, const BlockBatch& b, BlockSelectParams p, int32_t* index, int32_t* count, int64_t ld_index,
+                          void* workspace, cudaStream_t st) {
+  p.q = static_cast<const uint16_t*>(a.q); p.k = static_cast<const uint16_t*>(a.k);
+  p.ld_q = a.ld_q; p.ld_k = a.ld_k;
+  p.n_heads = a.n_heads; p.head_dim = a.head_dim; p.width = a.n_heads * a.head_dim;
+  const int q_blocks = b.first_qblock[b.n], k_blocks = b.first_kblock[b.n];
+  p.q_mean = static_cast<double*>(workspace);
+  p.k_mean = p.q_mean + static_cast<size_t>(q_blocks) * p.width;
+  p.index = index; p.count = count; p.ld_index = ld_index;
+  int longest = 1;
+  for (int r = 0; r < b.n; ++r) longest = std::max(longest, b.first_kblock[r + 1] - b.first_kblock[r]);
+  p.rows = std::max(1, std::min(kSelectRows, (kSelectSmemMax - kSelectFixedSmem) / (longest * 8)));
+  const unsigned grid = static_cast<unsigned>(q_blocks + k_blocks) * ((p.width + 255) / 256);
+  if (a.type == DIT_TYPE_BF16) block_means_kernel<true><<<grid, 256, 0, st>>>(p, b);
+  else block_means_kernel<false><<<grid, 256, 0, st>>>(p, b);
+  cudaError_t e = cudaGetLastError();
+  if (e != cudaSuccess) return e;
+  unsigned groups = 0;
+  for (int r = 0; r < b.n; ++r) groups += (b.first_qblock[r + 1] - b.first_qblock[r] + p.rows - 1) / p.rows;
+  block_select_kernel<<<groups * a.n_heads, 256, kSelectFixedSmem + static_cast<size_t>(p.rows) * longest * 8, st>>>(p, b);
+  return cudaGetLastError();
+}
+
+cudaError_t launch_block_attention(const dit_attention_batch& a, const BlockBatch& b, const int32_t* index, const int32_t* count, int64_t ld_index,
+                                   float scale, void* out, int64_t ld_out, const DeviceState& d, cudaStream_t st) {
+  BlockAttnParams p{};
+  p.out = out; p.ld_out = ld_out; p.index = index; p.count = count; p.ld_index = ld_index; p.n_heads = a.n_heads;
+  p.scale_log2 = 1.4426950408889634f * (scale > 0.f ? scale : 1.0f / sqrtf(static_cast<float>(a.head_dim)));
+  p.status = d.status;
+  if (a.head_dim == 128) return a.type == DIT_TYPE_BF16 ? launch_attend<128, true>(d, a, b, p, st) : launch_attend<128, false>(d, a, b, p, st);
+  return a.type == DIT_TYPE_BF16 ? launch_attend<64, true>(d, a, b, p, st) : launch_attend<64, false>(d, a, b, p, st);
+}
 
 }  // namespace
 
@@ -305,6 +441,60 @@ dit_status dit_gemm_block128(const dit_gemm_block128_args* a, void* stream) {
   b.m = static_cast<int>(a->m); b.n = static_cast<int>(a->n); b.k = static_cast<int>(a->k);
   b.epilogue = a->out_type == DIT_TYPE_F16 ? kBlkF16 : (a->out_type == DIT_TYPE_BF16 ? kBlkBF16 : kBlkF32);
   return launch_block_product(b, kNoSeq, static_cast<cudaStream_t>(stream)) == cudaSuccess ? DIT_OK : DIT_ERR_CUDA;
+}
+
+size_t dit_select_blocks_workspace(const dit_attention_batch* a) {
+  BlockBatch b;
+  dit_attention_batch shape;
+  if (!a) return 0;
+  shape = *a;                                    // sizes only: the matrices need not exist yet
+  shape.q = shape.k = shape.v = reinterpret_cast<const void*>(static_cast<uintptr_t>(16));
+  shape.ld_q = shape.ld_k = shape.ld_v = INT64_MAX / 16 * 8;
+  if (plan_batch(&shape, false, &b) != DIT_OK) return 0;
+  const size_t blocks = static_cast<size_t>(b.first_qblock[b.n]) + b.first_kblock[b.n];
+  return std::max<size_t>(16, blocks * a->n_heads * a->head_dim * sizeof(double));
+}
+
+dit_status dit_select_blocks(const dit_attention_batch* a, const int32_t* keep, const int32_t* tail_rows, int32_t* block_index,
+                             int32_t* block_count, int64_t ld_index, void* workspace, size_t workspace_bytes, void* stream) {
+  BlockBatch b;
+  dit_status s = plan_batch(a, false, &b);
+  if (s != DIT_OK) return s;
+  if (b.first_qblock[b.n] == 0) return DIT_OK;
+  if (!keep || !block_index || !block_count || !workspace || !aligned(workspace, 16) || !aligned(block_index, 4) || !aligned(block_count, 4))
+    return DIT_ERR_INVALID_ARG;
+  BlockSelectParams p{};
+  int longest = 1;
+  for (int r = 0; r < b.n; ++r) {
+    if (keep[r] < 1 || (tail_rows && tail_rows[r] < 0)) return DIT_ERR_INVALID_ARG;
+    p.keep[r] = keep[r];
+    p.tail[r] = tail_rows ? tail_rows[r] : 0;
+    p.widest = std::max(p.widest, keep[r]);
+    longest = std::max(longest, b.first_kblock[r + 1] - b.first_kblock[r]);
+  }
+  if (ld_index < p.widest) return DIT_ERR_INVALID_ARG;
+  if (workspace_bytes < dit_select_blocks_workspace(a)) return DIT_ERR_CAPACITY;
+  const DeviceState* d;
+  s = ready(&d);
+  if (s != DIT_OK) return s;
+  return launch_select(*a, b, p, block_index, block_count, ld_index, workspace, static_cast<cudaStream_t>(stream)) == cudaSuccess ? DIT_OK : DIT_ERR_CUDA;
+}
+
+dit_status dit_block_attention(const dit_attention_batch* a, const int32_t* block_index, const int32_t* block_count, int64_t ld_index,
+                               float scale, void* out, int64_t ld_out, void* stream) {
+  BlockBatch b;
+  dit_status s = plan_batch(a, true, &b);
+  if (s != DIT_OK) return s;
+  if (b.cu_q[b.n] == 0) return DIT_OK;
+  if (!block_index || !block_count || !out || ld_index < 1) return DIT_ERR_INVALID_ARG;
+  if (!aligned(block_index, 4) || !aligned(block_count, 4) || !aligned(out, 16) || ld_out % 8 || ld_out < static_cast<int64_t>(a->n_heads) * a->head_dim)
+    return DIT_ERR_INVALID_ARG;
+  if (!(scale >= 0.f) || !(scale <= 3.0e38f)) return DIT_ERR_INVALID_ARG;
+  const DeviceState* d;
+  s = ready(&d);
+  if (s != DIT_OK) return s;
+  return launch_block_attention(*a, b, block_index, block_count, ld_index, scale, out, ld_out, *d, static_cast<cudaStream_t>(stream)) == cudaSuccess
+             ? DIT_OK : DIT_ERR_CUDA;
 }
 
 dit_status dit_ops_poll_status(void) {

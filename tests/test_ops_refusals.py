@@ -76,3 +76,61 @@ def test_binding_refuses_what_it_cannot_describe():
     assert e.value.status == INVALID
     with pytest.raises(B.DitError):
         B.dit_gemm_block128(x, x, x, x)
+
+
+def batch(**kw):
+    """(struct, the arrays it points to): two requests, two heads of 64."""
+    a = dict(q=P, k=P, v=P, ld_q=128, ld_k=128, ld_v=128, type=0, n_heads=2, head_dim=64, q_lens=[200, 1], kv_lens=[300, 40])
+    a.update(kw)
+    n = a.pop("n", len(a["q_lens"] or a["kv_lens"] or []))
+    lens = [None if a[x] is None else (C.c_int32 * max(1, len(a[x])))(*a[x]) for x in ("q_lens", "kv_lens")]
+    return B.DitAttentionBatch(*[a[x] for x in ("q", "k", "v", "ld_q", "ld_k", "ld_v", "type", "n_heads", "head_dim")], n, *lens), lens
+
+
+BAD_BATCHES = [(dict(q=None), INVALID), (dict(k=None), INVALID), (dict(type=2), INVALID), (dict(type=-1), INVALID), (dict(n_heads=0), INVALID), (dict(n=-1), INVALID),
+               (dict(ld_q=120), INVALID), (dict(ld_k=132), INVALID), (dict(q=P + 8), INVALID), (dict(k=P + 2), INVALID), (dict(q_lens=[-1, 5]), INVALID),
+               (dict(kv_lens=[4, -1]), INVALID), (dict(q_lens=None, n=2), INVALID), (dict(kv_lens=None, n=2), INVALID), (dict(head_dim=96, ld_q=192, ld_k=192), SHAPE),
+               (dict(head_dim=32), SHAPE), (dict(kv_lens=[128 * 16384 + 1, 1]), SHAPE), (dict(q_lens=[2 ** 31 - 1, 2 ** 31 - 1]), SHAPE), (dict(n=65), 3)]
+
+
+@pytest.mark.parametrize("kw,status", BAD_BATCHES)
+def test_attention_batches_refused_by_both_operators(lib, kw, status):
+    b, _keep = batch(**kw)
+    two = (C.c_int32 * 2)(1, 1)
+    assert lib.dit_select_blocks(C.byref(b), two, None, P, P, 4, P, 1 << 30, None) == status
+    assert lib.dit_block_attention(C.byref(b), P, P, 4, 0.0, P, 128, None) == status
+    if "q" not in kw and "k" not in kw and "ld_q" not in kw and "ld_k" not in kw:
+        assert lib.dit_select_blocks_workspace(C.byref(b)) == 0
+
+
+def test_selector_refusals(lib):
+    b, _keep = batch()
+    size = lib.dit_select_blocks_workspace(C.byref(b))
+    assert size == (3 + 4) * 128 * 8 and lib.dit_select_blocks_workspace(None) == 0
+    ints = lambda *x: (C.c_int32 * len(x))(*x)
+
+    def call(keep=ints(2, 1), tail=None, index=P, count=P, ld=2, ws=P, nbytes=size):
+        return lib.dit_select_blocks(C.byref(b), keep, tail, index, count, ld, ws, nbytes, None)
+    for kw in (dict(keep=None), dict(keep=ints(0, 1)), dict(keep=ints(2, -1)), dict(tail=ints(-1, 0)), dict(index=None), dict(count=None), dict(ld=1),
+               dict(ws=None), dict(ws=P + 8), dict(index=P + 2)):
+        assert call(**kw) == INVALID, kw
+    assert call(nbytes=size - 1) == 3
+    empty, _e = batch(q_lens=[0, 0])
+    assert lib.dit_select_blocks(C.byref(empty), None, None, None, None, 0, None, 0, None) == OK
+    assert lib.dit_select_blocks(None, None, None, None, None, 0, None, 0, None) == INVALID
+
+
+def test_attention_refusals(lib):
+    b, _keep = batch()
+
+    def call(batch_=b, index=P, count=P, ld=2, scale=0.0, out=P, ld_out=128):
+        return lib.dit_block_attention(C.byref(batch_), index, count, ld, scale, out, ld_out, None)
+    for kw in (dict(index=None), dict(count=None), dict(out=None), dict(ld=0), dict(ld_out=120), dict(ld_out=129), dict(out=P + 8), dict(index=P + 1),
+               dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf"))):
+        assert call(**kw) == INVALID, kw
+    for kw in (dict(v=None), dict(ld_v=100), dict(ld_v=100, v=P), dict(v=P + 4)):
+        bad, _k = batch(**kw)
+        assert call(bad) == INVALID, kw
+    empty, _e = batch(q_lens=[0, 0])
+    assert call(empty, index=None, out=None) == OK
+    assert lib.dit_block_attention(None, P, P, 2, 0.0, P, 128, None) == INVALID
