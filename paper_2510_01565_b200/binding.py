@@ -599,45 +599,55 @@ def dit_modulation_noalloc(cond, w_ada, b_ada, mod_out, stream=None):
 
 
 # ---------------------------------------------------------------------- operators without a context (dit_ops.h)
-def _need(ok: bool, what: str):
-    if not ok:
-        raise DitError(1, what)
+# The small shapes of these operators take the GPU a few microseconds: their marshalling is kept short (no context
+# managers unless a device has to be switched, raw stream handles, one pass over the checks).
+def _refuse(what: str):
+    raise DitError(1, what)
+
+
+_TYPE_CODES: Dict[object, int] = {}
 
 
 def _type_code(dtype) -> int:
-    import torch
-    codes = {torch.float16: 0, torch.bfloat16: 1, torch.float32: 2}
-    _need(dtype in codes, f"{dtype} is not one of float16, bfloat16, float32")
-    return codes[dtype]
-
-
-def _matrix(t, what: str):
-    """A CUDA matrix whose rows are contiguous (rows themselves may lie apart): the row stride in elements."""
-    _need(t.is_cuda and t.dim() == 2, f"{what} must be a CUDA matrix")
-    _need(t.shape[1] <= 1 or t.stride(1) == 1, f"{what} must be contiguous along its columns")
-    return t.shape[1] if t.shape[0] <= 1 else t.stride(0)
-
-
-class _on_device:
-    """Makes the tensors' device current (they must share one) and hands out the stream to use there."""
-
-    def __init__(self, stream, first, *others):
+    if not _TYPE_CODES:
         import torch
-        for t in others:
-            _need(t is None or t.device == first.device, "tensors lie on different devices")
-        self.guard, self.torch, self.stream, self.device = torch.cuda.device(first.device), torch, stream, first.device
-
-    def __enter__(self):
-        self.guard.__enter__()
-        s = self.torch.cuda.current_stream(self.device) if self.stream is None else self.stream
-        _need(s.device == self.device, "the stream belongs to another device than the tensors")
-        return C.c_void_p(s.cuda_stream)
-
-    def __exit__(self, *exc):
-        return self.guard.__exit__(*exc)
+        _TYPE_CODES.update({torch.float16: 0, torch.bfloat16: 1, torch.float32: 2})
+    code = _TYPE_CODES.get(dtype)
+    if code is None:
+        _refuse(f"{dtype} is not one of float16, bfloat16, float32")
+    return code
 
 
-def _ops_check(st: int):
+def _matrix(t, what: str) -> int:
+    """Row stride in elements of a CUDA matrix whose rows are contiguous (the rows themselves may lie apart)."""
+    if not t.is_cuda or t.dim() != 2:
+        _refuse(f"{what} must be a CUDA matrix")
+    rows, cols = t.shape
+    ld, inner = t.stride()
+    if inner != 1 and cols > 1:
+        _refuse(f"{what} must be contiguous along its columns")
+    return ld if rows > 1 else cols
+
+
+def _launch(fn, args, stream, tensors):
+    """Calls fn(*args, stream) with the tensors' device current; they must share it."""
+    import torch
+    device = tensors[0].device
+    for t in tensors:
+        if t is not None and t.device != device:
+            _refuse("tensors lie on different devices")
+    index = device.index
+    if stream is None:
+        raw = torch._C._cuda_getCurrentRawStream(index)
+    else:
+        if stream.device != device:
+            _refuse("the stream belongs to another device than the tensors")
+        raw = stream.cuda_stream
+    if torch._C._cuda_getDevice() == index:
+        st = fn(*args, raw)
+    else:
+        with torch.cuda.device(device):
+            st = fn(*args, raw)
     if st != DIT_OK:
         raise DitError(st, load_library().dit_status_string(st).decode())
 
@@ -649,145 +659,158 @@ def _data(t):
 def _codes_for(rows: int, cols: int, device):
     """Uninitialised e4m3 codes [rows, cols] whose rows start on 16-byte boundaries."""
     import torch
+    if cols % 16 == 0:
+        return torch.empty((rows, cols), dtype=torch.float8_e4m3fn, device=device)
     return torch.empty((rows, (cols + 15) // 16 * 16), dtype=torch.float8_e4m3fn, device=device)[:, :cols]
+
+
+def _pitch(ld: int, rows: int) -> int:
+    """Row stride of codes; a single row has none of its own, and any multiple of 16 describes it."""
+    return ld if rows > 1 else (ld + 15) // 16 * 16
 
 
 def dit_quantize_block128(x, codes=None, scales=None, stream=None):
     """x [rows, cols] fp16 / bf16 / fp32 -> (codes [rows, cols] float8_e4m3fn, scales [ceil(cols / 128), rows] fp32)."""
     import torch
-    lib, ld = load_library(), _matrix(x, "x")
+    lib, ld = _lib or load_library(), _matrix(x, "x")
     rows, cols = x.shape
     groups = (cols + BLOCK - 1) // BLOCK
     if codes is None:
         codes = _codes_for(rows, cols, x.device)
+    elif codes.dtype != torch.float8_e4m3fn or codes.shape != x.shape:
+        _refuse("codes must be float8_e4m3fn, shaped like x")
     if scales is None:
         scales = torch.empty((groups, rows), dtype=torch.float32, device=x.device)
-    _need(codes.dtype == torch.float8_e4m3fn and codes.shape == x.shape, "codes must be float8_e4m3fn, shaped like x")
-    _need(scales.dtype == torch.float32 and scales.shape == (groups, rows), "scales must be fp32 [ceil(cols / 128), rows]")
-    ld_codes, ld_scales = _matrix(codes, "codes"), _matrix(scales, "scales")
-    if rows <= 1:
-        ld_codes = (ld_codes + 15) // 16 * 16
-    with _on_device(stream, x, codes, scales) as s:
-        _ops_check(lib.dit_quantize_block128(_data(x), _type_code(x.dtype), ld, rows, cols, _data(codes), ld_codes, _data(scales), ld_scales, s))
+    elif scales.dtype != torch.float32 or scales.shape != (groups, rows):
+        _refuse("scales must be fp32 [ceil(cols / 128), rows]")
+    ld_scales = _matrix(scales, "scales")
+    _launch(lib.dit_quantize_block128, (x.data_ptr(), _type_code(x.dtype), ld, rows, cols, codes.data_ptr(), _pitch(_matrix(codes, "codes"), rows),
+                                        scales.data_ptr(), max(ld_scales, rows)), stream, (x, codes, scales))
     return codes, scales
 
 
 def dit_quantize_weight_block128(w, codes=None, scales=None, stream=None):
     """w [in, out] -> (codes [out, in] float8_e4m3fn, scales [ceil(out / 128), ceil(in / 128)] fp32)."""
     import torch
-    lib, ld = load_library(), _matrix(w, "w")
+    lib, ld = _lib or load_library(), _matrix(w, "w")
     n_in, n_out = w.shape
     shape = ((n_out + BLOCK - 1) // BLOCK, (n_in + BLOCK - 1) // BLOCK)
     if codes is None:
         codes = _codes_for(n_out, n_in, w.device)
+    elif codes.dtype != torch.float8_e4m3fn or codes.shape != (n_out, n_in):
+        _refuse("codes must be float8_e4m3fn [out, in]")
     if scales is None:
         scales = torch.empty(shape, dtype=torch.float32, device=w.device)
-    _need(codes.dtype == torch.float8_e4m3fn and codes.shape == (n_out, n_in), "codes must be float8_e4m3fn [out, in]")
-    _need(scales.dtype == torch.float32 and scales.shape == shape and scales.is_contiguous(),
-          "scales must be contiguous fp32 [ceil(out / 128), ceil(in / 128)]")
-    ld_codes = _matrix(codes, "codes")
-    if n_out <= 1:
-        ld_codes = (ld_codes + 15) // 16 * 16
-    with _on_device(stream, w, codes, scales) as s:
-        _ops_check(lib.dit_quantize_weight_block128(_data(w), _type_code(w.dtype), ld, n_in, n_out, _data(codes), ld_codes, _data(scales), s))
+    elif scales.dtype != torch.float32 or scales.shape != shape or not scales.is_contiguous():
+        _refuse("scales must be contiguous fp32 [ceil(out / 128), ceil(in / 128)]")
+    _launch(lib.dit_quantize_weight_block128, (w.data_ptr(), _type_code(w.dtype), ld, n_in, n_out, codes.data_ptr(),
+                                               _pitch(_matrix(codes, "codes"), n_out), scales.data_ptr()), stream, (w, codes, scales))
     return codes, scales
 
 
 def dit_gemm_block128(a, a_scales, b, b_scales, bias=None, out=None, out_dtype=None, stream=None):
     """a [m, k], b [n, k] float8_e4m3fn codes with their scales -> a b^T [m, n] (+ bias) in out_dtype (default fp16)."""
     import torch
-    lib = load_library()
+    lib = _lib or load_library()
     lda, ldb, ld_sa = _matrix(a, "a"), _matrix(b, "b"), _matrix(a_scales, "a_scales")
     m, k = a.shape
     n = b.shape[0]
     groups = (k + BLOCK - 1) // BLOCK
-    _need(a.dtype == torch.float8_e4m3fn and b.dtype == torch.float8_e4m3fn, "a and b must be float8_e4m3fn codes")
-    _need(b.shape[1] == k, "a and b differ in k")
-    _need(a_scales.dtype == torch.float32 and a_scales.shape == (groups, m), "a_scales must be fp32 [ceil(k / 128), m]")
-    _need(b_scales.dtype == torch.float32 and b_scales.is_contiguous() and b_scales.shape == ((n + BLOCK - 1) // BLOCK, groups),
-          "b_scales must be contiguous fp32 [ceil(n / 128), ceil(k / 128)]")
-    _need(bias is None or (bias.is_cuda and bias.dtype == torch.float32 and bias.is_contiguous() and bias.shape == (n,)), "bias must be contiguous fp32 [n]")
+    if a.dtype != torch.float8_e4m3fn or b.dtype != torch.float8_e4m3fn:
+        _refuse("a and b must be float8_e4m3fn codes")
+    if b.shape[1] != k:
+        _refuse("a and b differ in k")
+    if a_scales.dtype != torch.float32 or a_scales.shape != (groups, m):
+        _refuse("a_scales must be fp32 [ceil(k / 128), m]")
+    if b_scales.dtype != torch.float32 or not b_scales.is_contiguous() or b_scales.shape != ((n + BLOCK - 1) // BLOCK, groups):
+        _refuse("b_scales must be contiguous fp32 [ceil(n / 128), ceil(k / 128)]")
+    if bias is not None and (not bias.is_cuda or bias.dtype != torch.float32 or not bias.is_contiguous() or bias.shape != (n,)):
+        _refuse("bias must be contiguous fp32 [n]")
     if out is None:
         out = torch.empty((m, n), dtype=out_dtype or torch.float16, device=a.device)
-    _need(out.shape == (m, n) and (out_dtype is None or out.dtype == out_dtype), "out must be [m, n] of out_dtype")
-    if m <= 1:
-        lda = (lda + 15) // 16 * 16
-    if n <= 1:
-        ldb = (ldb + 15) // 16 * 16
-    args = DitGemmBlock128Args(_data(a), _data(a_scales), _data(b), _data(b_scales), _data(bias), _data(out), lda, ld_sa, ldb,
-                               _matrix(out, "out"), m, n, k, _type_code(out.dtype))
-    with _on_device(stream, a, a_scales, b, b_scales, bias, out) as s:
-        _ops_check(lib.dit_gemm_block128(C.byref(args), s))
+    elif out.shape != (m, n) or (out_dtype is not None and out.dtype != out_dtype):
+        _refuse("out must be [m, n] of out_dtype")
+    args = DitGemmBlock128Args(a.data_ptr(), a_scales.data_ptr(), b.data_ptr(), b_scales.data_ptr(), _data(bias), out.data_ptr(), _pitch(lda, m),
+                               max(ld_sa, m), _pitch(ldb, n), _matrix(out, "out"), m, n, k, _type_code(out.dtype))
+    _launch(lib.dit_gemm_block128, (C.byref(args),), stream, (a, a_scales, b, b_scales, bias, out))
     return out
 
 
 def _attention_batch(q, k, v, q_lens, kv_lens, n_heads):
     """(struct, number of query blocks); v may be None.  The arrays of lengths live as long as the struct does."""
     n = len(q_lens)
-    _need(len(kv_lens) == n, "q_lens and kv_lens differ in length")
-    rows = {"q": sum(q_lens), "k": sum(kv_lens), "v": sum(kv_lens)}
-    width = q.shape[-1]
-    _need(n_heads >= 1 and width % n_heads == 0, "the columns of q do not divide into n_heads")
-    for t, what in ((q, "q"), (k, "k"), (v, "v")):
-        if t is not None:
-            _need(t.dim() == 2 and t.shape == (rows[what], width), f"{what} must be [{rows[what]}, {width}]")
-            _need(t.dtype == q.dtype, "q, k and v differ in type")
-    lds = [0 if t is None else _matrix(t, what) for t, what in ((q, "q"), (k, "k"), (v, "v"))]
+    if len(kv_lens) != n:
+        _refuse("q_lens and kv_lens differ in length")
+    ld_q, ld_k, ld_v = _matrix(q, "q"), _matrix(k, "k"), 0 if v is None else _matrix(v, "v")
+    width, kv_rows = q.shape[1], sum(kv_lens)
+    if n_heads < 1 or width % n_heads:
+        _refuse("the columns of q do not divide into n_heads")
+    if q.shape[0] != sum(q_lens) or k.shape != (kv_rows, width) or (v is not None and v.shape != k.shape):
+        _refuse("q, k and v must be [sum of lengths, width]")
+    if k.dtype != q.dtype or (v is not None and v.dtype != q.dtype):
+        _refuse("q, k and v differ in type")
     lens = C.c_int32 * max(n, 1)
-    batch = DitAttentionBatch(_data(q), _data(k), _data(v), *lds, _type_code(q.dtype), n_heads, width // n_heads, n, lens(*q_lens), lens(*kv_lens))
-    return batch, sum((l + BLOCK - 1) // BLOCK for l in q_lens)
+    batch = DitAttentionBatch(q.data_ptr(), k.data_ptr(), _data(v), ld_q, ld_k, ld_v, _type_code(q.dtype), n_heads, width // n_heads, n,
+                              lens(*q_lens), lens(*kv_lens))
+    return batch, sum([(l + BLOCK - 1) // BLOCK for l in q_lens])
+
+
+def _check_lists(index, count, n_heads, q_blocks):
+    import torch
+    if not index.is_cuda or index.dtype != torch.int32 or not index.is_contiguous() or index.dim() != 3 or index.shape[:2] != (n_heads, q_blocks):
+        _refuse("block_index must be contiguous int32 [n_heads, query blocks, entries]")
+    if not count.is_cuda or count.dtype != torch.int32 or not count.is_contiguous() or count.shape != (n_heads, q_blocks):
+        _refuse("block_count must be contiguous int32 [n_heads, query blocks]")
 
 
 def dit_select_blocks(q, k, q_lens, kv_lens, n_heads: int, keep, tail_rows=None, index=None, count=None, workspace=None, stream=None):
     """q [sum q_lens, width], k [sum kv_lens, width] fp16 or bf16; keep, tail_rows: one whole number per request.
     -> (block_index [n_heads, query blocks, max keep] int32, block_count [n_heads, query blocks] int32)."""
     import torch
-    lib = load_library()
+    lib = _lib or load_library()
     batch, q_blocks = _attention_batch(q, k, None, q_lens, kv_lens, n_heads)
     n = len(q_lens)
-    _need(len(keep) == n and (tail_rows is None or len(tail_rows) == n), "keep and tail_rows need one number per request")
-    widest = max(keep, default=1)
+    if len(keep) != n or (tail_rows is not None and len(tail_rows) != n):
+        _refuse("keep and tail_rows need one number per request")
     if index is None:
-        _need(widest >= 1, "keep must be at least 1")
+        widest = max(keep, default=1)
+        if widest < 1:
+            _refuse("keep must be at least 1")
         index = torch.empty((n_heads, q_blocks, widest), dtype=torch.int32, device=q.device)
     if count is None:
         count = torch.empty((n_heads, q_blocks), dtype=torch.int32, device=q.device)
     _check_lists(index, count, n_heads, q_blocks)
-    size = lib.dit_select_blocks_workspace(C.byref(batch))
     if workspace is None:
-        workspace = torch.empty(max(size, 16), dtype=torch.uint8, device=q.device)
+        workspace = torch.empty(max(lib.dit_select_blocks_workspace(C.byref(batch)), 16), dtype=torch.uint8, device=q.device)
     ints = C.c_int32 * max(n, 1)
-    with _on_device(stream, q, k, index, count, workspace) as s:
-        _ops_check(lib.dit_select_blocks(C.byref(batch), ints(*keep), None if tail_rows is None else ints(*tail_rows), _data(index), _data(count),
-                                         index.shape[2], _data(workspace), workspace.numel() * workspace.element_size(), s))
+    _launch(lib.dit_select_blocks, (C.byref(batch), ints(*keep), None if tail_rows is None else ints(*tail_rows), index.data_ptr(), count.data_ptr(),
+                                    index.shape[2], workspace.data_ptr(), workspace.numel() * workspace.element_size()), stream,
+            (q, k, index, count, workspace))
     return index, count
-
-
-def _check_lists(index, count, n_heads, q_blocks):
-    import torch
-    _need(index.is_cuda and index.dtype == torch.int32 and index.is_contiguous() and index.dim() == 3 and index.shape[:2] == (n_heads, q_blocks),
-          "block_index must be contiguous int32 [n_heads, query blocks, entries]")
-    _need(count.is_cuda and count.dtype == torch.int32 and count.is_contiguous() and count.shape == (n_heads, q_blocks),
-          "block_count must be contiguous int32 [n_heads, query blocks]")
 
 
 def dit_block_attention(q, k, v, q_lens, kv_lens, n_heads: int, index, count, scale: float = 0.0, out=None, stream=None):
     """Attention of every query block over its listed key blocks -> out, shaped and typed like q."""
     import torch
-    lib = load_library()
+    lib = _lib or load_library()
+    if v is None:
+        _refuse("v is missing")
     batch, q_blocks = _attention_batch(q, k, v, q_lens, kv_lens, n_heads)
     _check_lists(index, count, n_heads, q_blocks)
     if out is None:
         out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    _need(out.shape == q.shape and out.dtype == q.dtype, "out must be shaped and typed like q")
-    with _on_device(stream, q, k, v, index, count, out) as s:
-        _ops_check(lib.dit_block_attention(C.byref(batch), _data(index), _data(count), max(index.shape[2], 1), scale, _data(out), _matrix(out, "out"), s))
+    elif out.shape != q.shape or out.dtype != q.dtype:
+        _refuse("out must be shaped and typed like q")
+    _launch(lib.dit_block_attention, (C.byref(batch), index.data_ptr(), count.data_ptr(), max(index.shape[2], 1), scale, out.data_ptr(),
+                                      _matrix(out, "out")), stream, (q, k, v, index, count, out))
     return out
 
 
 def dit_ops_poll_status():
     """Raises DIT_ERR_TIMEOUT when a wait of one of these operators has run out on the current device since the last call."""
-    _ops_check(load_library().dit_ops_poll_status())
+    st = load_library().dit_ops_poll_status()
+    if st != DIT_OK:
+        raise DitError(st, "a bounded wait of an operator ran out" if st == 7 else "")
 
 
 def context_for(dims, max_blocks: int, max_total_tokens: int, max_requests: int = 8, flags: int = 0) -> DitContext:

@@ -1,7 +1,7 @@
 // Attention over selected key blocks (128 rows each), and the selection by the product of block means.
 //
 // block_attention_kernel   256 query rows of a head per CTA on the tensor cores, for query blocks of many rows
-// block_rows_kernel        up to 4 query rows of a head per cluster on the FMA pipe, for a few rows that read a long context
+// block_rows_kernel        up to 16 query rows of a head per cluster, for a few rows that read a long context
 // block_means_kernel, block_select_kernel   the selector
 #pragma once
 #include "attention.cuh"
@@ -435,22 +435,27 @@ done:
 
 // ------------------------------------------------------------------------------------------------
 // Few query rows per request (a new token or two against a stored context).  Reading the selected K and V blocks once is the
-// bound; one row per key does not fill a tensor-core tile.  A cluster of CTAs shares a (request, head): rank r takes
-// every splits-th selected block.  K and V tiles arrive by TMA in swizzled panels; warp w works on keys 32 w .. 32 w + 31 of
-// every tile on its own: lane = key for the scores (16-byte reads of 32 different rows, free of bank conflicts thanks
-// to the swizzle), lane = four (two) channels for P V, running maximum and sum per warp.  The warps' results
-// meet in shared memory, the CTAs' through distributed shared memory, in rank and warp order.
+// bound, and 16 rows or fewer do not fill a tensor-memory tile: the products are warp-level 16 x 8 x 16 ones, which
+// cost the same for one row as for sixteen (on the FMA pipe one row took 550 instructions per 64 keys and warp and
+// issue was the bound; this form takes about 150).  A cluster of CTAs shares a (request, head): rank r takes every splits-th selected
+// block.  K and V arrive by TMA as tiles of 64 keys in swizzled panels through one ring (K, V, K, V, ...), five of
+// six tiles in flight per CTA and two CTAs per SM.  Warp w works on keys 16 w .. 16 w + 15 of every tile on its
+// own, with its own running maximum and sum per row: the accumulator layout of the scores is the operand layout of
+// the second product, so probabilities stay in registers.  The warps' results meet in shared memory (the ring's,
+// once everything has been read), the CTAs' through distributed shared memory, in rank and warp order.
 // ------------------------------------------------------------------------------------------------
+constexpr int kRowsTile = 64;                  // keys per tile
+constexpr int kRowsMax = 16;                   // query rows
 template <int D>
 struct BlockRowsCfg {
-  static constexpr int NP = D / 64, PANEL = 128 * 128, TILE_BYTES = NP * PANEL;
-  static constexpr int K_STAGES = 2, V_STAGES = 1 * (128 / D);                   // 96 KB (d = 128), 64 KB (d = 64)
-  static constexpr int OFF_K = 0, OFF_V = K_STAGES * TILE_BYTES, OFF_BAR = OFF_V + V_STAGES * TILE_BYTES;
-  static constexpr int OFF_BITS = OFF_BAR + 128;                                 // uint32 [kMaxKeyBlocks / 32]
-  static constexpr int OFF_Q = OFF_BITS + kMaxKeyBlocks / 8;                     // float [4][D]
-  static constexpr int OFF_PART = OFF_Q + 4 * D * 4;                             // float [4 warps][4 rows][D + 2]
-  static constexpr int SMEM_BYTES = OFF_PART + 16 * (D + 2) * 4 + 1024;
+  static constexpr int NP = D / 64, PANEL = kRowsTile * 128, TILE_BYTES = NP * PANEL;
+  static constexpr int STAGES = 96 * 1024 / TILE_BYTES;                          // 6 (d = 128), 12 (d = 64)
+  static constexpr int OFF_BAR = STAGES * TILE_BYTES;
+  static constexpr int OFF_BITS = OFF_BAR + 256;                                 // uint32 [kMaxKeyBlocks / 32]
+  static constexpr int SMEM_BYTES = OFF_BITS + kMaxKeyBlocks / 8 + 1024;
   static constexpr int THREADS = 160;                                            // four key warps and a producer
+  static constexpr int PART = D + 2;                                             // floats of a row's partial result: channels, maximum, sum
+  static_assert(4 * kRowsMax * PART * 4 <= OFF_BAR, "the partial results take the ring's place");
   static_assert(2 * SMEM_BYTES <= 227 * 1024, "two CTAs per SM");
 };
 
@@ -460,8 +465,8 @@ __device__ __forceinline__ float2 widen2(uint32_t w) {
   return __half22float2(*reinterpret_cast<const __half2*>(&w));
 }
 
-template <int D, bool BF16, int R>
-__global__ void __launch_bounds__(BlockRowsCfg<D>::THREADS)
+template <int D, bool BF16>
+__global__ void __launch_bounds__(BlockRowsCfg<D>::THREADS, 2)
 block_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const BlockAttnParams p, const uint16_t* q,
                   const long long ld_q, const __grid_constant__ BlockBatch batch, const int splits) {
   using C = BlockRowsCfg<D>;
@@ -470,33 +475,35 @@ block_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
   const uint32_t base = (raw + 1023u) & ~1023u;
   uint8_t* aligned = smem_raw + (base - raw);
   const uint32_t bar0 = base + C::OFF_BAR;
-  auto k_full = [&](int s) { return bar0 + 8u * s; };
-  auto k_empty = [&](int s) { return bar0 + 8u * (2 + s); };
-  auto v_full = [&](int s) { return bar0 + 8u * (4 + s); };
-  auto v_empty = [&](int s) { return bar0 + 8u * (6 + s); };
-  volatile int* abort_flag = reinterpret_cast<volatile int*>(aligned + C::OFF_BAR + 64);
+  auto full = [&](int s) { return bar0 + 8u * s; };
+  auto empty = [&](int s) { return bar0 + 8u * (C::STAGES + s); };
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(aligned + C::OFF_BAR + 16 * C::STAGES);
   uint32_t* bits = reinterpret_cast<uint32_t*>(aligned + C::OFF_BITS);
-  float* qs = reinterpret_cast<float*>(aligned + C::OFF_Q);
-  float* part = reinterpret_cast<float*>(aligned + C::OFF_PART);
+  float* part = reinterpret_cast<float*>(aligned);                      // [4 warps][kRowsMax][PART], after the main loop
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int rank = splits > 1 ? static_cast<int>(cluster_ctarank()) : 0;
   const int item = blockIdx.x / splits, head = item % p.n_heads, req = item / p.n_heads;
-  const int q_begin = batch.cu_q[req], rows = batch.cu_q[req + 1] - q_begin;      // 0 .. R
+  const int q_begin = batch.cu_q[req], rows = batch.cu_q[req + 1] - q_begin;      // 0 .. kRowsMax
   const int kv_begin = batch.cu_kv[req], kv_len = batch.cu_kv[req + 1] - kv_begin;
   const int n_kv = (kv_len + 127) >> 7, words = (n_kv + 31) >> 5;
 
   for (int i = threadIdx.x; i < words; i += C::THREADS) bits[i] = 0;
-  for (int i = threadIdx.x; i < R * D; i += C::THREADS) {
-    const int r = i / D;
-    uint32_t v = 0;
-    if (r < rows) v = q[(static_cast<long long>(q_begin) + r) * ld_q + head * D + i % D];
-    qs[i] = widen2<BF16>(v).x;
-  }
   if (threadIdx.x == 0) {
-    for (int s = 0; s < 2; ++s) { mbar_init(k_full(s), 1); mbar_init(k_empty(s), 4); mbar_init(v_full(s), 1); mbar_init(v_empty(s), 4); }
+    for (int s = 0; s < C::STAGES; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 4); }
     *abort_flag = 0;
     fence_mbar_init();
+  }
+  // Q as the first operand: k step t, rows lane / 4 and + 8, channels 16 t + 2 (lane % 4) and + 8; absent rows are zero
+  uint32_t qa[D / 16][4];
+  if (warp < 4) {
+#pragma unroll
+    for (int t = 0; t < D / 16; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int r = (lane >> 2) + (i & 1) * 8, c = t * 16 + (lane & 3) * 2 + (i >> 1) * 8;
+        qa[t][i] = r < rows ? *reinterpret_cast<const uint32_t*>(q + (static_cast<long long>(q_begin) + r) * ld_q + head * D + c) : 0u;
+      }
   }
   __syncthreads();
   if (rows > 0) {
@@ -510,141 +517,149 @@ block_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
   }
   __syncthreads();
 
-  float m[R], l[R];                            // per warp: running maximum (of score * scale * log2 e), per-lane sum
-  constexpr int CPL = D / 32;                  // channels per lane: 4 or 2
-  float acc[R][CPL];
+  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};               // rows lane / 4 and + 8; l: this lane's columns only
+  float acc[D / 8][4];
 #pragma unroll
-  for (int r = 0; r < R; ++r) {
-    m[r] = -INFINITY; l[r] = 0.f;
+  for (int i = 0; i < D / 8; ++i)
 #pragma unroll
-    for (int i = 0; i < CPL; ++i) acc[r][i] = 0.f;
-  }
+    for (int k = 0; k < 4; ++k) acc[i][k] = 0.f;
   bool ok = true;
   if (warp == 4) {
     // ------------------------------------------------------------------ producer
     if (lane == 0) {
-      int ks = 0, vs = 0, turn = 0; uint32_t kph = 1, vph = 1;
+      int stage = 0, turn = 0; uint32_t phase = 1;
       for (int w = 0; w < words && ok; ++w)
         for (uint32_t b = bits[w]; b && ok; b &= b - 1) {
           if (turn++ % splits != rank) continue;
-          const int y = kv_begin + (w * 32 + __ffs(b) - 1) * 128;
-          if (!(ok = mbar_wait(k_empty(ks), kph, abort_flag))) break;
-          mbar_arrive_expect_tx(k_full(ks), C::TILE_BYTES);
-          for (int pn = 0; pn < C::NP; ++pn) tma_load_2d(base + C::OFF_K + ks * C::TILE_BYTES + pn * C::PANEL, &tmK, head * D + pn * 64, y, k_full(ks));
-          if (++ks == C::K_STAGES) { ks = 0; kph ^= 1u; }
-          if (!(ok = mbar_wait(v_empty(vs), vph, abort_flag))) break;
-          mbar_arrive_expect_tx(v_full(vs), C::TILE_BYTES);
-          for (int pn = 0; pn < C::NP; ++pn) tma_load_2d(base + C::OFF_V + vs * C::TILE_BYTES + pn * C::PANEL, &tmV, head * D + pn * 64, y, v_full(vs));
-          if (++vs == C::V_STAGES) { vs = 0; vph ^= 1u; }
+          const int y = (w * 32 + __ffs(b) - 1) * 128;
+          for (int t = 0; t < 4 && ok; ++t) {                           // K, V of the first 64 keys, K, V of the rest if there is one
+            const int y0 = y + (t >> 1) * kRowsTile;
+            if (y0 >= kv_len) break;
+            if (!(ok = mbar_wait(empty(stage), phase, abort_flag))) break;
+            mbar_arrive_expect_tx(full(stage), C::TILE_BYTES);
+            for (int pn = 0; pn < C::NP; ++pn)
+              tma_load_2d(base + stage * C::TILE_BYTES + pn * C::PANEL, (t & 1) ? &tmV : &tmK, head * D + pn * 64, kv_begin + y0, full(stage));
+            if (++stage == C::STAGES) { stage = 0; phase ^= 1u; }
+          }
         }
     }
   } else {
-    // ------------------------------------------------------------------ keys 32 * warp .. + 31 of every tile
-    int ks = 0, vs = 0, turn = 0; uint32_t kph = 0, vph = 0;
+    // ------------------------------------------------------------------ keys 16 * warp .. + 15 of every tile
+    int stage = 0, turn = 0; uint32_t phase = 0;
+    // row addresses of the ldmatrix loads: of K, matrices (keys 0-7 | 8-15) x (channels 0-7, 8-15 of a k step); of V, transposed,
+    // (channels 0-7 | 8-15 of a pair of output tiles) x (keys 0-7, 8-15)
+    const int k_row = 16 * warp + (lane >> 4) * 8 + (lane & 7), k_unit = (lane >> 3) & 1;
+    const int v_row = 16 * warp + ((lane >> 3) & 1) * 8 + (lane & 7), v_unit = lane >> 4;
     for (int w = 0; w < words && ok; ++w)
       for (uint32_t b = bits[w]; b && ok; b &= b - 1) {
         if (turn++ % splits != rank) continue;
-        const int keys = min(32, kv_len - (w * 32 + __ffs(b) - 1) * 128 - 32 * warp);    // of this warp (may be <= 0)
-        if (!(ok = __all_sync(0xffffffffu, mbar_wait(k_full(ks), kph, abort_flag)))) break;
-        float s[R];
+        for (int y0 = (w * 32 + __ffs(b) - 1) * 128, half = 0; half < 2 && y0 < kv_len; ++half, y0 += kRowsTile) {
+          const int keys = kv_len - y0 - 16 * warp;                     // of this warp: 16 or more, or the rest (may be <= 0)
+          if (!(ok = __all_sync(0xffffffffu, mbar_wait(full(stage), phase, abort_flag)))) break;
+          float s[2][4] = {};                                           // keys 0-7 and 8-15
+          {
+            const uint32_t kt = base + stage * C::TILE_BYTES + k_row * 128;
 #pragma unroll
-        for (int r = 0; r < R; ++r) s[r] = 0.f;
-        {
-          const int row = 32 * warp + lane;
-          const uint8_t* kt = aligned + C::OFF_K + ks * C::TILE_BYTES + row * 128;
-#pragma unroll 4
-          for (int u = 0; u < D / 8; ++u) {
-            const uint4 k4 = *reinterpret_cast<const uint4*>(kt + (u >> 3) * C::PANEL + (((u & 7) ^ (row & 7)) << 4));
-            const float2 k0 = widen2<BF16>(k4.x), k1 = widen2<BF16>(k4.y), k2 = widen2<BF16>(k4.z), k3 = widen2<BF16>(k4.w);
-#pragma unroll
-            for (int r = 0; r < R; ++r) {
-              const float4 qa = *reinterpret_cast<const float4*>(qs + r * D + u * 8), qb = *reinterpret_cast<const float4*>(qs + r * D + u * 8 + 4);
-              s[r] = fmaf(qa.x, k0.x, s[r]); s[r] = fmaf(qa.y, k0.y, s[r]); s[r] = fmaf(qa.z, k1.x, s[r]); s[r] = fmaf(qa.w, k1.y, s[r]);
-              s[r] = fmaf(qb.x, k2.x, s[r]); s[r] = fmaf(qb.y, k2.y, s[r]); s[r] = fmaf(qb.z, k3.x, s[r]); s[r] = fmaf(qb.w, k3.y, s[r]);
+            for (int t = 0; t < D / 16; ++t) {
+              const int u = 2 * t + k_unit;
+              uint32_t kb[4];
+              ldmatrix_x4(kb, kt + (u >> 3) * C::PANEL + (((u & 7) ^ (k_row & 7)) << 4));
+              mma_16816<BF16>(s[0], qa[t], kb[0], kb[1]);
+              mma_16816<BF16>(s[1], qa[t], kb[2], kb[3]);
             }
           }
-        }
-        __syncwarp();
-        if (lane == 0) mbar_arrive(k_empty(ks));
-        if (++ks == C::K_STAGES) { ks = 0; kph ^= 1u; }
-        float pr[R];
+          __syncwarp();
+          if (lane == 0) mbar_arrive(empty(stage));
+          if (++stage == C::STAGES) { stage = 0; phase ^= 1u; }
+          if (keys < 16) {                                              // drop the scores behind the request's last key
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-          const float x = lane < keys ? s[r] * p.scale_log2 : -INFINITY;
-          float mx = x;
+            for (int i = 0; i < 2; ++i)
 #pragma unroll
-          for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-          const float top = fmaxf(m[r], mx), at = top == -INFINITY ? 0.f : top;
-          const float alpha = exp2_approx(m[r] - at);                  // 0 while m is -inf
-          pr[r] = lane < keys ? exp2_approx(x - at) : 0.f;
-          l[r] = l[r] * alpha + pr[r];
-          m[r] = top;
+              for (int k = 0; k < 4; ++k)
+                if (8 * i + 2 * (lane & 3) + (k & 1) >= keys) s[i][k] = -INFINITY;
+          }
+          uint32_t pa[4];
 #pragma unroll
-          for (int i = 0; i < CPL; ++i) acc[r][i] *= alpha;
-        }
-        if (!(ok = __all_sync(0xffffffffu, mbar_wait(v_full(vs), vph, abort_flag)))) break;
-        {
-          // channels CPL * lane ..: 16-byte unit (lane * CPL) / 8 of the row, swizzled by the row
-          const int ch = lane * CPL, panel = ch / 64, unit = (ch % 64) / 8, in = (ch % 8) * 2;
-          const uint8_t* vt = aligned + C::OFF_V + vs * C::TILE_BYTES + panel * C::PANEL + in;
-#pragma unroll 8
-          for (int k = 0; k < keys; ++k) {
-            const int row = 32 * warp + k;
-            const uint8_t* at = vt + row * 128 + ((unit ^ (row & 7)) << 4);
-            float v[CPL];
-            if constexpr (CPL == 4) {
-              const uint2 t = *reinterpret_cast<const uint2*>(at);
-              const float2 a = widen2<BF16>(t.x), c = widen2<BF16>(t.y);
-              v[0] = a.x; v[1] = a.y; v[2] = c.x; v[3] = c.y;
-            } else {
-              const float2 a = widen2<BF16>(*reinterpret_cast<const uint32_t*>(at));
-              v[0] = a.x; v[1] = a.y;
-            }
+          for (int r = 0; r < 2; ++r) {                                 // rows lane / 4 + 8 r
+            float mx = fmaxf(fmaxf(s[0][2 * r], s[0][2 * r + 1]), fmaxf(s[1][2 * r], s[1][2 * r + 1]));
+            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+            const float top = fmaxf(m[r], mx * p.scale_log2), at = top == -INFINITY ? 0.f : top;
+            const float alpha = exp2_approx(m[r] - at);                 // 0 while m is -inf
+            m[r] = top;
+            float e[4];
 #pragma unroll
-            for (int r = 0; r < R; ++r) {
-              const float pk = __shfl_sync(0xffffffffu, pr[r], k);
+            for (int k = 0; k < 4; ++k) e[k] = exp2_approx(fmaf(s[k >> 1][2 * r + (k & 1)], p.scale_log2, -at));
+            l[r] = l[r] * alpha + (e[0] + e[1]) + (e[2] + e[3]);
+            pa[r] = pack16x2<BF16>(e[0], e[1]);
+            pa[2 + r] = pack16x2<BF16>(e[2], e[3]);
+            if (__any_sync(0xffffffffu, alpha != 1.0f)) {
 #pragma unroll
-              for (int i = 0; i < CPL; ++i) acc[r][i] = fmaf(pk, v[i], acc[r][i]);
+              for (int i = 0; i < D / 8; ++i) { acc[i][2 * r] *= alpha; acc[i][2 * r + 1] *= alpha; }
             }
           }
+          if (!(ok = __all_sync(0xffffffffu, mbar_wait(full(stage), phase, abort_flag)))) break;
+          if (keys < 16) {                                              // clear the V rows behind it: they may hold anything
+            for (int i = lane; i < 16 * 8; i += 32)
+              if ((i >> 3) >= keys)
+                for (int pn = 0; pn < C::NP; ++pn)
+                  *reinterpret_cast<uint4*>(aligned + stage * C::TILE_BYTES + pn * C::PANEL + (16 * warp * 8 + i) * 16) = make_uint4(0, 0, 0, 0);
+            fence_proxy_async_smem();                                   // the stage is refilled by TMA
+            __syncwarp();
+          }
+          {
+            const uint32_t vt = base + stage * C::TILE_BYTES + v_row * 128;
+#pragma unroll
+            for (int t = 0; t < D / 16; ++t) {
+              const int u = 2 * t + v_unit;
+              uint32_t vb[4];
+              ldmatrix_x4_trans(vb, vt + (u >> 3) * C::PANEL + (((u & 7) ^ (v_row & 7)) << 4));
+              mma_16816<BF16>(acc[2 * t], pa, vb[0], vb[1]);
+              mma_16816<BF16>(acc[2 * t + 1], pa, vb[2], vb[3]);
+            }
+          }
+          __syncwarp();
+          if (lane == 0) mbar_arrive(empty(stage));
+          if (++stage == C::STAGES) { stage = 0; phase ^= 1u; }
         }
-        __syncwarp();
-        if (lane == 0) mbar_arrive(v_empty(vs));
-        if (++vs == C::V_STAGES) { vs = 0; vph ^= 1u; }
       }
+  }
+  __syncthreads();                             // every tile has been read: the partial results take the ring's place
+  if (warp < 4) {
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
+    for (int r = 0; r < 2; ++r) {
+      l[r] += __shfl_xor_sync(0xffffffffu, l[r], 1);
+      l[r] += __shfl_xor_sync(0xffffffffu, l[r], 2);
+      const int row = (lane >> 2) + 8 * r;
+      if (row < rows) {
+        float* dst = part + (warp * kRowsMax + row) * C::PART;
 #pragma unroll
-      for (int o = 16; o > 0; o >>= 1) l[r] += __shfl_xor_sync(0xffffffffu, l[r], o);
-      float* dst = part + (warp * R + r) * (D + 2);
-#pragma unroll
-      for (int i = 0; i < CPL; ++i) dst[lane * CPL + i] = acc[r][i];
-      if (lane == 0) { dst[D] = m[r]; dst[D + 1] = l[r]; }
+        for (int i = 0; i < D / 8; ++i) *reinterpret_cast<float2*>(dst + i * 8 + (lane & 3) * 2) = make_float2(acc[i][2 * r], acc[i][2 * r + 1]);
+        if ((lane & 3) == 0) { dst[D] = m[r]; dst[D + 1] = l[r]; }
+      }
     }
   }
   __syncwarp();
   if (splits > 1) cluster_sync_all(); else __syncthreads();
-  if (rank == 0 && threadIdx.x < 128) {
-    // row after row, channel per thread: the parts rescaled to their common maximum
-    for (int r = 0; r < rows; ++r) {
+  if (threadIdx.x < D) {
+    // rank's share of the rows, channel per thread: the parts rescaled to their common maximum
+    for (int row = rank; row < rows; row += splits) {
       auto read = [&](int s, int w, int i) {
-        const float* at = part + (w * R + r) * (D + 2) + i;
+        const float* at = part + (w * kRowsMax + row) * C::PART + i;
         return splits > 1 ? ld_cluster_f32(map_to_cta(smem_u32(at), s)) : *at;
       };
-      float top = -INFINITY;
+      float ref = -INFINITY, sum = 0.f, o = 0.f;
       for (int s = 0; s < splits; ++s)
-        for (int w = 0; w < 4; ++w) top = fmaxf(top, read(s, w, D));
-      const float ref = top == -INFINITY ? 0.f : top;
-      for (int ch = threadIdx.x; ch < D; ch += 128) {
-        float sum = 0.f, o = 0.f;
-        for (int s = 0; s < splits; ++s)
-          for (int w = 0; w < 4; ++w) {
-            const float f = exp2_approx(read(s, w, D) - ref);
-            sum = fmaf(f, read(s, w, D + 1), sum);
-            o = fmaf(f, read(s, w, ch), o);
-          }
-        static_cast<uint16_t*>(p.out)[(static_cast<long long>(q_begin) + r) * p.ld_out + head * D + ch] = pack16<BF16>(sum == 0.f ? 0.f : o / sum);
-      }
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          const float pm = read(s, w, D), pl = read(s, w, D + 1), po = read(s, w, threadIdx.x);
+          const float top = fmaxf(ref, pm), at = top == -INFINITY ? 0.f : top;
+          const float keep = exp2_approx(ref - at), f = exp2_approx(pm - at);
+          sum = sum * keep + pl * f;
+          o = o * keep + po * f;
+          ref = top;
+        }
+      static_cast<uint16_t*>(p.out)[(static_cast<long long>(q_begin) + row) * p.ld_out + head * D + threadIdx.x] = pack16<BF16>(sum == 0.f ? 0.f : o / sum);
     }
   }
   __syncwarp();
@@ -656,14 +671,13 @@ block_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
 // Selector.  Means of the 128-row blocks of q and k in 64 bits (the sum of 128 fp16 values is exact there, and of bf16
 // values too unless their magnitudes are more than 2^38 apart), then their products in 64 bits: the order of two scores is decided by
 // their values and not by an order of summation, so lists do not change with the batch or the launch.
-// The means of k are stored transposed, [column][key block], as the products read them.
 // ------------------------------------------------------------------------------------------------
 struct BlockSelectParams {
   const uint16_t *q, *k;
   long long ld_q, ld_k;
   int width, n_heads, head_dim;
   double* q_mean;            // [query blocks, width]
-  double* k_mean;            // [width, key blocks]
+  double* k_mean;            // [key blocks, width]
   int* index;
   int* count;
   long long ld_index;
@@ -672,12 +686,27 @@ struct BlockSelectParams {
   int keep[DIT_MAX_REQUESTS], tail[DIT_MAX_REQUESTS];
 };
 
+// 16 bytes, read once by this kernel (volatile: the loads of a batch stay together in front of their uses).
+__device__ __forceinline__ uint4 load_stream(const void* p) {
+  uint4 v;
+  asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+  return v;
+}
+
+template <bool BF16>
+__device__ __forceinline__ double widen_double(uint16_t h) {
+  double d;
+  if (BF16) return static_cast<double>(__uint_as_float(static_cast<uint32_t>(h) << 16));
+  asm("cvt.f64.f16 %0, %1;" : "=d"(d) : "h"(h));
+  return d;
+}
+
 // One CTA per (block, 256 columns): eight warps take every eighth row, a lane 16 bytes of it.  Bound by reading q and k once.
 template <bool BF16>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(256, 3)
 block_means_kernel(const BlockSelectParams p, const __grid_constant__ BlockBatch batch) {
   __shared__ double sums[8][256];
-  const int q_blocks = batch.first_qblock[batch.n], k_blocks = batch.first_kblock[batch.n];
+  const int q_blocks = batch.first_qblock[batch.n];
   const int chunks = (p.width + 255) / 256;
   int block = blockIdx.x / chunks;
   const int col0 = blockIdx.x % chunks * 256;
@@ -698,21 +727,19 @@ block_means_kernel(const BlockSelectParams p, const __grid_constant__ BlockBatch
 #pragma unroll
   for (int i = 0; i < 8; ++i) acc[i] = 0.0;
   if (col < p.width) {
+    {
+      uint4 v[16];                             // all sixteen rows of the lane are requested before the first is used
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      uint4 v[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int r = warp + 8 * (8 * h + i);
-        v[i] = r < n ? __ldg(reinterpret_cast<const uint4*>(src + r * ld)) : make_uint4(0, 0, 0, 0);
+      for (int i = 0; i < 16; ++i) {
+        const int r = warp + 8 * i;
+        v[i] = r < n ? load_stream(src + r * ld) : make_uint4(0, 0, 0, 0);
       }
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
+      for (int i = 0; i < 16; ++i) {
         const uint32_t u[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
-          const float2 f = widen2<BF16>(u[c]);
-          acc[2 * c] += static_cast<double>(f.x); acc[2 * c + 1] += static_cast<double>(f.y);
+          acc[2 * c] += widen_double<BF16>(static_cast<uint16_t>(u[c])); acc[2 * c + 1] += widen_double<BF16>(static_cast<uint16_t>(u[c] >> 16));
         }
       }
     }
@@ -726,8 +753,7 @@ block_means_kernel(const BlockSelectParams p, const __grid_constant__ BlockBatch
 #pragma unroll
     for (int w = 0; w < 8; ++w) s += sums[w][threadIdx.x];
     s /= static_cast<double>(n);
-    if (is_k) p.k_mean[static_cast<long long>(mine) * k_blocks + block] = s;
-    else p.q_mean[static_cast<long long>(block) * p.width + mine] = s;
+    (is_k ? p.k_mean : p.q_mean)[static_cast<long long>(block) * p.width + mine] = s;
   }
 }
 
@@ -738,17 +764,18 @@ __device__ __forceinline__ unsigned long long score_key(double s) {
   return (u >> 63) ? ~u : (u | 0x8000000000000000ull);
 }
 
-// One CTA per (head, up to four query blocks of a request): every thread scores key blocks against the four rows, then a
-// warp per row finds the keep-th largest score by deciding its bits from the top (counting the scores that reach
-// the candidate; most rows are decided after a few bits, when exactly `keep` do) and writes the list in order.
-constexpr int kSelectRows = 4;
+// One CTA per (head, up to eight query blocks of a request).  Scores: 8 x 8 x 4 products in 64 bits, a warp per eight key
+// blocks (a thread per key block on the FMA pipe took three times as long, most of it in operand reads).  Lists: a
+// warp per row finds the keep-th largest score by deciding its bits from the top (counting the scores that reach the
+// candidate), starting at the first bit in which the row's scores differ and ending as soon as exactly `keep` reach it.
+constexpr int kSelectRows = 8, kSelectThreads = 256, kSelectPitch = 130;   // pitch: rows four banks apart
 
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(kSelectThreads, 4)
 block_select_kernel(const BlockSelectParams p, const __grid_constant__ BlockBatch batch) {
   extern __shared__ __align__(16) uint8_t smem_raw[];
-  double* qm = reinterpret_cast<double*>(smem_raw);                              // [head_dim][kSelectRows]
-  unsigned long long* keys = reinterpret_cast<unsigned long long*>(smem_raw + 128 * kSelectRows * 8);   // [rows][n_kv]
-  const int q_blocks = batch.first_qblock[batch.n], k_blocks = batch.first_kblock[batch.n];
+  double* qm = reinterpret_cast<double*>(smem_raw);                              // [kSelectRows][kSelectPitch]
+  unsigned long long* keys = reinterpret_cast<unsigned long long*>(qm + kSelectRows * kSelectPitch);   // [rows][n_kv]
+  const int q_blocks = batch.first_qblock[batch.n];
   int head = 0, group = blockIdx.x, req = 0;
   for (req = 0; req < batch.n; ++req) {
     const int groups = (batch.first_qblock[req + 1] - batch.first_qblock[req] + p.rows - 1) / p.rows;
@@ -759,35 +786,66 @@ block_select_kernel(const BlockSelectParams p, const __grid_constant__ BlockBatc
   const int kb0 = batch.first_kblock[req], n_kv = batch.first_kblock[req + 1] - kb0;
   const int kv_len = batch.cu_kv[req + 1] - batch.cu_kv[req];
   const int d = p.head_dim;
-  for (int i = threadIdx.x; i < d * kSelectRows; i += 256) {
-    const int r = i % kSelectRows, c = i / kSelectRows;
-    qm[i] = r < n_rows ? p.q_mean[static_cast<long long>(qb0 + r) * p.width + head * d + c] : 0.0;
+  for (int i = threadIdx.x; i < d * kSelectRows; i += kSelectThreads) {
+    const int r = i / d, c = i % d;
+    qm[r * kSelectPitch + c] = r < n_rows ? p.q_mean[static_cast<long long>(qb0 + r) * p.width + head * d + c] : 0.0;
   }
   __syncthreads();
-  for (int j = threadIdx.x; j < n_kv; j += 256) {
-    double s[kSelectRows];
+  {
+    const int lane = threadIdx.x & 31, row = lane >> 2, col = lane & 3;
+    const double* qa = qm + row * kSelectPitch + col;
+    for (int j0 = (threadIdx.x >> 5) * 8; j0 < n_kv; j0 += kSelectThreads / 32 * 8) {
+      const bool there = j0 + row < n_kv;                                        // this lane's key block as an operand
+      const double* km = p.k_mean + static_cast<long long>(kb0 + (there ? j0 + row : 0)) * p.width + head * d + col;
+      double s[2][2] = {};
+      for (int c0 = 0; c0 < d; c0 += 64) {
+        double k[16];
 #pragma unroll
-    for (int r = 0; r < kSelectRows; ++r) s[r] = 0.0;
-    const double* km = p.k_mean + static_cast<long long>(head * d) * k_blocks + kb0 + j;
-#pragma unroll 8
-    for (int c = 0; c < d; ++c) {
-      const double k = __ldg(km + static_cast<long long>(c) * k_blocks);
+        for (int i = 0; i < 16; ++i) k[i] = __ldg(km + c0 + 4 * i);
 #pragma unroll
-      for (int r = 0; r < kSelectRows; ++r) s[r] = fma(qm[c * kSelectRows + r], k, s[r]);
+        for (int i = 0; i < 16; ++i) mma_884_f64(s[i & 1], qa[c0 + 4 * i], k[i]);
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {                                              // score of (row, key block j)
+        const int j = j0 + 2 * col + i;
+        if (j < n_kv && row < n_rows) {
+          const bool forced = p.tail[req] > 0 && static_cast<long long>(j + 1) * 128 > static_cast<long long>(kv_len) - p.tail[req];
+          keys[static_cast<long long>(row) * n_kv + j] = forced ? ~0ull : score_key(s[0][i] + s[1][i]);
+        }
+      }
     }
-    const bool forced = p.tail[req] > 0 && static_cast<long long>(j + 1) * 128 > static_cast<long long>(kv_len) - p.tail[req];
-#pragma unroll
-    for (int r = 0; r < kSelectRows; ++r)
-      if (r < n_rows) keys[static_cast<long long>(r) * n_kv + j] = forced ? ~0ull : score_key(s[r]);
   }
   __syncthreads();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (warp >= n_rows) return;
   const unsigned long long* mine = keys + static_cast<long long>(warp) * n_kv;
   const int want = min(p.keep[req], n_kv);
-  unsigned long long least = 0;                // keys >= least: at least `want`
-  int reach = n_kv;                            // how many they are
-  for (int bit = 63; bit >= 0 && reach != want; --bit) {
+  unsigned long long high = 0, low = ~0ull;
+  for (int j = lane; j < n_kv; j += 32) { high = max(high, mine[j]); low = min(low, mine[j]); }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    high = max(high, __shfl_xor_sync(0xffffffffu, high, o));
+    low = min(low, __shfl_xor_sync(0xffffffffu, low, o));
+  }
+  const int first_bit = n_kv > 0 ? 63 - __clzll(static_cast<long long>(high ^ low)) : -1;   // -1: all alike
+  unsigned long long least = first_bit < 63 ? (high >> (first_bit + 1)) << (first_bit + 1) : 0ull;   // keys >= least: at least `want`
+  int reach = n_kv, bit = first_bit;           // how many they are; the next bit to decide
+  constexpr int kHeld = 8;
+  if (n_kv <= 32 * kHeld) {
+    // the upper 32 bits nearly always decide: they are held in registers for that part
+    uint32_t top[kHeld];
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) top[i] = i * 32 + lane < n_kv ? static_cast<uint32_t>(mine[i * 32 + lane] >> 32) : 0u;
+    for (; bit >= 32 && reach != want; --bit) {
+      const uint32_t candidate = static_cast<uint32_t>(least >> 32) | (1u << (bit - 32));
+      int n = 0;
+#pragma unroll
+      for (int i = 0; i < kHeld; ++i)
+        if (i * 32 < n_kv) n += __popc(__ballot_sync(0xffffffffu, top[i] >= candidate));
+      if (n >= want) { least = static_cast<unsigned long long>(candidate) << 32; reach = n; }
+    }
+  }
+  for (; bit >= 0 && reach != want; --bit) {
     const unsigned long long candidate = least | (1ull << bit);
     int n = 0;
     for (int j = lane; j < n_kv; j += 32) n += mine[j] >= candidate ? 1 : 0;

@@ -148,7 +148,7 @@ struct QuantWeightParams {
 };
 
 template <int kType, bool kVec>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(256, kType == 2 ? 3 : 4)
 quantize_weight_block128_kernel(const QuantWeightParams p) {
   using In = QuantIn<kType>;
   constexpr int COLS = 8, VECS = COLS / In::EPL;                  // 16-byte loads per eight columns: 1 (16-bit) or 2 (fp32)
@@ -158,7 +158,7 @@ quantize_weight_block128_kernel(const QuantWeightParams p) {
   const int k0 = gk * 128, n0 = gn * 128;
   const int c = threadIdx.x & 15, rq = threadIdx.x >> 4;          // columns n0 + 8c .., rows k0 + 4 rq + 64 i + j
   const typename In::Elem* src = static_cast<const typename In::Elem*>(p.w);
-  float v[2][4][COLS];
+  uint4 raw[2][4][VECS];                                          // as loaded: half the registers of the widened values
   uint32_t top = 0;
 #pragma unroll
   for (int i = 0; i < 2; ++i)
@@ -166,25 +166,30 @@ quantize_weight_block128_kernel(const QuantWeightParams p) {
     for (int j = 0; j < 4; ++j) {
       const int k = k0 + 4 * rq + 64 * i + j, n = n0 + 8 * c;
       const typename In::Elem* at = src + static_cast<long long>(k) * p.ld + n;
-      if (kVec && k < p.in_dim && n + COLS <= p.out_dim) {
 #pragma unroll
-        for (int q = 0; q < VECS; ++q) {
-          float t[In::EPL];
-          In::widen16(__ldg(reinterpret_cast<const uint4*>(at) + q), t);
+      for (int q = 0; q < VECS; ++q) {
+        raw[i][j][q] = make_uint4(0, 0, 0, 0);
+        if (kVec && k < p.in_dim && n + COLS <= p.out_dim) {
+          raw[i][j][q] = __ldg(reinterpret_cast<const uint4*>(at) + q);
+        } else if (k < p.in_dim) {
+          typename In::Elem part[In::EPL];
 #pragma unroll
-          for (int e = 0; e < In::EPL; ++e) v[i][j][q * In::EPL + e] = t[e];
+          for (int e = 0; e < In::EPL; ++e) part[e] = n + q * In::EPL + e < p.out_dim ? at[q * In::EPL + e] : typename In::Elem(0);
+          memcpy(&raw[i][j][q], part, 16);
         }
-      } else {
-#pragma unroll
-        for (int e = 0; e < COLS; ++e) v[i][j][e] = (k < p.in_dim && n + e < p.out_dim) ? In::widen(at[e]) : 0.f;
       }
     }
+  auto value = [&](int i, int j, int e) {                         // column n0 + 8c + e of row k0 + 4 rq + 64 i + j
+    float t[In::EPL];
+    In::widen16(raw[i][j][e / In::EPL], t);
+    return t[e % In::EPL];
+  };
 #pragma unroll
   for (int i = 0; i < 2; ++i)
 #pragma unroll
     for (int j = 0; j < 4; ++j)
 #pragma unroll
-      for (int e = 0; e < COLS; ++e) top = max(top, __float_as_uint(v[i][j][e]) & 0x7FFFFFFFu);
+      for (int e = 0; e < COLS; ++e) top = max(top, __float_as_uint(value(i, j, e)) & 0x7FFFFFFFu);
   top = __reduce_max_sync(0xffffffffu, top);
   if ((threadIdx.x & 31) == 0) warp_top[threadIdx.x >> 5] = top;
   __syncthreads();
@@ -198,7 +203,7 @@ quantize_weight_block128_kernel(const QuantWeightParams p) {
 #pragma unroll
     for (int e = 0; e < COLS; ++e) {
       const int n = 8 * c + e, kq = rq + 16 * i;
-      turned[n * 32 + (kq ^ (2 * c))] = e4m3x2(v[i][0][e] * inv, v[i][1][e] * inv) | (e4m3x2(v[i][2][e] * inv, v[i][3][e] * inv) << 16);
+      turned[n * 32 + (kq ^ (2 * c))] = e4m3x2(value(i, 0, e) * inv, value(i, 1, e) * inv) | (e4m3x2(value(i, 2, e) * inv, value(i, 3, e) * inv) << 16);
     }
   __syncthreads();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;

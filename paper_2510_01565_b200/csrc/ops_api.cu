@@ -21,9 +21,9 @@ typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t,
 
 constexpr int kMaxDevices = 64;
 constexpr int64_t kMaxSize = INT32_MAX - 1024;
-// selecting kernel: means of four query blocks, then the scores of one to four rows
-constexpr int kSelectFixedSmem = 128 * kSelectRows * 8;
-constexpr int kSelectSmemMax = kSelectFixedSmem + kMaxKeyBlocks * 8 + 32 * 1024;
+// selecting kernel: means of eight query blocks, then the scores of one to eight rows
+constexpr int kSelectFixedSmem = kSelectRows * kSelectPitch * 8;
+constexpr int kSelectSmemMax = kSelectFixedSmem + kMaxKeyBlocks * 8;
 
 // One status word per device, for waits that ran out.  In host code its name is a handle; the device
 // address is looked up once per device, with that device current.
@@ -55,9 +55,7 @@ cudaError_t allow_gemm() {
 template <int D, bool BF16>
 cudaError_t allow_attention() {
   cudaError_t e = allow_smem(&block_attention_kernel<D, BF16>, BlockAttnCfg<D>::SMEM_BYTES);
-  if (e == cudaSuccess) e = allow_smem(&block_rows_kernel<D, BF16, 1>, BlockRowsCfg<D>::SMEM_BYTES);
-  if (e == cudaSuccess) e = allow_smem(&block_rows_kernel<D, BF16, 2>, BlockRowsCfg<D>::SMEM_BYTES);
-  if (e == cudaSuccess) e = allow_smem(&block_rows_kernel<D, BF16, 4>, BlockRowsCfg<D>::SMEM_BYTES);
+  if (e == cudaSuccess) e = allow_smem(&block_rows_kernel<D, BF16>, BlockRowsCfg<D>::SMEM_BYTES);
   return e;
 }
 
@@ -140,11 +138,11 @@ bool out_map(CUtensorMap* m, const BlockProduct& b) {
                   CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// 16-bit matrix [rows, cols] with row stride ld: boxes of 64 columns x 128 rows, 128-byte swizzle, zeros outside.
-bool half_map(CUtensorMap* m, const void* ptr, uint64_t cols, uint64_t rows, uint64_t ld) {
+// 16-bit matrix [rows, cols] with row stride ld: boxes of 64 columns x box_rows rows, 128-byte swizzle, zeros outside.
+bool half_map(CUtensorMap* m, const void* ptr, uint64_t cols, uint64_t rows, uint64_t ld, uint32_t box_rows = 128) {
   const cuuint64_t dims[2] = {cols, rows};
   const cuuint64_t strides[1] = {ld * 2};
-  const cuuint32_t box[2] = {64, 128};
+  const cuuint32_t box[2] = {64, box_rows};
   const cuuint32_t estr[2] = {1, 1};
   return g_encode(m, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, const_cast<void*>(ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
@@ -181,7 +179,7 @@ dit_status plan_batch(const dit_attention_batch* a, bool values, BlockBatch* b) 
   return DIT_OK;
 }
 
-template <int D, bool BF16, int R>
+template <int D, bool BF16>
 cudaError_t launch_rows(const CUtensorMap& tmK, const CUtensorMap& tmV, const BlockAttnParams& p, const dit_attention_batch& a, const BlockBatch& b,
                         int splits, cudaStream_t st) {
   cudaLaunchConfig_t lc = {};
@@ -191,7 +189,7 @@ cudaError_t launch_rows(const CUtensorMap& tmK, const CUtensorMap& tmV, const Bl
   at.id = cudaLaunchAttributeClusterDimension;
   at.val.clusterDim.x = splits; at.val.clusterDim.y = 1; at.val.clusterDim.z = 1;
   lc.attrs = &at; lc.numAttrs = splits > 1 ? 1 : 0;
-  return cudaLaunchKernelEx(&lc, &block_rows_kernel<D, BF16, R>, tmK, tmV, p, static_cast<const uint16_t*>(a.q), static_cast<long long>(a.ld_q), b, splits);
+  return cudaLaunchKernelEx(&lc, &block_rows_kernel<D, BF16>, tmK, tmV, p, static_cast<const uint16_t*>(a.q), static_cast<long long>(a.ld_q), b, splits);
 }
 
 template <int D, bool BF16>
@@ -209,17 +207,19 @@ cudaError_t launch_attend(const DeviceState& d, const dit_attention_batch& a, co
   // without keys nothing is loaded; the maps still have to describe some memory
   const void* k = kv_rows > 0 ? a.k : a.q;
   const void* v = kv_rows > 0 ? a.v : a.q;
-  if (!half_map(&tmQ, a.q, width, q_rows, a.ld_q) || !half_map(&tmK, k, width, std::max(kv_rows, 1), kv_rows > 0 ? a.ld_k : a.ld_q) ||
-      !half_map(&tmV, v, width, std::max(kv_rows, 1), kv_rows > 0 ? a.ld_v : a.ld_q))
+  const uint32_t box = most <= kRowsMax ? kRowsTile : 128;
+  if (!half_map(&tmQ, a.q, width, q_rows, a.ld_q) || !half_map(&tmK, k, width, std::max(kv_rows, 1), kv_rows > 0 ? a.ld_k : a.ld_q, box) ||
+      !half_map(&tmV, v, width, std::max(kv_rows, 1), kv_rows > 0 ? a.ld_v : a.ld_q, box))
     return cudaErrorInvalidValue;
-  if (most <= 4) {
-    // a cluster of CTAs per (request, head): as many as two CTAs per SM hold, no more than there are blocks to share
+  if (most <= kRowsMax) {
+    // A cluster of CTAs per (request, head): the largest power of two with which all are resident at once, two CTAs per
+    // SM, and no more than there are blocks to share (96 items, 16 blocks each: 1, 2, 3, 4 CTAs 27, 20, 27, 27 us; clusters
+    // of three do not pack into the SMs' clusters, four of 96 need a second wave).
     const int items = b.n * a.n_heads;
     const long long listed = std::min<long long>(longest, p.ld_index);
-    const int splits = static_cast<int>(std::max<long long>(1, std::min<long long>({8, 2ll * d.num_sms / items, listed})));
-    if (most <= 1) return launch_rows<D, BF16, 1>(tmK, tmV, p, a, b, splits, st);
-    if (most <= 2) return launch_rows<D, BF16, 2>(tmK, tmV, p, a, b, splits, st);
-    return launch_rows<D, BF16, 4>(tmK, tmV, p, a, b, splits, st);
+    int splits = 1;
+    while (splits < 8 && 2 * splits <= listed && 2ll * splits * items <= 2ll * d.num_sms) splits *= 2;
+    return launch_rows<D, BF16>(tmK, tmV, p, a, b, splits, st);
   }
   block_attention_kernel<D, BF16><<<static_cast<unsigned>(qblocks) * a.n_heads, BlockAttnCfg<D>::THREADS, BlockAttnCfg<D>::SMEM_BYTES, st>>>(tmQ, tmK, tmV, p, b);
   return cudaGetLastError();
@@ -308,7 +308,7 @@ cudaError_t launch_select(const dit_attention_batch& a, const BlockBatch& b, Blo
   if (e != cudaSuccess) return e;
   unsigned groups = 0;
   for (int r = 0; r < b.n; ++r) groups += (b.first_qblock[r + 1] - b.first_qblock[r] + p.rows - 1) / p.rows;
-  block_select_kernel<<<groups * a.n_heads, 256, kSelectFixedSmem + static_cast<size_t>(p.rows) * longest * 8, st>>>(p, b);
+  block_select_kernel<<<groups * a.n_heads, kSelectThreads, kSelectFixedSmem + static_cast<size_t>(p.rows) * longest * 8, st>>>(p, b);
   return cudaGetLastError();
 }
 
