@@ -104,6 +104,18 @@ typedef struct {
  * the flag cannot be combined with the other three, and two-stream blocks are refused. */
 #define DIT_FLAG_BF16_OPERANDS 8u
 
+/* e4m3 operands with one scale for each block of 128, the finer-grained sibling of DIT_FLAG_FP8_GEMM: the four GEMMs of a
+ * block (three of a parallel one) take left operands quantised in groups of 128 columns of a row and weights
+ * quantised in blocks of 128 x 128 at load time, as dit_quantize_block128 and dit_quantize_weight_block128 (dit_ops.h) do, and
+ * scale each block's partial sum in fp32.  A channel so much louder than the others that
+ * they sink to the format's subnormal codes then costs precision in its own 128 columns only, not in the whole row.  Everything else stays as it is.  Plain sequential and parallel
+ * blocks only: the flag cannot be combined with the other GEMM or QK flags, and two-stream blocks are refused.
+ * (Bit 4 is not assigned.) */
+#define DIT_FLAG_FP8_BLOCK128 32u
+/* Attention over selected key blocks (dit_select_blocks and dit_block_attention of dit_ops.h) instead of all of them; off until
+ * dit_ctx_set_sparse_attention asks for less than everything.  Combines with every other flag and block form. */
+#define DIT_FLAG_SPARSE_ATTENTION 64u
+
 /* One request of the paper's problem statement (Section 3): an image resolution, a position in
  * its denoising schedule and the diffusion time of this step.  Image tokens = (height/16) *
  * (width/16) (Section 6.1: L = H*W/16^2; Table 1: 256/1024/4096/16384 for 256^2..2048^2). */
@@ -137,6 +149,14 @@ size_t dit_workspace_bytes(const dit_config *cfg);
  * DIT_ERR_UNSUPPORTED_ARCH on anything but sm_100 (there is no fallback path). */
 dit_status dit_ctx_create(const dit_config *cfg, void *workspace, size_t workspace_bytes, dit_ctx **out);
 dit_status dit_ctx_destroy(dit_ctx *ctx);
+
+/* For contexts created with DIT_FLAG_SPARSE_ATTENTION: from the next step on, every block of 128 query rows of a request with n
+ * blocks of 128 keys attends to max(min_blocks, ceil(keep * n)) of them (all n at most), chosen per head by the
+ * product of the blocks' mean query and mean key.  A request's text rows are always among the chosen keys (as far as
+ * they fit) where the call knows them, i.e. in dit_step_forward_requests, dit_denoise_step and dit_denoise_round.  0 < keep <= 1,
+ * min_blocks >= 1; keep == 1, the state after creation, is the dense step bit for bit, and so is any step in
+ * which every request keeps all of its blocks.  Timing counts selection and attention together as attention. */
+dit_status dit_ctx_set_sparse_attention(dit_ctx *ctx, float keep, int32_t min_blocks);
 
 /* Copies block `block_idx`'s ten tensors into the context (weights are re-laid out as fp16
  * [out, in] for the tensor-core kernels, biases widened to fp32).  Asynchronous on `stream`; the

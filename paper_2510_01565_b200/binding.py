@@ -20,12 +20,14 @@ DIT_FLAG_QK_RMSNORM = 1
 DIT_FLAG_ROPE_2D = 2
 DIT_FLAG_FP8_GEMM = 4
 DIT_FLAG_BF16_OPERANDS = 8
+DIT_FLAG_FP8_BLOCK128 = 32
+DIT_FLAG_SPARSE_ATTENTION = 64
 STATUS_NAMES = ["DIT_OK", "DIT_ERR_INVALID_ARG", "DIT_ERR_SHAPE", "DIT_ERR_CAPACITY", "DIT_ERR_NOT_LOADED",
                 "DIT_ERR_UNSUPPORTED_ARCH", "DIT_ERR_CUDA", "DIT_ERR_TIMEOUT", "DIT_ERR_INTERNAL"]
 KERNEL_KINDS = ["modulation", "ln_modulate", "gemm_qkv", "attention", "gemm_proj", "gemm_fc1", "gemm_fc2", "quantize"]
 TAPS = {"h": 0, "qkv": 1, "attn": 2, "u": 3, "mod": 4, "stream": 5}
 
-EXPORTS = ["dit_workspace_bytes", "dit_ctx_create", "dit_ctx_destroy", "dit_load_block_weights", "dit_load_parallel_block_weights", "dit_load_dual_block_weights",
+EXPORTS = ["dit_workspace_bytes", "dit_ctx_create", "dit_ctx_destroy", "dit_ctx_set_sparse_attention", "dit_load_block_weights", "dit_load_parallel_block_weights", "dit_load_dual_block_weights",
            "dit_pack_requests", "dit_pack_tokens", "dit_step_forward", "dit_step_forward_requests", "dit_step_forward_host", "dit_step_forward_host_async", "dit_host_wait",
            "dit_ctx_poll_status", "dit_debug_tap", "dit_debug_poison", "dit_debug_check_guards", "dit_debug_expire_wait", "dit_debug_clock_probe", "dit_ctx_set_timing", "dit_ctx_read_timing", "dit_modulation_noalloc",
            "dit_load_shell_weights", "dit_timestep_cond", "dit_embed_latents", "dit_final_layer", "dit_sampler_update",
@@ -109,6 +111,8 @@ def load_library() -> C.CDLL:
     lib.dit_ctx_create.argtypes = [C.POINTER(DitConfig), vp, C.c_size_t, C.POINTER(vp)]
     lib.dit_ctx_destroy.restype = C.c_int
     lib.dit_ctx_destroy.argtypes = [vp]
+    lib.dit_ctx_set_sparse_attention.restype = C.c_int
+    lib.dit_ctx_set_sparse_attention.argtypes = [vp, C.c_float, i32]
     lib.dit_load_block_weights.restype = C.c_int
     lib.dit_load_block_weights.argtypes = [vp, i32, C.POINTER(DitBlockWeights), vp]
     lib.dit_load_dual_block_weights.restype = C.c_int
@@ -328,6 +332,10 @@ class DitContext:
             assert t.is_cuda and t.dtype == self.torch.bfloat16 and t.is_contiguous(), name
             setattr(w, name, t.data_ptr())
         return w
+
+    def dit_ctx_set_sparse_attention(self, keep: float, min_blocks: int = 1):
+        """Share of the key blocks every query block attends to from now on (needs DIT_FLAG_SPARSE_ATTENTION; 1 = all)."""
+        self._check(self.lib.dit_ctx_set_sparse_attention(self.handle, keep, min_blocks))
 
     def dit_load_block_weights(self, block_idx: int, weights: Dict[str, "object"], stream=None):
         """weights: name -> CUDA bf16 tensor, [in, out] row-major; biases may be None."""

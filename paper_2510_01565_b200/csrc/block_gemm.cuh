@@ -33,6 +33,7 @@ struct BlockGemmParams {
   int vec_out;               // rows of out start on 16-byte boundaries
   int* status;
   // kBlkGateResidF32 only (row strides of resid and out are ld_out)
+  int row0;                  // packed row index of row 0 (a launch may cover a slice of the batch's rows)
   const float* resid;
   const float* gate;         // gate vector of request 0; request r at gate + r * gate_stride
   long long gate_stride;
@@ -77,7 +78,7 @@ __device__ __forceinline__ void block_store_chunk(const BlockGemmParams& p, cons
             float4 a = *reinterpret_cast<const float4*>(st + (rr & 15) * 36 + cg);
             const long long at = (row0 + rr) * p.ld_out + col0 + cg;
             if (EPI == kBlkGateResidF32) {
-              const int req = find_request(seq, static_cast<int>(row0) + rr);
+              const int req = find_request(seq, p.row0 + static_cast<int>(row0) + rr);
               const float4 g = __ldg(reinterpret_cast<const float4*>(p.gate + req * p.gate_stride + col0 + cg));
               const float4 x = *reinterpret_cast<const float4*>(p.resid + at);
               const float2 o0 = ffma2(make_float2(g.x, g.y), make_float2(a.x, a.y), make_float2(x.x, x.y));
@@ -90,7 +91,11 @@ __device__ __forceinline__ void block_store_chunk(const BlockGemmParams& p, cons
       } else if (col0 + lane < p.N) {
         for (int r = 0; r < 16; ++r) {
           const int rr = hf * 16 + r;
-          if ((rows_ok >> rr) & 1u) out[(row0 + rr) * p.ld_out + col0 + lane] = st[r * 36 + lane];
+          if (!((rows_ok >> rr) & 1u)) continue;
+          const long long at = (row0 + rr) * p.ld_out + col0 + lane;
+          float v1 = st[r * 36 + lane];
+          if (EPI == kBlkGateResidF32) v1 = fmaf(p.gate[find_request(seq, p.row0 + static_cast<int>(row0) + rr) * p.gate_stride + col0 + lane], v1, p.resid[at]);
+          out[at] = v1;
         }
       }
       __syncwarp();
@@ -382,7 +387,7 @@ __device__ __forceinline__ void block_store_one(const BlockGemmParams& p, const 
   else if constexpr (EPI == kBlkBF16) static_cast<uint16_t*>(p.out)[at] = pack16<true>(v);
   else if constexpr (EPI == kBlkGeluF16) static_cast<uint16_t*>(p.out)[at] = pack16<false>(gelu_tanh_f32(v));
   else if constexpr (EPI == kBlkF32) static_cast<float*>(p.out)[at] = v;
-  else static_cast<float*>(p.out)[at] = fmaf(p.gate[find_request(seq, row) * p.gate_stride + col], v, p.resid[at]);
+  else static_cast<float*>(p.out)[at] = fmaf(p.gate[find_request(seq, p.row0 + row) * p.gate_stride + col], v, p.resid[at]);
 }
 
 template <int EPI, int BT>

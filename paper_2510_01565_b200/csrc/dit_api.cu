@@ -12,6 +12,8 @@
 #include "common.cuh"
 #include "elementwise.cuh"
 #include "gemm.cuh"
+#include "block_gemm.cuh"
+#include "ops_launch.h"
 #include "shell.cuh"
 
 using namespace dit;
@@ -43,6 +45,8 @@ struct Layout {
   size_t row_scale;    // per-row scales of the e4m3 activations (DIT_FLAG_FP8_GEMM)
   size_t q8, row_scale2;   // e4m3 codes [T, H + F] and row scales of the operands quantised by a pass of their own
                            // (attention output, GELU output, or both side by side); empty without DIT_FLAG_FP8_GEMM
+  size_t blk_scale;    // DIT_FLAG_FP8_BLOCK128: scales of the quantised operand in q8, [ceil((H + F) / 128), T]
+  size_t sp_means, sp_index, sp_count;   // DIT_FLAG_SPARSE_ATTENTION: the selector's workspace and lists
   size_t items;        // two-stream launches: [0] item count, then per-tile flags, then the items
   // test hooks: 1 KiB guard areas after the activation regions, and the [begin, end) ranges that
   // dit_debug_poison fills
@@ -66,11 +70,19 @@ bool config_ok(const dit_config* c) {
   if (c->cond_dim < 1 || c->cond_dim > kMaxCondDim) return false;
   if (c->max_blocks < 1 || c->max_total_tokens < 1) return false;
   if (c->max_requests < 1 || c->max_requests > DIT_MAX_REQUESTS) return false;
-  if (!(c->ln_eps >= 0.f) || (c->flags & ~static_cast<uint32_t>(DIT_FLAG_QK_RMSNORM | DIT_FLAG_ROPE_2D | DIT_FLAG_FP8_GEMM | DIT_FLAG_BF16_OPERANDS))) return false;
+  if (!(c->ln_eps >= 0.f) || (c->flags & ~static_cast<uint32_t>(DIT_FLAG_QK_RMSNORM | DIT_FLAG_ROPE_2D | DIT_FLAG_FP8_GEMM | DIT_FLAG_BF16_OPERANDS |
+                                                              DIT_FLAG_FP8_BLOCK128 | DIT_FLAG_SPARSE_ATTENTION)))
+    return false;
   // the bf16-operand mode is built for the plain sequential and parallel blocks only
   if ((c->flags & DIT_FLAG_BF16_OPERANDS) && (c->flags & (DIT_FLAG_QK_RMSNORM | DIT_FLAG_ROPE_2D | DIT_FLAG_FP8_GEMM))) return false;
+  // so is the block-scaled e4m3 mode
+  if ((c->flags & DIT_FLAG_FP8_BLOCK128) && (c->flags & (DIT_FLAG_QK_RMSNORM | DIT_FLAG_ROPE_2D | DIT_FLAG_FP8_GEMM | DIT_FLAG_BF16_OPERANDS))) return false;
   return true;
 }
+
+inline size_t blocks_of(size_t n) { return (n + DIT_BLOCK - 1) / DIT_BLOCK; }
+// Query or key blocks that a batch within the context's capacity can have: every request may end in a short one.
+inline size_t max_batch_blocks(const dit_config& c) { return static_cast<size_t>(c.max_total_tokens) / DIT_BLOCK + c.max_requests; }
 
 Layout make_layout(const dit_config& c) {
   const size_t H = c.hidden, F = c.mlp_hidden, C = c.cond_dim, T = c.max_total_tokens, R = c.max_requests;
@@ -94,7 +106,8 @@ Layout make_layout(const dit_config& c) {
   L.blk.s_qkv = take(3 * H * 4);
   L.blk.s_fc1 = take(F * 4);
   L.blk.s_o = take(H * 4);
-  L.blk.s_fc2 = take(H * 4);
+  // one scale per output channel, or (DIT_FLAG_FP8_BLOCK128) per 128 x 128 block: fewer, except for very wide MLPs
+  L.blk.s_fc2 = take((c.flags & DIT_FLAG_FP8_BLOCK128) ? std::max(H, blocks_of(H) * blocks_of(H + F)) * 4 : H * 4);
   L.blk.bytes = o;
   o = 0;
   // every activation region (or run of regions) is followed by a guard area and is listed as a poison range
@@ -142,8 +155,17 @@ Layout make_layout(const dit_config& c) {
   L.row_scale = take(T * 4);
   const bool fp8_mode = (c.flags & DIT_FLAG_FP8_GEMM) != 0;
   L.row_scale2 = take(fp8_mode ? T * 4 : 0);
-  L.q8 = take(fp8_mode ? T * (H + F) : 0);
+  const bool block_mode = (c.flags & DIT_FLAG_FP8_BLOCK128) != 0, sparse_mode = (c.flags & DIT_FLAG_SPARSE_ATTENTION) != 0;
+  L.q8 = take(fp8_mode || block_mode ? T * (H + F) : 0);
+  L.blk_scale = take(block_mode ? blocks_of(H + F) * T * 4 : 0);
   guard(L.row_scale);
+  if (sparse_mode) {
+    const size_t nb = max_batch_blocks(c);
+    L.sp_means = take(2 * nb * H * 8);
+    L.sp_index = take(c.n_heads * nb * blocks_of(T) * 4);
+    L.sp_count = take(c.n_heads * nb * 4);
+    guard(L.sp_means);
+  }
   L.items = take((16 + 3 * (T / (2 * 128) + 2)) * 4);
   L.bytes = o;
   return L;
@@ -176,6 +198,8 @@ struct dit_ctx {
   CUtensorMap tm_wout;                     // W_out^T, fp16 [kWoutRows, H]
   CUtensorMap tm_wada;                     // every block's W_ada as one 3-D tensor [max_blocks, C, 6H] bf16, boxes of 10 x 256
   bool tm_wada_ok;
+  float sparse_keep;                       // DIT_FLAG_SPARSE_ATTENTION: share of the key blocks that a query block keeps, 1 = all
+  int sparse_min_blocks;
   bool attn_probe;                         // test hook: attention CTAs record the SM clock they ran at
   ActMaps maps;                            // valid for batch length maps_T (-1: none yet)
   int maps_T;
@@ -384,6 +408,7 @@ dit_status step_impl(dit_ctx* ctx, const void* tokens, const int32_t* lens, int 
   if (!build_seq(lens, n, &seq)) return fail(ctx, DIT_ERR_INVALID_ARG, "every request needs at least one token");
   const bool qk_variant = (c.flags & (DIT_FLAG_QK_RMSNORM | DIT_FLAG_ROPE_2D)) != 0;
   const bool fp8 = (c.flags & DIT_FLAG_FP8_GEMM) != 0;     // QKV and up-projection read e4m3 h and weights
+  const bool blk8 = (c.flags & DIT_FLAG_FP8_BLOCK128) != 0; // all four GEMMs read operands quantised in blocks of 128
   const bool bf = (c.flags & DIT_FLAG_BF16_OPERANDS) != 0; // h, qkv, a, u and the weights are bf16 instead of fp16
   if ((c.flags & DIT_FLAG_ROPE_2D) && !geo)
     return fail(ctx, DIT_ERR_INVALID_ARG, "the rotary term needs the requests' geometry: use dit_step_forward_requests");
@@ -430,6 +455,8 @@ dit_status step_impl(dit_ctx* ctx, const void* tokens, const int32_t* lens, int 
     return cudaGetLastError();
   };
 
+  float* blk_scale = ctx->at<float>(ctx->lay.blk_scale);
+
   int64_t launches = 0;
   const long long req_stride = static_cast<long long>(n_blocks) * 6 * H;
   // Runs one launch; with timing enabled, brackets it with a pair of events on the stream.
@@ -454,15 +481,70 @@ dit_status step_impl(dit_ctx* ctx, const void* tokens, const int32_t* lens, int 
     return cudaEventRecord(ctx->ev_pool[2 * i + 1], st);
   };
 
+  // Block-scaled mode: quantises `src` [T, K] into q8 (which holds one operand at a time), and multiplies rows
+  // [r0, r0 + rows) of it with a weight of block `wb`.  `g` carries bias, gate and residual as for the other GEMMs.
+  auto quantise_blocks = [&](const __half* src, long long ld, int K) -> dit_status {
+    DIT_CUDA_TRY(ctx, timed(DIT_KERNEL_QUANTIZE, [&] { return launch_quantize_rows(src, DIT_TYPE_F16, ld, T, K, q8, K, blk_scale, T, st); }));
+    return DIT_OK;
+  };
+  auto block_product = [&](int kind, const uint8_t* wb, size_t w_off, size_t s_off, const GemmParams& g, int epilogue, void* dst, long long ld_dst,
+                           int r0, int rows) -> dit_status {
+    BlockProduct bp{};
+    bp.a = q8 + static_cast<size_t>(r0) * g.K; bp.lda = g.K;
+    bp.a_scales = blk_scale + r0; bp.ld_a_scales = T;
+    bp.b = wb + w_off; bp.ldb = g.K; bp.b_scales = reinterpret_cast<const float*>(wb + s_off);
+    bp.bias = g.bias; bp.out = dst; bp.ld_out = ld_dst;
+    bp.m = rows; bp.plan_m = T; bp.n = g.N; bp.k = g.K; bp.epilogue = epilogue;
+    bp.row0 = r0; bp.resid = g.resid; bp.gate = g.gate; bp.gate_stride = g.gate_stride;
+    DIT_CUDA_TRY(ctx, timed(kind, [&] { return launch_block_product(bp, seq, st); }));
+    return DIT_OK;
+  };
+
+  // Attention over selected key blocks: how many each request's query blocks keep.  Where every request keeps all of
+  // its blocks the dense kernel runs.
+  int32_t sp_keep[DIT_MAX_REQUESTS], sp_tail[DIT_MAX_REQUESTS];
+  int sp_widest = 0;
+  bool sparse = false;
+  if ((c.flags & DIT_FLAG_SPARSE_ATTENTION) && ctx->sparse_keep < 1.0f) {
+    for (int r = 0; r < n; ++r) {
+      const int blocks = static_cast<int>(blocks_of(lens[r]));
+      const int share = static_cast<int>(std::ceil(static_cast<double>(ctx->sparse_keep) * blocks));
+      sp_keep[r] = std::min(blocks, std::max({1, share, ctx->sparse_min_blocks}));
+      sp_tail[r] = geo ? lens[r] - (geo->img_cu[r + 1] - geo->img_cu[r]) : 0;       // text rows
+      sp_widest = std::max(sp_widest, sp_keep[r]);
+      if (sp_keep[r] < blocks) sparse = true;
+    }
+  }
+  auto sparse_attention = [&](__half* dst, long long ld_dst) -> dit_status {
+    dit_attention_batch ab{};
+    ab.q = qkv; ab.k = qkv + H; ab.v = qkv + 2 * H;
+    ab.ld_q = ab.ld_k = ab.ld_v = 3 * H;
+    ab.type = bf ? DIT_TYPE_BF16 : DIT_TYPE_F16;
+    ab.n_heads = c.n_heads; ab.head_dim = c.head_dim; ab.n_requests = n; ab.q_lens = lens; ab.kv_lens = lens;
+    int32_t* index = ctx->at<int32_t>(ctx->lay.sp_index);
+    int32_t* count = ctx->at<int32_t>(ctx->lay.sp_count);
+    dit_status s = DIT_OK;
+    DIT_CUDA_TRY(ctx, timed(DIT_KERNEL_ATTENTION, [&] {
+      s = dit_select_blocks(&ab, sp_keep, sp_tail, index, count, sp_widest, ctx->at<void>(ctx->lay.sp_means), dit_select_blocks_workspace(&ab), st);
+      if (s == DIT_OK) s = dit_block_attention(&ab, index, count, sp_widest, 0.f, dst, ld_dst, st);
+      return cudaSuccess;
+    }));
+    launches += 2;                               // two kernels select, one attends
+    return s == DIT_OK ? DIT_OK : fail(ctx, s, "attention over selected blocks");
+  };
+
   // The gated-residual GEMM that writes `out`, sliced by rows when the result goes to the host.  A slice is a
   // whole number of 256-row tiles; every output element is computed exactly as in the unsliced launch.
   // In the e4m3 mode A is the quantised copy q8 (1 byte per element) and g carries the row and column scales.
+  const uint8_t* last_wb = nullptr;              // block-scaled mode: the last block and the offset of its output projection
+  size_t last_w = 0;
   auto last_gemm = [&](const __half* a_ptr, int K, const CUtensorMap& tmA_full, const CUtensorMap& tmB, const GemmParams& g) -> dit_status {
     auto launch = [&](const CUtensorMap& tmA, const GemmParams& q) {
       return fp8 ? launch_gemm<kEpiGateResidF32, 0, false, true>(ctx, tmA, tmB, q, seq, st)
                  : launch_gemm<kEpiGateResidF32>(ctx, tmA, tmB, q, seq, st);
     };
     if (!host_out) {
+      if (blk8) return block_product(DIT_KERNEL_GEMM_FC2, last_wb, last_w, ctx->lay.blk.s_fc2, g, kBlkGateResidF32, g.out32, g.N, 0, T);
       DIT_CUDA_TRY(ctx, timed(DIT_KERNEL_GEMM_FC2, [&] { return launch(tmA_full, g); }));
       return DIT_OK;
     }
@@ -473,7 +555,7 @@ dit_status step_impl(dit_ctx* ctx, const void* tokens, const int32_t* lens, int 
     for (int sidx = 0, r0 = 0; r0 < T; ++sidx, r0 += per) {
       const int rows = std::min(per, T - r0);
       CUtensorMap tmA;
-      if (!(fp8 ? make_map8(ctx, &tmA, q8 + static_cast<size_t>(r0) * K, K, rows, gemm_cfg::BM)
+      if (!blk8 && !(fp8 ? make_map8(ctx, &tmA, q8 + static_cast<size_t>(r0) * K, K, rows, gemm_cfg::BM)
                 : make_map(ctx, &tmA, a_ptr + static_cast<size_t>(r0) * K, K, rows, gemm_cfg::BM)))
         return fail(ctx, DIT_ERR_CUDA, "cuTensorMapEncodeTiled failed for an activation buffer");
       GemmParams q = g;
@@ -481,7 +563,12 @@ dit_status step_impl(dit_ctx* ctx, const void* tokens, const int32_t* lens, int 
       q.resid = g.resid + static_cast<size_t>(r0) * g.N;
       q.out32 = g.out32 + static_cast<size_t>(r0) * g.N;
       if (fp8) q.row_scale = g.row_scale + r0;
-      DIT_CUDA_TRY(ctx, timed(DIT_KERNEL_GEMM_FC2, [&] { return launch(tmA, q); }));
+      if (blk8) {
+        const dit_status ls = block_product(DIT_KERNEL_GEMM_FC2, last_wb, last_w, ctx->lay.blk.s_fc2, q, kBlkGateResidF32, q.out32, q.N, r0, rows);
+        if (ls != DIT_OK) return ls;
+      } else {
+        DIT_CUDA_TRY(ctx, timed(DIT_KERNEL_GEMM_FC2, [&] { return launch(tmA, q); }));
+      }
       DIT_CUDA_TRY(ctx, cudaEventRecord(ctx->slice_done[sidx], st));
       DIT_CUDA_TRY(ctx, cudaStreamWaitEvent(ctx->copy_stream, ctx->slice_done[sidx], 0));
       DIT_CUDA_TRY(ctx, cudaMemcpyAsync(host_out + static_cast<size_t>(r0) * g.N, g.out32 + static_cast<size_t>(r0) * g.N,
@@ -569,6 +656,10 @@ dit_status step_impl(dit_ctx* ctx, const void* tokens, const int32_t* lens, int 
                                         c.ln_eps, seq, st, ks, rg, nullptr, ctx->num_sms, status, r0, bf)
                       : launch_ln<false>(stream, nullptr, h, modb, modb + H, req_stride, T, H, c.ln_eps, seq, st, ks, rg, nullptr, ctx->num_sms, status, 0, bf);
       }));
+      if (blk8) {                                // (never in slices: q8 holds the whole operand)
+        const dit_status ls = quantise_blocks(h, H, H);
+        return ls != DIT_OK ? ls : block_product(DIT_KERNEL_GEMM_QKV, wb, ctx->lay.blk.w_qkv, ctx->lay.blk.s_qkv, g, kBlkF16, qkv, 3ll * H, 0, T);
+      }
       GemmParams q = g;
       q.M = rows; q.row0 = r0; q.out16 = qkv + static_cast<size_t>(r0) * 3 * H;
       if (qk_variant) {
@@ -592,7 +683,7 @@ dit_status step_impl(dit_ctx* ctx, const void* tokens, const int32_t* lens, int 
       }
       return DIT_OK;
     };
-    if (b == 0 && tokens_in_slices && !fp8 && !dual) {
+    if (b == 0 && tokens_in_slices && !fp8 && !blk8 && !dual) {
       // dit_step_forward_host: the tokens are on their way in row slices on the copy stream; each slice is
       // normalised and projected as soon as it has landed
       const int tile_rows = 2 * gemm_cfg::BM;
@@ -622,7 +713,10 @@ dit_status step_impl(dit_ctx* ctx, const void* tokens, const int32_t* lens, int 
     ap.H = H; ap.n_heads = c.n_heads; ap.status = status;
     ap.probe = ctx->attn_probe ? status + 4 : nullptr;
     ap.scale_log2 = 1.4426950408889634f / sqrtf(static_cast<float>(c.head_dim));
-    DIT_CUDA_TRY(ctx, timed(DIT_KERNEL_ATTENTION, [&] {
+    if (sparse) {
+      const dit_status ls = sparse_attention(ap.out, ap.ld_out);
+      if (ls != DIT_OK) return ls;
+    } else DIT_CUDA_TRY(ctx, timed(DIT_KERNEL_ATTENTION, [&] {
       if (bf) return c.head_dim == 128 ? launch_attention<128, true>(tm_qkv, ap, seq, st) : launch_attention<64, true>(tm_qkv, ap, seq, st);
       return c.head_dim == 128 ? launch_attention<128>(tm_qkv, ap, seq, st) : launch_attention<64>(tm_qkv, ap, seq, st);
     }));
@@ -634,7 +728,10 @@ dit_status step_impl(dit_ctx* ctx, const void* tokens, const int32_t* lens, int 
       g.bias = reinterpret_cast<const float*>(wb + ctx->lay.blk.b_fc1);
       g.out16 = cat + H; g.ld16 = H + F;
       if (fp8) { g.row_scale = row_scale; g.col_scale = reinterpret_cast<const float*>(wb + ctx->lay.blk.s_fc1); }
-      DIT_CUDA_TRY(ctx, timed(DIT_KERNEL_GEMM_FC1, [&] {
+      if (blk8) {                                // q8 still holds h
+        const dit_status ls = block_product(DIT_KERNEL_GEMM_FC1, wb, ctx->lay.blk.w_fc1, ctx->lay.blk.s_fc1, g, kBlkGeluF16, cat + H, H + F, 0, T);
+        if (ls != DIT_OK) return ls;
+      } else DIT_CUDA_TRY(ctx, timed(DIT_KERNEL_GEMM_FC1, [&] {
         if (bf) return launch_gemm<kEpiBiasGeluF16, 0, false, false, true>(ctx, tm_h, bs.tm_fc1, g, seq, st);
         return fp8 ? launch_gemm<kEpiBiasGeluF16, 0, false, true>(ctx, tm_h, bs.tm_fc1, g, seq, st)
                    : launch_gemm<kEpiBiasGeluF16>(ctx, tm_h, bs.tm_fc1, g, seq, st);
@@ -650,8 +747,16 @@ dit_status step_impl(dit_ctx* ctx, const void* tokens, const int32_t* lens, int 
         DIT_CUDA_TRY(ctx, timed(DIT_KERNEL_QUANTIZE, [&] { return quantise_rows(cat, H + F, H + F); }));
         g.row_scale = row_scale2; g.col_scale = reinterpret_cast<const float*>(wb + ctx->lay.blk.s_fc2);
       }
+      if (blk8) {
+        const dit_status ls = quantise_blocks(cat, H + F, H + F);
+        if (ls != DIT_OK) return ls;
+        last_wb = wb; last_w = ctx->lay.blk.w_o;
+      }
       if (last) {
         const dit_status ls = last_gemm(cat, H + F, fp8 ? tm_cat8 : tm_cat, bs.tm_fc2, g);
+        if (ls != DIT_OK) return ls;
+      } else if (blk8) {
+        const dit_status ls = block_product(DIT_KERNEL_GEMM_FC2, wb, ctx->lay.blk.w_o, ctx->lay.blk.s_fc2, g, kBlkGateResidF32, g.out32, H, 0, T);
         if (ls != DIT_OK) return ls;
       } else {
         DIT_CUDA_TRY(ctx, timed(DIT_KERNEL_GEMM_FC2, [&] {
@@ -661,7 +766,7 @@ dit_status step_impl(dit_ctx* ctx, const void* tokens, const int32_t* lens, int 
       }
       continue;
     }
-    if (last && host_out && !dual && !fp8) {
+    if (last && host_out && !dual && !fp8 && !blk8) {
       // dit_step_forward_host, last block: after attention every row is independent, so projection, LayerNorm,
       // up- and down-projection run slice by slice and a finished slice of the output goes to the host while
       // the next one is computed.  A slice is a whole number of 256-row tiles: every element is computed
@@ -724,7 +829,11 @@ dit_status step_impl(dit_ctx* ctx, const void* tokens, const int32_t* lens, int 
       DIT_CUDA_TRY(ctx, timed(DIT_KERNEL_QUANTIZE, [&] { return quantise_rows(a, H, H); }));
       g.row_scale = row_scale2; g.col_scale = reinterpret_cast<const float*>(wb + ctx->lay.blk.s_o);
     }
-    DIT_CUDA_TRY(ctx, timed(DIT_KERNEL_GEMM_PROJ, [&] {
+    if (blk8) {
+      dit_status ls = quantise_blocks(a, H, H);
+      if (ls == DIT_OK) ls = block_product(DIT_KERNEL_GEMM_PROJ, wb, ctx->lay.blk.w_o, ctx->lay.blk.s_o, g, kBlkGateResidF32, stream, H, 0, T);
+      if (ls != DIT_OK) return ls;
+    } else DIT_CUDA_TRY(ctx, timed(DIT_KERNEL_GEMM_PROJ, [&] {
       if (fp8) return launch_gemm<kEpiGateResidF32, 0, false, true>(ctx, tm_a8, bs.tm_o, g, seq, st);
       return dual ? launch_gemm<kEpiGateResidF32, 0, true>(ctx, tm_a, bs.tm_o, g, seq, st, rg, &bt.tm_o)
                   : launch_gemm<kEpiGateResidF32>(ctx, tm_a, bs.tm_o, g, seq, st);
@@ -742,7 +851,13 @@ dit_status step_impl(dit_ctx* ctx, const void* tokens, const int32_t* lens, int 
     g.out16 = u;
     two_stream(g, ctx->lay.blk.b_fc1);
     if (fp8) { g.row_scale = row_scale; g.col_scale = reinterpret_cast<const float*>(wb + ctx->lay.blk.s_fc1); }
-    DIT_CUDA_TRY(ctx, timed(DIT_KERNEL_GEMM_FC1, [&] {
+    if (blk8) {
+      dit_status ls = quantise_blocks(h, H, H);
+      if (ls == DIT_OK) ls = block_product(DIT_KERNEL_GEMM_FC1, wb, ctx->lay.blk.w_fc1, ctx->lay.blk.s_fc1, g, kBlkGeluF16, u, F, 0, T);
+      if (ls == DIT_OK) ls = quantise_blocks(u, F, F);
+      if (ls != DIT_OK) return ls;
+      last_wb = wb; last_w = ctx->lay.blk.w_fc2;
+    } else DIT_CUDA_TRY(ctx, timed(DIT_KERNEL_GEMM_FC1, [&] {
       if (fp8) return launch_gemm<kEpiBiasGeluF16, 0, false, true>(ctx, tm_h, bs.tm_fc1, g, seq, st);
       if (bf) return launch_gemm<kEpiBiasGeluF16, 0, false, false, true>(ctx, tm_h, bs.tm_fc1, g, seq, st);
       return dual ? launch_gemm<kEpiBiasGeluF16, 0, true>(ctx, tm_h, bs.tm_fc1, g, seq, st, rg, &bt.tm_fc1)
@@ -762,6 +877,9 @@ dit_status step_impl(dit_ctx* ctx, const void* tokens, const int32_t* lens, int 
     }
     if (last && !dual) {
       const dit_status ls = last_gemm(u, F, fp8 ? tm_u8 : tm_u, bs.tm_fc2, g);
+      if (ls != DIT_OK) return ls;
+    } else if (blk8) {
+      const dit_status ls = block_product(DIT_KERNEL_GEMM_FC2, wb, ctx->lay.blk.w_fc2, ctx->lay.blk.s_fc2, g, kBlkGateResidF32, g.out32, H, 0, T);
       if (ls != DIT_OK) return ls;
     } else if (fp8) {
       DIT_CUDA_TRY(ctx, timed(DIT_KERNEL_GEMM_FC2, [&] { return launch_gemm<kEpiGateResidF32, 0, false, true>(ctx, tm_u8, bs.tm_fc2, g, seq, st); }));
@@ -852,6 +970,8 @@ dit_status dit_ctx_create(const dit_config* cfg, void* workspace, size_t workspa
   ctx->last_launches = 0;
   ctx->maps_T = -1;
   ctx->attn_probe = false;
+  ctx->sparse_keep = 1.0f;
+  ctx->sparse_min_blocks = 1;
   ctx->last_T = ctx->last_R = ctx->last_nb = 0;
   ctx->last_parallel = false;
   ctx->timing = false;
@@ -902,6 +1022,8 @@ dit_status dit_ctx_create(const dit_config* cfg, void* workspace, size_t workspa
     ln_opt(&ln_modulate_tma_kernel<false, 8, true>);   ln_opt(&ln_modulate_tma_kernel<false, 24, true>);   ln_opt(&ln_modulate_tma_kernel<false, 32, true>);
     ln_opt(&ln_modulate_tma_kernel<true, 8, true>);    ln_opt(&ln_modulate_tma_kernel<true, 24, true>);    ln_opt(&ln_modulate_tma_kernel<true, 32, true>);
   }
+  // the first call of an operator on a device sets kernel attributes: here, so that steps may be captured at once
+  if (e == cudaSuccess && (cfg->flags & (DIT_FLAG_FP8_BLOCK128 | DIT_FLAG_SPARSE_ATTENTION))) e = ops_prepare_device();
   if (e == cudaSuccess) {
     cudaLaunchConfig_t lc = {};
     lc.gridDim = dim3(sms & ~1); lc.blockDim = dim3(gemm_cfg::THREADS); lc.dynamicSmemBytes = gemm_cfg::SMEM_BYTES;
@@ -970,6 +1092,17 @@ dit_status dit_ctx_destroy(dit_ctx* ctx) {
   return DIT_OK;
 }
 
+dit_status dit_ctx_set_sparse_attention(dit_ctx* ctx, float keep, int32_t min_blocks) {
+  if (!ctx) return DIT_ERR_INVALID_ARG;
+  ctx->err[0] = 0;
+  if (!(ctx->cfg.flags & DIT_FLAG_SPARSE_ATTENTION)) return fail(ctx, DIT_ERR_INVALID_ARG, "the context was created without DIT_FLAG_SPARSE_ATTENTION");
+  if (!(keep > 0.f) || !(keep <= 1.f)) return fail(ctx, DIT_ERR_INVALID_ARG, "keep must be in (0, 1]");
+  if (min_blocks < 1) return fail(ctx, DIT_ERR_INVALID_ARG, "min_blocks must be at least 1");
+  ctx->sparse_keep = keep;
+  ctx->sparse_min_blocks = min_blocks;
+  return DIT_OK;
+}
+
 dit_status dit_load_block_weights(dit_ctx* ctx, int32_t b, const dit_block_weights* w, void* stream) {
   if (!ctx) return DIT_ERR_INVALID_ARG;
   ctx->err[0] = 0;
@@ -998,8 +1131,10 @@ dit_status dit_load_block_weights(dit_ctx* ctx, int32_t b, const dit_block_weigh
       transpose_bf16_to_f16_kernel<false><<<grid, 256, 0, st>>>(static_cast<const __nv_bfloat16*>(src), reinterpret_cast<__half*>(base + off), K, N);
     return cudaGetLastError();
   };
-  const bool fp8 = (ctx->cfg.flags & DIT_FLAG_FP8_GEMM) != 0;
-  auto weight8 = [&](const void* src, size_t off, size_t scale_off, int K, int N) {   // [K, N] bf16 -> e4m3 [N, K] + scales [N]
+  const bool fp8 = (ctx->cfg.flags & (DIT_FLAG_FP8_GEMM | DIT_FLAG_FP8_BLOCK128)) != 0;
+  auto weight8 = [&](const void* src, size_t off, size_t scale_off, int K, int N) {   // [K, N] bf16 -> e4m3 [N, K] + scales [N] or per block
+    if (ctx->cfg.flags & DIT_FLAG_FP8_BLOCK128)
+      return launch_quantize_weight(src, DIT_TYPE_BF16, N, K, N, base + off, K, reinterpret_cast<float*>(base + scale_off), st);
     col_absmax_scale_kernel<<<(N + 255) / 256, 256, 0, st>>>(static_cast<const __nv_bfloat16*>(src), reinterpret_cast<float*>(base + scale_off), K, N);
     dim3 grid((N + 31) / 32, (K + 31) / 32);
     transpose_bf16_to_e4m3_kernel<<<grid, 256, 0, st>>>(static_cast<const __nv_bfloat16*>(src), reinterpret_cast<const float*>(base + scale_off), base + off, K, N);
@@ -1033,6 +1168,7 @@ dit_status dit_load_dual_block_weights(dit_ctx* ctx, int32_t b, const dit_block_
   if (b < 0 || b + 1 >= ctx->cfg.max_blocks) return fail(ctx, DIT_ERR_CAPACITY, "a two-stream block needs slots b and b + 1 inside [0, max_blocks)");
   if (ctx->cfg.flags & DIT_FLAG_FP8_GEMM) return fail(ctx, DIT_ERR_SHAPE, "two-stream blocks are not available with DIT_FLAG_FP8_GEMM");
   if (ctx->cfg.flags & DIT_FLAG_BF16_OPERANDS) return fail(ctx, DIT_ERR_SHAPE, "two-stream blocks are not available with DIT_FLAG_BF16_OPERANDS");
+  if (ctx->cfg.flags & DIT_FLAG_FP8_BLOCK128) return fail(ctx, DIT_ERR_SHAPE, "two-stream blocks are not available with DIT_FLAG_FP8_BLOCK128");
   dit_status s = dit_load_block_weights(ctx, b, image_stream, stream);
   if (s != DIT_OK) return s;
   s = dit_load_block_weights(ctx, b + 1, text_stream, stream);
@@ -1075,8 +1211,10 @@ dit_status dit_load_parallel_block_weights(dit_ctx* ctx, int32_t b, const dit_pa
     return cudaGetLastError();
   };
   DIT_CUDA_TRY(ctx, cudaMemsetAsync(base + L.b_ada, 0, static_cast<size_t>(6) * H * 4, st));
-  const bool fp8 = (ctx->cfg.flags & DIT_FLAG_FP8_GEMM) != 0;
-  auto weight8 = [&](const void* src, size_t off, size_t scale_off, int K, int N) {   // [K, N] bf16 -> e4m3 [N, K] + scales [N]
+  const bool fp8 = (ctx->cfg.flags & (DIT_FLAG_FP8_GEMM | DIT_FLAG_FP8_BLOCK128)) != 0;
+  auto weight8 = [&](const void* src, size_t off, size_t scale_off, int K, int N) {   // [K, N] bf16 -> e4m3 [N, K] + scales [N] or per block
+    if (ctx->cfg.flags & DIT_FLAG_FP8_BLOCK128)
+      return launch_quantize_weight(src, DIT_TYPE_BF16, N, K, N, base + off, K, reinterpret_cast<float*>(base + scale_off), st);
     col_absmax_scale_kernel<<<(N + 255) / 256, 256, 0, st>>>(static_cast<const __nv_bfloat16*>(src), reinterpret_cast<float*>(base + scale_off), K, N);
     dim3 grid((N + 31) / 32, (K + 31) / 32);
     transpose_bf16_to_e4m3_kernel<<<grid, 256, 0, st>>>(static_cast<const __nv_bfloat16*>(src), reinterpret_cast<const float*>(base + scale_off), base + off, K, N);

@@ -245,11 +245,13 @@ cudaError_t launch_product(const DeviceState& d, const BlockProduct& b, BlockGem
   CUtensorMap tmA, tmB;
   const long long tiles_n = (p.N + 127) / 128;
   const int groups = (p.K + 127) / 128;
+  const int rows = b.plan_m;
   const long long pair_tiles = static_cast<long long>((p.M + 255) / 256) * ((p.N + 255) / 256);
+  const long long planned_tiles = static_cast<long long>((rows + 255) / 256) * ((p.N + 255) / 256);
   // Few rows, or too few 256 x 256 tiles to fill the device: the split kernel.
-  if (p.M <= 128 || pair_tiles < d.pairs / 2) {
-    const int bt = p.M <= 16 ? 16 : (p.M <= 32 ? 32 : (p.M <= 64 ? 64 : 128));
-    const long long tiles = tiles_n * ((p.M + bt - 1) / bt);
+  if (rows <= 128 || planned_tiles < d.pairs / 2) {
+    const int bt = rows <= 16 ? 16 : (rows <= 32 ? 32 : (rows <= 64 ? 64 : 128));
+    const long long tiles = tiles_n * ((rows + bt - 1) / bt);
     int splits = 1;
     while (splits < 8 && 2 * splits <= groups && tiles * splits < d.num_sms) splits *= 2;
     if (!byte_map(&tmA, b.a, p.K, p.M, b.lda, bt) || !byte_map(&tmB, b.b, p.K, p.N, b.ldb, 128)) return cudaErrorInvalidValue;
@@ -344,7 +346,7 @@ cudaError_t launch_block_product(const BlockProduct& b, const SeqInfo& seq, cuda
   const int elem = (b.epilogue == kBlkF32 || b.epilogue == kBlkGateResidF32) ? 4 : 2;
   p.vec_out = aligned(b.out, 16) && b.ld_out * elem % 16 == 0;
   p.status = d->status;
-  p.resid = b.resid; p.gate = b.gate; p.gate_stride = b.gate_stride;
+  p.row0 = b.row0; p.resid = b.resid; p.gate = b.gate; p.gate_stride = b.gate_stride;
   switch (b.epilogue) {
     case kBlkF16: return launch_product<kBlkF16>(*d, b, p, seq, st);
     case kBlkBF16: return launch_product<kBlkBF16>(*d, b, p, seq, st);
@@ -439,6 +441,7 @@ dit_status dit_gemm_block128(const dit_gemm_block128_args* a, void* stream) {
   b.a = a->a; b.a_scales = a->a_scales; b.b = a->b; b.b_scales = a->b_scales; b.bias = a->bias; b.out = a->out;
   b.lda = a->lda; b.ld_a_scales = a->ld_a_scales; b.ldb = a->ldb; b.ld_out = a->ld_out;
   b.m = static_cast<int>(a->m); b.n = static_cast<int>(a->n); b.k = static_cast<int>(a->k);
+  b.plan_m = b.m;
   b.epilogue = a->out_type == DIT_TYPE_F16 ? kBlkF16 : (a->out_type == DIT_TYPE_BF16 ? kBlkBF16 : kBlkF32);
   return launch_block_product(b, kNoSeq, static_cast<cudaStream_t>(stream)) == cudaSuccess ? DIT_OK : DIT_ERR_CUDA;
 }

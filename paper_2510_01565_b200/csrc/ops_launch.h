@@ -18,8 +18,11 @@ struct BlockProduct {
   void* out;
   long long lda, ld_a_scales, ldb, ld_out;
   int m, n, k;
+  int plan_m;                // rows by which the kernel is chosen: the whole batch's where a launch covers a slice of its rows, so
+                             // that every element is summed in the same order as in one launch
   int epilogue;              // BlockGemmEpilogue
-  const float* resid;        // gated residual only
+  int row0;                  // gated residual only: packed row of row 0, residual, gate vectors
+  const float* resid;
   const float* gate;
   long long gate_stride;
 };
