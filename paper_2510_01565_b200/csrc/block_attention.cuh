@@ -26,10 +26,12 @@ struct BlockAttnParams {
   long long ld_index;
   int n_heads;
   float scale_log2;          // scale * log2(e), positive
+  int items;                 // (request, head, 256 query rows) triples
+  int wide_out;              // rows of out start on 32-byte boundaries
   int* status;
 };
 
-constexpr int kWindowBlocks = 512;      // key blocks whose lists are laid out in shared memory at a time
+constexpr int kWindowBlocks = 256;      // key blocks whose lists are laid out in shared memory at a time
 constexpr int kMaxKeyBlocks = 16384;    // of one request
 
 template <int D>
@@ -39,18 +41,21 @@ struct BlockAttnCfg {
   static constexpr int OFF_Q = 0, OFF_K = 2 * TILE_BYTES, OFF_V = OFF_K + K_STAGES * TILE_BYTES;
   static constexpr int OFF_BAR = OFF_V + V_STAGES * TILE_BYTES;
   static constexpr int OFF_BITS = OFF_BAR + 256;                                  // uint32 [2][kWindowBlocks / 32]
-  static constexpr int OFF_LIST = OFF_BITS + 2 * kWindowBlocks / 8;               // uint16 [kWindowBlocks]
-  static constexpr int SMEM_USED = OFF_LIST + 2 * kWindowBlocks + 1024;
+  static constexpr int OFF_LIST = OFF_BITS + 2 * kWindowBlocks / 8;               // uint16 [2][kWindowBlocks]
+  static constexpr int SMEM_USED = OFF_LIST + 2 * 2 * kWindowBlocks + 1024;
   // one CTA per SM: each takes all of tensor memory (see AttnCfg)
   static constexpr int SMEM_BYTES = SMEM_USED > 116 * 1024 ? SMEM_USED : 116 * 1024;
   static constexpr int THREADS = 384, Q_ROWS = 256;
   static_assert(SMEM_BYTES <= 227 * 1024, "shared memory of one CTA");
 };
 
-// Marks the listed key blocks of window [w0, w0 + kWindowBlocks) in `bits`; entries outside [0, n_kv) are ignored, repeated ones meet.
-__device__ __forceinline__ void mark_blocks(uint32_t* bits, const int* list, int n, int w0, int n_kv, int tid, int threads) {
-  for (int e = tid; e < n; e += threads) {
-    const int j = __ldg(list + e);
+// One warp marks the listed key blocks of window [w0, w0 + kWindowBlocks) in `bits`; entries outside [0, n_kv) are ignored, repeated
+// ones meet.  The first entries are read together with the list's length (all ld entries of a list exist).
+__device__ __forceinline__ void mark_blocks(uint32_t* bits, const int* list, const int* count, long long ld, int w0, int n_kv, int lane) {
+  const int first = lane < ld ? __ldg(list + lane) : -1;
+  const int n = static_cast<int>(min(static_cast<long long>(max(__ldg(count), 0)), ld));
+  for (int e = lane; e < n; e += 32) {
+    const int j = e < 32 ? first : __ldg(list + e);
     if (j >= w0 && j < min(n_kv, w0 + kWindowBlocks)) atomicOr(bits + ((j - w0) >> 5), 1u << (j & 31));
   }
 }
@@ -95,10 +100,36 @@ __device__ __forceinline__ int order_blocks(const uint32_t* bits, uint16_t* list
 // them.  The two tiles' lists are merged: a block in both is loaded once and used twice, as in the dense kernel; one
 // in a single list is loaded for that tile alone.  The key ring is three tiles deep (the dense kernel needs two):
 // without sharing every use of S needs a new K tile.
+// Lists are short, so what a CTA does before its first and after its last product counts: with one item per CTA that was
+// 7 us of 31 (14 blocks per list).  The grid is persistent instead, and all roles run on from item to item: a warp of its own
+// lays out the next lists meanwhile (two buffers), the next item's Q, K and V are requested as soon as the last
+// score product of the current one has been issued, and its first scores are computed under the current item's last softmax.
+// No barrier guards O between items: a warpgroup hands over an item's first P only after it has read the previous O.
 // A key block may end inside the tile.  The scores behind the end are dropped before the row maximum, and the V rows there,
 // which belong to somebody else and may hold anything, are cleared in shared memory before the product
 // (a zero probability times an infinity or NaN would be NaN).
 // ------------------------------------------------------------------------------------------------
+struct BlockItem {
+  int head, qb, req, q_begin, q_len, kv_begin, kv_len, n_kv, n_windows;
+  bool tile1;                                  // the second query tile has rows
+};
+template <int Q_ROWS>
+__device__ __forceinline__ BlockItem block_item(const BlockBatch& batch, int n_heads, int item) {
+  // heads of a request one after the other, so that the CTAs at work at one time share the keys of a few heads
+  BlockItem it{};
+  for (int i = 0; i < batch.n; ++i) {
+    it.req = batch.order[i];
+    const int nb = (batch.cu_q[it.req + 1] - batch.cu_q[it.req] + Q_ROWS - 1) / Q_ROWS;
+    if (item < nb * n_heads) { it.head = item / nb; it.qb = item - it.head * nb; break; }
+    item -= nb * n_heads;
+  }
+  it.q_begin = batch.cu_q[it.req]; it.q_len = batch.cu_q[it.req + 1] - it.q_begin;
+  it.kv_begin = batch.cu_kv[it.req]; it.kv_len = batch.cu_kv[it.req + 1] - it.kv_begin;
+  it.n_kv = (it.kv_len + 127) >> 7; it.n_windows = (it.n_kv + kWindowBlocks - 1) / kWindowBlocks;
+  it.tile1 = it.qb * Q_ROWS + 128 < it.q_len;
+  return it;
+}
+
 template <int D, bool BF16>
 __global__ void __launch_bounds__(BlockAttnCfg<D>::THREADS, 1)
 block_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
@@ -109,48 +140,26 @@ block_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
   const uint32_t base = (raw + 1023u) & ~1023u;
   uint8_t* aligned = smem_raw + (base - raw);
   const uint32_t bar0 = base + C::OFF_BAR;
-  const uint32_t q_full = bar0, s_free = bar0 + 8u, win_full = bar0 + 16u, win_empty = bar0 + 24u;
-  auto k_full = [&](int s) { return bar0 + 8u * (4 + s); };
-  auto k_empty = [&](int s) { return bar0 + 8u * (7 + s); };
-  auto v_full = [&](int s) { return bar0 + 8u * (10 + s); };
-  auto v_empty = [&](int s) { return bar0 + 8u * (12 + s); };
-  auto s_full = [&](int i) { return bar0 + 8u * (14 + i); };
-  auto p_full = [&](int i) { return bar0 + 8u * (16 + i); };
-  auto o_full = [&](int i) { return bar0 + 8u * (18 + i); };
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(aligned + C::OFF_BAR + 8 * 20);
+  const uint32_t q_full = bar0, q_empty = bar0 + 8u, s_free = bar0 + 16u;
+  auto seg_full = [&](int b) { return bar0 + 8u * (3 + b); };                     // a window's entries lie in list b
+  auto seg_empty = [&](int b) { return bar0 + 8u * (5 + b); };
+  auto k_full = [&](int s) { return bar0 + 8u * (7 + s); };
+  auto k_empty = [&](int s) { return bar0 + 8u * (10 + s); };
+  auto v_full = [&](int s) { return bar0 + 8u * (13 + s); };
+  auto v_empty = [&](int s) { return bar0 + 8u * (15 + s); };
+  auto s_full = [&](int i) { return bar0 + 8u * (17 + i); };
+  auto p_full = [&](int i) { return bar0 + 8u * (19 + i); };
+  auto o_full = [&](int i) { return bar0 + 8u * (21 + i); };
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(aligned + C::OFF_BAR + 8 * 23);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-  volatile int* n_entries = reinterpret_cast<volatile int*>(tmem_slot + 2);
+  volatile int* n_entries = reinterpret_cast<volatile int*>(tmem_slot + 2);       // [2]
   uint32_t* bits = reinterpret_cast<uint32_t*>(aligned + C::OFF_BITS);
-  uint16_t* list = reinterpret_cast<uint16_t*>(aligned + C::OFF_LIST);
-  volatile const uint16_t* entries = list;
+  uint16_t* lists = reinterpret_cast<uint16_t*>(aligned + C::OFF_LIST);
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  // ---- (request, head, 256 query rows) of this CTA; heads of a request one after the other, so that the CTAs resident at
-  // one time share the keys of a few heads
-  int head = 0, qb = blockIdx.x, req = 0;
-  for (int i = 0; i < batch.n; ++i) {
-    req = batch.order[i];
-    const int nb = (batch.cu_q[req + 1] - batch.cu_q[req] + C::Q_ROWS - 1) / C::Q_ROWS;
-    if (qb < nb * p.n_heads) { head = qb / nb; qb -= head * nb; break; }
-    qb -= nb * p.n_heads;
-  }
-  const int q_begin = batch.cu_q[req], q_len = batch.cu_q[req + 1] - q_begin;
-  const int kv_begin = batch.cu_kv[req], kv_len = batch.cu_kv[req + 1] - kv_begin;
-  const int n_kv = (kv_len + 127) >> 7, n_windows = (n_kv + kWindowBlocks - 1) / kWindowBlocks;
-  const bool tile1_valid = qb * C::Q_ROWS + 128 < q_len;
-  const long long row_of_lists = static_cast<long long>(head) * batch.first_qblock[batch.n] + batch.first_qblock[req] + 2 * qb;
-  const int* lists[2] = {p.index + row_of_lists * p.ld_index, p.index + (row_of_lists + 1) * p.ld_index};
-  auto list_length = [&](int i) {
-    if (i == 1 && !tile1_valid) return 0;
-    return static_cast<int>(min(static_cast<long long>(max(__ldg(p.count + row_of_lists + i), 0)), p.ld_index));
-  };
-
-  if (threadIdx.x < 2 * kWindowBlocks / 32) bits[threadIdx.x] = 0;
   if (threadIdx.x == 0) {
-    mbar_init(q_full, 1);
-    mbar_init(s_free, 4);
-    mbar_init(win_full, 1);
-    mbar_init(win_empty, tile1_valid ? 11 : 7);          // producer, two issuers, four warps per query tile
+    mbar_init(q_full, 1); mbar_init(q_empty, 1); mbar_init(s_free, 4);
+    for (int b = 0; b < 2; ++b) { mbar_init(seg_full(b), 1); mbar_init(seg_empty(b), 11); }   // producer, two issuers, eight softmax warps
     for (int s = 0; s < C::K_STAGES; ++s) { mbar_init(k_full(s), 1); mbar_init(k_empty(s), 1); }
     for (int s = 0; s < C::V_STAGES; ++s) { mbar_init(v_full(s), 1); mbar_init(v_empty(s), 1); }
     for (int i = 0; i < 2; ++i) { mbar_init(s_full(i), 1); mbar_init(p_full(i), 4); mbar_init(o_full(i), 1); }
@@ -159,48 +168,50 @@ block_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
   }
   if (warp == 0 && lane == 0) { prefetch_tmap(&tmQ); prefetch_tmap(&tmK); prefetch_tmap(&tmV); }
   if (warp == 1) { tmem_alloc(smem_u32(tmem_slot), 512); tmem_relinquish(); }
-  __syncthreads();
-  for (int i = 0; i < 2; ++i) mark_blocks(bits + i * (kWindowBlocks / 32), lists[i], list_length(i), 0, n_kv, threadIdx.x, C::THREADS);
-  __syncthreads();
-  if (warp == 3) {
-    const int n = order_blocks(bits, list, lane);
-    if (lane == 0) *n_entries = n;
-  }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
   const uint32_t tS = tmem_base, tP = tmem_base + 128, tO = tmem_base + 256;      // columns: S 128, P 2 x 64, O 2 x 128
-  // Every role walks all windows: waits until the window's entries are laid out, and says when it has read them.
-  auto window_begin = [&](int w) { return w == 0 || mbar_wait(win_full, (w - 1) & 1u, abort_flag); };
+
+  // Every role walks the same items and windows; `seg` counts the windows.  The entries of a window are read between these two.
+  auto seg_begin = [&](uint32_t seg) { return mbar_wait(seg_full(seg & 1), (seg >> 1) & 1u, abort_flag); };
+  auto seg_entries = [&](uint32_t seg) { return static_cast<volatile const uint16_t*>(lists + (seg & 1) * kWindowBlocks); };
+  uint32_t seg = 0;
 
   if (warp < 4) {
     DIT_SETMAXNREG_DEC(96);
     if (warp == 0) {
       if (lane == 0) {
         // ---------------------------------------------------------------- TMA producer
-        mbar_arrive_expect_tx(q_full, 2 * C::TILE_BYTES);
-        for (int i = 0; i < 2; ++i)
-          for (int pn = 0; pn < C::NP; ++pn)
-            tma_load_2d(base + C::OFF_Q + i * C::TILE_BYTES + pn * C::PANEL, &tmQ, head * D + pn * 64, q_begin + qb * C::Q_ROWS + i * 128, q_full);
-        int ks = 0, vs = 0; uint32_t kph = 1, vph = 1;
-        for (int w = 0; w < n_windows; ++w) {
-          if (!window_begin(w)) goto done;
-          const int n = *n_entries;
-          for (int e = 0; e < n; ++e) {
-            const int y = kv_begin + (w * kWindowBlocks + (entries[e] >> 2)) * 128;
-            if (!mbar_wait(k_empty(ks), kph, abort_flag)) goto done;
-            mbar_arrive_expect_tx(k_full(ks), C::TILE_BYTES);
+        int ks = 0, vs = 0; uint32_t kph = 1, vph = 1, qph = 1;
+        for (int item = blockIdx.x; item < p.items; item += gridDim.x) {
+          const BlockItem it = block_item<C::Q_ROWS>(batch, p.n_heads, item);
+          if (!mbar_wait(q_empty, qph, abort_flag)) goto done;
+          qph ^= 1u;
+          mbar_arrive_expect_tx(q_full, 2 * C::TILE_BYTES);
+          for (int i = 0; i < 2; ++i)
             for (int pn = 0; pn < C::NP; ++pn)
-              tma_load_2d(base + C::OFF_K + ks * C::TILE_BYTES + pn * C::PANEL, &tmK, head * D + pn * 64, y, k_full(ks));
-            if (++ks == C::K_STAGES) { ks = 0; kph ^= 1u; }
-            if (!mbar_wait(v_empty(vs), vph, abort_flag)) goto done;
-            mbar_arrive_expect_tx(v_full(vs), C::TILE_BYTES);
-            for (int pn = 0; pn < C::NP; ++pn)
-              tma_load_2d(base + C::OFF_V + vs * C::TILE_BYTES + pn * C::PANEL, &tmV, head * D + pn * 64, y, v_full(vs));
-            if (++vs == C::V_STAGES) { vs = 0; vph ^= 1u; }
+              tma_load_2d(base + C::OFF_Q + i * C::TILE_BYTES + pn * C::PANEL, &tmQ, it.head * D + pn * 64, it.q_begin + it.qb * C::Q_ROWS + i * 128, q_full);
+          for (int w = 0; w < it.n_windows; ++w, ++seg) {
+            if (!seg_begin(seg)) goto done;
+            volatile const uint16_t* entries = seg_entries(seg);
+            const int n = n_entries[seg & 1];
+            for (int e = 0; e < n; ++e) {
+              const int y = it.kv_begin + (w * kWindowBlocks + (entries[e] >> 2)) * 128;
+              if (!mbar_wait(k_empty(ks), kph, abort_flag)) goto done;
+              mbar_arrive_expect_tx(k_full(ks), C::TILE_BYTES);
+              for (int pn = 0; pn < C::NP; ++pn)
+                tma_load_2d(base + C::OFF_K + ks * C::TILE_BYTES + pn * C::PANEL, &tmK, it.head * D + pn * 64, y, k_full(ks));
+              if (++ks == C::K_STAGES) { ks = 0; kph ^= 1u; }
+              if (!mbar_wait(v_empty(vs), vph, abort_flag)) goto done;
+              mbar_arrive_expect_tx(v_full(vs), C::TILE_BYTES);
+              for (int pn = 0; pn < C::NP; ++pn)
+                tma_load_2d(base + C::OFF_V + vs * C::TILE_BYTES + pn * C::PANEL, &tmV, it.head * D + pn * 64, y, v_full(vs));
+              if (++vs == C::V_STAGES) { vs = 0; vph ^= 1u; }
+            }
+            mbar_arrive(seg_empty(seg & 1));
           }
-          if (w + 1 < n_windows) mbar_arrive(win_empty);
         }
       }
     } else if (warp == 1) {
@@ -209,218 +220,236 @@ block_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
         constexpr uint32_t idesc_s = idesc_f16(128, 128, false, BF16);
         const uint64_t qdesc0 = smem_desc_sw128(base + C::OFF_Q, 16, 1024), kdesc0 = smem_desc_sw128(base + C::OFF_K, 16, 1024);
         constexpr uint32_t kTileStep = C::TILE_BYTES >> 4;
-        int ks = 0; uint32_t kph = 0, u = 0;                                      // u: uses of S so far
-        if (!mbar_wait(q_full, 0, abort_flag)) goto done;
-        for (int w = 0; w < n_windows; ++w) {
-          if (!window_begin(w)) goto done;
-          const int n = *n_entries;
-          for (int e = 0; e < n; ++e) {
-            const int tiles = entries[e] & 3;
-            if (!mbar_wait(k_full(ks), kph, abort_flag)) goto done;
-            for (int i = 0; i < 2; ++i) {
-              if (!((tiles >> i) & 1)) continue;
-              if (u > 0 && !mbar_wait(s_free, (u - 1) & 1u, abort_flag)) goto done;
-              ++u;
-              tc_fence_after();
-              const uint64_t qd = qdesc0 + i * kTileStep, kd = kdesc0 + ks * kTileStep;
+        int ks = 0; uint32_t kph = 0, qph = 0, u = 0;                             // u: uses of S so far
+        for (int item = blockIdx.x; item < p.items; item += gridDim.x) {
+          const BlockItem it = block_item<C::Q_ROWS>(batch, p.n_heads, item);
+          if (!mbar_wait(q_full, qph, abort_flag)) goto done;
+          qph ^= 1u;
+          for (int w = 0; w < it.n_windows; ++w, ++seg) {
+            if (!seg_begin(seg)) goto done;
+            volatile const uint16_t* entries = seg_entries(seg);
+            const int n = n_entries[seg & 1];
+            for (int e = 0; e < n; ++e) {
+              const int tiles = entries[e] & 3;
+              if (!mbar_wait(k_full(ks), kph, abort_flag)) goto done;
+              for (int i = 0; i < 2; ++i) {
+                if (!((tiles >> i) & 1)) continue;
+                if (u > 0 && !mbar_wait(s_free, (u - 1) & 1u, abort_flag)) goto done;
+                ++u;
+                tc_fence_after();
+                const uint64_t qd = qdesc0 + i * kTileStep, kd = kdesc0 + ks * kTileStep;
 #pragma unroll
-              for (int kk = 0; kk < D / 16; ++kk) {
-                const uint32_t off = ((kk >> 2) * C::PANEL + (kk & 3) * 32) >> 4;
-                umma_f16(tS, qd + off, kd + off, idesc_s, kk != 0);
+                for (int kk = 0; kk < D / 16; ++kk) {
+                  const uint32_t off = ((kk >> 2) * C::PANEL + (kk & 3) * 32) >> 4;
+                  umma_f16(tS, qd + off, kd + off, idesc_s, kk != 0);
+                }
+                if (i == 1 || tiles == 1) umma_commit(k_empty(ks));               // the entry's last use of its K tile
+                umma_commit(s_full(i));
               }
-              if (i == 1 || tiles == 1) umma_commit(k_empty(ks));                 // the entry's last use of its K tile
-              umma_commit(s_full(i));
+              if (++ks == C::K_STAGES) { ks = 0; kph ^= 1u; }
             }
-            if (++ks == C::K_STAGES) { ks = 0; kph ^= 1u; }
+            mbar_arrive(seg_empty(seg & 1));
           }
-          if (w + 1 < n_windows) mbar_arrive(win_empty);
+          umma_commit(q_empty);                                                   // Q may be replaced once these products have read it
         }
       }
     } else if (warp == 2) {
-      // ------------------------------------------------------------------ MMA issuer 2: P V (the whole warp walks the list: it also
-      // clears the V rows behind the request's last key)
+      // ------------------------------------------------------------------ MMA issuer 2: P V (the whole warp walks the lists: it also
+      // clears the V rows behind a request's last key)
       constexpr uint32_t idesc_pv = idesc_f16(128, D, true, BF16);
       const uint64_t vdesc0 = smem_desc_sw128(base + C::OFF_V, C::PANEL, 1024);
       constexpr uint32_t kTileStep = C::TILE_BYTES >> 4;
-      int vs = 0; uint32_t vph = 0, uses[2] = {0, 0};
-      for (int w = 0; w < n_windows; ++w) {
-        if (!__all_sync(0xffffffffu, window_begin(w))) goto done;
-        const int n = *n_entries;
-        for (int e = 0; e < n; ++e) {
-          const int tiles = entries[e] & 3, j = w * kWindowBlocks + (entries[e] >> 2);
-          if (!__all_sync(0xffffffffu, mbar_wait(v_full(vs), vph, abort_flag))) goto done;
-          const int valid = kv_len - j * 128;
-          if (valid < 128) {
-            for (int r = valid * 8 + lane; r < 128 * 8; r += 32)                  // 16-byte units of rows valid .. 127
-              for (int pn = 0; pn < C::NP; ++pn)
-                *reinterpret_cast<uint4*>(aligned + C::OFF_V + vs * C::TILE_BYTES + pn * C::PANEL + r * 16) = make_uint4(0, 0, 0, 0);
-            fence_proxy_async_smem();
-            __syncwarp();
-          }
-          const uint64_t vd = vdesc0 + vs * kTileStep;
-          for (int i = 0; i < 2; ++i) {
-            if (!((tiles >> i) & 1)) continue;
-            if (!__all_sync(0xffffffffu, mbar_wait(p_full(i), uses[i] & 1u, abort_flag))) goto done;
-            tc_fence_after();
-            if (lane == 0) {
-#pragma unroll
-              for (int kk = 0; kk < 8; ++kk)
-                umma_f16_ts(tO + i * 128, tP + i * 64 + kk * 8, vd + kk * (2048 >> 4), idesc_pv, (uses[i] | kk) != 0);
-              if (i == 1 || tiles == 1) umma_commit(v_empty(vs));
-              umma_commit(o_full(i));
+      int vs = 0; uint32_t vph = 0, done_uses[2] = {0, 0};
+      for (int item = blockIdx.x; item < p.items; item += gridDim.x) {
+        const BlockItem it = block_item<C::Q_ROWS>(batch, p.n_heads, item);
+        bool more[2] = {false, false};                                            // O holds products of this item
+        for (int w = 0; w < it.n_windows; ++w, ++seg) {
+          if (!__all_sync(0xffffffffu, seg_begin(seg))) goto done;
+          volatile const uint16_t* entries = seg_entries(seg);
+          const int n = n_entries[seg & 1];
+          for (int e = 0; e < n; ++e) {
+            const int tiles = entries[e] & 3, j = w * kWindowBlocks + (entries[e] >> 2);
+            if (!__all_sync(0xffffffffu, mbar_wait(v_full(vs), vph, abort_flag))) goto done;
+            const int valid = it.kv_len - j * 128;
+            if (valid < 128) {
+              for (int r = valid * 8 + lane; r < 128 * 8; r += 32)                // 16-byte units of rows valid .. 127
+                for (int pn = 0; pn < C::NP; ++pn)
+                  *reinterpret_cast<uint4*>(aligned + C::OFF_V + vs * C::TILE_BYTES + pn * C::PANEL + r * 16) = make_uint4(0, 0, 0, 0);
+              fence_proxy_async_smem();
+              __syncwarp();
             }
-            __syncwarp();
-            ++uses[i];
+            const uint64_t vd = vdesc0 + vs * kTileStep;
+            for (int i = 0; i < 2; ++i) {
+              if (!((tiles >> i) & 1)) continue;
+              if (!__all_sync(0xffffffffu, mbar_wait(p_full(i), done_uses[i] & 1u, abort_flag))) goto done;
+              tc_fence_after();
+              if (lane == 0) {
+#pragma unroll
+                for (int kk = 0; kk < 8; ++kk)
+                  umma_f16_ts(tO + i * 128, tP + i * 64 + kk * 8, vd + kk * (2048 >> 4), idesc_pv, more[i] || kk != 0);
+                if (i == 1 || tiles == 1) umma_commit(v_empty(vs));
+                umma_commit(o_full(i));
+              }
+              __syncwarp();
+              ++done_uses[i];
+              more[i] = true;
+            }
+            if (++vs == C::V_STAGES) { vs = 0; vph ^= 1u; }
           }
-          if (++vs == C::V_STAGES) { vs = 0; vph ^= 1u; }
+          __syncwarp();
+          if (lane == 0) mbar_arrive(seg_empty(seg & 1));
         }
-        __syncwarp();
-        if (w + 1 < n_windows && lane == 0) mbar_arrive(win_empty);
       }
     } else {
-      // ------------------------------------------------------------------ further windows' lists
-      for (int w = 1; w < n_windows; ++w) {
-        if (!__all_sync(0xffffffffu, mbar_wait(win_empty, (w - 1) & 1u, abort_flag))) goto done;
-        bits[lane] = 0;
-        __syncwarp();
-        for (int i = 0; i < 2; ++i) mark_blocks(bits + i * (kWindowBlocks / 32), lists[i], list_length(i), w * kWindowBlocks, n_kv, lane, 32);
-        __syncwarp();
-        const int n = order_blocks(bits, list, lane);
-        if (lane == 0) *n_entries = n;
-        __syncwarp();
-        if (lane == 0) mbar_arrive(win_full);
+      // ------------------------------------------------------------------ lists of the coming windows
+      for (int item = blockIdx.x; item < p.items; item += gridDim.x) {
+        const BlockItem it = block_item<C::Q_ROWS>(batch, p.n_heads, item);
+        const long long row = static_cast<long long>(it.head) * batch.first_qblock[batch.n] + batch.first_qblock[it.req] + 2 * it.qb;
+        for (int w = 0; w < it.n_windows; ++w, ++seg) {
+          if (lane < 2 * kWindowBlocks / 32) bits[lane] = 0;
+          __syncwarp();
+          mark_blocks(bits, p.index + row * p.ld_index, p.count + row, p.ld_index, w * kWindowBlocks, it.n_kv, lane);
+          if (it.tile1)
+            mark_blocks(bits + kWindowBlocks / 32, p.index + (row + 1) * p.ld_index, p.count + row + 1, p.ld_index, w * kWindowBlocks, it.n_kv, lane);
+          __syncwarp();
+          if (!__all_sync(0xffffffffu, mbar_wait(seg_empty(seg & 1), ((seg >> 1) & 1u) ^ 1u, abort_flag))) goto done;
+          const int n = order_blocks(bits, lists + (seg & 1) * kWindowBlocks, lane);
+          if (lane == 0) n_entries[seg & 1] = n;
+          __syncwarp();
+          if (lane == 0) mbar_arrive(seg_full(seg & 1));
+        }
       }
     }
   } else {
     // -------------------------------------------------------------------- softmax + accumulate (2 warpgroups)
     DIT_SETMAXNREG_INC(200);
     const int tile = (warp >> 2) - 1, quarter = warp & 3;
-    if (tile == 1 && !tile1_valid) goto done;
     const uint32_t lane_sel = static_cast<uint32_t>(quarter * 32) << 16;
     const uint32_t tSi = tS + lane_sel, tPi = tP + tile * 64 + lane_sel, tOi = tO + tile * 128 + lane_sel;
     const float c = p.scale_log2;
     const float2 c2 = make_float2(c, c);
     constexpr float kRescaleLog2 = 8.0f;       // O is rescaled when a row's maximum has grown by more than 2^8: P stays <= 2^8
-    float m_ref = -INFINITY, l = 0.f;
-    uint32_t use = 0;                          // key blocks of this tile so far
+    uint32_t use = 0;                          // key blocks of this warpgroup so far
 
-    for (int w = 0; w < n_windows; ++w) {
-      if (!__all_sync(0xffffffffu, window_begin(w))) goto done;
-      const int n = *n_entries;
-      for (int e = 0; e < n; ++e) {
-        const int entry = entries[e];
-        if (!((entry >> tile) & 1)) continue;
-        if (!__all_sync(0xffffffffu, mbar_wait(s_full(tile), use & 1u, abort_flag))) goto done;
-        tc_fence_after();
-        const int valid = kv_len - (w * kWindowBlocks + (entry >> 2)) * 128;
-        uint32_t sv[128];
-        __syncwarp();
+    for (int item = blockIdx.x; item < p.items; item += gridDim.x) {
+      const BlockItem it = block_item<C::Q_ROWS>(batch, p.n_heads, item);
+      float m_ref = -INFINITY, l = 0.f;
+      const uint32_t first_use = use;
+      for (int w = 0; w < it.n_windows; ++w, ++seg) {
+        if (!__all_sync(0xffffffffu, seg_begin(seg))) goto done;
+        volatile const uint16_t* entries = seg_entries(seg);
+        const int n = n_entries[seg & 1];
+        for (int e = 0; e < n; ++e) {
+          const int entry = entries[e];
+          if (!((entry >> tile) & 1)) continue;
+          if (!__all_sync(0xffffffffu, mbar_wait(s_full(tile), use & 1u, abort_flag))) goto done;
+          tc_fence_after();
+          const int valid = it.kv_len - (w * kWindowBlocks + (entry >> 2)) * 128;
+          uint32_t sv[128];
+          __syncwarp();
 #pragma unroll
-        for (int ch = 0; ch < 4; ++ch) tmem_ld32p(tSi + ch * 32, sv + ch * 32);
-        tmem_ld_wait();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(s_free);
-        if (valid < 128) {
+          for (int ch = 0; ch < 4; ++ch) tmem_ld32p(tSi + ch * 32, sv + ch * 32);
+          tmem_ld_wait();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(s_free);
+          if (valid < 128) {
 #pragma unroll
-          for (int i = 0; i < 128; ++i)
-            if (i >= valid) sv[i] = 0xff800000u;
-        }
-        float mx0 = -INFINITY, mx1 = -INFINITY, mx2 = -INFINITY, mx3 = -INFINITY;
+            for (int i = 0; i < 128; ++i)
+              if (i >= valid) sv[i] = 0xff800000u;
+          }
+          float mx0 = -INFINITY, mx1 = -INFINITY, mx2 = -INFINITY, mx3 = -INFINITY;
 #pragma unroll
-        for (int i = 0; i < 128; i += 8) {
-          mx0 = fmax3(mx0, __uint_as_float(sv[i]), __uint_as_float(sv[i + 1]));
-          mx1 = fmax3(mx1, __uint_as_float(sv[i + 2]), __uint_as_float(sv[i + 3]));
-          mx2 = fmax3(mx2, __uint_as_float(sv[i + 4]), __uint_as_float(sv[i + 5]));
-          mx3 = fmax3(mx3, __uint_as_float(sv[i + 6]), __uint_as_float(sv[i + 7]));
-        }
-        const float mx = fmaxf(fmaxf(mx0, mx1), fmaxf(mx2, mx3));
-        if (use == 0) {
-          m_ref = mx;
-        } else {
-          const bool grow = (mx - m_ref) * c > kRescaleLog2;
-          if (__any_sync(0xffffffffu, grow)) {
+          for (int i = 0; i < 128; i += 8) {
+            mx0 = fmax3(mx0, __uint_as_float(sv[i]), __uint_as_float(sv[i + 1]));
+            mx1 = fmax3(mx1, __uint_as_float(sv[i + 2]), __uint_as_float(sv[i + 3]));
+            mx2 = fmax3(mx2, __uint_as_float(sv[i + 4]), __uint_as_float(sv[i + 5]));
+            mx3 = fmax3(mx3, __uint_as_float(sv[i + 6]), __uint_as_float(sv[i + 7]));
+          }
+          const float mx = fmaxf(fmaxf(mx0, mx1), fmaxf(mx2, mx3));
+          if (use == first_use) {
+            m_ref = mx;
+          } else {
+            const bool grow = (mx - m_ref) * c > kRescaleLog2;
+            if (__any_sync(0xffffffffu, grow)) {
+              if (!__all_sync(0xffffffffu, mbar_wait(o_full(tile), (use - 1) & 1u, abort_flag))) goto done;
+              tc_fence_after();
+              const float alpha = grow ? exp2_approx((m_ref - mx) * c) : 1.0f;
+              if (grow) { m_ref = mx; l *= alpha; }
+#pragma unroll 1
+              for (int ch = 0; ch < D / 32; ++ch) {
+                uint32_t r[32];
+                __syncwarp();
+                tmem_ld32(tOi + ch * 32, r);
+                tmem_ld_wait();
+#pragma unroll
+                for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * alpha);
+                tmem_st32(tOi + ch * 32, r);
+              }
+              tmem_st_wait();
+            }
+          }
+          // a reference of -inf (every score so far -inf, from infinite inputs) would make the exponents NaN
+          const float neg_mc = m_ref == -INFINITY ? 0.f : -m_ref * c;
+          const float2 nm2 = make_float2(neg_mc, neg_mc);
+          float2 rs0 = make_float2(0.f, 0.f), rs1 = make_float2(0.f, 0.f);
+#pragma unroll
+          for (int i = 0; i < 128; i += 2) {
+            const float2 x = ffma2(make_float2(__uint_as_float(sv[i]), __uint_as_float(sv[i + 1])), c2, nm2);
+            const float2 ex = make_float2(exp2_approx(x.x), exp2_approx(x.y));
+            if (i & 2) rs1 = fadd2(rs1, ex); else rs0 = fadd2(rs0, ex);
+            sv[i >> 1] = pack16x2<BF16>(ex.x, ex.y);
+          }
+          if (use != first_use) {              // P is still read by this tile's previous product until that has finished
             if (!__all_sync(0xffffffffu, mbar_wait(o_full(tile), (use - 1) & 1u, abort_flag))) goto done;
             tc_fence_after();
-            const float alpha = grow ? exp2_approx((m_ref - mx) * c) : 1.0f;
-            if (grow) { m_ref = mx; l *= alpha; }
-#pragma unroll 1
-            for (int ch = 0; ch < D / 32; ++ch) {
-              uint32_t r[32];
-              __syncwarp();
-              tmem_ld32(tOi + ch * 32, r);
-              tmem_ld_wait();
-#pragma unroll
-              for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * alpha);
-              tmem_st32(tOi + ch * 32, r);
-            }
-            tmem_st_wait();
           }
-        }
-        // a reference of -inf (every score so far -inf, from infinite inputs) would make the exponents NaN
-        const float neg_mc = m_ref == -INFINITY ? 0.f : -m_ref * c;
-        const float2 nm2 = make_float2(neg_mc, neg_mc);
-        float2 rs0 = make_float2(0.f, 0.f), rs1 = make_float2(0.f, 0.f);
 #pragma unroll
-        for (int i = 0; i < 128; i += 2) {
-          const float2 x = ffma2(make_float2(__uint_as_float(sv[i]), __uint_as_float(sv[i + 1])), c2, nm2);
-          const float2 ex = make_float2(exp2_approx(x.x), exp2_approx(x.y));
-          if (i & 2) rs1 = fadd2(rs1, ex); else rs0 = fadd2(rs0, ex);
-          sv[i >> 1] = pack16x2<BF16>(ex.x, ex.y);
+          for (int ch = 0; ch < 4; ++ch) tmem_st16(tPi + ch * 16, *reinterpret_cast<const uint32_t(*)[16]>(sv + ch * 16));
+          tmem_st_wait();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(p_full(tile));
+          l += (rs0.x + rs0.y) + (rs1.x + rs1.y);
+          ++use;
         }
-        if (use > 0) {                         // P is still read by this tile's previous product until that has finished
-          if (!__all_sync(0xffffffffu, mbar_wait(o_full(tile), (use - 1) & 1u, abort_flag))) goto done;
-          tc_fence_after();
-        }
-#pragma unroll
-        for (int ch = 0; ch < 4; ++ch) tmem_st16(tPi + ch * 16, *reinterpret_cast<const uint32_t(*)[16]>(sv + ch * 16));
-        tmem_st_wait();
-        tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(p_full(tile));
-        l += (rs0.x + rs0.y) + (rs1.x + rs1.y);
-        ++use;
+        if (lane == 0) mbar_arrive(seg_empty(seg & 1));
       }
-      __syncwarp();
-      if (w + 1 < n_windows && lane == 0) mbar_arrive(win_empty);
-    }
-    {
-      constexpr int ROW_BYTES = D * 2, UNITS = ROW_BYTES / 16, ROWS_PER_STORE = 32 / UNITS;
-      const int row0 = qb * C::Q_ROWS + tile * 128 + quarter * 32;               // in the request
-      uint16_t* out0 = static_cast<uint16_t*>(p.out) + (static_cast<long long>(q_begin) + row0) * p.ld_out + head * D;
-      const int unit = lane % UNITS, sub = lane / UNITS;
-      if (use == 0) {                          // no key at all: zeros (Q may still be arriving: nothing is staged)
-        for (int rr = sub; rr < 32 && row0 + rr < q_len; rr += ROWS_PER_STORE)
-          *(reinterpret_cast<uint4*>(out0 + rr * p.ld_out) + unit) = make_uint4(0, 0, 0, 0);
-        goto done;
+      if (tile == 1 && !it.tile1) continue;
+      const int row = it.qb * C::Q_ROWS + tile * 128 + quarter * 32 + lane;       // in the request
+      uint16_t* out = static_cast<uint16_t*>(p.out) + (static_cast<long long>(it.q_begin) + row) * p.ld_out + it.head * D;
+      const bool any = use != first_use;       // without a key: zeros
+      if (any) {
+        if (!__all_sync(0xffffffffu, mbar_wait(o_full(tile), (use - 1) & 1u, abort_flag))) goto done;
+        tc_fence_after();
       }
-      if (!__all_sync(0xffffffffu, mbar_wait(o_full(tile), (use - 1) & 1u, abort_flag))) goto done;
-      tc_fence_after();
       const float inv = l == 0.f ? 0.f : 1.0f / l;
-      // rows leave through the shared memory of the tile's Q (its last score product has finished), 16-byte units
-      // XOR-swizzled by the row, so that stores cover whole rows
-      uint8_t* stage = aligned + C::OFF_Q + tile * C::TILE_BYTES + quarter * 32 * ROW_BYTES;
 #pragma unroll 1
       for (int ch = 0; ch < D / 32; ++ch) {
         uint32_t r[32];
         __syncwarp();
-        tmem_ld32(tOi + ch * 32, r);
-        tmem_ld_wait();
+        if (any) {
+          tmem_ld32(tOi + ch * 32, r);
+          tmem_ld_wait();
+        } else {
 #pragma unroll
-        for (int v = 0; v < 4; ++v) {
-          uint32_t wd[4];
-#pragma unroll
-          for (int h = 0; h < 4; ++h) wd[h] = pack16x2<BF16>(__uint_as_float(r[8 * v + 2 * h]) * inv, __uint_as_float(r[8 * v + 2 * h + 1]) * inv);
-          *reinterpret_cast<uint4*>(stage + lane * ROW_BYTES + (((ch * 4 + v) ^ (lane & (UNITS - 1))) << 4)) = make_uint4(wd[0], wd[1], wd[2], wd[3]);
+          for (int i = 0; i < 32; ++i) r[i] = 0u;
         }
-      }
-      __syncwarp();
-#pragma unroll 4
-      for (int it = 0; it < 32 / ROWS_PER_STORE; ++it) {
-        const int rr = it * ROWS_PER_STORE + sub;
-        if (row0 + rr < q_len) {
-          const uint4 val = *reinterpret_cast<const uint4*>(stage + rr * ROW_BYTES + ((unit ^ (rr & (UNITS - 1))) << 4));
-          *(reinterpret_cast<uint4*>(out0 + rr * p.ld_out) + unit) = val;
+        if (row < it.q_len) {
+#pragma unroll
+          for (int v = 0; v < 2; ++v) {        // a lane writes its own row, a whole 32-byte sector per store
+            uint32_t wd[8];
+#pragma unroll
+            for (int h = 0; h < 8; ++h) wd[h] = pack16x2<BF16>(__uint_as_float(r[16 * v + 2 * h]) * inv, __uint_as_float(r[16 * v + 2 * h + 1]) * inv);
+            uint16_t* at = out + ch * 32 + v * 16;
+            if (p.wide_out) {
+              st_global_v8(at, wd);
+            } else {
+              reinterpret_cast<uint4*>(at)[0] = make_uint4(wd[0], wd[1], wd[2], wd[3]);
+              reinterpret_cast<uint4*>(at)[1] = make_uint4(wd[4], wd[5], wd[6], wd[7]);
+            }
+          }
         }
       }
     }

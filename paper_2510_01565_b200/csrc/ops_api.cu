@@ -221,7 +221,10 @@ cudaError_t launch_attend(const DeviceState& d, const dit_attention_batch& a, co
     while (splits < 8 && 2 * splits <= listed && 2ll * splits * items <= 2ll * d.num_sms) splits *= 2;
     return launch_rows<D, BF16>(tmK, tmV, p, a, b, splits, st);
   }
-  block_attention_kernel<D, BF16><<<static_cast<unsigned>(qblocks) * a.n_heads, BlockAttnCfg<D>::THREADS, BlockAttnCfg<D>::SMEM_BYTES, st>>>(tmQ, tmK, tmV, p, b);
+  BlockAttnParams q = p;
+  q.items = qblocks * a.n_heads;
+  q.wide_out = aligned(p.out, 32) && p.ld_out % 16 == 0;
+  block_attention_kernel<D, BF16><<<std::min(q.items, d.num_sms), BlockAttnCfg<D>::THREADS, BlockAttnCfg<D>::SMEM_BYTES, st>>>(tmQ, tmK, tmV, q, b);
   return cudaGetLastError();
 }
 

@@ -135,7 +135,7 @@ def test_all_blocks_listed_is_dense_attention(B, q_lens):
 
 @pytest.mark.parametrize("rows", [1, 13, 140])
 def test_more_key_blocks_than_one_window(B, rows):
-    """70000 keys (547 blocks: two windows of the tiled kernel), lists that reach into both, into the second only, or neither."""
+    """70000 keys (547 blocks: three windows of the tiled kernel), lists that reach into all of them, into the last only, or the first."""
     import torch
     heads, dim, kv = 2, 64, 70000
     q, k, v = draw(17, [rows], [kv], heads, dim, "float16")
