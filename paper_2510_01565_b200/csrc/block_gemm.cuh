@@ -40,26 +40,35 @@ struct BlockGemmParams {
 };
 
 namespace bgemm {
-constexpr int BM = 128, BN = 256, STAGES = 4;
+constexpr int BM = 128, BN = 256;
 constexpr int A_BYTES = BM * 128, B_BYTES = (BN / 2) * 128;
 constexpr int STAGE_BYTES = A_BYTES + B_BYTES;
 constexpr int EPI_WARPS = 8;
 constexpr int THREADS = 128 + 32 * EPI_WARPS;
 constexpr int REGS_ISSUE = 56, REGS_EPILOGUE = 224;   // (56 + 2 * 224) * 32 <= 16384 per scheduler
-constexpr int STAGE_OUT_BYTES = 8192;                 // per epilogue warp: 32 rows x 256 bytes, as two swizzled boxes of 128 bytes x 32 rows
-constexpr int BIAS_BYTES = 512;                       // per epilogue warp: the bias of its 128 columns
-constexpr int OFF_OUT = STAGES * STAGE_BYTES, OFF_BAR = OFF_OUT + EPI_WARPS * (STAGE_OUT_BYTES + BIAS_BYTES);
-constexpr int SMEM_BYTES = OFF_BAR + 256 + 1024;
+constexpr int BOX_BYTES = 4096;                       // 128 bytes x 32 rows of the output
+// Per epilogue warp: two boxes of its 32 rows, or, where a residual is added, all four of its 32 rows x 128 fp32 columns: the
+// residual arrives there by TMA during the main loop and is replaced by the result in place.  Three stages of operands
+// are left room for then instead of four (five and six measured no faster than four).
+template <int EPI>
+struct Cfg {
+  static constexpr bool kResid = EPI == kBlkGateResidF32;
+  static constexpr int STAGES = kResid ? 3 : 4;
+  static constexpr int STAGE_OUT_BYTES = (kResid ? 4 : 2) * BOX_BYTES;
+  static constexpr int BIAS_BYTES = kResid ? 0 : 512;         // the bias of the warp's 128 columns
+  static constexpr int OFF_OUT = STAGES * STAGE_BYTES, OFF_BAR = OFF_OUT + EPI_WARPS * (STAGE_OUT_BYTES + BIAS_BYTES);
+  static constexpr int SMEM_BYTES = OFF_BAR + 256 + 1024;
+  static_assert(SMEM_BYTES <= 227 * 1024, "shared memory of one CTA");
+};
 }  // namespace bgemm
 
 // Writes 32 columns x 32 rows of a warp (this lane's row in v) through `stage`, so that a store instruction covers
-// whole sectors of a few rows.  `rows_ok`: bit r set when row r of the warp's 32 exists.  16-bit outputs: rows
+// whole sectors of a few rows (outputs whose rows start off 16-byte boundaries, and ragged columns).  `rows_ok`: bit r set when row r of the warp's 32 exists.  16-bit outputs: rows
 // padded to 80 bytes; fp32: two halves of 16 rows padded to 144 bytes.
 template <int EPI>
-__device__ __forceinline__ void block_store_chunk(const BlockGemmParams& p, const SeqInfo& seq, uint8_t* stage, float (&v)[32],
-                                                  int lane, long long row0, int col0, unsigned rows_ok) {
+__device__ __forceinline__ void block_store_chunk(const BlockGemmParams& p, uint8_t* stage, float (&v)[32], int lane, long long row0, int col0, unsigned rows_ok) {
   const bool whole = p.vec_out && col0 + 32 <= p.N;                   // warp-uniform
-  if constexpr (EPI == kBlkF32 || EPI == kBlkGateResidF32) {
+  if constexpr (EPI == kBlkF32) {
     float* st = reinterpret_cast<float*>(stage);
     float* out = static_cast<float*>(p.out);
 #pragma unroll
@@ -75,27 +84,13 @@ __device__ __forceinline__ void block_store_chunk(const BlockGemmParams& p, cons
         for (int it = 0; it < 4; ++it) {
           const int rr = hf * 16 + it * 4 + (lane >> 3);
           if ((rows_ok >> rr) & 1u) {
-            float4 a = *reinterpret_cast<const float4*>(st + (rr & 15) * 36 + cg);
-            const long long at = (row0 + rr) * p.ld_out + col0 + cg;
-            if (EPI == kBlkGateResidF32) {
-              const int req = find_request(seq, p.row0 + static_cast<int>(row0) + rr);
-              const float4 g = __ldg(reinterpret_cast<const float4*>(p.gate + req * p.gate_stride + col0 + cg));
-              const float4 x = *reinterpret_cast<const float4*>(p.resid + at);
-              const float2 o0 = ffma2(make_float2(g.x, g.y), make_float2(a.x, a.y), make_float2(x.x, x.y));
-              const float2 o1 = ffma2(make_float2(g.z, g.w), make_float2(a.z, a.w), make_float2(x.z, x.w));
-              a = make_float4(o0.x, o0.y, o1.x, o1.y);
-            }
-            *reinterpret_cast<float4*>(out + at) = a;
+            *reinterpret_cast<float4*>(out + (row0 + rr) * p.ld_out + col0 + cg) = *reinterpret_cast<const float4*>(st + (rr & 15) * 36 + cg);
           }
         }
       } else if (col0 + lane < p.N) {
         for (int r = 0; r < 16; ++r) {
           const int rr = hf * 16 + r;
-          if (!((rows_ok >> rr) & 1u)) continue;
-          const long long at = (row0 + rr) * p.ld_out + col0 + lane;
-          float v1 = st[r * 36 + lane];
-          if (EPI == kBlkGateResidF32) v1 = fmaf(p.gate[find_request(seq, p.row0 + static_cast<int>(row0) + rr) * p.gate_stride + col0 + lane], v1, p.resid[at]);
-          out[at] = v1;
+          if ((rows_ok >> rr) & 1u) out[(row0 + rr) * p.ld_out + col0 + lane] = st[r * 36 + lane];
         }
       }
       __syncwarp();
@@ -142,18 +137,21 @@ __device__ __forceinline__ void block_store_chunk(const BlockGemmParams& p, cons
 template <int EPI>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(bgemm::THREADS, 1)
 gemm_block128_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
-                          const __grid_constant__ CUtensorMap tmOut, const BlockGemmParams p,
+                          const __grid_constant__ CUtensorMap tmOut, const __grid_constant__ CUtensorMap tmResid, const BlockGemmParams p,
                           const __grid_constant__ SeqInfo seq) {
   using namespace bgemm;
+  using C = Cfg<EPI>;
+  constexpr int STAGES = C::STAGES;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw);
   const uint32_t base = (raw + 1023u) & ~1023u;
   uint8_t* aligned = smem_raw + (base - raw);
-  const uint32_t bar0 = base + OFF_BAR;
+  const uint32_t bar0 = base + C::OFF_BAR;
   auto full_bar = [&](int s) { return bar0 + 8u * s; };
   auto done_bar = [&](int s, int h) { return bar0 + 8u * (STAGES + 2 * s + h); };      // half h's MMAs of stage s have completed
   auto tempty_bar = [&](int buf, int h) { return bar0 + 8u * (3 * STAGES + 2 * buf + h); };
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(aligned + OFF_BAR + 8 * (3 * STAGES + 4));
+  auto resid_bar = [&](int w) { return bar0 + 8u * (3 * STAGES + 4 + w); };            // epilogue warp w's residual rows have arrived
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(aligned + C::OFF_BAR + 8 * (3 * STAGES + 4 + EPI_WARPS));
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -166,6 +164,7 @@ gemm_block128_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_
   if (threadIdx.x == 0) {
     for (int s = 0; s < STAGES; ++s) { mbar_init(full_bar(s), 1); mbar_init(done_bar(s, 0), 1); mbar_init(done_bar(s, 1), 1); }
     for (int a = 0; a < 4; ++a) mbar_init(tempty_bar(a >> 1, a & 1), 2 * EPI_WARPS);
+    for (int w = 0; w < EPI_WARPS; ++w) mbar_init(resid_bar(w), 1);
     *abort_flag = 0;
     fence_mbar_init();
   }
@@ -223,8 +222,9 @@ gemm_block128_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_
     const int quarter = warp & 3, chalf = (warp - 4) >> 2;
     const uint32_t t_row = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) + chalf * 64;
     const uint32_t tempty_leader = map_to_cta(tempty_bar(0, 0), 0);
-    uint8_t* stage = aligned + OFF_OUT + (warp - 4) * STAGE_OUT_BYTES;
-    float* bias_of = reinterpret_cast<float*>(aligned + OFF_OUT + EPI_WARPS * STAGE_OUT_BYTES + (warp - 4) * BIAS_BYTES);
+    uint8_t* stage = aligned + C::OFF_OUT + (warp - 4) * C::STAGE_OUT_BYTES;
+    float* bias_of = reinterpret_cast<float*>(aligned + C::OFF_OUT + EPI_WARPS * C::STAGE_OUT_BYTES + (warp - 4) * C::BIAS_BYTES);
+    uint32_t resid_phase = 0;
     // What a tile needs from memory before its first group: requested for the next tile before the current one is
     // written.  Lane l holds the bias of columns l, 32 + l, 64 + l, 96 + l; scales run two groups ahead of their use.
     struct Ahead { int row0, n0; const float *sa, *sb; float bias[4], sa_at[3], sb_at[3]; } next;
@@ -235,7 +235,7 @@ gemm_block128_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_
       next.sa = p.sa + (next.row0 + lane < p.M ? next.row0 + lane : 0);
       next.sb = p.sb + static_cast<long long>(next.n0 < p.N ? next.n0 >> 7 : 0) * groups;
 #pragma unroll
-      for (int c = 0; c < 4; ++c) next.bias[c] = (p.bias && next.n0 + c * 32 + lane < p.N) ? __ldg(p.bias + next.n0 + c * 32 + lane) : 0.f;
+      for (int c = 0; c < 4; ++c) next.bias[c] = (!C::kResid && p.bias && next.n0 + c * 32 + lane < p.N) ? __ldg(p.bias + next.n0 + c * 32 + lane) : 0.f;
 #pragma unroll
       for (int d = 0; d < 2; ++d) {
         const int at = min(d, groups - 1);
@@ -249,8 +249,17 @@ gemm_block128_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_
       const int row0 = next.row0, n0 = next.n0;
       const float *sa = next.sa, *sb = next.sb;
       float sa_at[3] = {next.sa_at[0], next.sa_at[1], 0.f}, sb_at[3] = {next.sb_at[0], next.sb_at[1], 0.f};
+      const bool mine = n0 < p.N && row0 < p.M;                        // something of this warp's part exists (warp-uniform)
+      if constexpr (C::kResid) {
+        if (mine && lane == 0) {
+          bulk_store_read_done();                                      // the previous tile's rows have left
+          mbar_arrive_expect_tx(resid_bar(warp - 4), 4 * BOX_BYTES);
+          for (int c = 0; c < 4; ++c) tma_load_2d(smem_u32(stage) + c * BOX_BYTES, &tmResid, n0 + c * 32, row0, resid_bar(warp - 4));
+        }
+      } else {
 #pragma unroll
-      for (int c = 0; c < 4; ++c) bias_of[c * 32 + lane] = next.bias[c];
+        for (int c = 0; c < 4; ++c) bias_of[c * 32 + lane] = next.bias[c];
+      }
       float2 acc[64];
 #pragma unroll
       for (int i = 0; i < 64; ++i) acc[i] = make_float2(0.f, 0.f);
@@ -284,14 +293,46 @@ gemm_block128_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_
         buf ^= 1;
       }
       if (t + num_pairs < num_tiles) request(t + num_pairs);
-      if (n0 >= p.N || row0 >= p.M) continue;                          // nothing of this warp's part exists (warp-uniform)
+      if (!mine) continue;
+      if constexpr (C::kResid) {
+        // out = resid + gate (acc + bias), where the residual lies in the boxes: column 32 c + 4 q of the lane's row in 16-byte unit q of box c
+        const int row = row0 + lane;
+        const float* gate = p.gate + (row < p.M ? find_request(seq, p.row0 + row) : 0) * p.gate_stride + n0;
+        if (!__all_sync(0xffffffffu, mbar_wait(resid_bar(warp - 4), resid_phase, abort_flag))) goto done;
+        resid_phase ^= 1u;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          if (n0 + c * 32 >= p.N) break;                               // warp-uniform; N is a multiple of 32 here
+#pragma unroll
+          for (int q = 0; q < 8; ++q) {
+            const int at = c * 32 + q * 4;
+            const float4 g = __ldg(reinterpret_cast<const float4*>(gate + at));
+            const float4 b = p.bias ? __ldg(reinterpret_cast<const float4*>(p.bias + n0 + at)) : make_float4(0.f, 0.f, 0.f, 0.f);
+            float4* cell = reinterpret_cast<float4*>(stage + c * BOX_BYTES + lane * 128 + ((q ^ (lane & 7)) << 4));
+            const float4 x = *cell;
+            const float2 lo = fadd2(acc[at / 2], make_float2(b.x, b.y)), hi = fadd2(acc[at / 2 + 1], make_float2(b.z, b.w));
+            const float2 o0 = ffma2(make_float2(g.x, g.y), lo, make_float2(x.x, x.y)), o1 = ffma2(make_float2(g.z, g.w), hi, make_float2(x.z, x.w));
+            *cell = make_float4(o0.x, o0.y, o1.x, o1.y);
+          }
+        }
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) {
+          for (int c = 0; c < 4; ++c)
+            if (n0 + c * 32 < p.N) tma_store_2d(&tmOut, smem_u32(stage) + c * BOX_BYTES, n0 + c * 32, row0);
+          bulk_store_commit();
+        }
+        __syncwarp();
+        continue;
+      }
       __syncwarp();                                                    // bias_of is complete
       auto finished = [&](int i) {                                     // columns 2i .. 2i + 3 of the warp's 128, i even
         const float4 b4 = *reinterpret_cast<const float4*>(bias_of + 2 * i);
         const float2 lo = fadd2(acc[i], make_float2(b4.x, b4.y)), hi = fadd2(acc[i + 1], make_float2(b4.z, b4.w));
         return make_float4(lo.x, lo.y, hi.x, hi.y);
       };
-      if (EPI != kBlkGateResidF32 && p.vec_out) {
+      if constexpr (!C::kResid) {
+      if (p.vec_out) {
         // Through shared memory and out by TMA: the warp is free again as soon as its rows lie there, and what lies
         // outside the matrix is dropped.  A box is 128 bytes x 32 rows, 16-byte units XOR-swizzled by the row.
         constexpr bool kWide = EPI == kBlkF32;
@@ -341,7 +382,8 @@ gemm_block128_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_
           const float4 v4 = finished(c * 16 + i);
           v[2 * i] = v4.x; v[2 * i + 1] = v4.y; v[2 * i + 2] = v4.z; v[2 * i + 3] = v4.w;
         }
-        block_store_chunk<EPI>(p, seq, stage, v, lane, row0, n0 + c * 32, rows_ok);
+        block_store_chunk<EPI>(p, stage, v, lane, row0, n0 + c * 32, rows_ok);
+      }
       }
     }
   }

@@ -44,7 +44,7 @@ cudaError_t allow_smem(Kernel kernel, int bytes) {
 }
 template <int EPI>
 cudaError_t allow_gemm() {
-  cudaError_t e = allow_smem(&gemm_block128_pair_kernel<EPI>, bgemm::SMEM_BYTES);
+  cudaError_t e = allow_smem(&gemm_block128_pair_kernel<EPI>, bgemm::Cfg<EPI>::SMEM_BYTES);
   if (e == cudaSuccess) e = allow_smem(&gemm_block128_split_kernel<EPI, 16>, SplitCfg<16>::SMEM_BYTES);
   if (e == cudaSuccess) e = allow_smem(&gemm_block128_split_kernel<EPI, 32>, SplitCfg<32>::SMEM_BYTES);
   if (e == cudaSuccess) e = allow_smem(&gemm_block128_split_kernel<EPI, 64>, SplitCfg<64>::SMEM_BYTES);
@@ -91,7 +91,7 @@ cudaError_t device_state(const DeviceState** out, bool* unsupported) {
         (e = allow_smem(&block_select_kernel, kSelectSmemMax)) != cudaSuccess)
       return e;
     cudaLaunchConfig_t lc = {};
-    lc.gridDim = dim3(s.num_sms & ~1); lc.blockDim = dim3(bgemm::THREADS); lc.dynamicSmemBytes = bgemm::SMEM_BYTES;
+    lc.gridDim = dim3(s.num_sms & ~1); lc.blockDim = dim3(bgemm::THREADS); lc.dynamicSmemBytes = bgemm::Cfg<kBlkF16>::SMEM_BYTES;
     cudaLaunchAttribute at;
     at.id = cudaLaunchAttributeClusterDimension;
     at.val.clusterDim.x = 2; at.val.clusterDim.y = 1; at.val.clusterDim.z = 1;
@@ -127,14 +127,14 @@ bool byte_map(CUtensorMap* m, const void* ptr, uint64_t inner, uint64_t rows, ui
 }
 
 // Output matrix: boxes of 128 bytes x 32 rows, 128-byte swizzle.
-bool out_map(CUtensorMap* m, const BlockProduct& b) {
-  const bool wide = b.epilogue == kBlkF32;
+bool out_map(CUtensorMap* m, const BlockProduct& b, const void* matrix) {
+  const bool wide = b.epilogue == kBlkF32 || b.epilogue == kBlkGateResidF32;
   const cuuint64_t dims[2] = {static_cast<cuuint64_t>(b.n), static_cast<cuuint64_t>(b.m)};
   const cuuint64_t strides[1] = {static_cast<cuuint64_t>(b.ld_out) * (wide ? 4 : 2)};
   const cuuint32_t box[2] = {wide ? 32u : 64u, 32u};
   const cuuint32_t estr[2] = {1, 1};
   const CUtensorMapDataType type = wide ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : (b.epilogue == kBlkBF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16);
-  return g_encode(m, type, 2, b.out, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+  return g_encode(m, type, 2, const_cast<void*>(matrix), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                   CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -252,7 +252,9 @@ cudaError_t launch_product(const DeviceState& d, const BlockProduct& b, BlockGem
   const long long pair_tiles = static_cast<long long>((p.M + 255) / 256) * ((p.N + 255) / 256);
   const long long planned_tiles = static_cast<long long>((rows + 255) / 256) * ((p.N + 255) / 256);
   // Few rows, or too few 256 x 256 tiles to fill the device: the split kernel.
-  if (rows <= 128 || planned_tiles < d.pairs / 2) {
+  // The pair kernel moves residual rows in boxes of 32 columns and reads bias and gates in fours.
+  const bool resid_ok = EPI != kBlkGateResidF32 || (p.vec_out && aligned(p.resid, 16) && aligned(p.bias, 16) && aligned(p.gate, 16) && p.gate_stride % 4 == 0 && p.N % 32 == 0);
+  if (rows <= 128 || planned_tiles < d.pairs / 2 || !resid_ok) {
     const int bt = rows <= 16 ? 16 : (rows <= 32 ? 32 : (rows <= 64 ? 64 : 128));
     const long long tiles = tiles_n * ((rows + bt - 1) / bt);
     int splits = 1;
@@ -273,9 +275,10 @@ cudaError_t launch_product(const DeviceState& d, const BlockProduct& b, BlockGem
     p.band = cost_cols < cost_rows ? -static_cast<int>(cb) : static_cast<int>(rb);
   }
   const int grid = 2 * static_cast<int>(std::min<long long>(pair_tiles, d.pairs));
-  CUtensorMap tmOut = tmA;                       // unused where the output is written directly
-  if (p.vec_out && EPI != kBlkGateResidF32 && !out_map(&tmOut, b)) return cudaErrorInvalidValue;
-  gemm_block128_pair_kernel<EPI><<<grid, bgemm::THREADS, bgemm::SMEM_BYTES, st>>>(tmA, tmB, tmOut, p, seq);
+  CUtensorMap tmOut = tmA, tmResid = tmA;        // unused where the output is written directly, without a residual
+  if (p.vec_out && !out_map(&tmOut, b, b.out)) return cudaErrorInvalidValue;
+  if (EPI == kBlkGateResidF32 && !out_map(&tmResid, b, b.resid)) return cudaErrorInvalidValue;
+  gemm_block128_pair_kernel<EPI><<<grid, bgemm::THREADS, bgemm::Cfg<EPI>::SMEM_BYTES, st>>>(tmA, tmB, tmOut, tmResid, p, seq);
   return cudaGetLastError();
 }
 
