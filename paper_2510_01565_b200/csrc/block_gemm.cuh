@@ -263,6 +263,21 @@ gemm_block128_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_
       float2 acc[64];
 #pragma unroll
       for (int i = 0; i < 64; ++i) acc[i] = make_float2(0.f, 0.f);
+      // A group's half is read out in two pieces of 32 columns; the next piece is on its way (into the other buffer)
+      // while one is added.  Piece by piece with nothing ahead, waits, reads and additions of a half took about 550 cycles
+      // one after the other, and with two warps per scheduler these, not the MMAs, set the pace.
+      uint32_t ra[32], rb[32];
+      auto await = [&](int h) { return __all_sync(0xffffffffu, ready || mbar_wait(done_bar(stage_of, h), phase, abort_flag)); };
+      auto fetch = [&](int h, int piece, uint32_t (&r)[32]) { tmem_ld32(t_row + buf * BN + h * 128 + piece * 32, r); };
+      auto release = [&](int h) {              // the half is in registers: hand its columns back
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cluster_light(tempty_leader + 8u * (2 * buf + h));
+      };
+      if (!await(0)) goto done;
+      tc_fence_after();
+      fetch(0, 0, ra);
+      tmem_ld_wait();
       for (int g = 0; g < groups; ++g) {
         {
           const int at = min(g + 2, groups - 1);
@@ -270,27 +285,37 @@ gemm_block128_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_
         }
         const float fs = sa_at[0] * sb_at[0];
         const float2 f = make_float2(fs, fs);
+        auto add = [&](const uint32_t (&r)[32], int first) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          if (!__all_sync(0xffffffffu, ready || mbar_wait(done_bar(stage_of, h), phase, abort_flag))) goto done;
+          for (int i = 0; i < 16; ++i)
+            ffma2_here(acc[first + i], make_float2(__uint_as_float(r[2 * i]), __uint_as_float(r[2 * i + 1])), f);
+        };
+        fetch(0, 1, rb);
+        add(ra, 0);
+        tmem_ld_wait();
+        release(0);
+        ready = mbar_test_wait(done_bar(stage_of, 1), phase);
+        if (!await(1)) goto done;
+        tc_fence_after();
+        fetch(1, 0, ra);
+        add(rb, 16);
+        tmem_ld_wait();
+        fetch(1, 1, rb);
+        add(ra, 32);
+        tmem_ld_wait();
+        release(1);
+        if (++stage_of == STAGES) { stage_of = 0; phase ^= 1u; }
+        buf ^= 1;
+        ready = mbar_test_wait(done_bar(stage_of, 0), phase);
+        if (g + 1 < groups) {
+          if (!await(0)) goto done;
           tc_fence_after();
-          uint32_t r[64];
-          __syncwarp();
-          tmem_ld32p(t_row + buf * BN + h * 128, r);
-          tmem_ld32p(t_row + buf * BN + h * 128 + 32, r + 32);
-          tmem_ld_wait();
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive_cluster_light(tempty_leader + 8u * (2 * buf + h));
-          if (h == 1 && ++stage_of == STAGES) { stage_of = 0; phase ^= 1u; }
-          ready = mbar_test_wait(done_bar(stage_of, h ^ 1), phase);    // the answer arrives under the multiply-adds
-#pragma unroll
-          for (int i = 0; i < 32; ++i)
-            acc[h * 32 + i] = ffma2(make_float2(__uint_as_float(r[2 * i]), __uint_as_float(r[2 * i + 1])), f, acc[h * 32 + i]);
+          fetch(0, 0, ra);
         }
+        add(rb, 48);
+        tmem_ld_wait();
 #pragma unroll
         for (int d = 0; d < 2; ++d) { sa_at[d] = sa_at[d + 1]; sb_at[d] = sb_at[d + 1]; }
-        buf ^= 1;
       }
       if (t + num_pairs < num_tiles) request(t + num_pairs);
       if (!mine) continue;

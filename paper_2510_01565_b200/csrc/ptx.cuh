@@ -379,6 +379,12 @@ __device__ __forceinline__ float2 ffma2(float2 a, float2 b, float2 c) {
         "l"(*reinterpret_cast<unsigned long long*>(&c)));
   return *reinterpret_cast<float2*>(&d);
 }
+// c += a * b, kept where it is written (between an asynchronous request and the wait for it)
+__device__ __forceinline__ void ffma2_here(float2& c, float2 a, float2 b) {
+  asm volatile("fma.rn.f32x2 %0, %1, %2, %0;"
+               : "+l"(*reinterpret_cast<unsigned long long*>(&c))
+               : "l"(*reinterpret_cast<unsigned long long*>(&a)), "l"(*reinterpret_cast<unsigned long long*>(&b)));
+}
 __device__ __forceinline__ float2 fadd2(float2 a, float2 b) {
 #ifdef DIT_NO_F32X2
   return make_float2(a.x + b.x, a.y + b.y);
