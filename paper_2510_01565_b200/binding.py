@@ -640,21 +640,20 @@ def _matrix(t, what: str) -> int:
 def _launch(fn, args, stream, tensors):
     """Calls fn(*args, stream) with the tensors' device current; they must share it."""
     import torch
-    device = tensors[0].device
+    index = tensors[0].get_device()
     for t in tensors:
-        if t is not None and t.device != device:
+        if t is not None and t.get_device() != index:
             _refuse("tensors lie on different devices")
-    index = device.index
     if stream is None:
         raw = torch._C._cuda_getCurrentRawStream(index)
     else:
-        if stream.device != device:
+        if stream.device.index != index:
             _refuse("the stream belongs to another device than the tensors")
         raw = stream.cuda_stream
     if torch._C._cuda_getDevice() == index:
         st = fn(*args, raw)
     else:
-        with torch.cuda.device(device):
+        with torch.cuda.device(index):
             st = fn(*args, raw)
     if st != DIT_OK:
         raise DitError(st, load_library().dit_status_string(st).decode())
@@ -667,9 +666,9 @@ def _data(t):
 def _codes_for(rows: int, cols: int, device):
     """Uninitialised e4m3 codes [rows, cols] whose rows start on 16-byte boundaries."""
     import torch
-    if cols % 16 == 0:
-        return torch.empty((rows, cols), dtype=torch.float8_e4m3fn, device=device)
-    return torch.empty((rows, (cols + 15) // 16 * 16), dtype=torch.float8_e4m3fn, device=device)[:, :cols]
+    if cols % 16 == 0:                       # (sizes as separate arguments: a tuple costs half as much again)
+        return torch.empty(rows, cols, dtype=torch.float8_e4m3fn, device=device)
+    return torch.empty(rows, (cols + 15) // 16 * 16, dtype=torch.float8_e4m3fn, device=device)[:, :cols]
 
 
 def _pitch(ld: int, rows: int) -> int:
@@ -688,7 +687,7 @@ def dit_quantize_block128(x, codes=None, scales=None, stream=None):
     elif codes.dtype != torch.float8_e4m3fn or codes.shape != x.shape:
         _refuse("codes must be float8_e4m3fn, shaped like x")
     if scales is None:
-        scales = torch.empty((groups, rows), dtype=torch.float32, device=x.device)
+        scales = torch.empty(groups, rows, dtype=torch.float32, device=x.device)
     elif scales.dtype != torch.float32 or scales.shape != (groups, rows):
         _refuse("scales must be fp32 [ceil(cols / 128), rows]")
     ld_scales = _matrix(scales, "scales")
@@ -708,7 +707,7 @@ def dit_quantize_weight_block128(w, codes=None, scales=None, stream=None):
     elif codes.dtype != torch.float8_e4m3fn or codes.shape != (n_out, n_in):
         _refuse("codes must be float8_e4m3fn [out, in]")
     if scales is None:
-        scales = torch.empty(shape, dtype=torch.float32, device=w.device)
+        scales = torch.empty(*shape, dtype=torch.float32, device=w.device)
     elif scales.dtype != torch.float32 or scales.shape != shape or not scales.is_contiguous():
         _refuse("scales must be contiguous fp32 [ceil(out / 128), ceil(in / 128)]")
     _launch(lib.dit_quantize_weight_block128, (w.data_ptr(), _type_code(w.dtype), ld, n_in, n_out, codes.data_ptr(),
@@ -735,7 +734,7 @@ def dit_gemm_block128(a, a_scales, b, b_scales, bias=None, out=None, out_dtype=N
     if bias is not None and (not bias.is_cuda or bias.dtype != torch.float32 or not bias.is_contiguous() or bias.shape != (n,)):
         _refuse("bias must be contiguous fp32 [n]")
     if out is None:
-        out = torch.empty((m, n), dtype=out_dtype or torch.float16, device=a.device)
+        out = torch.empty(m, n, dtype=out_dtype or torch.float16, device=a.device)
     elif out.shape != (m, n) or (out_dtype is not None and out.dtype != out_dtype):
         _refuse("out must be [m, n] of out_dtype")
     args = DitGemmBlock128Args(a.data_ptr(), a_scales.data_ptr(), b.data_ptr(), b_scales.data_ptr(), _data(bias), out.data_ptr(), _pitch(lda, m),
@@ -784,9 +783,9 @@ def dit_select_blocks(q, k, q_lens, kv_lens, n_heads: int, keep, tail_rows=None,
         widest = max(keep, default=1)
         if widest < 1:
             _refuse("keep must be at least 1")
-        index = torch.empty((n_heads, q_blocks, widest), dtype=torch.int32, device=q.device)
+        index = torch.empty(n_heads, q_blocks, widest, dtype=torch.int32, device=q.device)
     if count is None:
-        count = torch.empty((n_heads, q_blocks), dtype=torch.int32, device=q.device)
+        count = torch.empty(n_heads, q_blocks, dtype=torch.int32, device=q.device)
     _check_lists(index, count, n_heads, q_blocks)
     if workspace is None:
         workspace = torch.empty(max(lib.dit_select_blocks_workspace(C.byref(batch)), 16), dtype=torch.uint8, device=q.device)
@@ -806,7 +805,7 @@ def dit_block_attention(q, k, v, q_lens, kv_lens, n_heads: int, index, count, sc
     batch, q_blocks = _attention_batch(q, k, v, q_lens, kv_lens, n_heads)
     _check_lists(index, count, n_heads, q_blocks)
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        out = torch.empty(*q.shape, dtype=q.dtype, device=q.device)
     elif out.shape != q.shape or out.dtype != q.dtype:
         _refuse("out must be shaped and typed like q")
     _launch(lib.dit_block_attention, (C.byref(batch), index.data_ptr(), count.data_ptr(), max(index.shape[2], 1), scale, out.data_ptr(),

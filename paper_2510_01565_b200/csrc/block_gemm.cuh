@@ -596,10 +596,21 @@ gemm_block128_split_kernel(const __grid_constant__ CUtensorMap tmA, const __grid
     if (warp >= 2 && col < p.N) {
       const float bias = p.bias ? __ldg(p.bias + col) : 0.f;
       const int rows = min(BT, p.M - m0);
-      for (int i = rank; i < rows; i += splits) {
-        float v = bias;
-        for (int r = 0; r < splits; ++r) v += ld_cluster_f32(map_to_cta(base + (i * 128 + quarter * 32 + lane) * 4, r));
-        block_store_one<EPI>(p, seq, m0 + i, col, v);
+      const uint32_t mine = base + (quarter * 32 + lane) * 4;
+      for (int i0 = rank; i0 < rows; i0 += 4 * splits) {               // four rows at a time: their loads are in flight together
+        float v[4][8];
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+          for (int r = 0; r < 8; ++r)
+            v[k][r] = (r < splits && i0 + k * splits < rows) ? ld_cluster_f32(map_to_cta(mine + (i0 + k * splits) * 512, r)) : 0.f;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          float sum = bias;
+#pragma unroll
+          for (int r = 0; r < 8; ++r) sum += v[k][r];
+          if (i0 + k * splits < rows) block_store_one<EPI>(p, seq, m0 + i0 + k * splits, col, sum);
+        }
       }
     }
     __syncwarp();

@@ -305,10 +305,11 @@ __device__ __forceinline__ uint32_t map_to_cta(uint32_t saddr, uint32_t rank) {
 __device__ __forceinline__ void cluster_sync_all() {
   asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
-// 32-bit load from a shared::cluster address (the shared memory of any CTA of the cluster)
+// 32-bit load from a shared::cluster address (the shared memory of any CTA of the cluster).  No memory clobber: volatile alone
+// keeps it behind the cluster barrier, and several may be in flight.
 __device__ __forceinline__ float ld_cluster_f32(uint32_t cluster_addr) {
   float v;
-  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(cluster_addr) : "memory");
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(cluster_addr));
   return v;
 }
 // arrive on an mbarrier that may live in the peer CTA (shared::cluster address)
