@@ -8,7 +8,7 @@
 // partial tiles, so the next group's MMAs run while the last one's sums are added.
 //
 // Two kernels.  gemm_block128_pair_kernel: persistent, one 256 x 256 tile per CTA pair, for shapes with
-// enough tiles.  gemm_block128_split_kernel: 128 output columns x up to 128 rows per CTA, k split over a
+// enough tiles.  gemm_block128_split_kernel: 128 output columns x up to 64 rows per CTA, k split over a
 // cluster and joined through distributed shared memory in rank order, for few rows, where reading B once is
 // the bound.
 #pragma once
@@ -423,8 +423,8 @@ done:
 }
 
 // ------------------------------------------------------------------------------------------------
-// Few rows.  The roles of the operands are swapped: 128 rows of B (output columns) are the MMA's M, up to BT rows of A its
-// N, so that a lane owns one output column and the MMA wastes nothing on absent rows beyond the rounding to 16.
+// Few rows, in tiles of BT = 16, 32 or 64 (128 lost to two of 64 at every size: one CTA per SM).  The roles of the operands are
+// swapped: 128 rows of B (output columns) are the MMA's M, up to BT rows of A its N, so that a lane owns one output column and the MMA wastes nothing on absent rows beyond the rounding to 16.
 // Reading B once is the bound (1 byte per 2 M flops): the k groups are split over the CTAs of a cluster until the
 // launch fills the device, each CTA streams its part through a ring of TMA boxes, and the partial
 // accumulators meet in distributed shared memory, where rank r sums its share of the rows in rank order.
@@ -434,9 +434,9 @@ done:
 template <int BT>
 struct SplitCfg {
   static constexpr int A_BYTES = 128 * 128, T_BYTES = BT * 128, STAGE_BYTES = A_BYTES + T_BYTES;
-  static constexpr int STAGES = BT <= 32 ? 5 : (BT == 64 ? 4 : 3);
-  static constexpr int BUFS = BT <= 64 ? 4 : 2;                        // partial tiles in tensor memory
-  static constexpr int COLS = BUFS * BT < 32 ? 32 : BUFS * BT;         // 64, 128, 256, 256
+  static constexpr int STAGES = BT <= 32 ? 5 : 4;
+  static constexpr int BUFS = 4;                                       // partial tiles in tensor memory
+  static constexpr int COLS = BUFS * BT;                               // 64, 128, 256
   static constexpr int SCALE_GROUPS = 8;                               // groups of row scales staged at a time
   static constexpr int OFF_SCALE = STAGES * STAGE_BYTES;
   static constexpr int OFF_BAR = OFF_SCALE + 2 * SCALE_GROUPS * BT * 4;

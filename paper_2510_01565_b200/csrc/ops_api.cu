@@ -48,7 +48,6 @@ cudaError_t allow_gemm() {
   if (e == cudaSuccess) e = allow_smem(&gemm_block128_split_kernel<EPI, 16>, SplitCfg<16>::SMEM_BYTES);
   if (e == cudaSuccess) e = allow_smem(&gemm_block128_split_kernel<EPI, 32>, SplitCfg<32>::SMEM_BYTES);
   if (e == cudaSuccess) e = allow_smem(&gemm_block128_split_kernel<EPI, 64>, SplitCfg<64>::SMEM_BYTES);
-  if (e == cudaSuccess) e = allow_smem(&gemm_block128_split_kernel<EPI, 128>, SplitCfg<128>::SMEM_BYTES);
   return e;
 }
 
@@ -250,20 +249,27 @@ cudaError_t launch_product(const DeviceState& d, const BlockProduct& b, BlockGem
   const int groups = (p.K + 127) / 128;
   const int rows = b.plan_m;
   const long long pair_tiles = static_cast<long long>((p.M + 255) / 256) * ((p.N + 255) / 256);
-  const long long planned_tiles = static_cast<long long>((rows + 255) / 256) * ((p.N + 255) / 256);
-  // Few rows, or too few 256 x 256 tiles to fill the device: the split kernel.
   // The pair kernel moves residual rows in boxes of 32 columns and reads bias and gates in fours.
   const bool resid_ok = EPI != kBlkGateResidF32 || (p.vec_out && aligned(p.resid, 16) && aligned(p.bias, 16) && aligned(p.gate, 16) && p.gate_stride % 4 == 0 && p.N % 32 == 0);
-  if (rows <= 128 || planned_tiles < d.pairs / 2 || !resid_ok) {
-    const int bt = rows <= 16 ? 16 : (rows <= 32 ? 32 : (rows <= 64 ? 64 : 128));
+  // Few rows, or a product with so few tiles of 128 x 64 that most of the pair kernel's 256 x 256 ones would be missing: the split
+  // kernel.  Measured, us, split against pair: n 3072, k 3072: m 64 9 / 15, m 128 11 / 16, m 256 17 / 16; n 3072, k 12288:
+  // m 64 14 / 45, m 256 37 / 45, m 512 51 / 46; n 9216, k 3072: m 64 14 / 16, m 128 17 / 17, m 256 21 / 17.
+  if (rows <= 32 || 3 * tiles_n * ((rows + 63) / 64) <= 2ll * d.num_sms || !resid_ok) {
+    const int bt = rows <= 16 ? 16 : (rows <= 32 ? 32 : 64);
     const long long tiles = tiles_n * ((rows + bt - 1) / bt);
+    // CTAs per tile: doubled up to about four CTAs per three SMs as long as each keeps two groups, and up to two per SM as long as
+    // each keeps twelve (us for 1, 2, 4, 8: 24 tiles of 24 groups 11, 8, 6, 7; 72 tiles of 24 groups 11, 9, 11, 15;
+    // 24 tiles of 96 groups 35, 21, 12, 10; 144 tiles of 24 groups 11.6, 10.9, 17, 25)
     int splits = 1;
-    while (splits < 8 && 2 * splits <= groups && tiles * splits < d.num_sms) splits *= 2;
+    while (splits < 8) {
+      const long long ctas = tiles * 2 * splits, each = groups / (2 * splits);
+      if (!(3 * ctas <= 4ll * d.num_sms ? each >= 2 : (ctas <= 2ll * d.num_sms && each >= 12))) break;
+      splits *= 2;
+    }
     if (!byte_map(&tmA, b.a, p.K, p.M, b.lda, bt) || !byte_map(&tmB, b.b, p.K, p.N, b.ldb, 128)) return cudaErrorInvalidValue;
     if (bt == 16) return launch_split<EPI, 16>(tmA, tmB, p, seq, splits, st);
     if (bt == 32) return launch_split<EPI, 32>(tmA, tmB, p, seq, splits, st);
-    if (bt == 64) return launch_split<EPI, 64>(tmA, tmB, p, seq, splits, st);
-    return launch_split<EPI, 128>(tmA, tmB, p, seq, splits, st);
+    return launch_split<EPI, 64>(tmA, tmB, p, seq, splits, st);
   }
   if (!byte_map(&tmA, b.a, p.K, p.M, b.lda, 128) || !byte_map(&tmB, b.b, p.K, p.N, b.ldb, 128)) return cudaErrorInvalidValue;
   {  // tile order: hold the panels of whichever operand costs fewer DRAM reads in L2 (as launch_gemm of the step does)
