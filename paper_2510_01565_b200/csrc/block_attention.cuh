@@ -715,13 +715,6 @@ struct BlockSelectParams {
   int keep[DIT_MAX_REQUESTS], tail[DIT_MAX_REQUESTS];
 };
 
-// 16 bytes, read once by this kernel (volatile: the loads of a batch stay together in front of their uses).
-__device__ __forceinline__ uint4 load_stream(const void* p) {
-  uint4 v;
-  asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
-  return v;
-}
-
 template <bool BF16>
 __device__ __forceinline__ double widen_double(uint16_t h) {
   double d;
@@ -761,7 +754,7 @@ block_means_kernel(const BlockSelectParams p, const __grid_constant__ BlockBatch
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         const int r = warp + 8 * i;
-        v[i] = r < n ? load_stream(src + r * ld) : make_uint4(0, 0, 0, 0);
+        v[i] = r < n ? load_once(src + r * ld) : make_uint4(0, 0, 0, 0);
       }
 #pragma unroll
       for (int i = 0; i < 16; ++i) {

@@ -3,18 +3,17 @@
 //   top = max(max|x|, 2^-100),  scale = top / 448,  code = e4m3(x * (448 / top))
 // Both divisions and the product are single IEEE fp32 operations, so the codes are a function of the
 // inputs alone that any fp32 implementation reproduces bit for bit.  The floor keeps 448 / top finite
-// for groups of zeros and of tiny numbers.  The maximum is taken on the absolute values' bit patterns,
-// whose integer order is the numbers' order with infinity above every number and NaN above infinity.
+// for groups of zeros and of tiny numbers.  A NaN passes through the maximum into scale and codes.
 #pragma once
 #include "common.cuh"
 #include "ptx.cuh"
 
 namespace dit {
 
-constexpr uint32_t kQuantFloorBits = 0x0D800000u;   // 2^-100
+constexpr float kQuantFloor = 7.888609052210118e-31f;   // 2^-100
 
-__device__ __forceinline__ void quant_factors(uint32_t top_bits, float& inv, float& scale) {
-  const float top = __uint_as_float(max(top_bits, kQuantFloorBits));
+__device__ __forceinline__ void quant_factors(float top, float& inv, float& scale) {
+  top = fmax_nan(top, kQuantFloor);
   inv = __fdiv_rn(448.0f, top);
   scale = __fdiv_rn(top, 448.0f);
 }
@@ -33,6 +32,16 @@ struct QuantIn {
     if constexpr (kType == 2) return e;
     else if constexpr (kType == 1) return __uint_as_float(static_cast<uint32_t>(e) << 16);
     else return __half2float(__ushort_as_half(e));
+  }
+  // Magnitudes by their bit patterns, whose integer order is the numbers' with infinity above every number and NaN above it.
+  static __device__ __forceinline__ uint32_t max_bits(uint32_t top, uint32_t word) {
+    if constexpr (kType == 2) return max(top, word & 0x7FFFFFFFu);
+    else return __vmaxu2(top, word & 0x7FFF7FFFu);
+  }
+  static __device__ __forceinline__ uint32_t fold_bits(uint32_t top) { return kType == 2 ? top : max(top & 0xFFFFu, top >> 16); }
+  static __device__ __forceinline__ float from_bits(uint32_t top) {
+    if constexpr (kType == 2) return __uint_as_float(top);
+    else return widen(static_cast<uint16_t>(top));
   }
   static __device__ __forceinline__ void widen16(const uint4& r, float (&v)[EPL]) {
     const uint32_t u[4] = {r.x, r.y, r.z, r.w};
@@ -86,7 +95,7 @@ quantize_block128_kernel(const QuantParams p) {
 #pragma unroll
       for (int i = 0; i < BATCH; ++i) {
         const int r = b + i * RPI + sub;
-        raw[i] = r < n_rows ? __ldg(reinterpret_cast<const uint4*>(src + r * p.ld)) : make_uint4(0, 0, 0, 0);
+        raw[i] = r < n_rows ? load_once(src + r * p.ld) : make_uint4(0, 0, 0, 0);
       }
 #pragma unroll
       for (int i = 0; i < BATCH; ++i) In::widen16(raw[i], v[i]);
@@ -98,27 +107,36 @@ quantize_block128_kernel(const QuantParams p) {
         for (int e = 0; e < EPL; ++e) v[i][e] = (r < n_rows && e < n_in) ? In::widen(src[r * p.ld + e]) : 0.f;
       }
     }
+    float top[BATCH];
 #pragma unroll
     for (int i = 0; i < BATCH; ++i) {
-      uint32_t top = 0;
+      top[i] = 0.f;
 #pragma unroll
-      for (int e = 0; e < EPL; ++e) top = max(top, __float_as_uint(v[i][e]) & 0x7FFFFFFFu);
+      for (int e = 0; e < EPL; e += 2) top[i] = fmax3_nan(top[i], fabsf(v[i][e]), fabsf(v[i][e + 1]));
 #pragma unroll
-      for (int o = LPR / 2; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-      float inv, scale;
-      quant_factors(top, inv, scale);
+      for (int o = LPR / 2; o > 0; o >>= 1) top[i] = fmax_nan(top[i], __shfl_xor_sync(0xffffffffu, top[i], o));
+    }
+    // The divisions of the batch's rows are shared out over the lanes: lane k works for row b + k % ROWS, which is also the
+    // row of the run whose scale it keeps.
+    constexpr int ROWS = BATCH * RPI;
+    float row_top = 0.f, inv, scale;
+#pragma unroll
+    for (int i = 0; i < BATCH; ++i) {
+      const float t = __shfl_sync(0xffffffffu, top[i], lane % RPI * LPR);
+      if (lane % ROWS / RPI == i) row_top = t;
+    }
+    quant_factors(row_top, inv, scale);
+    if (lane / ROWS == b / ROWS) my_scale = scale;
+#pragma unroll
+    for (int i = 0; i < BATCH; ++i) {
       const int r = b + i * RPI + sub;
-#pragma unroll
-      for (int s = 0; s < RPI; ++s) {                             // lane k of the warp keeps the scale of row k of the run
-        const float sc = __shfl_sync(0xffffffffu, scale, s * LPR);
-        if (lane == b + i * RPI + s) my_scale = sc;
-      }
+      const float my_inv = __shfl_sync(0xffffffffu, inv, i * RPI + sub);
       if (r < n_rows && n_in > 0) {
         uint8_t* d = dst + r * p.ld_codes;
         uint32_t w[EPL / 4];
 #pragma unroll
         for (int q = 0; q < EPL / 4; ++q)
-          w[q] = e4m3x2(v[i][4 * q] * inv, v[i][4 * q + 1] * inv) | (e4m3x2(v[i][4 * q + 2] * inv, v[i][4 * q + 3] * inv) << 16);
+          w[q] = e4m3x2(v[i][4 * q] * my_inv, v[i][4 * q + 1] * my_inv) | (e4m3x2(v[i][4 * q + 2] * my_inv, v[i][4 * q + 3] * my_inv) << 16);
         if (n_in == EPL) {                                        // rows of codes start on 16-byte boundaries
           if constexpr (EPL == 8) *reinterpret_cast<uint2*>(d) = make_uint2(w[0], w[1]);
           else *reinterpret_cast<uint32_t*>(d) = w[0];
@@ -153,13 +171,13 @@ quantize_weight_block128_kernel(const QuantWeightParams p) {
   using In = QuantIn<kType>;
   constexpr int COLS = 8, VECS = COLS / In::EPL;                  // 16-byte loads per eight columns: 1 (16-bit) or 2 (fp32)
   __shared__ uint32_t turned[128 * 32];
-  __shared__ uint32_t warp_top[8];
+  __shared__ float warp_top[8];
   const int gk = blockIdx.x % p.in_groups, gn = blockIdx.x / p.in_groups;
   const int k0 = gk * 128, n0 = gn * 128;
   const int c = threadIdx.x & 15, rq = threadIdx.x >> 4;          // columns n0 + 8c .., rows k0 + 4 rq + 64 i + j
   const typename In::Elem* src = static_cast<const typename In::Elem*>(p.w);
   uint4 raw[2][4][VECS];                                          // as loaded: half the registers of the widened values
-  uint32_t top = 0;
+  uint32_t top_bits = 0;                                          // largest magnitude as bits (a pair of them for 16-bit inputs)
 #pragma unroll
   for (int i = 0; i < 2; ++i)
 #pragma unroll
@@ -189,12 +207,17 @@ quantize_weight_block128_kernel(const QuantWeightParams p) {
 #pragma unroll
     for (int j = 0; j < 4; ++j)
 #pragma unroll
-      for (int e = 0; e < COLS; ++e) top = max(top, __float_as_uint(value(i, j, e)) & 0x7FFFFFFFu);
-  top = __reduce_max_sync(0xffffffffu, top);
+      for (int q = 0; q < VECS; ++q) {
+        const uint32_t u[4] = {raw[i][j][q].x, raw[i][j][q].y, raw[i][j][q].z, raw[i][j][q].w};
+#pragma unroll
+        for (int w = 0; w < 4; ++w) top_bits = In::max_bits(top_bits, u[w]);
+      }
+  top_bits = __reduce_max_sync(0xffffffffu, In::fold_bits(top_bits));
+  float top = In::from_bits(top_bits);
   if ((threadIdx.x & 31) == 0) warp_top[threadIdx.x >> 5] = top;
   __syncthreads();
 #pragma unroll
-  for (int i = 0; i < 8; ++i) top = max(top, warp_top[i]);
+  for (int i = 0; i < 8; ++i) top = fmax_nan(top, warp_top[i]);
   float inv, scale;
   quant_factors(top, inv, scale);
   if (threadIdx.x == 0) p.scales[static_cast<long long>(gn) * p.in_groups + gk] = scale;
