@@ -67,7 +67,8 @@ struct QuantParams {
 // (16-bit inputs) or one (fp32), the maximum is a shuffle reduction over the lanes of a row, and the
 // run's scales leave as one coalesced store (they lie group-major).  Neighbouring warps take
 // neighbouring groups, so a CTA reads runs of 2 KB.  Bound by HBM: 3 bytes per 16-bit element; four loads
-// per lane are requested ahead of use.
+// per lane are in flight (two or eight, a second batch ahead, more warps by fewer registers: all slower).  9216 x 12288 fp16: 58 us, 5.8 TB/s
+// (66 us while every lane did the divisions of its rows).
 // kVec: rows start on 16-byte boundaries; otherwise elements are loaded one by one.
 constexpr int kQuantBlockWarps = 8;
 
@@ -156,7 +157,7 @@ quantize_block128_kernel(const QuantParams p) {
 // through shared memory as packed quadruples of codes along `in`.  A thread's vectors are four
 // consecutive `in` rows at the same eight columns, so each of its 16 words holds four consecutive
 // codes of one output row; word kq of row n lies at kq ^ 2 (n / 8), which keeps both phases free of
-// bank conflicts.  Bound by HBM: 3 bytes per element.
+// bank conflicts.  Bound by HBM: 3 bytes per element.  3072 x 12288 bf16: 23 us, 4.9 TB/s (46 us with the widened values held: half the CTAs).
 struct QuantWeightParams {
   const void* w;
   uint8_t* codes;
