@@ -495,7 +495,7 @@ dit_status step_impl(dit_ctx* ctx, const void* tokens, const int32_t* lens, int 
     bp.b = wb + w_off; bp.ldb = g.K; bp.b_scales = reinterpret_cast<const float*>(wb + s_off);
     bp.bias = g.bias; bp.out = dst; bp.ld_out = ld_dst;
     bp.m = rows; bp.plan_m = T; bp.n = g.N; bp.k = g.K; bp.epilogue = epilogue;
-    bp.row0 = r0; bp.resid = g.resid; bp.gate = g.gate; bp.gate_stride = g.gate_stride;
+    bp.status = status; bp.row0 = r0; bp.resid = g.resid; bp.gate = g.gate; bp.gate_stride = g.gate_stride;
     DIT_CUDA_TRY(ctx, timed(kind, [&] { return launch_block_product(bp, seq, st); }));
     return DIT_OK;
   };
@@ -526,7 +526,7 @@ dit_status step_impl(dit_ctx* ctx, const void* tokens, const int32_t* lens, int 
     dit_status s = DIT_OK;
     DIT_CUDA_TRY(ctx, timed(DIT_KERNEL_ATTENTION, [&] {
       s = dit_select_blocks(&ab, sp_keep, sp_tail, index, count, sp_widest, ctx->at<void>(ctx->lay.sp_means), dit_select_blocks_workspace(&ab), st);
-      if (s == DIT_OK) s = dit_block_attention(&ab, index, count, sp_widest, 0.f, dst, ld_dst, st);
+      if (s == DIT_OK) s = run_block_attention(&ab, index, count, sp_widest, 0.f, dst, ld_dst, status, st);
       return cudaSuccess;
     }));
     launches += 2;                               // two kernels select, one attends

@@ -327,11 +327,11 @@ cudaError_t launch_select(const dit_attention_batch& a, const BlockBatch& b, Blo
 }
 
 cudaError_t launch_block_attention(const dit_attention_batch& a, const BlockBatch& b, const int32_t* index, const int32_t* count, int64_t ld_index,
-                                   float scale, void* out, int64_t ld_out, const DeviceState& d, cudaStream_t st) {
+                                   float scale, void* out, int64_t ld_out, int* status, const DeviceState& d, cudaStream_t st) {
   BlockAttnParams p{};
   p.out = out; p.ld_out = ld_out; p.index = index; p.count = count; p.ld_index = ld_index; p.n_heads = a.n_heads;
   p.scale_log2 = 1.4426950408889634f * (scale > 0.f ? scale : 1.0f / sqrtf(static_cast<float>(a.head_dim)));
-  p.status = d.status;
+  p.status = status ? status : d.status;
   if (a.head_dim == 128) return a.type == DIT_TYPE_BF16 ? launch_attend<128, true>(d, a, b, p, st) : launch_attend<128, false>(d, a, b, p, st);
   return a.type == DIT_TYPE_BF16 ? launch_attend<64, true>(d, a, b, p, st) : launch_attend<64, false>(d, a, b, p, st);
 }
@@ -357,7 +357,7 @@ cudaError_t launch_block_product(const BlockProduct& b, const SeqInfo& seq, cuda
   p.ld_sa = b.ld_a_scales; p.ld_out = b.ld_out;
   const int elem = (b.epilogue == kBlkF32 || b.epilogue == kBlkGateResidF32) ? 4 : 2;
   p.vec_out = aligned(b.out, 16) && b.ld_out * elem % 16 == 0;
-  p.status = d->status;
+  p.status = b.status ? b.status : d->status;
   p.row0 = b.row0; p.resid = b.resid; p.gate = b.gate; p.gate_stride = b.gate_stride;
   switch (b.epilogue) {
     case kBlkF16: return launch_product<kBlkF16>(*d, b, p, seq, st);
@@ -398,6 +398,22 @@ cudaError_t launch_quantize_weight(const void* w, dit_type type, long long ld, i
   if (type == DIT_TYPE_F16) return launch_quant_weight<0>(p, vec, st);
   if (type == DIT_TYPE_BF16) return launch_quant_weight<1>(p, vec, st);
   return launch_quant_weight<2>(p, vec, st);
+}
+
+dit_status run_block_attention(const dit_attention_batch* a, const int32_t* block_index, const int32_t* block_count, int64_t ld_index,
+                               float scale, void* out, int64_t ld_out, int* status, cudaStream_t st) {
+  BlockBatch b;
+  dit_status s = plan_batch(a, true, &b);
+  if (s != DIT_OK) return s;
+  if (b.cu_q[b.n] == 0) return DIT_OK;
+  if (!block_index || !block_count || !out || ld_index < 1) return DIT_ERR_INVALID_ARG;
+  if (!aligned(block_index, 4) || !aligned(block_count, 4) || !aligned(out, 16) || ld_out % 8 || ld_out < static_cast<int64_t>(a->n_heads) * a->head_dim)
+    return DIT_ERR_INVALID_ARG;
+  if (!(scale >= 0.f) || !(scale <= 3.0e38f)) return DIT_ERR_INVALID_ARG;
+  const DeviceState* d;
+  s = ready(&d);
+  if (s != DIT_OK) return s;
+  return launch_block_attention(*a, b, block_index, block_count, ld_index, scale, out, ld_out, status, *d, st) == cudaSuccess ? DIT_OK : DIT_ERR_CUDA;
 }
 
 }  // namespace dit
@@ -497,19 +513,7 @@ dit_status dit_select_blocks(const dit_attention_batch* a, const int32_t* keep, 
 
 dit_status dit_block_attention(const dit_attention_batch* a, const int32_t* block_index, const int32_t* block_count, int64_t ld_index,
                                float scale, void* out, int64_t ld_out, void* stream) {
-  BlockBatch b;
-  dit_status s = plan_batch(a, true, &b);
-  if (s != DIT_OK) return s;
-  if (b.cu_q[b.n] == 0) return DIT_OK;
-  if (!block_index || !block_count || !out || ld_index < 1) return DIT_ERR_INVALID_ARG;
-  if (!aligned(block_index, 4) || !aligned(block_count, 4) || !aligned(out, 16) || ld_out % 8 || ld_out < static_cast<int64_t>(a->n_heads) * a->head_dim)
-    return DIT_ERR_INVALID_ARG;
-  if (!(scale >= 0.f) || !(scale <= 3.0e38f)) return DIT_ERR_INVALID_ARG;
-  const DeviceState* d;
-  s = ready(&d);
-  if (s != DIT_OK) return s;
-  return launch_block_attention(*a, b, block_index, block_count, ld_index, scale, out, ld_out, *d, static_cast<cudaStream_t>(stream)) == cudaSuccess
-             ? DIT_OK : DIT_ERR_CUDA;
+  return run_block_attention(a, block_index, block_count, ld_index, scale, out, ld_out, nullptr, static_cast<cudaStream_t>(stream));
 }
 
 dit_status dit_ops_poll_status(void) {

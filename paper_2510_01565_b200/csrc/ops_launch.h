@@ -25,10 +25,14 @@ struct BlockProduct {
   const float* resid;
   const float* gate;
   long long gate_stride;
+  int* status;               // device word for waits that ran out; NULL: the device's own (dit_ops_poll_status)
 };
 
 cudaError_t ops_prepare_device();                      // sets kernel attributes once per device
 cudaError_t launch_block_product(const BlockProduct& b, const SeqInfo& seq, cudaStream_t st);
+// dit_block_attention with a status word of the caller's
+dit_status run_block_attention(const dit_attention_batch* batch, const int32_t* block_index, const int32_t* block_count, int64_t ld_index, float scale,
+                               void* out, int64_t ld_out, int* status, cudaStream_t st);
 cudaError_t launch_quantize_rows(const void* x, dit_type type, long long ld, long long rows, long long cols, void* codes,
                                  long long ld_codes, float* scales, long long ld_scales, cudaStream_t st);
 cudaError_t launch_quantize_weight(const void* w, dit_type type, long long ld, int in_dim, int out_dim, void* codes, long long ld_codes,

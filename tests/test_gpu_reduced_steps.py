@@ -160,6 +160,38 @@ def test_a_parallel_blocks_products(B, dims):
         assert rms(out[rows] - x - branch) <= QKV_RMS * rms(branch) + OUTPUT * rms(x)
 
 
+@pytest.mark.parametrize("form", ["dual", "parallel_then_sequential", "qk_rope"])
+def test_sparse_attention_in_the_other_block_forms(B, form):
+    """The attention output of the last block against the oracle's selected attention on the GPU's own q, k, v, text rows kept."""
+    reqs = [(384, 384, 77), (160, 208, 9), (64, 64, 200)]
+    wl = W.make_custom("forms", W.SMALL, 2, reqs, seed=60)
+    flags = B.DIT_FLAG_SPARSE_ATTENTION
+    if form == "dual":
+        wl.weights = [dict(wl.weights[0], txt=wl.weights[1])]
+    elif form == "parallel_then_sequential":
+        wl.weights = [W.draw_parallel_block_weights(np.random.default_rng(60), wl.dims), wl.weights[0]]
+    else:
+        flags |= B.DIT_FLAG_QK_RMSNORM | B.DIT_FLAG_ROPE_2D
+    import torch
+    ctx = B.context_for(wl.dims, 2, wl.total_tokens, 3, flags=flags)
+    slots = B.upload_weights(ctx, wl.weights)
+    ctx.dit_ctx_set_sparse_attention(0.45, 1)
+    ctx.dit_debug_poison()
+    out = ctx.dit_step_forward_requests(B.bits_to_cuda_bf16(wl.packed_tokens()), wl.requests, B.bits_to_cuda_bf16(wl.cond), slots)
+    torch.cuda.synchronize()
+    ctx.dit_ctx_poll_status()
+    assert ctx.dit_debug_check_guards() == 0 and bool(out.isfinite().all())
+    qkv, attn = (ctx.dit_debug_tap(n).double().cpu().numpy() for n in ("qkv", "attn"))
+    ctx.close()
+    p, H = 0, wl.dims.hidden
+    for r, n in enumerate(wl.token_lens):
+        rows = slice(p, p + n)
+        p += n
+        q, k, v = (qkv[rows, i * H:(i + 1) * H] for i in range(3))
+        a = K.sparse_attention(q, k, v, wl.dims.n_heads, K.select_blocks(q, k, wl.dims.n_heads, keep_of(n, 0.45, 1), reqs[r][2]))
+        assert np.abs(attn[rows] - a).max() <= STAGE * rms(a)
+
+
 def test_keeping_everything_is_the_dense_step_bit_for_bit(B):
     import torch
     wl = W.make_custom("dense", W.SMALL, 2, [(256, 256, 3), (64, 64, 0)], seed=53)
