@@ -607,210 +607,51 @@ def dit_modulation_noalloc(cond, w_ada, b_ada, mod_out, stream=None):
 
 
 # ---------------------------------------------------------------------- operators without a context (dit_ops.h)
-# The small shapes of these operators take the GPU a few microseconds: their marshalling is kept short (no context
-# managers unless a device has to be switched, raw stream handles, one pass over the checks).
-def _refuse(what: str):
-    raise DitError(1, what)
+# Their small shapes take the GPU a few microseconds, so the marshalling of these is native (csrc/marshal.cc): it checks the
+# tensors, allocates the results that the caller did not bring, makes the tensors' device current and calls the library on
+# `stream` (default: the current stream of that device).  Refusals are DitError, as everywhere.
+_native = None
 
 
-_TYPE_CODES: Dict[object, int] = {}
-
-
-def _type_code(dtype) -> int:
-    if not _TYPE_CODES:
-        import torch
-        _TYPE_CODES.update({torch.float16: 0, torch.bfloat16: 1, torch.float32: 2})
-    code = _TYPE_CODES.get(dtype)
-    if code is None:
-        _refuse(f"{dtype} is not one of float16, bfloat16, float32")
-    return code
-
-
-def _matrix(t, what: str) -> int:
-    """Row stride in elements of a CUDA matrix whose rows are contiguous (the rows themselves may lie apart)."""
-    if not t.is_cuda or t.dim() != 2:
-        _refuse(f"{what} must be a CUDA matrix")
-    rows, cols = t.shape
-    ld, inner = t.stride()
-    if inner != 1 and cols > 1:
-        _refuse(f"{what} must be contiguous along its columns")
-    return ld if rows > 1 else cols
-
-
-def _launch(fn, args, stream, tensors):
-    """Calls fn(*args, stream) with the tensors' device current; they must share it."""
-    import torch
-    index = tensors[0].get_device()
-    for t in tensors:
-        if t is not None and t.get_device() != index:
-            _refuse("tensors lie on different devices")
-    if stream is None:
-        raw = torch._C._cuda_getCurrentRawStream(index)
-    else:
-        if stream.device.index != index:
-            _refuse("the stream belongs to another device than the tensors")
-        raw = stream.cuda_stream
-    if torch._C._cuda_getDevice() == index:
-        st = fn(*args, raw)
-    else:
-        with torch.cuda.device(index):
-            st = fn(*args, raw)
-    if st != DIT_OK:
-        raise DitError(st, load_library().dit_status_string(st).decode())
-
-
-def _data(t):
-    return None if t is None else t.data_ptr()
-
-
-def _codes_for(rows: int, cols: int, device):
-    """Uninitialised e4m3 codes [rows, cols] whose rows start on 16-byte boundaries."""
-    import torch
-    if cols % 16 == 0:                       # (sizes as separate arguments: a tuple costs half as much again)
-        return torch.empty(rows, cols, dtype=torch.float8_e4m3fn, device=device)
-    return torch.empty(rows, (cols + 15) // 16 * 16, dtype=torch.float8_e4m3fn, device=device)[:, :cols]
-
-
-def _pitch(ld: int, rows: int) -> int:
-    """Row stride of codes; a single row has none of its own, and any multiple of 16 describes it."""
-    return ld if rows > 1 else (ld + 15) // 16 * 16
+def _marshal():
+    global _native
+    if _native is None:
+        import torch  # noqa: F401  (its libraries must be loaded first)
+        load_library()
+        try:
+            from paper_2510_01565_b200 import _marshal as native
+        except ImportError as e:
+            raise ImportError("_marshal.so is missing or stale: build it with `python -m paper_2510_01565_b200.build` "
+                              f"(there is no fallback path): {e}") from e
+        native.set_error(DitError)
+        _native = native
+    return _native
 
 
 def dit_quantize_block128(x, codes=None, scales=None, stream=None):
     """x [rows, cols] fp16 / bf16 / fp32 -> (codes [rows, cols] float8_e4m3fn, scales [ceil(cols / 128), rows] fp32)."""
-    import torch
-    lib, ld = _lib or load_library(), _matrix(x, "x")
-    rows, cols = x.shape
-    groups = (cols + BLOCK - 1) // BLOCK
-    if codes is None:
-        codes = _codes_for(rows, cols, x.device)
-    elif codes.dtype != torch.float8_e4m3fn or codes.shape != x.shape:
-        _refuse("codes must be float8_e4m3fn, shaped like x")
-    if scales is None:
-        scales = torch.empty(groups, rows, dtype=torch.float32, device=x.device)
-    elif scales.dtype != torch.float32 or scales.shape != (groups, rows):
-        _refuse("scales must be fp32 [ceil(cols / 128), rows]")
-    ld_scales = _matrix(scales, "scales")
-    _launch(lib.dit_quantize_block128, (x.data_ptr(), _type_code(x.dtype), ld, rows, cols, codes.data_ptr(), _pitch(_matrix(codes, "codes"), rows),
-                                        scales.data_ptr(), max(ld_scales, rows)), stream, (x, codes, scales))
-    return codes, scales
+    return (_native or _marshal()).quantize_block128(x, codes, scales, stream)
 
 
 def dit_quantize_weight_block128(w, codes=None, scales=None, stream=None):
     """w [in, out] -> (codes [out, in] float8_e4m3fn, scales [ceil(out / 128), ceil(in / 128)] fp32)."""
-    import torch
-    lib, ld = _lib or load_library(), _matrix(w, "w")
-    n_in, n_out = w.shape
-    shape = ((n_out + BLOCK - 1) // BLOCK, (n_in + BLOCK - 1) // BLOCK)
-    if codes is None:
-        codes = _codes_for(n_out, n_in, w.device)
-    elif codes.dtype != torch.float8_e4m3fn or codes.shape != (n_out, n_in):
-        _refuse("codes must be float8_e4m3fn [out, in]")
-    if scales is None:
-        scales = torch.empty(*shape, dtype=torch.float32, device=w.device)
-    elif scales.dtype != torch.float32 or scales.shape != shape or not scales.is_contiguous():
-        _refuse("scales must be contiguous fp32 [ceil(out / 128), ceil(in / 128)]")
-    _launch(lib.dit_quantize_weight_block128, (w.data_ptr(), _type_code(w.dtype), ld, n_in, n_out, codes.data_ptr(),
-                                               _pitch(_matrix(codes, "codes"), n_out), scales.data_ptr()), stream, (w, codes, scales))
-    return codes, scales
+    return (_native or _marshal()).quantize_weight_block128(w, codes, scales, stream)
 
 
 def dit_gemm_block128(a, a_scales, b, b_scales, bias=None, out=None, out_dtype=None, stream=None):
-    """a [m, k], b [n, k] float8_e4m3fn codes with their scales -> a b^T [m, n] (+ bias) in out_dtype (default fp16)."""
-    import torch
-    lib = _lib or load_library()
-    lda, ldb, ld_sa = _matrix(a, "a"), _matrix(b, "b"), _matrix(a_scales, "a_scales")
-    m, k = a.shape
-    n = b.shape[0]
-    groups = (k + BLOCK - 1) // BLOCK
-    if a.dtype != torch.float8_e4m3fn or b.dtype != torch.float8_e4m3fn:
-        _refuse("a and b must be float8_e4m3fn codes")
-    if b.shape[1] != k:
-        _refuse("a and b differ in k")
-    if a_scales.dtype != torch.float32 or a_scales.shape != (groups, m):
-        _refuse("a_scales must be fp32 [ceil(k / 128), m]")
-    if b_scales.dtype != torch.float32 or not b_scales.is_contiguous() or b_scales.shape != ((n + BLOCK - 1) // BLOCK, groups):
-        _refuse("b_scales must be contiguous fp32 [ceil(n / 128), ceil(k / 128)]")
-    if bias is not None and (not bias.is_cuda or bias.dtype != torch.float32 or not bias.is_contiguous() or bias.shape != (n,)):
-        _refuse("bias must be contiguous fp32 [n]")
-    if out is None:
-        out = torch.empty(m, n, dtype=out_dtype or torch.float16, device=a.device)
-    elif out.shape != (m, n) or (out_dtype is not None and out.dtype != out_dtype):
-        _refuse("out must be [m, n] of out_dtype")
-    args = DitGemmBlock128Args(a.data_ptr(), a_scales.data_ptr(), b.data_ptr(), b_scales.data_ptr(), _data(bias), out.data_ptr(), _pitch(lda, m),
-                               max(ld_sa, m), _pitch(ldb, n), _matrix(out, "out"), m, n, k, _type_code(out.dtype))
-    _launch(lib.dit_gemm_block128, (C.byref(args),), stream, (a, a_scales, b, b_scales, bias, out))
-    return out
-
-
-def _attention_batch(q, k, v, q_lens, kv_lens, n_heads):
-    """(struct, number of query blocks); v may be None.  The arrays of lengths live as long as the struct does."""
-    n = len(q_lens)
-    if len(kv_lens) != n:
-        _refuse("q_lens and kv_lens differ in length")
-    ld_q, ld_k, ld_v = _matrix(q, "q"), _matrix(k, "k"), 0 if v is None else _matrix(v, "v")
-    width, kv_rows = q.shape[1], sum(kv_lens)
-    if n_heads < 1 or width % n_heads:
-        _refuse("the columns of q do not divide into n_heads")
-    if q.shape[0] != sum(q_lens) or k.shape != (kv_rows, width) or (v is not None and v.shape != k.shape):
-        _refuse("q, k and v must be [sum of lengths, width]")
-    if k.dtype != q.dtype or (v is not None and v.dtype != q.dtype):
-        _refuse("q, k and v differ in type")
-    lens = C.c_int32 * max(n, 1)
-    batch = DitAttentionBatch(q.data_ptr(), k.data_ptr(), _data(v), ld_q, ld_k, ld_v, _type_code(q.dtype), n_heads, width // n_heads, n,
-                              lens(*q_lens), lens(*kv_lens))
-    return batch, sum([(l + BLOCK - 1) // BLOCK for l in q_lens])
-
-
-def _check_lists(index, count, n_heads, q_blocks):
-    import torch
-    if not index.is_cuda or index.dtype != torch.int32 or not index.is_contiguous() or index.dim() != 3 or index.shape[:2] != (n_heads, q_blocks):
-        _refuse("block_index must be contiguous int32 [n_heads, query blocks, entries]")
-    if not count.is_cuda or count.dtype != torch.int32 or not count.is_contiguous() or count.shape != (n_heads, q_blocks):
-        _refuse("block_count must be contiguous int32 [n_heads, query blocks]")
+    """a [m, k], b [n, k] float8_e4m3fn codes with their scales -> a b^T [m, n] (+ bias) in out_dtype (default: out's, or fp16)."""
+    return (_native or _marshal()).gemm_block128(a, a_scales, b, b_scales, bias, out, out_dtype, stream)
 
 
 def dit_select_blocks(q, k, q_lens, kv_lens, n_heads: int, keep, tail_rows=None, index=None, count=None, workspace=None, stream=None):
     """q [sum q_lens, width], k [sum kv_lens, width] fp16 or bf16; keep, tail_rows: one whole number per request.
     -> (block_index [n_heads, query blocks, max keep] int32, block_count [n_heads, query blocks] int32)."""
-    import torch
-    lib = _lib or load_library()
-    batch, q_blocks = _attention_batch(q, k, None, q_lens, kv_lens, n_heads)
-    n = len(q_lens)
-    if len(keep) != n or (tail_rows is not None and len(tail_rows) != n):
-        _refuse("keep and tail_rows need one number per request")
-    if index is None:
-        widest = max(keep, default=1)
-        if widest < 1:
-            _refuse("keep must be at least 1")
-        index = torch.empty(n_heads, q_blocks, widest, dtype=torch.int32, device=q.device)
-    if count is None:
-        count = torch.empty(n_heads, q_blocks, dtype=torch.int32, device=q.device)
-    _check_lists(index, count, n_heads, q_blocks)
-    if workspace is None:
-        workspace = torch.empty(max(lib.dit_select_blocks_workspace(C.byref(batch)), 16), dtype=torch.uint8, device=q.device)
-    ints = C.c_int32 * max(n, 1)
-    _launch(lib.dit_select_blocks, (C.byref(batch), ints(*keep), None if tail_rows is None else ints(*tail_rows), index.data_ptr(), count.data_ptr(),
-                                    index.shape[2], workspace.data_ptr(), workspace.numel() * workspace.element_size()), stream,
-            (q, k, index, count, workspace))
-    return index, count
+    return (_native or _marshal()).select_blocks(q, k, q_lens, kv_lens, n_heads, keep, tail_rows, index, count, workspace, stream)
 
 
 def dit_block_attention(q, k, v, q_lens, kv_lens, n_heads: int, index, count, scale: float = 0.0, out=None, stream=None):
     """Attention of every query block over its listed key blocks -> out, shaped and typed like q."""
-    import torch
-    lib = _lib or load_library()
-    if v is None:
-        _refuse("v is missing")
-    batch, q_blocks = _attention_batch(q, k, v, q_lens, kv_lens, n_heads)
-    _check_lists(index, count, n_heads, q_blocks)
-    if out is None:
-        out = torch.empty(*q.shape, dtype=q.dtype, device=q.device)
-    elif out.shape != q.shape or out.dtype != q.dtype:
-        _refuse("out must be shaped and typed like q")
-    _launch(lib.dit_block_attention, (C.byref(batch), index.data_ptr(), count.data_ptr(), max(index.shape[2], 1), scale, out.data_ptr(),
-                                      _matrix(out, "out")), stream, (q, k, v, index, count, out))
-    return out
+    return (_native or _marshal()).block_attention(q, k, v, q_lens, kv_lens, n_heads, index, count, scale, out, stream)
 
 
 def dit_ops_poll_status():
