@@ -109,7 +109,9 @@ typedef struct {
  * quantised in blocks of 128 x 128 at load time, as dit_quantize_block128 and dit_quantize_weight_block128 (dit_ops.h) do, and
  * scale each block's partial sum in fp32.  A channel so much louder than the others that
  * they sink to the format's subnormal codes then costs precision in its own 128 columns only, not in the whole row.  Everything else stays as it is.  Plain sequential and parallel
- * blocks only: the flag cannot be combined with the other GEMM or QK flags, and two-stream blocks are refused.
+ * blocks only: the flag cannot be combined with the other GEMM or QK flags, and two-stream blocks are refused.  The
+ * order in which a product's partial sums are added depends on the whole batch's number of rows, so a request's result may
+ * differ in its last bits with the batch that it is packed in.
  * (Bit 4 is not assigned.) */
 #define DIT_FLAG_FP8_BLOCK128 32u
 /* Attention over selected key blocks (dit_select_blocks and dit_block_attention of dit_ops.h) instead of all of them; off until
@@ -151,7 +153,7 @@ dit_status dit_ctx_create(const dit_config *cfg, void *workspace, size_t workspa
 dit_status dit_ctx_destroy(dit_ctx *ctx);
 
 /* For contexts created with DIT_FLAG_SPARSE_ATTENTION: from the next step on, every block of 128 query rows of a request with n
- * blocks of 128 keys attends to max(min_blocks, ceil(keep * n)) of them (all n at most), chosen per head by the
+ * blocks of 128 keys attends to max(min_blocks, ceil(keep * n)) of them (all n at most; n <= 16384), chosen per head by the
  * product of the blocks' mean query and mean key.  A request's text rows are always among the chosen keys (as far as
  * they fit) where the call knows them, i.e. in dit_step_forward_requests, dit_denoise_step and dit_denoise_round.  0 < keep <= 1,
  * min_blocks >= 1; keep == 1, the state after creation, is the dense step bit for bit, and so is any step in

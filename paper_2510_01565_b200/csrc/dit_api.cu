@@ -80,6 +80,7 @@ bool config_ok(const dit_config* c) {
   return true;
 }
 
+constexpr int kMaxSelectBlocks = 16384;        // key blocks of one request that the selector and its attention take
 inline size_t blocks_of(size_t n) { return (n + DIT_BLOCK - 1) / DIT_BLOCK; }
 // Query or key blocks that a batch within the context's capacity can have: every request may end in a short one.
 inline size_t max_batch_blocks(const dit_config& c) { return static_cast<size_t>(c.max_total_tokens) / DIT_BLOCK + c.max_requests; }
@@ -508,7 +509,9 @@ dit_status step_impl(dit_ctx* ctx, const void* tokens, const int32_t* lens, int 
   if ((c.flags & DIT_FLAG_SPARSE_ATTENTION) && ctx->sparse_keep < 1.0f) {
     for (int r = 0; r < n; ++r) {
       const int blocks = static_cast<int>(blocks_of(lens[r]));
-      const int share = static_cast<int>(std::ceil(static_cast<double>(ctx->sparse_keep) * blocks));
+      if (blocks > kMaxSelectBlocks) return fail(ctx, DIT_ERR_CAPACITY, "a request is too long for attention over selected blocks");
+      // (keep is rounded to fp32: a product that is above a whole number by no more than that rounding counts as that number)
+      const int share = static_cast<int>(std::ceil(static_cast<double>(ctx->sparse_keep) * blocks * (1.0 - 1e-6)));
       sp_keep[r] = std::min(blocks, std::max({1, share, ctx->sparse_min_blocks}));
       sp_tail[r] = geo ? lens[r] - (geo->img_cu[r + 1] - geo->img_cu[r]) : 0;       // text rows
       sp_widest = std::max(sp_widest, sp_keep[r]);

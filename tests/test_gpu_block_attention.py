@@ -101,7 +101,7 @@ def check(got, want):
 
 
 BATCHES = [([1], [1]), ([1], [128]), ([1], [1000]), ([3, 1, 0, 4], [129, 5000, 77, 0]), ([2, 2], [300, 4096]), ([5], [40]), ([16, 9], [700, 64]), ([17], [400]), ([128], [128]), ([129], [129]),
-           ([130, 1, 257], [130, 1, 257]), ([300, 40, 0, 512], [1000, 0, 50, 700]), ([640], [2300])]
+           ([130, 1, 257], [130, 1, 257]), ([300, 40, 0, 512], [1000, 0, 50, 700]), ([200, 3], [0, 0]), ([4], [0]), ([640], [2300])]
 
 
 @pytest.mark.parametrize("q_lens,kv_lens", BATCHES)

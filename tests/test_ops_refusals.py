@@ -134,3 +134,25 @@ def test_attention_refusals(lib):
     empty, _e = batch(q_lens=[0, 0])
     assert call(empty, index=None, out=None) == OK
     assert lib.dit_block_attention(None, P, P, 2, 0.0, P, 128, None) == INVALID
+
+
+def test_workspace_of_the_reduced_modes(lib):
+    def ws(**kw):
+        base = dict(hidden=384, n_heads=6, head_dim=64, mlp_hidden=1536, cond_dim=384, max_blocks=2, max_total_tokens=1000, max_requests=3, ln_eps=1e-6, flags=0)
+        base.update(kw)
+        return lib.dit_workspace_bytes(C.byref(B.DitConfig(*base.values())))
+    full, slack = ws(), 8 * 1024
+    # the quantised operand [T, H + F] and its scales [(H + F) / 128, T]
+    need = 1000 * (384 + 1536) + 15 * 1000 * 4
+    assert need <= ws(flags=B.DIT_FLAG_FP8_BLOCK128) - full <= need + slack
+    # means of at most T / 128 + requests query and key blocks in 64 bits, lists of at most ceil(T / 128) entries
+    blocks = 1000 // 128 + 3
+    need = 2 * blocks * 384 * 8 + 6 * blocks * 8 * 4 + 6 * blocks * 4
+    assert need <= ws(flags=B.DIT_FLAG_SPARSE_ATTENTION) - full <= need + slack
+    assert ws(flags=B.DIT_FLAG_SPARSE_ATTENTION | 8) > 0 and ws(flags=B.DIT_FLAG_SPARSE_ATTENTION | 7) > 0
+    # a very wide MLP has more 128 x 128 blocks than output channels
+    wide = dict(hidden=64, n_heads=1, mlp_hidden=64 * 300)
+    assert ws(flags=B.DIT_FLAG_FP8_BLOCK128, **wide) > ws(**wide)
+    for bad in (16, 32 | 1, 32 | 2, 32 | 4, 32 | 8, 128):
+        assert ws(flags=bad) == 0, bad
+    assert lib.dit_ctx_set_sparse_attention(None, 0.5, 1) == INVALID
