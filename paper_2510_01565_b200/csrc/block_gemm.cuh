@@ -71,9 +71,9 @@ struct Cfg {
 // Writes a warp's 32 rows x 128 columns (this lane's row in acc) to an output whose rows start off 16-byte boundaries, which TMA cannot
 // address: through `stage` (16-byte units XOR-swizzled by the row), then row by row in 32-bit words.  A 16-bit row that
 // starts in the middle of a word is shifted by one element on the way (a whole warp works on one row, so nothing
-// diverges), its first and last element may go out alone.  m 4000, n 4001, k 1000: fp16 42 us, fp32 36, against 25 and 32 for
-// n 4000 (42 and 39 with an element per lane and store, 61 and 68 in 16-byte segments put together by each lane): the
-// stores hold the warps where TMA would not.
+// diverges), its first and last element may go out alone.  m 4000, n 4001, k 1000: fp16 39 us, fp32 35, against 26 and 31 for
+// n 4000 (42 and 39 with an element per lane and store, 43 and 37 row by row without the batches, 61 and 68 in 16-byte
+// segments put together by each lane): the stores hold the warps where TMA would not.
 template <int EPI>
 __device__ __forceinline__ void block_store_unaligned(const BlockGemmParams& p, uint8_t* stage, const float2 (&acc)[64], int lane, int row0, int n0) {
   constexpr bool kWide = EPI == kBlkF32;
@@ -97,24 +97,42 @@ __device__ __forceinline__ void block_store_unaligned(const BlockGemmParams& p, 
     }
     __syncwarp();
     const int rows = min(32, p.M - row0);
-#pragma unroll 4
-    for (int r = 0; r < rows; ++r) {
-      if constexpr (kWide) {
-        float* at = static_cast<float*>(p.out) + (static_cast<long long>(row0) + r) * p.ld_out + c0;
+    constexpr int BATCH = 8;                   // rows whose words are read before the first is written
+    for (int r0 = 0; r0 < rows; r0 += BATCH) {
+      uint32_t v[BATCH][2];
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
-          if (h * 32 + lane < cols) at[h * 32 + lane] = __uint_as_float(word(r, h * 32 + lane));
-      } else {
-        uint16_t* at = static_cast<uint16_t*>(p.out) + (static_cast<long long>(row0) + r) * p.ld_out + c0;
-        const int odd = static_cast<int>(reinterpret_cast<uintptr_t>(at) >> 1) & 1;        // the row starts in the middle of a word
-        if (odd && lane == 0 && cols > 0) at[0] = static_cast<uint16_t>(word(r, 0));
+      for (int k = 0; k < BATCH; ++k) { v[k][0] = word(r0 + k, lane); v[k][1] = word(r0 + k, 32 + lane); }
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int w = h * 32 + lane, c = 2 * w + odd;                // elements c and c + 1 make a word of the destination
-          uint32_t v = word(r, w);
-          if (odd) v = __funnelshift_r(v, word(r, min(w + 1, 63)), 16);
-          if (c + 1 < cols) *reinterpret_cast<uint32_t*>(at + c) = v;
-          else if (c < cols) at[c] = static_cast<uint16_t>(v);
+      for (int k = 0; k < BATCH; ++k) {
+        if (r0 + k >= rows) break;
+        const long long first = (static_cast<long long>(row0) + r0 + k) * p.ld_out + c0;
+        if constexpr (kWide) {
+          float* at = static_cast<float*>(p.out) + first;
+          if (lane < cols) at[lane] = __uint_as_float(v[k][0]);
+          if (32 + lane < cols) at[32 + lane] = __uint_as_float(v[k][1]);
+        } else {
+          uint16_t* at = static_cast<uint16_t*>(p.out) + first;
+          if ((reinterpret_cast<uintptr_t>(at) >> 1) & 1) {            // the row starts in the middle of a word (warp-uniform)
+            if (lane == 0 && cols > 0) at[0] = static_cast<uint16_t>(v[k][0]);
+            const uint32_t wrap = __shfl_sync(0xffffffffu, v[k][1], 0);
+            uint32_t n0 = __shfl_down_sync(0xffffffffu, v[k][0], 1), n1 = __shfl_down_sync(0xffffffffu, v[k][1], 1);
+            if (lane == 31) n0 = wrap;
+            v[k][0] = __funnelshift_r(v[k][0], n0, 16); v[k][1] = __funnelshift_r(v[k][1], n1, 16);
+            ++at;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const int c = 2 * (h * 32 + lane);
+              if (c + 2 < cols) *reinterpret_cast<uint32_t*>(at + c) = v[k][h];
+              else if (c + 1 < cols) at[c] = static_cast<uint16_t>(v[k][h]);
+            }
+          } else {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const int c = 2 * (h * 32 + lane);
+              if (c + 1 < cols) *reinterpret_cast<uint32_t*>(at + c) = v[k][h];
+              else if (c < cols) at[c] = static_cast<uint16_t>(v[k][h]);
+            }
+          }
         }
       }
     }
