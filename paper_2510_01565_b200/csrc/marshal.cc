@@ -148,7 +148,7 @@ PyObject* quantize_block128(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (codes.scalar_type() != at::kFloat8_e4m3fn || !shaped(codes, rows, cols)) refuse("codes must be float8_e4m3fn, shaped like x");
     if (scales.scalar_type() != at::kFloat || !shaped(scales, groups, rows)) refuse("scales must be fp32 [ceil(cols / 128), rows]");
     same_device(x, {&codes, &scales});
-    const int64_t ld_codes = pitch(matrix(codes, "codes"), rows), ld_scales = std::max(matrix(scales, "scales"), rows);
+    const int64_t ld_codes = pitch(matrix(codes, "codes"), rows), ld_scales = matrix(scales, "scales");
     c10::cuda::CUDAGuard guard(x.device());
     check(dit_quantize_block128(x.data_ptr(), type, ld, rows, cols, codes.data_ptr(), ld_codes, static_cast<float*>(scales.data_ptr()), ld_scales,
                                 stream_on(a[3], x.device())));
@@ -206,7 +206,7 @@ PyObject* gemm_block128(PyObject*, PyObject* const* a, Py_ssize_t n) {
     g.a = x.data_ptr(); g.a_scales = static_cast<const float*>(sx.data_ptr()); g.b = y.data_ptr(); g.b_scales = static_cast<const float*>(sy.data_ptr());
     g.bias = bias.defined() ? static_cast<const float*>(bias.data_ptr()) : nullptr;
     g.out = out.data_ptr();
-    g.lda = pitch(lda, g.m); g.ldb = pitch(ldb, g.n); g.ld_a_scales = std::max(ld_sa, g.m); g.ld_out = matrix(out, "out");
+    g.lda = pitch(lda, g.m); g.ldb = pitch(ldb, g.n); g.ld_a_scales = ld_sa; g.ld_out = matrix(out, "out");
     g.out_type = type_of(out.scalar_type());
     c10::cuda::CUDAGuard guard(x.device());
     check(dit_gemm_block128(&g, stream_on(a[7], x.device())));

@@ -125,3 +125,22 @@ def test_binding_refuses_mismatched_arguments(B):
         B.dit_quantize_block128(q[0])
     with pytest.raises(B.DitError):
         B.dit_quantize_block128(q.int())
+
+
+@pytest.mark.parametrize("rows", [1, 4])
+def test_scales_whose_groups_share_their_memory_are_refused(B, rows):
+    """An expanded [1, rows] matrix has room for one group; it has the shape of all of them."""
+    import torch
+    x = torch.ones(rows, 512, device="cuda")
+    codes, scales = B.dit_quantize_block128(x)
+    w, sw = B.dit_quantize_weight_block128(torch.ones(512, 128, device="cuda"))
+    shared = torch.full((1, 1), -1.0, device="cuda").expand(4, rows) if rows == 1 else torch.full((1, rows), -1.0, device="cuda").expand(4, rows)
+    with pytest.raises(B.DitError):
+        B.dit_quantize_block128(x, scales=shared)
+    with pytest.raises(B.DitError):
+        B.dit_gemm_block128(codes, shared, w, sw)
+    assert bool((shared == -1.0).all())
+    apart = torch.full((4, rows + 3), -1.0, device="cuda")             # a wider matrix is served, its rest left alone
+    B.dit_quantize_block128(x, scales=apart[:, :rows])
+    assert torch.equal(apart[:, :rows], scales) and bool((apart[:, rows:] == -1.0).all())
+    assert torch.equal(B.dit_gemm_block128(codes, apart[:, :rows], w, sw), B.dit_gemm_block128(codes, scales, w, sw))
