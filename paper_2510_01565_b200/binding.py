@@ -609,7 +609,8 @@ def dit_modulation_noalloc(cond, w_ada, b_ada, mod_out, stream=None):
 # ---------------------------------------------------------------------- operators without a context (dit_ops.h)
 # Their small shapes take the GPU a few microseconds, so the marshalling of these is native (csrc/marshal.cc): it checks the
 # tensors, allocates the results that the caller did not bring, makes the tensors' device current and calls the library on
-# `stream` (default: the current stream of that device).  Refusals are DitError, as everywhere.
+# `stream` (default: the current stream of that device), to which everything that it allocates belongs.  Refusals are DitError, as
+# everywhere.
 _native = None
 
 

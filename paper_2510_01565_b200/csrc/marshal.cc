@@ -82,9 +82,17 @@ void same_device(const at::Tensor& first, std::initializer_list<const at::Tensor
     if (t && t->defined() && t->device() != first.device()) refuse("tensors lie on different devices");
 }
 
-// The stream to use on `device`: the given torch.cuda.Stream's, or the current one of that device.
-void* stream_on(PyObject* stream, c10::Device device) {
-  if (!given(stream)) return c10::cuda::getCurrentCUDAStream(device.index()).stream();
+// The stream of a call on `device`: the given torch.cuda.Stream, or the current one.  While it lives, device and stream are
+// current, so that what the call allocates belongs to the stream that uses it: memory of another stream could be
+// handed out again, or still be in use, while the kernels run.
+struct OnStream {
+  c10::cuda::OptionalCUDAGuard device;
+  c10::cuda::OptionalCUDAStreamGuard stream;
+  void* raw;
+  OnStream(PyObject* given_stream, c10::Device on);
+};
+
+cudaStream_t given_stream_on(PyObject* stream, c10::Device device) {
   PyObject* index = PyObject_GetAttrString(stream, "device_index");
   if (!index) throw PythonError{};
   const long at = PyLong_AsLong(index);
@@ -95,7 +103,17 @@ void* stream_on(PyObject* stream, c10::Device device) {
   Py_DECREF(raw);
   if (PyErr_Occurred()) throw PythonError{};
   if (at != device.index()) refuse("the stream belongs to another device than the tensors");
-  return s;
+  return static_cast<cudaStream_t>(s);
+}
+
+OnStream::OnStream(PyObject* given_stream, c10::Device on) {
+  if (!given(given_stream)) {
+    device.set_device(on);
+    raw = c10::cuda::getCurrentCUDAStream(on.index()).stream();
+  } else {
+    raw = given_stream_on(given_stream, on);
+    stream.reset_stream(c10::cuda::getStreamFromExternal(static_cast<cudaStream_t>(raw), on.index()));
+  }
 }
 
 int64_t number(PyObject* o, const char* what) {
@@ -143,15 +161,15 @@ PyObject* quantize_block128(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const at::Tensor& x = tensor(a[0], "x");
     const int64_t ld = matrix(x, "x"), rows = x.size(0), cols = x.size(1), groups = (cols + DIT_BLOCK - 1) / DIT_BLOCK;
     const dit_type type = type_of(x.scalar_type());
+    const OnStream on(a[3], x.device());
     const at::Tensor codes = given(a[1]) ? tensor(a[1], "codes") : codes_for(rows, cols, x);
     const at::Tensor scales = given(a[2]) ? tensor(a[2], "scales") : empty({groups, rows}, at::kFloat, x);
     if (codes.scalar_type() != at::kFloat8_e4m3fn || !shaped(codes, rows, cols)) refuse("codes must be float8_e4m3fn, shaped like x");
     if (scales.scalar_type() != at::kFloat || !shaped(scales, groups, rows)) refuse("scales must be fp32 [ceil(cols / 128), rows]");
     same_device(x, {&codes, &scales});
     const int64_t ld_codes = pitch(matrix(codes, "codes"), rows), ld_scales = matrix(scales, "scales");
-    c10::cuda::CUDAGuard guard(x.device());
     check(dit_quantize_block128(x.data_ptr(), type, ld, rows, cols, codes.data_ptr(), ld_codes, static_cast<float*>(scales.data_ptr()), ld_scales,
-                                stream_on(a[3], x.device())));
+                                on.raw));
     return pair(codes, scales);
   });
 }
@@ -164,6 +182,7 @@ PyObject* quantize_weight_block128(PyObject*, PyObject* const* a, Py_ssize_t n) 
     const int64_t ld = matrix(w, "w"), n_in = w.size(0), n_out = w.size(1);
     const int64_t gn = (n_out + DIT_BLOCK - 1) / DIT_BLOCK, gk = (n_in + DIT_BLOCK - 1) / DIT_BLOCK;
     const dit_type type = type_of(w.scalar_type());
+    const OnStream on(a[3], w.device());
     const at::Tensor codes = given(a[1]) ? tensor(a[1], "codes") : codes_for(n_out, n_in, w);
     const at::Tensor scales = given(a[2]) ? tensor(a[2], "scales") : empty({gn, gk}, at::kFloat, w);
     if (codes.scalar_type() != at::kFloat8_e4m3fn || !shaped(codes, n_out, n_in)) refuse("codes must be float8_e4m3fn [out, in]");
@@ -171,9 +190,8 @@ PyObject* quantize_weight_block128(PyObject*, PyObject* const* a, Py_ssize_t n) 
       refuse("scales must be contiguous fp32 [ceil(out / 128), ceil(in / 128)]");
     same_device(w, {&codes, &scales});
     const int64_t ld_codes = pitch(matrix(codes, "codes"), n_out);
-    c10::cuda::CUDAGuard guard(w.device());
     check(dit_quantize_weight_block128(w.data_ptr(), type, ld, n_in, n_out, codes.data_ptr(), ld_codes, static_cast<float*>(scales.data_ptr()),
-                                       stream_on(a[3], w.device())));
+                                       on.raw));
     return pair(codes, scales);
   });
 }
@@ -200,6 +218,7 @@ PyObject* gemm_block128(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (given(a[6]) && !THPDtype_Check(a[6])) refuse("out_dtype must be a dtype");
     const at::ScalarType wanted = given(a[6]) ? reinterpret_cast<THPDtype*>(a[6])->scalar_type : at::kHalf;
     type_of(wanted);
+    const OnStream on(a[7], x.device());
     const at::Tensor out = given(a[5]) ? tensor(a[5], "out") : empty({g.m, g.n}, wanted, x);
     if (!shaped(out, g.m, g.n) || (given(a[6]) && out.scalar_type() != wanted)) refuse("out must be [m, n] of out_dtype");
     same_device(x, {&sx, &y, &sy, &bias, &out});
@@ -208,8 +227,7 @@ PyObject* gemm_block128(PyObject*, PyObject* const* a, Py_ssize_t n) {
     g.out = out.data_ptr();
     g.lda = pitch(lda, g.m); g.ldb = pitch(ldb, g.n); g.ld_a_scales = ld_sa; g.ld_out = matrix(out, "out");
     g.out_type = type_of(out.scalar_type());
-    c10::cuda::CUDAGuard guard(x.device());
-    check(dit_gemm_block128(&g, stream_on(a[7], x.device())));
+    check(dit_gemm_block128(&g, on.raw));
     return THPVariable_Wrap(out);
   });
 }
@@ -268,15 +286,15 @@ PyObject* select_blocks(PyObject*, PyObject* const* a, Py_ssize_t n) {
       if (x < 1) refuse("keep must be at least 1");
       widest = std::max<int64_t>(widest, x);
     }
+    const OnStream on(a[10], t.q.device());
     const at::Tensor index = given(a[7]) ? tensor(a[7], "block_index") : empty({t.b.n_heads, t.q_blocks, widest}, at::kInt, t.q);
     const at::Tensor count = given(a[8]) ? tensor(a[8], "block_count") : empty({t.b.n_heads, t.q_blocks}, at::kInt, t.q);
     check_lists(index, count, t);
     const at::Tensor workspace = given(a[9]) ? tensor(a[9], "workspace") : empty({static_cast<int64_t>(std::max<size_t>(16, dit_select_blocks_workspace(&t.b)))}, at::kByte, t.q);
     if (!workspace.is_cuda() || !workspace.is_contiguous()) refuse("workspace must be a contiguous CUDA tensor");
     same_device(t.q, {&t.k, &index, &count, &workspace});
-    c10::cuda::CUDAGuard guard(t.q.device());
     check(dit_select_blocks(&t.b, keep.data(), given(a[6]) ? tail.data() : nullptr, static_cast<int32_t*>(index.data_ptr()), static_cast<int32_t*>(count.data_ptr()),
-                            index.size(2), workspace.data_ptr(), workspace.nbytes(), stream_on(a[10], t.q.device())));
+                            index.size(2), workspace.data_ptr(), workspace.nbytes(), on.raw));
     return pair(index, count);
   });
 }
@@ -291,13 +309,13 @@ PyObject* block_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
     check_lists(index, count, t);
     const double scale = PyFloat_AsDouble(a[8]);
     if (scale == -1.0 && PyErr_Occurred()) throw PythonError{};
+    const OnStream on(a[10], t.q.device());
     const at::Tensor out = given(a[9]) ? tensor(a[9], "out") : empty({t.q.size(0), t.q.size(1)}, t.q.scalar_type(), t.q);
     if (!shaped(out, t.q.size(0), t.q.size(1)) || out.scalar_type() != t.q.scalar_type()) refuse("out must be shaped and typed like q");
     same_device(t.q, {&t.k, &t.v, &index, &count, &out});
     const int64_t ld_out = matrix(out, "out");
-    c10::cuda::CUDAGuard guard(t.q.device());
     check(dit_block_attention(&t.b, static_cast<const int32_t*>(index.data_ptr()), static_cast<const int32_t*>(count.data_ptr()), std::max<int64_t>(index.size(2), 1),
-                              static_cast<float>(scale), out.data_ptr(), ld_out, stream_on(a[10], t.q.device())));
+                              static_cast<float>(scale), out.data_ptr(), ld_out, on.raw));
     return THPVariable_Wrap(out);
   });
 }

@@ -144,3 +144,36 @@ def test_scales_whose_groups_share_their_memory_are_refused(B, rows):
     B.dit_quantize_block128(x, scales=apart[:, :rows])
     assert torch.equal(apart[:, :rows], scales) and bool((apart[:, rows:] == -1.0).all())
     assert torch.equal(B.dit_gemm_block128(codes, apart[:, :rows], w, sw), B.dit_gemm_block128(codes, scales, w, sw))
+
+
+def test_what_a_call_allocates_belongs_to_the_stream_it_is_given(B):
+    """Results and the selector's workspace; from the current stream's memory they could be handed out again, or still be in use, while
+    the kernels run on the other stream."""
+    import torch
+    heads, dim, L = 4, 128, [128 * 2000]
+    q = torch.randn(L[0], heads * dim, device="cuda").half()
+    w, sw = B.dit_quantize_weight_block128(torch.randn(heads * dim, 512, device="cuda"))
+    want = [B.dit_quantize_block128(q), B.dit_select_blocks(q, q, L, L, heads, [3])]
+    want += [(B.dit_gemm_block128(*want[0], w, sw),), (B.dit_block_attention(q, q, q, L, L, heads, *want[1]),)]
+    side = torch.cuda.Stream()
+
+    def owner(address):
+        for s in torch.cuda.memory_snapshot():
+            if s["address"] <= address < s["address"] + s["total_size"]:
+                return s["stream"]
+
+    def held():
+        return sum(s["total_size"] for s in torch.cuda.memory_snapshot() if s["stream"] == side.cuda_stream)
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    before = held()
+    got = [B.dit_select_blocks(q, q, L, L, heads, [3], stream=side)]
+    assert held() - before >= 2 * 2000 * heads * dim * 8               # the workspace (16 MB): means of the blocks of q and k
+    got = [B.dit_quantize_block128(q, stream=side)] + got
+    got += [(B.dit_gemm_block128(*got[0], w, sw, stream=side),), (B.dit_block_attention(q, q, q, L, L, heads, *got[1], stream=side),)]
+    torch.cuda.synchronize()
+    for made, expected in zip(got, want):
+        for x, y in zip(made, expected):
+            assert owner(x.data_ptr()) == side.cuda_stream
+            assert torch.equal(x.view(torch.uint8) if x.element_size() == 1 else x, y.view(torch.uint8) if y.element_size() == 1 else y)
+    assert torch.cuda.current_stream() != side and torch.cuda.current_device() == 0
