@@ -126,14 +126,14 @@ int64_t number(PyObject* o, const char* what) {
 }
 
 std::vector<int32_t> numbers(PyObject* o, const char* what) {
-  PyObject* seq = PySequence_Fast(o, "");
+  PyObject* seq = PySequence_Tuple(o);           // a copy: an item's __index__ may change a list
   if (!seq) { PyErr_Clear(); refuse(std::string(what) + " must be a sequence of whole numbers"); }
   std::vector<int32_t> v;
   try {
-    const Py_ssize_t n = PySequence_Fast_GET_SIZE(seq);
+    const Py_ssize_t n = PyTuple_GET_SIZE(seq);
     v.reserve(n);
     for (Py_ssize_t i = 0; i < n; ++i) {
-      const int64_t x = number(PySequence_Fast_GET_ITEM(seq, i), what);
+      const int64_t x = number(PyTuple_GET_ITEM(seq, i), what);
       if (x < INT32_MIN || x > INT32_MAX) refuse(std::string(what) + " is out of range", DIT_ERR_SHAPE);
       v.push_back(static_cast<int32_t>(x));
     }

@@ -177,3 +177,16 @@ def test_what_a_call_allocates_belongs_to_the_stream_it_is_given(B):
             assert owner(x.data_ptr()) == side.cuda_stream
             assert torch.equal(x.view(torch.uint8) if x.element_size() == 1 else x, y.view(torch.uint8) if y.element_size() == 1 else y)
     assert torch.cuda.current_stream() != side and torch.cuda.current_device() == 0
+
+
+def test_lengths_that_change_while_they_are_read(B):
+    import torch
+    q = torch.zeros(10, 128, dtype=torch.float16, device="cuda")
+
+    class Shrinking:
+        def __index__(self):
+            del lens[1:]
+            return 4
+    lens = [Shrinking()] + [3, 3]
+    index, count = B.dit_select_blocks(q, q, lens, (4, 3, 3), 2, [1, 1, 1])
+    assert len(lens) == 1 and index.shape == (2, 3, 1) and bool((count == 1).all())
