@@ -86,7 +86,7 @@ dit_status dit_gemm_block128(const dit_gemm_block128_args *args, void *stream);
  *   request after request: n_query_blocks = sum of ceil(q_lens[r] / 128).
  *   q, k, v   device, type f16 or bf16, 16-byte aligned, leading dimensions multiples of 8 and >= n_heads * head_dim
  *             (three column ranges of one packed [rows, 3 * width] buffer are fine)
- *   head_dim  64 or 128; n_requests <= DIT_MAX_REQUESTS */
+ *   head_dim  64 or 128; n_requests <= DIT_MAX_REQUESTS; at most 16384 key blocks in a request (DIT_ERR_SHAPE beyond) */
 typedef struct {
   const void *q, *k, *v;
   int64_t ld_q, ld_k, ld_v;
@@ -120,7 +120,7 @@ dit_status dit_select_blocks(const dit_attention_batch *batch, const int32_t *ke
  * request's key blocks are ignored.  A row without any key gets zeros.  Rows of other requests are never
  * part of a result, whatever they hold.  Scores, the softmax and the sums are held in fp32; probabilities are rounded
  * to the inputs' type for the second product, as the step's attention does.
- *   scale   0 for 1 / sqrt(head_dim)
+ *   scale   0 for 1 / sqrt(head_dim); at most 2e38
  *   out     device, the inputs' type, rows as q's, 16-byte aligned, ld_out a multiple of 8 and >= n_heads * head_dim;
  *           must not overlap the inputs */
 dit_status dit_block_attention(const dit_attention_batch *batch, const int32_t *block_index, const int32_t *block_count,

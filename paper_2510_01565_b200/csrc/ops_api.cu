@@ -409,7 +409,7 @@ dit_status run_block_attention(const dit_attention_batch* a, const int32_t* bloc
   if (!block_index || !block_count || !out || ld_index < 1) return DIT_ERR_INVALID_ARG;
   if (!aligned(block_index, 4) || !aligned(block_count, 4) || !aligned(out, 16) || ld_out % 8 || ld_out < static_cast<int64_t>(a->n_heads) * a->head_dim)
     return DIT_ERR_INVALID_ARG;
-  if (!(scale >= 0.f) || !(scale <= 3.0e38f)) return DIT_ERR_INVALID_ARG;
+  if (!(scale >= 0.f) || !(scale <= 2.0e38f)) return DIT_ERR_INVALID_ARG;      // scale * log2(e) has to be finite
   const DeviceState* d;
   s = ready(&d);
   if (s != DIT_OK) return s;

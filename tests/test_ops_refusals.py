@@ -156,3 +156,11 @@ def test_workspace_of_the_reduced_modes(lib):
     for bad in (16, 32 | 1, 32 | 2, 32 | 4, 32 | 8, 128):
         assert ws(flags=bad) == 0, bad
     assert lib.dit_ctx_set_sparse_attention(None, 0.5, 1) == INVALID
+
+
+def test_a_scale_whose_product_with_log2_e_is_infinite_is_refused(lib):
+    b, keepalive = B.DitAttentionBatch(), (C.c_int32 * 1)(4)
+    for name, value in dict(q=P, k=P, v=P, ld_q=128, ld_k=128, ld_v=128, type=0, n_heads=1, head_dim=128, n_requests=1, q_lens=keepalive, kv_lens=keepalive).items():
+        setattr(b, name, value)
+    for scale in (2.4e38, 3.0e38):
+        assert lib.dit_block_attention(C.byref(b), P, P, 1, scale, P, 128, None) == INVALID
