@@ -462,6 +462,8 @@ block_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
 done:
   tc_fence_before();
   __syncthreads();
+  settle_if_aborted(abort_flag);
+  __syncwarp();
   if (warp == 1) { tc_fence_after(); tmem_dealloc(tmem_base, 512); }
   if (threadIdx.x == 0 && *abort_flag) atomicMax(p.status, kStatusAttnTimeout);
 }
@@ -659,6 +661,7 @@ block_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
       }
   }
   __syncthreads();                             // every tile has been read: the partial results take the ring's place
+  settle_if_aborted(abort_flag);
   if (warp < 4) {
 #pragma unroll
     for (int r = 0; r < 2; ++r) {

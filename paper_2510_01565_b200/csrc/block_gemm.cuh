@@ -428,6 +428,8 @@ done:
   bulk_store_done();                                                   // (threads that stored nothing pass at once)
   tc_fence_before();
   __syncthreads();
+  settle_if_aborted(abort_flag);
+  __syncwarp();
   cluster_sync_all();
   if (warp == 1) { tc_fence_after(); tmem_dealloc_pair(tmem_base, 512); }
   if (threadIdx.x == 0 && *abort_flag) atomicMax(p.status, kStatusGemmTimeout);
@@ -603,7 +605,7 @@ gemm_block128_split_kernel(const __grid_constant__ CUtensorMap tmA, const __grid
   }
   if (splits > 1) {
     __syncwarp();
-    cluster_sync_all();
+    cluster_sync_all();                        // (a CTA that gave up may have copies under way: it settles below)
     if (warp >= 2 && col < p.N) {
       const float bias = p.bias ? __ldg(p.bias + col) : 0.f;
       const int rows = min(BT, p.M - m0);
@@ -629,6 +631,8 @@ gemm_block128_split_kernel(const __grid_constant__ CUtensorMap tmA, const __grid
   }
   tc_fence_before();
   __syncthreads();
+  settle_if_aborted(abort_flag);
+  __syncwarp();
   if (warp == 1) { tc_fence_after(); tmem_dealloc(tmem_base, C::COLS); }
   if (threadIdx.x == 0 && *abort_flag) atomicMax(p.status, kStatusGemmTimeout);
 }

@@ -105,6 +105,14 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
   return mbar_wait_limited<(1 << 16), kWaitLimitNs>(bar, parity, abort_flag);
 }
 
+// For a CTA that gave up waiting, called by all its threads after they have met: copies into its shared memory and products in its tensor
+// memory may still be under way, so it stays for the 2 ms in which any that can complete does, then returns them.
+__device__ __forceinline__ void settle_if_aborted(volatile int* abort_flag) {
+  if (!*abort_flag) return;
+  const uint64_t t0 = global_ns();
+  for (int i = 0; i < (1 << 16) && global_ns() - t0 < 2000000ull; ++i) __nanosleep(256);
+}
+
 // One-dimensional bulk copy global -> shared (no tensor map): both addresses 16-byte aligned, size a
 // multiple of 16 bytes; completion is reported to the mbarrier as transferred bytes.
 __device__ __forceinline__ void bulk_load(uint32_t smem_dst, const void* gmem_src, uint32_t bytes, uint32_t bar) {
