@@ -118,7 +118,8 @@ dit_status dit_select_blocks(const dit_attention_batch *batch, const int32_t *ke
  * The lists are those of dit_select_blocks or the caller's own: the first block_count entries of each list count, clamped
  * to [0, ld_index]; their order does not matter, an entry listed twice counts once, and entries outside the
  * request's key blocks are ignored.  A row without any key gets zeros.  Rows of other requests are never
- * part of a result, whatever they hold.  Scores, the softmax and the sums are held in fp32; probabilities are rounded
+ * part of a result, whatever they hold.  Scores, their differences, the softmax and the sums are held in fp32, so scaled scores may
+ * be of any size as long as q_i . k_j itself and the difference of two of them stay inside fp32; probabilities are rounded
  * to the inputs' type for the second product, as the step's attention does.
  *   scale   0 for 1 / sqrt(head_dim); at most 2e38
  *   out     device, the inputs' type, rows as q's, 16-byte aligned, ld_out a multiple of 8 and >= n_heads * head_dim;

@@ -333,6 +333,7 @@ block_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
     const float c = p.scale_log2;
     const float2 c2 = make_float2(c, c);
     constexpr float kRescaleLog2 = 8.0f;       // O is rescaled when a row's maximum has grown by more than 2^8: P stays <= 2^8
+    constexpr float kFarLog2 = 1024.0f;        // scaled references beyond it are taken off before the scaling
     uint32_t use = 0;                          // key blocks of this warpgroup so far
 
     for (int item = blockIdx.x; item < p.items; item += gridDim.x) {
@@ -393,8 +394,18 @@ block_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
               tmem_st_wait();
             }
           }
-          // a reference of -inf (every score so far -inf, from infinite inputs) would make the exponents NaN
-          const float neg_mc = m_ref == -INFINITY ? 0.f : -m_ref * c;
+          // The exponent is s * c - round(m_ref * c): the rounding, at most 2^-14 below the limit, is common to all that share a reference.
+          // It grows with the product and from 2^28 on would leave the 16-bit probabilities, so beyond the limit the reference
+          // is taken off the scores first: (s - m_ref) * c is 0 for the largest one whatever c is.  Decided row by row (the loop, for
+          // the warp, is one that ordinary scores never run), so that a row does not depend on its neighbours.
+          // A reference of -inf (every score so far -inf, from infinite inputs) would make the exponents NaN: none is taken off.
+          const bool far = fabsf(m_ref * c) > kFarLog2 && m_ref != -INFINITY;
+          if (__any_sync(0xffffffffu, far)) {
+            const float off = far ? m_ref : 0.f;
+#pragma unroll
+            for (int i = 0; i < 128; ++i) sv[i] = __float_as_uint(__uint_as_float(sv[i]) - off);
+          }
+          const float neg_mc = (far || m_ref == -INFINITY) ? 0.f : -m_ref * c;
           const float2 nm2 = make_float2(neg_mc, neg_mc);
           float2 rs0 = make_float2(0.f, 0.f), rs1 = make_float2(0.f, 0.f);
 #pragma unroll
@@ -620,12 +631,13 @@ block_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
             float mx = fmaxf(fmaxf(s[0][2 * r], s[0][2 * r + 1]), fmaxf(s[1][2 * r], s[1][2 * r + 1]));
             mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
             mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-            const float top = fmaxf(m[r], mx * p.scale_log2), at = top == -INFINITY ? 0.f : top;
-            const float alpha = exp2_approx(m[r] - at);                 // 0 while m is -inf
+            // the reference is taken off before the scaling: the largest score's exponent is 0 however large the factor is
+            const float top = fmaxf(m[r], mx), at = top == -INFINITY ? 0.f : top;
+            const float alpha = exp2_approx((m[r] - at) * p.scale_log2);                 // 0 while m is -inf
             m[r] = top;
             float e[4];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) e[k] = exp2_approx(fmaf(s[k >> 1][2 * r + (k & 1)], p.scale_log2, -at));
+            for (int k = 0; k < 4; ++k) e[k] = exp2_approx((s[k >> 1][2 * r + (k & 1)] - at) * p.scale_log2);
             l[r] = l[r] * alpha + (e[0] + e[1]) + (e[2] + e[3]);
             pa[r] = pack16x2<BF16>(e[0], e[1]);
             pa[2 + r] = pack16x2<BF16>(e[2], e[3]);
@@ -691,7 +703,7 @@ block_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
         for (int w = 0; w < 4; ++w) {
           const float pm = read(s, w, D), pl = read(s, w, D + 1), po = read(s, w, threadIdx.x);
           const float top = fmaxf(ref, pm), at = top == -INFINITY ? 0.f : top;
-          const float keep = exp2_approx(ref - at), f = exp2_approx(pm - at);
+          const float keep = exp2_approx((ref - at) * p.scale_log2), f = exp2_approx((pm - at) * p.scale_log2);
           sum = sum * keep + pl * f;
           o = o * keep + po * f;
           ref = top;

@@ -332,3 +332,67 @@ def test_select_and_attend_on_another_stream_and_in_a_graph(B):
     want = both()
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(third, want)) and not torch.equal(first[1], third[1])
+
+
+# ------------------------------------------------------------------------------------------------ scores and values at the format's edges
+def whole_numbers(seed, q_lens, kv_lens, heads, dim, kind, unit, offset):
+    """q and k of small whole numbers times `unit`, every other row of q louder by powers of two, and a channel that shifts all of a row's
+    scores alike: products and their sums are whole multiples of unit^2 below 2^24, which fp32 holds without rounding in any order."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    n = lambda rows: torch.randint(-2, 3, (rows, heads * dim), generator=g, device="cuda").float()
+    q, k, v = n(sum(q_lens)), n(sum(kv_lens)), torch.randn(sum(kv_lens), heads * dim, generator=g, device="cuda")
+    q[:, ::dim], k[:, ::dim] = 30.0 * (offset != 0), float(offset)
+    q *= torch.exp2((torch.arange(len(q), device="cuda") % 4).float() * (torch.arange(len(q), device="cuda") % 2))[:, None]
+    t = getattr(torch, kind)
+    return (q * unit).to(t), (k * unit).to(t), v.to(t)
+
+
+def exact_scores(q, k, v, q_lens, kv_lens, heads, index, count, scale):
+    """(result, allowed error) in 64 bits where the scores are exact.  What is left of the error, in natural units of the exponent: the factor
+    scale * log2 e (off by 2^-22 of itself, with exponents of at most 40 where a probability counts: 40 * 2^-22), the hardware's exp2 (2^-21), and
+    a reference rounded after scaling while it is below 2^10 (2^-14, for two references of one row 2^-13); below 2^-12 together.
+    Then as for `plain`: probabilities and result rounded to the inputs' type, sums in fp32, the smallest probabilities."""
+    import torch
+    dim, eps = q.shape[1] // heads, torch.finfo(q.dtype).eps
+    scale = float(np.float32(scale or np.float32(1.0) / np.sqrt(np.float32(dim))))
+    out, room = torch.zeros(q.shape, dtype=torch.float64, device="cuda"), torch.zeros(q.shape, dtype=torch.float64, device="cuda")
+    b = q0 = k0 = 0
+    for ql, kl in zip(q_lens, kv_lens):
+        for first in range(0, ql, 128):
+            rows = slice(q0 + first, q0 + min(ql, first + 128))
+            for h in range(heads):
+                cols = slice(h * dim, (h + 1) * dim)
+                chosen = sorted(set(index[h, b, :int(count[h, b])].tolist()))
+                keys = torch.tensor([k0 + i for j in chosen for i in range(128 * j, min(kl, 128 * j + 128))], dtype=torch.long, device="cuda")
+                s = scale * (q[rows, cols].double() @ k[keys, cols].double().t())
+                p, z = torch.softmax(s, dim=1), v[keys, cols].double()
+                out[rows, cols], mag, n = p @ z, p @ z.abs(), len(keys)
+                room[rows, cols] = mag * (2 * 2.0 ** -12 + eps / 2 + n * 2.0 ** -23) + n * 2.0 ** -25 * z.abs().amax()
+            b += 1
+        q0, k0 = q0 + ql, k0 + kl
+    room += eps / 2 * (out.abs() + room) + (2.0 ** -25 if q.dtype == torch.float16 else 0.0)
+    return out, room
+
+
+@pytest.mark.parametrize("q_lens", [[3, 16], [140, 16]])
+@pytest.mark.parametrize("kind,dim,unit,scale", [("float16", 64, 1.0, s) for s in (0.0, 2.0 ** -4, 1e4, 1e6, 1e8, 1e12, 2e38)]
+                         + [("bfloat16", 128, 1.0, s) for s in (1e8, 2e38)]
+                         + [("float16", 128, 2048.0, 0.0), ("bfloat16", 64, 2.0 ** 20, 0.0), ("bfloat16", 128, 2.0 ** 56, 0.0), ("bfloat16", 64, 2.0 ** 54, 1.0)])
+@pytest.mark.parametrize("offset", [0, 30, -30])
+def test_large_scaled_scores(B, q_lens, kind, dim, unit, scale, offset):
+    """Scaled scores of any size fp32 holds, and factors up to the largest that is accepted: the largest keys of a row share its result, whatever
+    the sign of their scores.  (An exponent formed as s * c - round(m * c) is off by the rounding of m * c, which is 16 at 2^28 and
+    infinite soon after 2^128: the row then came out as zeros.)"""
+    import torch
+    heads, kv_lens = 2, [700, 300]
+    if kind == "float16" and unit > 1 and offset:
+        unit /= 32.0                                                    # 30 * 8 * unit has to stay below 65504
+    q, k, v = whole_numbers(71 + dim, q_lens, kv_lens, heads, dim, kind, unit, offset)
+    n_q = sum(blocks_of(l) for l in q_lens)
+    index = torch.tensor([5, 0, 2], dtype=torch.int32, device="cuda").expand(heads, n_q, 3).contiguous()
+    index[:, -1] = torch.tensor([2, 0, 1], dtype=torch.int32)
+    count = torch.full((heads, n_q), 3, dtype=torch.int32, device="cuda")
+    out = B.dit_block_attention(q, k, v, q_lens, kv_lens, heads, index, count, scale=scale)
+    B.dit_ops_poll_status()
+    check(out, exact_scores(q, k, v, q_lens, kv_lens, heads, index, count, scale))
