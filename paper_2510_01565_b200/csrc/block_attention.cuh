@@ -372,10 +372,15 @@ block_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
             mx3 = fmax3(mx3, __uint_as_float(sv[i + 6]), __uint_as_float(sv[i + 7]));
           }
           const float mx = fmaxf(fmaxf(mx0, mx1), fmaxf(mx2, mx3));
-          if (use == first_use) {
-            m_ref = mx;
-          } else {
-            const bool grow = (mx - m_ref) * c > kRescaleLog2;
+          // Two rare things, behind one vote.  A row's maximum has grown far beyond its reference: this warp's rows of O are rescaled.
+          // Or its reference is large: the exponent s * c - round(m_ref * c) is off by that rounding, which is at most 2^-14 below the
+          // limit and common to all that share the reference, but from 2^28 on would leave the 16-bit probabilities.  Beyond the
+          // limit the reference is therefore taken off the scores before the scaling: (s - m_ref) * c is 0 for the largest
+          // whatever c is.  Decided row by row, so that a row does not depend on its neighbours.
+          if (use == first_use) m_ref = mx;
+          const bool grow = (mx - m_ref) * c > kRescaleLog2;
+          bool far = fabsf(m_ref * c) > kFarLog2;
+          if (__any_sync(0xffffffffu, grow || far)) {
             if (__any_sync(0xffffffffu, grow)) {
               if (!__all_sync(0xffffffffu, mbar_wait(o_full(tile), (use - 1) & 1u, abort_flag))) goto done;
               tc_fence_after();
@@ -393,19 +398,13 @@ block_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
               }
               tmem_st_wait();
             }
-          }
-          // The exponent is s * c - round(m_ref * c): the rounding, at most 2^-14 below the limit, is common to all that share a reference.
-          // It grows with the product and from 2^28 on would leave the 16-bit probabilities, so beyond the limit the reference
-          // is taken off the scores first: (s - m_ref) * c is 0 for the largest one whatever c is.  Decided row by row (the loop, for
-          // the warp, is one that ordinary scores never run), so that a row does not depend on its neighbours.
-          // A reference of -inf (every score so far -inf, from infinite inputs) would make the exponents NaN: none is taken off.
-          const bool far = fabsf(m_ref * c) > kFarLog2 && m_ref != -INFINITY;
-          if (__any_sync(0xffffffffu, far)) {
-            const float off = far ? m_ref : 0.f;
+            far = fabsf(m_ref * c) > kFarLog2;
+            // (a reference of -inf, every score so far -inf from infinite inputs, would make the exponents NaN: nothing is taken off)
+            const float off = far && m_ref != -INFINITY ? m_ref : 0.f;
 #pragma unroll
             for (int i = 0; i < 128; ++i) sv[i] = __float_as_uint(__uint_as_float(sv[i]) - off);
           }
-          const float neg_mc = (far || m_ref == -INFINITY) ? 0.f : -m_ref * c;
+          const float neg_mc = far ? 0.f : -m_ref * c;
           const float2 nm2 = make_float2(neg_mc, neg_mc);
           float2 rs0 = make_float2(0.f, 0.f), rs1 = make_float2(0.f, 0.f);
 #pragma unroll
