@@ -120,7 +120,10 @@ dit_status dit_select_blocks(const dit_attention_batch *batch, const int32_t *ke
  * request's key blocks are ignored.  A row without any key gets zeros.  Rows of other requests are never
  * part of a result, whatever they hold.  Scores, their differences, the softmax and the sums are held in fp32, so scaled scores may
  * be of any size as long as q_i . k_j itself and the difference of two of them stay inside fp32; probabilities are rounded
- * to the inputs' type for the second product, as the step's attention does.
+ * to the inputs' type for the second product, as the step's attention does.  An infinite value makes its channel of the rows that
+ * list it infinite, or NaN where its probability rounds to zero or the other infinity is listed as well; finite values above 2^98 may
+ * do the same by the sums, which are taken before the division.  Finite results clamp to the type's largest value.  A row all of whose
+ * scores are -infinity gets zeros.
  *   scale   0 for 1 / sqrt(head_dim); at most 2e38
  *   out     device, the inputs' type, rows as q's, 16-byte aligned, ld_out a multiple of 8 and >= n_heads * head_dim;
  *           must not overlap the inputs */

@@ -4,6 +4,8 @@
 // block_rows_kernel        up to 16 query rows of a head per cluster, for a few rows that read a long context
 // block_means_kernel, block_select_kernel   the selector
 #pragma once
+#include <type_traits>
+
 #include "attention.cuh"
 #include "common.cuh"
 #include "ptx.cuh"
@@ -28,8 +30,20 @@ struct BlockAttnParams {
   float scale_log2;          // scale * log2(e), positive
   int items;                 // (request, head, 256 query rows) triples
   int wide_out;              // rows of out start on 32-byte boundaries
+  int clamp;                 // infinite results become the largest finite value (steps, whose activations all do)
   int* status;
 };
+
+// Results are packed with finite values clamped (rounded probabilities may add up to a little more than one, and a value at the
+// format's limit must not leave it); an infinite result stays one.
+template <bool BF16>
+__device__ __forceinline__ uint32_t infinity_bits(float x) { return (BF16 ? 0x7F80u : 0x7C00u) | (x < 0.f ? 0x8000u : 0u); }
+template <bool BF16>
+__device__ __forceinline__ uint32_t put_infinities(uint32_t packed, float lo, float hi) {
+  if (fabsf(lo) == INFINITY) packed = (packed & 0xFFFF0000u) | infinity_bits<BF16>(lo);
+  if (fabsf(hi) == INFINITY) packed = (packed & 0x0000FFFFu) | infinity_bits<BF16>(hi) << 16;
+  return packed;
+}
 
 constexpr int kWindowBlocks = 256;      // key blocks whose lists are laid out in shared memory at a time
 constexpr int kMaxKeyBlocks = 16384;    // of one request
@@ -439,33 +453,51 @@ block_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
         tc_fence_after();
       }
       const float inv = l == 0.f ? 0.f : 1.0f / l;
+      // The results of 32 channels at a time; `kept` writes infinities as such and is a second pass over the rare rows that have one, so that
+      // the ordinary one pays for the largest magnitude only.
+      float largest[2] = {0.f, 0.f};
+      auto write = [&](auto kept) {
 #pragma unroll 1
-      for (int ch = 0; ch < D / 32; ++ch) {
-        uint32_t r[32];
-        __syncwarp();
-        if (any) {
-          tmem_ld32(tOi + ch * 32, r);
-          tmem_ld_wait();
-        } else {
+        for (int ch = 0; ch < D / 32; ++ch) {
+          uint32_t r[32];
+          __syncwarp();
+          if (any) {
+            tmem_ld32(tOi + ch * 32, r);
+            tmem_ld_wait();
+          } else {
 #pragma unroll
-          for (int i = 0; i < 32; ++i) r[i] = 0u;
-        }
-        if (row < it.q_len) {
+            for (int i = 0; i < 32; ++i) r[i] = 0u;
+          }
+          if (row < it.q_len) {
 #pragma unroll
-          for (int v = 0; v < 2; ++v) {        // a lane writes its own row, a whole 32-byte sector per store
-            uint32_t wd[8];
+            for (int v = 0; v < 2; ++v) {      // a lane writes its own row, a whole 32-byte sector per store
+              uint32_t wd[8];
 #pragma unroll
-            for (int h = 0; h < 8; ++h) wd[h] = pack16x2<BF16>(__uint_as_float(r[16 * v + 2 * h]) * inv, __uint_as_float(r[16 * v + 2 * h + 1]) * inv);
-            uint16_t* at = out + ch * 32 + v * 16;
-            if (p.wide_out) {
-              st_global_v8(at, wd);
-            } else {
-              reinterpret_cast<uint4*>(at)[0] = make_uint4(wd[0], wd[1], wd[2], wd[3]);
-              reinterpret_cast<uint4*>(at)[1] = make_uint4(wd[4], wd[5], wd[6], wd[7]);
+              for (int h = 0; h < 8; ++h) {
+                const float lo = __uint_as_float(r[16 * v + 2 * h]), hi = __uint_as_float(r[16 * v + 2 * h + 1]);
+                wd[h] = pack16x2<BF16>(lo * inv, hi * inv);
+                if constexpr (decltype(kept)::value) wd[h] = put_infinities<BF16>(wd[h], lo * inv, hi * inv);
+              }
+              uint16_t* at = out + ch * 32 + v * 16;
+              if (p.wide_out) {
+                st_global_v8(at, wd);
+              } else {
+                reinterpret_cast<uint4*>(at)[0] = make_uint4(wd[0], wd[1], wd[2], wd[3]);
+                reinterpret_cast<uint4*>(at)[1] = make_uint4(wd[4], wd[5], wd[6], wd[7]);
+              }
+            }
+            if constexpr (!decltype(kept)::value) {
+#pragma unroll
+              for (int i = 0; i < 32; i += 4) {
+                largest[0] = fmax3(largest[0], fabsf(__uint_as_float(r[i])), fabsf(__uint_as_float(r[i + 1])));
+                largest[1] = fmax3(largest[1], fabsf(__uint_as_float(r[i + 2])), fabsf(__uint_as_float(r[i + 3])));
+              }
             }
           }
         }
-      }
+      };
+      write(std::false_type{});
+      if (!p.clamp && __any_sync(0xffffffffu, fmaxf(largest[0], largest[1]) == INFINITY)) write(std::true_type{});
     }
   }
 
@@ -707,7 +739,9 @@ block_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
           o = o * keep + po * f;
           ref = top;
         }
-      static_cast<uint16_t*>(p.out)[(static_cast<long long>(q_begin) + row) * p.ld_out + head * D + threadIdx.x] = pack16<BF16>(sum == 0.f ? 0.f : o / sum);
+      const float x = sum == 0.f ? 0.f : o / sum;
+      static_cast<uint16_t*>(p.out)[(static_cast<long long>(q_begin) + row) * p.ld_out + head * D + threadIdx.x] =
+          fabsf(x) == INFINITY && !p.clamp ? static_cast<uint16_t>(infinity_bits<BF16>(x)) : pack16<BF16>(x);
     }
   }
   __syncwarp();

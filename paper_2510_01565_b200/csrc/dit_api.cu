@@ -529,7 +529,7 @@ dit_status step_impl(dit_ctx* ctx, const void* tokens, const int32_t* lens, int 
     dit_status s = DIT_OK;
     DIT_CUDA_TRY(ctx, timed(DIT_KERNEL_ATTENTION, [&] {
       s = dit_select_blocks(&ab, sp_keep, sp_tail, index, count, sp_widest, ctx->at<void>(ctx->lay.sp_means), dit_select_blocks_workspace(&ab), st);
-      if (s == DIT_OK) s = run_block_attention(&ab, index, count, sp_widest, 0.f, dst, ld_dst, status, st);
+      if (s == DIT_OK) s = run_block_attention(&ab, index, count, sp_widest, 0.f, dst, ld_dst, status, true, st);
       return cudaSuccess;
     }));
     launches += 2;                               // two kernels select, one attends

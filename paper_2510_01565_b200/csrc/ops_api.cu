@@ -327,11 +327,12 @@ cudaError_t launch_select(const dit_attention_batch& a, const BlockBatch& b, Blo
 }
 
 cudaError_t launch_block_attention(const dit_attention_batch& a, const BlockBatch& b, const int32_t* index, const int32_t* count, int64_t ld_index,
-                                   float scale, void* out, int64_t ld_out, int* status, const DeviceState& d, cudaStream_t st) {
+                                   float scale, void* out, int64_t ld_out, int* status, bool clamp, const DeviceState& d, cudaStream_t st) {
   BlockAttnParams p{};
   p.out = out; p.ld_out = ld_out; p.index = index; p.count = count; p.ld_index = ld_index; p.n_heads = a.n_heads;
   p.scale_log2 = 1.4426950408889634f * (scale > 0.f ? scale : 1.0f / sqrtf(static_cast<float>(a.head_dim)));
   p.status = status ? status : d.status;
+  p.clamp = clamp;
   if (a.head_dim == 128) return a.type == DIT_TYPE_BF16 ? launch_attend<128, true>(d, a, b, p, st) : launch_attend<128, false>(d, a, b, p, st);
   return a.type == DIT_TYPE_BF16 ? launch_attend<64, true>(d, a, b, p, st) : launch_attend<64, false>(d, a, b, p, st);
 }
@@ -401,7 +402,7 @@ cudaError_t launch_quantize_weight(const void* w, dit_type type, long long ld, i
 }
 
 dit_status run_block_attention(const dit_attention_batch* a, const int32_t* block_index, const int32_t* block_count, int64_t ld_index,
-                               float scale, void* out, int64_t ld_out, int* status, cudaStream_t st) {
+                               float scale, void* out, int64_t ld_out, int* status, bool clamp, cudaStream_t st) {
   BlockBatch b;
   dit_status s = plan_batch(a, true, &b);
   if (s != DIT_OK) return s;
@@ -413,7 +414,7 @@ dit_status run_block_attention(const dit_attention_batch* a, const int32_t* bloc
   const DeviceState* d;
   s = ready(&d);
   if (s != DIT_OK) return s;
-  return launch_block_attention(*a, b, block_index, block_count, ld_index, scale, out, ld_out, status, *d, st) == cudaSuccess ? DIT_OK : DIT_ERR_CUDA;
+  return launch_block_attention(*a, b, block_index, block_count, ld_index, scale, out, ld_out, status, clamp, *d, st) == cudaSuccess ? DIT_OK : DIT_ERR_CUDA;
 }
 
 }  // namespace dit
@@ -513,7 +514,7 @@ dit_status dit_select_blocks(const dit_attention_batch* a, const int32_t* keep, 
 
 dit_status dit_block_attention(const dit_attention_batch* a, const int32_t* block_index, const int32_t* block_count, int64_t ld_index,
                                float scale, void* out, int64_t ld_out, void* stream) {
-  return run_block_attention(a, block_index, block_count, ld_index, scale, out, ld_out, nullptr, static_cast<cudaStream_t>(stream));
+  return run_block_attention(a, block_index, block_count, ld_index, scale, out, ld_out, nullptr, false, static_cast<cudaStream_t>(stream));
 }
 
 dit_status dit_ops_poll_status(void) {

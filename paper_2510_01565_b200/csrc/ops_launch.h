@@ -30,9 +30,10 @@ struct BlockProduct {
 
 cudaError_t ops_prepare_device();                      // sets kernel attributes once per device
 cudaError_t launch_block_product(const BlockProduct& b, const SeqInfo& seq, cudaStream_t st);
-// dit_block_attention with a status word of the caller's
+// dit_block_attention with a status word of the caller's.  clamp: infinite results become the largest finite value, as in every
+// activation of a step, where an infinity would meet zeros further on.
 dit_status run_block_attention(const dit_attention_batch* batch, const int32_t* block_index, const int32_t* block_count, int64_t ld_index, float scale,
-                               void* out, int64_t ld_out, int* status, cudaStream_t st);
+                               void* out, int64_t ld_out, int* status, bool clamp, cudaStream_t st);
 cudaError_t launch_quantize_rows(const void* x, dit_type type, long long ld, long long rows, long long cols, void* codes,
                                  long long ld_codes, float* scales, long long ld_scales, cudaStream_t st);
 cudaError_t launch_quantize_weight(const void* w, dit_type type, long long ld, int in_dim, int out_dim, void* codes, long long ld_codes,

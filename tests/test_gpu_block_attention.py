@@ -396,3 +396,34 @@ def test_large_scaled_scores(B, q_lens, kind, dim, unit, scale, offset):
     out = B.dit_block_attention(q, k, v, q_lens, kv_lens, heads, index, count, scale=scale)
     B.dit_ops_poll_status()
     check(out, exact_scores(q, k, v, q_lens, kv_lens, heads, index, count, scale))
+
+
+@pytest.mark.parametrize("q_lens", [[3, 16], [140, 16]])
+@pytest.mark.parametrize("kind", ["float16", "bfloat16"])
+def test_an_infinity_in_a_listed_block_is_not_hidden(B, q_lens, kind):
+    """As in the definition, an infinite value makes its channel infinite, and two of opposite signs a NaN; a channel at the type's largest
+    value stays there although the rounded probabilities may add up to a little more than one."""
+    import torch
+    heads, dim, kv_lens = 1, 64, [300, 200]
+    q, k, v = draw(73, q_lens, kv_lens, heads, dim, kind, sharp=0.25)   # every probability is far above what rounds to zero
+    n_q = sum(blocks_of(l) for l in q_lens)
+    index = torch.tensor([[[0, 2]] * (n_q - 1) + [[0, 1]]], dtype=torch.int32, device="cuda")
+    count = torch.full((1, n_q), 2, dtype=torch.int32, device="cuda")
+    v[10], v[300 + 150] = 0.0, 0.0
+    clean = B.dit_block_attention(q, k, v, q_lens, kv_lens, heads, index, count)
+    inf = float("inf")
+    top = 65504.0 if kind == "float16" else 2.0 ** 98
+    for r in (10, 300 + 150):
+        v[r, 3], v[r, 4], v[r, 5] = inf, -inf, inf
+    for r in (11, 300 + 20):
+        v[r, 5] = -inf
+    v[:, 6], v[:, 7], v[130, :] = top, -top, inf                        # (row 130 belongs to a block that nobody lists)
+    out = B.dit_block_attention(q, k, v, q_lens, kv_lens, heads, index, count)
+    B.dit_ops_poll_status()
+    assert bool((out[:, 3] == inf).all()) and bool((out[:, 4] == -inf).all()) and bool(out[:, 5].isnan().all())
+    # top times a weighted mean of ones: off by the probabilities' rounding, the sums' and the result's
+    for c, want in ((6, top), (7, -top)):
+        assert bool((out[:, c].double() / want - 1.0).abs().max() <= torch.finfo(out.dtype).eps + 2.0 ** -11)
+        assert bool(out[:, c].isfinite().all())
+    rest = [c for c in range(64) if not 3 <= c <= 7]
+    assert torch.equal(out[:, rest], clean[:, rest])
