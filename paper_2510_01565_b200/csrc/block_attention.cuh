@@ -948,7 +948,7 @@ block_select_kernel(const BlockSelectParams p, const __grid_constant__ BlockBatc
     written += __popc(taken);
     if (ties != INT32_MAX) ties = max(0, ties - __popc(equal));
   }
-  for (int e = want + lane; e < p.widest; e += 32) list[e] = -1;
+  for (long long e = want + lane; e < p.widest; e += 32) list[e] = -1;           // (widest may be the largest int: `all of them`)
   if (lane == 0) p.count[at] = want;
 }
 

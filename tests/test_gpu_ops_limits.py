@@ -190,3 +190,21 @@ def test_lengths_that_change_while_they_are_read(B):
     lens = [Shrinking()] + [3, 3]
     index, count = B.dit_select_blocks(q, q, lens, (4, 3, 3), 2, [1, 1, 1])
     assert len(lens) == 1 and index.shape == (2, 3, 1) and bool((count == 1).all())
+
+
+def test_a_selector_asked_for_more_blocks_than_any_request_has(B):
+    """keep = 2^31 - 1, as a caller may write `all of them`: every block, then -1 to the end of the list, and nothing around it.  (A 32-bit
+    counter of the entries behind the last block would pass the largest int in its last step and go on in front of the list.)"""
+    import torch
+    if torch.cuda.mem_get_info()[0] < 20 << 30:
+        pytest.skip("needs a list of 8.6 GB")
+    keep, pad = 2 ** 31 - 1, 4096
+    q = torch.randn(300, 64, device="cuda").half()
+    buf = torch.full((keep + 2 * pad,), 7, dtype=torch.int32, device="cuda")
+    index = buf[pad:pad + keep].view(1, 1, keep)
+    count = torch.empty(1, 1, dtype=torch.int32, device="cuda")
+    B.dit_select_blocks(q[:100], q, [100], [300], 1, [keep], index=index, count=count)
+    torch.cuda.synchronize()
+    assert count.tolist() == [[3]] and index[0, 0, :3].tolist() == [0, 1, 2]
+    assert bool((buf[:pad] == 7).all()) and bool((buf[pad + keep:] == 7).all())
+    assert int(buf[pad + 3:pad + keep].max()) == -1 and int(buf[pad + 3:pad + keep].min()) == -1
