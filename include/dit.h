@@ -153,7 +153,8 @@ dit_status dit_ctx_create(const dit_config *cfg, void *workspace, size_t workspa
 dit_status dit_ctx_destroy(dit_ctx *ctx);
 
 /* For contexts created with DIT_FLAG_SPARSE_ATTENTION: from the next step on, every block of 128 query rows of a request with n
- * blocks of 128 keys attends to max(min_blocks, ceil(keep * n)) of them (all n at most; n <= 16384), chosen per head by the
+ * blocks of 128 keys attends to max(min_blocks, ceil(keep * n)) of them (all n at most; n <= 16384; a keep * n above a whole number by
+ * no more than 2^-24 of itself, what rounding keep to a float can add, counts as that number), chosen per head by the
  * product of the blocks' mean query and mean key.  A request's text rows are always among the chosen keys (as far as
  * they fit) where the call knows them, i.e. in dit_step_forward_requests, dit_denoise_step and dit_denoise_round.  0 < keep <= 1,
  * min_blocks >= 1; keep == 1, the state after creation, is the dense step bit for bit, and so is any step in

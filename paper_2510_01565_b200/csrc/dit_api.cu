@@ -510,8 +510,9 @@ dit_status step_impl(dit_ctx* ctx, const void* tokens, const int32_t* lens, int 
     for (int r = 0; r < n; ++r) {
       const int blocks = static_cast<int>(blocks_of(lens[r]));
       if (blocks > kMaxSelectBlocks) return fail(ctx, DIT_ERR_CAPACITY, "a request is too long for attention over selected blocks");
-      // (keep is rounded to fp32: a product that is above a whole number by no more than that rounding counts as that number)
-      const int share = static_cast<int>(std::ceil(static_cast<double>(ctx->sparse_keep) * blocks * (1.0 - 1e-6)));
+      // keep is rounded to fp32, by at most 2^-24 of itself: a product that is above a whole number by no more than that counts as that
+      // number.  (The first product is exact in 64 bits; 1 - 2^-24 times the largest one forgiven is that number less 2^-48 of it.)
+      const int share = static_cast<int>(std::ceil(static_cast<double>(ctx->sparse_keep) * blocks * (1.0 - 0x1p-24)));
       sp_keep[r] = std::min(blocks, std::max({1, share, ctx->sparse_min_blocks}));
       sp_tail[r] = geo ? lens[r] - (geo->img_cu[r + 1] - geo->img_cu[r]) : 0;       // text rows
       sp_widest = std::max(sp_widest, sp_keep[r]);

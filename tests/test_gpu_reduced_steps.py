@@ -301,3 +301,23 @@ def test_reduced_modes_refuse_what_they_were_not_built_for(B):
             ctx.dit_ctx_set_sparse_attention(keep, least)
         assert e.value.status == 1
     ctx.close()
+
+
+def test_a_share_above_a_whole_number_of_blocks_takes_one_more(B):
+    """ceil(keep * n), where only what rounding keep to fp32 adds (2^-24 of the product) is forgiven: 0.1 of ten blocks is one, the next
+    float above 0.1 takes two, and the next above a half of two blocks takes both, which is the dense step bit for bit."""
+    import torch
+    above = lambda x: float(np.nextafter(np.float32(x), np.float32(1)))
+    wl = W.make_custom("share", W.SMALL, 1, [(256, 256, 0), (512, 320, 640)], seed=61)
+    assert wl.token_lens == [256, 1280]
+    ctx = context(B, wl, B.DIT_FLAG_SPARSE_ATTENTION)
+
+    def step(keep, least=1):
+        ctx.dit_ctx_set_sparse_attention(keep, least)
+        out = run(B, wl, ctx)
+        return out[:256], out[256:]
+    dense, one, two = step(1.0)[0], step(0.05)[1], step(0.15)[1]
+    assert not torch.equal(step(0.5)[0], dense) and torch.equal(step(above(0.5))[0], dense)
+    assert not torch.equal(one, two)
+    assert torch.equal(step(0.1)[1], one) and torch.equal(step(above(0.1))[1], two) and torch.equal(step(0.2)[1], two)
+    ctx.close()
