@@ -321,3 +321,47 @@ def test_a_share_above_a_whole_number_of_blocks_takes_one_more(B):
     assert not torch.equal(one, two)
     assert torch.equal(step(0.1)[1], one) and torch.equal(step(above(0.1))[1], two) and torch.equal(step(0.2)[1], two)
     ctx.close()
+
+
+def test_the_least_number_of_blocks_makes_a_short_request_dense(B):
+    """Requests of three blocks and of one: with three blocks at least the step is the dense one bit for bit, with one at least it is not."""
+    import torch
+    wl = W.make_custom("least", W.SMALL, 2, [(256, 256, 3), (64, 64, 0)], seed=62)
+    ctx = context(B, wl, B.DIT_FLAG_SPARSE_ATTENTION)
+    want = run(B, wl, ctx)
+    ctx.dit_ctx_set_sparse_attention(0.2, 3)
+    assert torch.equal(run(B, wl, ctx), want)
+    ctx.dit_ctx_set_sparse_attention(0.2, 1)
+    assert not torch.equal(run(B, wl, ctx)[:259], want[:259])
+    ctx.close()
+
+
+@pytest.mark.parametrize("sparse", [False, True])
+def test_host_steps_and_graphs_where_the_products_take_the_large_tiles(B, sparse):
+    """4466 rows: the gated products run on 256 x 256 tiles, whose residual and output maps move with the host step's slices of rows; requests
+    begin and end inside the slices and inside the tiles."""
+    import torch
+    flags = B.DIT_FLAG_FP8_BLOCK128 | (B.DIT_FLAG_SPARSE_ATTENTION if sparse else 0)
+    wl = W.make_custom("slices", W.SMALL, 1, [(784, 784, 77), (160, 208, 9), (672, 704, 0), (16, 16, 0)], seed=63)
+    assert wl.total_tokens == 4466
+    wl.weights = [wl.weights[0], W.draw_parallel_block_weights(np.random.default_rng(63), wl.dims)]
+    for weights in (wl.weights, wl.weights[::-1]):                      # the last block, whose product is sliced, in both forms
+        wl.weights = weights
+        ctx = context(B, wl, flags, 0.3 if sparse else None)
+        want = run(B, wl, ctx, with_geometry=False)
+        assert bool(want.isfinite().all())
+        tok, cond = B.bits_to_cuda_bf16(wl.packed_tokens()), B.bits_to_cuda_bf16(wl.cond)
+        graph, replayed = torch.cuda.CUDAGraph(), torch.empty_like(want)
+        with torch.cuda.graph(graph):
+            ctx.dit_step_forward(tok, wl.token_lens, cond, 2, out=replayed)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(replayed, want)
+        del graph
+        host = torch.empty(want.shape, dtype=torch.float32).pin_memory()
+        pin = lambda bits: torch.from_numpy(np.ascontiguousarray(bits).view(np.int16)).view(torch.bfloat16).pin_memory()
+        for _ in range(2):
+            host.fill_(float("nan"))
+            ctx.dit_step_forward_host(pin(wl.packed_tokens()), wl.token_lens, pin(wl.cond), 2, host)
+            assert torch.equal(host, want.cpu())
+        ctx.close()
