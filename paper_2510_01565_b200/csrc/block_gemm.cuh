@@ -412,14 +412,16 @@ gemm_block128_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_
         __syncwarp();
         continue;
       }
-      if (p.bias) {
+      if constexpr (EPI != kBlkGeluF16) {                              // (always vec_out there)
+        if (p.bias) {
 #pragma unroll
-        for (int i = 0; i < 64; i += 2) {
-          const float4 v = finished(i);
-          acc[i] = make_float2(v.x, v.y); acc[i + 1] = make_float2(v.z, v.w);
+          for (int i = 0; i < 64; i += 2) {
+            const float4 v = finished(i);
+            acc[i] = make_float2(v.x, v.y); acc[i + 1] = make_float2(v.z, v.w);
+          }
         }
+        block_store_unaligned<EPI>(p, stage, acc, lane, row0, n0);
       }
-      block_store_unaligned<EPI>(p, stage, acc, lane, row0, n0);
       }
     }
   }

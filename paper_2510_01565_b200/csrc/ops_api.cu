@@ -348,6 +348,9 @@ cudaError_t ops_prepare_device() {
 }
 
 cudaError_t launch_block_product(const BlockProduct& b, const SeqInfo& seq, cudaStream_t st) {
+  const int elem = (b.epilogue == kBlkF32 || b.epilogue == kBlkGateResidF32) ? 4 : 2;
+  const bool vec_out = aligned(b.out, 16) && b.ld_out * elem % 16 == 0;
+  if (b.epilogue == kBlkGeluF16 && !vec_out) return cudaErrorInvalidValue;     // (the step's widths are multiples of 64)
   const DeviceState* d;
   bool unsupported;
   const cudaError_t e = device_state(&d, &unsupported);
@@ -356,8 +359,7 @@ cudaError_t launch_block_product(const BlockProduct& b, const SeqInfo& seq, cuda
   p.M = b.m; p.N = b.n; p.K = b.k;
   p.sa = b.a_scales; p.sb = b.b_scales; p.bias = b.bias; p.out = b.out;
   p.ld_sa = b.ld_a_scales; p.ld_out = b.ld_out;
-  const int elem = (b.epilogue == kBlkF32 || b.epilogue == kBlkGateResidF32) ? 4 : 2;
-  p.vec_out = aligned(b.out, 16) && b.ld_out * elem % 16 == 0;
+  p.vec_out = vec_out;
   p.status = b.status ? b.status : d->status;
   p.row0 = b.row0; p.resid = b.resid; p.gate = b.gate; p.gate_stride = b.gate_stride;
   switch (b.epilogue) {

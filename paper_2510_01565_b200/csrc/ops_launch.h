@@ -20,7 +20,7 @@ struct BlockProduct {
   int m, n, k;
   int plan_m;                // rows by which the kernel is chosen: the whole batch's where a launch covers a slice of its rows, so
                              // that every element is summed in the same order as in one launch
-  int epilogue;              // BlockGemmEpilogue
+  int epilogue;              // BlockGemmEpilogue; kBlkGeluF16 wants rows of out on 16-byte boundaries
   int row0;                  // gated residual only: packed row of row 0, residual, gate vectors
   const float* resid;
   const float* gate;

@@ -164,3 +164,23 @@ def test_a_scale_whose_product_with_log2_e_is_infinite_is_refused(lib):
         setattr(b, name, value)
     for scale in (2.4e38, 3.0e38):
         assert lib.dit_block_attention(C.byref(b), P, P, 1, scale, P, 128, None) == INVALID
+
+
+def test_the_steps_gelu_product_refuses_rows_off_16_byte_boundaries(lib):
+    """The library's own launcher (C++, no entry point reaches it with such an output): before, the kernel for many rows would have stored
+    the values in front of the GELU there.  The refusal comes before the device is looked at, without which this machine has another error
+    to report; the product has no rows, so that nothing could run where there is a device."""
+    class Product(C.Structure):
+        _fields_ = ([(n, C.c_void_p) for n in ("a", "a_scales", "b", "b_scales", "bias", "out")] + [(n, C.c_longlong) for n in ("lda", "ld_a_scales", "ldb", "ld_out")]
+                    + [(n, C.c_int) for n in ("m", "n", "k", "plan_m", "epilogue", "row0")] + [("resid", C.c_void_p), ("gate", C.c_void_p), ("gate_stride", C.c_longlong),
+                                                                                               ("status", C.c_void_p)])
+    launch = lib["_ZN3dit20launch_block_productERKNS_12BlockProductERKNS_7SeqInfoEP11CUstream_st"]
+    launch.restype, launch.argtypes = C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p]
+    seq = C.create_string_buffer(1 << 16)
+    gelu, invalid_value = 3, 1
+
+    def call(out, ld_out):
+        b = Product(P, P, P, P, None, out, 128, 4096, 128, ld_out, 0, 4096, 128, 4096, gelu, 0, None, None, 0, None)
+        return launch(C.byref(b), C.cast(seq, C.c_void_p), None)
+    for out, ld_out in ((P + 2, 4096), (P + 8, 4096), (P, 4097), (P, 4100)):
+        assert call(out, ld_out) == invalid_value
