@@ -537,12 +537,6 @@ struct BlockRowsCfg {
   static_assert(2 * SMEM_BYTES <= 227 * 1024, "two CTAs per SM");
 };
 
-template <bool BF16>
-__device__ __forceinline__ float2 widen2(uint32_t w) {
-  if (BF16) return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
-  return __half22float2(*reinterpret_cast<const __half2*>(&w));
-}
-
 template <int D, bool BF16>
 __global__ void __launch_bounds__(BlockRowsCfg<D>::THREADS, 2)
 block_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const BlockAttnParams p, const uint16_t* q,

@@ -207,7 +207,7 @@ cudaError_t launch_attend(const DeviceState& d, const dit_attention_batch& a, co
   const void* k = kv_rows > 0 ? a.k : a.q;
   const void* v = kv_rows > 0 ? a.v : a.q;
   const uint32_t box = most <= kRowsMax ? kRowsTile : 128;
-  if (!half_map(&tmQ, a.q, width, q_rows, a.ld_q) || !half_map(&tmK, k, width, std::max(kv_rows, 1), kv_rows > 0 ? a.ld_k : a.ld_q, box) ||
+  if (!half_map(&tmK, k, width, std::max(kv_rows, 1), kv_rows > 0 ? a.ld_k : a.ld_q, box) ||
       !half_map(&tmV, v, width, std::max(kv_rows, 1), kv_rows > 0 ? a.ld_v : a.ld_q, box))
     return cudaErrorInvalidValue;
   if (most <= kRowsMax) {
@@ -220,6 +220,7 @@ cudaError_t launch_attend(const DeviceState& d, const dit_attention_batch& a, co
     while (splits < 8 && 2 * splits <= listed && 2ll * splits * items <= 2ll * d.num_sms) splits *= 2;
     return launch_rows<D, BF16>(tmK, tmV, p, a, b, splits, st);
   }
+  if (!half_map(&tmQ, a.q, width, q_rows, a.ld_q)) return cudaErrorInvalidValue;
   BlockAttnParams q = p;
   q.items = qblocks * a.n_heads;
   q.wide_out = aligned(p.out, 32) && p.ld_out % 16 == 0;
@@ -463,7 +464,8 @@ dit_status dit_gemm_block128(const dit_gemm_block128_args* a, void* stream) {
   if (!aligned(a->a, 16) || !aligned(a->b, 16) || !aligned(a->a_scales, 4) || !aligned(a->b_scales, 4) || !aligned(a->bias, 4) ||
       !aligned(a->out, type_bytes(a->out_type)))
     return DIT_ERR_INVALID_ARG;
-  // tiles are counted in 32 bits: with the split kernel's smallest tile, 128 x 128
+  // tiles of 128 x 128 are counted in 32 bits, with room for CTAs per tile; the split kernel's smaller ones (128 columns x 16, 32 or 64
+  // rows) are few by the rule that chooses it
   if (((a->m + 127) / 128) * ((a->n + 127) / 128) > INT32_MAX / 16) return DIT_ERR_SHAPE;
   const DeviceState* d;
   const dit_status s = ready(&d);
@@ -498,13 +500,11 @@ dit_status dit_select_blocks(const dit_attention_batch* a, const int32_t* keep, 
   if (!keep || !block_index || !block_count || !workspace || !aligned(workspace, 16) || !aligned(block_index, 4) || !aligned(block_count, 4))
     return DIT_ERR_INVALID_ARG;
   BlockSelectParams p{};
-  int longest = 1;
   for (int r = 0; r < b.n; ++r) {
     if (keep[r] < 1 || (tail_rows && tail_rows[r] < 0)) return DIT_ERR_INVALID_ARG;
     p.keep[r] = keep[r];
     p.tail[r] = tail_rows ? tail_rows[r] : 0;
     p.widest = std::max(p.widest, keep[r]);
-    longest = std::max(longest, b.first_kblock[r + 1] - b.first_kblock[r]);
   }
   if (ld_index < p.widest) return DIT_ERR_INVALID_ARG;
   if (workspace_bytes < dit_select_blocks_workspace(a)) return DIT_ERR_CAPACITY;

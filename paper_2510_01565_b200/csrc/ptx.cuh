@@ -140,11 +140,6 @@ __device__ __forceinline__ void tma_load_2d(uint32_t dst, const void* tmap, int 
       : "memory");
 }
 
-// The same box into L2 only.
-__device__ __forceinline__ void tma_prefetch_2d(const void* tmap, int x, int y) {
-  asm volatile("cp.async.bulk.prefetch.tensor.2d.L2.global.tile [%0, {%1, %2}];" ::"l"(reinterpret_cast<uint64_t>(tmap)), "r"(x), "r"(y) : "memory");
-}
-
 // 2-D tiled store shared -> global (x, y >= 0; elements outside the tensor are dropped).  The writes to shared memory must
 // have been fenced for the async proxy; the buffer may be reused once bulk_store_read_done has returned in the issuing thread.
 __device__ __forceinline__ void tma_store_2d(const void* tmap, uint32_t src, int x, int y) {
