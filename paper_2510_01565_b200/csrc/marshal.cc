@@ -309,6 +309,7 @@ PyObject* block_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
     check_lists(index, count, t);
     const double scale = PyFloat_AsDouble(a[8]);
     if (scale == -1.0 && PyErr_Occurred()) throw PythonError{};
+    if (scale != 0.0 && static_cast<float>(scale) == 0.f) refuse("scale rounds to zero, which stands for 1 / sqrt(head_dim)");
     const OnStream on(a[10], t.q.device());
     const at::Tensor out = given(a[9]) ? tensor(a[9], "out") : empty({t.q.size(0), t.q.size(1)}, t.q.scalar_type(), t.q);
     if (!shaped(out, t.q.size(0), t.q.size(1)) || out.scalar_type() != t.q.scalar_type()) refuse("out must be shaped and typed like q");

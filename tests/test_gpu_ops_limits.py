@@ -208,3 +208,18 @@ def test_a_selector_asked_for_more_blocks_than_any_request_has(B):
     assert count.tolist() == [[3]] and index[0, 0, :3].tolist() == [0, 1, 2]
     assert bool((buf[:pad] == 7).all()) and bool((buf[pad + keep:] == 7).all())
     assert int(buf[pad + 3:pad + keep].max()) == -1 and int(buf[pad + 3:pad + keep].min()) == -1
+
+
+def test_a_scale_that_fp32_cannot_tell_from_zero_is_refused(B):
+    """Zero stands for 1 / sqrt(head_dim): a tiny or negative number that rounds to it must not be taken for that."""
+    import torch
+    q = torch.randn(10, 128, dtype=torch.float16, device="cuda")
+    index, count = torch.zeros(2, 1, 1, dtype=torch.int32, device="cuda"), torch.ones(2, 1, dtype=torch.int32, device="cuda")
+    call = lambda scale: B.dit_block_attention(q, q, q, [10], [10], 2, index, count, scale=scale)
+    for scale in (1e-46, 5e-324, -1e-46, -1e-300):
+        with pytest.raises(B.DitError) as e:
+            call(scale)
+        assert e.value.status == 1
+    assert torch.equal(call(0.0), call(-0.0)) and torch.equal(call(0.0), call(64 ** -0.5))
+    # the smallest number that fp32 has: every key counts alike
+    assert float((call(1e-45).double() - q.double().mean(0)).abs().max()) <= 2.0 ** -10 * float(q.abs().max())
