@@ -44,7 +44,9 @@ bool given(PyObject* o) { return o != Py_None; }
 
 const at::Tensor& tensor(PyObject* o, const char* what) {
   if (!THPVariable_Check(o)) refuse(std::string(what) + " must be a tensor");
-  return THPVariable_Unpack(o);
+  const at::Tensor& t = THPVariable_Unpack(o);
+  if (t.is_neg()) refuse(std::string(what) + " is a lazily negated view, whose memory holds the other sign (resolve_neg)");
+  return t;
 }
 
 // Row stride in elements of a CUDA matrix whose rows are contiguous (the rows themselves may lie apart).

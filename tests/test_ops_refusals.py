@@ -184,3 +184,14 @@ def test_the_steps_gelu_product_refuses_rows_off_16_byte_boundaries(lib):
         return launch(C.byref(b), C.cast(seq, C.c_void_p), None)
     for out, ld_out in ((P + 2, 4096), (P + 8, 4096), (P, 4097), (P, 4100)):
         assert call(out, ld_out) == invalid_value
+
+
+def test_binding_refuses_lazily_negated_views():
+    """The imaginary part of a conjugate has its sign in a flag of the tensor, not in its memory."""
+    import torch
+    x = torch.randn(40, 1, dtype=torch.complex64).conj().imag
+    assert x.is_neg()
+    for call in (lambda: B.dit_quantize_block128(x), lambda: B.dit_quantize_weight_block128(x), lambda: B.dit_select_blocks(x, x, [40], [40], 1, [1])):
+        with pytest.raises(B.DitError, match="negated") as e:
+            call()
+        assert e.value.status == INVALID
