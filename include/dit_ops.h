@@ -14,8 +14,10 @@
  *     is the distance between the starts of two rows.  Element offsets may exceed 32 bits.
  *   - outputs are written exactly where they are defined: padding columns between a row's last element
  *     and the next row, and rows behind the last one, stay as they were.
- *   - results do not depend on timing: every sum is taken in an order fixed by the shapes, without
- *     atomics.
+ *   - results do not depend on timing: every sum is taken in an order fixed by the shapes of the call, without
+ *     atomics.  Quantised values and selected lists depend on their own group or request alone.  The order of a product's sum over the
+ *     groups depends on m, n and k, and that of attention for a request of up to 16 query rows on the whole batch, whose longest
+ *     request chooses the kernel: such results may differ in their last bits with the rows they are packed with.
  *   - kernels bound their waits; one that gave up leaves its output undefined and sets a status word of
  *     the device, which dit_ops_poll_status reads.
  */
@@ -56,8 +58,9 @@ dit_status dit_quantize_weight_block128(const void *w, dit_type type, int64_t ld
 
 /* Product of two quantised operands, both with k contiguous in a row:
  *   out[m, n] = sum_g a_scales[g, m] * b_scales[n / 128, g] * (sum over the group's k of a[m, k] b[n, k]) + bias[n]
- * Each group's inner sum is a tensor-core sum of exact products in fp32; the scaled sum over the groups is
- * held in fp32 and rounded once into out.  16-bit outputs clamp to the largest finite value.
+ * Each group's inner sum is a tensor-core sum of exact products in fp32; the two scales are multiplied first, in fp32 as well (so
+ * their product has to lie inside fp32's normal range: below it bits are lost, above it a sum of zero gives NaN); the scaled sum over
+ * the groups is held in fp32 and rounded once into out.  16-bit outputs clamp to the largest finite value.
  *   a        device e4m3 codes [m, lda], 16-byte aligned, lda >= k and a multiple of 16; columns k.. are not used
  *   a_scales device fp32 [ceil(k / 128), ld_a_scales], ld_a_scales >= m   (dit_quantize_block128)
  *   b        device e4m3 codes [n, ldb], likewise;  b_scales device fp32 [ceil(n / 128), ceil(k / 128)]
@@ -100,7 +103,7 @@ typedef struct {
  * min(keep[r], key blocks of its request) key blocks with the largest scores; of equal scores the lower block
  * wins; a NaN counts as less than any number.  Key blocks that hold one of the request's last tail_rows[r] rows (its text
  * tokens) come before every score; where there are more of them than keep[r], the lowest of them.  v is not read.
- *   keep, tail_rows  HOST [n_requests], keep >= 1, tail_rows >= 0 or NULL (no tail)
+ *   keep, tail_rows  HOST [n_requests], keep >= 1 (beyond a request's key blocks: all of them), tail_rows >= 0 or NULL (no tail)
  *   block_index      device int32 [n_heads, n_query_blocks, ld_index], ld_index >= the largest keep: the selected key
  *                    blocks in ascending order, then -1 up to the largest keep of the batch
  *   block_count      device int32 [n_heads, n_query_blocks]

@@ -610,7 +610,8 @@ def dit_modulation_noalloc(cond, w_ada, b_ada, mod_out, stream=None):
 # Their small shapes take the GPU a few microseconds, so the marshalling of these is native (csrc/marshal.cc): it checks the
 # tensors, allocates the results that the caller did not bring, makes the tensors' device current and calls the library on
 # `stream` (default: the current stream of that device), to which everything that it allocates belongs.  Refusals are DitError, as
-# everywhere.
+# everywhere.  They have no backward pass, like the rest of the library: inputs that require a gradient are taken as they are, results
+# require none.
 _native = None
 
 

@@ -118,7 +118,7 @@ __device__ __forceinline__ int order_blocks(const uint32_t* bits, uint16_t* list
 // 7 us of 31 (14 blocks per list).  The grid is persistent instead, and all roles run on from item to item: a warp of its own
 // lays out the next lists meanwhile (two buffers), the next item's Q, K and V are requested as soon as the last
 // score product of the current one has been issued, and its first scores are computed under the current item's last softmax.
-// 24 heads of 128, 16896 rows, 14 of 132 blocks: 362-392 us (950-1030 TFLOP/s) under the power cap, 308 us when neighbouring tiles list the
+// 24 heads of 128, 16896 rows, 14 of 132 blocks: 362-397 us (940-1030 TFLOP/s) under the power cap, 308 us when neighbouring tiles list the
 // same blocks and 384 us when they share none; marginal rate 1400 TFLOP/s shared, 1100 not, and about 4 us per item that the
 // hand-over still costs.  (Separate barriers for the two tiles' Q, so that the first scores need only half of it, cost
 // 8 %: the warpgroups then fall out of turn.)
@@ -520,7 +520,8 @@ done:
 // own, with its own running maximum and sum per row: the accumulator layout of the scores is the operand layout of
 // the second product, so probabilities stay in registers.  The warps' results meet in shared memory (the ring's,
 // once everything has been read), the CTAs' through distributed shared memory, in rank and warp order.
-// Four requests of one row, 24 heads of 128, 60 blocks in all (94 MB): 19 us, 4.9 TB/s; longer lists 5.7-6.2 TB/s.
+// Four requests of one row, 24 heads of 128, 60 blocks in all (94 MB): 19 us when they are in L2, 23.6 us (4.0 TB/s) from DRAM; longer
+// lists, beyond L2, 5.7-6.2 TB/s.
 // ------------------------------------------------------------------------------------------------
 constexpr int kRowsTile = 64;                  // keys per tile
 constexpr int kRowsMax = 16;                   // query rows

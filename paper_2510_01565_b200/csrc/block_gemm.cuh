@@ -12,11 +12,13 @@
 // cluster and joined through distributed shared memory in rank order, for few rows, where reading B once is
 // the bound.
 //
-// Measured (pair kernel, m 16896, n 12288, k 3072, fp16 out): 577 us = 2.21 PFLOP/s in short runs, 660-690 us under the power
-// cap.  Trial builds of the same kernel with parts left out: no additions 496 us, no tensor-memory reads 539 us, neither 490 us, a
-// quarter of the MMAs 502 us.  The floor of this tile is therefore its operands' way from L2 (64 KB per group and pair,
-// 10 TB/s over the device), not the MMAs; reads and additions beside it cost the remaining 15 %.  A larger tile
-// would need fewer bytes, but its accumulators would not fit the registers.  Split kernel, m 1, n 18432, k 3072: 11 us, 5.2 TB/s.
+// Measured (pair kernel, m 16896, n 12288, k 3072, fp16 out): 568 us = 2.25 PFLOP/s in a single call, 640-690 us in long runs under
+// the power cap.  Trial builds of the same kernel with parts left out, in short runs of 577 us: no additions 496 us, no tensor-memory
+// reads 539 us, neither 490 us, a quarter of the MMAs 502 us.  So what remains at 490 us is the way of the operands into this
+// kernel's ring (64 KB per group and pair, 10 TB/s over the device), and reads and additions beside it cost 15 %.  It is not a
+// limit of L2: the 16-bit product on the same tile, with six stages, takes in 12.4 TB/s.  Four stages (64 KB stage the outputs) and a
+// stage given back after two commits are the differences; which of them counts has not been measured.
+// Split kernel, m 1, n 18432, k 3072 (57 MB of weights): 10.7 us when they are in L2, 16.1 us (3.5 TB/s) from DRAM.
 #pragma once
 #include "common.cuh"
 #include "gemm.cuh"

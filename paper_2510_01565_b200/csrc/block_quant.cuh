@@ -157,7 +157,8 @@ quantize_block128_kernel(const QuantParams p) {
 // through shared memory as packed quadruples of codes along `in`.  A thread's vectors are four
 // consecutive `in` rows at the same eight columns, so each of its 16 words holds four consecutive
 // codes of one output row; word kq of row n lies at kq ^ 2 (n / 8), which keeps both phases free of
-// bank conflicts.  Bound by HBM: 3 bytes per element.  3072 x 12288 bf16: 23 us, 4.9 TB/s (46 us with the widened values held: half the CTAs).
+// bank conflicts.  HBM is the floor: 3 bytes per element.  3072 x 12288 bf16: 23.6 us, 4.8 TB/s (46 us with the widened values held: half the
+// CTAs); what keeps it from 17.6 us is not known (2304 blocks of 32 KB on 592 resident CTAs: the tail is 3 %).
 struct QuantWeightParams {
   const void* w;
   uint8_t* codes;
