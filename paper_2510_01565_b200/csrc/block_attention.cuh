@@ -520,7 +520,7 @@ done:
 // own, with its own running maximum and sum per row: the accumulator layout of the scores is the operand layout of
 // the second product, so probabilities stay in registers.  The warps' results meet in shared memory (the ring's,
 // once everything has been read), the CTAs' through distributed shared memory, in rank and warp order.
-// Four requests of one row, 24 heads of 128, 60 blocks in all (94 MB): 19 us when they are in L2, 23.6 us (4.0 TB/s) from DRAM; longer
+// Four requests of one row, 24 heads of 128, 60 blocks in all (94 MB): 19 us when they are in L2, 24.8 us (3.8 TB/s) from DRAM; longer
 // lists, beyond L2, 5.7-6.2 TB/s.
 // ------------------------------------------------------------------------------------------------
 constexpr int kRowsTile = 64;                  // keys per tile
