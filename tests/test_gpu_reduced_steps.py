@@ -387,3 +387,18 @@ def test_block_scales_hold_where_a_loud_channel_takes_the_row_scales_bits(B):
     print(off)
     assert abs(off[0.0, B.DIT_FLAG_FP8_GEMM] - off[0.0, B.DIT_FLAG_FP8_BLOCK128]) <= 0.2 * off[0.0, B.DIT_FLAG_FP8_GEMM]
     assert off[3e4, B.DIT_FLAG_FP8_BLOCK128] <= 0.6 * off[3e4, B.DIT_FLAG_FP8_GEMM]
+
+
+def test_a_steps_attention_clamps_what_its_sums_carry_beyond_fp32(B):
+    """A value channel at 3e38: the weighted sum, taken before the division, is infinite.  The operator would write an infinity, a step the largest
+    finite value, like every activation of it (further on an infinity would meet zeros)."""
+    import torch
+    wl = W.make_custom("clamp", W.SMALL, 1, [(384, 384, 77), (64, 64, 0)], seed=65)
+    H = wl.dims.hidden
+    wl.weights[0]["b_qkv"] = wl.weights[0]["b_qkv"].copy()
+    wl.weights[0]["b_qkv"][2 * H + 5] = W.f32_to_bf16_bits(np.float32([3e38]))[0]
+    ctx = context(B, wl, B.DIT_FLAG_SPARSE_ATTENTION | B.DIT_FLAG_BF16_OPERANDS, 0.5)
+    run(B, wl, ctx)
+    attn, rows = ctx.dit_debug_tap("attn"), wl.token_lens[0]
+    ctx.close()
+    assert bool(attn.isfinite().all()) and bool((attn[:rows, 5].float() >= 2.9e38).all())
