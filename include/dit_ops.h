@@ -133,6 +133,93 @@ dit_status dit_select_blocks(const dit_attention_batch *batch, const int32_t *ke
 dit_status dit_block_attention(const dit_attention_batch *batch, const int32_t *block_index, const int32_t *block_count,
                                int64_t ld_index, float scale, void *out, int64_t ld_out, void *stream);
 
+/* ------------------------------------------------------------------------------------------------------------
+ * Microscaled 4-bit floating point.  A matrix [rows, cols] is held as e2m1 codes (0, 1/2, 1, 3/2, 2, 3, 4, 6 and their negatives) with one
+ * scale for each `group` of 16 or 32 consecutive columns of a row (the last group may be short):
+ *   group 32   scale = 2^e, e the smallest integer with top <= 6 * 2^e, top = max(max |x| of the group, 2^-100)
+ *              code = e2m1 nearest to x * 2^-e
+ *   group 16   scale = s * 2^e, e the smallest integer with row_top <= 6 * 448 * 2^e, row_top = max(max |x| of the row, 2^-100)
+ *              s = e4m3 nearest to top * 2^-e / 6, code = e2m1 nearest to (x * 2^-e) / s, 0 where s is 0
+ * (quotients rounded to fp32 first; ties to even; codes beyond 6 clamp).
+ *   codes       device bytes [rows, ld_codes], 16-byte aligned, ld_codes a multiple of 16 and >= (cols + 1) / 2 (bytes): column 2 i in the
+ *               low half of byte i, column 2 i + 1 in the high half; where cols is odd the last high half is 0
+ *   scales      device bytes, 16-byte aligned, dit_fp4_scale_bytes(rows, cols, group): tiles of 128 rows x 4 groups, 512 bytes each,
+ *               [ceil(rows / 128)][ceil(cols / (4 * group))], in them byte (row % 32) * 16 + (row % 128) / 32 * 4 + group % 4:
+ *               the e4m3 number s (group 16; its sign bit is 0) or e + 127 (group 32; 255 is NaN).  The quantisers write whole tiles, zeros
+ *               where there is no row or group; scales that a caller makes need finite values for the groups behind a row's last one
+ *   row_scales  device fp32 [rows]: 2^e (group 16).  NULL (group 32)
+ * A row (group 16) or group (group 32) that holds a NaN or an infinity gets codes 0 and a NaN row scale or scale.
+ * cols, k, rows >= 1 unless stated otherwise, at most 2^31 - 1024 (DIT_ERR_SHAPE); other groups are DIT_ERR_INVALID_ARG. */
+
+/* Bytes of the scales of a [rows, cols] matrix; 0 for sizes or groups that the calls below refuse. */
+size_t dit_fp4_scale_bytes(int64_t rows, int64_t cols, int32_t group);
+
+/* x  device [rows, cols], type f16, bf16 or f32, element-aligned, ld >= cols.  rows == 0 is a no-op. */
+dit_status dit_quantize_fp4(const void *x, dit_type type, int64_t ld, int64_t rows, int64_t cols, int32_t group, void *codes,
+                            int64_t ld_codes, void *scales, float *row_scales, void *stream);
+
+/* The same for a weight w [in, out] (y = x w), transposed: codes [out, ld_codes] with in columns, scales of an [out, in] matrix,
+ * row_scales [out]. */
+dit_status dit_quantize_weight_fp4(const void *w, dit_type type, int64_t ld, int64_t in_dim, int64_t out_dim, int32_t group, void *codes,
+                                   int64_t ld_codes, void *scales, float *row_scales, void *stream);
+
+/* The values code * scale * row_scale (row_scales NULL: 1), the last product rounded to fp32, then to out_type (16-bit outputs
+ * clamp to the largest finite value).
+ *   out  device [rows, ld_out] of out_type, element-aligned, ld_out >= cols.  rows == 0 is a no-op. */
+dit_status dit_dequantize_fp4(const void *codes, int64_t ld_codes, const void *scales, const float *row_scales, int64_t rows, int64_t cols,
+                              int32_t group, void *out, dit_type out_type, int64_t ld_out, void *stream);
+
+/* Product of two such operands of the same group, both with k along a row:
+ *   out[m, n] = a_rows[m] * b_rows[n] * sum_k (a's code * scale)[m, k] * (b's code * scale)[n, k] + bias[n]
+ * The sum is the tensor cores', in fp32; the row scales (each NULL for 1) and the bias follow in fp32; rounded once into out, 16-bit outputs
+ * clamp to the largest finite value.  Products of two scales have to lie inside fp32's range.
+ *   a, a_scales, a_rows   [m, k] as above, lda in bytes;  b, b_scales, b_rows  [n, k] likewise;  bias  device fp32 [n] or NULL
+ *   out  device [m, ld_out] of out_type, element-aligned, ld_out >= n; must not overlap the operands
+ * m == 0 is a no-op. */
+typedef struct {
+  const void *a, *a_scales;
+  const float *a_rows;
+  const void *b, *b_scales;
+  const float *b_rows;
+  const float *bias;
+  void *out;
+  int64_t lda, ldb, ld_out;
+  int64_t m, n, k;
+  int32_t group;
+  dit_type out_type;
+} dit_gemm_fp4_args;
+dit_status dit_gemm_fp4(const dit_gemm_fp4_args *args, void *stream);
+
+/* Rotary positions.  The first rotary_dim channels of each head are turned in pairs, (a, b) -> magnitude * (a cos t - b sin t,
+ * a sin t + b cos t) with t = position * f_i, i < rotary_dim / 2: channels (2 i, 2 i + 1) where `interleaved`, (i, i + rotary_dim / 2)
+ * otherwise; the other channels are copied.  inverse: by -t, which takes a rotation of magnitude 1 back and is the transposed map, i.e. the
+ * gradient of the rotation.
+ *   f_i = base^(-2 i / rotary_dim), for longer contexts than the trained one scaled:
+ *     trained_len == 0:  f_i / factor
+ *     trained_len > 0:   f_i (g + (1 - g) / factor), g = clamp((trained_len * f_i / (2 pi) - low) / (high - low), 0, 1): pairs that turn
+ *                        more than `high` times over the trained context stay, those that turn fewer than `low` times are stretched
+ *   x, out      device [rows, n_heads * head_dim], type f16, bf16 or f32, element-aligned, leading dimensions >= n_heads * head_dim.  out
+ *               may be x itself (with the same leading dimension) and must not overlap it otherwise.  Adjacent columns of a packed
+ *               q | k | v buffer may be turned in one call: n_heads = query heads + key heads
+ *   positions   device int32 [rows], any values, or NULL: request r has lens[r] rows at positions first[r], first[r] + 1, ...
+ *               (HOST arrays; first NULL: 0, otherwise >= 0; positions end before 2^31)
+ * Angles are taken in 64 bits and reduced before they are narrowed: cosine and sine are off by at most 2^-21 up to position 2^24.  Results are
+ * rounded once from fp32; infinities and NaN spread within their pair.  rotary_dim even, 2 .. min(head_dim, 256); head_dim <= 4096;
+ * base > 0, factor >= 1, high > low where trained_len > 0, all finite.  rows == 0 is a no-op. */
+typedef struct {
+  const void *x;
+  void *out;
+  int64_t ld_x, ld_out, rows;
+  dit_type type;
+  int32_t n_heads, head_dim, rotary_dim, interleaved, inverse;
+  double base, factor, trained_len, low, high;
+  float magnitude;
+  const int32_t *positions;
+  int32_t n_requests;
+  const int32_t *lens, *first;
+} dit_rotary_args;
+dit_status dit_rotary(const dit_rotary_args *args, void *stream);
+
 /* Reads and clears (with a synchronisation of the current device) the status word that a kernel of this
  * header sets when a bounded wait ran out: DIT_OK or DIT_ERR_TIMEOUT. */
 dit_status dit_ops_poll_status(void);

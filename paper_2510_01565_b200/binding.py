@@ -70,9 +70,22 @@ class DitAttentionBatch(C.Structure):
                 + [(n, C.c_int32) for n in ("n_heads", "head_dim", "n_requests")] + [("q_lens", C.POINTER(C.c_int32)), ("kv_lens", C.POINTER(C.c_int32))])
 
 
+class DitGemmFp4Args(C.Structure):
+    _fields_ = ([(n, C.c_void_p) for n in ("a", "a_scales", "a_rows", "b", "b_scales", "b_rows", "bias", "out")]
+                + [(n, C.c_int64) for n in ("lda", "ldb", "ld_out", "m", "n", "k")] + [("group", C.c_int32), ("out_type", C.c_int)])
+
+
+class DitRotaryArgs(C.Structure):
+    _fields_ = ([("x", C.c_void_p), ("out", C.c_void_p)] + [(n, C.c_int64) for n in ("ld_x", "ld_out", "rows")] + [("type", C.c_int)]
+                + [(n, C.c_int32) for n in ("n_heads", "head_dim", "rotary_dim", "interleaved", "inverse")]
+                + [(n, C.c_double) for n in ("base", "factor", "trained_len", "low", "high")] + [("magnitude", C.c_float), ("positions", C.c_void_p)]
+                + [("n_requests", C.c_int32), ("lens", C.POINTER(C.c_int32)), ("first", C.POINTER(C.c_int32))])
+
+
 SCHED_EXPORTS = ["dit_sched_allocate", "dit_sched_round"]
 OPS_EXPORTS = ["dit_quantize_block128", "dit_quantize_weight_block128", "dit_gemm_block128", "dit_select_blocks_workspace", "dit_select_blocks",
-               "dit_block_attention", "dit_ops_poll_status"]
+               "dit_block_attention", "dit_fp4_scale_bytes", "dit_quantize_fp4", "dit_quantize_weight_fp4", "dit_dequantize_fp4", "dit_gemm_fp4",
+               "dit_rotary", "dit_ops_poll_status"]
 BLOCK = 128      # columns per scale; rows per query block and per key block
 
 
@@ -187,6 +200,17 @@ def load_library() -> C.CDLL:
     lib.dit_select_blocks.argtypes = [bp, C.POINTER(i32), C.POINTER(i32), vp, vp, i64, vp, C.c_size_t, vp]
     lib.dit_block_attention.restype = C.c_int
     lib.dit_block_attention.argtypes = [bp, vp, vp, i64, C.c_float, vp, i64, vp]
+    lib.dit_fp4_scale_bytes.restype = C.c_size_t
+    lib.dit_fp4_scale_bytes.argtypes = [i64, i64, i32]
+    for name in ("dit_quantize_fp4", "dit_quantize_weight_fp4"):
+        getattr(lib, name).restype = C.c_int
+        getattr(lib, name).argtypes = [vp, C.c_int, i64, i64, i64, i32, vp, i64, vp, vp, vp]
+    lib.dit_dequantize_fp4.restype = C.c_int
+    lib.dit_dequantize_fp4.argtypes = [vp, i64, vp, vp, i64, i64, i32, vp, C.c_int, i64, vp]
+    lib.dit_gemm_fp4.restype = C.c_int
+    lib.dit_gemm_fp4.argtypes = [C.POINTER(DitGemmFp4Args), vp]
+    lib.dit_rotary.restype = C.c_int
+    lib.dit_rotary.argtypes = [C.POINTER(DitRotaryArgs), vp]
     lib.dit_ops_poll_status.restype = C.c_int
     lib.dit_ops_poll_status.argtypes = []
     lib.dit_last_launch_count.restype = i64
@@ -654,6 +678,37 @@ def dit_select_blocks(q, k, q_lens, kv_lens, n_heads: int, keep, tail_rows=None,
 def dit_block_attention(q, k, v, q_lens, kv_lens, n_heads: int, index, count, scale: float = 0.0, out=None, stream=None):
     """Attention of every query block over its listed key blocks -> out, shaped and typed like q."""
     return (_native or _marshal()).block_attention(q, k, v, q_lens, kv_lens, n_heads, index, count, scale, out, stream)
+
+
+def dit_quantize_fp4(x, group: int = 16, codes=None, scales=None, row_scales=None, stream=None):
+    """x [rows, cols] fp16 / bf16 / fp32 -> (codes [rows, ceil(cols / 2)] uint8, two e2m1 codes to a byte,
+    scales [ceil(rows / 128), ceil(cols / (4 group)), 512] uint8 in tiles, row_scales [rows] fp32 for groups of 16, None for 32)."""
+    return (_native or _marshal()).quantize_fp4(x, group, codes, scales, row_scales, stream)
+
+
+def dit_quantize_weight_fp4(w, group: int = 16, codes=None, scales=None, row_scales=None, stream=None):
+    """w [in, out] -> the same for the matrix [out, in]."""
+    return (_native or _marshal()).quantize_weight_fp4(w, group, codes, scales, row_scales, stream)
+
+
+def dit_dequantize_fp4(codes, scales, cols: int, group: int = 16, row_scales=None, out=None, out_dtype=None, stream=None):
+    """The values [rows, cols] that codes and scales stand for, in out_dtype (default: out's, or fp16)."""
+    return (_native or _marshal()).dequantize_fp4(codes, scales, cols, group, row_scales, out, out_dtype, stream)
+
+
+def dit_gemm_fp4(a, a_scales, b, b_scales, k: int, group: int = 16, a_row_scales=None, b_row_scales=None, bias=None, out=None, out_dtype=None,
+                 stream=None):
+    """Two quantised operands [m, k] and [n, k] of the same group -> a b^T [m, n] (+ bias) in out_dtype (default: out's, or fp16)."""
+    return (_native or _marshal()).gemm_fp4(a, a_scales, b, b_scales, k, group, a_row_scales, b_row_scales, bias, out, out_dtype, stream)
+
+
+def dit_rotary(x, n_heads: int, lens=None, first=None, positions=None, rotary_dim=None, interleaved: bool = False, base: float = 10000.0,
+               factor: float = 1.0, ramp=None, magnitude: float = 1.0, inverse: bool = False, out=None, stream=None):
+    """x [rows, n_heads * head_dim] fp16 / bf16 / fp32, rotated by position -> out (x itself: in place).  Positions: request r's lens[r] rows
+    count from first[r] (default 0), or a device int32 tensor `positions` [rows].  rotary_dim: channels of a head that turn (default:
+    all).  factor, ramp = (low, high, trained length): scaling for longer contexts than the trained one.  inverse: the rotation back, which
+    is its gradient."""
+    return (_native or _marshal()).rotary(x, n_heads, lens, first, positions, rotary_dim, interleaved, base, factor, ramp, magnitude, inverse, out, stream)
 
 
 def dit_ops_poll_status():

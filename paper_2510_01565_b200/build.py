@@ -9,9 +9,9 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libdit.so")
 MARSHAL = os.path.join(HERE, "_marshal.so")
-SOURCES = [os.path.join(CSRC, "dit_api.cu"), os.path.join(CSRC, "ops_api.cu"), os.path.join(CSRC, "sched.cc")]
-NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-              "-shared", "-Xcompiler", "-fPIC"]
+SOURCES = [os.path.join(CSRC, name) for name in ("dit_api.cu", "ops_api.cu", "fp4_api.cu", "prompt_api.cu", "sched.cc")]
+OBJECTS = os.path.join(HERE, "_obj")
+NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17", "-Xcompiler", "-fPIC"]
 
 
 def _newest_source_mtime() -> float:
@@ -22,18 +22,37 @@ def _newest_source_mtime() -> float:
     return t
 
 
+def _fresh(obj: str) -> bool:
+    """Whether an object is newer than every file that its dependency list names."""
+    try:
+        named = open(obj + ".d").read().replace("\\\n", " ").split()[1:]
+        return all(os.path.getmtime(p) < os.path.getmtime(obj) for p in named)
+    except OSError:
+        return False
+
+
 def build_library(force: bool = False, verbose: bool = False) -> str:
     """Compiles the library if it is missing or older than its sources; returns its path."""
     newest = _newest_source_mtime()
     if not force and all(os.path.exists(p) and os.path.getmtime(p) >= newest for p in (LIB, MARSHAL)):
         return LIB
     nvcc = os.environ.get("NVCC", "nvcc")
-    cmd = [nvcc] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + ["-o", LIB] + SOURCES
-    res = subprocess.run(cmd, capture_output=True, text=True)
+    os.makedirs(OBJECTS, exist_ok=True)
+    objects = [os.path.join(OBJECTS, os.path.basename(src) + ".o") for src in SOURCES]
+    jobs = []                                      # sources are compiled side by side, those whose object is older than what it was made of
+    for src, obj in zip(SOURCES, objects):
+        if force or not _fresh(obj):
+            cmd = [nvcc] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + ["-MMD", "-MF", obj + ".d", "-c", src, "-o", obj]
+            jobs.append((src, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
+    done = [(src, job.communicate()[0], job.returncode) for src, job in jobs]
     if verbose:
-        print(res.stderr)
+        print("".join(out for _, out, _ in done))
+    for src, out, code in done:
+        if code != 0:
+            raise RuntimeError(f"nvcc failed on {src}:\n{out}")
+    res = subprocess.run([nvcc] + NVCC_FLAGS[:2] + ["-shared", "-o", LIB] + objects, capture_output=True, text=True)
     if res.returncode != 0:
-        raise RuntimeError("nvcc failed:\n" + res.stdout + res.stderr)
+        raise RuntimeError("linking failed:\n" + res.stdout + res.stderr)
     build_marshal()
     return LIB
 

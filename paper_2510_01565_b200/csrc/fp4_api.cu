@@ -1,0 +1,312 @@
+// 4-bit operators of include/dit_ops.h: argument checks, tensor maps, launch rules.
+#include <algorithm>
+#include <mutex>
+
+#include "common.cuh"
+#include "fp4_gemm.cuh"
+#include "fp4_quant.cuh"
+#include "ops_launch.h"
+
+using namespace dit;
+
+namespace {
+
+constexpr int64_t kMaxSize = INT32_MAX - 1024;
+
+int type_bytes(dit_type t) { return t == DIT_TYPE_F32 ? 4 : 2; }
+bool type_ok(dit_type t) { return t == DIT_TYPE_F16 || t == DIT_TYPE_BF16 || t == DIT_TYPE_F32; }
+bool aligned(const void* p, uintptr_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
+
+std::mutex g_mutex;
+struct Prepared { bool ready; int pairs; } g_prepared[kOpsMaxDevices];
+
+template <class Kernel>
+cudaError_t allow_smem(Kernel kernel, int bytes) {
+  return cudaFuncSetAttribute(reinterpret_cast<const void*>(kernel), cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+}
+template <int EPI, int G>
+cudaError_t allow_gemm() {
+  cudaError_t e = allow_smem(&gemm_fp4_pair_kernel<EPI, G>, fgemm::Cfg<G>::SMEM_BYTES);
+  if (e == cudaSuccess) e = allow_smem(&gemm_fp4_split_kernel<EPI, G, 16>, Fp4SplitCfg<16, G>::SMEM_BYTES);
+  if (e == cudaSuccess) e = allow_smem(&gemm_fp4_split_kernel<EPI, G, 32>, Fp4SplitCfg<32, G>::SMEM_BYTES);
+  if (e == cudaSuccess) e = allow_smem(&gemm_fp4_split_kernel<EPI, G, 64>, Fp4SplitCfg<64, G>::SMEM_BYTES);
+  return e;
+}
+
+// The device's state for products; *pairs: CTA pairs of the pair kernel that are resident at once.
+cudaError_t prepare(const OpsDevice& d, int* pairs) {
+  std::lock_guard<std::mutex> lock(g_mutex);
+  Prepared& s = g_prepared[d.index];
+  if (!s.ready) {
+    cudaError_t e;
+    if ((e = allow_gemm<kBlkF16, 16>()) != cudaSuccess || (e = allow_gemm<kBlkBF16, 16>()) != cudaSuccess || (e = allow_gemm<kBlkF32, 16>()) != cudaSuccess ||
+        (e = allow_gemm<kBlkF16, 32>()) != cudaSuccess || (e = allow_gemm<kBlkBF16, 32>()) != cudaSuccess || (e = allow_gemm<kBlkF32, 32>()) != cudaSuccess)
+      return e;
+    cudaLaunchConfig_t lc = {};
+    lc.gridDim = dim3(d.num_sms & ~1); lc.blockDim = dim3(fgemm::THREADS); lc.dynamicSmemBytes = fgemm::Cfg<16>::SMEM_BYTES;
+    cudaLaunchAttribute at;
+    at.id = cudaLaunchAttributeClusterDimension;
+    at.val.clusterDim.x = 2; at.val.clusterDim.y = 1; at.val.clusterDim.z = 1;
+    lc.attrs = &at; lc.numAttrs = 1;
+    int clusters = 0;
+    if ((e = cudaOccupancyMaxActiveClusters(&clusters, reinterpret_cast<const void*>(&gemm_fp4_pair_kernel<kBlkF16, 16>), &lc)) != cudaSuccess) return e;
+    s.pairs = std::max(1, std::min(clusters, d.num_sms / 2));
+    s.ready = true;
+  }
+  *pairs = s.pairs;
+  return cudaSuccess;
+}
+
+// Codes [rows, bytes]: boxes of 128 bytes x box_rows, 128-byte swizzle, zeros outside.
+bool code_map(const OpsDevice& d, CUtensorMap* m, const void* ptr, uint64_t bytes, uint64_t rows, uint64_t pitch, uint32_t box_rows) {
+  const cuuint64_t dims[2] = {bytes, rows};
+  const cuuint64_t strides[1] = {pitch};
+  const cuuint32_t box[2] = {128, box_rows};
+  const cuuint32_t estr[2] = {1, 1};
+  return d.encode(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+// Scale tiles [row tiles][chunks] of 512 bytes (128 words): boxes of box_chunks x box_tiles.
+bool scale_map(const OpsDevice& d, CUtensorMap* m, const void* ptr, uint64_t tiles, uint64_t chunks, uint32_t box_chunks, uint32_t box_tiles) {
+  const cuuint64_t dims[3] = {128, chunks, tiles};
+  const cuuint64_t strides[2] = {512, 512 * chunks};
+  const cuuint32_t box[3] = {128, box_chunks, box_tiles};
+  const cuuint32_t estr[3] = {1, 1, 1};
+  return d.encode(m, CU_TENSOR_MAP_DATA_TYPE_UINT32, 3, const_cast<void*>(ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+// Output matrix: boxes of 128 bytes x 32 rows, 128-byte swizzle.
+bool out_map(const OpsDevice& d, CUtensorMap* m, void* ptr, dit_type type, uint64_t n, uint64_t rows, uint64_t ld) {
+  const bool wide = type == DIT_TYPE_F32;
+  const cuuint64_t dims[2] = {n, rows};
+  const cuuint64_t strides[1] = {ld * (wide ? 4 : 2)};
+  const cuuint32_t box[2] = {wide ? 32u : 64u, 32u};
+  const cuuint32_t estr[2] = {1, 1};
+  const CUtensorMapDataType t = wide ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : (type == DIT_TYPE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16);
+  return d.encode(m, t, 2, ptr, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                  CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int EPI, int G, int BT>
+cudaError_t launch_split(const CUtensorMap& tmA, const CUtensorMap& tmB, const dit_gemm_fp4_args& a, const Fp4GemmParams& p, int splits, cudaStream_t st) {
+  using C = Fp4SplitCfg<BT, G>;
+  const long long tiles = static_cast<long long>((p.N + 127) / 128) * ((p.M + BT - 1) / BT);
+  cudaLaunchConfig_t lc = {};
+  lc.gridDim = dim3(static_cast<unsigned>(tiles * splits)); lc.blockDim = dim3(C::THREADS);
+  lc.dynamicSmemBytes = C::SMEM_BYTES; lc.stream = st;
+  cudaLaunchAttribute at;
+  at.id = cudaLaunchAttributeClusterDimension;
+  at.val.clusterDim.x = splits; at.val.clusterDim.y = 1; at.val.clusterDim.z = 1;
+  lc.attrs = &at; lc.numAttrs = splits > 1 ? 1 : 0;
+  return cudaLaunchKernelEx(&lc, &gemm_fp4_split_kernel<EPI, G, BT>, tmA, tmB, static_cast<const uint8_t*>(a.a_scales), static_cast<const uint8_t*>(a.b_scales), p, splits);
+}
+
+template <int EPI, int G>
+cudaError_t launch_product(const OpsDevice& d, int pairs, const dit_gemm_fp4_args& a, Fp4GemmParams p, cudaStream_t st) {
+  using S = Fp4Scales<G>;
+  CUtensorMap tmA, tmB, tmSA, tmSB;
+  const uint64_t bytes = (static_cast<uint64_t>(p.K) + 1) / 2;
+  const long long tiles_n = (p.N + 127) / 128;
+  const int stages = (p.K + 255) / 256;
+  const long long pair_tiles = static_cast<long long>((p.M + 255) / 256) * ((p.N + 255) / 256);
+  // Few rows, or so few tiles of 128 x 64 that most of the pair kernel's would be missing: the split kernel.
+  if (p.M <= 32 || 3 * tiles_n * ((p.M + 63) / 64) <= 2ll * d.num_sms) {
+    const int bt = p.M <= 16 ? 16 : (p.M <= 32 ? 32 : 64);
+    const long long tiles = tiles_n * ((p.M + bt - 1) / bt);
+    // CTAs per tile: doubled up to about two per SM as long as each keeps a stage or more
+    int splits = 1;
+    while (splits < 8 && tiles * 2 * splits <= 2ll * d.num_sms && stages / (2 * splits) >= 1) splits *= 2;
+    if (!code_map(d, &tmA, a.a, bytes, p.M, a.lda, bt) || !code_map(d, &tmB, a.b, bytes, p.N, a.ldb, 128)) return cudaErrorInvalidValue;
+    if (bt == 16) return launch_split<EPI, G, 16>(tmA, tmB, a, p, splits, st);
+    if (bt == 32) return launch_split<EPI, G, 32>(tmA, tmB, a, p, splits, st);
+    return launch_split<EPI, G, 64>(tmA, tmB, a, p, splits, st);
+  }
+  const uint64_t chunks = (static_cast<uint64_t>(p.K) + 4 * G - 1) / (4 * G);
+  if (!code_map(d, &tmA, a.a, bytes, p.M, a.lda, 128) || !code_map(d, &tmB, a.b, bytes, p.N, a.ldb, 128) ||
+      !scale_map(d, &tmSA, a.a_scales, (p.M + 127) / 128, chunks, S::TILES, 1) || !scale_map(d, &tmSB, a.b_scales, (p.N + 127) / 128, chunks, S::TILES, 2))
+    return cudaErrorInvalidValue;
+  {  // tile order: hold the panels of whichever operand costs fewer DRAM reads in L2 (as launch_gemm of the step does)
+    const long long panel = 128ll * p.K, num_m = (p.M + 255) / 256, num_n = (p.N + 255) / 256;
+    const long long fit = std::max(1ll, (38ll << 20) / panel);
+    const long long rb = std::min(fit, num_m), cb = std::min(fit, num_n);
+    const long long cost_rows = num_m * panel + num_n * panel * ((num_m + rb - 1) / rb);
+    const long long cost_cols = num_n * panel + num_m * panel * ((num_n + cb - 1) / cb);
+    p.band = cost_cols < cost_rows ? -static_cast<int>(cb) : static_cast<int>(rb);
+  }
+  CUtensorMap tmOut = tmA;                       // unused where the output is written directly
+  if (p.vec_out && !out_map(d, &tmOut, a.out, a.out_type, p.N, p.M, a.ld_out)) return cudaErrorInvalidValue;
+  const int grid = 2 * static_cast<int>(std::min<long long>(pair_tiles, pairs));
+  gemm_fp4_pair_kernel<EPI, G><<<grid, fgemm::THREADS, fgemm::Cfg<G>::SMEM_BYTES, st>>>(tmA, tmB, tmSA, tmSB, tmOut, p);
+  return cudaGetLastError();
+}
+
+template <int G>
+cudaError_t dispatch_product(const OpsDevice& d, int pairs, const dit_gemm_fp4_args& a, const Fp4GemmParams& p, cudaStream_t st) {
+  if (a.out_type == DIT_TYPE_F16) return launch_product<kBlkF16, G>(d, pairs, a, p, st);
+  if (a.out_type == DIT_TYPE_BF16) return launch_product<kBlkBF16, G>(d, pairs, a, p, st);
+  return launch_product<kBlkF32, G>(d, pairs, a, p, st);
+}
+
+template <int kType, int G, bool kVec, int THREADS>
+cudaError_t launch_rows(const Fp4QuantParams& p, int loads, cudaStream_t st) {
+  constexpr int CTA = THREADS < 256 ? 256 : THREADS, PER = CTA / THREADS;
+  const unsigned grid = (static_cast<unsigned>((static_cast<long long>(p.rows) + 127) / 128 * 128) + PER - 1) / PER;
+  if (loads <= 1) quantize_fp4_kernel<kType, G, kVec, THREADS, 1><<<grid, CTA, 0, st>>>(p);
+  else if (loads <= 2) quantize_fp4_kernel<kType, G, kVec, THREADS, 2><<<grid, CTA, 0, st>>>(p);
+  else if (loads <= 4) quantize_fp4_kernel<kType, G, kVec, THREADS, 4><<<grid, CTA, 0, st>>>(p);
+  else quantize_fp4_kernel<kType, G, kVec, THREADS, 8><<<grid, CTA, 0, st>>>(p);
+  return cudaGetLastError();
+}
+template <int kType, int G, bool kVec>
+cudaError_t launch_quant(const Fp4QuantParams& p, cudaStream_t st) {
+  // a warp per row up to 128 loads of 16 bytes, beyond that a CTA
+  constexpr int EPL = QuantIn<kType>::EPL;
+  const long long loads = (static_cast<long long>(p.cols) + EPL - 1) / EPL;
+  if (loads <= 32 * 4) return launch_rows<kType, G, kVec, 32>(p, static_cast<int>((loads + 31) / 32), st);
+  return launch_rows<kType, G, kVec, 256>(p, static_cast<int>(std::min<long long>(8, (loads + 255) / 256)), st);
+}
+template <int kType>
+cudaError_t launch_quant(const Fp4QuantParams& p, int group, bool vec, cudaStream_t st) {
+  if (group == 16) return vec ? launch_quant<kType, 16, true>(p, st) : launch_quant<kType, 16, false>(p, st);
+  return vec ? launch_quant<kType, 32, true>(p, st) : launch_quant<kType, 32, false>(p, st);
+}
+
+template <int kType, bool kVec>
+cudaError_t launch_weight(const Fp4QuantWeightParams& p, int group, cudaStream_t st) {
+  const unsigned k_tiles = static_cast<unsigned>((static_cast<long long>(p.in_dim) + 127) / 128);
+  const unsigned grid = static_cast<unsigned>((static_cast<long long>(p.out_dim) + 127) / 128 * 2) * k_tiles;
+  if (group == 16) {
+    cudaError_t e = cudaMemsetAsync(p.row_scales, 0, static_cast<size_t>(p.out_dim) * sizeof(float), st);
+    if (e != cudaSuccess) return e;
+    const unsigned columns = static_cast<unsigned>((static_cast<long long>(p.out_dim) + 63) / 64) * static_cast<unsigned>((static_cast<long long>(p.in_dim) + kColumnRows - 1) / kColumnRows);
+    fp4_column_scales_kernel<kType, kVec><<<columns, 256, 0, st>>>(p);
+    if ((e = cudaGetLastError()) != cudaSuccess) return e;
+    quantize_weight_fp4_kernel<kType, 16, kVec><<<grid, 256, 0, st>>>(p);
+  } else {
+    quantize_weight_fp4_kernel<kType, 32, kVec><<<grid, 256, 0, st>>>(p);
+  }
+  return cudaGetLastError();
+}
+
+template <int kType, int G>
+cudaError_t launch_values(const Fp4ValuesParams& p, bool vec, cudaStream_t st) {
+  const unsigned grid = static_cast<unsigned>((static_cast<long long>(p.rows) + 127) / 128 * ((static_cast<long long>(p.cols) + 127) / 128));
+  if (vec) dequantize_fp4_kernel<kType, G, true><<<grid, 256, 0, st>>>(p);
+  else dequantize_fp4_kernel<kType, G, false><<<grid, 256, 0, st>>>(p);
+  return cudaGetLastError();
+}
+
+dit_status status_of(cudaError_t e) { return e == cudaSuccess ? DIT_OK : DIT_ERR_CUDA; }
+
+// Sizes of a quantised matrix.
+dit_status check_matrix(int64_t rows, int64_t cols, int32_t group) {
+  if (group != 16 && group != 32) return DIT_ERR_INVALID_ARG;
+  if (rows < 0) return DIT_ERR_INVALID_ARG;
+  if (cols < 1 || cols > kMaxSize || rows > kMaxSize) return DIT_ERR_SHAPE;
+  // tiles of 128 x 128 (64 x 128 of a weight) are counted in 32 bits
+  if (((rows + 127) / 128) * ((cols + 127) / 128) > INT32_MAX / 16) return DIT_ERR_SHAPE;
+  return DIT_OK;
+}
+bool codes_ok(const void* codes, int64_t ld, int64_t cols) { return codes && aligned(codes, 16) && ld % 16 == 0 && ld >= (cols + 1) / 2; }
+int chunks_of(int64_t cols, int32_t group) { return static_cast<int>((cols + 4 * group - 1) / (4 * group)); }
+
+}  // namespace
+
+// =============================================================================================== C ABI
+extern "C" {
+
+size_t dit_fp4_scale_bytes(int64_t rows, int64_t cols, int32_t group) {
+  if (check_matrix(rows, cols, group) != DIT_OK) return 0;
+  return static_cast<size_t>((rows + 127) / 128) * chunks_of(cols, group) * 512;
+}
+
+dit_status dit_quantize_fp4(const void* x, dit_type type, int64_t ld, int64_t rows, int64_t cols, int32_t group, void* codes, int64_t ld_codes,
+                            void* scales, float* row_scales, void* stream) {
+  if (!type_ok(type)) return DIT_ERR_INVALID_ARG;
+  const dit_status bad = check_matrix(rows, cols, group);
+  if (bad != DIT_OK) return bad;
+  if (rows == 0) return DIT_OK;
+  if (!x || !codes_ok(codes, ld_codes, cols) || !scales || !aligned(scales, 16) || (group == 16) != (row_scales != nullptr) || !aligned(row_scales, 4) ||
+      ld < cols || !aligned(x, type_bytes(type)))
+    return DIT_ERR_INVALID_ARG;
+  OpsDevice d;
+  const dit_status s = ops_device(&d);
+  if (s != DIT_OK) return s;
+  Fp4QuantParams p{};
+  p.x = x; p.codes = static_cast<uint8_t*>(codes); p.scales = static_cast<uint8_t*>(scales); p.row_scales = row_scales;
+  p.ld = ld; p.ld_codes = ld_codes; p.rows = static_cast<int>(rows); p.cols = static_cast<int>(cols); p.chunks = chunks_of(cols, group);
+  const bool vec = aligned(x, 16) && ld * type_bytes(type) % 16 == 0;
+  const cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (type == DIT_TYPE_F16) return status_of(launch_quant<0>(p, group, vec, st));
+  if (type == DIT_TYPE_BF16) return status_of(launch_quant<1>(p, group, vec, st));
+  return status_of(launch_quant<2>(p, group, vec, st));
+}
+
+dit_status dit_quantize_weight_fp4(const void* w, dit_type type, int64_t ld, int64_t in_dim, int64_t out_dim, int32_t group, void* codes,
+                                   int64_t ld_codes, void* scales, float* row_scales, void* stream) {
+  if (!type_ok(type)) return DIT_ERR_INVALID_ARG;
+  if (out_dim < 1) return DIT_ERR_SHAPE;
+  const dit_status bad = check_matrix(out_dim, in_dim, group);
+  if (bad != DIT_OK) return bad;
+  if (!w || !codes_ok(codes, ld_codes, in_dim) || !scales || !aligned(scales, 16) || (group == 16) != (row_scales != nullptr) || !aligned(row_scales, 4) ||
+      ld < out_dim || !aligned(w, type_bytes(type)))
+    return DIT_ERR_INVALID_ARG;
+  OpsDevice d;
+  const dit_status s = ops_device(&d);
+  if (s != DIT_OK) return s;
+  Fp4QuantWeightParams p{};
+  p.w = w; p.codes = static_cast<uint8_t*>(codes); p.scales = static_cast<uint8_t*>(scales); p.row_scales = row_scales;
+  p.ld = ld; p.ld_codes = ld_codes; p.in_dim = static_cast<int>(in_dim); p.out_dim = static_cast<int>(out_dim); p.chunks = chunks_of(in_dim, group);
+  const bool vec = aligned(w, 16) && ld * type_bytes(type) % 16 == 0;
+  const cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (type == DIT_TYPE_F16) return status_of(vec ? launch_weight<0, true>(p, group, st) : launch_weight<0, false>(p, group, st));
+  if (type == DIT_TYPE_BF16) return status_of(vec ? launch_weight<1, true>(p, group, st) : launch_weight<1, false>(p, group, st));
+  return status_of(vec ? launch_weight<2, true>(p, group, st) : launch_weight<2, false>(p, group, st));
+}
+
+dit_status dit_dequantize_fp4(const void* codes, int64_t ld_codes, const void* scales, const float* row_scales, int64_t rows, int64_t cols,
+                              int32_t group, void* out, dit_type out_type, int64_t ld_out, void* stream) {
+  if (!type_ok(out_type)) return DIT_ERR_INVALID_ARG;
+  const dit_status bad = check_matrix(rows, cols, group);
+  if (bad != DIT_OK) return bad;
+  if (rows == 0) return DIT_OK;
+  if (!codes_ok(codes, ld_codes, cols) || !scales || !aligned(scales, 16) || !aligned(row_scales, 4) || !out || ld_out < cols || !aligned(out, type_bytes(out_type)))
+    return DIT_ERR_INVALID_ARG;
+  OpsDevice d;
+  const dit_status s = ops_device(&d);
+  if (s != DIT_OK) return s;
+  Fp4ValuesParams p{};
+  p.codes = static_cast<const uint8_t*>(codes); p.scales = static_cast<const uint8_t*>(scales); p.row_scales = row_scales; p.out = out;
+  p.ld_codes = ld_codes; p.ld_out = ld_out; p.rows = static_cast<int>(rows); p.cols = static_cast<int>(cols); p.chunks = chunks_of(cols, group);
+  const bool vec = aligned(out, 16) && ld_out * type_bytes(out_type) % 16 == 0;
+  const cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (out_type == DIT_TYPE_F16) return status_of(group == 16 ? launch_values<0, 16>(p, vec, st) : launch_values<0, 32>(p, vec, st));
+  if (out_type == DIT_TYPE_BF16) return status_of(group == 16 ? launch_values<1, 16>(p, vec, st) : launch_values<1, 32>(p, vec, st));
+  return status_of(group == 16 ? launch_values<2, 16>(p, vec, st) : launch_values<2, 32>(p, vec, st));
+}
+
+dit_status dit_gemm_fp4(const dit_gemm_fp4_args* a, void* stream) {
+  if (!a || !type_ok(a->out_type)) return DIT_ERR_INVALID_ARG;
+  dit_status s = check_matrix(a->m, a->k, a->group);
+  if (s != DIT_OK) return s;
+  if (a->n < 1) return DIT_ERR_SHAPE;
+  if ((s = check_matrix(a->n, a->k, a->group)) != DIT_OK || (s = check_matrix(a->m, a->n, a->group)) != DIT_OK) return s;
+  if (a->m == 0) return DIT_OK;
+  if (!codes_ok(a->a, a->lda, a->k) || !codes_ok(a->b, a->ldb, a->k) || !a->a_scales || !aligned(a->a_scales, 16) || !a->b_scales || !aligned(a->b_scales, 16) ||
+      !aligned(a->a_rows, 4) || !aligned(a->b_rows, 4) || !aligned(a->bias, 4) || !a->out || a->ld_out < a->n || !aligned(a->out, type_bytes(a->out_type)))
+    return DIT_ERR_INVALID_ARG;
+  OpsDevice d;
+  s = ops_device(&d);
+  if (s != DIT_OK) return s;
+  int pairs = 0;
+  if (prepare(d, &pairs) != cudaSuccess) return DIT_ERR_CUDA;
+  Fp4GemmParams p{};
+  p.M = static_cast<int>(a->m); p.N = static_cast<int>(a->n); p.K = static_cast<int>(a->k);
+  p.ra = a->a_rows; p.rb = a->b_rows; p.bias = a->bias; p.out = a->out; p.ld_out = a->ld_out;
+  p.vec_out = aligned(a->out, 16) && a->ld_out * type_bytes(a->out_type) % 16 == 0;
+  p.status = d.status;
+  const cudaStream_t st = static_cast<cudaStream_t>(stream);
+  return status_of(a->group == 16 ? dispatch_product<16>(d, pairs, *a, p, st) : dispatch_product<32>(d, pairs, *a, p, st));
+}
+
+}  // extern "C"

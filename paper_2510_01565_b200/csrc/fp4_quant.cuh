@@ -1,0 +1,446 @@
+// Microscaled 4-bit floating point: e2m1 codes (0, 1/2, 1, 3/2, 2, 3, 4, 6 and their negatives), two to a byte, the even column
+// in the low half, under one of two scales (`kGroup` columns of a row share one):
+//   32   scale = 2^e, e the smallest integer with top <= 6 * 2^e           (byte e + 127), code = e2m1(x * 2^-e)
+//   16   scale = s * 2^e, e the smallest integer with row top <= 6 * 448 * 2^e (one fp32 2^e per row),
+//        s = e4m3(top * 2^-e / 6), code = e2m1((x * 2^-e) / s), zero where s is zero
+// with top = max(max|x|, 2^-100) of the group or row.  The row's factor is a power of two, so every product above is exact and each
+// decision rests on one division: a quotient of 16-bit inputs that lies on a border between two codes is then the same in
+// 32 bits as in any wider arithmetic, and codes can be tested bit for bit.
+//
+// Scale bytes lie in the order in which the tensor cores take them: tiles of 128 rows x 4 groups, 512 bytes,
+//   byte (row % 32) * 16 + (row % 128) / 32 * 4 + group % 4   of tile [row / 128][group / 4]
+// Whole tiles are written, zeros where no row or group is.
+#pragma once
+#include "block_quant.cuh"
+#include "common.cuh"
+#include "ptx.cuh"
+
+namespace dit {
+
+// Eight values -> eight codes, nearest with ties to the even code, |x| > 6 clamped.
+__device__ __forceinline__ uint32_t e2m1x8(const float (&v)[8]) {
+  uint32_t r;
+  asm("{\n\t.reg .b8 a, b, c, d;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\tcvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n\tcvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n\t"
+      "mov.b32 %0, {a, b, c, d};\n\t}\n"
+      : "=r"(r) : "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]));
+  return r;
+}
+__device__ __forceinline__ uint32_t e2m1x4(float v0, float v1, float v2, float v3) {
+  uint32_t r;
+  asm("{\n\t.reg .b8 a, b;\n\t.reg .b16 h;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\tcvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n\t"
+      "mov.b16 h, {a, b};\n\tcvt.u32.u16 %0, h;\n\t}\n"
+      : "=r"(r) : "f"(v0), "f"(v1), "f"(v2), "f"(v3));
+  return r;
+}
+// Eight codes -> eight values.
+__device__ __forceinline__ void e2m1_values(uint32_t codes, float (&v)[8]) {
+  uint32_t h[4];
+  asm("{\n\t.reg .b8 a, b, c, d;\n\tmov.b32 {a, b, c, d}, %4;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %0, a;\n\tcvt.rn.f16x2.e2m1x2 %1, b;\n\tcvt.rn.f16x2.e2m1x2 %2, c;\n\tcvt.rn.f16x2.e2m1x2 %3, d;\n\t}\n"
+      : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3]) : "r"(codes));
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h[i]));
+    v[2 * i] = f.x; v[2 * i + 1] = f.y;
+  }
+}
+
+__device__ __forceinline__ float pow2(int e) { return __uint_as_float(static_cast<uint32_t>(e + 127) << 23); }   // -126 <= e <= 127
+
+// Smallest e with top <= limit * 2^e, where limit = (1 + kMantissa / 2^23) * 2^kExponent; top is finite and >= 2^-100.
+template <uint32_t kMantissa, int kExponent>
+__device__ __forceinline__ int scale_exponent(float top) {
+  const uint32_t u = __float_as_uint(top);
+  return static_cast<int>(u >> 23) - 127 - kExponent + ((u & 0x7FFFFFu) > kMantissa ? 1 : 0);
+}
+__device__ __forceinline__ int group_exponent(float top) { return scale_exponent<0x400000u, 2>(top); }        // 6 = 1.5 * 4
+__device__ __forceinline__ int row_exponent(float top) { return scale_exponent<0x280000u, 11>(top); }         // 2688 = 1.3125 * 2048
+
+// Values of scale bytes.
+__device__ __forceinline__ float e8m0_value(uint32_t b) { return b == 0 ? __uint_as_float(0x00400000u) : (b == 255 ? __uint_as_float(0x7FC00000u) : __uint_as_float(b << 23)); }
+__device__ __forceinline__ float e4m3_value(uint32_t b) { return __half2float(__half(__nv_cvt_fp8_to_halfraw(static_cast<__nv_fp8_storage_t>(b), __NV_E4M3))); }
+
+// What a lane needs to code values of its group.
+struct GroupScale {
+  uint32_t byte;
+  float up;                  // 2^-e
+  float s, inv;              // e4m3 value and its reciprocal; inv 0: every code is zero
+};
+// e: the row's exponent (groups of 16); bad: the row (16) or group (32) holds a NaN or an infinity
+template <int kGroup>
+__device__ __forceinline__ GroupScale group_scale(float top, int e, bool bad) {
+  GroupScale g;
+  if constexpr (kGroup == 32) {
+    const int ge = group_exponent(fmaxf(top, kQuantFloor));
+    g.byte = bad ? 255u : static_cast<uint32_t>(ge + 127);
+    g.up = bad ? 0.f : pow2(-ge);
+    g.s = 1.f; g.inv = bad ? 0.f : 1.f;
+  } else {
+    g.up = bad ? 0.f : pow2(-e);
+    g.byte = bad ? 0u : __nv_cvt_float_to_fp8(__fdiv_rn(top * g.up, 6.0f), __NV_SATFINITE, __NV_E4M3);
+    g.s = e4m3_value(g.byte);
+    g.inv = g.s > 0.f ? __frcp_rn(g.s) : 0.f;
+  }
+  return g;
+}
+
+// Two quotients x / s.  16-bit inputs multiply by the reciprocal: the product is off by less than 2^-22, and since a true
+// quotient is either on a border of two codes or at least 2^-11 away from it (x has at most 11 bits, s four, borders three),
+// rounding the product to 18 bits puts it back on the border exactly where the quotient is.  (y + 64 y) - 64 y is that rounding.
+__device__ __forceinline__ float2 quotients(float2 x, const GroupScale& g) {
+  const float f = g.up * g.inv;
+  const float2 y = fmul2(x, make_float2(f, f));
+  const float2 high = fmul2(y, make_float2(65.f, 65.f));
+  return fadd2(high, ffma2(high, make_float2(-1.f, -1.f), y));
+}
+
+// Codes of the EPL values of a 16-byte load (8 codes for 16-bit inputs, 4 for fp32).
+template <int kType, int kGroup, int EPL>
+__device__ __forceinline__ uint32_t encode(const float (&v)[EPL], const GroupScale& g) {
+  float q[EPL];
+  if constexpr (kGroup == 32) {
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) q[i] = g.inv == 0.f ? 0.f : v[i] * g.up;
+  } else if constexpr (kType == 2) {
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) q[i] = g.inv == 0.f ? 0.f : __fdiv_rn(v[i] * g.up, g.s);
+  } else {
+#pragma unroll
+    for (int i = 0; i < EPL; i += 2) {
+      const float2 r = quotients(make_float2(v[i], v[i + 1]), g);
+      q[i] = g.inv == 0.f ? 0.f : r.x; q[i + 1] = g.inv == 0.f ? 0.f : r.y;
+    }
+  }
+  if constexpr (EPL == 8) return e2m1x8(q);
+  else return e2m1x4(q[0], q[1], q[2], q[3]);
+}
+
+struct Fp4QuantParams {
+  const void* x;             // [rows, cols], row stride ld
+  uint8_t* codes;
+  uint8_t* scales;
+  float* row_scales;         // groups of 16 only
+  long long ld, ld_codes;    // ld_codes in bytes
+  int rows, cols, chunks;    // chunks: scale tiles of a row
+};
+
+__device__ __forceinline__ long long scale_at(int row, int group, int chunks) {
+  return (static_cast<long long>(row >> 7) * chunks + (group >> 2)) * 512 + (row & 31) * 16 + ((row & 127) >> 5) * 4 + (group & 3);
+}
+
+// A row per THREADS lanes (a warp, or a whole CTA), a 16-byte load of consecutive columns per lane: EPL values, kGroup / EPL lanes
+// to a group.  A row of up to THREADS * kLoads loads stays in registers between its maximum and its codes; a longer one
+// is read twice.  Rows behind the last one up to the tile's end get their zero scales only.  Bound by HBM.
+// kVec: rows start on 16-byte boundaries; otherwise elements are loaded one by one.
+template <int kType, int kGroup, bool kVec, int THREADS, int kLoads>
+__global__ void __launch_bounds__(THREADS < 256 ? 256 : THREADS)
+quantize_fp4_kernel(const Fp4QuantParams p) {
+  using In = QuantIn<kType>;
+  constexpr int EPL = In::EPL, LPG = kGroup / EPL;                // lanes per group
+  constexpr int CTA = THREADS < 256 ? 256 : THREADS;
+  __shared__ uint32_t warp_top[CTA / 32];
+  const int at = threadIdx.x % THREADS;                           // lane of the row
+  const long long row_l = static_cast<long long>(blockIdx.x) * (CTA / THREADS) + threadIdx.x / THREADS;
+  const int padded = (p.rows + 127) / 128 * 128;
+  if (row_l >= padded) return;                                    // (a whole warp; with a row per CTA none)
+  const int row = static_cast<int>(row_l);
+  const bool there = row < p.rows;
+  const int span = THREADS * EPL * kLoads;                        // columns held at a time
+  const int wide = p.chunks * 4 * kGroup;                         // columns with a scale byte
+  const typename In::Elem* src = static_cast<const typename In::Elem*>(p.x) + (there ? row : 0) * p.ld;
+  uint4 raw[kLoads];
+  auto load = [&](int base) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int c = base + (i * THREADS + at) * EPL;
+      raw[i] = make_uint4(0, 0, 0, 0);
+      if (there && c < p.cols) {
+        if (kVec && c + EPL <= p.cols) {
+          raw[i] = load_once(src + c);
+        } else {
+          uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+          for (int e = 0; e < EPL; ++e)
+            if (c + e < p.cols) {
+              if constexpr (kType == 2) w[e] = __float_as_uint(src[c + e]);
+              else w[e >> 1] |= static_cast<uint32_t>(src[c + e]) << (16 * (e & 1));
+            }
+          raw[i] = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+      }
+    }
+  };
+  auto top_of = [&](const uint4& r) { return In::max_bits(In::max_bits(In::max_bits(In::max_bits(0u, r.x), r.y), r.z), r.w); };
+  load(0);
+  int e = 0;
+  bool bad = false;
+  if constexpr (kGroup == 16) {
+    uint32_t top = 0;
+    for (int base = 0;;) {
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) top = kType == 2 ? max(top, top_of(raw[i])) : __vmaxu2(top, top_of(raw[i]));
+      base += span;
+      if (base >= p.cols) break;
+      load(base);
+    }
+    top = In::fold_bits(top);
+    top = __reduce_max_sync(0xffffffffu, top);
+    if constexpr (THREADS > 32) {
+      if ((threadIdx.x & 31) == 0) warp_top[threadIdx.x >> 5] = top;
+      __syncthreads();
+      top = warp_top[threadIdx.x & (CTA / 32 - 1)];
+      top = __reduce_max_sync(0xffffffffu, top);
+    }
+    const float row_top = In::from_bits(top);
+    bad = !(row_top < INFINITY);
+    e = row_exponent(fmaxf(bad ? 1.f : row_top, kQuantFloor));
+    if (there && at == 0) p.row_scales[row] = bad ? __uint_as_float(0x7FC00000u) : pow2(e);
+    if (span < p.cols) load(0);
+  }
+  for (int base = 0; base < wide; base += span) {
+    if (base > 0) load(base);
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int c = base + (i * THREADS + at) * EPL;              // (a warp's lanes part here only between whole groups' chunks of 4)
+      uint32_t bits = In::fold_bits(top_of(raw[i]));
+#pragma unroll
+      for (int o = 1; o < LPG; o <<= 1) bits = max(bits, __shfl_xor_sync(0xffffffffu, bits, o));
+      const float top = In::from_bits(bits);
+      const bool odd = kGroup == 32 ? !(top < INFINITY) : bad;
+      const GroupScale g = group_scale<kGroup>(top, e, odd);
+      if (c < wide && (at % LPG) == 0) p.scales[scale_at(row, c / kGroup, p.chunks)] = there && c < p.cols ? static_cast<uint8_t>(g.byte) : 0;
+      if (there && c < p.cols) {
+        float v[EPL];
+        In::widen16(raw[i], v);
+        const uint32_t code = encode<kType, kGroup, EPL>(v, g);
+        uint8_t* dst = p.codes + row * p.ld_codes + c / 2;
+        if (c + EPL <= p.cols) {
+          if constexpr (EPL == 8) *reinterpret_cast<uint32_t*>(dst) = code;
+          else *reinterpret_cast<uint16_t*>(dst) = static_cast<uint16_t>(code);
+        } else {
+          for (int b = 0; 2 * b < p.cols - c; ++b) dst[b] = static_cast<uint8_t>(code >> (8 * b));
+        }
+      }
+    }
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ weights
+struct Fp4QuantWeightParams {
+  const void* w;             // [in_dim, out_dim], row stride ld
+  uint8_t* codes;            // [out_dim, ld_codes]
+  uint8_t* scales;
+  float* row_scales;         // [out_dim], groups of 16 only
+  long long ld, ld_codes;
+  int in_dim, out_dim, chunks;
+};
+
+// Row scales of a weight for groups of 16: the largest 2^e over a column, by an atomic maximum of positive numbers' bits (whose order does
+// not matter), over row_scales cleared to zero before.  A CTA takes 64 columns x kColumnRows rows.
+constexpr int kColumnRows = 256;
+template <int kType, bool kVec>
+__global__ void __launch_bounds__(256)
+fp4_column_scales_kernel(const Fp4QuantWeightParams p) {
+  using In = QuantIn<kType>;
+  constexpr int EPL = In::EPL, LPR = 64 / EPL, RPI = 256 / LPR;    // lanes per row, rows per iteration
+  __shared__ uint32_t tops[64];
+  const int tiles = (p.out_dim + 63) / 64;
+  const int col0 = blockIdx.x % tiles * 64;
+  const long long row0 = static_cast<long long>(blockIdx.x / tiles) * kColumnRows;
+  const int c = col0 + threadIdx.x % LPR * EPL, sub = threadIdx.x / LPR;
+  if (threadIdx.x < 64) tops[threadIdx.x] = 0;
+  __syncthreads();
+  const typename In::Elem* src = static_cast<const typename In::Elem*>(p.w) + row0 * p.ld + c;
+  const int n = static_cast<int>(min(static_cast<long long>(kColumnRows), p.in_dim - row0));
+  uint4 top = make_uint4(0, 0, 0, 0);
+  auto take = [&](uint32_t a, uint32_t b) { return kType == 2 ? max(a, b & 0x7FFFFFFFu) : __vmaxu2(a, b & 0x7FFF7FFFu); };
+#pragma unroll 4
+  for (int r = sub; r < n; r += RPI) {
+    uint4 v = make_uint4(0, 0, 0, 0);
+    if (kVec && c + EPL <= p.out_dim) {
+      v = *reinterpret_cast<const uint4*>(src + r * p.ld);
+    } else {
+      uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+      for (int e = 0; e < EPL; ++e)
+        if (c + e < p.out_dim) {
+          if constexpr (kType == 2) w[e] = __float_as_uint(src[r * p.ld + e]);
+          else w[e >> 1] |= static_cast<uint32_t>(src[r * p.ld + e]) << (16 * (e & 1));
+        }
+      v = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    top = make_uint4(take(top.x, v.x), take(top.y, v.y), take(top.z, v.z), take(top.w, v.w));
+  }
+  const uint32_t t[4] = {top.x, top.y, top.z, top.w};
+  const int at = threadIdx.x % LPR * EPL;
+#pragma unroll
+  for (int i = 0; i < EPL; ++i) atomicMax(&tops[at + i], kType == 2 ? t[i] : (t[i >> 1] >> (16 * (i & 1))) & 0xFFFFu);
+  __syncthreads();
+  if (threadIdx.x < 64 && col0 + threadIdx.x < p.out_dim) {
+    const float x = In::from_bits(tops[threadIdx.x]);
+    const bool bad = !(x < INFINITY);
+    const uint32_t bits = bad ? 0x7FC00000u : __float_as_uint(pow2(row_exponent(fmaxf(x, kQuantFloor))));
+    atomicMax(reinterpret_cast<unsigned int*>(p.row_scales) + col0 + threadIdx.x, bits);
+  }
+}
+
+// A CTA transposes kIn x 64 weights through shared memory, a group of one output row per thread and turn.
+constexpr int kWeightOut = 64;
+template <int kType, int kGroup, bool kVec>
+__global__ void __launch_bounds__(256)
+quantize_weight_fp4_kernel(const Fp4QuantWeightParams p) {
+  using In = QuantIn<kType>;
+  using Elem = typename In::Elem;
+  constexpr int EPL = In::EPL, kIn = 128, LPR = kWeightOut / EPL, RPI = 256 / LPR;
+  constexpr int PITCH = kWeightOut + (kType == 2 ? 1 : 2);         // rows of the tile an odd number of words apart
+  __shared__ Elem tile[kIn * PITCH];
+  const int out_tiles = (p.out_dim + 127) / 128 * 2;               // whole scale tiles
+  const int n0 = blockIdx.x % out_tiles * kWeightOut;
+  const int k0 = blockIdx.x / out_tiles * kIn;
+  {
+    const int c = threadIdx.x % LPR * EPL;
+    const Elem* src = static_cast<const Elem*>(p.w) + static_cast<long long>(k0) * p.ld + n0 + c;
+#pragma unroll
+    for (int i = 0; i < kIn / RPI; ++i) {
+      const int r = i * RPI + threadIdx.x / LPR;
+      uint32_t w[4] = {0, 0, 0, 0};
+      if (k0 + r < p.in_dim) {
+        if (kVec && n0 + c + EPL <= p.out_dim) {
+          const uint4 v = load_once(src + r * p.ld);
+          w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+        } else {
+#pragma unroll
+          for (int e = 0; e < EPL; ++e)
+            if (n0 + c + e < p.out_dim) {
+              if constexpr (kType == 2) w[e] = __float_as_uint(src[r * p.ld + e]);
+              else w[e >> 1] |= static_cast<uint32_t>(src[r * p.ld + e]) << (16 * (e & 1));
+            }
+        }
+      }
+      if constexpr (kType == 2) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) tile[r * PITCH + c + e] = __uint_as_float(w[e]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) *reinterpret_cast<uint32_t*>(&tile[r * PITCH + c + 2 * e]) = w[e];
+      }
+    }
+  }
+  __syncthreads();
+  constexpr int GROUPS = kIn / kGroup;                             // of the tile's columns: 8 or 4, one or two scale tiles
+#pragma unroll
+  for (int turn = 0; turn < GROUPS * kWeightOut / 256; ++turn) {
+    // neighbouring lanes take neighbouring output rows (no bank conflicts); a row's groups lie in four warps or eight
+    const int n = threadIdx.x % kWeightOut, gi = turn * (256 / kWeightOut) + threadIdx.x / kWeightOut;
+    const int row = n0 + n, k = k0 + gi * kGroup, group = k / kGroup;
+    if (group >= 4 * p.chunks) continue;
+    const bool there = row < p.out_dim && k < p.in_dim;
+    float v[kGroup];
+    float top = 0.f;
+#pragma unroll
+    for (int i = 0; i < kGroup; ++i) {
+      v[i] = In::widen(tile[(gi * kGroup + i) * PITCH + n]);
+      top = fmax_nan(top, fabsf(v[i]));
+    }
+    int e = 0;
+    bool bad = !(top < INFINITY);
+    if constexpr (kGroup == 16) {
+      const uint32_t u = there ? __float_as_uint(p.row_scales[row]) : 0x3F800000u;
+      bad = u >= 0x7F800000u;
+      e = static_cast<int>(u >> 23) - 127;
+    }
+    const GroupScale g = group_scale<kGroup>(bad ? 0.f : top, e, bad);
+    p.scales[scale_at(row, group, p.chunks)] = there ? static_cast<uint8_t>(g.byte) : 0;
+    if (!there) continue;
+    uint32_t code[kGroup / 8];
+#pragma unroll
+    for (int b = 0; b < kGroup / 8; ++b) {
+      float part[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) part[i] = v[8 * b + i];
+      if constexpr (kType == 2 && kGroup == 16) {
+        float lo[4] = {part[0], part[1], part[2], part[3]}, hi[4] = {part[4], part[5], part[6], part[7]};
+        code[b] = encode<kType, kGroup, 4>(lo, g) | encode<kType, kGroup, 4>(hi, g) << 16;
+      } else {
+        code[b] = encode<kType, kGroup, 8>(part, g);
+      }
+    }
+    uint8_t* dst = p.codes + row * p.ld_codes + k / 2;
+    const int bytes = min(kGroup, p.in_dim - k + 1) / 2;           // of the group: all of its kGroup / 2, or the row's last ones
+    if (bytes == kGroup / 2) {
+      if constexpr (kGroup == 32) *reinterpret_cast<uint4*>(dst) = make_uint4(code[0], code[1], code[2], code[3]);
+      else *reinterpret_cast<uint2*>(dst) = make_uint2(code[0], code[1]);
+    } else {
+      for (int b = 0; b < bytes; ++b) dst[b] = static_cast<uint8_t>(code[b >> 2] >> (8 * (b & 3)));
+    }
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ the values
+struct Fp4ValuesParams {
+  const uint8_t *codes, *scales;
+  const float* row_scales;   // or NULL
+  void* out;
+  long long ld_codes, ld_out;
+  int rows, cols, chunks;
+};
+
+// code * scale (exact) * row scale, rounded to fp32 and then to the output's type.  A CTA takes 128 rows x 128 columns, a lane eight
+// consecutive codes at a time.  Bound by HBM.  kVec: rows of out start on 16-byte boundaries.
+template <int kType, int kGroup, bool kVec>
+__global__ void __launch_bounds__(256)
+dequantize_fp4_kernel(const Fp4ValuesParams p) {
+  const int col_tiles = (p.cols + 127) / 128;
+  const int row0 = blockIdx.x / col_tiles * 128, c = blockIdx.x % col_tiles * 128 + (threadIdx.x & 15) * 8;
+  if (c >= p.cols) return;
+  const int bytes = min(4, (p.cols - c + 1) / 2);
+  uint32_t code[8], byte[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int row = row0 + i * 16 + (threadIdx.x >> 4);
+    code[i] = 0; byte[i] = 0;
+    if (row >= p.rows) continue;
+    const uint8_t* src = p.codes + row * p.ld_codes + c / 2;
+    if (bytes == 4) code[i] = __ldg(reinterpret_cast<const uint32_t*>(src));
+    else for (int b = 0; b < bytes; ++b) code[i] |= static_cast<uint32_t>(src[b]) << (8 * b);
+    byte[i] = __ldg(p.scales + scale_at(row, c / kGroup, p.chunks));
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int row = row0 + i * 16 + (threadIdx.x >> 4);
+    if (row >= p.rows) break;
+    const float scale = kGroup == 16 ? e4m3_value(byte[i]) : e8m0_value(byte[i]);
+    const float factor = p.row_scales ? __ldg(p.row_scales + row) : 1.f;
+    float v[8];
+    e2m1_values(code[i], v);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = v[j] * scale * factor;
+    if constexpr (kType == 2) {
+      float* out = static_cast<float*>(p.out) + row * p.ld_out + c;
+      if (kVec && c + 8 <= p.cols) {
+        reinterpret_cast<float4*>(out)[0] = make_float4(v[0], v[1], v[2], v[3]);
+        reinterpret_cast<float4*>(out)[1] = make_float4(v[4], v[5], v[6], v[7]);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (c + j < p.cols) out[j] = v[j];
+      }
+    } else {
+      uint16_t* out = static_cast<uint16_t*>(p.out) + row * p.ld_out + c;
+      const uint32_t w[4] = {pack16x2<kType == 1>(v[0], v[1]), pack16x2<kType == 1>(v[2], v[3]), pack16x2<kType == 1>(v[4], v[5]),
+                             pack16x2<kType == 1>(v[6], v[7])};
+      if (kVec && c + 8 <= p.cols) {
+        *reinterpret_cast<uint4*>(out) = make_uint4(w[0], w[1], w[2], w[3]);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (c + j < p.cols) out[j] = static_cast<uint16_t>(w[j >> 1] >> (16 * (j & 1)));
+      }
+    }
+  }
+}
+
+}  // namespace dit

@@ -323,6 +323,198 @@ PyObject* block_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// ------------------------------------------------------------------------------------------------ 4-bit floating point
+PyObject* triple(const at::Tensor& a, const at::Tensor& b, const at::Tensor& c) {
+  PyObject* t = PyTuple_New(3);
+  if (!t) throw PythonError{};
+  PyTuple_SET_ITEM(t, 0, THPVariable_Wrap(a));
+  PyTuple_SET_ITEM(t, 1, THPVariable_Wrap(b));
+  if (c.defined()) PyTuple_SET_ITEM(t, 2, THPVariable_Wrap(c));
+  else { Py_INCREF(Py_None); PyTuple_SET_ITEM(t, 2, Py_None); }
+  return t;
+}
+
+int32_t group_of(PyObject* o) {
+  const int64_t g = number(o, "group");
+  if (g != 16 && g != 32) refuse("group must be 16 or 32");
+  return static_cast<int32_t>(g);
+}
+
+int64_t pitch16(const at::Tensor& codes) {       // row stride of codes in bytes; a single row has none of its own
+  return pitch(matrix(codes, "codes"), codes.size(0));
+}
+void check_fp4(const at::Tensor& codes, const at::Tensor& scales, const at::Tensor& row_scales, int64_t rows, int64_t cols, int32_t group, const char* of) {
+  if (codes.scalar_type() != at::kByte || !shaped(codes, rows, (cols + 1) / 2)) refuse(std::string(of) + " must be uint8 codes [rows, ceil(columns / 2)]");
+  if (!scales.is_cuda() || scales.scalar_type() != at::kByte || !scales.is_contiguous() || scales.dim() != 3 || scales.size(0) != (rows + 127) / 128 ||
+      scales.size(1) != (cols + 4 * group - 1) / (4 * group) || scales.size(2) != 512)
+    refuse(std::string("the scales of ") + of + " must be contiguous uint8 [ceil(rows / 128), ceil(columns / (4 group)), 512]");
+  if (row_scales.defined() && (!row_scales.is_cuda() || row_scales.scalar_type() != at::kFloat || row_scales.dim() != 1 || row_scales.size(0) != rows || !row_scales.is_contiguous()))
+    refuse(std::string("the row scales of ") + of + " must be contiguous fp32 [rows]");
+}
+at::Tensor optional(PyObject* o, const char* what) { return given(o) ? tensor(o, what) : at::Tensor(); }
+float* floats(const at::Tensor& t) { return t.defined() ? static_cast<float*>(t.data_ptr()) : nullptr; }
+
+// x, group, codes, scales, row_scales, stream
+template <bool kWeight>
+PyObject* quantize_to_fp4(PyObject* const* a, Py_ssize_t n) {
+  return guarded([&] {
+    arity(n, 6);
+    const char* name = kWeight ? "w" : "x";
+    const at::Tensor& x = tensor(a[0], name);
+    const int64_t ld = matrix(x, name);
+    const int32_t group = group_of(a[1]);
+    const int64_t rows = x.size(kWeight ? 1 : 0), cols = x.size(kWeight ? 0 : 1);    // of the quantised matrix
+    const dit_type type = type_of(x.scalar_type());
+    if (cols < 1 || (kWeight && rows < 1)) refuse("an empty row has no scales", DIT_ERR_SHAPE);
+    const OnStream on(a[5], x.device());
+    at::Tensor codes = optional(a[2], "codes"), scales = optional(a[3], "scales"), row_scales = optional(a[4], "row_scales");
+    if (!codes.defined()) {
+      const int64_t half = (cols + 1) / 2, wide = (half + 15) / 16 * 16;
+      codes = empty({rows, wide}, at::kByte, x);
+      if (wide != half) codes = codes.narrow(1, 0, half);
+    }
+    if (!scales.defined()) scales = empty({(rows + 127) / 128, (cols + 4 * group - 1) / (4 * group), 512}, at::kByte, x);
+    if (group == 32 && row_scales.defined()) refuse("groups of 32 have no row scales");
+    if (group == 16 && !row_scales.defined()) row_scales = empty({rows}, at::kFloat, x);
+    check_fp4(codes, scales, row_scales, rows, cols, group, "the result");
+    same_device(x, {&codes, &scales, &row_scales});
+    check((kWeight ? dit_quantize_weight_fp4 : dit_quantize_fp4)(x.data_ptr(), type, ld, x.size(0), x.size(1), group, codes.data_ptr(), pitch16(codes), scales.data_ptr(),
+                                                                 floats(row_scales), on.raw));
+    return triple(codes, scales, row_scales);
+  });
+}
+PyObject* quantize_fp4(PyObject*, PyObject* const* a, Py_ssize_t n) { return quantize_to_fp4<false>(a, n); }
+PyObject* quantize_weight_fp4(PyObject*, PyObject* const* a, Py_ssize_t n) { return quantize_to_fp4<true>(a, n); }
+
+at::ScalarType wanted_type(PyObject* dtype, PyObject* out) {
+  if (given(dtype) && !THPDtype_Check(dtype)) refuse("out_dtype must be a dtype");
+  const at::ScalarType t = given(dtype) ? reinterpret_cast<THPDtype*>(dtype)->scalar_type : (given(out) ? tensor(out, "out").scalar_type() : at::kHalf);
+  type_of(t);
+  return t;
+}
+
+// codes, scales, cols, group, row_scales, out, out_dtype, stream
+PyObject* dequantize_fp4(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&] {
+    arity(n, 8);
+    const at::Tensor &codes = tensor(a[0], "codes"), &scales = tensor(a[1], "scales");
+    const int64_t cols = number(a[2], "cols");
+    const int32_t group = group_of(a[3]);
+    const int64_t ld = pitch16(codes), rows = codes.size(0);
+    const at::Tensor row_scales = optional(a[4], "row_scales");
+    if (cols < 1) refuse("cols must be at least 1", DIT_ERR_SHAPE);
+    check_fp4(codes, scales, row_scales, rows, cols, group, "codes");
+    const at::ScalarType wanted = wanted_type(a[6], a[5]);
+    const OnStream on(a[7], codes.device());
+    const at::Tensor out = given(a[5]) ? tensor(a[5], "out") : empty({rows, cols}, wanted, codes);
+    if (!shaped(out, rows, cols) || out.scalar_type() != wanted) refuse("out must be [rows, cols] of out_dtype");
+    same_device(codes, {&scales, &row_scales, &out});
+    const int64_t ld_out = matrix(out, "out");
+    check(dit_dequantize_fp4(codes.data_ptr(), ld, scales.data_ptr(), floats(row_scales), rows, cols, group, out.data_ptr(), type_of(wanted), ld_out, on.raw));
+    return THPVariable_Wrap(out);
+  });
+}
+
+// a, a_scales, b, b_scales, k, group, a_row_scales, b_row_scales, bias, out, out_dtype, stream
+PyObject* gemm_fp4(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&] {
+    arity(n, 12);
+    const at::Tensor &x = tensor(a[0], "a"), &sx = tensor(a[1], "a_scales"), &y = tensor(a[2], "b"), &sy = tensor(a[3], "b_scales");
+    dit_gemm_fp4_args g{};
+    g.k = number(a[4], "k");
+    g.group = group_of(a[5]);
+    if (g.k < 1) refuse("k must be at least 1", DIT_ERR_SHAPE);
+    g.lda = pitch16(x); g.ldb = pitch16(y);
+    g.m = x.size(0); g.n = y.size(0);
+    const at::Tensor rx = optional(a[6], "a_row_scales"), ry = optional(a[7], "b_row_scales"), bias = optional(a[8], "bias");
+    check_fp4(x, sx, rx, g.m, g.k, g.group, "a");
+    check_fp4(y, sy, ry, g.n, g.k, g.group, "b");
+    if (bias.defined() && (!bias.is_cuda() || bias.scalar_type() != at::kFloat || bias.dim() != 1 || bias.size(0) != g.n || !bias.is_contiguous()))
+      refuse("bias must be contiguous fp32 [n]");
+    const at::ScalarType wanted = wanted_type(a[10], a[9]);
+    const OnStream on(a[11], x.device());
+    const at::Tensor out = given(a[9]) ? tensor(a[9], "out") : empty({g.m, g.n}, wanted, x);
+    if (!shaped(out, g.m, g.n) || out.scalar_type() != wanted) refuse("out must be [m, n] of out_dtype");
+    same_device(x, {&sx, &rx, &y, &sy, &ry, &bias, &out});
+    g.ld_out = matrix(out, "out");
+    g.a = x.data_ptr(); g.a_scales = sx.data_ptr(); g.a_rows = floats(rx);
+    g.b = y.data_ptr(); g.b_scales = sy.data_ptr(); g.b_rows = floats(ry);
+    g.bias = floats(bias); g.out = out.data_ptr(); g.out_type = type_of(wanted);
+    check(dit_gemm_fp4(&g, on.raw));
+    return THPVariable_Wrap(out);
+  });
+}
+
+// ------------------------------------------------------------------------------------------------ prompts
+double real(PyObject* o, const char* what) {
+  const double v = PyFloat_AsDouble(o);
+  if (v == -1.0 && PyErr_Occurred()) { PyErr_Clear(); refuse(std::string(what) + " must be a number"); }
+  return v;
+}
+bool truth(PyObject* o) {
+  const int t = PyObject_IsTrue(o);
+  if (t < 0) throw PythonError{};
+  return t != 0;
+}
+
+// x, n_heads, lens, first, positions, rotary_dim, interleaved, base, factor, ramp, magnitude, inverse, out, stream
+PyObject* rotary(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&] {
+    arity(n, 14);
+    const at::Tensor& x = tensor(a[0], "x");
+    dit_rotary_args r{};
+    r.ld_x = matrix(x, "x"); r.rows = x.size(0); r.type = type_of(x.scalar_type());
+    const int64_t heads = number(a[1], "n_heads"), width = x.size(1);
+    if (heads < 1 || heads > INT32_MAX || width < 1 || width % heads) refuse("the columns of x do not divide into n_heads");
+    if (width / heads > INT32_MAX) refuse("head_dim is out of range", DIT_ERR_SHAPE);
+    r.n_heads = static_cast<int32_t>(heads); r.head_dim = static_cast<int32_t>(width / heads);
+    if (given(a[2]) == given(a[4])) refuse("either lens or positions");
+    if (given(a[4]) && given(a[3])) refuse("first goes with lens");
+    std::vector<int32_t> lens, first;
+    at::Tensor positions;
+    if (given(a[2])) {
+      lens = numbers(a[2], "lens");
+      if (given(a[3])) first = numbers(a[3], "first");
+      if (given(a[3]) && first.size() != lens.size()) refuse("lens and first differ in length");
+      if (lens.size() > DIT_MAX_REQUESTS) refuse("too many requests", DIT_ERR_CAPACITY);
+      r.n_requests = static_cast<int32_t>(lens.size()); r.lens = lens.data(); r.first = given(a[3]) ? first.data() : nullptr;
+      if (lens.empty()) r.lens = r.first = nullptr;
+    } else {
+      positions = tensor(a[4], "positions");
+      if (!positions.is_cuda() || positions.scalar_type() != at::kInt || positions.dim() != 1 || positions.size(0) != r.rows || !positions.is_contiguous())
+        refuse("positions must be contiguous int32 [rows]");
+      r.positions = static_cast<const int32_t*>(positions.data_ptr());
+    }
+    const int64_t rotary_dim = given(a[5]) ? number(a[5], "rotary_dim") : r.head_dim;
+    if (rotary_dim < 2 || rotary_dim > r.head_dim) refuse("rotary_dim must lie between 2 and head_dim", DIT_ERR_SHAPE);
+    r.rotary_dim = static_cast<int32_t>(rotary_dim);
+    r.interleaved = truth(a[6]); r.base = real(a[7], "base"); r.factor = real(a[8], "factor");
+    if (given(a[9])) {
+      PyObject* ramp = PySequence_Tuple(a[9]);
+      if (!ramp) { PyErr_Clear(); refuse("ramp must be (low, high, trained length)"); }
+      double v[3] = {};
+      const bool three = PyTuple_GET_SIZE(ramp) == 3;
+      try {
+        for (int i = 0; three && i < 3; ++i) v[i] = real(PyTuple_GET_ITEM(ramp, i), "ramp");
+      } catch (...) { Py_DECREF(ramp); throw; }
+      Py_DECREF(ramp);
+      if (!three || !(v[2] > 0.0)) refuse("ramp must be (low, high, trained length), the length positive");
+      r.low = v[0]; r.high = v[1]; r.trained_len = v[2];
+    }
+    const double magnitude = real(a[10], "magnitude");
+    r.magnitude = static_cast<float>(magnitude);
+    r.inverse = truth(a[11]);
+    const OnStream on(a[13], x.device());
+    const at::Tensor out = given(a[12]) ? tensor(a[12], "out") : empty({x.size(0), x.size(1)}, x.scalar_type(), x);
+    if (!shaped(out, x.size(0), x.size(1)) || out.scalar_type() != x.scalar_type()) refuse("out must be shaped and typed like x");
+    same_device(x, {&positions, &out});
+    r.ld_out = matrix(out, "out");
+    r.x = x.data_ptr(); r.out = out.data_ptr();
+    check(dit_rotary(&r, on.raw));
+    return THPVariable_Wrap(out);
+  });
+}
+
 PyObject* set_error(PyObject*, PyObject* cls) {
   Py_INCREF(cls);
   Py_XDECREF(g_error);
@@ -332,6 +524,7 @@ PyObject* set_error(PyObject*, PyObject* cls) {
 
 #define FAST(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(&name)), METH_FASTCALL, nullptr}
 PyMethodDef kMethods[] = {FAST(quantize_block128), FAST(quantize_weight_block128), FAST(gemm_block128), FAST(select_blocks), FAST(block_attention),
+                          FAST(quantize_fp4), FAST(quantize_weight_fp4), FAST(dequantize_fp4), FAST(gemm_fp4), FAST(rotary),
                           {"set_error", &set_error, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 

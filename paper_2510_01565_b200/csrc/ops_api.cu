@@ -15,11 +15,7 @@ using namespace dit;
 
 namespace {
 
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
-                                  const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-constexpr int kMaxDevices = 64;
+constexpr int kMaxDevices = kOpsMaxDevices;
 constexpr int64_t kMaxSize = INT32_MAX - 1024;
 // selecting kernel: means of eight query blocks, then the scores of one to eight rows
 constexpr int kSelectFixedSmem = kSelectRows * kSelectPitch * 8;
@@ -31,7 +27,7 @@ static __device__ int g_ops_status;
 
 struct DeviceState {
   bool ready;
-  int num_sms, pairs;                  // pairs: CTA pairs of the pair kernel that are resident at once
+  int index, num_sms, pairs;                  // pairs: CTA pairs of the pair kernel that are resident at once
   int* status;
 };
 std::mutex g_mutex;
@@ -98,6 +94,7 @@ cudaError_t device_state(const DeviceState** out, bool* unsupported) {
     int clusters = 0;
     if ((e = cudaOccupancyMaxActiveClusters(&clusters, reinterpret_cast<const void*>(&gemm_block128_pair_kernel<kBlkF16>), &lc)) != cudaSuccess) return e;
     s.pairs = std::max(1, std::min(clusters, s.num_sms / 2));
+    s.index = dev;
     s.ready = true;
   }
   *out = &s;
@@ -346,6 +343,14 @@ cudaError_t ops_prepare_device() {
   const DeviceState* d;
   bool unsupported;
   return device_state(&d, &unsupported);
+}
+
+dit_status ops_device(OpsDevice* d) {
+  const DeviceState* state;
+  const dit_status s = ready(&state);
+  if (s != DIT_OK) return s;
+  *d = OpsDevice{state->index, state->num_sms, state->status, g_encode};
+  return DIT_OK;
 }
 
 cudaError_t launch_block_product(const BlockProduct& b, const SeqInfo& seq, cudaStream_t st) {

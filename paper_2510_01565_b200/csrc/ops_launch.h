@@ -29,6 +29,18 @@ struct BlockProduct {
 };
 
 cudaError_t ops_prepare_device();                      // sets kernel attributes once per device
+
+// What the context-free operators share on the current device.
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                  const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+constexpr int kOpsMaxDevices = 64;
+struct OpsDevice {
+  int index, num_sms;
+  int* status;               // word for waits that ran out (dit_ops_poll_status)
+  EncodeTiledFn encode;
+};
+dit_status ops_device(OpsDevice* d);
 cudaError_t launch_block_product(const BlockProduct& b, const SeqInfo& seq, cudaStream_t st);
 // dit_block_attention with a status word of the caller's.  clamp: infinite results become the largest finite value, as in every
 // activation of a step, where an infinity would meet zeros further on.
