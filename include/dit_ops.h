@@ -220,6 +220,39 @@ typedef struct {
 } dit_rotary_args;
 dit_status dit_rotary(const dit_rotary_args *args, void *stream);
 
+/* Softmax attention of a batch of packed requests with grouped heads: request r owns q_lens[r] rows of q and out and kv_lens[r] rows of k and
+ * v, one request after the other; head h is columns h * head_dim .. of q and out and reads key head h / (n_heads / n_kv_heads).
+ *   out[i] = sum_j softmax_j(scale * q_i . k_j) v_j
+ * over the keys j <= kv_len - q_len + i of row i's request where `causal` (the new rows are the last ones of their context: whole prompts have
+ * equal lengths, a single new token has q_len 1), over all keys of the request otherwise.  A row that sees no key gets zeros, and so does
+ * one all of whose scores are -infinity.  Keys and values that a row does not see are never part of its result, whatever they hold.
+ * Scores, their differences, the softmax and the sums are held in fp32, probabilities are rounded to the inputs' type for the second product;
+ * scores of any size and infinite or NaN values are treated as dit_block_attention treats them.  A request's results do not depend on the
+ * values of the others; those of one with few rows (q_len * n_heads / n_kv_heads <= DIT_PROMPT_FEW_ROWS) are summed in parts that depend on
+ * the lengths of the whole batch, and may differ in their last bits with the batch that it comes in.
+ *   q, k, v, out  device, type f16 or bf16, 16-byte aligned, leading dimensions multiples of 8 and >= n_heads * head_dim (q, out) or
+ *                 n_kv_heads * head_dim (k, v); column ranges of one packed buffer are fine; out must not overlap the inputs
+ *   head_dim      64 or 128 (DIT_ERR_SHAPE); n_kv_heads divides n_heads; n_requests <= DIT_MAX_REQUESTS; sums of lengths < 2^31 - 1024
+ *   scale         0 for 1 / sqrt(head_dim); at most 2e38
+ *   workspace     device, 16-byte aligned, dit_prompt_attention_workspace(args) bytes (sizes only are read; may be 0, then NULL is fine); its
+ *                 contents need not be kept between calls, and calls that may run at the same time need workspaces of their own
+ * A request may have no rows of q, or none of k. */
+#define DIT_PROMPT_FEW_ROWS 64
+typedef struct {
+  const void *q, *k, *v;
+  void *out;
+  int64_t ld_q, ld_k, ld_v, ld_out;
+  dit_type type;
+  int32_t n_heads, n_kv_heads, head_dim, causal;
+  float scale;
+  int32_t n_requests;
+  const int32_t *q_lens, *kv_lens;
+  void *workspace;
+  size_t workspace_bytes;
+} dit_prompt_attention_args;
+size_t dit_prompt_attention_workspace(const dit_prompt_attention_args *args);
+dit_status dit_prompt_attention(const dit_prompt_attention_args *args, void *stream);
+
 /* Reads and clears (with a synchronisation of the current device) the status word that a kernel of this
  * header sets when a bounded wait ran out: DIT_OK or DIT_ERR_TIMEOUT. */
 dit_status dit_ops_poll_status(void);

@@ -82,10 +82,16 @@ class DitRotaryArgs(C.Structure):
                 + [("n_requests", C.c_int32), ("lens", C.POINTER(C.c_int32)), ("first", C.POINTER(C.c_int32))])
 
 
+class DitPromptAttentionArgs(C.Structure):
+    _fields_ = ([(n, C.c_void_p) for n in ("q", "k", "v", "out")] + [(n, C.c_int64) for n in ("ld_q", "ld_k", "ld_v", "ld_out")] + [("type", C.c_int)]
+                + [(n, C.c_int32) for n in ("n_heads", "n_kv_heads", "head_dim", "causal")] + [("scale", C.c_float), ("n_requests", C.c_int32)]
+                + [("q_lens", C.POINTER(C.c_int32)), ("kv_lens", C.POINTER(C.c_int32)), ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t)])
+
+
 SCHED_EXPORTS = ["dit_sched_allocate", "dit_sched_round"]
 OPS_EXPORTS = ["dit_quantize_block128", "dit_quantize_weight_block128", "dit_gemm_block128", "dit_select_blocks_workspace", "dit_select_blocks",
                "dit_block_attention", "dit_fp4_scale_bytes", "dit_quantize_fp4", "dit_quantize_weight_fp4", "dit_dequantize_fp4", "dit_gemm_fp4",
-               "dit_rotary", "dit_ops_poll_status"]
+               "dit_rotary", "dit_prompt_attention_workspace", "dit_prompt_attention", "dit_ops_poll_status"]
 BLOCK = 128      # columns per scale; rows per query block and per key block
 
 
@@ -211,6 +217,11 @@ def load_library() -> C.CDLL:
     lib.dit_gemm_fp4.argtypes = [C.POINTER(DitGemmFp4Args), vp]
     lib.dit_rotary.restype = C.c_int
     lib.dit_rotary.argtypes = [C.POINTER(DitRotaryArgs), vp]
+    pp = C.POINTER(DitPromptAttentionArgs)
+    lib.dit_prompt_attention_workspace.restype = C.c_size_t
+    lib.dit_prompt_attention_workspace.argtypes = [pp]
+    lib.dit_prompt_attention.restype = C.c_int
+    lib.dit_prompt_attention.argtypes = [pp, vp]
     lib.dit_ops_poll_status.restype = C.c_int
     lib.dit_ops_poll_status.argtypes = []
     lib.dit_last_launch_count.restype = i64
@@ -709,6 +720,13 @@ def dit_rotary(x, n_heads: int, lens=None, first=None, positions=None, rotary_di
     all).  factor, ramp = (low, high, trained length): scaling for longer contexts than the trained one.  inverse: the rotation back, which
     is its gradient."""
     return (_native or _marshal()).rotary(x, n_heads, lens, first, positions, rotary_dim, interleaved, base, factor, ramp, magnitude, inverse, out, stream)
+
+
+def dit_prompt_attention(q, k, v, q_lens, kv_lens, n_heads: int, n_kv_heads=None, causal: bool = True, scale: float = 0.0, out=None, workspace=None,
+                         stream=None):
+    """q [sum q_lens, n_heads * d], k and v [sum kv_lens, n_kv_heads * d] fp16 or bf16 (d 64 or 128; n_kv_heads: default n_heads) -> out, shaped
+    and typed like q.  causal: row i of a request sees its keys up to kv_len - q_len + i; otherwise all of them."""
+    return (_native or _marshal()).prompt_attention(q, k, v, q_lens, kv_lens, n_heads, n_kv_heads, causal, scale, out, workspace, stream)
 
 
 def dit_ops_poll_status():

@@ -368,4 +368,20 @@ done:
   }
 }
 
+// ----------------------------------------------------------------------------------- shared with the context-free operators
+// Results are packed with finite values clamped (rounded probabilities may add up to a little more than one, and a value at the
+// format's limit must not leave it); an infinite result stays one.
+template <bool BF16>
+__device__ __forceinline__ uint32_t infinity_bits(float x) { return (BF16 ? 0x7F80u : 0x7C00u) | (x < 0.f ? 0x8000u : 0u); }
+template <bool BF16>
+__device__ __forceinline__ uint32_t put_infinities(uint32_t packed, float lo, float hi) {
+  if (fabsf(lo) == INFINITY) packed = (packed & 0xFFFF0000u) | infinity_bits<BF16>(lo);
+  if (fabsf(hi) == INFINITY) packed = (packed & 0x0000FFFFu) | infinity_bits<BF16>(hi) << 16;
+  return packed;
+}
+
+// Kernels for a few query rows.
+constexpr int kRowsTile = 64;                  // keys per tile
+constexpr int kRowsMax = 16;                   // query rows
+
 }  // namespace dit

@@ -34,17 +34,6 @@ struct BlockAttnParams {
   int* status;
 };
 
-// Results are packed with finite values clamped (rounded probabilities may add up to a little more than one, and a value at the
-// format's limit must not leave it); an infinite result stays one.
-template <bool BF16>
-__device__ __forceinline__ uint32_t infinity_bits(float x) { return (BF16 ? 0x7F80u : 0x7C00u) | (x < 0.f ? 0x8000u : 0u); }
-template <bool BF16>
-__device__ __forceinline__ uint32_t put_infinities(uint32_t packed, float lo, float hi) {
-  if (fabsf(lo) == INFINITY) packed = (packed & 0xFFFF0000u) | infinity_bits<BF16>(lo);
-  if (fabsf(hi) == INFINITY) packed = (packed & 0x0000FFFFu) | infinity_bits<BF16>(hi) << 16;
-  return packed;
-}
-
 constexpr int kWindowBlocks = 256;      // key blocks whose lists are laid out in shared memory at a time
 constexpr int kMaxKeyBlocks = 16384;    // of one request
 
@@ -523,8 +512,6 @@ done:
 // Four requests of one row, 24 heads of 128, 60 blocks in all (94 MB): 19 us when they are in L2, 24.8 us (3.8 TB/s) from DRAM; longer
 // lists, beyond L2, 5.7-6.2 TB/s.
 // ------------------------------------------------------------------------------------------------
-constexpr int kRowsTile = 64;                  // keys per tile
-constexpr int kRowsMax = 16;                   // query rows
 template <int D>
 struct BlockRowsCfg {
   static constexpr int NP = D / 64, PANEL = kRowsTile * 128, TILE_BYTES = NP * PANEL;

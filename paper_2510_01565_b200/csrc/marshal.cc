@@ -515,6 +515,52 @@ PyObject* rotary(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// q, k, v, q_lens, kv_lens, n_heads, n_kv_heads, causal, scale, out, workspace, stream
+PyObject* prompt_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&] {
+    arity(n, 12);
+    const at::Tensor &q = tensor(a[0], "q"), &k = tensor(a[1], "k"), &v = tensor(a[2], "v");
+    const std::vector<int32_t> q_lens = numbers(a[3], "q_lens"), kv_lens = numbers(a[4], "kv_lens");
+    if (q_lens.size() != kv_lens.size()) refuse("q_lens and kv_lens differ in length");
+    if (q_lens.size() > DIT_MAX_REQUESTS) refuse("too many requests", DIT_ERR_CAPACITY);
+    const int64_t heads = number(a[5], "n_heads"), kv_heads = given(a[6]) ? number(a[6], "n_kv_heads") : heads;
+    dit_prompt_attention_args p{};
+    p.ld_q = matrix(q, "q"); p.ld_k = matrix(k, "k"); p.ld_v = matrix(v, "v");
+    const int64_t width = q.size(1);
+    if (heads < 1 || width < 1 || width % heads) refuse("the columns of q do not divide into n_heads");
+    if (kv_heads < 1 || heads % kv_heads) refuse("n_kv_heads must divide n_heads");
+    if (heads > INT32_MAX || width / heads > INT32_MAX) refuse("n_heads is out of range", DIT_ERR_SHAPE);
+    const int64_t kv_width = width / heads * kv_heads;
+    int64_t rows = 0, kv_rows = 0;
+    for (size_t r = 0; r < q_lens.size(); ++r) {
+      if (q_lens[r] < 0 || kv_lens[r] < 0) refuse("a length is negative");
+      rows += q_lens[r]; kv_rows += kv_lens[r];
+    }
+    if (q.size(0) != rows || !shaped(k, kv_rows, kv_width) || !shaped(v, kv_rows, kv_width)) refuse("q must be [sum of q_lens, n_heads * d], k and v [sum of kv_lens, n_kv_heads * d]");
+    if (k.scalar_type() != q.scalar_type() || v.scalar_type() != q.scalar_type()) refuse("q, k and v differ in type");
+    p.type = type_of(q.scalar_type());
+    p.n_heads = static_cast<int32_t>(heads); p.n_kv_heads = static_cast<int32_t>(kv_heads); p.head_dim = static_cast<int32_t>(width / heads);
+    p.causal = truth(a[7]);
+    const double scale = real(a[8], "scale");
+    if (scale != 0.0 && static_cast<float>(scale) == 0.f) refuse("scale rounds to zero, which stands for 1 / sqrt(head_dim)");
+    p.scale = static_cast<float>(scale);
+    p.n_requests = static_cast<int32_t>(q_lens.size()); p.q_lens = q_lens.data(); p.kv_lens = kv_lens.data();
+    const OnStream on(a[11], q.device());
+    const at::Tensor out = given(a[9]) ? tensor(a[9], "out") : empty({rows, width}, q.scalar_type(), q);
+    if (!shaped(out, rows, width) || out.scalar_type() != q.scalar_type()) refuse("out must be shaped and typed like q");
+    at::Tensor workspace = optional(a[10], "workspace");
+    const size_t need = dit_prompt_attention_workspace(&p);
+    if (!workspace.defined() && need > 0) workspace = empty({static_cast<int64_t>(need)}, at::kByte, q);
+    if (workspace.defined() && (!workspace.is_cuda() || !workspace.is_contiguous())) refuse("workspace must be a contiguous CUDA tensor");
+    same_device(q, {&k, &v, &out, &workspace});
+    p.ld_out = matrix(out, "out");
+    p.q = q.data_ptr(); p.k = k.data_ptr(); p.v = v.data_ptr(); p.out = out.data_ptr();
+    if (workspace.defined()) { p.workspace = workspace.data_ptr(); p.workspace_bytes = workspace.nbytes(); }
+    check(dit_prompt_attention(&p, on.raw));
+    return THPVariable_Wrap(out);
+  });
+}
+
 PyObject* set_error(PyObject*, PyObject* cls) {
   Py_INCREF(cls);
   Py_XDECREF(g_error);
@@ -524,7 +570,7 @@ PyObject* set_error(PyObject*, PyObject* cls) {
 
 #define FAST(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(&name)), METH_FASTCALL, nullptr}
 PyMethodDef kMethods[] = {FAST(quantize_block128), FAST(quantize_weight_block128), FAST(gemm_block128), FAST(select_blocks), FAST(block_attention),
-                          FAST(quantize_fp4), FAST(quantize_weight_fp4), FAST(dequantize_fp4), FAST(gemm_fp4), FAST(rotary),
+                          FAST(quantize_fp4), FAST(quantize_weight_fp4), FAST(dequantize_fp4), FAST(gemm_fp4), FAST(rotary), FAST(prompt_attention),
                           {"set_error", &set_error, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 

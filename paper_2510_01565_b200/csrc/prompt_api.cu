@@ -1,9 +1,11 @@
-// Rotary positions of include/dit_ops.h: argument checks and launches.
+// Rotary positions and attention over packed prompts (include/dit_ops.h): argument checks, tensor maps, launch rules.
 #include <algorithm>
 #include <cmath>
+#include <mutex>
 
 #include "common.cuh"
 #include "ops_launch.h"
+#include "prompt_attention.cuh"
 #include "rotary.cuh"
 
 using namespace dit;
@@ -22,6 +24,146 @@ cudaError_t launch_rotary(const RotaryParams& p, bool vec, cudaStream_t st) {
   if (vec) rotary_kernel<kType, true><<<grid, kRotaryThreads, 0, st>>>(p);
   else rotary_kernel<kType, false><<<grid, kRotaryThreads, 0, st>>>(p);
   return cudaGetLastError();
+}
+
+// ------------------------------------------------------------------------------------------------ attention
+std::mutex g_mutex;
+bool g_ready[kOpsMaxDevices];
+
+template <class Kernel>
+cudaError_t allow_smem(Kernel kernel, int bytes) {
+  return cudaFuncSetAttribute(reinterpret_cast<const void*>(kernel), cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+}
+template <int D, bool BF16>
+cudaError_t allow_attention() {
+  const cudaError_t e = allow_smem(&prompt_attention_kernel<D, BF16>, PromptAttnCfg<D>::SMEM_BYTES);
+  return e == cudaSuccess ? allow_smem(&prompt_rows_kernel<D, BF16>, PromptRowsCfg<D>::SMEM_BYTES) : e;
+}
+cudaError_t prepare(const OpsDevice& d) {
+  std::lock_guard<std::mutex> lock(g_mutex);
+  if (g_ready[d.index]) return cudaSuccess;
+  cudaError_t e;
+  if ((e = allow_attention<64, false>()) != cudaSuccess || (e = allow_attention<64, true>()) != cudaSuccess ||
+      (e = allow_attention<128, false>()) != cudaSuccess || (e = allow_attention<128, true>()) != cudaSuccess)
+    return e;
+  g_ready[d.index] = true;
+  return cudaSuccess;
+}
+
+// 16-bit matrix [rows, cols] with row stride ld: boxes of 64 columns x box_rows rows, 128-byte swizzle, zeros outside.
+bool half_map(const OpsDevice& d, CUtensorMap* m, const void* ptr, uint64_t cols, uint64_t rows, uint64_t ld, uint32_t box_rows) {
+  const cuuint64_t dims[2] = {cols, rows};
+  const cuuint64_t strides[1] = {ld * 2};
+  const cuuint32_t box[2] = {64, box_rows};
+  const cuuint32_t estr[2] = {1, 1};
+  return d.encode(m, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, const_cast<void*>(ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// How a batch is worked on: which requests go to which kernel, and into how many parts the few-row requests are cut.
+struct PromptPlan {
+  PromptBatch tiled, few;
+  int64_t items;             // of the tiled kernel
+  int64_t row_tiles, ctas;   // of the few-row kernel
+  int chunk;
+  bool join;                 // some request has several parts
+};
+constexpr int kFewRowCtas = 296;                 // two on each of 148 SMs
+
+int64_t few_row_ctas(const PromptPlan& p, const dit_prompt_attention_args& a, int chunk) {
+  int64_t n = 0;
+  for (int i = 0; i < p.few.n; ++i) {
+    const int r = p.few.order[i];
+    n += static_cast<int64_t>(a.n_kv_heads) * prompt_row_tiles(a.q_lens[r], a.n_heads / a.n_kv_heads) * prompt_parts(a.kv_lens[r], chunk);
+  }
+  return n;
+}
+
+// Checks sizes and lays the batch out.
+dit_status plan_prompts(const dit_prompt_attention_args& a, PromptPlan* p) {
+  if (a.n_requests < 0 || a.n_heads < 1 || a.n_kv_heads < 1 || a.n_heads % a.n_kv_heads || (a.type != DIT_TYPE_F16 && a.type != DIT_TYPE_BF16)) return DIT_ERR_INVALID_ARG;
+  if (a.head_dim != 64 && a.head_dim != 128) return DIT_ERR_SHAPE;
+  if (a.n_requests > DIT_MAX_REQUESTS) return DIT_ERR_CAPACITY;
+  if (a.n_requests > 0 && (!a.q_lens || !a.kv_lens)) return DIT_ERR_INVALID_ARG;
+  if (static_cast<int64_t>(a.n_heads) * a.head_dim > (1 << 20)) return DIT_ERR_SHAPE;
+  *p = PromptPlan{};
+  const int64_t group = a.n_heads / a.n_kv_heads;
+  int64_t q = 0, kv = 0, keys = 0;
+  for (int r = 0; r <= a.n_requests; ++r) {
+    p->tiled.cu_q[r] = p->few.cu_q[r] = static_cast<int>(q);
+    p->tiled.cu_kv[r] = p->few.cu_kv[r] = static_cast<int>(kv);
+    if (r == a.n_requests) break;
+    if (a.q_lens[r] < 0 || a.kv_lens[r] < 0) return DIT_ERR_INVALID_ARG;
+    q += a.q_lens[r]; kv += a.kv_lens[r];
+    if (q > kMaxSize || kv > kMaxSize) return DIT_ERR_SHAPE;
+    if (a.q_lens[r] == 0) continue;
+    PromptBatch& b = a.q_lens[r] * group <= DIT_PROMPT_FEW_ROWS ? p->few : p->tiled;
+    int at = b.n++;
+    for (; at > 0 && a.kv_lens[b.order[at - 1]] < a.kv_lens[r]; --at) b.order[at] = b.order[at - 1];      // most keys first
+    b.order[at] = r;
+    if (&b == &p->tiled) {
+      p->items += ((((static_cast<int64_t>(a.q_lens[r]) + 127) / 128) * group + 1) / 2) * a.n_kv_heads;
+    } else {
+      const int64_t tiles = static_cast<int64_t>(a.n_kv_heads) * prompt_row_tiles(a.q_lens[r], static_cast<int>(group));
+      p->row_tiles += tiles;
+      keys += tiles * a.kv_lens[r];
+    }
+  }
+  if (p->items > INT32_MAX / 16) return DIT_ERR_SHAPE;
+  if (p->few.n > 0) {
+    // Parts of equal length, as short as lets all of them run at once; where that would leave parts of more than 2048 keys the batch takes
+    // several waves anyway, and parts of 1024 keep them even.
+    int64_t chunk = std::max<int64_t>(256, (keys / kFewRowCtas + 63) / 64 * 64);
+    if (chunk <= 2048) {
+      for (const int64_t least = chunk; few_row_ctas(*p, a, static_cast<int>(chunk)) > kFewRowCtas && chunk < 2 * least;) chunk += std::max<int64_t>(64, least / 16 / 64 * 64);
+    } else {
+      chunk = 1024;
+    }
+    p->chunk = static_cast<int>(chunk);
+    p->ctas = few_row_ctas(*p, a, p->chunk);
+    if (p->ctas > INT32_MAX / 16) return DIT_ERR_SHAPE;
+    p->join = p->ctas > p->row_tiles;
+  }
+  return DIT_OK;
+}
+size_t part_bytes(const PromptPlan& p, int head_dim) { return p.join ? static_cast<size_t>(p.ctas) * kRowsMax * (head_dim + 2) * sizeof(float) : 0; }
+
+template <int D, bool BF16>
+cudaError_t launch_attention(const OpsDevice& d, const dit_prompt_attention_args& a, const PromptPlan& plan, PromptAttnParams p, cudaStream_t st) {
+  const uint64_t width = static_cast<uint64_t>(a.n_heads) * D, kv_width = static_cast<uint64_t>(a.n_kv_heads) * D;
+  const int q_rows = plan.tiled.cu_q[a.n_requests], kv_rows = plan.tiled.cu_kv[a.n_requests];
+  // without keys nothing is loaded; the maps still have to describe some memory
+  const void* k = kv_rows > 0 ? a.k : a.q;
+  const void* v = kv_rows > 0 ? a.v : a.q;
+  const uint64_t ld_k = kv_rows > 0 ? a.ld_k : a.ld_q, ld_v = kv_rows > 0 ? a.ld_v : a.ld_q;
+  CUtensorMap tmQ, tmK, tmV;
+  cudaError_t e;
+  if (plan.items > 0) {
+    if (!half_map(d, &tmQ, a.q, width, q_rows, a.ld_q, 128) || !half_map(d, &tmK, k, kv_width, std::max(kv_rows, 1), ld_k, 128) ||
+        !half_map(d, &tmV, v, kv_width, std::max(kv_rows, 1), ld_v, 128))
+      return cudaErrorInvalidValue;
+    p.items = static_cast<int>(plan.items);
+    prompt_attention_kernel<D, BF16><<<std::min(p.items, d.num_sms), PromptAttnCfg<D>::THREADS, PromptAttnCfg<D>::SMEM_BYTES, st>>>(tmQ, tmK, tmV, p, plan.tiled);
+    if ((e = cudaGetLastError()) != cudaSuccess) return e;
+  }
+  if (plan.few.n > 0) {
+    if (!half_map(d, &tmK, k, kv_width, std::max(kv_rows, 1), ld_k, kRowsTile) || !half_map(d, &tmV, v, kv_width, std::max(kv_rows, 1), ld_v, kRowsTile))
+      return cudaErrorInvalidValue;
+    p.chunk = plan.chunk;
+    p.parts = static_cast<float*>(a.workspace);
+    prompt_rows_kernel<D, BF16><<<static_cast<unsigned>(plan.ctas), PromptRowsCfg<D>::THREADS, PromptRowsCfg<D>::SMEM_BYTES, st>>>(tmK, tmV, p, plan.few);
+    if ((e = cudaGetLastError()) != cudaSuccess) return e;
+    if (plan.join) {
+      cudaLaunchConfig_t lc = {};
+      lc.gridDim = dim3(static_cast<unsigned>(plan.row_tiles), kRowsMax); lc.blockDim = dim3(D); lc.stream = st;
+      cudaLaunchAttribute at;
+      at.id = cudaLaunchAttributeProgrammaticStreamSerialization;               // set up while the parts are still being computed
+      at.val.programmaticStreamSerializationAllowed = 1;
+      lc.attrs = &at; lc.numAttrs = 1;
+      if ((e = cudaLaunchKernelEx(&lc, &prompt_join_kernel<D, BF16>, p, plan.few)) != cudaSuccess) return e;
+    }
+  }
+  return cudaSuccess;
 }
 
 }  // namespace
@@ -87,6 +229,46 @@ dit_status dit_rotary(const dit_rotary_args* a, void* stream) {
   if (a->type == DIT_TYPE_F16) e = launch_rotary<0>(p, vec, st);
   else if (a->type == DIT_TYPE_BF16) e = launch_rotary<1>(p, vec, st);
   else e = launch_rotary<2>(p, vec, st);
+  return e == cudaSuccess ? DIT_OK : DIT_ERR_CUDA;
+}
+
+size_t dit_prompt_attention_workspace(const dit_prompt_attention_args* a) {
+  PromptPlan plan;
+  if (!a || plan_prompts(*a, &plan) != DIT_OK) return 0;
+  return part_bytes(plan, a->head_dim);
+}
+
+dit_status dit_prompt_attention(const dit_prompt_attention_args* a, void* stream) {
+  if (!a) return DIT_ERR_INVALID_ARG;
+  PromptPlan plan;
+  dit_status s = plan_prompts(*a, &plan);
+  if (s != DIT_OK) return s;
+  const int64_t width = static_cast<int64_t>(a->n_heads) * a->head_dim, kv_width = static_cast<int64_t>(a->n_kv_heads) * a->head_dim;
+  auto matrix = [&](const void* p, int64_t ld, int64_t rows, int64_t cols) { return rows == 0 || (p && aligned(p, 16) && ld >= cols && ld % 8 == 0); };
+  const int q_rows = plan.tiled.cu_q[a->n_requests], kv_rows = plan.tiled.cu_kv[a->n_requests];
+  if (!matrix(a->q, a->ld_q, q_rows, width) || !matrix(a->out, a->ld_out, q_rows, width) || !matrix(a->k, a->ld_k, kv_rows, kv_width) ||
+      !matrix(a->v, a->ld_v, kv_rows, kv_width))
+    return DIT_ERR_INVALID_ARG;
+  if (!(a->scale >= 0.f) || !(a->scale <= 2.0e38f)) return DIT_ERR_INVALID_ARG;      // scale * log2(e) has to be finite
+  if (q_rows == 0) return DIT_OK;
+  const size_t need = part_bytes(plan, a->head_dim);
+  if (need > 0 && (!a->workspace || !aligned(a->workspace, 16))) return DIT_ERR_INVALID_ARG;
+  if (a->workspace_bytes < need) return DIT_ERR_CAPACITY;
+  OpsDevice d;
+  s = ops_device(&d);
+  if (s != DIT_OK) return s;
+  if (prepare(d) != cudaSuccess) return DIT_ERR_CUDA;
+  PromptAttnParams p{};
+  p.out = a->out; p.ld_out = a->ld_out; p.q = static_cast<const uint16_t*>(a->q); p.v = static_cast<const uint16_t*>(a->v);
+  p.ld_q = a->ld_q; p.ld_v = a->ld_v; p.n_heads = a->n_heads; p.kv_heads = a->n_kv_heads; p.group = a->n_heads / a->n_kv_heads;
+  p.causal = a->causal != 0;
+  p.scale_log2 = 1.4426950408889634f * (a->scale > 0.f ? a->scale : 1.0f / sqrtf(static_cast<float>(a->head_dim)));
+  p.wide_out = aligned(a->out, 32) && a->ld_out % 16 == 0;
+  p.status = d.status;
+  const cudaStream_t st = static_cast<cudaStream_t>(stream);
+  cudaError_t e;
+  if (a->head_dim == 128) e = a->type == DIT_TYPE_BF16 ? launch_attention<128, true>(d, *a, plan, p, st) : launch_attention<128, false>(d, *a, plan, p, st);
+  else e = a->type == DIT_TYPE_BF16 ? launch_attention<64, true>(d, *a, plan, p, st) : launch_attention<64, false>(d, *a, plan, p, st);
   return e == cudaSuccess ? DIT_OK : DIT_ERR_CUDA;
 }
 

@@ -1,0 +1,763 @@
+// Attention over packed requests with grouped heads: every query row over the keys of its request up to its own place (causal) or over all.
+//
+// prompt_attention_kernel   two tiles of 128 query rows that share a key head per CTA, on the tensor cores, for many rows
+// prompt_rows_kernel        up to 16 rows (query rows x heads of a group) per CTA over a part of the keys, for a few rows against a long
+//                           context; prompt_join_kernel joins the parts
+#pragma once
+#include <type_traits>
+
+#include "attention.cuh"
+#include "common.cuh"
+#include "ptx.cuh"
+
+namespace dit {
+
+// Packed batch, passed by value.  `order`: the requests that a launch takes.
+struct PromptBatch {
+  int n;                     // entries of order
+  int cu_q[DIT_MAX_REQUESTS + 1], cu_kv[DIT_MAX_REQUESTS + 1];
+  int order[DIT_MAX_REQUESTS];
+};
+
+struct PromptAttnParams {
+  void* out;
+  long long ld_out;
+  const uint16_t* q;
+  const uint16_t* v;         // for values that are no finite numbers in places that only some rows see
+  long long ld_q, ld_v;
+  int n_heads, kv_heads, group;
+  int causal;
+  float scale_log2;          // scale * log2(e), positive
+  int items;                 // tiled kernel: (request, key head, pair of query tiles)
+  int wide_out;              // rows of out start on 32-byte boundaries
+  int* status;
+  // few rows
+  int chunk;                 // keys per CTA, a multiple of 64
+  float* parts;              // [CTAs][16][head_dim + 2]
+};
+
+// The 16-bit value's exponent is all ones: an infinity or NaN.
+template <bool BF16>
+__device__ __forceinline__ bool odd_bits(uint32_t h) { return (h & (BF16 ? 0x7F80u : 0x7C00u)) == (BF16 ? 0x7F80u : 0x7C00u); }
+template <bool BF16>
+__device__ __forceinline__ float widen16bit(uint32_t h) {
+  return BF16 ? __uint_as_float(h << 16) : __half2float(__ushort_as_half(static_cast<unsigned short>(h)));
+}
+// A pair of 16-bit values with infinities and NaN replaced by zero; *odd becomes true where one was.
+template <bool BF16>
+__device__ __forceinline__ uint32_t finite_pair(uint32_t w, bool* odd) {
+  const bool lo = odd_bits<BF16>(w & 0xFFFFu), hi = odd_bits<BF16>(w >> 16);
+  *odd |= lo || hi;
+  return (lo ? 0u : w & 0xFFFFu) | (hi ? 0u : w & 0xFFFF0000u);
+}
+
+template <int D>
+struct PromptAttnCfg {
+  static constexpr int NP = D / 64, PANEL = 128 * 128, TILE_BYTES = NP * PANEL;
+  static constexpr int K_STAGES = 3, V_STAGES = 2;
+  static constexpr int OFF_Q = 0, OFF_K = 2 * TILE_BYTES, OFF_V = OFF_K + K_STAGES * TILE_BYTES;
+  static constexpr int OFF_BAR = OFF_V + V_STAGES * TILE_BYTES;
+  static constexpr int SMEM_USED = OFF_BAR + 256 + 1024;
+  // one CTA per SM: each takes all of tensor memory
+  static constexpr int SMEM_BYTES = SMEM_USED > 116 * 1024 ? SMEM_USED : 116 * 1024;
+  static constexpr int THREADS = 384;
+  static_assert(SMEM_BYTES <= 227 * 1024, "shared memory of one CTA");
+};
+
+// Two query tiles: consecutive ones of the list (last 128-row block first, the heads of the group one after the other) of a request and a key
+// head.  With an even group they are two heads' tiles of the same rows; otherwise also neighbouring row blocks.
+struct PromptItem {
+  int kv_head, req, q_begin, q_len, kv_begin, kv_len;
+  int before;                // keys before the first query row's own (may be negative), or all of them where nothing is masked
+  int head[2], qb[2];
+  int n_kv[2];               // key blocks that a tile's last row sees; n_kv[0] >= n_kv[1]
+  int ragged;                // first key block of which some row of a tile sees only a part
+  bool tile1;
+  __device__ __forceinline__ int limit(int row, int causal) const { return causal ? min(kv_len, before + row + 1) : kv_len; }   // keys of a row
+};
+__device__ __forceinline__ PromptItem prompt_item(const PromptBatch& batch, const PromptAttnParams& p, int item) {
+  PromptItem it{};
+  int tiles = 0, pair = 0;
+  for (int i = 0; i < batch.n; ++i) {
+    it.req = batch.order[i];
+    tiles = ((batch.cu_q[it.req + 1] - batch.cu_q[it.req] + 127) >> 7) * p.group;
+    const int here = ((tiles + 1) >> 1) * p.kv_heads;
+    if (item < here) { pair = item / p.kv_heads; it.kv_head = item - pair * p.kv_heads; break; }
+    item -= here;
+  }
+  it.q_begin = batch.cu_q[it.req]; it.q_len = batch.cu_q[it.req + 1] - it.q_begin;
+  it.kv_begin = batch.cu_kv[it.req]; it.kv_len = batch.cu_kv[it.req + 1] - it.kv_begin;
+  it.before = it.kv_len - it.q_len;
+  it.tile1 = 2 * pair + 1 < tiles;
+  const int last_block = ((it.q_len + 127) >> 7) - 1;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int t = min(2 * pair + i, tiles - 1), back = t / p.group;
+    it.qb[i] = last_block - back;
+    it.head[i] = it.kv_head * p.group + t - back * p.group;
+    it.n_kv[i] = (max(0, it.limit(min(it.q_len, it.qb[i] * 128 + 128) - 1, p.causal)) + 127) >> 7;
+  }
+  if (!it.tile1) it.n_kv[1] = 0;
+  it.ragged = p.causal ? max(0, it.limit((it.tile1 ? it.qb[1] : it.qb[0]) * 128, 1)) >> 7 : it.n_kv[0];
+  return it;
+}
+
+// The scheme of the list kernel (block_attention_kernel: two 128-row query tiles with a softmax warpgroup each, one S buffer handed between
+// them, P in tensor memory, O rescaled rarely, persistent grid whose roles run on from item to item) over the key blocks 0 .. n - 1 of a
+// request.  Sharing a key head is what makes a pair: a key block is loaded once and used by both tiles.
+// Items are ordered by their cost and dealt out forwards and backwards in turn, so that CTAs come out even.
+// A causal tile masks its last block or two.  Scores that a row does not see are dropped before its maximum.  Values that it does not
+// see meet a probability of zero, which an infinity or NaN would turn into NaN: in the blocks that some rows see only in part such values are
+// replaced by zeros in shared memory, and if there was one, the rows that do see it add it to their results at the end.
+template <int D, bool BF16>
+__global__ void __launch_bounds__(PromptAttnCfg<D>::THREADS, 1)
+prompt_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
+                        const PromptAttnParams p, const __grid_constant__ PromptBatch batch) {
+  using C = PromptAttnCfg<D>;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t raw = smem_u32(smem_raw);
+  const uint32_t base = (raw + 1023u) & ~1023u;
+  uint8_t* aligned = smem_raw + (base - raw);
+  const uint32_t bar0 = base + C::OFF_BAR;
+  const uint32_t q_full = bar0, q_empty = bar0 + 8u, s_free = bar0 + 16u;
+  auto k_full = [&](int s) { return bar0 + 8u * (3 + s); };
+  auto k_empty = [&](int s) { return bar0 + 8u * (6 + s); };
+  auto v_full = [&](int s) { return bar0 + 8u * (9 + s); };
+  auto v_empty = [&](int s) { return bar0 + 8u * (11 + s); };
+  auto s_full = [&](int i) { return bar0 + 8u * (13 + i); };
+  auto p_full = [&](int i) { return bar0 + 8u * (15 + i); };
+  auto o_full = [&](int i) { return bar0 + 8u * (17 + i); };
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(aligned + C::OFF_BAR + 8 * 19);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  volatile int* odd_values = reinterpret_cast<volatile int*>(tmem_slot + 2);      // [2]: a tile's item met values that were replaced
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    mbar_init(q_full, 1); mbar_init(q_empty, 1); mbar_init(s_free, 4);
+    for (int s = 0; s < C::K_STAGES; ++s) { mbar_init(k_full(s), 1); mbar_init(k_empty(s), 1); }
+    for (int s = 0; s < C::V_STAGES; ++s) { mbar_init(v_full(s), 1); mbar_init(v_empty(s), 1); }
+    for (int i = 0; i < 2; ++i) { mbar_init(s_full(i), 1); mbar_init(p_full(i), 4); mbar_init(o_full(i), 1); }
+    *abort_flag = 0;
+    fence_mbar_init();
+  }
+  if (warp == 0 && lane == 0) { prefetch_tmap(&tmQ); prefetch_tmap(&tmK); prefetch_tmap(&tmV); }
+  if (warp == 1) { tmem_alloc(smem_u32(tmem_slot), 512); tmem_relinquish(); }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+  const uint32_t tS = tmem_base, tP = tmem_base + 128, tO = tmem_base + 256;      // columns: S 128, P 2 x 64, O 2 x 128
+
+  // this CTA's k-th item: forwards and backwards in turn
+  auto item_at = [&](int k) { return k * static_cast<int>(gridDim.x) + ((k & 1) ? static_cast<int>(gridDim.x - 1 - blockIdx.x) : static_cast<int>(blockIdx.x)); };
+
+  if (warp < 4) {
+    DIT_SETMAXNREG_DEC(96);
+    if (warp == 0) {
+      if (lane == 0) {
+        // ---------------------------------------------------------------- TMA producer
+        int ks = 0, vs = 0; uint32_t kph = 1, vph = 1, qph = 1;
+        for (int k = 0, item; (item = item_at(k)) < p.items; ++k) {
+          const PromptItem it = prompt_item(batch, p, item);
+          if (!mbar_wait(q_empty, qph, abort_flag)) goto done;
+          qph ^= 1u;
+          mbar_arrive_expect_tx(q_full, (it.tile1 ? 2 : 1) * C::TILE_BYTES);
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+            for (int pn = 0; pn < (i == 0 || it.tile1 ? C::NP : 0); ++pn)
+              tma_load_2d(base + C::OFF_Q + i * C::TILE_BYTES + pn * C::PANEL, &tmQ, it.head[i] * D + pn * 64, it.q_begin + it.qb[i] * 128, q_full);
+          for (int j = 0; j < it.n_kv[0]; ++j) {
+            const int y = it.kv_begin + j * 128;
+            if (!mbar_wait(k_empty(ks), kph, abort_flag)) goto done;
+            mbar_arrive_expect_tx(k_full(ks), C::TILE_BYTES);
+            for (int pn = 0; pn < C::NP; ++pn)
+              tma_load_2d(base + C::OFF_K + ks * C::TILE_BYTES + pn * C::PANEL, &tmK, it.kv_head * D + pn * 64, y, k_full(ks));
+            if (++ks == C::K_STAGES) { ks = 0; kph ^= 1u; }
+            if (!mbar_wait(v_empty(vs), vph, abort_flag)) goto done;
+            mbar_arrive_expect_tx(v_full(vs), C::TILE_BYTES);
+            for (int pn = 0; pn < C::NP; ++pn)
+              tma_load_2d(base + C::OFF_V + vs * C::TILE_BYTES + pn * C::PANEL, &tmV, it.kv_head * D + pn * 64, y, v_full(vs));
+            if (++vs == C::V_STAGES) { vs = 0; vph ^= 1u; }
+          }
+        }
+      }
+    } else if (warp == 1) {
+      if (lane == 0) {
+        // ---------------------------------------------------------------- MMA issuer 1: scores
+        constexpr uint32_t idesc_s = idesc_f16(128, 128, false, BF16);
+        const uint64_t qdesc0 = smem_desc_sw128(base + C::OFF_Q, 16, 1024), kdesc0 = smem_desc_sw128(base + C::OFF_K, 16, 1024);
+        constexpr uint32_t kTileStep = C::TILE_BYTES >> 4;
+        int ks = 0; uint32_t kph = 0, qph = 0, u = 0;                             // u: uses of S so far
+        for (int k = 0, item; (item = item_at(k)) < p.items; ++k) {
+          const PromptItem it = prompt_item(batch, p, item);
+          if (!mbar_wait(q_full, qph, abort_flag)) goto done;
+          qph ^= 1u;
+          for (int j = 0; j < it.n_kv[0]; ++j) {
+            const int tiles = j < it.n_kv[1] ? 2 : 1;
+            if (!mbar_wait(k_full(ks), kph, abort_flag)) goto done;
+            for (int i = 0; i < tiles; ++i) {
+              if (u > 0 && !mbar_wait(s_free, (u - 1) & 1u, abort_flag)) goto done;
+              ++u;
+              tc_fence_after();
+              const uint64_t qd = qdesc0 + i * kTileStep, kd = kdesc0 + ks * kTileStep;
+#pragma unroll
+              for (int kk = 0; kk < D / 16; ++kk) {
+                const uint32_t off = ((kk >> 2) * C::PANEL + (kk & 3) * 32) >> 4;
+                umma_f16(tS, qd + off, kd + off, idesc_s, kk != 0);
+              }
+              if (i == tiles - 1) umma_commit(k_empty(ks));
+              umma_commit(s_full(i));
+            }
+            if (++ks == C::K_STAGES) { ks = 0; kph ^= 1u; }
+          }
+          umma_commit(q_empty);                                                   // Q may be replaced once these products have read it
+        }
+      }
+    } else if (warp == 2) {
+      // ------------------------------------------------------------------ MMA issuer 2: P V; the whole warp clears the V rows behind a
+      // request's last key and replaces what is no finite number in blocks that some rows see in part
+      constexpr uint32_t idesc_pv = idesc_f16(128, D, true, BF16);
+      const uint64_t vdesc0 = smem_desc_sw128(base + C::OFF_V, C::PANEL, 1024);
+      constexpr uint32_t kTileStep = C::TILE_BYTES >> 4;
+      int vs = 0; uint32_t vph = 0, done_uses[2] = {0, 0};
+      for (int k = 0, item; (item = item_at(k)) < p.items; ++k) {
+        const PromptItem it = prompt_item(batch, p, item);
+        bool odd = false;                                                         // values replaced in this item (warp-uniform)
+        for (int j = 0; j < it.n_kv[0]; ++j) {
+          const int tiles = j < it.n_kv[1] ? 2 : 1;
+          if (!__all_sync(0xffffffffu, mbar_wait(v_full(vs), vph, abort_flag))) goto done;
+          const int valid = it.kv_len - j * 128;
+          uint8_t* tile = aligned + C::OFF_V + vs * C::TILE_BYTES;
+          if (valid < 128) {
+            for (int r = valid * 8 + lane; r < 128 * 8; r += 32)                  // 16-byte units of rows valid .. 127
+              for (int pn = 0; pn < C::NP; ++pn) *reinterpret_cast<uint4*>(tile + pn * C::PANEL + r * 16) = make_uint4(0, 0, 0, 0);
+          }
+          if (j >= it.ragged) {
+            constexpr uint32_t kExp = BF16 ? 0x7F807F80u : 0x7C007C00u;
+            const int units = min(128, valid) * 8;
+            uint32_t most = 0;                                                    // largest magnitudes of the odd and the even columns
+            for (int pn = 0; pn < C::NP; ++pn)
+#pragma unroll 4
+              for (int r = lane; r < units; r += 32) {
+                const uint4 w = *reinterpret_cast<const uint4*>(tile + pn * C::PANEL + r * 16);
+                most = __vmaxu2(__vmaxu2(__vmaxu2(most, w.x & 0x7FFF7FFFu), __vmaxu2(w.y & 0x7FFF7FFFu, w.z & 0x7FFF7FFFu)), w.w & 0x7FFF7FFFu);
+              }
+            if (__any_sync(0xffffffffu, (most & 0xFFFFu) >= (kExp & 0xFFFFu) || (most >> 16) >= (kExp >> 16))) {
+              odd = true;
+              bool unused = false;
+              for (int pn = 0; pn < C::NP; ++pn)
+                for (int r = lane; r < units; r += 32) {
+                  uint4* at = reinterpret_cast<uint4*>(tile + pn * C::PANEL + r * 16);
+                  const uint4 w = *at;
+                  *at = make_uint4(finite_pair<BF16>(w.x, &unused), finite_pair<BF16>(w.y, &unused), finite_pair<BF16>(w.z, &unused), finite_pair<BF16>(w.w, &unused));
+                }
+            }
+          }
+          if (valid < 128 || odd) {
+            fence_proxy_async_smem();
+            __syncwarp();
+          }
+          const uint64_t vd = vdesc0 + vs * kTileStep;
+          for (int i = 0; i < tiles; ++i) {
+            if (!__all_sync(0xffffffffu, mbar_wait(p_full(i), done_uses[i] & 1u, abort_flag))) goto done;
+            tc_fence_after();
+            if (lane == 0) {
+              // (the tile's warps are in this item, since they have handed over a P of it: they no longer read the last item's word)
+              odd_values[i] = odd;
+              __threadfence_block();
+#pragma unroll
+              for (int kk = 0; kk < 8; ++kk)
+                umma_f16_ts(tO + i * 128, tP + i * 64 + kk * 8, vd + kk * (2048 >> 4), idesc_pv, j != 0 || kk != 0);
+              if (i == tiles - 1) umma_commit(v_empty(vs));
+              umma_commit(o_full(i));
+            }
+            __syncwarp();
+            ++done_uses[i];
+          }
+          if (++vs == C::V_STAGES) { vs = 0; vph ^= 1u; }
+        }
+      }
+    }
+  } else {
+    // -------------------------------------------------------------------- softmax + accumulate (2 warpgroups)
+    DIT_SETMAXNREG_INC(200);
+    const int tile = (warp >> 2) - 1, quarter = warp & 3;
+    const uint32_t lane_sel = static_cast<uint32_t>(quarter * 32) << 16;
+    const uint32_t tSi = tS + lane_sel, tPi = tP + tile * 64 + lane_sel, tOi = tO + tile * 128 + lane_sel;
+    const float c = p.scale_log2;
+    const float2 c2 = make_float2(c, c);
+    constexpr float kRescaleLog2 = 8.0f;       // O is rescaled when a row's maximum has grown by more than 2^8: P stays <= 2^8
+    constexpr float kFarLog2 = 1024.0f;        // scaled references beyond it are taken off before the scaling
+    uint32_t use = 0;                          // key blocks of this warpgroup so far
+
+    for (int k = 0, item; (item = item_at(k)) < p.items; ++k) {
+      const PromptItem it = prompt_item(batch, p, item);
+      const int qb = tile == 0 ? it.qb[0] : it.qb[1], head = tile == 0 ? it.head[0] : it.head[1], n_kv = tile == 0 ? it.n_kv[0] : it.n_kv[1];
+      const int row = qb * 128 + quarter * 32 + lane;                             // in the request
+      const int limit = it.limit(row, p.causal);
+      float m_ref = -INFINITY, l = 0.f;
+      const uint32_t first_use = use;
+      for (int j = 0; j < n_kv; ++j) {
+        if (!__all_sync(0xffffffffu, mbar_wait(s_full(tile), use & 1u, abort_flag))) goto done;
+        tc_fence_after();
+        const int valid = limit - j * 128;   // keys of the block that the row sees (may be <= 0)
+        uint32_t sv[128];
+        __syncwarp();
+#pragma unroll
+        for (int ch = 0; ch < 4; ++ch) tmem_ld32p(tSi + ch * 32, sv + ch * 32);
+        tmem_ld_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(s_free);
+        if (__any_sync(0xffffffffu, valid < 128)) {
+#pragma unroll
+          for (int i = 0; i < 128; ++i)
+            if (i >= valid) sv[i] = 0xff800000u;
+        }
+        float mx0 = -INFINITY, mx1 = -INFINITY, mx2 = -INFINITY, mx3 = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < 128; i += 8) {
+          mx0 = fmax3(mx0, __uint_as_float(sv[i]), __uint_as_float(sv[i + 1]));
+          mx1 = fmax3(mx1, __uint_as_float(sv[i + 2]), __uint_as_float(sv[i + 3]));
+          mx2 = fmax3(mx2, __uint_as_float(sv[i + 4]), __uint_as_float(sv[i + 5]));
+          mx3 = fmax3(mx3, __uint_as_float(sv[i + 6]), __uint_as_float(sv[i + 7]));
+        }
+        const float mx = fmaxf(fmaxf(mx0, mx1), fmaxf(mx2, mx3));
+        // Two rare things, behind one vote.  A row's maximum has grown far beyond its reference: this warp's rows of O are rescaled.
+        // Or its reference is large: the exponent s * c - round(m_ref * c) is off by that rounding, which is at most 2^-14 below the
+        // limit and common to all that share the reference, but from 2^28 on would leave the 16-bit probabilities.  Beyond the
+        // limit the reference is therefore taken off the scores before the scaling: (s - m_ref) * c is 0 for the largest
+        // whatever c is.  Decided row by row, so that a row does not depend on its neighbours.
+        if (use == first_use) m_ref = mx;
+        const bool grow = (mx - m_ref) * c > kRescaleLog2;
+        bool far = fabsf(m_ref * c) > kFarLog2;
+        if (__any_sync(0xffffffffu, grow || far)) {
+          if (__any_sync(0xffffffffu, grow)) {
+            if (!__all_sync(0xffffffffu, mbar_wait(o_full(tile), (use - 1) & 1u, abort_flag))) goto done;
+            tc_fence_after();
+            const float alpha = grow ? exp2_approx((m_ref - mx) * c) : 1.0f;
+            if (grow) { m_ref = mx; l *= alpha; }
+#pragma unroll 1
+            for (int ch = 0; ch < D / 32; ++ch) {
+              uint32_t r[32];
+              __syncwarp();
+              tmem_ld32(tOi + ch * 32, r);
+              tmem_ld_wait();
+#pragma unroll
+              for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * alpha);
+              tmem_st32(tOi + ch * 32, r);
+            }
+            tmem_st_wait();
+          }
+          far = fabsf(m_ref * c) > kFarLog2;
+          // (a reference of -inf, every score so far -inf from infinite inputs, would make the exponents NaN: nothing is taken off)
+          const float off = far && m_ref != -INFINITY ? m_ref : 0.f;
+#pragma unroll
+          for (int i = 0; i < 128; ++i) sv[i] = __float_as_uint(__uint_as_float(sv[i]) - off);
+        }
+        const float neg_mc = far ? 0.f : -m_ref * c;
+        const float2 nm2 = make_float2(neg_mc, neg_mc);
+        float2 rs0 = make_float2(0.f, 0.f), rs1 = make_float2(0.f, 0.f);
+#pragma unroll
+        for (int i = 0; i < 128; i += 2) {
+          const float2 x = ffma2(make_float2(__uint_as_float(sv[i]), __uint_as_float(sv[i + 1])), c2, nm2);
+          const float2 ex = make_float2(exp2_approx(x.x), exp2_approx(x.y));
+          if (i & 2) rs1 = fadd2(rs1, ex); else rs0 = fadd2(rs0, ex);
+          sv[i >> 1] = pack16x2<BF16>(ex.x, ex.y);
+        }
+        if (use != first_use) {              // P is still read by this tile's previous product until that has finished
+          if (!__all_sync(0xffffffffu, mbar_wait(o_full(tile), (use - 1) & 1u, abort_flag))) goto done;
+          tc_fence_after();
+        }
+#pragma unroll
+        for (int ch = 0; ch < 4; ++ch) tmem_st16(tPi + ch * 16, *reinterpret_cast<const uint32_t(*)[16]>(sv + ch * 16));
+        tmem_st_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(p_full(tile));
+        l += (rs0.x + rs0.y) + (rs1.x + rs1.y);
+        ++use;
+      }
+      if (tile == 1 && !it.tile1) continue;
+      uint16_t* out = static_cast<uint16_t*>(p.out) + (static_cast<long long>(it.q_begin) + row) * p.ld_out + head * D;
+      const bool any = use != first_use;       // without a key: zeros
+      bool odd = false;
+      if (any) {
+        if (!__all_sync(0xffffffffu, mbar_wait(o_full(tile), (use - 1) & 1u, abort_flag))) goto done;
+        tc_fence_after();
+        odd = odd_values[tile] != 0;
+      }
+      const float inv = l == 0.f ? 0.f : 1.0f / l;
+      // The results of 32 channels at a time; `kept` writes infinities as such, with the replaced values that the row sees, and is a second
+      // pass over the rare rows that have one, so that the ordinary one pays for the largest magnitude only.
+      float largest[2] = {0.f, 0.f};
+      auto write = [&](auto kept) {
+#pragma unroll 1
+        for (int ch = 0; ch < D / 32; ++ch) {
+          uint32_t r[32];
+          __syncwarp();
+          if (any) {
+            tmem_ld32(tOi + ch * 32, r);
+            tmem_ld_wait();
+          } else {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) r[i] = 0u;
+          }
+          if (row < it.q_len) {
+            if constexpr (decltype(kept)::value) {
+              if (odd) {                       // (a factor of 1 / l is positive: it leaves infinities and NaN as they are)
+                const uint16_t* v = p.v + (static_cast<long long>(it.kv_begin) + it.ragged * 128) * p.ld_v + it.kv_head * D + ch * 32;
+                for (int key = it.ragged * 128; key < limit; ++key, v += p.ld_v) {
+#pragma unroll
+                  for (int i = 0; i < 32; ++i)
+                    if (odd_bits<BF16>(__ldg(v + i))) r[i] = __float_as_uint(__uint_as_float(r[i]) + widen16bit<BF16>(__ldg(v + i)));
+                }
+              }
+            }
+#pragma unroll
+            for (int v = 0; v < 2; ++v) {      // a lane writes its own row, a whole 32-byte sector per store
+              uint32_t wd[8];
+#pragma unroll
+              for (int h = 0; h < 8; ++h) {
+                const float lo = __uint_as_float(r[16 * v + 2 * h]), hi = __uint_as_float(r[16 * v + 2 * h + 1]);
+                wd[h] = pack16x2<BF16>(lo * inv, hi * inv);
+                if constexpr (decltype(kept)::value) wd[h] = put_infinities<BF16>(wd[h], lo * inv, hi * inv);
+              }
+              uint16_t* at = out + ch * 32 + v * 16;
+              if (p.wide_out) {
+                st_global_v8(at, wd);
+              } else {
+                reinterpret_cast<uint4*>(at)[0] = make_uint4(wd[0], wd[1], wd[2], wd[3]);
+                reinterpret_cast<uint4*>(at)[1] = make_uint4(wd[4], wd[5], wd[6], wd[7]);
+              }
+            }
+            if constexpr (!decltype(kept)::value) {
+#pragma unroll
+              for (int i = 0; i < 32; i += 4) {
+                largest[0] = fmax3(largest[0], fabsf(__uint_as_float(r[i])), fabsf(__uint_as_float(r[i + 1])));
+                largest[1] = fmax3(largest[1], fabsf(__uint_as_float(r[i + 2])), fabsf(__uint_as_float(r[i + 3])));
+              }
+            }
+          }
+        }
+      };
+      write(std::false_type{});
+      if (__any_sync(0xffffffffu, odd || fmaxf(largest[0], largest[1]) == INFINITY)) write(std::true_type{});
+    }
+  }
+
+done:
+  tc_fence_before();
+  __syncthreads();
+  settle_if_aborted(abort_flag);
+  __syncwarp();
+  if (warp == 1) { tc_fence_after(); tmem_dealloc(tmem_base, 512); }
+  if (threadIdx.x == 0 && *abort_flag) atomicMax(p.status, kStatusAttnTimeout);
+}
+
+// ------------------------------------------------------------------------------------------------
+// Few rows.  The query rows of a request and the heads of a group make rows of one product with the group's keys (row i * group + h), 16 to
+// a CTA, so that a new token's heads read the keys once.  Reading the stored keys and values is the bound: a CTA takes p.chunk of them,
+// chosen so that one wave of two CTAs per SM covers the batch, however uneven its requests are.  Inside it is block_rows_kernel: K and V by TMA in
+// tiles of 64 keys through one ring, four warps with 16 keys of every tile each, warp-level products, the warps' results joined in
+// shared memory.  A request with one chunk writes its rows; the parts of the others go to memory as (sums, maximum, sum of
+// probabilities) and prompt_join_kernel joins them in their order.
+// ------------------------------------------------------------------------------------------------
+template <int D>
+struct PromptRowsCfg {
+  static constexpr int NP = D / 64, PANEL = kRowsTile * 128, TILE_BYTES = NP * PANEL;
+  static constexpr int STAGES = 96 * 1024 / TILE_BYTES;                          // 6 (d = 128), 12 (d = 64)
+  static constexpr int OFF_BAR = STAGES * TILE_BYTES;
+  static constexpr int SMEM_BYTES = OFF_BAR + 256 + 1024;
+  static constexpr int THREADS = 160;                                            // four key warps and a producer
+  static constexpr int PART = D + 2;                                             // floats of a row's partial result: channels, maximum, sum
+  static_assert(4 * kRowsMax * PART * 4 <= OFF_BAR, "the partial results take the ring's place");
+  static_assert(2 * SMEM_BYTES <= 227 * 1024, "two CTAs per SM");
+};
+
+// Where a CTA of the few-row kernels works: CTAs are counted request by request, key head by key head, row tile by row tile, chunk by chunk.
+struct PromptPart {
+  int req, kv_head, row0, part, parts;         // parts of the request
+  int q_begin, q_len, kv_begin, kv_len, before;
+};
+__host__ __device__ inline int prompt_row_tiles(int q_len, int group) { return (q_len * group + kRowsMax - 1) / kRowsMax; }
+__host__ __device__ inline int prompt_parts(int kv_len, int chunk) { return kv_len > chunk ? (kv_len + chunk - 1) / chunk : 1; }
+__device__ __forceinline__ PromptPart prompt_part(const PromptBatch& batch, const PromptAttnParams& p, int cta) {
+  PromptPart w{};
+  for (int i = 0; i < batch.n; ++i) {
+    w.req = batch.order[i];
+    w.q_begin = batch.cu_q[w.req]; w.q_len = batch.cu_q[w.req + 1] - w.q_begin;
+    w.kv_begin = batch.cu_kv[w.req]; w.kv_len = batch.cu_kv[w.req + 1] - w.kv_begin;
+    w.parts = prompt_parts(w.kv_len, p.chunk);
+    const int tiles = prompt_row_tiles(w.q_len, p.group), here = tiles * w.parts * p.kv_heads;
+    if (cta < here) {
+      w.part = cta % w.parts;
+      const int rest = cta / w.parts;
+      w.row0 = rest % tiles * kRowsMax;
+      w.kv_head = rest / tiles;
+      break;
+    }
+    cta -= here;
+  }
+  w.before = w.kv_len - w.q_len;
+  return w;
+}
+// Keys that row i of the request sees.
+__device__ __forceinline__ int prompt_limit(const PromptPart& w, const PromptAttnParams& p, int i) {
+  return p.causal ? max(0, min(w.kv_len, w.before + i + 1)) : w.kv_len;
+}
+// A finished result of a row: replaced values that it sees (keys first .. limit - 1) are added.
+template <bool BF16>
+__device__ __forceinline__ void prompt_store(const PromptAttnParams& p, const PromptPart& w, int row, int channel, int d, float x, int first) {
+  const int i = row / p.group, head = w.kv_head * p.group + row - i * p.group, limit = prompt_limit(w, p, i);
+  const uint16_t* v = p.v + (static_cast<long long>(w.kv_begin) + first) * p.ld_v + w.kv_head * d + channel;
+  for (int key = first; key < limit; ++key, v += p.ld_v)
+    if (odd_bits<BF16>(__ldg(v))) x += widen16bit<BF16>(__ldg(v));
+  static_cast<uint16_t*>(p.out)[(static_cast<long long>(w.q_begin) + i) * p.ld_out + head * d + channel] =
+      fabsf(x) == INFINITY ? static_cast<uint16_t>(infinity_bits<BF16>(x)) : pack16<BF16>(x);
+}
+
+template <int D, bool BF16>
+__global__ void __launch_bounds__(PromptRowsCfg<D>::THREADS, 2)
+prompt_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const PromptAttnParams p,
+                   const __grid_constant__ PromptBatch batch) {
+  using C = PromptRowsCfg<D>;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t raw = smem_u32(smem_raw);
+  const uint32_t base = (raw + 1023u) & ~1023u;
+  uint8_t* aligned = smem_raw + (base - raw);
+  const uint32_t bar0 = base + C::OFF_BAR;
+  auto full = [&](int s) { return bar0 + 8u * s; };
+  auto empty = [&](int s) { return bar0 + 8u * (C::STAGES + s); };
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(aligned + C::OFF_BAR + 16 * C::STAGES);
+  float* part = reinterpret_cast<float*>(aligned);                      // [4 warps][kRowsMax][PART], after the main loop
+
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");       // (the joining kernel waits for this one's end itself)
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const PromptPart w = prompt_part(batch, p, blockIdx.x);
+  const int rows = min(kRowsMax, w.q_len * p.group - w.row0);           // of this CTA, 1 .. kRowsMax
+  const int first = prompt_limit(w, p, w.row0 / p.group);               // keys that all of its rows see
+  const int most = prompt_limit(w, p, (w.row0 + rows - 1) / p.group);   // keys that the last one sees
+  const int begin = w.part * p.chunk, end = min(most, begin + p.chunk); // of this CTA (begin may be >= end)
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < C::STAGES; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 4); }
+    *abort_flag = 0;
+    fence_mbar_init();
+    prefetch_tmap(&tmK); prefetch_tmap(&tmV);
+  }
+  // Q as the first operand: k step t, rows lane / 4 and + 8, channels 16 t + 2 (lane % 4) and + 8; absent rows are zero
+  uint32_t qa[D / 16][4];
+  int limit[2] = {0, 0};                                                // keys of the lane's two rows
+  if (warp < 4) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int r = (lane >> 2) + 8 * h, row = w.row0 + r, i = row / p.group;
+      const uint16_t* q = p.q + (static_cast<long long>(w.q_begin) + i) * p.ld_q + (w.kv_head * p.group + row - i * p.group) * D;
+      if (r < rows) limit[h] = prompt_limit(w, p, i);
+#pragma unroll
+      for (int t = 0; t < D / 16; ++t) {
+        const int c = t * 16 + (lane & 3) * 2;
+        qa[t][h] = r < rows ? *reinterpret_cast<const uint32_t*>(q + c) : 0u;
+        qa[t][2 + h] = r < rows ? *reinterpret_cast<const uint32_t*>(q + c + 8) : 0u;
+      }
+    }
+  }
+  __syncthreads();
+
+  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};               // rows lane / 4 and + 8; l: this lane's columns only
+  float acc[D / 8][4];
+#pragma unroll
+  for (int i = 0; i < D / 8; ++i)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) acc[i][k] = 0.f;
+  bool ok = true;
+  if (warp == 4) {
+    // ------------------------------------------------------------------ producer
+    if (lane == 0) {
+      int stage = 0; uint32_t phase = 1;
+      for (int y = begin; y < end && ok; y += kRowsTile)
+        for (int t = 0; t < 2 && ok; ++t) {                             // K, V
+          if (!(ok = mbar_wait(empty(stage), phase, abort_flag))) break;
+          mbar_arrive_expect_tx(full(stage), C::TILE_BYTES);
+          for (int pn = 0; pn < C::NP; ++pn)
+            tma_load_2d(base + stage * C::TILE_BYTES + pn * C::PANEL, t ? &tmV : &tmK, w.kv_head * D + pn * 64, w.kv_begin + y, full(stage));
+          if (++stage == C::STAGES) { stage = 0; phase ^= 1u; }
+        }
+    }
+  } else {
+    // ------------------------------------------------------------------ keys 16 * warp .. + 15 of every tile
+    int stage = 0; uint32_t phase = 0;
+    // row addresses of the ldmatrix loads: of K, matrices (keys 0-7 | 8-15) x (channels 0-7, 8-15 of a k step); of V, transposed,
+    // (channels 0-7 | 8-15 of a pair of output tiles) x (keys 0-7, 8-15)
+    const int k_row = 16 * warp + (lane >> 4) * 8 + (lane & 7), k_unit = (lane >> 3) & 1;
+    const int v_row = 16 * warp + ((lane >> 3) & 1) * 8 + (lane & 7), v_unit = lane >> 4;
+    for (int y = begin; y < end && ok; y += kRowsTile) {
+      const int key0 = y + 16 * warp;                                   // this warp's first key
+      if (!(ok = __all_sync(0xffffffffu, mbar_wait(full(stage), phase, abort_flag)))) break;
+      float s[2][4] = {};                                               // keys 0-7 and 8-15
+      {
+        const uint32_t kt = base + stage * C::TILE_BYTES + k_row * 128;
+#pragma unroll
+        for (int t = 0; t < D / 16; ++t) {
+          const int u = 2 * t + k_unit;
+          uint32_t kb[4];
+          ldmatrix_x4(kb, kt + (u >> 3) * C::PANEL + (((u & 7) ^ (k_row & 7)) << 4));
+          mma_16816<BF16>(s[0], qa[t], kb[0], kb[1]);
+          mma_16816<BF16>(s[1], qa[t], kb[2], kb[3]);
+        }
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(empty(stage));
+      if (++stage == C::STAGES) { stage = 0; phase ^= 1u; }
+      const bool ragged = key0 + 16 > first;                            // some row does not see all of the warp's keys
+      if (ragged) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            if (key0 + 8 * i + 2 * (lane & 3) + (k & 1) >= limit[k >> 1]) s[i][k] = -INFINITY;
+      }
+      uint32_t pa[4];
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {                                     // rows lane / 4 + 8 r
+        float mx = fmaxf(fmaxf(s[0][2 * r], s[0][2 * r + 1]), fmaxf(s[1][2 * r], s[1][2 * r + 1]));
+        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+        // the reference is taken off before the scaling: the largest score's exponent is 0 however large the factor is
+        const float top = fmaxf(m[r], mx), at = top == -INFINITY ? 0.f : top;
+        const float alpha = exp2_approx((m[r] - at) * p.scale_log2);    // 0 while m is -inf
+        m[r] = top;
+        float e[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) e[k] = exp2_approx((s[k >> 1][2 * r + (k & 1)] - at) * p.scale_log2);
+        l[r] = l[r] * alpha + (e[0] + e[1]) + (e[2] + e[3]);
+        pa[r] = pack16x2<BF16>(e[0], e[1]);
+        pa[2 + r] = pack16x2<BF16>(e[2], e[3]);
+        if (__any_sync(0xffffffffu, alpha != 1.0f)) {
+#pragma unroll
+          for (int i = 0; i < D / 8; ++i) { acc[i][2 * r] *= alpha; acc[i][2 * r + 1] *= alpha; }
+        }
+      }
+      if (!(ok = __all_sync(0xffffffffu, mbar_wait(full(stage), phase, abort_flag)))) break;
+      if (ragged) {                            // V rows that no row sees are cleared, of the others what is no finite number
+        for (int i = lane; i < 16 * 8; i += 32) {
+          const int key = key0 + (i >> 3);
+          if (key < first) continue;
+          for (int pn = 0; pn < C::NP; ++pn) {
+            uint4* at = reinterpret_cast<uint4*>(aligned + stage * C::TILE_BYTES + pn * C::PANEL + (16 * warp * 8 + i) * 16);
+            uint4 v = make_uint4(0, 0, 0, 0);
+            if (key < most) {
+              bool unused = false;
+              v = *at;
+              v = make_uint4(finite_pair<BF16>(v.x, &unused), finite_pair<BF16>(v.y, &unused), finite_pair<BF16>(v.z, &unused), finite_pair<BF16>(v.w, &unused));
+            }
+            *at = v;
+          }
+        }
+        fence_proxy_async_smem();              // the stage is refilled by TMA
+        __syncwarp();
+      }
+      {
+        const uint32_t vt = base + stage * C::TILE_BYTES + v_row * 128;
+#pragma unroll
+        for (int t = 0; t < D / 16; ++t) {
+          const int u = 2 * t + v_unit;
+          uint32_t vb[4];
+          ldmatrix_x4_trans(vb, vt + (u >> 3) * C::PANEL + (((u & 7) ^ (v_row & 7)) << 4));
+          mma_16816<BF16>(acc[2 * t], pa, vb[0], vb[1]);
+          mma_16816<BF16>(acc[2 * t + 1], pa, vb[2], vb[3]);
+        }
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(empty(stage));
+      if (++stage == C::STAGES) { stage = 0; phase ^= 1u; }
+    }
+  }
+  __syncthreads();                             // every tile has been read: the partial results take the ring's place
+  settle_if_aborted(abort_flag);
+  if (warp < 4) {
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      l[r] += __shfl_xor_sync(0xffffffffu, l[r], 1);
+      l[r] += __shfl_xor_sync(0xffffffffu, l[r], 2);
+      const int row = (lane >> 2) + 8 * r;
+      if (row < rows) {
+        float* dst = part + (warp * kRowsMax + row) * C::PART;
+#pragma unroll
+        for (int i = 0; i < D / 8; ++i) *reinterpret_cast<float2*>(dst + i * 8 + (lane & 3) * 2) = make_float2(acc[i][2 * r], acc[i][2 * r + 1]);
+        if ((lane & 3) == 0) { dst[D] = m[r]; dst[D + 1] = l[r]; }
+      }
+    }
+  }
+  __syncthreads();
+  if (threadIdx.x < D) {
+    for (int row = 0; row < rows; ++row) {     // channel per thread: the warps' parts rescaled to their common maximum
+      float top = -INFINITY;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) top = fmaxf(top, part[(k * kRowsMax + row) * C::PART + D]);
+      const float at = top == -INFINITY ? 0.f : top;
+      float sum = 0.f, o = 0.f;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float* from = part + (k * kRowsMax + row) * C::PART;
+        const float f = exp2_approx((from[D] - at) * p.scale_log2);
+        sum += from[D + 1] * f;
+        o += from[threadIdx.x] * f;
+      }
+      if (w.parts == 1) {
+        prompt_store<BF16>(p, w, w.row0 + row, threadIdx.x, D, sum == 0.f ? 0.f : o / sum, first);
+      } else {
+        float* to = p.parts + (static_cast<long long>(blockIdx.x) * kRowsMax + row) * C::PART;
+        to[threadIdx.x] = o;
+        if (threadIdx.x == 0) { to[D] = top; to[D + 1] = sum; }
+      }
+    }
+  }
+  if (threadIdx.x == 0 && *abort_flag) atomicMax(p.status, kStatusAttnTimeout);
+}
+
+// One CTA per (row tile with several parts, row): the parts' results rescaled to their common maximum, in order.
+// Grid: (CTAs of the few-row kernel that hold a first part) x 16; the others leave at once.
+template <int D, bool BF16>
+__global__ void __launch_bounds__(D)
+prompt_join_kernel(const PromptAttnParams p, const __grid_constant__ PromptBatch batch) {
+  constexpr int PART = PromptRowsCfg<D>::PART;
+  asm volatile("griddepcontrol.wait;" ::: "memory");                    // the parts are complete
+  // row tiles are counted request by request, key head by key head
+  int tile = blockIdx.x, cta = 0;
+  PromptPart w{};
+  for (int i = 0; i < batch.n; ++i) {
+    w.req = batch.order[i];
+    w.q_begin = batch.cu_q[w.req]; w.q_len = batch.cu_q[w.req + 1] - w.q_begin;
+    w.kv_begin = batch.cu_kv[w.req]; w.kv_len = batch.cu_kv[w.req + 1] - w.kv_begin;
+    w.parts = prompt_parts(w.kv_len, p.chunk);
+    const int tiles = prompt_row_tiles(w.q_len, p.group), here = tiles * p.kv_heads;
+    if (tile < here) {
+      w.row0 = tile % tiles * kRowsMax;
+      w.kv_head = tile / tiles;
+      cta += tile * w.parts;
+      break;
+    }
+    tile -= here;
+    cta += here * w.parts;
+  }
+  w.before = w.kv_len - w.q_len;
+  const int row = blockIdx.y;
+  if (w.parts == 1 || row >= w.q_len * p.group - w.row0) return;
+  const float* from = p.parts + (static_cast<long long>(cta) * kRowsMax + row) * PART;
+  constexpr long long kStep = static_cast<long long>(kRowsMax) * PART;
+  float top = -INFINITY;
+  for (int k = 0; k < w.parts; ++k) top = fmaxf(top, from[k * kStep + D]);
+  const float at = top == -INFINITY ? 0.f : top;
+  float sum = 0.f, o = 0.f;
+#pragma unroll 4
+  for (int k = 0; k < w.parts; ++k) {
+    const float f = exp2_approx((from[k * kStep + D] - at) * p.scale_log2);
+    sum += from[k * kStep + D + 1] * f;
+    o += from[k * kStep + threadIdx.x] * f;
+  }
+  prompt_store<BF16>(p, w, w.row0 + row, threadIdx.x, D, sum == 0.f ? 0.f : o / sum, prompt_limit(w, p, w.row0 / p.group));
+}
+
+}  // namespace dit
