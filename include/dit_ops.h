@@ -228,8 +228,8 @@ dit_status dit_rotary(const dit_rotary_args *args, void *stream);
  * one all of whose scores are -infinity.  Keys and values that a row does not see are never part of its result, whatever they hold.
  * Scores, their differences, the softmax and the sums are held in fp32, probabilities are rounded to the inputs' type for the second product;
  * scores of any size and infinite or NaN values are treated as dit_block_attention treats them.  A request's results do not depend on the
- * values of the others; those of one with few rows (q_len * n_heads / n_kv_heads <= DIT_PROMPT_FEW_ROWS) are summed in parts that depend on
- * the lengths of the whole batch, and may differ in their last bits with the batch that it comes in.
+ * values of the others; where few rows (q_len * n_heads / n_kv_heads <= 512) read more than 256 keys, the keys may be summed in parts that
+ * depend on the lengths of the whole batch, so that results may differ in their last bits with the batch that a request comes in.
  *   q, k, v, out  device, type f16 or bf16, 16-byte aligned, leading dimensions multiples of 8 and >= n_heads * head_dim (q, out) or
  *                 n_kv_heads * head_dim (k, v); column ranges of one packed buffer are fine; out must not overlap the inputs
  *   head_dim      64 or 128 (DIT_ERR_SHAPE); n_kv_heads divides n_heads; n_requests <= DIT_MAX_REQUESTS; sums of lengths < 2^31 - 1024
@@ -237,7 +237,6 @@ dit_status dit_rotary(const dit_rotary_args *args, void *stream);
  *   workspace     device, 16-byte aligned, dit_prompt_attention_workspace(args) bytes (sizes only are read; may be 0, then NULL is fine); its
  *                 contents need not be kept between calls, and calls that may run at the same time need workspaces of their own
  * A request may have no rows of q, or none of k. */
-#define DIT_PROMPT_FEW_ROWS 64
 typedef struct {
   const void *q, *k, *v;
   void *out;

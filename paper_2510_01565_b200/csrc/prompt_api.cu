@@ -64,11 +64,12 @@ bool half_map(const OpsDevice& d, CUtensorMap* m, const void* ptr, uint64_t cols
 struct PromptPlan {
   PromptBatch tiled, few;
   int64_t items;             // of the tiled kernel
+  int most_blocks;
   int64_t row_tiles, ctas;   // of the few-row kernel
   int chunk;
   bool join;                 // some request has several parts
 };
-constexpr int kFewRowCtas = 296;                 // two on each of 148 SMs
+constexpr int kFewRowCtas = 148;                 // one for each SM
 
 int64_t few_row_ctas(const PromptPlan& p, const dit_prompt_attention_args& a, int chunk) {
   int64_t n = 0;
@@ -77,6 +78,22 @@ int64_t few_row_ctas(const PromptPlan& p, const dit_prompt_attention_args& a, in
     n += static_cast<int64_t>(a.n_kv_heads) * prompt_row_tiles(a.q_lens[r], a.n_heads / a.n_kv_heads) * prompt_parts(a.kv_lens[r], chunk);
   }
   return n;
+}
+
+// Whether a request goes to the few-row kernel.  Decided by its own sizes, so that packing does not change a request's kernel.  That kernel reads the
+// keys once for every 16 rows, from L2 behind the first time, at 7 TB/s; the tiled one needs
+// 1.8 us for a key block of a pair of tiles and 2.6 us per pair, and leaves SMs idle where there are few pairs.  17 rows of 32 heads over 8 key heads
+// against 8192 keys, us: tiled 98, few rows 23; 64 rows of 32 heads over as many: 84 and 77.  A request that takes
+// more than twice the device's time that way stays with the tiled kernel, since others beside it would pay for that.
+bool few_rows(int64_t q_len, int64_t kv_len, int64_t group, int64_t kv_heads, int64_t head_dim, bool causal) {
+  const int64_t rows = q_len * group;
+  if (rows <= kRowsMax) return true;
+  if (rows > 512) return false;
+  const double few = static_cast<double>((rows + kRowsMax - 1) / kRowsMax) * kv_heads * kv_len * head_dim * 4 * 1e-6 / 7.0;          // us
+  const double pairs = static_cast<double>(((q_len + 127) / 128 * group + 1) / 2 * kv_heads);
+  const double keys = causal ? std::max<double>(0.0, kv_len - 0.5 * q_len) : static_cast<double>(kv_len);
+  const double each = 2.6 + 1.8 * std::ceil(keys / 128);
+  return few + 2.0 < std::ceil(pairs / 148) * each && few < 2.0 * pairs * each / 148;
 }
 
 // Checks sizes and lays the batch out.
@@ -97,11 +114,12 @@ dit_status plan_prompts(const dit_prompt_attention_args& a, PromptPlan* p) {
     q += a.q_lens[r]; kv += a.kv_lens[r];
     if (q > kMaxSize || kv > kMaxSize) return DIT_ERR_SHAPE;
     if (a.q_lens[r] == 0) continue;
-    PromptBatch& b = a.q_lens[r] * group <= DIT_PROMPT_FEW_ROWS ? p->few : p->tiled;
+    PromptBatch& b = few_rows(a.q_lens[r], a.kv_lens[r], group, a.n_kv_heads, a.head_dim, a.causal != 0) ? p->few : p->tiled;
     int at = b.n++;
     for (; at > 0 && a.kv_lens[b.order[at - 1]] < a.kv_lens[r]; --at) b.order[at] = b.order[at - 1];      // most keys first
     b.order[at] = r;
     if (&b == &p->tiled) {
+      p->most_blocks = std::max(p->most_blocks, (a.kv_lens[r] + 127) / 128);
       p->items += ((((static_cast<int64_t>(a.q_lens[r]) + 127) / 128) * group + 1) / 2) * a.n_kv_heads;
     } else {
       const int64_t tiles = static_cast<int64_t>(a.n_kv_heads) * prompt_row_tiles(a.q_lens[r], static_cast<int>(group));
@@ -111,14 +129,12 @@ dit_status plan_prompts(const dit_prompt_attention_args& a, PromptPlan* p) {
   }
   if (p->items > INT32_MAX / 16) return DIT_ERR_SHAPE;
   if (p->few.n > 0) {
-    // Parts of equal length, as short as lets all of them run at once; where that would leave parts of more than 2048 keys the batch takes
-    // several waves anyway, and parts of 1024 keep them even.
+    // Parts of equal length, one for each SM: what a CTA costs before its first product and after its last one is several us, and one per SM
+    // keeps enough loads in flight (one row of 32 heads against 32768 keys, parts of 256, 896, 1792 keys: 60, 34, 29 us).  Beyond 4096 keys
+    // a part is only cut off: more CTAs than SMs are resident at once, and share the memory's bandwidth evenly.
     int64_t chunk = std::max<int64_t>(256, (keys / kFewRowCtas + 63) / 64 * 64);
-    if (chunk <= 2048) {
-      for (const int64_t least = chunk; few_row_ctas(*p, a, static_cast<int>(chunk)) > kFewRowCtas && chunk < 2 * least;) chunk += std::max<int64_t>(64, least / 16 / 64 * 64);
-    } else {
-      chunk = 1024;
-    }
+    for (const int64_t least = chunk; few_row_ctas(*p, a, static_cast<int>(chunk)) > kFewRowCtas && chunk < 2 * least;) chunk += std::max<int64_t>(64, least / 16 / 64 * 64);
+    chunk = std::min<int64_t>(chunk, 4096);
     p->chunk = static_cast<int>(chunk);
     p->ctas = few_row_ctas(*p, a, p->chunk);
     if (p->ctas > INT32_MAX / 16) return DIT_ERR_SHAPE;
@@ -126,7 +142,7 @@ dit_status plan_prompts(const dit_prompt_attention_args& a, PromptPlan* p) {
   }
   return DIT_OK;
 }
-size_t part_bytes(const PromptPlan& p, int head_dim) { return p.join ? static_cast<size_t>(p.ctas) * kRowsMax * (head_dim + 2) * sizeof(float) : 0; }
+size_t part_bytes(const PromptPlan& p, int head_dim) { return p.join ? static_cast<size_t>(p.ctas) * kRowsMax * (head_dim + 4) * sizeof(float) : 0; }
 
 template <int D, bool BF16>
 cudaError_t launch_attention(const OpsDevice& d, const dit_prompt_attention_args& a, const PromptPlan& plan, PromptAttnParams p, cudaStream_t st) {
@@ -142,7 +158,7 @@ cudaError_t launch_attention(const OpsDevice& d, const dit_prompt_attention_args
     if (!half_map(d, &tmQ, a.q, width, q_rows, a.ld_q, 128) || !half_map(d, &tmK, k, kv_width, std::max(kv_rows, 1), ld_k, 128) ||
         !half_map(d, &tmV, v, kv_width, std::max(kv_rows, 1), ld_v, 128))
       return cudaErrorInvalidValue;
-    p.items = static_cast<int>(plan.items);
+    p.items = static_cast<int>(plan.items); p.most_blocks = plan.most_blocks;
     prompt_attention_kernel<D, BF16><<<std::min(p.items, d.num_sms), PromptAttnCfg<D>::THREADS, PromptAttnCfg<D>::SMEM_BYTES, st>>>(tmQ, tmK, tmV, p, plan.tiled);
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
   }
@@ -151,14 +167,17 @@ cudaError_t launch_attention(const OpsDevice& d, const dit_prompt_attention_args
       return cudaErrorInvalidValue;
     p.chunk = plan.chunk;
     p.parts = static_cast<float*>(a.workspace);
-    prompt_rows_kernel<D, BF16><<<static_cast<unsigned>(plan.ctas), PromptRowsCfg<D>::THREADS, PromptRowsCfg<D>::SMEM_BYTES, st>>>(tmK, tmV, p, plan.few);
-    if ((e = cudaGetLastError()) != cudaSuccess) return e;
+    cudaLaunchAttribute at;
+    at.id = cudaLaunchAttributeProgrammaticStreamSerialization;                 // beside the tiled kernel; set up while the parts are being computed
+    at.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t lc = {};
+    lc.gridDim = dim3(static_cast<unsigned>(plan.ctas)); lc.blockDim = dim3(PromptRowsCfg<D>::THREADS);
+    lc.dynamicSmemBytes = PromptRowsCfg<D>::SMEM_BYTES; lc.stream = st;
+    lc.attrs = &at; lc.numAttrs = plan.items > 0 ? 1 : 0;
+    if ((e = cudaLaunchKernelEx(&lc, &prompt_rows_kernel<D, BF16>, tmK, tmV, p, plan.few)) != cudaSuccess) return e;
     if (plan.join) {
-      cudaLaunchConfig_t lc = {};
-      lc.gridDim = dim3(static_cast<unsigned>(plan.row_tiles), kRowsMax); lc.blockDim = dim3(D); lc.stream = st;
-      cudaLaunchAttribute at;
-      at.id = cudaLaunchAttributeProgrammaticStreamSerialization;               // set up while the parts are still being computed
-      at.val.programmaticStreamSerializationAllowed = 1;
+      lc = cudaLaunchConfig_t{};
+      lc.gridDim = dim3(static_cast<unsigned>(plan.row_tiles), kRowsMax / kJoinRows); lc.blockDim = dim3(kJoinRows * 32); lc.stream = st;
       lc.attrs = &at; lc.numAttrs = 1;
       if ((e = cudaLaunchKernelEx(&lc, &prompt_join_kernel<D, BF16>, p, plan.few)) != cudaSuccess) return e;
     }

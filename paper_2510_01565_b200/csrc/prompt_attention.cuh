@@ -29,11 +29,12 @@ struct PromptAttnParams {
   int causal;
   float scale_log2;          // scale * log2(e), positive
   int items;                 // tiled kernel: (request, key head, pair of query tiles)
+  int most_blocks;           // key blocks of the longest of its requests
   int wide_out;              // rows of out start on 32-byte boundaries
   int* status;
   // few rows
   int chunk;                 // keys per CTA, a multiple of 64
-  float* parts;              // [CTAs][16][head_dim + 2]
+  float* parts;              // [CTAs][16][head_dim + 4]
 };
 
 // The 16-bit value's exponent is all ones: an infinity or NaN.
@@ -57,7 +58,8 @@ struct PromptAttnCfg {
   static constexpr int K_STAGES = 3, V_STAGES = 2;
   static constexpr int OFF_Q = 0, OFF_K = 2 * TILE_BYTES, OFF_V = OFF_K + K_STAGES * TILE_BYTES;
   static constexpr int OFF_BAR = OFF_V + V_STAGES * TILE_BYTES;
-  static constexpr int SMEM_USED = OFF_BAR + 256 + 1024;
+  static constexpr int OFF_ITEM = OFF_BAR + 256;                                  // PromptItem [2]
+  static constexpr int SMEM_USED = OFF_ITEM + 2 * 64 + 1024;
   // one CTA per SM: each takes all of tensor memory
   static constexpr int SMEM_BYTES = SMEM_USED > 116 * 1024 ? SMEM_USED : 116 * 1024;
   static constexpr int THREADS = 384;
@@ -67,35 +69,71 @@ struct PromptAttnCfg {
 // Two query tiles: consecutive ones of the list (last 128-row block first, the heads of the group one after the other) of a request and a key
 // head.  With an even group they are two heads' tiles of the same rows; otherwise also neighbouring row blocks.
 struct PromptItem {
-  int kv_head, req, q_begin, q_len, kv_begin, kv_len;
-  int before;                // keys before the first query row's own (may be negative), or all of them where nothing is masked
+  int kv_head, q_begin, q_len, kv_begin, kv_len;
+  int before;                // keys before the first query row's own (may be negative)
   int head[2], qb[2];
   int n_kv[2];               // key blocks that a tile's last row sees; n_kv[0] >= n_kv[1]
   int ragged;                // first key block of which some row of a tile sees only a part
-  bool tile1;
+  int tile1;
   __device__ __forceinline__ int limit(int row, int causal) const { return causal ? min(kv_len, before + row + 1) : kv_len; }   // keys of a row
 };
-__device__ __forceinline__ PromptItem prompt_item(const PromptBatch& batch, const PromptAttnParams& p, int item) {
-  PromptItem it{};
-  int tiles = 0, pair = 0;
-  for (int i = 0; i < batch.n; ++i) {
-    it.req = batch.order[i];
-    tiles = ((batch.cu_q[it.req + 1] - batch.cu_q[it.req] + 127) >> 7) * p.group;
-    const int here = ((tiles + 1) >> 1) * p.kv_heads;
-    if (item < here) { pair = item / p.kv_heads; it.kv_head = item - pair * p.kv_heads; break; }
-    item -= here;
+// Pairs of tiles of a request whose first tile sees `blocks` key blocks or more (they are the request's first ones).
+__device__ __forceinline__ int pairs_with(const PromptBatch& batch, int group, int causal, int i, int blocks) {
+  if (i >= batch.n) return 0;
+  const int r = batch.order[i], q_len = batch.cu_q[r + 1] - batch.cu_q[r], kv_len = batch.cu_kv[r + 1] - batch.cu_kv[r];
+  const int nb = (q_len + 127) >> 7;
+  int from = 0;                                // first row block that qualifies
+  if (blocks > 0) {
+    if (blocks > (kv_len + 127) >> 7) return 0;
+    if (causal) from = max(0, ((128 * (blocks - 1) + 1 - (kv_len - q_len) + 127) >> 7) - 1);
   }
-  it.q_begin = batch.cu_q[it.req]; it.q_len = batch.cu_q[it.req + 1] - it.q_begin;
-  it.kv_begin = batch.cu_kv[it.req]; it.kv_len = batch.cu_kv[it.req + 1] - it.kv_begin;
-  it.before = it.kv_len - it.q_len;
-  it.tile1 = 2 * pair + 1 < tiles;
-  const int last_block = ((it.q_len + 127) >> 7) - 1;
+  return ((nb - from) * group + 1) >> 1;
+}
+// The item-th item of the batch, most key blocks first, whatever request they belong to; the whole warp looks for it.
+__device__ __forceinline__ PromptItem prompt_item(const PromptBatch& batch, const PromptAttnParams& p, int item, int lane) {
+  auto count = [&](int half, int blocks) { return pairs_with(batch, p.group, p.causal, lane + 32 * half, blocks); };
+  auto all = [&](int blocks) {
+    const unsigned mine = static_cast<unsigned>(count(0, blocks) + (batch.n > 32 ? count(1, blocks) : 0));
+    return static_cast<int>(__reduce_add_sync(0xffffffffu, mine)) * p.kv_heads;
+  };
+  int low = 0, high = p.most_blocks + 1, behind = 0;              // more than `item` items have `low` blocks or more; `behind` of them `high`
+  while (high - low > 1) {
+    const int mid = (low + high) >> 1, n = all(mid);
+    if (n > item) low = mid; else { high = mid; behind = n; }
+  }
+  int rank = item - behind, i = 0, pair = 0, kv_head = 0;         // among the items with exactly `low` blocks
+  for (int half = 0; half < 2; ++half) {
+    const int first = count(half, high), mine = (count(half, low) - first) * p.kv_heads;
+    int sum = mine;
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int t = min(2 * pair + i, tiles - 1), back = t / p.group;
-    it.qb[i] = last_block - back;
-    it.head[i] = it.kv_head * p.group + t - back * p.group;
-    it.n_kv[i] = (max(0, it.limit(min(it.q_len, it.qb[i] * 128 + 128) - 1, p.causal)) + 127) >> 7;
+    for (int o = 1; o < 32; o <<= 1) {
+      const int up = __shfl_up_sync(0xffffffffu, sum, o);
+      if (lane >= o) sum += up;
+    }
+    const unsigned past = __ballot_sync(0xffffffffu, sum > rank);
+    if (past) {
+      const int at = __ffs(past) - 1, within = rank - __shfl_sync(0xffffffffu, sum - mine, at);
+      i = at + 32 * half;
+      pair = __shfl_sync(0xffffffffu, first, at) + within / p.kv_heads;
+      kv_head = within % p.kv_heads;
+      break;
+    }
+    rank -= __shfl_sync(0xffffffffu, sum, 31);
+  }
+  PromptItem it{};
+  const int r = batch.order[i];
+  it.kv_head = kv_head;
+  it.q_begin = batch.cu_q[r]; it.q_len = batch.cu_q[r + 1] - it.q_begin;
+  it.kv_begin = batch.cu_kv[r]; it.kv_len = batch.cu_kv[r + 1] - it.kv_begin;
+  it.before = it.kv_len - it.q_len;
+  const int row_blocks = (it.q_len + 127) >> 7, tiles = row_blocks * p.group;
+  it.tile1 = 2 * pair + 1 < tiles;
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    const int tile = min(2 * pair + t, tiles - 1), back = tile / p.group;
+    it.qb[t] = row_blocks - 1 - back;
+    it.head[t] = kv_head * p.group + tile - back * p.group;
+    it.n_kv[t] = (max(0, it.limit(min(it.q_len, it.qb[t] * 128 + 128) - 1, p.causal)) + 127) >> 7;
   }
   if (!it.tile1) it.n_kv[1] = 0;
   it.ragged = p.causal ? max(0, it.limit((it.tile1 ? it.qb[1] : it.qb[0]) * 128, 1)) >> 7 : it.n_kv[0];
@@ -105,7 +143,8 @@ __device__ __forceinline__ PromptItem prompt_item(const PromptBatch& batch, cons
 // The scheme of the list kernel (block_attention_kernel: two 128-row query tiles with a softmax warpgroup each, one S buffer handed between
 // them, P in tensor memory, O rescaled rarely, persistent grid whose roles run on from item to item) over the key blocks 0 .. n - 1 of a
 // request.  Sharing a key head is what makes a pair: a key block is loaded once and used by both tiles.
-// Items are ordered by their cost and dealt out forwards and backwards in turn, so that CTAs come out even.
+// Items are ordered by their cost over the whole batch and dealt out forwards and backwards in turn, so that CTAs come out even (four requests of
+// 2048 rows one after the other: 159 us, ordered: 131).  A warp of its own finds them ahead and hands them to the others through shared memory.
 // A causal tile masks its last block or two.  Scores that a row does not see are dropped before its maximum.  Values that it does not
 // see meet a probability of zero, which an infinity or NaN would turn into NaN: in the blocks that some rows see only in part such values are
 // replaced by zeros in shared memory, and if there was one, the rows that do see it add it to their results at the end.
@@ -127,16 +166,20 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
   auto s_full = [&](int i) { return bar0 + 8u * (13 + i); };
   auto p_full = [&](int i) { return bar0 + 8u * (15 + i); };
   auto o_full = [&](int i) { return bar0 + 8u * (17 + i); };
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(aligned + C::OFF_BAR + 8 * 19);
+  auto item_full = [&](int b) { return bar0 + 8u * (19 + b); };
+  auto item_empty = [&](int b) { return bar0 + 8u * (21 + b); };
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(aligned + C::OFF_BAR + 8 * 23);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   volatile int* odd_values = reinterpret_cast<volatile int*>(tmem_slot + 2);      // [2]: a tile's item met values that were replaced
 
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");       // (the few-row kernel of the same call)
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     mbar_init(q_full, 1); mbar_init(q_empty, 1); mbar_init(s_free, 4);
     for (int s = 0; s < C::K_STAGES; ++s) { mbar_init(k_full(s), 1); mbar_init(k_empty(s), 1); }
     for (int s = 0; s < C::V_STAGES; ++s) { mbar_init(v_full(s), 1); mbar_init(v_empty(s), 1); }
     for (int i = 0; i < 2; ++i) { mbar_init(s_full(i), 1); mbar_init(p_full(i), 4); mbar_init(o_full(i), 1); }
+    for (int b = 0; b < 2; ++b) { mbar_init(item_full(b), 1); mbar_init(item_empty(b), 11); }     // producer, two issuers, eight softmax warps
     *abort_flag = 0;
     fence_mbar_init();
   }
@@ -150,6 +193,22 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
 
   // this CTA's k-th item: forwards and backwards in turn
   auto item_at = [&](int k) { return k * static_cast<int>(gridDim.x) + ((k & 1) ? static_cast<int>(gridDim.x - 1 - blockIdx.x) : static_cast<int>(blockIdx.x)); };
+  static_assert(sizeof(PromptItem) <= 64, "room of an item");
+  auto item_slot = [&](int k) { return reinterpret_cast<PromptItem*>(aligned + C::OFF_ITEM + (k & 1) * 64); };
+  // its description, copied; `one`: called by a single thread
+  auto take_item = [&](int k, PromptItem& it, bool one) {
+    if (one) {
+      if (!mbar_wait(item_full(k & 1), (k >> 1) & 1u, abort_flag)) return false;
+      it = *item_slot(k);
+      mbar_arrive(item_empty(k & 1));
+    } else {
+      if (!__all_sync(0xffffffffu, mbar_wait(item_full(k & 1), (k >> 1) & 1u, abort_flag))) return false;
+      it = *item_slot(k);
+      __syncwarp();
+      if (lane == 0) mbar_arrive(item_empty(k & 1));
+    }
+    return true;
+  };
 
   if (warp < 4) {
     DIT_SETMAXNREG_DEC(96);
@@ -157,8 +216,9 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
       if (lane == 0) {
         // ---------------------------------------------------------------- TMA producer
         int ks = 0, vs = 0; uint32_t kph = 1, vph = 1, qph = 1;
-        for (int k = 0, item; (item = item_at(k)) < p.items; ++k) {
-          const PromptItem it = prompt_item(batch, p, item);
+        PromptItem it;
+        for (int k = 0; item_at(k) < p.items; ++k) {
+          if (!take_item(k, it, true)) goto done;
           if (!mbar_wait(q_empty, qph, abort_flag)) goto done;
           qph ^= 1u;
           mbar_arrive_expect_tx(q_full, (it.tile1 ? 2 : 1) * C::TILE_BYTES);
@@ -188,8 +248,9 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
         const uint64_t qdesc0 = smem_desc_sw128(base + C::OFF_Q, 16, 1024), kdesc0 = smem_desc_sw128(base + C::OFF_K, 16, 1024);
         constexpr uint32_t kTileStep = C::TILE_BYTES >> 4;
         int ks = 0; uint32_t kph = 0, qph = 0, u = 0;                             // u: uses of S so far
-        for (int k = 0, item; (item = item_at(k)) < p.items; ++k) {
-          const PromptItem it = prompt_item(batch, p, item);
+        PromptItem it;
+        for (int k = 0; item_at(k) < p.items; ++k) {
+          if (!take_item(k, it, true)) goto done;
           if (!mbar_wait(q_full, qph, abort_flag)) goto done;
           qph ^= 1u;
           for (int j = 0; j < it.n_kv[0]; ++j) {
@@ -220,20 +281,25 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
       const uint64_t vdesc0 = smem_desc_sw128(base + C::OFF_V, C::PANEL, 1024);
       constexpr uint32_t kTileStep = C::TILE_BYTES >> 4;
       int vs = 0; uint32_t vph = 0, done_uses[2] = {0, 0};
-      for (int k = 0, item; (item = item_at(k)) < p.items; ++k) {
-        const PromptItem it = prompt_item(batch, p, item);
+      PromptItem it;
+      for (int k = 0; item_at(k) < p.items; ++k) {
+        if (!take_item(k, it, false)) goto done;
         bool odd = false;                                                         // values replaced in this item (warp-uniform)
-        for (int j = 0; j < it.n_kv[0]; ++j) {
-          const int tiles = j < it.n_kv[1] ? 2 : 1;
-          if (!__all_sync(0xffffffffu, mbar_wait(v_full(vs), vph, abort_flag))) goto done;
+        int checked = -1;                                                         // last key block that has been looked through
+        // Looks through the V tile of key block j in `stage`, which has arrived.
+        auto look_through = [&](int j, int stage) {
+          checked = j;
           const int valid = it.kv_len - j * 128;
-          uint8_t* tile = aligned + C::OFF_V + vs * C::TILE_BYTES;
+          if (valid >= 128 && j < it.ragged) return;
+          uint8_t* tile = aligned + C::OFF_V + stage * C::TILE_BYTES;
+          bool wrote = false;
           if (valid < 128) {
+            wrote = true;
             for (int r = valid * 8 + lane; r < 128 * 8; r += 32)                  // 16-byte units of rows valid .. 127
               for (int pn = 0; pn < C::NP; ++pn) *reinterpret_cast<uint4*>(tile + pn * C::PANEL + r * 16) = make_uint4(0, 0, 0, 0);
           }
           if (j >= it.ragged) {
-            constexpr uint32_t kExp = BF16 ? 0x7F807F80u : 0x7C007C00u;
+            constexpr uint32_t kExp = BF16 ? 0x7F80u : 0x7C00u;
             const int units = min(128, valid) * 8;
             uint32_t most = 0;                                                    // largest magnitudes of the odd and the even columns
             for (int pn = 0; pn < C::NP; ++pn)
@@ -242,8 +308,8 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
                 const uint4 w = *reinterpret_cast<const uint4*>(tile + pn * C::PANEL + r * 16);
                 most = __vmaxu2(__vmaxu2(__vmaxu2(most, w.x & 0x7FFF7FFFu), __vmaxu2(w.y & 0x7FFF7FFFu, w.z & 0x7FFF7FFFu)), w.w & 0x7FFF7FFFu);
               }
-            if (__any_sync(0xffffffffu, (most & 0xFFFFu) >= (kExp & 0xFFFFu) || (most >> 16) >= (kExp >> 16))) {
-              odd = true;
+            if (__any_sync(0xffffffffu, (most & 0xFFFFu) >= kExp || (most >> 16) >= kExp)) {
+              odd = wrote = true;
               bool unused = false;
               for (int pn = 0; pn < C::NP; ++pn)
                 for (int r = lane; r < units; r += 32) {
@@ -253,9 +319,17 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
                 }
             }
           }
-          if (valid < 128 || odd) {
+          if (wrote) {
             fence_proxy_async_smem();
             __syncwarp();
+          }
+        };
+        for (int j = 0; j < it.n_kv[0]; ++j) {
+          const int tiles = j < it.n_kv[1] ? 2 : 1;
+          const int next = vs + 1 == C::V_STAGES ? 0 : vs + 1;
+          if (checked != j) {
+            if (!__all_sync(0xffffffffu, mbar_wait(v_full(vs), vph, abort_flag))) goto done;
+            look_through(j, vs);
           }
           const uint64_t vd = vdesc0 + vs * kTileStep;
           for (int i = 0; i < tiles; ++i) {
@@ -273,9 +347,23 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
             }
             __syncwarp();
             ++done_uses[i];
+            // the next block, while the other tile's P is still being made (looking through it in its own turn cost 3 % of long prompts)
+            if (i == 0 && tiles == 2 && j + 1 < it.n_kv[0] && __all_sync(0xffffffffu, mbar_test_wait(v_full(next), vph ^ (next == 0 ? 1u : 0u)))) look_through(j + 1, next);
           }
-          if (++vs == C::V_STAGES) { vs = 0; vph ^= 1u; }
+          vs = next;
+          if (vs == 0) vph ^= 1u;
         }
+      }
+    } else {
+      // ------------------------------------------------------------------ the coming items
+      for (int k = 0; item_at(k) < p.items; ++k) {
+        const PromptItem it = prompt_item(batch, p, item_at(k), lane);
+        if (!__all_sync(0xffffffffu, mbar_wait(item_empty(k & 1), ((k >> 1) & 1u) ^ 1u, abort_flag))) goto done;
+        if (lane == 0) {
+          *item_slot(k) = it;
+          mbar_arrive(item_full(k & 1));
+        }
+        __syncwarp();
       }
     }
   } else {
@@ -290,8 +378,9 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
     constexpr float kFarLog2 = 1024.0f;        // scaled references beyond it are taken off before the scaling
     uint32_t use = 0;                          // key blocks of this warpgroup so far
 
-    for (int k = 0, item; (item = item_at(k)) < p.items; ++k) {
-      const PromptItem it = prompt_item(batch, p, item);
+    PromptItem it;
+    for (int k = 0; item_at(k) < p.items; ++k) {
+      if (!take_item(k, it, false)) goto done;
       const int qb = tile == 0 ? it.qb[0] : it.qb[1], head = tile == 0 ? it.head[0] : it.head[1], n_kv = tile == 0 ? it.n_kv[0] : it.n_kv[1];
       const int row = qb * 128 + quarter * 32 + lane;                             // in the request
       const int limit = it.limit(row, p.causal);
@@ -458,10 +547,13 @@ done:
 // ------------------------------------------------------------------------------------------------
 // Few rows.  The query rows of a request and the heads of a group make rows of one product with the group's keys (row i * group + h), 16 to
 // a CTA, so that a new token's heads read the keys once.  Reading the stored keys and values is the bound: a CTA takes p.chunk of them,
-// chosen so that one wave of two CTAs per SM covers the batch, however uneven its requests are.  Inside it is block_rows_kernel: K and V by TMA in
+// chosen so that one CTA per SM covers the batch, however uneven its requests are.  Inside it is block_rows_kernel: K and V by TMA in
 // tiles of 64 keys through one ring, four warps with 16 keys of every tile each, warp-level products, the warps' results joined in
 // shared memory.  A request with one chunk writes its rows; the parts of the others go to memory as (sums, maximum, sum of
 // probabilities) and prompt_join_kernel joins them in their order.
+// 32 heads of 128 over 8 key heads, us: one row against 32768 keys (134 MB) 28, of which 3 are the joining; 64 rows of 64 requests against 4096 keys
+// each (1.07 GB) 153 = 7.0 TB/s, part of it from L2.  Heads of 64 take half the bytes and nearly the same time per key (23 us): a tile's waits and
+// dependent steps, not its bytes, are the bound there.
 // ------------------------------------------------------------------------------------------------
 template <int D>
 struct PromptRowsCfg {
@@ -470,7 +562,7 @@ struct PromptRowsCfg {
   static constexpr int OFF_BAR = STAGES * TILE_BYTES;
   static constexpr int SMEM_BYTES = OFF_BAR + 256 + 1024;
   static constexpr int THREADS = 160;                                            // four key warps and a producer
-  static constexpr int PART = D + 2;                                             // floats of a row's partial result: channels, maximum, sum
+  static constexpr int PART = D + 4;                                             // floats of a row's partial result: channels, maximum, sum, values replaced
   static_assert(4 * kRowsMax * PART * 4 <= OFF_BAR, "the partial results take the ring's place");
   static_assert(2 * SMEM_BYTES <= 227 * 1024, "two CTAs per SM");
 };
@@ -506,15 +598,23 @@ __device__ __forceinline__ PromptPart prompt_part(const PromptBatch& batch, cons
 __device__ __forceinline__ int prompt_limit(const PromptPart& w, const PromptAttnParams& p, int i) {
   return p.causal ? max(0, min(w.kv_len, w.before + i + 1)) : w.kv_len;
 }
-// A finished result of a row: replaced values that it sees (keys first .. limit - 1) are added.
+// Four finished channels of a row; odd: some values were replaced, and those that the row sees (keys first .. limit - 1) are added.
 template <bool BF16>
-__device__ __forceinline__ void prompt_store(const PromptAttnParams& p, const PromptPart& w, int row, int channel, int d, float x, int first) {
-  const int i = row / p.group, head = w.kv_head * p.group + row - i * p.group, limit = prompt_limit(w, p, i);
-  const uint16_t* v = p.v + (static_cast<long long>(w.kv_begin) + first) * p.ld_v + w.kv_head * d + channel;
-  for (int key = first; key < limit; ++key, v += p.ld_v)
-    if (odd_bits<BF16>(__ldg(v))) x += widen16bit<BF16>(__ldg(v));
-  static_cast<uint16_t*>(p.out)[(static_cast<long long>(w.q_begin) + i) * p.ld_out + head * d + channel] =
-      fabsf(x) == INFINITY ? static_cast<uint16_t>(infinity_bits<BF16>(x)) : pack16<BF16>(x);
+__device__ __forceinline__ void prompt_store(const PromptAttnParams& p, const PromptPart& w, int row, int channel, int d, float4 o, int first, bool odd) {
+  const int i = row / p.group, head = w.kv_head * p.group + row - i * p.group;
+  float x[4] = {o.x, o.y, o.z, o.w};
+  if (odd) {
+    const int limit = prompt_limit(w, p, i);
+    const uint16_t* v = p.v + (static_cast<long long>(w.kv_begin) + first) * p.ld_v + w.kv_head * d + channel;
+    for (int key = first; key < limit; ++key, v += p.ld_v)
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+        if (odd_bits<BF16>(__ldg(v + c))) x[c] += widen16bit<BF16>(__ldg(v + c));
+  }
+  uint2 r = make_uint2(pack16x2<BF16>(x[0], x[1]), pack16x2<BF16>(x[2], x[3]));
+  r.x = put_infinities<BF16>(r.x, x[0], x[1]);
+  r.y = put_infinities<BF16>(r.y, x[2], x[3]);
+  *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.out) + (static_cast<long long>(w.q_begin) + i) * p.ld_out + head * d + channel) = r;
 }
 
 template <int D, bool BF16>
@@ -530,6 +630,7 @@ prompt_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
   auto full = [&](int s) { return bar0 + 8u * s; };
   auto empty = [&](int s) { return bar0 + 8u * (C::STAGES + s); };
   volatile int* abort_flag = reinterpret_cast<volatile int*>(aligned + C::OFF_BAR + 16 * C::STAGES);
+  volatile int* odd_values = abort_flag + 1;                            // a value was replaced
   float* part = reinterpret_cast<float*>(aligned);                      // [4 warps][kRowsMax][PART], after the main loop
 
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");       // (the joining kernel waits for this one's end itself)
@@ -540,11 +641,18 @@ prompt_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
   const int most = prompt_limit(w, p, (w.row0 + rows - 1) / p.group);   // keys that the last one sees
   const int begin = w.part * p.chunk, end = min(most, begin + p.chunk); // of this CTA (begin may be >= end)
 
-  if (threadIdx.x == 0) {
+  // The producer's thread sets the barriers up and requests the first tiles before the CTA meets.
+  auto load = [&](int n, int stage) {          // tile n: K, V, K, V, ... of the keys from `begin` on
+    mbar_arrive_expect_tx(full(stage), C::TILE_BYTES);
+    for (int pn = 0; pn < C::NP; ++pn)
+      tma_load_2d(base + stage * C::TILE_BYTES + pn * C::PANEL, (n & 1) ? &tmV : &tmK, w.kv_head * D + pn * 64, w.kv_begin + begin + (n >> 1) * kRowsTile, full(stage));
+  };
+  const int tiles = end > begin ? 2 * ((end - begin + kRowsTile - 1) / kRowsTile) : 0;
+  if (threadIdx.x == 128) {
     for (int s = 0; s < C::STAGES; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 4); }
-    *abort_flag = 0;
+    *abort_flag = 0; *odd_values = 0;
     fence_mbar_init();
-    prefetch_tmap(&tmK); prefetch_tmap(&tmV);
+    for (int n = 0; n < min(tiles, C::STAGES); ++n) load(n, n);
   }
   // Q as the first operand: k step t, rows lane / 4 and + 8, channels 16 t + 2 (lane % 4) and + 8; absent rows are zero
   uint32_t qa[D / 16][4];
@@ -575,15 +683,12 @@ prompt_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
   if (warp == 4) {
     // ------------------------------------------------------------------ producer
     if (lane == 0) {
-      int stage = 0; uint32_t phase = 1;
-      for (int y = begin; y < end && ok; y += kRowsTile)
-        for (int t = 0; t < 2 && ok; ++t) {                             // K, V
-          if (!(ok = mbar_wait(empty(stage), phase, abort_flag))) break;
-          mbar_arrive_expect_tx(full(stage), C::TILE_BYTES);
-          for (int pn = 0; pn < C::NP; ++pn)
-            tma_load_2d(base + stage * C::TILE_BYTES + pn * C::PANEL, t ? &tmV : &tmK, w.kv_head * D + pn * 64, w.kv_begin + y, full(stage));
-          if (++stage == C::STAGES) { stage = 0; phase ^= 1u; }
-        }
+      int stage = 0; uint32_t phase = 0;
+      for (int n = C::STAGES; n < tiles && ok; ++n) {
+        if (!(ok = mbar_wait(empty(stage), phase, abort_flag))) break;
+        load(n, stage);
+        if (++stage == C::STAGES) { stage = 0; phase ^= 1u; }
+      }
     }
   } else {
     // ------------------------------------------------------------------ keys 16 * warp .. + 15 of every tile
@@ -641,6 +746,7 @@ prompt_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
       }
       if (!(ok = __all_sync(0xffffffffu, mbar_wait(full(stage), phase, abort_flag)))) break;
       if (ragged) {                            // V rows that no row sees are cleared, of the others what is no finite number
+        bool odd = false;
         for (int i = lane; i < 16 * 8; i += 32) {
           const int key = key0 + (i >> 3);
           if (key < first) continue;
@@ -648,13 +754,13 @@ prompt_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
             uint4* at = reinterpret_cast<uint4*>(aligned + stage * C::TILE_BYTES + pn * C::PANEL + (16 * warp * 8 + i) * 16);
             uint4 v = make_uint4(0, 0, 0, 0);
             if (key < most) {
-              bool unused = false;
               v = *at;
-              v = make_uint4(finite_pair<BF16>(v.x, &unused), finite_pair<BF16>(v.y, &unused), finite_pair<BF16>(v.z, &unused), finite_pair<BF16>(v.w, &unused));
+              v = make_uint4(finite_pair<BF16>(v.x, &odd), finite_pair<BF16>(v.y, &odd), finite_pair<BF16>(v.z, &odd), finite_pair<BF16>(v.w, &odd));
             }
             *at = v;
           }
         }
+        if (odd) *odd_values = 1;
         fence_proxy_async_smem();              // the stage is refilled by TMA
         __syncwarp();
       }
@@ -691,39 +797,56 @@ prompt_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
     }
   }
   __syncthreads();
-  if (threadIdx.x < D) {
-    for (int row = 0; row < rows; ++row) {     // channel per thread: the warps' parts rescaled to their common maximum
-      float top = -INFINITY;
+  // The warps' parts rescaled to their common maximum: a thread per row finds the factors, which take the places of the maxima, then four
+  // channels per thread and turn.
+  if (threadIdx.x < rows) {
+    float top = -INFINITY, sum = 0.f;
+    float* at = part + threadIdx.x * C::PART + D;
+    constexpr int kWarp = kRowsMax * C::PART;
 #pragma unroll
-      for (int k = 0; k < 4; ++k) top = fmaxf(top, part[(k * kRowsMax + row) * C::PART + D]);
-      const float at = top == -INFINITY ? 0.f : top;
-      float sum = 0.f, o = 0.f;
+    for (int k = 0; k < 4; ++k) top = fmaxf(top, at[k * kWarp]);
+    const float ref = top == -INFINITY ? 0.f : top;
+    float f[4];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const float* from = part + (k * kRowsMax + row) * C::PART;
-        const float f = exp2_approx((from[D] - at) * p.scale_log2);
-        sum += from[D + 1] * f;
-        o += from[threadIdx.x] * f;
-      }
-      if (w.parts == 1) {
-        prompt_store<BF16>(p, w, w.row0 + row, threadIdx.x, D, sum == 0.f ? 0.f : o / sum, first);
-      } else {
-        float* to = p.parts + (static_cast<long long>(blockIdx.x) * kRowsMax + row) * C::PART;
-        to[threadIdx.x] = o;
-        if (threadIdx.x == 0) { to[D] = top; to[D + 1] = sum; }
-      }
+    for (int k = 0; k < 4; ++k) {
+      f[k] = exp2_approx((at[k * kWarp] - ref) * p.scale_log2);
+      sum += at[k * kWarp + 1] * f[k];
     }
+    if (w.parts > 1) {
+      float* to = p.parts + (static_cast<long long>(blockIdx.x) * kRowsMax + threadIdx.x) * C::PART + D;
+      *reinterpret_cast<float4*>(to) = make_float4(top, sum, static_cast<float>(*odd_values), 0.f);
+      sum = 1.f;
+    }
+    const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) at[k * kWarp] = f[k] * inv;
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < rows * (D / 4); i += C::THREADS) {
+    const int row = i / (D / 4), c = i % (D / 4) * 4;
+    const float* from = part + row * C::PART;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float4 x = *reinterpret_cast<const float4*>(from + k * kRowsMax * C::PART + c);
+      const float f = from[k * kRowsMax * C::PART + D];
+      o = make_float4(fmaf(x.x, f, o.x), fmaf(x.y, f, o.y), fmaf(x.z, f, o.z), fmaf(x.w, f, o.w));
+    }
+    if (w.parts > 1) *reinterpret_cast<float4*>(p.parts + (static_cast<long long>(blockIdx.x) * kRowsMax + row) * C::PART + c) = o;
+    else prompt_store<BF16>(p, w, w.row0 + row, c, D, o, first, *odd_values != 0);
   }
   if (threadIdx.x == 0 && *abort_flag) atomicMax(p.status, kStatusAttnTimeout);
+  // Where the tiled kernel is in front, this one runs beside it; it ends after it, so that what follows is behind both.
+  asm volatile("griddepcontrol.wait;" ::: "memory");
 }
 
-// One CTA per (row tile with several parts, row): the parts' results rescaled to their common maximum, in order.
-// Grid: (CTAs of the few-row kernel that hold a first part) x 16; the others leave at once.
+// A warp per row of a row tile with several parts (grid: row tiles x 4, four rows each): the parts rescaled to their common maximum, in order.  Lanes hold
+// the parts' factors, 32 at a time, and four (d = 128) or two channels each.
+constexpr int kJoinRows = 4;
 template <int D, bool BF16>
-__global__ void __launch_bounds__(D)
+__global__ void __launch_bounds__(kJoinRows * 32)
 prompt_join_kernel(const PromptAttnParams p, const __grid_constant__ PromptBatch batch) {
   constexpr int PART = PromptRowsCfg<D>::PART;
-  asm volatile("griddepcontrol.wait;" ::: "memory");                    // the parts are complete
   // row tiles are counted request by request, key head by key head
   int tile = blockIdx.x, cta = 0;
   PromptPart w{};
@@ -743,21 +866,39 @@ prompt_join_kernel(const PromptAttnParams p, const __grid_constant__ PromptBatch
     cta += here * w.parts;
   }
   w.before = w.kv_len - w.q_len;
-  const int row = blockIdx.y;
+  const int row = blockIdx.y * kJoinRows + (threadIdx.x >> 5), lane = threadIdx.x & 31;
   if (w.parts == 1 || row >= w.q_len * p.group - w.row0) return;
+  asm volatile("griddepcontrol.wait;" ::: "memory");                    // the parts are complete
   const float* from = p.parts + (static_cast<long long>(cta) * kRowsMax + row) * PART;
   constexpr long long kStep = static_cast<long long>(kRowsMax) * PART;
-  float top = -INFINITY;
-  for (int k = 0; k < w.parts; ++k) top = fmaxf(top, from[k * kStep + D]);
-  const float at = top == -INFINITY ? 0.f : top;
-  float sum = 0.f, o = 0.f;
-#pragma unroll 4
-  for (int k = 0; k < w.parts; ++k) {
-    const float f = exp2_approx((from[k * kStep + D] - at) * p.scale_log2);
-    sum += from[k * kStep + D + 1] * f;
-    o += from[k * kStep + threadIdx.x] * f;
+  const int c = lane * 4;                                               // (d = 64: half of the lanes hold channels)
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  float ref = -INFINITY, sum = 0.f, odd = 0.f;
+  for (int k0 = 0; k0 < w.parts; k0 += 32) {
+    const int n = min(32, w.parts - k0);
+    const float4 mine = lane < n ? *reinterpret_cast<const float4*>(from + (k0 + lane) * kStep + D) : make_float4(-INFINITY, 0.f, 0.f, 0.f);
+    float top = fmaxf(ref, mine.x);
+#pragma unroll
+    for (int s = 16; s > 0; s >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, s));
+    const float at = top == -INFINITY ? 0.f : top;
+    const float keep = exp2_approx((ref - at) * p.scale_log2), f = exp2_approx((mine.x - at) * p.scale_log2);
+    float part = mine.y * f;
+#pragma unroll
+    for (int s = 16; s > 0; s >>= 1) part += __shfl_xor_sync(0xffffffffu, part, s);
+    sum = sum * keep + part;
+    odd = __any_sync(0xffffffffu, mine.z != 0.f) ? 1.f : odd;
+    o = make_float4(o.x * keep, o.y * keep, o.z * keep, o.w * keep);
+    ref = top;
+#pragma unroll 8
+    for (int k = 0; k < n; ++k) {
+      const float fk = __shfl_sync(0xffffffffu, f, k);
+      const float4 x = c < D ? *reinterpret_cast<const float4*>(from + (k0 + k) * kStep + c) : make_float4(0.f, 0.f, 0.f, 0.f);
+      o = make_float4(fmaf(x.x, fk, o.x), fmaf(x.y, fk, o.y), fmaf(x.z, fk, o.z), fmaf(x.w, fk, o.w));
+    }
   }
-  prompt_store<BF16>(p, w, w.row0 + row, threadIdx.x, D, sum == 0.f ? 0.f : o / sum, prompt_limit(w, p, w.row0 / p.group));
+  const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+  if (c < D)
+    prompt_store<BF16>(p, w, w.row0 + row, c, D, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv), prompt_limit(w, p, w.row0 / p.group), odd != 0.f);
 }
 
 }  // namespace dit
