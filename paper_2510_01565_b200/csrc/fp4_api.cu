@@ -148,22 +148,26 @@ cudaError_t dispatch_product(const OpsDevice& d, int pairs, const dit_gemm_fp4_a
 }
 
 template <int kType, int G, bool kVec, int THREADS>
-cudaError_t launch_rows(const Fp4QuantParams& p, int loads, cudaStream_t st) {
-  constexpr int CTA = THREADS < 256 ? 256 : THREADS, PER = CTA / THREADS;
+cudaError_t launch_rows(const Fp4QuantParams& p, long long loads, cudaStream_t st) {
+  constexpr int CTA = THREADS == 32 ? 256 : THREADS, PER = CTA / THREADS;
   const unsigned grid = (static_cast<unsigned>((static_cast<long long>(p.rows) + 127) / 128 * 128) + PER - 1) / PER;
-  if (loads <= 1) quantize_fp4_kernel<kType, G, kVec, THREADS, 1><<<grid, CTA, 0, st>>>(p);
-  else if (loads <= 2) quantize_fp4_kernel<kType, G, kVec, THREADS, 2><<<grid, CTA, 0, st>>>(p);
-  else if (loads <= 4) quantize_fp4_kernel<kType, G, kVec, THREADS, 4><<<grid, CTA, 0, st>>>(p);
-  else quantize_fp4_kernel<kType, G, kVec, THREADS, 8><<<grid, CTA, 0, st>>>(p);
+  const long long each = (loads + THREADS - 1) / THREADS;
+  if (each <= 1) quantize_fp4_kernel<kType, G, kVec, THREADS, 1><<<grid, CTA, 0, st>>>(p);
+  else if (each <= 2) quantize_fp4_kernel<kType, G, kVec, THREADS, 2><<<grid, CTA, 0, st>>>(p);
+  else if (each <= 4) quantize_fp4_kernel<kType, G, kVec, THREADS, 4><<<grid, CTA, 0, st>>>(p);
+  else quantize_fp4_kernel<kType, G, kVec, THREADS, 6><<<grid, CTA, 0, st>>>(p);
   return cudaGetLastError();
 }
 template <int kType, int G, bool kVec>
 cudaError_t launch_quant(const Fp4QuantParams& p, cudaStream_t st) {
-  // a warp per row up to 128 loads of 16 bytes, beyond that a CTA
+  // As few lanes per row as hold it in six 16-byte loads each: what a row's maximum costs grows with them.
   constexpr int EPL = QuantIn<kType>::EPL;
   const long long loads = (static_cast<long long>(p.cols) + EPL - 1) / EPL;
-  if (loads <= 32 * 4) return launch_rows<kType, G, kVec, 32>(p, static_cast<int>((loads + 31) / 32), st);
-  return launch_rows<kType, G, kVec, 256>(p, static_cast<int>(std::min<long long>(8, (loads + 255) / 256)), st);
+  if (loads <= 32 * 6) return launch_rows<kType, G, kVec, 32>(p, loads, st);
+  if (loads <= 64 * 6) return launch_rows<kType, G, kVec, 64>(p, loads, st);
+  if (loads <= 128 * 6) return launch_rows<kType, G, kVec, 128>(p, loads, st);
+  if (loads <= 256 * 6) return launch_rows<kType, G, kVec, 256>(p, loads, st);
+  return launch_rows<kType, G, kVec, 512>(p, loads, st);
 }
 template <int kType>
 cudaError_t launch_quant(const Fp4QuantParams& p, int group, bool vec, cudaStream_t st) {
@@ -190,7 +194,7 @@ cudaError_t launch_weight(const Fp4QuantWeightParams& p, int group, cudaStream_t
 
 template <int kType, int G>
 cudaError_t launch_values(const Fp4ValuesParams& p, bool vec, cudaStream_t st) {
-  const unsigned grid = static_cast<unsigned>((static_cast<long long>(p.rows) + 127) / 128 * ((static_cast<long long>(p.cols) + 127) / 128));
+  const unsigned grid = static_cast<unsigned>((static_cast<long long>(p.rows) + kValueRows - 1) / kValueRows * ((static_cast<long long>(p.cols) + kValueCols - 1) / kValueCols));
   if (vec) dequantize_fp4_kernel<kType, G, true><<<grid, 256, 0, st>>>(p);
   else dequantize_fp4_kernel<kType, G, false><<<grid, 256, 0, st>>>(p);
   return cudaGetLastError();
@@ -278,7 +282,8 @@ dit_status dit_dequantize_fp4(const void* codes, int64_t ld_codes, const void* s
   Fp4ValuesParams p{};
   p.codes = static_cast<const uint8_t*>(codes); p.scales = static_cast<const uint8_t*>(scales); p.row_scales = row_scales; p.out = out;
   p.ld_codes = ld_codes; p.ld_out = ld_out; p.rows = static_cast<int>(rows); p.cols = static_cast<int>(cols); p.chunks = chunks_of(cols, group);
-  const bool vec = aligned(out, 16) && ld_out * type_bytes(out_type) % 16 == 0;
+  const int unit = 8 * type_bytes(out_type);     // eight values leave in one store
+  const bool vec = aligned(out, unit) && ld_out * type_bytes(out_type) % unit == 0;
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (out_type == DIT_TYPE_F16) return status_of(group == 16 ? launch_values<0, 16>(p, vec, st) : launch_values<0, 32>(p, vec, st));
   if (out_type == DIT_TYPE_BF16) return status_of(group == 16 ? launch_values<1, 16>(p, vec, st) : launch_values<1, 32>(p, vec, st));

@@ -4,8 +4,8 @@
 //   16   scale = s * 2^e, e the smallest integer with row top <= 6 * 448 * 2^e (one fp32 2^e per row),
 //        s = e4m3(top * 2^-e / 6), code = e2m1((x * 2^-e) / s), zero where s is zero
 // with top = max(max|x|, 2^-100) of the group or row.  The row's factor is a power of two, so every product above is exact and each
-// decision rests on one division: a quotient of 16-bit inputs that lies on a border between two codes is then the same in
-// 32 bits as in any wider arithmetic, and codes can be tested bit for bit.
+// decision rests on one quotient, rounded to fp32: for 16-bit inputs it lies on a border between two codes exactly where the true one does, and
+// codes can be tested bit for bit.
 //
 // Scale bytes lie in the order in which the tensor cores take them: tiles of 128 rows x 4 groups, 512 bytes,
 //   byte (row % 32) * 16 + (row % 128) / 32 * 4 + group % 4   of tile [row / 128][group / 4]
@@ -63,59 +63,54 @@ __device__ __forceinline__ int row_exponent(float top) { return scale_exponent<0
 __device__ __forceinline__ float e8m0_value(uint32_t b) { return b == 0 ? __uint_as_float(0x00400000u) : (b == 255 ? __uint_as_float(0x7FC00000u) : __uint_as_float(b << 23)); }
 __device__ __forceinline__ float e4m3_value(uint32_t b) { return __half2float(__half(__nv_cvt_fp8_to_halfraw(static_cast<__nv_fp8_storage_t>(b), __NV_E4M3))); }
 
-// What a lane needs to code values of its group.
+// What a lane needs to code values of its group: codes are e2m1(x * up * (high + low)).
 struct GroupScale {
   uint32_t byte;
-  float up;                  // 2^-e
-  float s, inv;              // e4m3 value and its reciprocal; inv 0: every code is zero
+  float up, high, low;       // 2^-e; the reciprocal of the e4m3 number in two parts (groups of 16)
+  bool none;                 // every code is zero
 };
-// e: the row's exponent (groups of 16); bad: the row (16) or group (32) holds a NaN or an infinity
+// up: 2^-e of the row (groups of 16); bad: the row (16) or group (32) holds a NaN or an infinity.
+//
+// There are no divisions.  A quotient x / s of a 24-bit x and an s of four bits (or 6, two bits) that fp32 does not hold is at least 2^-29 of
+// itself away from the middle between two fp32 numbers.  With the reciprocal in two parts, low = (1 - s high) high, the sum x high + x low is off
+// by less than 2^-44 before its one rounding: it is the correctly rounded quotient.
 template <int kGroup>
-__device__ __forceinline__ GroupScale group_scale(float top, int e, bool bad) {
+__device__ __forceinline__ GroupScale group_scale(float top, float up, bool bad) {
   GroupScale g;
   if constexpr (kGroup == 32) {
-    const int ge = group_exponent(fmaxf(top, kQuantFloor));
-    g.byte = bad ? 255u : static_cast<uint32_t>(ge + 127);
-    g.up = bad ? 0.f : pow2(-ge);
-    g.s = 1.f; g.inv = bad ? 0.f : 1.f;
+    const int e = group_exponent(fmaxf(bad ? 0.f : top, kQuantFloor));
+    g.byte = bad ? 255u : static_cast<uint32_t>(e + 127);
+    g.up = pow2(-e);
+    g.high = 1.f; g.low = 0.f;
+    g.none = bad;
   } else {
-    g.up = bad ? 0.f : pow2(-e);
-    g.byte = bad ? 0u : __nv_cvt_float_to_fp8(__fdiv_rn(top * g.up, 6.0f), __NV_SATFINITE, __NV_E4M3);
-    g.s = e4m3_value(g.byte);
-    g.inv = g.s > 0.f ? __frcp_rn(g.s) : 0.f;
+    const float t = top * up;
+    constexpr float kSixth = 0.16666667163372039794921875f, kRest = -4.967053879312289e-09f;      // 1/6 = kSixth + kRest, |error| < 2^-50
+    g.byte = bad ? 0u : __nv_cvt_float_to_fp8(fmaf(t, kSixth, t * kRest), __NV_SATFINITE, __NV_E4M3);
+    g.none = g.byte == 0;
+    g.up = up;
+    const float s = e4m3_value(g.byte);
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(g.high) : "f"(s));
+    g.low = g.high * fmaf(-s, g.high, 1.0f);
   }
   return g;
 }
 
-// Two quotients x / s.  16-bit inputs multiply by the reciprocal: the product is off by less than 2^-22, and since a true
-// quotient is either on a border of two codes or at least 2^-11 away from it (x has at most 11 bits, s four, borders three),
-// rounding the product to 18 bits puts it back on the border exactly where the quotient is.  (y + 64 y) - 64 y is that rounding.
-__device__ __forceinline__ float2 quotients(float2 x, const GroupScale& g) {
-  const float f = g.up * g.inv;
-  const float2 y = fmul2(x, make_float2(f, f));
-  const float2 high = fmul2(y, make_float2(65.f, 65.f));
-  return fadd2(high, ffma2(high, make_float2(-1.f, -1.f), y));
-}
-
-// Codes of the EPL values of a 16-byte load (8 codes for 16-bit inputs, 4 for fp32).
-template <int kType, int kGroup, int EPL>
-__device__ __forceinline__ uint32_t encode(const float (&v)[EPL], const GroupScale& g) {
-  float q[EPL];
-  if constexpr (kGroup == 32) {
+// Codes of eight (16-bit inputs) or four values.
+template <int kGroup, int N>
+__device__ __forceinline__ uint32_t encode(const float (&v)[N], const GroupScale& g) {
+  float q[N];
+  const float2 up = make_float2(g.up, g.up), high = make_float2(g.high, g.high), low = make_float2(g.low, g.low);
 #pragma unroll
-    for (int i = 0; i < EPL; ++i) q[i] = g.inv == 0.f ? 0.f : v[i] * g.up;
-  } else if constexpr (kType == 2) {
-#pragma unroll
-    for (int i = 0; i < EPL; ++i) q[i] = g.inv == 0.f ? 0.f : __fdiv_rn(v[i] * g.up, g.s);
-  } else {
-#pragma unroll
-    for (int i = 0; i < EPL; i += 2) {
-      const float2 r = quotients(make_float2(v[i], v[i + 1]), g);
-      q[i] = g.inv == 0.f ? 0.f : r.x; q[i + 1] = g.inv == 0.f ? 0.f : r.y;
-    }
+  for (int i = 0; i < N; i += 2) {
+    float2 x = fmul2(make_float2(v[i], v[i + 1]), up);
+    if constexpr (kGroup == 16) x = ffma2(x, high, fmul2(x, low));
+    q[i] = x.x; q[i + 1] = x.y;
   }
-  if constexpr (EPL == 8) return e2m1x8(q);
-  else return e2m1x4(q[0], q[1], q[2], q[3]);
+  uint32_t code;
+  if constexpr (N == 8) code = e2m1x8(q);
+  else code = e2m1x4(q[0], q[1], q[2], q[3]);
+  return g.none ? 0u : code;
 }
 
 struct Fp4QuantParams {
@@ -131,16 +126,16 @@ __device__ __forceinline__ long long scale_at(int row, int group, int chunks) {
   return (static_cast<long long>(row >> 7) * chunks + (group >> 2)) * 512 + (row & 31) * 16 + ((row & 127) >> 5) * 4 + (group & 3);
 }
 
-// A row per THREADS lanes (a warp, or a whole CTA), a 16-byte load of consecutive columns per lane: EPL values, kGroup / EPL lanes
+// A row per THREADS lanes (a warp of a CTA of eight, or a whole CTA), a 16-byte load of consecutive columns per lane: EPL values, kGroup / EPL lanes
 // to a group.  A row of up to THREADS * kLoads loads stays in registers between its maximum and its codes; a longer one
 // is read twice.  Rows behind the last one up to the tile's end get their zero scales only.  Bound by HBM.
 // kVec: rows start on 16-byte boundaries; otherwise elements are loaded one by one.
 template <int kType, int kGroup, bool kVec, int THREADS, int kLoads>
-__global__ void __launch_bounds__(THREADS < 256 ? 256 : THREADS)
+__global__ void __launch_bounds__(THREADS == 32 ? 256 : THREADS, THREADS == 256 && kLoads == 6 ? 5 : 1)
 quantize_fp4_kernel(const Fp4QuantParams p) {
   using In = QuantIn<kType>;
   constexpr int EPL = In::EPL, LPG = kGroup / EPL;                // lanes per group
-  constexpr int CTA = THREADS < 256 ? 256 : THREADS;
+  constexpr int CTA = THREADS == 32 ? 256 : THREADS;
   __shared__ uint32_t warp_top[CTA / 32];
   const int at = threadIdx.x % THREADS;                           // lane of the row
   const long long row_l = static_cast<long long>(blockIdx.x) * (CTA / THREADS) + threadIdx.x / THREADS;
@@ -175,7 +170,7 @@ quantize_fp4_kernel(const Fp4QuantParams p) {
   };
   auto top_of = [&](const uint4& r) { return In::max_bits(In::max_bits(In::max_bits(In::max_bits(0u, r.x), r.y), r.z), r.w); };
   load(0);
-  int e = 0;
+  float up = 0.f;
   bool bad = false;
   if constexpr (kGroup == 16) {
     uint32_t top = 0;
@@ -196,27 +191,32 @@ quantize_fp4_kernel(const Fp4QuantParams p) {
     }
     const float row_top = In::from_bits(top);
     bad = !(row_top < INFINITY);
-    e = row_exponent(fmaxf(bad ? 1.f : row_top, kQuantFloor));
+    const int e = row_exponent(fmaxf(bad ? 1.f : row_top, kQuantFloor));
+    up = pow2(-e);
     if (there && at == 0) p.row_scales[row] = bad ? __uint_as_float(0x7FC00000u) : pow2(e);
     if (span < p.cols) load(0);
   }
+  // the lane's first byte and code of the row; a load further on they are fixed distances away
+  uint8_t* scale = p.scales + scale_at(row, at * EPL / kGroup, p.chunks);
+  uint8_t* codes = p.codes + row * p.ld_codes + at * (EPL / 2);
   for (int base = 0; base < wide; base += span) {
     if (base > 0) load(base);
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
-      const int c = base + (i * THREADS + at) * EPL;              // (a warp's lanes part here only between whole groups' chunks of 4)
+      const int c = base + (i * THREADS + at) * EPL;
+      if (base + i * THREADS * EPL >= wide) break;
       uint32_t bits = In::fold_bits(top_of(raw[i]));
 #pragma unroll
       for (int o = 1; o < LPG; o <<= 1) bits = max(bits, __shfl_xor_sync(0xffffffffu, bits, o));
       const float top = In::from_bits(bits);
-      const bool odd = kGroup == 32 ? !(top < INFINITY) : bad;
-      const GroupScale g = group_scale<kGroup>(top, e, odd);
-      if (c < wide && (at % LPG) == 0) p.scales[scale_at(row, c / kGroup, p.chunks)] = there && c < p.cols ? static_cast<uint8_t>(g.byte) : 0;
+      const GroupScale g = group_scale<kGroup>(top, up, kGroup == 32 ? !(top < INFINITY) : bad);
+      // (THREADS * EPL columns are whole tiles of four groups: 512 bytes each)
+      if (c < wide && (at % LPG) == 0) scale[(base / EPL + i * THREADS) / (4 * LPG) * 512] = there && c < p.cols ? static_cast<uint8_t>(g.byte) : 0;
       if (there && c < p.cols) {
         float v[EPL];
         In::widen16(raw[i], v);
-        const uint32_t code = encode<kType, kGroup, EPL>(v, g);
-        uint8_t* dst = p.codes + row * p.ld_codes + c / 2;
+        const uint32_t code = encode<kGroup, EPL>(v, g);
+        uint8_t* dst = codes + (base + i * THREADS * EPL) / 2;
         if (c + EPL <= p.cols) {
           if constexpr (EPL == 8) *reinterpret_cast<uint32_t*>(dst) = code;
           else *reinterpret_cast<uint16_t*>(dst) = static_cast<uint16_t>(code);
@@ -257,22 +257,29 @@ fp4_column_scales_kernel(const Fp4QuantWeightParams p) {
   const int n = static_cast<int>(min(static_cast<long long>(kColumnRows), p.in_dim - row0));
   uint4 top = make_uint4(0, 0, 0, 0);
   auto take = [&](uint32_t a, uint32_t b) { return kType == 2 ? max(a, b & 0x7FFFFFFFu) : __vmaxu2(a, b & 0x7FFF7FFFu); };
-#pragma unroll 4
-  for (int r = sub; r < n; r += RPI) {
-    uint4 v = make_uint4(0, 0, 0, 0);
-    if (kVec && c + EPL <= p.out_dim) {
-      v = *reinterpret_cast<const uint4*>(src + r * p.ld);
-    } else {
-      uint32_t w[4] = {0, 0, 0, 0};
+  constexpr int BATCH = kColumnRows / RPI < 8 ? kColumnRows / RPI : 8;             // all are requested before the first is used
+  for (int r0 = sub; r0 < n; r0 += BATCH * RPI) {
+    uint4 v[BATCH];
 #pragma unroll
-      for (int e = 0; e < EPL; ++e)
-        if (c + e < p.out_dim) {
-          if constexpr (kType == 2) w[e] = __float_as_uint(src[r * p.ld + e]);
-          else w[e >> 1] |= static_cast<uint32_t>(src[r * p.ld + e]) << (16 * (e & 1));
-        }
-      v = make_uint4(w[0], w[1], w[2], w[3]);
+    for (int i = 0; i < BATCH; ++i) {
+      const int r = r0 + i * RPI;
+      v[i] = make_uint4(0, 0, 0, 0);
+      if (r >= n) continue;
+      if (kVec && c + EPL <= p.out_dim) {
+        v[i] = *reinterpret_cast<const uint4*>(src + r * p.ld);
+      } else {
+        uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+        for (int e = 0; e < EPL; ++e)
+          if (c + e < p.out_dim) {
+            if constexpr (kType == 2) w[e] = __float_as_uint(src[r * p.ld + e]);
+            else w[e >> 1] |= static_cast<uint32_t>(src[r * p.ld + e]) << (16 * (e & 1));
+          }
+        v[i] = make_uint4(w[0], w[1], w[2], w[3]);
+      }
     }
-    top = make_uint4(take(top.x, v.x), take(top.y, v.y), take(top.z, v.z), take(top.w, v.w));
+#pragma unroll
+    for (int i = 0; i < BATCH; ++i) top = make_uint4(take(top.x, v[i].x), take(top.y, v[i].y), take(top.z, v[i].z), take(top.w, v[i].w));
   }
   const uint32_t t[4] = {top.x, top.y, top.z, top.w};
   const int at = threadIdx.x % LPR * EPL;
@@ -287,7 +294,8 @@ fp4_column_scales_kernel(const Fp4QuantWeightParams p) {
   }
 }
 
-// A CTA transposes kIn x 64 weights through shared memory, a group of one output row per thread and turn.
+// A CTA transposes 128 x 64 weights through shared memory.  Neighbouring lanes then take the groups of one output row, so that a row's codes leave as
+// 64 consecutive bytes and its scales as words.
 constexpr int kWeightOut = 64;
 template <int kType, int kGroup, bool kVec>
 __global__ void __launch_bounds__(256)
@@ -295,65 +303,77 @@ quantize_weight_fp4_kernel(const Fp4QuantWeightParams p) {
   using In = QuantIn<kType>;
   using Elem = typename In::Elem;
   constexpr int EPL = In::EPL, kIn = 128, LPR = kWeightOut / EPL, RPI = 256 / LPR;
-  constexpr int PITCH = kWeightOut + (kType == 2 ? 1 : 2);         // rows of the tile an odd number of words apart
-  __shared__ Elem tile[kIn * PITCH];
+  // rows an odd number of words apart, and groups shifted against one another: lanes of several groups and rows meet in different banks
+  constexpr int PITCH = kWeightOut + (kType == 2 ? 1 : 2), SHIFT = kGroup == 32 ? 8 : 4;
+  auto place = [](int r) { return r * PITCH + r / kGroup * SHIFT; };
+  __shared__ Elem tile[kIn * PITCH + kIn / kGroup * SHIFT];
   const int out_tiles = (p.out_dim + 127) / 128 * 2;               // whole scale tiles
   const int n0 = blockIdx.x % out_tiles * kWeightOut;
   const int k0 = blockIdx.x / out_tiles * kIn;
   {
     const int c = threadIdx.x % LPR * EPL;
     const Elem* src = static_cast<const Elem*>(p.w) + static_cast<long long>(k0) * p.ld + n0 + c;
+    uint4 v[kIn / RPI];                                            // all are requested before the first is used
 #pragma unroll
     for (int i = 0; i < kIn / RPI; ++i) {
       const int r = i * RPI + threadIdx.x / LPR;
-      uint32_t w[4] = {0, 0, 0, 0};
+      v[i] = make_uint4(0, 0, 0, 0);
       if (k0 + r < p.in_dim) {
         if (kVec && n0 + c + EPL <= p.out_dim) {
-          const uint4 v = load_once(src + r * p.ld);
-          w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+          v[i] = load_once(src + r * p.ld);
         } else {
+          uint32_t w[4] = {0, 0, 0, 0};
 #pragma unroll
           for (int e = 0; e < EPL; ++e)
             if (n0 + c + e < p.out_dim) {
               if constexpr (kType == 2) w[e] = __float_as_uint(src[r * p.ld + e]);
               else w[e >> 1] |= static_cast<uint32_t>(src[r * p.ld + e]) << (16 * (e & 1));
             }
+          v[i] = make_uint4(w[0], w[1], w[2], w[3]);
         }
       }
+    }
+#pragma unroll
+    for (int i = 0; i < kIn / RPI; ++i) {
+      const int r = i * RPI + threadIdx.x / LPR;
+      const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
       if constexpr (kType == 2) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) tile[r * PITCH + c + e] = __uint_as_float(w[e]);
+        for (int e = 0; e < 4; ++e) tile[place(r) + c + e] = __uint_as_float(w[e]);
       } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) *reinterpret_cast<uint32_t*>(&tile[r * PITCH + c + 2 * e]) = w[e];
+        for (int e = 0; e < 4; ++e) *reinterpret_cast<uint32_t*>(&tile[place(r) + c + 2 * e]) = w[e];
       }
     }
   }
   __syncthreads();
-  constexpr int GROUPS = kIn / kGroup;                             // of the tile's columns: 8 or 4, one or two scale tiles
+  constexpr int GROUPS = kIn / kGroup;                             // of the tile's columns: 8 or 4, two scale tiles or one
+  const int gi = threadIdx.x % GROUPS, group = k0 / kGroup + gi, k = k0 + gi * kGroup;
+  const bool tiled = group < 4 * p.chunks;
 #pragma unroll
   for (int turn = 0; turn < GROUPS * kWeightOut / 256; ++turn) {
-    // neighbouring lanes take neighbouring output rows (no bank conflicts); a row's groups lie in four warps or eight
-    const int n = threadIdx.x % kWeightOut, gi = turn * (256 / kWeightOut) + threadIdx.x / kWeightOut;
-    const int row = n0 + n, k = k0 + gi * kGroup, group = k / kGroup;
-    if (group >= 4 * p.chunks) continue;
+    const int n = turn * (256 / GROUPS) + threadIdx.x / GROUPS, row = n0 + n;
     const bool there = row < p.out_dim && k < p.in_dim;
     float v[kGroup];
     float top = 0.f;
+    const Elem* from = tile + place(gi * kGroup) + n;
 #pragma unroll
     for (int i = 0; i < kGroup; ++i) {
-      v[i] = In::widen(tile[(gi * kGroup + i) * PITCH + n]);
+      v[i] = In::widen(from[i * PITCH]);
       top = fmax_nan(top, fabsf(v[i]));
     }
-    int e = 0;
+    float up = 0.f;
     bool bad = !(top < INFINITY);
     if constexpr (kGroup == 16) {
       const uint32_t u = there ? __float_as_uint(p.row_scales[row]) : 0x3F800000u;
       bad = u >= 0x7F800000u;
-      e = static_cast<int>(u >> 23) - 127;
+      up = bad ? 1.f : pow2(127 - static_cast<int>(u >> 23));
     }
-    const GroupScale g = group_scale<kGroup>(bad ? 0.f : top, e, bad);
-    p.scales[scale_at(row, group, p.chunks)] = there ? static_cast<uint8_t>(g.byte) : 0;
+    const GroupScale g = group_scale<kGroup>(bad ? 0.f : top, up, bad);
+    uint32_t word = there ? g.byte << (8 * (gi & 3)) : 0u;         // four neighbouring groups' bytes
+    word |= __shfl_xor_sync(0xffffffffu, word, 1);
+    word |= __shfl_xor_sync(0xffffffffu, word, 2);
+    if (tiled && (gi & 3) == 0) *reinterpret_cast<uint32_t*>(p.scales + scale_at(row, group, p.chunks)) = word;
     if (!there) continue;
     uint32_t code[kGroup / 8];
 #pragma unroll
@@ -361,12 +381,7 @@ quantize_weight_fp4_kernel(const Fp4QuantWeightParams p) {
       float part[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) part[i] = v[8 * b + i];
-      if constexpr (kType == 2 && kGroup == 16) {
-        float lo[4] = {part[0], part[1], part[2], part[3]}, hi[4] = {part[4], part[5], part[6], part[7]};
-        code[b] = encode<kType, kGroup, 4>(lo, g) | encode<kType, kGroup, 4>(hi, g) << 16;
-      } else {
-        code[b] = encode<kType, kGroup, 8>(part, g);
-      }
+      code[b] = encode<kGroup, 8>(part, g);
     }
     uint8_t* dst = p.codes + row * p.ld_codes + k / 2;
     const int bytes = min(kGroup, p.in_dim - k + 1) / 2;           // of the group: all of its kGroup / 2, or the row's last ones
@@ -388,41 +403,47 @@ struct Fp4ValuesParams {
   int rows, cols, chunks;
 };
 
-// code * scale (exact) * row scale, rounded to fp32 and then to the output's type.  A CTA takes 128 rows x 128 columns, a lane eight
-// consecutive codes at a time.  Bound by HBM.  kVec: rows of out start on 16-byte boundaries.
+// code * scale (exact) * row scale, rounded to fp32 and then to the output's type.  A CTA takes 64 rows x 256 columns, a lane eight
+// consecutive codes at a time, a warp a row.  Bound by HBM.  kVec: rows of out start on 16-byte boundaries (fp32: on 32-byte ones).
+constexpr int kValueRows = 64, kValueCols = 256;
 template <int kType, int kGroup, bool kVec>
 __global__ void __launch_bounds__(256)
 dequantize_fp4_kernel(const Fp4ValuesParams p) {
-  const int col_tiles = (p.cols + 127) / 128;
-  const int row0 = blockIdx.x / col_tiles * 128, c = blockIdx.x % col_tiles * 128 + (threadIdx.x & 15) * 8;
+  constexpr int TURNS = kValueRows / 8;
+  const int col_tiles = (p.cols + kValueCols - 1) / kValueCols;
+  const int row0 = blockIdx.x / col_tiles * kValueRows + (threadIdx.x >> 5), c = blockIdx.x % col_tiles * kValueCols + (threadIdx.x & 31) * 8;
   if (c >= p.cols) return;
   const int bytes = min(4, (p.cols - c + 1) / 2);
-  uint32_t code[8], byte[8];
+  const uint8_t* codes = p.codes + row0 * p.ld_codes + c / 2;
+  uint32_t code[TURNS], byte[TURNS];
+  float factor[TURNS];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int row = row0 + i * 16 + (threadIdx.x >> 4);
-    code[i] = 0; byte[i] = 0;
+  for (int i = 0; i < TURNS; ++i) {
+    const int row = row0 + i * 8;
+    code[i] = 0; byte[i] = 0; factor[i] = 1.f;
     if (row >= p.rows) continue;
-    const uint8_t* src = p.codes + row * p.ld_codes + c / 2;
+    const uint8_t* src = codes + i * 8 * p.ld_codes;
     if (bytes == 4) code[i] = __ldg(reinterpret_cast<const uint32_t*>(src));
     else for (int b = 0; b < bytes; ++b) code[i] |= static_cast<uint32_t>(src[b]) << (8 * b);
     byte[i] = __ldg(p.scales + scale_at(row, c / kGroup, p.chunks));
+    if (p.row_scales) factor[i] = __ldg(p.row_scales + row);
   }
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int row = row0 + i * 16 + (threadIdx.x >> 4);
+  for (int i = 0; i < TURNS; ++i) {
+    const int row = row0 + i * 8;
     if (row >= p.rows) break;
     const float scale = kGroup == 16 ? e4m3_value(byte[i]) : e8m0_value(byte[i]);
-    const float factor = p.row_scales ? __ldg(p.row_scales + row) : 1.f;
     float v[8];
     e2m1_values(code[i], v);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = v[j] * scale * factor;
+    for (int j = 0; j < 8; ++j) v[j] = v[j] * scale * factor[i];
     if constexpr (kType == 2) {
       float* out = static_cast<float*>(p.out) + row * p.ld_out + c;
       if (kVec && c + 8 <= p.cols) {
-        reinterpret_cast<float4*>(out)[0] = make_float4(v[0], v[1], v[2], v[3]);
-        reinterpret_cast<float4*>(out)[1] = make_float4(v[4], v[5], v[6], v[7]);
+        uint32_t w[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w[j] = __float_as_uint(v[j]);
+        st_global_v8(out, w);
       } else {
 #pragma unroll
         for (int j = 0; j < 8; ++j)

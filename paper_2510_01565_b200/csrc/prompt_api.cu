@@ -18,12 +18,36 @@ int type_bytes(dit_type t) { return t == DIT_TYPE_F32 ? 4 : 2; }
 bool type_ok(dit_type t) { return t == DIT_TYPE_F16 || t == DIT_TYPE_BF16 || t == DIT_TYPE_F32; }
 bool aligned(const void* p, uintptr_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 
-template <int kType>
-cudaError_t launch_rotary(const RotaryParams& p, bool vec, cudaStream_t st) {
+// units: pieces of a head that lanes take, 0 for the form that takes any alignment.
+template <int kType, int kBytes, bool kInterleaved>
+cudaError_t launch_rotary(const RotaryParams& p, int units, cudaStream_t st) {
   const unsigned grid = static_cast<unsigned>((p.rows + p.rows_per_cta - 1) / p.rows_per_cta);
-  if (vec) rotary_kernel<kType, true><<<grid, kRotaryThreads, 0, st>>>(p);
-  else rotary_kernel<kType, false><<<grid, kRotaryThreads, 0, st>>>(p);
+  switch (units) {
+    case 4: rotary_kernel<kType, 4, kBytes, kInterleaved><<<grid, kRotaryThreads, 0, st>>>(p); break;
+    case 8: rotary_kernel<kType, 8, kBytes, kInterleaved><<<grid, kRotaryThreads, 0, st>>>(p); break;
+    case 16: rotary_kernel<kType, 16, kBytes, kInterleaved><<<grid, kRotaryThreads, 0, st>>>(p); break;
+    case 32: rotary_kernel<kType, 32, kBytes, kInterleaved><<<grid, kRotaryThreads, 0, st>>>(p); break;
+    default: rotary_kernel<kType, 0, 16, kInterleaved><<<grid, kRotaryThreads, 0, st>>>(p);
+  }
   return cudaGetLastError();
+}
+template <int kType>
+cudaError_t launch_rotary(RotaryParams p, const dit_rotary_args& a, cudaStream_t st) {
+  // pieces of 16 bytes, of 8 where rows, heads or halves start off 16-byte boundaries; the pieces of a head are rounded up to a power of two,
+  // whose last lanes idle (heads of 80: 5 of 8)
+  constexpr int kElem = kType == 2 ? 4 : 2;
+  for (int bytes = 16; bytes >= 8; bytes /= 2) {
+    const int per = bytes / kElem;
+    if (!aligned(a.x, bytes) || !aligned(a.out, bytes) || a.ld_x % per || a.ld_out % per || a.head_dim % per || a.rotary_dim % per ||
+        (!a.interleaved && p.pairs % per))
+      continue;
+    p.pieces = (a.interleaved ? a.rotary_dim : p.pairs) / per + (a.head_dim - a.rotary_dim) / per;
+    if (p.pieces > 32) break;
+    const int units = p.pieces <= 4 ? 4 : (p.pieces <= 8 ? 8 : (p.pieces <= 16 ? 16 : 32));
+    if (bytes == 16) return a.interleaved ? launch_rotary<kType, 16, true>(p, units, st) : launch_rotary<kType, 16, false>(p, units, st);
+    return a.interleaved ? launch_rotary<kType, 8, true>(p, units, st) : launch_rotary<kType, 8, false>(p, units, st);
+  }
+  return a.interleaved ? launch_rotary<kType, 16, true>(p, 0, st) : launch_rotary<kType, 16, false>(p, 0, st);
 }
 
 // ------------------------------------------------------------------------------------------------ attention
@@ -225,7 +249,7 @@ dit_status dit_rotary(const dit_rotary_args* a, void* stream) {
   const dit_status s = ops_device(&d);
   if (s != DIT_OK) return s;
   p.x = a->x; p.out = a->out; p.ld_x = a->ld_x; p.ld_out = a->ld_out; p.rows = a->rows; p.positions = a->positions;
-  p.n_heads = a->n_heads; p.head_dim = a->head_dim; p.pairs = a->rotary_dim / 2; p.interleaved = a->interleaved != 0; p.inverse = a->inverse != 0;
+  p.n_heads = a->n_heads; p.head_dim = a->head_dim; p.pairs = a->rotary_dim / 2; p.inverse = a->inverse != 0;
   p.magnitude = a->magnitude;
   constexpr double kTurn = 6.283185307179586476925287;
   for (int i = 0; i < p.pairs; ++i) {
@@ -240,14 +264,11 @@ dit_status dit_rotary(const dit_rotary_args* a, void* stream) {
   }
   // four rows per CTA once that leaves every SM a few CTAs
   p.rows_per_cta = a->rows >= 8ll * kRotaryRows * d.num_sms ? kRotaryRows : 1;
-  const int per = 16 / type_bytes(a->type);
-  const bool vec = aligned(a->x, 16) && aligned(a->out, 16) && a->ld_x % per == 0 && a->ld_out % per == 0 && a->head_dim % per == 0 &&
-                   (p.interleaved ? a->rotary_dim : p.pairs) % per == 0 && a->rotary_dim % per == 0;
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
   cudaError_t e;
-  if (a->type == DIT_TYPE_F16) e = launch_rotary<0>(p, vec, st);
-  else if (a->type == DIT_TYPE_BF16) e = launch_rotary<1>(p, vec, st);
-  else e = launch_rotary<2>(p, vec, st);
+  if (a->type == DIT_TYPE_F16) e = launch_rotary<0>(p, *a, st);
+  else if (a->type == DIT_TYPE_BF16) e = launch_rotary<1>(p, *a, st);
+  else e = launch_rotary<2>(p, *a, st);
   return e == cudaSuccess ? DIT_OK : DIT_ERR_CUDA;
 }
 
