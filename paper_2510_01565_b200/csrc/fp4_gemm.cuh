@@ -73,24 +73,58 @@ constexpr int A_BYTES = BM * 128, B_BYTES = (BN / 2) * 128;            // 256 k 
 constexpr int EPI_WARPS = 8;
 constexpr int THREADS = 128 + 32 * EPI_WARPS;
 constexpr int REGS_ISSUE = 56, REGS_EPILOGUE = 224;                    // (56 + 2 * 224) * 32 <= 16384 per scheduler
-constexpr int BOX_BYTES = 4096, STAGE_OUT_BYTES = 2 * BOX_BYTES;
-constexpr int COL_BYTES = 2 * 512;                                     // column factors and bias of a warp's 128 columns
+constexpr int BOX_BYTES = 4096;                                        // 128 bytes x 32 rows of the output, one per epilogue warp
+constexpr int COL_BYTES = 2 * 512;                                     // column factors and bias of 128 columns, shared by four warps
 constexpr int kOverlap = 64;                                           // columns that the two accumulators share
 constexpr int kScaleCols = 512 - (2 * BN - kOverlap);                  // 64 columns for scales behind them
 template <int kGroup>
 struct Cfg {
   using S = Fp4Scales<kGroup>;
-  static constexpr int STAGES = 4;
+  static constexpr int STAGES = 5;
   static constexpr int STAGE_BYTES = A_BYTES + B_BYTES + 3 * S::BYTES;
   static constexpr int SLOT = 12;                                      // columns of one tile of a's scales and two of b's
   static constexpr int SLOTS = kScaleCols / SLOT;
   static constexpr int OFF_OUT = (STAGES * STAGE_BYTES + 1023) / 1024 * 1024;
-  static constexpr int OFF_BAR = OFF_OUT + EPI_WARPS * (STAGE_OUT_BYTES + COL_BYTES);
+  static constexpr int OFF_COL = OFF_OUT + EPI_WARPS * BOX_BYTES, OFF_BAR = OFF_COL + 2 * COL_BYTES;
   static constexpr int SMEM_BYTES = OFF_BAR + 256 + 1024;
   static_assert(STAGE_BYTES % 1024 == 0, "swizzled tiles start on 1 KB boundaries");
   static_assert(SMEM_BYTES <= 227 * 1024, "shared memory of one CTA");
 };
 }  // namespace fgemm
+
+// Writes a warp's box (32 rows of 128 bytes, 16-byte units XOR-swizzled by the row) to an output whose rows start off 16-byte boundaries, row by
+// row in 32-bit words.  A 16-bit row that starts in the middle of a word is shifted by one element on the way; its first and last element may go
+// out alone.  `cols` columns from c0 on exist (may be <= 0).
+template <int EPI>
+__device__ __forceinline__ void fp4_store_box(const Fp4GemmParams& p, const uint8_t* box, int lane, int row0, int c0, int cols) {
+  constexpr int BATCH = 8;                     // rows whose words are read before the first is written
+  const int rows = min(32, p.M - row0);
+  for (int r0 = 0; r0 < rows; r0 += BATCH) {
+    uint32_t v[BATCH];
+#pragma unroll
+    for (int k = 0; k < BATCH; ++k) v[k] = *reinterpret_cast<const uint32_t*>(box + (r0 + k) * 128 + ((((lane >> 2) ^ ((r0 + k) & 7)) << 4) | ((lane & 3) << 2)));
+#pragma unroll
+    for (int k = 0; k < BATCH; ++k) {
+      if (r0 + k >= rows) break;
+      const long long first = (static_cast<long long>(row0) + r0 + k) * p.ld_out + c0;
+      if constexpr (EPI == kBlkF32) {
+        if (lane < cols) static_cast<float*>(p.out)[first + lane] = __uint_as_float(v[k]);
+      } else {
+        uint16_t* at = static_cast<uint16_t*>(p.out) + first;
+        int left = cols;
+        if ((reinterpret_cast<uintptr_t>(at) >> 1) & 1) {              // the row starts in the middle of a word (warp-uniform)
+          if (lane == 0 && cols > 0) at[0] = static_cast<uint16_t>(v[k]);
+          const uint32_t next = __shfl_down_sync(0xffffffffu, v[k], 1);
+          v[k] = __funnelshift_r(v[k], next, 16);
+          ++at; --left;
+        }
+        const int c = 2 * lane;
+        if (c + 1 < left) *reinterpret_cast<uint32_t*>(at + c) = v[k];
+        else if (c < left) at[c] = static_cast<uint16_t>(v[k]);
+      }
+    }
+  }
+}
 
 // Persistent, one 256 x 256 tile per CTA pair, 256 k per stage.  Roles: warp 0 TMA producer, warp 1 issues scale copies and MMAs (leader CTA;
 // it owns tensor memory), warps 4..11 take finished tiles out: two per quarter of the tile's rows, one for each 128 columns.
@@ -206,10 +240,9 @@ gemm_fp4_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
     const int quarter = warp & 3, chalf = (warp - 4) >> 2;
     const uint32_t lane_sel = static_cast<uint32_t>(quarter * 32) << 16;
     const uint32_t tempty_leader = map_to_cta(tempty_bar(0), 0), shared_leader = map_to_cta(shared_bar, 0);
-    uint8_t* stage = aligned + C::OFF_OUT + (warp - 4) * STAGE_OUT_BYTES;
-    float* col_of = reinterpret_cast<float*>(aligned + C::OFF_OUT + EPI_WARPS * STAGE_OUT_BYTES + (warp - 4) * COL_BYTES);   // factors, then bias
-    BlockGemmParams store{};                                           // what the unaligned store looks at
-    store.M = p.M; store.N = p.N; store.out = p.out; store.ld_out = p.ld_out;
+    uint8_t* box = aligned + C::OFF_OUT + (warp - 4) * BOX_BYTES;
+    float* col_of = reinterpret_cast<float*>(aligned + C::OFF_COL + chalf * COL_BYTES);      // factors, then bias
+    const uint64_t policy = evict_first_policy();
     int n = 0;
     for (int t = pair; t < num_tiles; t += num_pairs, ++n) {
       const int buf = n & 1;
@@ -218,13 +251,14 @@ gemm_fp4_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
       const int row0 = mb * (2 * BM) + rank * BM + quarter * 32, n0 = nb * BN + chalf * 128;
       const bool mine = n0 < p.N && row0 < p.M;                        // something of this warp's part exists (warp-uniform)
       const float fr = p.ra && row0 + lane < p.M ? __ldg(p.ra + row0 + lane) : 1.f;
-#pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        const int col = n0 + c * 32 + lane;
-        col_of[c * 32 + lane] = p.rb && col < p.N ? __ldg(p.rb + col) : 1.f;
-        col_of[128 + c * 32 + lane] = p.bias && col < p.N ? __ldg(p.bias + col) : 0.f;
+      {
+        const int c = quarter * 32 + lane;                             // the four warps of these columns fetch 32 each
+        const float f = p.rb && n0 + c < p.N ? __ldg(p.rb + n0 + c) : 1.f, b = p.bias && n0 + c < p.N ? __ldg(p.bias + n0 + c) : 0.f;
+        asm volatile("bar.sync %0, 128;" ::"r"(1 + chalf) : "memory"); // the last tile's have been read
+        col_of[c] = f;
+        col_of[128 + c] = b;
+        asm volatile("bar.sync %0, 128;" ::"r"(1 + chalf) : "memory");
       }
-      __syncwarp();
       if (!__all_sync(0xffffffffu, mbar_wait(tfull_bar(buf), (n >> 1) & 1u, abort_flag))) goto done;
       tc_fence_after();
       float2 acc[64];
@@ -248,7 +282,7 @@ gemm_fp4_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive_cluster_light(tempty_leader + 8u * buf);
-      if (!mine) continue;
+      if (!mine) continue;                     // (its warps of the next tile wait at its column factors)
 #pragma unroll
       for (int i = 0; i < 64; i += 2) {                                // (row factor * sum) * column factor + bias
         const float4 f = *reinterpret_cast<const float4*>(col_of + 2 * i), b = *reinterpret_cast<const float4*>(col_of + 128 + 2 * i);
@@ -256,40 +290,40 @@ gemm_fp4_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
         acc[i] = ffma2(fmul2(acc[i], r), make_float2(f.x, f.y), make_float2(b.x, b.y));
         acc[i + 1] = ffma2(fmul2(acc[i + 1], r), make_float2(f.z, f.w), make_float2(b.z, b.w));
       }
-      if (p.vec_out) {
-        // through shared memory and out by TMA, boxes of 128 bytes x 32 rows, 16-byte units XOR-swizzled by the row
-        constexpr bool kWide = EPI == kBlkF32;
-        constexpr bool kBf = EPI == kBlkBF16;
-        constexpr int COLS = kWide ? 32 : 64;
+      // through shared memory, and out by TMA where rows start on 16-byte boundaries
+      constexpr bool kWide = EPI == kBlkF32;
+      constexpr bool kBf = EPI == kBlkBF16;
+      constexpr int COLS = kWide ? 32 : 64;
 #pragma unroll
-        for (int round = 0; round < (kWide ? 2 : 1); ++round) {
-          if (lane == 0) bulk_store_read_done();                       // the previous boxes have left
-          __syncwarp();
+      for (int round = 0; round < 128 / COLS; ++round) {
+        if (lane == 0) bulk_store_read_done();                         // the previous box has left
+        __syncwarp();
 #pragma unroll
-          for (int q = 0; q < 16; ++q) {
-            uint4 w;
-            if constexpr (kWide) {
-              const float2 a = acc[round * 32 + 2 * q], b = acc[round * 32 + 2 * q + 1];
-              w = make_uint4(__float_as_uint(a.x), __float_as_uint(a.y), __float_as_uint(b.x), __float_as_uint(b.y));
-            } else {
-              w = make_uint4(pack16x2<kBf>(acc[4 * q].x, acc[4 * q].y), pack16x2<kBf>(acc[4 * q + 1].x, acc[4 * q + 1].y),
-                             pack16x2<kBf>(acc[4 * q + 2].x, acc[4 * q + 2].y), pack16x2<kBf>(acc[4 * q + 3].x, acc[4 * q + 3].y));
-            }
-            *reinterpret_cast<uint4*>(stage + (q >> 3) * 4096 + lane * 128 + (((q & 7) ^ (lane & 7)) << 4)) = w;
+        for (int q = 0; q < 8; ++q) {
+          uint4 w;
+          if constexpr (kWide) {
+            const float2 a = acc[round * 16 + 2 * q], b = acc[round * 16 + 2 * q + 1];
+            w = make_uint4(__float_as_uint(a.x), __float_as_uint(a.y), __float_as_uint(b.x), __float_as_uint(b.y));
+          } else {
+            const float2* a = acc + round * 32 + 4 * q;
+            w = make_uint4(pack16x2<kBf>(a[0].x, a[0].y), pack16x2<kBf>(a[1].x, a[1].y), pack16x2<kBf>(a[2].x, a[2].y), pack16x2<kBf>(a[3].x, a[3].y));
           }
+          *reinterpret_cast<uint4*>(box + lane * 128 + ((q ^ (lane & 7)) << 4)) = w;
+        }
+        const int x = n0 + round * COLS;
+        if (p.vec_out) {
           fence_proxy_async_smem();
           __syncwarp();
-          if (lane == 0) {
-            const int x = n0 + round * 2 * COLS;
-            if (x < p.N) tma_store_2d(&tmOut, smem_u32(stage), x, row0);
-            if (x + COLS < p.N) tma_store_2d(&tmOut, smem_u32(stage) + 4096, x + COLS, row0);
+          if (lane == 0 && x < p.N) {
+            tma_store_2d_hint(&tmOut, smem_u32(box), x, row0, policy);
             bulk_store_commit();
           }
+        } else {
+          __syncwarp();
+          fp4_store_box<EPI>(p, box, lane, row0, x, min(COLS, p.N - x));
         }
-        __syncwarp();
-      } else {
-        block_store_unaligned<EPI>(store, stage, acc, lane, row0, n0);
       }
+      __syncwarp();
     }
   }
 
