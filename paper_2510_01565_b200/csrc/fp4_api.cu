@@ -101,25 +101,34 @@ cudaError_t launch_split(const CUtensorMap& tmA, const CUtensorMap& tmB, const d
   return cudaLaunchKernelEx(&lc, &gemm_fp4_split_kernel<EPI, G, BT>, tmA, tmB, static_cast<const uint8_t*>(a.a_scales), static_cast<const uint8_t*>(a.b_scales), p, splits);
 }
 
+template <int EPI, int G, int BT>
+cudaError_t launch_split(const OpsDevice& d, const CUtensorMap& tmA, const CUtensorMap& tmB, const dit_gemm_fp4_args& a, const Fp4GemmParams& p, cudaStream_t st) {
+  const long long tiles = static_cast<long long>((p.N + 127) / 128) * ((p.M + BT - 1) / BT);
+  const int stages = (p.K + 255) / 256;
+  // CTAs per tile: doubled up to two CTAs per SM as long as each keeps a stage of four or more; with 32 rows or fewer, beyond one per SM only
+  // where each has more than eight stages to share (us for 1, 2, 4, 8: 144 tiles of 16 stages 12.6, 9.5, 17.2, 22.9; 72 of 16 13.0, 9.5, 12.5, 15.1;
+  // 32 of 16 12.3, 8.4, 6.4, 6.8; with 64 rows 32 of 16 15.3, 12.9, 9.2, 9.5; 12 of 2 7.0, 8.7).
+  int splits = 1;
+  while (splits < 8 && tiles * 2 * splits <= 2ll * d.num_sms && stages >= std::max(4, 2 * splits) &&
+         (BT == 64 || tiles * 2 * splits <= d.num_sms || stages > 8 * splits))
+    splits *= 2;
+  return launch_split<EPI, G, BT>(tmA, tmB, a, p, splits, st);
+}
+
 template <int EPI, int G>
 cudaError_t launch_product(const OpsDevice& d, int pairs, const dit_gemm_fp4_args& a, Fp4GemmParams p, cudaStream_t st) {
   using S = Fp4Scales<G>;
   CUtensorMap tmA, tmB, tmSA, tmSB;
   const uint64_t bytes = (static_cast<uint64_t>(p.K) + 1) / 2;
   const long long tiles_n = (p.N + 127) / 128;
-  const int stages = (p.K + 255) / 256;
   const long long pair_tiles = static_cast<long long>((p.M + 255) / 256) * ((p.N + 255) / 256);
   // Few rows, or so few tiles of 128 x 64 that most of the pair kernel's would be missing: the split kernel.
   if (p.M <= 32 || 3 * tiles_n * ((p.M + 63) / 64) <= 2ll * d.num_sms) {
     const int bt = p.M <= 16 ? 16 : (p.M <= 32 ? 32 : 64);
-    const long long tiles = tiles_n * ((p.M + bt - 1) / bt);
-    // CTAs per tile: doubled up to about two per SM as long as each keeps a stage or more
-    int splits = 1;
-    while (splits < 8 && tiles * 2 * splits <= 2ll * d.num_sms && stages / (2 * splits) >= 1) splits *= 2;
     if (!code_map(d, &tmA, a.a, bytes, p.M, a.lda, bt) || !code_map(d, &tmB, a.b, bytes, p.N, a.ldb, 128)) return cudaErrorInvalidValue;
-    if (bt == 16) return launch_split<EPI, G, 16>(tmA, tmB, a, p, splits, st);
-    if (bt == 32) return launch_split<EPI, G, 32>(tmA, tmB, a, p, splits, st);
-    return launch_split<EPI, G, 64>(tmA, tmB, a, p, splits, st);
+    if (bt == 16) return launch_split<EPI, G, 16>(d, tmA, tmB, a, p, st);
+    if (bt == 32) return launch_split<EPI, G, 32>(d, tmA, tmB, a, p, st);
+    return launch_split<EPI, G, 64>(d, tmA, tmB, a, p, st);
   }
   const uint64_t chunks = (static_cast<uint64_t>(p.K) + 4 * G - 1) / (4 * G);
   if (!code_map(d, &tmA, a.a, bytes, p.M, a.lda, 128) || !code_map(d, &tmB, a.b, bytes, p.N, a.ldb, 128) ||

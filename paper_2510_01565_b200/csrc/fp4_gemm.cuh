@@ -350,14 +350,15 @@ struct Fp4SplitCfg {
   using S = Fp4Scales<kGroup>;
   static constexpr int W_BYTES = 128 * 128, T_BYTES = BT * 128;
   static constexpr int STAGE_BYTES = (W_BYTES + T_BYTES + 2 * S::BYTES + 1023) / 1024 * 1024;
-  static constexpr int STAGES = BT <= 32 ? 4 : 3;
+  static constexpr int STAGES = BT <= 32 ? 4 : 3;                      // two CTAs per SM (one with twice the ring: 13.5 us where this takes 10.6)
   static constexpr int SLOT = 8, SLOTS = BT == 64 ? 8 : 7;             // scale columns in turn, behind the accumulator
   static constexpr int COLS = 128;
-  static constexpr int OFF_BAR = STAGES * STAGE_BYTES;
-  static constexpr int SMEM_BYTES = OFF_BAR + 256 + 1024;
+  static constexpr int OFF_BAR = STAGES * STAGE_BYTES, OFF_ROWS = OFF_BAR + 256;   // row factors [BT]
+  static constexpr int SMEM_BYTES = OFF_ROWS + 256 + 1024;
   static constexpr int THREADS = 192;
   static_assert(BT + SLOT * SLOTS <= COLS, "tensor memory of one CTA");
   static_assert(BT * 128 * 4 <= STAGES * STAGE_BYTES, "the partial sums reuse the ring");
+  static_assert(SMEM_BYTES <= 227 * 1024, "shared memory of one CTA");
   static_assert(5 * SMEM_BYTES > 227 * 1024, "CTAs that fit an SM's shared memory must fit its tensor memory (4 x 128 columns)");
 };
 
@@ -394,13 +395,24 @@ gemm_fp4_split_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_cons
   const int steps = (p.K + 63) / 64, stages = (steps + 3) / 4, chunks = (p.K + 4 * kGroup - 1) / (4 * kGroup);
   const int g0 = static_cast<int>(static_cast<long long>(stages) * rank / splits), g1 = static_cast<int>(static_cast<long long>(stages) * (rank + 1) / splits);
 
+  // The producer's thread sets the barriers up and requests the first stages before tensor memory is there and the CTA meets.
+  const uint8_t *wa = sb + static_cast<long long>(n0 >> 7) * chunks * 512, *ta = sa + static_cast<long long>(m0 >> 7) * chunks * 512;
+  auto load = [&](int g, int stage) {
+    const uint32_t s = base + stage * C::STAGE_BYTES;
+    const uint32_t bytes = min(S::TILES, chunks - g * S::TILES) * 512;
+    mbar_arrive_expect_tx(full_bar(stage), C::W_BYTES + C::T_BYTES + 2 * bytes);
+    tma_load_2d(s, &tmB, g * 128, n0, full_bar(stage));
+    tma_load_2d(s + C::W_BYTES, &tmA, g * 128, m0, full_bar(stage));
+    bulk_load(s + C::W_BYTES + C::T_BYTES, wa + static_cast<long long>(g) * S::BYTES, bytes, full_bar(stage));
+    bulk_load(s + C::W_BYTES + C::T_BYTES + S::BYTES, ta + static_cast<long long>(g) * S::BYTES, bytes, full_bar(stage));
+  };
   if (threadIdx.x == 0) {
     for (int s = 0; s < C::STAGES; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
     mbar_init(tfull_bar, 1);
     *abort_flag = 0;
     fence_mbar_init();
+    for (int s = 0; s < min(C::STAGES, g1 - g0); ++s) load(g0 + s, s);
   }
-  if (warp == 0 && lane == 0) { prefetch_tmap(&tmA); prefetch_tmap(&tmB); }
   if (warp == 1) { tmem_alloc(smem_u32(tmem_slot), C::COLS); tmem_relinquish(); }
   tc_fence_before();
   __syncthreads();
@@ -408,20 +420,15 @@ gemm_fp4_split_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_cons
   const uint32_t tmem_base = *tmem_slot;
   const int quarter = warp & 3;                                        // warps 2..5 -> quarters 2, 3, 0, 1
   const int col = n0 + quarter * 32 + lane;                            // this lane's output column (warps 2..5)
+  float* row_of = reinterpret_cast<float*>(aligned + C::OFF_ROWS);
+  float fc = 1.f, bias = 0.f;
 
   if (warp == 0) {
     if (lane == 0) {
       int stage = 0; uint32_t phase = 0;
-      const uint8_t *wa = sb + static_cast<long long>(n0 >> 7) * chunks * 512, *ta = sa + static_cast<long long>(m0 >> 7) * chunks * 512;
-      for (int g = g0; g < g1; ++g) {
-        if (!mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag)) break;
-        const uint32_t s = base + stage * C::STAGE_BYTES;
-        const uint32_t bytes = min(S::TILES, chunks - g * S::TILES) * 512;
-        mbar_arrive_expect_tx(full_bar(stage), C::W_BYTES + C::T_BYTES + 2 * bytes);
-        tma_load_2d(s, &tmB, g * 128, n0, full_bar(stage));
-        tma_load_2d(s + C::W_BYTES, &tmA, g * 128, m0, full_bar(stage));
-        bulk_load(s + C::W_BYTES + C::T_BYTES, wa + g * S::BYTES, bytes, full_bar(stage));
-        bulk_load(s + C::W_BYTES + C::T_BYTES + S::BYTES, ta + g * S::BYTES, bytes, full_bar(stage));
+      for (int g = g0 + C::STAGES; g < g1; ++g) {
+        if (!mbar_wait(empty_bar(stage), phase, abort_flag)) break;
+        load(g, stage);
         if (++stage == C::STAGES) { stage = 0; phase ^= 1u; }
       }
     }
@@ -455,11 +462,18 @@ gemm_fp4_split_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_cons
       if (ok) umma_commit(tfull_bar);
     }
   } else {
+    // what the sums are finished with is fetched under the stream
+    const int row = threadIdx.x - 64;
+    if (row < BT) row_of[row] = p.ra && m0 + row < p.M ? __ldg(p.ra + m0 + row) : 1.f;
+    if (col < p.N) {
+      fc = p.rb ? __ldg(p.rb + col) : 1.f;
+      bias = p.bias ? __ldg(p.bias + col) : 0.f;
+    }
+    asm volatile("bar.sync 1, 128;" ::: "memory");
     const bool ok = __all_sync(0xffffffffu, mbar_wait(tfull_bar, 0, abort_flag));
     if (ok) {
       tc_fence_after();
       const uint32_t t_row = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16);
-      const float fc = p.rb && col < p.N ? __ldg(p.rb + col) : 1.f, bias = p.bias && col < p.N ? __ldg(p.bias + col) : 0.f;
       float* part = reinterpret_cast<float*>(aligned);                 // every MMA has completed: the sums may take the ring's place
 #pragma unroll
       for (int c = 0; c < BT / 16; ++c) {
@@ -473,8 +487,7 @@ gemm_fp4_split_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_cons
           if (splits > 1) {
             part[row * 128 + quarter * 32 + lane] = __uint_as_float(r[i]);
           } else if (col < p.N && m0 + row < p.M) {
-            const float fr = p.ra ? __ldg(p.ra + m0 + row) : 1.f;
-            fp4_store_one<EPI>(p, m0 + row, col, fmaf(__uint_as_float(r[i]) * fr, fc, bias));
+            fp4_store_one<EPI>(p, m0 + row, col, fmaf(__uint_as_float(r[i]) * row_of[row], fc, bias));
           }
         }
       }
@@ -484,7 +497,6 @@ gemm_fp4_split_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_cons
     __syncwarp();
     cluster_sync_all();                        // (a CTA that gave up may have copies under way: it settles below)
     if (warp >= 2 && col < p.N) {
-      const float fc = p.rb ? __ldg(p.rb + col) : 1.f, bias = p.bias ? __ldg(p.bias + col) : 0.f;
       const int rows = min(BT, p.M - m0);
       const uint32_t mine = base + (quarter * 32 + lane) * 4;
       for (int i0 = rank; i0 < rows; i0 += 4 * splits) {               // four rows at a time: their loads are in flight together
@@ -500,7 +512,7 @@ gemm_fp4_split_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_cons
 #pragma unroll
           for (int r = 0; r < 8; ++r) sum += v[k][r];
           const int row = m0 + i0 + k * splits;
-          if (i0 + k * splits < rows) fp4_store_one<EPI>(p, row, col, fmaf(sum * (p.ra ? __ldg(p.ra + row) : 1.f), fc, bias));
+          if (i0 + k * splits < rows) fp4_store_one<EPI>(p, row, col, fmaf(sum * row_of[row - m0], fc, bias));
         }
       }
     }
