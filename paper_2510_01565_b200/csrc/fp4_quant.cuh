@@ -113,6 +113,36 @@ __device__ __forceinline__ uint32_t encode(const float (&v)[N], const GroupScale
   return g.none ? 0u : code;
 }
 
+// EPL consecutive elements from any element address, as the words of a 16-byte load; `n` of them exist (may be <= 0), the rest are zero.  kVec: the
+// address is a multiple of 16.  Otherwise whole runs come as 32-bit words, of 16-bit elements that start in the middle of a word as the
+// words around them, shifted (`before`: the element in front of the run may be read as well, and so may the one behind it where n > EPL).
+template <int kType, bool kVec>
+__device__ __forceinline__ uint4 load_run(const typename QuantIn<kType>::Elem* src, int n, bool before) {
+  constexpr int EPL = QuantIn<kType>::EPL;
+  if (n >= EPL) {
+    if constexpr (kVec) return load_once(src);
+    if constexpr (kType == 2) {
+      return make_uint4(__float_as_uint(__ldg(src)), __float_as_uint(__ldg(src + 1)), __float_as_uint(__ldg(src + 2)), __float_as_uint(__ldg(src + 3)));
+    } else {
+      const uintptr_t at = reinterpret_cast<uintptr_t>(src);
+      const uint32_t* words = reinterpret_cast<const uint32_t*>(at & ~static_cast<uintptr_t>(3));
+      if (!(at & 2)) return make_uint4(__ldg(words), __ldg(words + 1), __ldg(words + 2), __ldg(words + 3));
+      if (before && n > EPL) {
+        const uint32_t w0 = __ldg(words), w1 = __ldg(words + 1), w2 = __ldg(words + 2), w3 = __ldg(words + 3), w4 = __ldg(words + 4);
+        return make_uint4(__funnelshift_r(w0, w1, 16), __funnelshift_r(w1, w2, 16), __funnelshift_r(w2, w3, 16), __funnelshift_r(w3, w4, 16));
+      }
+    }
+  }
+  uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+  for (int e = 0; e < EPL; ++e)
+    if (e < n) {
+      if constexpr (kType == 2) w[e] = __float_as_uint(src[e]);
+      else w[e >> 1] |= static_cast<uint32_t>(src[e]) << (16 * (e & 1));
+    }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
 struct Fp4QuantParams {
   const void* x;             // [rows, cols], row stride ld
   uint8_t* codes;
@@ -151,21 +181,7 @@ quantize_fp4_kernel(const Fp4QuantParams p) {
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
       const int c = base + (i * THREADS + at) * EPL;
-      raw[i] = make_uint4(0, 0, 0, 0);
-      if (there && c < p.cols) {
-        if (kVec && c + EPL <= p.cols) {
-          raw[i] = load_once(src + c);
-        } else {
-          uint32_t w[4] = {0, 0, 0, 0};
-#pragma unroll
-          for (int e = 0; e < EPL; ++e)
-            if (c + e < p.cols) {
-              if constexpr (kType == 2) w[e] = __float_as_uint(src[c + e]);
-              else w[e >> 1] |= static_cast<uint32_t>(src[c + e]) << (16 * (e & 1));
-            }
-          raw[i] = make_uint4(w[0], w[1], w[2], w[3]);
-        }
-      }
+      raw[i] = load_run<kType, kVec>(src + c, there ? p.cols - c : 0, c > 0);
     }
   };
   auto top_of = [&](const uint4& r) { return In::max_bits(In::max_bits(In::max_bits(In::max_bits(0u, r.x), r.y), r.z), r.w); };
@@ -263,20 +279,7 @@ fp4_column_scales_kernel(const Fp4QuantWeightParams p) {
 #pragma unroll
     for (int i = 0; i < BATCH; ++i) {
       const int r = r0 + i * RPI;
-      v[i] = make_uint4(0, 0, 0, 0);
-      if (r >= n) continue;
-      if (kVec && c + EPL <= p.out_dim) {
-        v[i] = *reinterpret_cast<const uint4*>(src + r * p.ld);
-      } else {
-        uint32_t w[4] = {0, 0, 0, 0};
-#pragma unroll
-        for (int e = 0; e < EPL; ++e)
-          if (c + e < p.out_dim) {
-            if constexpr (kType == 2) w[e] = __float_as_uint(src[r * p.ld + e]);
-            else w[e >> 1] |= static_cast<uint32_t>(src[r * p.ld + e]) << (16 * (e & 1));
-          }
-        v[i] = make_uint4(w[0], w[1], w[2], w[3]);
-      }
+      v[i] = load_run<kType, kVec>(src + r * p.ld, r < n ? p.out_dim - c : 0, c > 0);
     }
 #pragma unroll
     for (int i = 0; i < BATCH; ++i) top = make_uint4(take(top.x, v[i].x), take(top.y, v[i].y), take(top.z, v[i].z), take(top.w, v[i].w));
@@ -317,21 +320,7 @@ quantize_weight_fp4_kernel(const Fp4QuantWeightParams p) {
 #pragma unroll
     for (int i = 0; i < kIn / RPI; ++i) {
       const int r = i * RPI + threadIdx.x / LPR;
-      v[i] = make_uint4(0, 0, 0, 0);
-      if (k0 + r < p.in_dim) {
-        if (kVec && n0 + c + EPL <= p.out_dim) {
-          v[i] = load_once(src + r * p.ld);
-        } else {
-          uint32_t w[4] = {0, 0, 0, 0};
-#pragma unroll
-          for (int e = 0; e < EPL; ++e)
-            if (n0 + c + e < p.out_dim) {
-              if constexpr (kType == 2) w[e] = __float_as_uint(src[r * p.ld + e]);
-              else w[e >> 1] |= static_cast<uint32_t>(src[r * p.ld + e]) << (16 * (e & 1));
-            }
-          v[i] = make_uint4(w[0], w[1], w[2], w[3]);
-        }
-      }
+      v[i] = load_run<kType, kVec>(src + r * p.ld, k0 + r < p.in_dim ? p.out_dim - n0 - c : 0, n0 + c > 0);
     }
 #pragma unroll
     for (int i = 0; i < kIn / RPI; ++i) {
@@ -411,9 +400,11 @@ __global__ void __launch_bounds__(256)
 dequantize_fp4_kernel(const Fp4ValuesParams p) {
   constexpr int TURNS = kValueRows / 8;
   const int col_tiles = (p.cols + kValueCols - 1) / kValueCols;
-  const int row0 = blockIdx.x / col_tiles * kValueRows + (threadIdx.x >> 5), c = blockIdx.x % col_tiles * kValueCols + (threadIdx.x & 31) * 8;
-  if (c >= p.cols) return;
-  const int bytes = min(4, (p.cols - c + 1) / 2);
+  __shared__ float lines[kVec ? 1 : 8][kVec ? 1 : 32 * 9];
+  const int lane = threadIdx.x & 31;
+  const int row0 = blockIdx.x / col_tiles * kValueRows + (threadIdx.x >> 5), c = blockIdx.x % col_tiles * kValueCols + lane * 8;
+  if (kVec && c >= p.cols) return;
+  const int bytes = max(0, min(4, (p.cols - c + 1) / 2));
   const uint8_t* codes = p.codes + row0 * p.ld_codes + c / 2;
   uint32_t code[TURNS], byte[TURNS];
   float factor[TURNS];
@@ -425,40 +416,53 @@ dequantize_fp4_kernel(const Fp4ValuesParams p) {
     const uint8_t* src = codes + i * 8 * p.ld_codes;
     if (bytes == 4) code[i] = __ldg(reinterpret_cast<const uint32_t*>(src));
     else for (int b = 0; b < bytes; ++b) code[i] |= static_cast<uint32_t>(src[b]) << (8 * b);
-    byte[i] = __ldg(p.scales + scale_at(row, c / kGroup, p.chunks));
+    if (bytes > 0) byte[i] = __ldg(p.scales + scale_at(row, c / kGroup, p.chunks));
     if (p.row_scales) factor[i] = __ldg(p.row_scales + row);
   }
 #pragma unroll
   for (int i = 0; i < TURNS; ++i) {
     const int row = row0 + i * 8;
-    if (row >= p.rows) break;
+    if (row >= p.rows) break;                                      // (the whole warp)
     const float scale = kGroup == 16 ? e4m3_value(byte[i]) : e8m0_value(byte[i]);
     float v[8];
     e2m1_values(code[i], v);
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] = v[j] * scale * factor[i];
-    if constexpr (kType == 2) {
-      float* out = static_cast<float*>(p.out) + row * p.ld_out + c;
-      if (kVec && c + 8 <= p.cols) {
-        uint32_t w[8];
+    if constexpr (kVec) {
+      if (c + 8 <= p.cols) {
+        if constexpr (kType == 2) {
+          uint32_t w[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) w[j] = __float_as_uint(v[j]);
-        st_global_v8(out, w);
+          for (int j = 0; j < 8; ++j) w[j] = __float_as_uint(v[j]);
+          st_global_v8(static_cast<float*>(p.out) + row * p.ld_out + c, w);
+        } else {
+          *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.out) + row * p.ld_out + c) =
+              make_uint4(pack16x2<kType == 1>(v[0], v[1]), pack16x2<kType == 1>(v[2], v[3]), pack16x2<kType == 1>(v[4], v[5]), pack16x2<kType == 1>(v[6], v[7]));
+        }
       } else {
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-          if (c + j < p.cols) out[j] = v[j];
+          if (c + j < p.cols) {
+            if constexpr (kType == 2) static_cast<float*>(p.out)[row * p.ld_out + c + j] = v[j];
+            else static_cast<uint16_t*>(p.out)[row * p.ld_out + c + j] = pack16<kType == 1>(v[j]);
+          }
       }
     } else {
-      uint16_t* out = static_cast<uint16_t*>(p.out) + row * p.ld_out + c;
-      const uint32_t w[4] = {pack16x2<kType == 1>(v[0], v[1]), pack16x2<kType == 1>(v[2], v[3]), pack16x2<kType == 1>(v[4], v[5]),
-                             pack16x2<kType == 1>(v[6], v[7])};
-      if (kVec && c + 8 <= p.cols) {
-        *reinterpret_cast<uint4*>(out) = make_uint4(w[0], w[1], w[2], w[3]);
-      } else {
+      // rows start anywhere: through shared memory, so that neighbouring lanes write neighbouring elements
+      float* line = lines[threadIdx.x >> 5];
+      __syncwarp();
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (c + j < p.cols) out[j] = static_cast<uint16_t>(w[j >> 1] >> (16 * (j & 1)));
+      for (int j = 0; j < 8; ++j) line[lane * 9 + j] = v[j];       // (nine words apart: no two lanes in a bank)
+      __syncwarp();
+      const int c0 = c - lane * 8;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int e = j * 32 + lane;
+        if (c0 + e < p.cols) {
+          const float x = line[e / 8 * 9 + e % 8];
+          if constexpr (kType == 2) static_cast<float*>(p.out)[row * p.ld_out + c0 + e] = x;
+          else static_cast<uint16_t*>(p.out)[row * p.ld_out + c0 + e] = pack16<kType == 1>(x);
+        }
       }
     }
   }

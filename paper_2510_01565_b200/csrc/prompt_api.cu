@@ -262,8 +262,8 @@ dit_status dit_rotary(const dit_rotary_args* a, void* stream) {
     }
     p.turns[i] = f / kTurn;
   }
-  // four rows per CTA once that leaves every SM a few CTAs
-  p.rows_per_cta = a->rows >= 8ll * kRotaryRows * d.num_sms ? kRotaryRows : 1;
+  // four rows per CTA once that leaves every SM one
+  p.rows_per_cta = a->rows >= static_cast<int64_t>(kRotaryRows) * d.num_sms ? kRotaryRows : 1;
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
   cudaError_t e;
   if (a->type == DIT_TYPE_F16) e = launch_rotary<0>(p, *a, st);
