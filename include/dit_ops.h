@@ -228,8 +228,8 @@ dit_status dit_rotary(const dit_rotary_args *args, void *stream);
  * one all of whose scores are -infinity.  Keys and values that a row does not see are never part of its result, whatever they hold.
  * Scores, their differences, the softmax and the sums are held in fp32, probabilities are rounded to the inputs' type for the second product;
  * scores of any size and infinite or NaN values are treated as dit_block_attention treats them.  A request's results do not depend on the
- * values of the others; where few rows (q_len * n_heads / n_kv_heads <= 512) read more than 256 keys, the keys may be summed in parts that
- * depend on the lengths of the whole batch, so that results may differ in their last bits with the batch that a request comes in.
+ * values of the others.  Which of two kernels serves a request, and into how many parts long keys are cut, depends on the lengths and heads of the
+ * whole batch: results may differ in their last bits with the batch that a request comes in.  The same call gives the same bits.
  *   q, k, v, out  device, type f16 or bf16, 16-byte aligned, leading dimensions multiples of 8 and >= n_heads * head_dim (q, out) or
  *                 n_kv_heads * head_dim (k, v); column ranges of one packed buffer are fine; out must not overlap the inputs
  *   head_dim      64 or 128 (DIT_ERR_SHAPE); n_kv_heads divides n_heads; n_requests <= DIT_MAX_REQUESTS; sums of lengths < 2^31 - 1024

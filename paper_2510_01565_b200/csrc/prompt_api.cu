@@ -60,7 +60,8 @@ cudaError_t allow_smem(Kernel kernel, int bytes) {
 }
 template <int D, bool BF16>
 cudaError_t allow_attention() {
-  const cudaError_t e = allow_smem(&prompt_attention_kernel<D, BF16>, PromptAttnCfg<D>::SMEM_BYTES);
+  cudaError_t e = allow_smem(&prompt_attention_kernel<D, BF16, false>, PromptAttnCfg<D>::SMEM_BYTES);
+  if (e == cudaSuccess) e = allow_smem(&prompt_attention_kernel<D, BF16, true>, PromptAttnCfg<D>::SMEM_BYTES);
   return e == cudaSuccess ? allow_smem(&prompt_rows_kernel<D, BF16>, PromptRowsCfg<D>::SMEM_BYTES) : e;
 }
 cudaError_t prepare(const OpsDevice& d) {
@@ -84,16 +85,17 @@ bool half_map(const OpsDevice& d, CUtensorMap* m, const void* ptr, uint64_t cols
                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// How a batch is worked on: which requests go to which kernel, and into how many parts the few-row requests are cut.
+// How a batch is worked on: which requests go to which kernel, and into how many parts their keys are cut.
 struct PromptPlan {
   PromptBatch tiled, few;
-  int64_t items;             // of the tiled kernel
-  int most_blocks;
+  int64_t pairs, items;      // of the tiled kernel
+  int most_blocks, part_blocks;
+  int64_t cut;               // pairs with several parts
   int64_t row_tiles, ctas;   // of the few-row kernel
   int chunk;
-  bool join;                 // some request has several parts
+  bool join;                 // some request of it has several parts
 };
-constexpr int kFewRowCtas = 148;                 // one for each SM
+constexpr int kSms = 148;                        // (plans, and with them workspaces, depend on the sizes of a call alone)
 
 int64_t few_row_ctas(const PromptPlan& p, const dit_prompt_attention_args& a, int chunk) {
   int64_t n = 0;
@@ -103,21 +105,74 @@ int64_t few_row_ctas(const PromptPlan& p, const dit_prompt_attention_args& a, in
   }
   return n;
 }
+int64_t pairs_with(const PromptPlan& p, const dit_prompt_attention_args& a, int blocks) {
+  int64_t n = 0;
+  for (int i = 0; i < p.tiled.n; ++i) {
+    const int r = p.tiled.order[i];
+    n += pairs_of(a.q_lens[r], a.kv_lens[r], a.n_heads / a.n_kv_heads, a.causal != 0, blocks);
+  }
+  return n * a.n_kv_heads;
+}
 
-// Whether a request goes to the few-row kernel.  Decided by its own sizes, so that packing does not change a request's kernel.  That kernel reads the
-// keys once for every 16 rows, from L2 behind the first time, at 7 TB/s; the tiled one needs
-// 1.8 us for a key block of a pair of tiles and 2.6 us per pair, and leaves SMs idle where there are few pairs.  17 rows of 32 heads over 8 key heads
-// against 8192 keys, us: tiled 98, few rows 23; 64 rows of 32 heads over as many: 84 and 77.  A request that takes
-// more than twice the device's time that way stays with the tiled kernel, since others beside it would pay for that.
-bool few_rows(int64_t q_len, int64_t kv_len, int64_t group, int64_t kv_heads, int64_t head_dim, bool causal) {
-  const int64_t rows = q_len * group;
-  if (rows <= kRowsMax) return true;
-  if (rows > 512) return false;
-  const double few = static_cast<double>((rows + kRowsMax - 1) / kRowsMax) * kv_heads * kv_len * head_dim * 4 * 1e-6 / 7.0;          // us
-  const double pairs = static_cast<double>(((q_len + 127) / 128 * group + 1) / 2 * kv_heads);
-  const double keys = causal ? std::max<double>(0.0, kv_len - 0.5 * q_len) : static_cast<double>(kv_len);
-  const double each = 2.6 + 1.8 * std::ceil(keys / 128);
-  return few + 2.0 < std::ceil(pairs / 148) * each && few < 2.0 * pairs * each / 148;
+// Estimates in us, from measurements.  The tiled kernel takes 7 us for anything, 1.7 for a key block of a pair of tiles (pairs side by side on the
+// SMs) and 2.6 per pair; the few-row kernel 4 us, 0.45 for 64 keys of a part, and altogether the time to read the keys once for every 16
+// rows, from L2 behind the first time, at 7 TB/s.
+constexpr double kPairBlock = 1.7, kPair = 2.6;
+struct RequestCost { double few, few_chain, blocks, most, pairs; int64_t rows; int r; };
+
+// Which requests go to the few-row kernel: those of up to some number of rows, which is chosen so that the slower of the longest chain of
+// dependent work in either kernel and the work of both spread over the device is least (3 us more where both run).  A lone short prompt of few heads has rows to spread over
+// more CTAs than it has pairs (612 rows of 3 heads: 9 pairs, 18.5 us tiled, 10.7 by rows), a batch of many is better off in tiles.
+int few_of(const dit_prompt_attention_args& a, RequestCost* c, int n) {
+  std::sort(c, c + n, [](const RequestCost& x, const RequestCost& y) { return x.rows != y.rows ? x.rows < y.rows : x.r < y.r; });
+  double blocks = 0, pairs = 0, few = 0, chain = 0, most[DIT_MAX_REQUESTS + 1] = {};
+  for (int i = n - 1; i >= 0; --i) {             // most[i]: longest pair of the requests i ..
+    most[i] = std::max(most[i + 1], c[i].most);
+    blocks += c[i].blocks; pairs += c[i].pairs;
+  }
+  int best = 0;
+  double least = 0;
+  for (int i = 0; i <= n; ++i) {                 // requests 0 .. i - 1 by rows
+    const double work = few + (kPairBlock * blocks + kPair * pairs) / kSms;
+    const double time = std::max({work, i > 0 ? 4 + std::max(few, chain) : 0.0, i < n ? 7 + kPairBlock * most[i] : 0.0}) + (i > 0 && i < n ? 3 : 0);
+    if (i == 0 || time <= least) { best = i; least = time; }
+    if (i == n || c[i].rows > 2048) break;
+    few += c[i].few; chain = std::max(chain, c[i].few_chain); blocks -= c[i].blocks; pairs -= c[i].pairs;
+  }
+  return best;
+}
+
+// Key blocks of an item at most, 0 for whole pairs: cut where the longest pair would outlast the work of all by far, so that few pairs are dealt
+// out to many SMs.  The time of a cut is that of the fullest CTA, as the items will be dealt out, and what the parts cost: their results through
+// memory and a joining kernel.  us whole, and for the cut that is chosen: 8 heads of 64, 3240 rows 45, 33; 4 heads of 128, 8192 rows
+// 101, 77; one head, 16384 rows 190, 78; 128 rows of 32 heads over 8 key heads against 32768 keys 369, 79.
+int choose_parts(const PromptPlan& p, const dit_prompt_attention_args& a, double blocks) {
+  constexpr int kMost = 512;
+  const double chain = kPairBlock * p.most_blocks + kPair, work = (kPairBlock * blocks + kPair * p.pairs) / kSms;
+  if (p.pairs > kMost || chain < 1.3 * work + 8.0) return 0;
+  int length[kMost], n = 0;                      // key blocks of the pairs, most first
+  for (int c = p.most_blocks, before = 0; c >= 0; --c) {
+    const int now = static_cast<int>(pairs_with(p, a, c));
+    for (; before < now; ++before) length[n++] = c;
+  }
+  double least = 0.95 * chain;
+  int best = 0;
+  for (int part = std::max(4, (p.most_blocks + kTileParts - 1) / kTileParts); 3 * part <= 2 * p.most_blocks; part += std::max(1, part / 4)) {
+    double load[kSms] = {}, most = 0;
+    int items = 0;
+    for (int t = 0, m = n; m > 0 && most < least; ++t) {
+      for (int i = 0; i < m; ++i, ++items) {
+        const int round = items / kSms, at = items - round * kSms;
+        double& mine = load[(round & 1) ? kSms - 1 - at : at];
+        mine += kPairBlock * std::min(part, length[i] - t * part) + kPair;
+        most = std::max(most, mine);
+      }
+      while (m > 0 && length[m - 1] <= (t + 1) * part) --m;
+    }
+    const double time = most + 6.0 + 0.06 * items;
+    if (time < least) { least = time; best = part; }
+  }
+  return best;
 }
 
 // Checks sizes and lays the batch out.
@@ -129,44 +184,71 @@ dit_status plan_prompts(const dit_prompt_attention_args& a, PromptPlan* p) {
   if (static_cast<int64_t>(a.n_heads) * a.head_dim > (1 << 20)) return DIT_ERR_SHAPE;
   *p = PromptPlan{};
   const int64_t group = a.n_heads / a.n_kv_heads;
-  int64_t q = 0, kv = 0, keys = 0;
+  const bool causal = a.causal != 0;
+  int64_t q = 0, kv = 0;
+  RequestCost cost[DIT_MAX_REQUESTS];
+  int n = 0;
   for (int r = 0; r <= a.n_requests; ++r) {
     p->tiled.cu_q[r] = p->few.cu_q[r] = static_cast<int>(q);
     p->tiled.cu_kv[r] = p->few.cu_kv[r] = static_cast<int>(kv);
     if (r == a.n_requests) break;
-    if (a.q_lens[r] < 0 || a.kv_lens[r] < 0) return DIT_ERR_INVALID_ARG;
-    q += a.q_lens[r]; kv += a.kv_lens[r];
+    const int64_t q_len = a.q_lens[r], kv_len = a.kv_lens[r];
+    if (q_len < 0 || kv_len < 0) return DIT_ERR_INVALID_ARG;
+    q += q_len; kv += kv_len;
     if (q > kMaxSize || kv > kMaxSize) return DIT_ERR_SHAPE;
-    if (a.q_lens[r] == 0) continue;
-    PromptBatch& b = few_rows(a.q_lens[r], a.kv_lens[r], group, a.n_kv_heads, a.head_dim, a.causal != 0) ? p->few : p->tiled;
+    if (q_len == 0) continue;
+    RequestCost& c = cost[n++];
+    c.r = r; c.rows = q_len * group;
+    c.few = static_cast<double>((c.rows + kRowsMax - 1) / kRowsMax) * a.n_kv_heads * kv_len * a.head_dim * 4 * 1e-6 / 7.0;
+    const double tiles = static_cast<double>((c.rows + kRowsMax - 1) / kRowsMax) * a.n_kv_heads;
+    c.few_chain = 0.45 / 64 * std::max(std::min<double>(kv_len, 256.0), std::min<double>(kv_len, tiles * kv_len / kSms)) + (kv_len > 256 ? 3.0 : 0.0);
+    c.pairs = static_cast<double>(((q_len + 127) / 128 * group + 1) / 2 * a.n_kv_heads);
+    c.most = static_cast<double>((kv_len + 127) / 128);
+    // keys that the row blocks' last rows see: evenly from the first block's to the last one's
+    const double first = causal ? std::max<double>(0.0, std::min<double>(kv_len, kv_len - q_len + std::min<int64_t>(q_len, 128))) : static_cast<double>(kv_len);
+    c.blocks = c.pairs * (0.5 * (first + kv_len) / 128 + 0.5);
+  }
+  const int few = few_of(a, cost, n);
+  double blocks = 0, keys = 0;
+  for (int i = 0; i < n; ++i) {
+    const int r = cost[i].r;
+    PromptBatch& b = i < few ? p->few : p->tiled;
     int at = b.n++;
     for (; at > 0 && a.kv_lens[b.order[at - 1]] < a.kv_lens[r]; --at) b.order[at] = b.order[at - 1];      // most keys first
     b.order[at] = r;
-    if (&b == &p->tiled) {
-      p->most_blocks = std::max(p->most_blocks, (a.kv_lens[r] + 127) / 128);
-      p->items += ((((static_cast<int64_t>(a.q_lens[r]) + 127) / 128) * group + 1) / 2) * a.n_kv_heads;
-    } else {
+    if (i < few) {
       const int64_t tiles = static_cast<int64_t>(a.n_kv_heads) * prompt_row_tiles(a.q_lens[r], static_cast<int>(group));
       p->row_tiles += tiles;
-      keys += tiles * a.kv_lens[r];
+      keys += static_cast<double>(tiles) * a.kv_lens[r];
+    } else {
+      p->most_blocks = std::max(p->most_blocks, static_cast<int>((static_cast<int64_t>(a.kv_lens[r]) + 127) / 128));
+      blocks += cost[i].blocks;
+      p->pairs += ((((static_cast<int64_t>(a.q_lens[r]) + 127) / 128) * group + 1) / 2) * a.n_kv_heads;
     }
   }
-  if (p->items > INT32_MAX / 16) return DIT_ERR_SHAPE;
+  if (p->pairs > INT32_MAX / 16) return DIT_ERR_SHAPE;
+  p->items = p->pairs;
+  if (p->pairs > 0 && (p->part_blocks = choose_parts(*p, a, blocks)) > 0) {
+    p->cut = pairs_with(*p, a, p->part_blocks + 1);
+    for (int t = 1; t * p->part_blocks < p->most_blocks; ++t) p->items += pairs_with(*p, a, t * p->part_blocks + 1);
+  }
   if (p->few.n > 0) {
     // Parts of equal length, one for each SM: what a CTA costs before its first product and after its last one is several us, and one per SM
     // keeps enough loads in flight (one row of 32 heads against 32768 keys, parts of 256, 896, 1792 keys: 60, 34, 29 us).  Beyond 4096 keys
     // a part is only cut off: more CTAs than SMs are resident at once, and share the memory's bandwidth evenly.
-    int64_t chunk = std::max<int64_t>(256, (keys / kFewRowCtas + 63) / 64 * 64);
-    for (const int64_t least = chunk; few_row_ctas(*p, a, static_cast<int>(chunk)) > kFewRowCtas && chunk < 2 * least;) chunk += std::max<int64_t>(64, least / 16 / 64 * 64);
-    chunk = std::min<int64_t>(chunk, 4096);
-    p->chunk = static_cast<int>(chunk);
+    const int least = static_cast<int>(std::min(4096.0, std::max(256.0, std::ceil(keys / kSms / 64) * 64)));
+    int chunk = least;
+    while (few_row_ctas(*p, a, chunk) > kSms && chunk < 2 * least) chunk += std::max(64, least / 16 / 64 * 64);
+    p->chunk = std::min(chunk, 4096);
     p->ctas = few_row_ctas(*p, a, p->chunk);
     if (p->ctas > INT32_MAX / 16) return DIT_ERR_SHAPE;
     p->join = p->ctas > p->row_tiles;
   }
   return DIT_OK;
 }
-size_t part_bytes(const PromptPlan& p, int head_dim) { return p.join ? static_cast<size_t>(p.ctas) * kRowsMax * (head_dim + 4) * sizeof(float) : 0; }
+// Room for the parts of the few-row kernel, then for those of the tiled one.
+size_t few_bytes(const PromptPlan& p, int head_dim) { return p.join ? static_cast<size_t>(p.ctas) * kRowsMax * (head_dim + 4) * sizeof(float) : 0; }
+size_t part_bytes(const PromptPlan& p, int head_dim) { return few_bytes(p, head_dim) + (p.part_blocks > 0 ? static_cast<size_t>(p.items) * 2 * 128 * (head_dim + 4) * sizeof(float) : 0); }
 
 template <int D, bool BF16>
 cudaError_t launch_attention(const OpsDevice& d, const dit_prompt_attention_args& a, const PromptPlan& plan, PromptAttnParams p, cudaStream_t st) {
@@ -182,30 +264,36 @@ cudaError_t launch_attention(const OpsDevice& d, const dit_prompt_attention_args
     if (!half_map(d, &tmQ, a.q, width, q_rows, a.ld_q, 128) || !half_map(d, &tmK, k, kv_width, std::max(kv_rows, 1), ld_k, 128) ||
         !half_map(d, &tmV, v, kv_width, std::max(kv_rows, 1), ld_v, 128))
       return cudaErrorInvalidValue;
-    p.items = static_cast<int>(plan.items); p.most_blocks = plan.most_blocks;
-    prompt_attention_kernel<D, BF16><<<std::min(p.items, d.num_sms), PromptAttnCfg<D>::THREADS, PromptAttnCfg<D>::SMEM_BYTES, st>>>(tmQ, tmK, tmV, p, plan.tiled);
+    p.items = static_cast<int>(plan.items); p.pairs = static_cast<int>(plan.pairs);
+    p.most_blocks = plan.most_blocks; p.part_blocks = plan.part_blocks;
+    p.tile_parts = reinterpret_cast<float*>(static_cast<char*>(a.workspace) + few_bytes(plan, D));
+    const int grid = std::min(p.items, d.num_sms);
+    if (p.part_blocks > 0) prompt_attention_kernel<D, BF16, true><<<grid, PromptAttnCfg<D>::THREADS, PromptAttnCfg<D>::SMEM_BYTES, st>>>(tmQ, tmK, tmV, p, plan.tiled);
+    else prompt_attention_kernel<D, BF16, false><<<grid, PromptAttnCfg<D>::THREADS, PromptAttnCfg<D>::SMEM_BYTES, st>>>(tmQ, tmK, tmV, p, plan.tiled);
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
   }
+  cudaLaunchAttribute at;
+  at.id = cudaLaunchAttributeProgrammaticStreamSerialization;                   // beside the kernel in front; set up while parts are being computed
+  at.val.programmaticStreamSerializationAllowed = 1;
+  auto launch = [&](auto kernel, dim3 grid, int threads, int smem, bool beside, auto... args) {
+    cudaLaunchConfig_t lc = {};
+    lc.gridDim = grid; lc.blockDim = dim3(threads); lc.dynamicSmemBytes = smem; lc.stream = st;
+    lc.attrs = &at; lc.numAttrs = beside ? 1 : 0;
+    return cudaLaunchKernelEx(&lc, kernel, args...);
+  };
   if (plan.few.n > 0) {
     if (!half_map(d, &tmK, k, kv_width, std::max(kv_rows, 1), ld_k, kRowsTile) || !half_map(d, &tmV, v, kv_width, std::max(kv_rows, 1), ld_v, kRowsTile))
       return cudaErrorInvalidValue;
     p.chunk = plan.chunk;
     p.parts = static_cast<float*>(a.workspace);
-    cudaLaunchAttribute at;
-    at.id = cudaLaunchAttributeProgrammaticStreamSerialization;                 // beside the tiled kernel; set up while the parts are being computed
-    at.val.programmaticStreamSerializationAllowed = 1;
-    cudaLaunchConfig_t lc = {};
-    lc.gridDim = dim3(static_cast<unsigned>(plan.ctas)); lc.blockDim = dim3(PromptRowsCfg<D>::THREADS);
-    lc.dynamicSmemBytes = PromptRowsCfg<D>::SMEM_BYTES; lc.stream = st;
-    lc.attrs = &at; lc.numAttrs = plan.items > 0 ? 1 : 0;
-    if ((e = cudaLaunchKernelEx(&lc, &prompt_rows_kernel<D, BF16>, tmK, tmV, p, plan.few)) != cudaSuccess) return e;
-    if (plan.join) {
-      lc = cudaLaunchConfig_t{};
-      lc.gridDim = dim3(static_cast<unsigned>(plan.row_tiles), kRowsMax / kJoinRows); lc.blockDim = dim3(kJoinRows * 32); lc.stream = st;
-      lc.attrs = &at; lc.numAttrs = 1;
-      if ((e = cudaLaunchKernelEx(&lc, &prompt_join_kernel<D, BF16>, p, plan.few)) != cudaSuccess) return e;
-    }
+    if ((e = launch(&prompt_rows_kernel<D, BF16>, dim3(static_cast<unsigned>(plan.ctas)), PromptRowsCfg<D>::THREADS, PromptRowsCfg<D>::SMEM_BYTES, plan.items > 0, tmK, tmV, p, plan.few)) != cudaSuccess)
+      return e;
+    if (plan.join &&
+        (e = launch(&prompt_join_kernel<D, BF16>, dim3(static_cast<unsigned>(plan.row_tiles), kRowsMax / kJoinRows), kJoinRows * 32, 0, true, p, plan.few)) != cudaSuccess)
+      return e;
   }
+  if (plan.part_blocks > 0)
+    return launch(&prompt_tile_join_kernel<D, BF16>, dim3(static_cast<unsigned>(plan.cut), 2 * D / 32), 256, 0, true, p, plan.tiled);
   return cudaSuccess;
 }
 

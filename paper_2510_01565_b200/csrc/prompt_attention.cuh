@@ -28,8 +28,11 @@ struct PromptAttnParams {
   int n_heads, kv_heads, group;
   int causal;
   float scale_log2;          // scale * log2(e), positive
-  int items;                 // tiled kernel: (request, key head, pair of query tiles)
+  int items;                 // tiled kernel: pairs, or their parts
   int most_blocks;           // key blocks of the longest of its requests
+  int pairs;                 // (request, key head, pair of query tiles)
+  int part_blocks;           // key blocks of an item at most (0: a pair is one item)
+  float* tile_parts;         // [items][2][head_dim + 4][128]
   int wide_out;              // rows of out start on 32-byte boundaries
   int* status;
   // few rows
@@ -67,43 +70,63 @@ struct PromptAttnCfg {
 };
 
 // Two query tiles: consecutive ones of the list (last 128-row block first, the heads of the group one after the other) of a request and a key
-// head.  With an even group they are two heads' tiles of the same rows; otherwise also neighbouring row blocks.
+// head.  With an even group they are two heads' tiles of the same rows; otherwise also neighbouring row blocks.  An item is a pair, or, where
+// there are few pairs and long ones, up to part_blocks of its key blocks.
 struct PromptItem {
   int kv_head, q_begin, q_len, kv_begin, kv_len;
   int before;                // keys before the first query row's own (may be negative)
   int head[2], qb[2];
-  int n_kv[2];               // key blocks that a tile's last row sees; n_kv[0] >= n_kv[1]
+  int first, end[2];         // key blocks of the item, per tile (end[1] <= end[0]; none where end <= first)
   int ragged;                // first key block of which some row of a tile sees only a part
   int tile1;
+  int slot;                  // place of its partial results, or -1: it is the whole pair
   __device__ __forceinline__ int limit(int row, int causal) const { return causal ? min(kv_len, before + row + 1) : kv_len; }   // keys of a row
 };
 // Pairs of tiles of a request whose first tile sees `blocks` key blocks or more (they are the request's first ones).
-__device__ __forceinline__ int pairs_with(const PromptBatch& batch, int group, int causal, int i, int blocks) {
-  if (i >= batch.n) return 0;
-  const int r = batch.order[i], q_len = batch.cu_q[r + 1] - batch.cu_q[r], kv_len = batch.cu_kv[r + 1] - batch.cu_kv[r];
+__host__ __device__ inline int pairs_of(int q_len, int kv_len, int group, int causal, int blocks) {
   const int nb = (q_len + 127) >> 7;
   int from = 0;                                // first row block that qualifies
   if (blocks > 0) {
     if (blocks > (kv_len + 127) >> 7) return 0;
-    if (causal) from = max(0, ((128 * (blocks - 1) + 1 - (kv_len - q_len) + 127) >> 7) - 1);
+    if (causal) {
+      from = ((128 * (blocks - 1) + 1 - (kv_len - q_len) + 127) >> 7) - 1;
+      if (from < 0) from = 0;
+    }
   }
   return ((nb - from) * group + 1) >> 1;
 }
-// The item-th item of the batch, most key blocks first, whatever request they belong to; the whole warp looks for it.
+__device__ __forceinline__ int pairs_with(const PromptBatch& batch, int group, int causal, int i, int blocks) {
+  if (i >= batch.n) return 0;
+  const int r = batch.order[i];
+  return pairs_of(batch.cu_q[r + 1] - batch.cu_q[r], batch.cu_kv[r + 1] - batch.cu_kv[r], group, causal, blocks);
+}
+// Pairs of the batch that see `blocks` key blocks or more; the whole warp counts.
+__device__ __forceinline__ int all_pairs_with(const PromptBatch& batch, const PromptAttnParams& p, int blocks, int lane) {
+  const unsigned mine = static_cast<unsigned>(pairs_with(batch, p.group, p.causal, lane, blocks) + (batch.n > 32 ? pairs_with(batch, p.group, p.causal, lane + 32, blocks) : 0));
+  return static_cast<int>(__reduce_add_sync(0xffffffffu, mine)) * p.kv_heads;
+}
+// The item-th item: the first parts of all pairs, most key blocks first, whatever request they belong to, then the second parts of those that
+// have one, and so on.  (The pairs with a t-th part are the first ones of that order.)  The whole warp looks for it.
+template <bool kParts>
 __device__ __forceinline__ PromptItem prompt_item(const PromptBatch& batch, const PromptAttnParams& p, int item, int lane) {
-  auto count = [&](int half, int blocks) { return pairs_with(batch, p.group, p.causal, lane + 32 * half, blocks); };
-  auto all = [&](int blocks) {
-    const unsigned mine = static_cast<unsigned>(count(0, blocks) + (batch.n > 32 ? count(1, blocks) : 0));
-    return static_cast<int>(__reduce_add_sync(0xffffffffu, mine)) * p.kv_heads;
-  };
-  int low = 0, high = p.most_blocks + 1, behind = 0;              // more than `item` items have `low` blocks or more; `behind` of them `high`
+  int layer = 0, rank = item;
+  if constexpr (kParts)
+    for (int n = p.pairs; rank >= n;) {
+      rank -= n;
+      ++layer;
+      n = all_pairs_with(batch, p, layer * p.part_blocks + 1, lane);
+      if (n == 0) break;                       // (no such item)
+    }
+  int low = 0, high = p.most_blocks + 1, behind = 0;              // more than `rank` pairs have `low` blocks or more; `behind` of them `high`
   while (high - low > 1) {
-    const int mid = (low + high) >> 1, n = all(mid);
-    if (n > item) low = mid; else { high = mid; behind = n; }
+    const int mid = (low + high) >> 1, n = all_pairs_with(batch, p, mid, lane);
+    if (n > rank) low = mid; else { high = mid; behind = n; }
   }
-  int rank = item - behind, i = 0, pair = 0, kv_head = 0;         // among the items with exactly `low` blocks
+  rank -= behind;                                                 // among the pairs with exactly `low` blocks
+  int i = 0, pair = 0, kv_head = 0;
   for (int half = 0; half < 2; ++half) {
-    const int first = count(half, high), mine = (count(half, low) - first) * p.kv_heads;
+    const int first = pairs_with(batch, p.group, p.causal, lane + 32 * half, high);
+    const int mine = (pairs_with(batch, p.group, p.causal, lane + 32 * half, low) - first) * p.kv_heads;
     int sum = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -133,10 +156,17 @@ __device__ __forceinline__ PromptItem prompt_item(const PromptBatch& batch, cons
     const int tile = min(2 * pair + t, tiles - 1), back = tile / p.group;
     it.qb[t] = row_blocks - 1 - back;
     it.head[t] = kv_head * p.group + tile - back * p.group;
-    it.n_kv[t] = (max(0, it.limit(min(it.q_len, it.qb[t] * 128 + 128) - 1, p.causal)) + 127) >> 7;
+    it.end[t] = (max(0, it.limit(min(it.q_len, it.qb[t] * 128 + 128) - 1, p.causal)) + 127) >> 7;
   }
-  if (!it.tile1) it.n_kv[1] = 0;
-  it.ragged = p.causal ? max(0, it.limit((it.tile1 ? it.qb[1] : it.qb[0]) * 128, 1)) >> 7 : it.n_kv[0];
+  if (!it.tile1) it.end[1] = 0;
+  it.ragged = p.causal ? max(0, it.limit((it.tile1 ? it.qb[1] : it.qb[0]) * 128, 1)) >> 7 : it.end[0];
+  it.first = layer * p.part_blocks;
+  it.slot = -1;
+  if (kParts && it.end[0] > p.part_blocks) {
+    it.slot = item;
+    it.end[0] = min(it.end[0], it.first + p.part_blocks);
+    it.end[1] = min(it.end[1], it.first + p.part_blocks);
+  }
   return it;
 }
 
@@ -148,7 +178,10 @@ __device__ __forceinline__ PromptItem prompt_item(const PromptBatch& batch, cons
 // A causal tile masks its last block or two.  Scores that a row does not see are dropped before its maximum.  Values that it does not
 // see meet a probability of zero, which an infinity or NaN would turn into NaN: in the blocks that some rows see only in part such values are
 // replaced by zeros in shared memory, and if there was one, the rows that do see it add it to their results at the end.
-template <int D, bool BF16>
+// What bounds it: the softmax chain of two tiles against the products of one S buffer, 1.7 us per key block and pair of tiles, 2.6 us more per pair.
+// 8192 rows, 32 heads of 128 over 8 key heads, causal: 396-430 us (1.28-1.39 PFLOP/s) under the power cap.
+// kParts: items may be parts of pairs.  (A kernel of its own: with it the ordinary one took 4 to 8 % longer, 8192 rows of 32 heads 452 us for 419.)
+template <int D, bool BF16, bool kParts>
 __global__ void __launch_bounds__(PromptAttnCfg<D>::THREADS, 1)
 prompt_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
                         const PromptAttnParams p, const __grid_constant__ PromptBatch batch) {
@@ -226,7 +259,7 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
           for (int i = 0; i < 2; ++i)
             for (int pn = 0; pn < (i == 0 || it.tile1 ? C::NP : 0); ++pn)
               tma_load_2d(base + C::OFF_Q + i * C::TILE_BYTES + pn * C::PANEL, &tmQ, it.head[i] * D + pn * 64, it.q_begin + it.qb[i] * 128, q_full);
-          for (int j = 0; j < it.n_kv[0]; ++j) {
+          for (int j = kParts ? it.first : 0; j < it.end[0]; ++j) {
             const int y = it.kv_begin + j * 128;
             if (!mbar_wait(k_empty(ks), kph, abort_flag)) goto done;
             mbar_arrive_expect_tx(k_full(ks), C::TILE_BYTES);
@@ -253,8 +286,8 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
           if (!take_item(k, it, true)) goto done;
           if (!mbar_wait(q_full, qph, abort_flag)) goto done;
           qph ^= 1u;
-          for (int j = 0; j < it.n_kv[0]; ++j) {
-            const int tiles = j < it.n_kv[1] ? 2 : 1;
+          for (int j = kParts ? it.first : 0; j < it.end[0]; ++j) {
+            const int tiles = j < it.end[1] ? 2 : 1;
             if (!mbar_wait(k_full(ks), kph, abort_flag)) goto done;
             for (int i = 0; i < tiles; ++i) {
               if (u > 0 && !mbar_wait(s_free, (u - 1) & 1u, abort_flag)) goto done;
@@ -324,8 +357,8 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
             __syncwarp();
           }
         };
-        for (int j = 0; j < it.n_kv[0]; ++j) {
-          const int tiles = j < it.n_kv[1] ? 2 : 1;
+        for (int j = kParts ? it.first : 0; j < it.end[0]; ++j) {
+          const int tiles = j < it.end[1] ? 2 : 1;
           const int next = vs + 1 == C::V_STAGES ? 0 : vs + 1;
           if (checked != j) {
             if (!__all_sync(0xffffffffu, mbar_wait(v_full(vs), vph, abort_flag))) goto done;
@@ -341,14 +374,14 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
               __threadfence_block();
 #pragma unroll
               for (int kk = 0; kk < 8; ++kk)
-                umma_f16_ts(tO + i * 128, tP + i * 64 + kk * 8, vd + kk * (2048 >> 4), idesc_pv, j != 0 || kk != 0);
+                umma_f16_ts(tO + i * 128, tP + i * 64 + kk * 8, vd + kk * (2048 >> 4), idesc_pv, j != (kParts ? it.first : 0) || kk != 0);
               if (i == tiles - 1) umma_commit(v_empty(vs));
               umma_commit(o_full(i));
             }
             __syncwarp();
             ++done_uses[i];
             // the next block, while the other tile's P is still being made (looking through it in its own turn cost 3 % of long prompts)
-            if (i == 0 && tiles == 2 && j + 1 < it.n_kv[0] && __all_sync(0xffffffffu, mbar_test_wait(v_full(next), vph ^ (next == 0 ? 1u : 0u)))) look_through(j + 1, next);
+            if (i == 0 && tiles == 2 && j + 1 < it.end[0] && __all_sync(0xffffffffu, mbar_test_wait(v_full(next), vph ^ (next == 0 ? 1u : 0u)))) look_through(j + 1, next);
           }
           vs = next;
           if (vs == 0) vph ^= 1u;
@@ -357,7 +390,7 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
     } else {
       // ------------------------------------------------------------------ the coming items
       for (int k = 0; item_at(k) < p.items; ++k) {
-        const PromptItem it = prompt_item(batch, p, item_at(k), lane);
+        const PromptItem it = prompt_item<kParts>(batch, p, item_at(k), lane);
         if (!__all_sync(0xffffffffu, mbar_wait(item_empty(k & 1), ((k >> 1) & 1u) ^ 1u, abort_flag))) goto done;
         if (lane == 0) {
           *item_slot(k) = it;
@@ -381,12 +414,12 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
     PromptItem it;
     for (int k = 0; item_at(k) < p.items; ++k) {
       if (!take_item(k, it, false)) goto done;
-      const int qb = tile == 0 ? it.qb[0] : it.qb[1], head = tile == 0 ? it.head[0] : it.head[1], n_kv = tile == 0 ? it.n_kv[0] : it.n_kv[1];
+      const int qb = tile == 0 ? it.qb[0] : it.qb[1], head = tile == 0 ? it.head[0] : it.head[1], end = tile == 0 ? it.end[0] : it.end[1];
       const int row = qb * 128 + quarter * 32 + lane;                             // in the request
       const int limit = it.limit(row, p.causal);
       float m_ref = -INFINITY, l = 0.f;
       const uint32_t first_use = use;
-      for (int j = 0; j < n_kv; ++j) {
+      for (int j = kParts ? it.first : 0; j < end; ++j) {
         if (!__all_sync(0xffffffffu, mbar_wait(s_full(tile), use & 1u, abort_flag))) goto done;
         tc_fence_after();
         const int valid = limit - j * 128;   // keys of the block that the row sees (may be <= 0)
@@ -476,6 +509,23 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
         tc_fence_after();
         odd = odd_values[tile] != 0;
       }
+      if (kParts && it.slot >= 0) {            // a part: sums as they are, reference and sum of probabilities (nothing where the tile has no block in it)
+        if (any) {
+          // channel by channel, so that a warp's rows lie side by side
+          float* to = p.tile_parts + (static_cast<long long>(it.slot) * 2 + tile) * (D + 4) * 128 + quarter * 32 + lane;
+#pragma unroll 1
+          for (int ch = 0; ch < D / 32; ++ch) {
+            uint32_t r[32];
+            __syncwarp();
+            tmem_ld32(tOi + ch * 32, r);
+            tmem_ld_wait();
+#pragma unroll
+            for (int i = 0; i < 32; ++i) to[(ch * 32 + i) * 128] = __uint_as_float(r[i]);
+          }
+          to[D * 128] = m_ref; to[(D + 1) * 128] = l; to[(D + 2) * 128] = odd ? 1.f : 0.f;
+        }
+        continue;
+      }
       const float inv = l == 0.f ? 0.f : 1.0f / l;
       // The results of 32 channels at a time; `kept` writes infinities as such, with the replaced values that the row sees, and is a second
       // pass over the rare rows that have one, so that the ordinary one pays for the largest magnitude only.
@@ -551,7 +601,7 @@ done:
 // tiles of 64 keys through one ring, four warps with 16 keys of every tile each, warp-level products, the warps' results joined in
 // shared memory.  A request with one chunk writes its rows; the parts of the others go to memory as (sums, maximum, sum of
 // probabilities) and prompt_join_kernel joins them in their order.
-// 32 heads of 128 over 8 key heads, us: one row against 32768 keys (134 MB) 28, of which 3 are the joining; 64 rows of 64 requests against 4096 keys
+// 32 heads of 128 over 8 key heads, us: one row against 32768 keys (134 MB) 28, of which 3 are the joining kernel; 64 rows of 64 requests against 4096 keys
 // each (1.07 GB) 153 = 7.0 TB/s, part of it from L2.  Heads of 64 take half the bytes and nearly the same time per key (23 us): a tile's waits and
 // dependent steps, not its bytes, are the bound there.
 // ------------------------------------------------------------------------------------------------
@@ -899,6 +949,70 @@ prompt_join_kernel(const PromptAttnParams p, const __grid_constant__ PromptBatch
   const float inv = sum == 0.f ? 0.f : 1.0f / sum;
   if (c < D)
     prompt_store<BF16>(p, w, w.row0 + row, c, D, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv), prompt_limit(w, p, w.row0 / p.group), odd != 0.f);
+}
+
+// For a tile of a pair with several parts and 32 of its channels: a thread per row and 16 channels.  grid: (pairs, 2 tiles x head_dim / 32).
+constexpr int kTileParts = 32;                 // parts of a pair at most
+template <int D, bool BF16>
+__global__ void __launch_bounds__(256)
+prompt_tile_join_kernel(const PromptAttnParams p, const __grid_constant__ PromptBatch batch) {
+  __shared__ PromptItem item;
+  __shared__ int slot_of[kTileParts];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, tile = blockIdx.y / (D / 32);
+  if (warp == 0) {
+    const PromptItem it = prompt_item<true>(batch, p, blockIdx.x, lane);          // the pair's first part
+    if (lane == 0) item = it;
+    int n = p.pairs, base = 0;
+    for (int t = 0; t < kTileParts && n > static_cast<int>(blockIdx.x); ++t) {    // (the pairs with a t-th part: the first n)
+      if (lane == 0) slot_of[t] = base + blockIdx.x;
+      base += n;
+      n = all_pairs_with(batch, p, (t + 1) * p.part_blocks + 1, lane);
+    }
+  }
+  __syncthreads();
+  const PromptItem it = item;
+  const int qb = tile == 0 ? it.qb[0] : it.qb[1], head = tile == 0 ? it.head[0] : it.head[1];
+  const int blocks = (max(0, it.limit(min(it.q_len, qb * 128 + 128) - 1, p.causal)) + 127) >> 7;
+  const int parts = (blocks + p.part_blocks - 1) / p.part_blocks;
+  const int in = threadIdx.x & 127, row = qb * 128 + in, c = blockIdx.y % (D / 32) * 32 + (threadIdx.x >> 7) * 16;
+  if ((tile == 1 && !it.tile1) || row >= it.q_len) return;
+  asm volatile("griddepcontrol.wait;" ::: "memory");                    // the parts are complete
+  auto part = [&](int t) { return p.tile_parts + (static_cast<long long>(slot_of[t]) * 2 + tile) * (D + 4) * 128 + in; };
+  float top = -INFINITY, odd = 0.f;
+#pragma unroll 4
+  for (int t = 0; t < parts; ++t) {
+    top = fmaxf(top, part(t)[D * 128]);
+    odd = fmaxf(odd, part(t)[(D + 2) * 128]);
+  }
+  const float at = top == -INFINITY ? 0.f : top;
+  float sum = 0.f, o[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) o[i] = 0.f;
+#pragma unroll 2
+  for (int t = 0; t < parts; ++t) {
+    const float* from = part(t);
+    const float f = exp2_approx((from[D * 128] - at) * p.scale_log2);
+    sum += from[(D + 1) * 128] * f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[i] = fmaf(from[(c + i) * 128], f, o[i]);
+  }
+  const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) o[i] *= inv;
+  if (odd != 0.f) {                            // values were replaced in the blocks that rows see in part: those that this row sees are added
+    const int limit = it.limit(row, p.causal);
+    const uint16_t* v = p.v + (static_cast<long long>(it.kv_begin) + it.ragged * 128) * p.ld_v + it.kv_head * D + c;
+    for (int key = it.ragged * 128; key < limit; ++key, v += p.ld_v)
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (odd_bits<BF16>(__ldg(v + i))) o[i] += widen16bit<BF16>(__ldg(v + i));
+  }
+  uint32_t w[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) w[i] = put_infinities<BF16>(pack16x2<BF16>(o[2 * i], o[2 * i + 1]), o[2 * i], o[2 * i + 1]);
+  uint4* out = reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.out) + (static_cast<long long>(it.q_begin) + row) * p.ld_out + head * D + c);
+  out[0] = make_uint4(w[0], w[1], w[2], w[3]);
+  out[1] = make_uint4(w[4], w[5], w[6], w[7]);
 }
 
 }  // namespace dit
