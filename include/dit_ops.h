@@ -146,10 +146,12 @@ dit_status dit_block_attention(const dit_attention_batch *batch, const int32_t *
  *   scales      device bytes, 16-byte aligned, dit_fp4_scale_bytes(rows, cols, group): tiles of 128 rows x 4 groups, 512 bytes each,
  *               [ceil(rows / 128)][ceil(cols / (4 * group))], in them byte (row % 32) * 16 + (row % 128) / 32 * 4 + group % 4:
  *               the e4m3 number s (group 16; its sign bit is 0) or e + 127 (group 32; 255 is NaN).  The quantisers write whole tiles, zeros
- *               where there is no row or group; scales that a caller makes need finite values for the groups behind a row's last one
+ *               where there is no row or group; scales that a caller makes need finite values for the groups behind a row's last one up to
+ *               its tile's end
  *   row_scales  device fp32 [rows]: 2^e (group 16).  NULL (group 32)
  * A row (group 16) or group (group 32) that holds a NaN or an infinity gets codes 0 and a NaN row scale or scale.
- * cols, k, rows >= 1 unless stated otherwise, at most 2^31 - 1024 (DIT_ERR_SHAPE); other groups are DIT_ERR_INVALID_ARG. */
+ * cols, k and n are at least 1 and at most 2^30, rows and m at most 2^31 - 1024 (DIT_ERR_SHAPE); other groups are DIT_ERR_INVALID_ARG.  Results
+ * must not overlap what they are made from. */
 
 /* Bytes of the scales of a [rows, cols] matrix; 0 for sizes or groups that the calls below refuse. */
 size_t dit_fp4_scale_bytes(int64_t rows, int64_t cols, int32_t group);

@@ -12,6 +12,7 @@ using namespace dit;
 namespace {
 
 constexpr int64_t kMaxSize = INT32_MAX - 1024;
+constexpr int64_t kMaxCols = 1 << 30;            // of a row: places in it, a CTA's stride further on, are counted in 32 bits
 
 int type_bytes(dit_type t) { return t == DIT_TYPE_F32 ? 4 : 2; }
 bool type_ok(dit_type t) { return t == DIT_TYPE_F16 || t == DIT_TYPE_BF16 || t == DIT_TYPE_F32; }
@@ -215,7 +216,7 @@ dit_status status_of(cudaError_t e) { return e == cudaSuccess ? DIT_OK : DIT_ERR
 dit_status check_matrix(int64_t rows, int64_t cols, int32_t group) {
   if (group != 16 && group != 32) return DIT_ERR_INVALID_ARG;
   if (rows < 0) return DIT_ERR_INVALID_ARG;
-  if (cols < 1 || cols > kMaxSize || rows > kMaxSize) return DIT_ERR_SHAPE;
+  if (cols < 1 || cols > kMaxCols || rows > kMaxSize) return DIT_ERR_SHAPE;
   // tiles of 128 x 128 (64 x 128 of a weight) are counted in 32 bits
   if (((rows + 127) / 128) * ((cols + 127) / 128) > INT32_MAX / 16) return DIT_ERR_SHAPE;
   return DIT_OK;

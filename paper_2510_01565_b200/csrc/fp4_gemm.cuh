@@ -261,6 +261,7 @@ gemm_fp4_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
     uint8_t* box = aligned + C::OFF_OUT + (warp - 4) * BOX_BYTES;
     float* col_of = reinterpret_cast<float*>(aligned + C::OFF_COL + chalf * COL_BYTES);      // factors, then bias
     const uint64_t policy = evict_first_policy();
+    bool ok = true;                            // after a failed wait the warps still meet at their barriers, tile after tile
     int n = 0;
     for (int t = pair; t < num_tiles; t += num_pairs, ++n) {
       const int buf = n & 1;
@@ -277,7 +278,8 @@ gemm_fp4_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
         col_of[128 + c] = b;
         asm volatile("bar.sync %0, 128;" ::"r"(1 + chalf) : "memory");
       }
-      if (!__all_sync(0xffffffffu, mbar_wait(tfull_bar(buf), (n >> 1) & 1u, abort_flag))) goto done;
+      ok = ok && __all_sync(0xffffffffu, mbar_wait(tfull_bar(buf), (n >> 1) & 1u, abort_flag));
+      if (!ok) continue;
       tc_fence_after();
       float2 acc[64];
       const uint32_t from = acc_of(buf) + lane_sel + chalf * 128;

@@ -227,7 +227,7 @@ quantize_fp4_kernel(const Fp4QuantParams p) {
       const float top = In::from_bits(bits);
       const GroupScale g = group_scale<kGroup>(top, up, kGroup == 32 ? !(top < INFINITY) : bad);
       // (THREADS * EPL columns are whole tiles of four groups: 512 bytes each)
-      if (c < wide && (at % LPG) == 0) scale[(base / EPL + i * THREADS) / (4 * LPG) * 512] = there && c < p.cols ? static_cast<uint8_t>(g.byte) : 0;
+      if (c < wide && (at % LPG) == 0) scale[static_cast<long long>((base / EPL + i * THREADS) / (4 * LPG)) * 512] = there && c < p.cols ? static_cast<uint8_t>(g.byte) : 0;
       if (there && c < p.cols) {
         float v[EPL];
         In::widen16(raw[i], v);

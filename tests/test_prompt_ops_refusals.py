@@ -37,7 +37,7 @@ def test_quantiser_refusals(lib, weight):
     bad += [dict(ldc=112)] if weight else [dict(ldc=176), dict(a=-1)]
     for kw in bad:                                       # (group 32 has no row scales: a pointer to some is refused)
         assert call(**kw) == INVALID, kw
-    for kw in (dict(a=BIG), dict(b=BIG), dict(a=2 ** 30, b=2 ** 30, ld=2 ** 30, ldc=2 ** 30), dict(b=0), dict(b=-3)) + ((dict(a=0),) if weight else ()):
+    for kw in (dict(a=2 ** 30 + 1, ld=2 ** 31, ldc=2 ** 30) if weight else dict(b=2 ** 30 + 1, ld=2 ** 31, ldc=2 ** 30), dict(a=BIG), dict(b=BIG), dict(a=2 ** 30, b=2 ** 30, ld=2 ** 30, ldc=2 ** 30), dict(b=0), dict(b=-3)) + ((dict(a=0),) if weight else ()):
         assert call(**kw) == SHAPE, kw
     if not weight:
         assert call(a=0) == OK and call(a=0, x=None, codes=None) == OK and call(a=0, group=7) == INVALID
@@ -66,7 +66,7 @@ def test_product_refusals(lib):
     for kw in (dict(type=3), dict(group=4), dict(m=-1), dict(lda=112), dict(lda=136), dict(ldb=120), dict(ld_out=63), dict(a=P + 8), dict(b=P + 1), dict(a_scales=P + 8),
                dict(b_scales=P + 1), dict(a_rows=P + 1), dict(b_rows=P + 2), dict(bias=P + 2), dict(out=P + 1), dict(out=P + 2, type=2)):
         assert call(**kw) == INVALID, kw
-    for kw in (dict(n=0), dict(k=0), dict(n=-3), dict(m=BIG), dict(n=BIG), dict(k=BIG), dict(m=2 ** 30, n=2 ** 30, ld_out=2 ** 30)):
+    for kw in (dict(n=0), dict(k=0), dict(n=-3), dict(m=BIG), dict(n=2 ** 30 + 1), dict(k=2 ** 30 + 1), dict(m=2 ** 30, n=2 ** 30, ld_out=2 ** 30)):
         assert call(**kw) == SHAPE, kw
     assert call(m=0, a=None, out=None) == OK
     assert lib.dit_gemm_fp4(None, None) == INVALID
