@@ -95,10 +95,12 @@ cudaError_t launch_split(const CUtensorMap& tmA, const CUtensorMap& tmB, const d
   cudaLaunchConfig_t lc = {};
   lc.gridDim = dim3(static_cast<unsigned>(tiles * splits)); lc.blockDim = dim3(C::THREADS);
   lc.dynamicSmemBytes = C::SMEM_BYTES; lc.stream = st;
-  cudaLaunchAttribute at;
-  at.id = cudaLaunchAttributeClusterDimension;
-  at.val.clusterDim.x = splits; at.val.clusterDim.y = 1; at.val.clusterDim.z = 1;
-  lc.attrs = &at; lc.numAttrs = splits > 1 ? 1 : 0;
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  at[1].id = cudaLaunchAttributeClusterDimension;
+  at[1].val.clusterDim.x = splits; at[1].val.clusterDim.y = 1; at[1].val.clusterDim.z = 1;
+  lc.attrs = at; lc.numAttrs = splits > 1 ? 2 : 1;
   return cudaLaunchKernelEx(&lc, &gemm_fp4_split_kernel<EPI, G, BT>, tmA, tmB, static_cast<const uint8_t*>(a.a_scales), static_cast<const uint8_t*>(a.b_scales), p, splits);
 }
 
@@ -146,8 +148,7 @@ cudaError_t launch_product(const OpsDevice& d, int pairs, const dit_gemm_fp4_arg
   CUtensorMap tmOut = tmA;                       // unused where the output is written directly
   if (p.vec_out && !out_map(d, &tmOut, a.out, a.out_type, p.N, p.M, a.ld_out)) return cudaErrorInvalidValue;
   const int grid = 2 * static_cast<int>(std::min<long long>(pair_tiles, pairs));
-  gemm_fp4_pair_kernel<EPI, G><<<grid, fgemm::THREADS, fgemm::Cfg<G>::SMEM_BYTES, st>>>(tmA, tmB, tmSA, tmSB, tmOut, p);
-  return cudaGetLastError();
+  return launch_overlapping(&gemm_fp4_pair_kernel<EPI, G>, dim3(grid), fgemm::THREADS, fgemm::Cfg<G>::SMEM_BYTES, st, tmA, tmB, tmSA, tmSB, tmOut, p);
 }
 
 template <int G>
@@ -162,11 +163,10 @@ cudaError_t launch_rows(const Fp4QuantParams& p, long long loads, cudaStream_t s
   constexpr int CTA = THREADS == 32 ? 256 : THREADS, PER = CTA / THREADS;
   const unsigned grid = (static_cast<unsigned>((static_cast<long long>(p.rows) + 127) / 128 * 128) + PER - 1) / PER;
   const long long each = (loads + THREADS - 1) / THREADS;
-  if (each <= 1) quantize_fp4_kernel<kType, G, kVec, THREADS, 1><<<grid, CTA, 0, st>>>(p);
-  else if (each <= 2) quantize_fp4_kernel<kType, G, kVec, THREADS, 2><<<grid, CTA, 0, st>>>(p);
-  else if (each <= 4) quantize_fp4_kernel<kType, G, kVec, THREADS, 4><<<grid, CTA, 0, st>>>(p);
-  else quantize_fp4_kernel<kType, G, kVec, THREADS, 6><<<grid, CTA, 0, st>>>(p);
-  return cudaGetLastError();
+  if (each <= 1) return launch_overlapping(&quantize_fp4_kernel<kType, G, kVec, THREADS, 1>, dim3(grid), CTA, 0, st, p);
+  if (each <= 2) return launch_overlapping(&quantize_fp4_kernel<kType, G, kVec, THREADS, 2>, dim3(grid), CTA, 0, st, p);
+  if (each <= 4) return launch_overlapping(&quantize_fp4_kernel<kType, G, kVec, THREADS, 4>, dim3(grid), CTA, 0, st, p);
+  return launch_overlapping(&quantize_fp4_kernel<kType, G, kVec, THREADS, 6>, dim3(grid), CTA, 0, st, p);
 }
 template <int kType, int G, bool kVec>
 cudaError_t launch_quant(const Fp4QuantParams& p, cudaStream_t st) {
@@ -195,19 +195,16 @@ cudaError_t launch_weight(const Fp4QuantWeightParams& p, int group, cudaStream_t
     const unsigned columns = static_cast<unsigned>((static_cast<long long>(p.out_dim) + 63) / 64) * static_cast<unsigned>((static_cast<long long>(p.in_dim) + kColumnRows - 1) / kColumnRows);
     fp4_column_scales_kernel<kType, kVec><<<columns, 256, 0, st>>>(p);
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
-    quantize_weight_fp4_kernel<kType, 16, kVec><<<grid, 256, 0, st>>>(p);
-  } else {
-    quantize_weight_fp4_kernel<kType, 32, kVec><<<grid, 256, 0, st>>>(p);
+    return launch_overlapping(&quantize_weight_fp4_kernel<kType, 16, kVec>, dim3(grid), 256, 0, st, p);
   }
-  return cudaGetLastError();
+  return launch_overlapping(&quantize_weight_fp4_kernel<kType, 32, kVec>, dim3(grid), 256, 0, st, p);
 }
 
 template <int kType, int G>
 cudaError_t launch_values(const Fp4ValuesParams& p, bool vec, cudaStream_t st) {
   const unsigned grid = static_cast<unsigned>((static_cast<long long>(p.rows) + kValueRows - 1) / kValueRows * ((static_cast<long long>(p.cols) + kValueCols - 1) / kValueCols));
-  if (vec) dequantize_fp4_kernel<kType, G, true><<<grid, 256, 0, st>>>(p);
-  else dequantize_fp4_kernel<kType, G, false><<<grid, 256, 0, st>>>(p);
-  return cudaGetLastError();
+  if (vec) return launch_overlapping(&dequantize_fp4_kernel<kType, G, true>, dim3(grid), 256, 0, st, p);
+  return launch_overlapping(&dequantize_fp4_kernel<kType, G, false>, dim3(grid), 256, 0, st, p);
 }
 
 dit_status status_of(cudaError_t e) { return e == cudaSuccess ? DIT_OK : DIT_ERR_CUDA; }

@@ -189,6 +189,8 @@ gemm_fp4_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
   __syncthreads();
   cluster_sync_all();
   tc_fence_after();
+  dependents_may_start();
+  await_predecessor();
   const uint32_t tmem_base = *tmem_slot;
   auto acc_of = [&](int b) { return tmem_base + b * (BN - kOverlap); };
 
@@ -269,10 +271,10 @@ gemm_fp4_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
       tile_coords(t, num_m, num_n, p.band, mb, nb);
       const int row0 = mb * (2 * BM) + rank * BM + quarter * 32, n0 = nb * BN + chalf * 128;
       const bool mine = n0 < p.N && row0 < p.M;                        // something of this warp's part exists (warp-uniform)
-      const float fr = p.ra && row0 + lane < p.M ? __ldg(p.ra + row0 + lane) : 1.f;
+      const float fr = p.ra && row0 + lane < p.M ? p.ra[row0 + lane] : 1.f;
       {
         const int c = quarter * 32 + lane;                             // the four warps of these columns fetch 32 each
-        const float f = p.rb && n0 + c < p.N ? __ldg(p.rb + n0 + c) : 1.f, b = p.bias && n0 + c < p.N ? __ldg(p.bias + n0 + c) : 0.f;
+        const float f = p.rb && n0 + c < p.N ? p.rb[n0 + c] : 1.f, b = p.bias && n0 + c < p.N ? p.bias[n0 + c] : 0.f;
         asm volatile("bar.sync %0, 128;" ::"r"(1 + chalf) : "memory"); // the last tile's have been read
         col_of[c] = f;
         col_of[128 + c] = b;
@@ -431,8 +433,11 @@ gemm_fp4_split_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_cons
     mbar_init(tfull_bar, 1);
     *abort_flag = 0;
     fence_mbar_init();
+    prefetch_tmap(&tmA); prefetch_tmap(&tmB);
+    await_predecessor();
     for (int s = 0; s < min(C::STAGES, g1 - g0); ++s) load(g0 + s, s);
   }
+  dependents_may_start();
   if (warp == 1) { tmem_alloc(smem_u32(tmem_slot), C::COLS); tmem_relinquish(); }
   tc_fence_before();
   __syncthreads();
@@ -483,11 +488,12 @@ gemm_fp4_split_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_cons
     }
   } else {
     // what the sums are finished with is fetched under the stream
+    await_predecessor();
     const int row = threadIdx.x - 64;
-    if (row < BT) row_of[row] = p.ra && m0 + row < p.M ? __ldg(p.ra + m0 + row) : 1.f;
+    if (row < BT) row_of[row] = p.ra && m0 + row < p.M ? p.ra[m0 + row] : 1.f;
     if (col < p.N) {
-      fc = p.rb ? __ldg(p.rb + col) : 1.f;
-      bias = p.bias ? __ldg(p.bias + col) : 0.f;
+      fc = p.rb ? p.rb[col] : 1.f;
+      bias = p.bias ? p.bias[col] : 0.f;
     }
     asm volatile("bar.sync 1, 128;" ::: "memory");
     const bool ok = __all_sync(0xffffffffu, mbar_wait(tfull_bar, 0, abort_flag));

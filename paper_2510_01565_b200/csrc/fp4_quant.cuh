@@ -122,13 +122,13 @@ __device__ __forceinline__ uint4 load_run(const typename QuantIn<kType>::Elem* s
   if (n >= EPL) {
     if constexpr (kVec) return load_once(src);
     if constexpr (kType == 2) {
-      return make_uint4(__float_as_uint(__ldg(src)), __float_as_uint(__ldg(src + 1)), __float_as_uint(__ldg(src + 2)), __float_as_uint(__ldg(src + 3)));
+      return make_uint4(__float_as_uint(*src), __float_as_uint(src[1]), __float_as_uint(src[2]), __float_as_uint(src[3]));
     } else {
       const uintptr_t at = reinterpret_cast<uintptr_t>(src);
       const uint32_t* words = reinterpret_cast<const uint32_t*>(at & ~static_cast<uintptr_t>(3));
-      if (!(at & 2)) return make_uint4(__ldg(words), __ldg(words + 1), __ldg(words + 2), __ldg(words + 3));
+      if (!(at & 2)) return make_uint4(words[0], words[1], words[2], words[3]);
       if (before && n > EPL) {
-        const uint32_t w0 = __ldg(words), w1 = __ldg(words + 1), w2 = __ldg(words + 2), w3 = __ldg(words + 3), w4 = __ldg(words + 4);
+        const uint32_t w0 = words[0], w1 = words[1], w2 = words[2], w3 = words[3], w4 = words[4];
         return make_uint4(__funnelshift_r(w0, w1, 16), __funnelshift_r(w1, w2, 16), __funnelshift_r(w2, w3, 16), __funnelshift_r(w3, w4, 16));
       }
     }
@@ -167,6 +167,8 @@ quantize_fp4_kernel(const Fp4QuantParams p) {
   constexpr int EPL = In::EPL, LPG = kGroup / EPL;                // lanes per group
   constexpr int CTA = THREADS == 32 ? 256 : THREADS;
   __shared__ uint32_t warp_top[CTA / 32];
+  dependents_may_start();
+  await_predecessor();
   const int at = threadIdx.x % THREADS;                           // lane of the row
   const long long row_l = static_cast<long long>(blockIdx.x) * (CTA / THREADS) + threadIdx.x / THREADS;
   const int padded = (p.rows + 127) / 128 * 128;
@@ -263,6 +265,7 @@ fp4_column_scales_kernel(const Fp4QuantWeightParams p) {
   using In = QuantIn<kType>;
   constexpr int EPL = In::EPL, LPR = 64 / EPL, RPI = 256 / LPR;    // lanes per row, rows per iteration
   __shared__ uint32_t tops[64];
+  dependents_may_start();
   const int tiles = (p.out_dim + 63) / 64;
   const int col0 = blockIdx.x % tiles * 64;
   const long long row0 = static_cast<long long>(blockIdx.x / tiles) * kColumnRows;
@@ -310,6 +313,8 @@ quantize_weight_fp4_kernel(const Fp4QuantWeightParams p) {
   constexpr int PITCH = kWeightOut + (kType == 2 ? 1 : 2), SHIFT = kGroup == 32 ? 8 : 4;
   auto place = [](int r) { return r * PITCH + r / kGroup * SHIFT; };
   __shared__ Elem tile[kIn * PITCH + kIn / kGroup * SHIFT];
+  dependents_may_start();
+  await_predecessor();
   const int out_tiles = (p.out_dim + 127) / 128 * 2;               // whole scale tiles
   const int n0 = blockIdx.x % out_tiles * kWeightOut;
   const int k0 = blockIdx.x / out_tiles * kIn;
@@ -401,6 +406,8 @@ dequantize_fp4_kernel(const Fp4ValuesParams p) {
   constexpr int TURNS = kValueRows / 8;
   const int col_tiles = (p.cols + kValueCols - 1) / kValueCols;
   __shared__ float lines[kVec ? 1 : 8][kVec ? 1 : 32 * 9];
+  dependents_may_start();
+  await_predecessor();
   const int lane = threadIdx.x & 31;
   const int row0 = blockIdx.x / col_tiles * kValueRows + (threadIdx.x >> 5), c = blockIdx.x % col_tiles * kValueCols + lane * 8;
   if (kVec && c >= p.cols) return;
@@ -414,10 +421,10 @@ dequantize_fp4_kernel(const Fp4ValuesParams p) {
     code[i] = 0; byte[i] = 0; factor[i] = 1.f;
     if (row >= p.rows) continue;
     const uint8_t* src = codes + i * 8 * p.ld_codes;
-    if (bytes == 4) code[i] = __ldg(reinterpret_cast<const uint32_t*>(src));
+    if (bytes == 4) code[i] = *reinterpret_cast<const uint32_t*>(src);
     else for (int b = 0; b < bytes; ++b) code[i] |= static_cast<uint32_t>(src[b]) << (8 * b);
-    if (bytes > 0) byte[i] = __ldg(p.scales + scale_at(row, c / kGroup, p.chunks));
-    if (p.row_scales) factor[i] = __ldg(p.row_scales + row);
+    if (bytes > 0) byte[i] = p.scales[scale_at(row, c / kGroup, p.chunks)];
+    if (p.row_scales) factor[i] = p.row_scales[row];
   }
 #pragma unroll
   for (int i = 0; i < TURNS; ++i) {

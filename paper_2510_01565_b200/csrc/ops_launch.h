@@ -41,6 +41,18 @@ struct OpsDevice {
   EncodeTiledFn encode;
 };
 dit_status ops_device(OpsDevice* d);
+
+// Launches a kernel that calls await_predecessor() before it touches memory: it may set itself up while the kernel in front of it ends.
+template <class... Params, class... Args>
+cudaError_t launch_overlapping(void (*kernel)(Params...), dim3 grid, int threads, int smem, cudaStream_t st, Args... args) {
+  cudaLaunchConfig_t lc = {};
+  lc.gridDim = grid; lc.blockDim = dim3(threads); lc.dynamicSmemBytes = smem; lc.stream = st;
+  cudaLaunchAttribute at;
+  at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at.val.programmaticStreamSerializationAllowed = 1;
+  lc.attrs = &at; lc.numAttrs = 1;
+  return cudaLaunchKernelEx(&lc, kernel, Params(args)...);
+}
 cudaError_t launch_block_product(const BlockProduct& b, const SeqInfo& seq, cudaStream_t st);
 // dit_block_attention with a status word of the caller's.  clamp: infinite results become the largest finite value, as in every
 // activation of a step, where an infinity would meet zeros further on.

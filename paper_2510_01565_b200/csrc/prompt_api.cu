@@ -23,13 +23,12 @@ template <int kType, int kBytes, bool kInterleaved>
 cudaError_t launch_rotary(const RotaryParams& p, int units, cudaStream_t st) {
   const unsigned grid = static_cast<unsigned>((p.rows + p.rows_per_cta - 1) / p.rows_per_cta);
   switch (units) {
-    case 4: rotary_kernel<kType, 4, kBytes, kInterleaved><<<grid, kRotaryThreads, 0, st>>>(p); break;
-    case 8: rotary_kernel<kType, 8, kBytes, kInterleaved><<<grid, kRotaryThreads, 0, st>>>(p); break;
-    case 16: rotary_kernel<kType, 16, kBytes, kInterleaved><<<grid, kRotaryThreads, 0, st>>>(p); break;
-    case 32: rotary_kernel<kType, 32, kBytes, kInterleaved><<<grid, kRotaryThreads, 0, st>>>(p); break;
-    default: rotary_kernel<kType, 0, 16, kInterleaved><<<grid, kRotaryThreads, 0, st>>>(p);
+    case 4: return launch_overlapping(&rotary_kernel<kType, 4, kBytes, kInterleaved>, dim3(grid), kRotaryThreads, 0, st, p);
+    case 8: return launch_overlapping(&rotary_kernel<kType, 8, kBytes, kInterleaved>, dim3(grid), kRotaryThreads, 0, st, p);
+    case 16: return launch_overlapping(&rotary_kernel<kType, 16, kBytes, kInterleaved>, dim3(grid), kRotaryThreads, 0, st, p);
+    case 32: return launch_overlapping(&rotary_kernel<kType, 32, kBytes, kInterleaved>, dim3(grid), kRotaryThreads, 0, st, p);
+    default: return launch_overlapping(&rotary_kernel<kType, 0, 16, kInterleaved>, dim3(grid), kRotaryThreads, 0, st, p);
   }
-  return cudaGetLastError();
 }
 template <int kType>
 cudaError_t launch_rotary(RotaryParams p, const dit_rotary_args& a, cudaStream_t st) {
@@ -268,32 +267,26 @@ cudaError_t launch_attention(const OpsDevice& d, const dit_prompt_attention_args
     p.most_blocks = plan.most_blocks; p.part_blocks = plan.part_blocks;
     p.tile_parts = reinterpret_cast<float*>(static_cast<char*>(a.workspace) + few_bytes(plan, D));
     const int grid = std::min(p.items, d.num_sms);
-    if (p.part_blocks > 0) prompt_attention_kernel<D, BF16, true><<<grid, PromptAttnCfg<D>::THREADS, PromptAttnCfg<D>::SMEM_BYTES, st>>>(tmQ, tmK, tmV, p, plan.tiled);
-    else prompt_attention_kernel<D, BF16, false><<<grid, PromptAttnCfg<D>::THREADS, PromptAttnCfg<D>::SMEM_BYTES, st>>>(tmQ, tmK, tmV, p, plan.tiled);
+    auto kernel = p.part_blocks > 0 ? &prompt_attention_kernel<D, BF16, true> : &prompt_attention_kernel<D, BF16, false>;
+    // (beside the few-row kernel, which starts under this one and does not wait for what is in front of both, the ordinary launch)
+    if (plan.few.n > 0) kernel<<<grid, PromptAttnCfg<D>::THREADS, PromptAttnCfg<D>::SMEM_BYTES, st>>>(tmQ, tmK, tmV, p, plan.tiled);
+    else if ((e = launch_overlapping(kernel, dim3(grid), PromptAttnCfg<D>::THREADS, PromptAttnCfg<D>::SMEM_BYTES, st, tmQ, tmK, tmV, p, plan.tiled)) != cudaSuccess) return e;
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
   }
-  cudaLaunchAttribute at;
-  at.id = cudaLaunchAttributeProgrammaticStreamSerialization;                   // beside the kernel in front; set up while parts are being computed
-  at.val.programmaticStreamSerializationAllowed = 1;
-  auto launch = [&](auto kernel, dim3 grid, int threads, int smem, bool beside, auto... args) {
-    cudaLaunchConfig_t lc = {};
-    lc.gridDim = grid; lc.blockDim = dim3(threads); lc.dynamicSmemBytes = smem; lc.stream = st;
-    lc.attrs = &at; lc.numAttrs = beside ? 1 : 0;
-    return cudaLaunchKernelEx(&lc, kernel, args...);
-  };
   if (plan.few.n > 0) {
     if (!half_map(d, &tmK, k, kv_width, std::max(kv_rows, 1), ld_k, kRowsTile) || !half_map(d, &tmV, v, kv_width, std::max(kv_rows, 1), ld_v, kRowsTile))
       return cudaErrorInvalidValue;
     p.chunk = plan.chunk;
     p.parts = static_cast<float*>(a.workspace);
-    if ((e = launch(&prompt_rows_kernel<D, BF16>, dim3(static_cast<unsigned>(plan.ctas)), PromptRowsCfg<D>::THREADS, PromptRowsCfg<D>::SMEM_BYTES, plan.items > 0, tmK, tmV, p, plan.few)) != cudaSuccess)
+    p.beside = plan.items > 0;
+    if ((e = launch_overlapping(&prompt_rows_kernel<D, BF16>, dim3(static_cast<unsigned>(plan.ctas)), PromptRowsCfg<D>::THREADS, PromptRowsCfg<D>::SMEM_BYTES, st, tmK, tmV, p, plan.few)) != cudaSuccess)
       return e;
     if (plan.join &&
-        (e = launch(&prompt_join_kernel<D, BF16>, dim3(static_cast<unsigned>(plan.row_tiles), kRowsMax / kJoinRows), kJoinRows * 32, 0, true, p, plan.few)) != cudaSuccess)
+        (e = launch_overlapping(&prompt_join_kernel<D, BF16>, dim3(static_cast<unsigned>(plan.row_tiles), kRowsMax / kJoinRows), kJoinRows * 32, 0, st, p, plan.few)) != cudaSuccess)
       return e;
   }
   if (plan.part_blocks > 0)
-    return launch(&prompt_tile_join_kernel<D, BF16>, dim3(static_cast<unsigned>(plan.cut), 2 * D / 32), 256, 0, true, p, plan.tiled);
+    return launch_overlapping(&prompt_tile_join_kernel<D, BF16>, dim3(static_cast<unsigned>(plan.cut), 2 * D / 32), 256, 0, st, p, plan.tiled);
   return cudaSuccess;
 }
 

@@ -37,6 +37,7 @@ struct PromptAttnParams {
   int* status;
   // few rows
   int chunk;                 // keys per CTA, a multiple of 64
+  int beside;                // the tiled kernel of the same call is in front
   float* parts;              // [CTAs][16][head_dim + 4]
 };
 
@@ -205,7 +206,6 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   volatile int* odd_values = reinterpret_cast<volatile int*>(tmem_slot + 2);      // [2]: a tile's item met values that were replaced
 
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");       // (the few-row kernel of the same call)
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     mbar_init(q_full, 1); mbar_init(q_empty, 1); mbar_init(s_free, 4);
@@ -221,6 +221,9 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
+  // What is in front is complete before anything of this call begins: the few-row kernel beside this one does not wait itself.
+  await_predecessor();
+  dependents_may_start();
   const uint32_t tmem_base = *tmem_slot;
   const uint32_t tS = tmem_base, tP = tmem_base + 128, tO = tmem_base + 256;      // columns: S 128, P 2 x 64, O 2 x 128
 
@@ -549,7 +552,7 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
                 for (int key = it.ragged * 128; key < limit; ++key, v += p.ld_v) {
 #pragma unroll
                   for (int i = 0; i < 32; ++i)
-                    if (odd_bits<BF16>(__ldg(v + i))) r[i] = __float_as_uint(__uint_as_float(r[i]) + widen16bit<BF16>(__ldg(v + i)));
+                    if (odd_bits<BF16>(v[i])) r[i] = __float_as_uint(__uint_as_float(r[i]) + widen16bit<BF16>(v[i]));
                 }
               }
             }
@@ -659,7 +662,7 @@ __device__ __forceinline__ void prompt_store(const PromptAttnParams& p, const Pr
     for (int key = first; key < limit; ++key, v += p.ld_v)
 #pragma unroll
       for (int c = 0; c < 4; ++c)
-        if (odd_bits<BF16>(__ldg(v + c))) x[c] += widen16bit<BF16>(__ldg(v + c));
+        if (odd_bits<BF16>(v[c])) x[c] += widen16bit<BF16>(v[c]);
   }
   uint2 r = make_uint2(pack16x2<BF16>(x[0], x[1]), pack16x2<BF16>(x[2], x[3]));
   r.x = put_infinities<BF16>(r.x, x[0], x[1]);
@@ -683,7 +686,6 @@ prompt_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
   volatile int* odd_values = abort_flag + 1;                            // a value was replaced
   float* part = reinterpret_cast<float*>(aligned);                      // [4 warps][kRowsMax][PART], after the main loop
 
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");       // (the joining kernel waits for this one's end itself)
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const PromptPart w = prompt_part(batch, p, blockIdx.x);
   const int rows = min(kRowsMax, w.q_len * p.group - w.row0);           // of this CTA, 1 .. kRowsMax
@@ -691,6 +693,10 @@ prompt_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
   const int most = prompt_limit(w, p, (w.row0 + rows - 1) / p.group);   // keys that the last one sees
   const int begin = w.part * p.chunk, end = min(most, begin + p.chunk); // of this CTA (begin may be >= end)
 
+  // Beside the tiled kernel, which has waited for what is in front of both, this one waits at its end only.  (Then too what follows the call
+  // is behind both.)
+  if (!p.beside) await_predecessor();
+  dependents_may_start();                      // (the joining kernel waits for this one's end)
   // The producer's thread sets the barriers up and requests the first tiles before the CTA meets.
   auto load = [&](int n, int stage) {          // tile n: K, V, K, V, ... of the keys from `begin` on
     mbar_arrive_expect_tx(full(stage), C::TILE_BYTES);
@@ -886,8 +892,7 @@ prompt_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
     else prompt_store<BF16>(p, w, w.row0 + row, c, D, o, first, *odd_values != 0);
   }
   if (threadIdx.x == 0 && *abort_flag) atomicMax(p.status, kStatusAttnTimeout);
-  // Where the tiled kernel is in front, this one runs beside it; it ends after it, so that what follows is behind both.
-  asm volatile("griddepcontrol.wait;" ::: "memory");
+  await_predecessor();
 }
 
 // A warp per row of a row tile with several parts (grid: row tiles x 4, four rows each): the parts rescaled to their common maximum, in order.  Lanes hold
@@ -918,7 +923,7 @@ prompt_join_kernel(const PromptAttnParams p, const __grid_constant__ PromptBatch
   w.before = w.kv_len - w.q_len;
   const int row = blockIdx.y * kJoinRows + (threadIdx.x >> 5), lane = threadIdx.x & 31;
   if (w.parts == 1 || row >= w.q_len * p.group - w.row0) return;
-  asm volatile("griddepcontrol.wait;" ::: "memory");                    // the parts are complete
+  await_predecessor();                    // the parts are complete
   const float* from = p.parts + (static_cast<long long>(cta) * kRowsMax + row) * PART;
   constexpr long long kStep = static_cast<long long>(kRowsMax) * PART;
   const int c = lane * 4;                                               // (d = 64: half of the lanes hold channels)
@@ -976,7 +981,7 @@ prompt_tile_join_kernel(const PromptAttnParams p, const __grid_constant__ Prompt
   const int parts = (blocks + p.part_blocks - 1) / p.part_blocks;
   const int in = threadIdx.x & 127, row = qb * 128 + in, c = blockIdx.y % (D / 32) * 32 + (threadIdx.x >> 7) * 16;
   if ((tile == 1 && !it.tile1) || row >= it.q_len) return;
-  asm volatile("griddepcontrol.wait;" ::: "memory");                    // the parts are complete
+  await_predecessor();                    // the parts are complete
   auto part = [&](int t) { return p.tile_parts + (static_cast<long long>(slot_of[t]) * 2 + tile) * (D + 4) * 128 + in; };
   float top = -INFINITY, odd = 0.f;
 #pragma unroll 4
@@ -1005,7 +1010,7 @@ prompt_tile_join_kernel(const PromptAttnParams p, const __grid_constant__ Prompt
     for (int key = it.ragged * 128; key < limit; ++key, v += p.ld_v)
 #pragma unroll
       for (int i = 0; i < 16; ++i)
-        if (odd_bits<BF16>(__ldg(v + i))) o[i] += widen16bit<BF16>(__ldg(v + i));
+        if (odd_bits<BF16>(v[i])) o[i] += widen16bit<BF16>(v[i]);
   }
   uint32_t w[8];
 #pragma unroll

@@ -384,6 +384,12 @@ __device__ __forceinline__ void umma_commit_pair(uint32_t bar, uint16_t cta_mask
                ::"r"(bar), "h"(cta_mask) : "memory");
 }
 
+// ----------------------------------------------------------------------------------- launches that overlap
+// A kernel launched with programmatic stream serialization may start while the one in front of it ends: it sets itself up and waits here, until
+// that one is complete and its writes are visible, before it touches memory.  dependents_may_start: the next one may do the same from now on.
+__device__ __forceinline__ void await_predecessor() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void dependents_may_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
 // ----------------------------------------------------------------------------------- registers, packed math
 // Register re-balancing between warpgroups (all four warps of a warpgroup must execute it).
 #define DIT_SETMAXNREG_INC(n) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(n))

@@ -73,6 +73,8 @@ rotary_kernel(const __grid_constant__ RotaryParams p) {
   using Elem = typename In::Elem;
   constexpr int EPL = In::EPL, EPP = EPL * kBytes / 16;                            // elements of a 16-byte load, of a piece
   __shared__ float2 cs[kRotaryRows][kRotaryMaxPairs];
+  dependents_may_start();
+  await_predecessor();
   const long long row0 = static_cast<long long>(blockIdx.x) * p.rows_per_cta;
   const int n_rows = static_cast<int>(min(static_cast<long long>(p.rows_per_cta), p.rows - row0));
   const int rotated = 2 * p.pairs;
@@ -105,7 +107,7 @@ rotary_kernel(const __grid_constant__ RotaryParams p) {
     const long long row = row0 + r;
     int position;
     if (p.positions) {
-      position = __ldg(p.positions + row);
+      position = p.positions[row];
     } else {
       int lo = 0, hi = p.n - 1;                // the row's request: the last one that begins at or before it
       while (lo < hi) {

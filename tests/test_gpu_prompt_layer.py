@@ -275,3 +275,50 @@ def test_inputs_that_require_a_gradient_are_taken_as_they_are(B):
         assert not out.requires_grad
     with pytest.raises(B.DitError):
         B.dit_rotary(torch._neg_view(x.detach()), 2, [5])                # lazily negated
+
+
+@pytest.mark.parametrize("lens,contexts", [([1] * 9, [700] * 9), ([300, 1, 77], [300, 2000, 90]), ([900, 31], [900, 31])])
+def test_calls_on_the_heels_of_one_another_wait_for_one_another(B, lens, contexts):
+    """Operators set themselves up while the one in front of them ends.  A run of layers without a pause, whose intermediate tensors take one another's
+    memory, gives bit for bit what the same calls give with a synchronisation behind each."""
+    import torch
+    layer = Layer(B, 384, 6, 2, 64, 16, 5)
+    h, g, d, rows = 6, 2, 64, sum(lens)
+    gen = torch.Generator().manual_seed(6)
+    x = torch.randn(rows, 384, generator=gen).half().cuda()
+    keys, values = (torch.randn(sum(contexts), g * d, generator=gen).half().cuda() for _ in range(2))
+    first = [c - l for l, c in zip(lens, contexts)]
+    mixed, out = (torch.empty(rows, 384, dtype=torch.float16, device="cuda") for _ in range(2))
+    qkv = torch.empty(rows, (h + 2 * g) * d, dtype=torch.float16, device="cuda")
+
+    def run(pause):
+        results, y = [], x
+        for i in range(12):
+            a = B.dit_quantize_fp4(y, 16); pause()
+            B.dit_gemm_fp4(a[0], a[1], layer.qkv_codes[0], layer.qkv_codes[1], 384, 16, a[2], layer.qkv_codes[2], bias=layer.b_qkv, out=qkv); pause()
+            B.dit_rotary(qkv[:, :(h + g) * d], h + g, lens, first=first, out=qkv[:, :(h + g) * d]); pause()
+            B.dit_rotary(keys, g, contexts, out=keys); pause()           # what attention reads has just been written
+            B.dit_prompt_attention(qkv[:, :h * d], keys, values, lens, contexts, h, g, out=mixed); pause()
+            a = B.dit_quantize_fp4(mixed, 16); pause()
+            B.dit_gemm_fp4(a[0], a[1], layer.out_codes[0], layer.out_codes[1], h * d, 16, a[2], layer.out_codes[2], out=out); pause()
+            back = B.dit_dequantize_fp4(a[0], a[1], h * d, 16, a[2], out_dtype=torch.float16); pause()
+            B.dit_rotary(keys, g, contexts, inverse=True, out=keys); pause()
+            y = out.clone() if i % 2 else out                            # (torch's kernels in between as well)
+            results += [qkv.clone(), mixed.clone(), out.clone(), back]
+        return results
+
+    saved = keys.clone()
+    want = run(torch.cuda.synchronize)
+    keys.copy_(saved)
+    got = run(lambda: None)
+    graph, start = torch.cuda.CUDAGraph(), saved.clone()
+    with torch.cuda.graph(graph):                                        # the host is not in between then
+        keys.copy_(start)
+        captured = run(lambda: None)
+    for results in (got, captured):
+        if results is captured:
+            graph.replay()
+        B.dit_ops_poll_status()
+        torch.cuda.synchronize()
+        for i, (a, b) in enumerate(zip(want, results)):
+            assert torch.equal(a.view(torch.int16), b.view(torch.int16)), i
