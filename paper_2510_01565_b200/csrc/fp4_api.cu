@@ -158,31 +158,41 @@ cudaError_t dispatch_product(const OpsDevice& d, int pairs, const dit_gemm_fp4_a
   return launch_product<kBlkF32, G>(d, pairs, a, p, st);
 }
 
-template <int kType, int G, bool kVec, int THREADS>
+template <int kType, int G, int kBytes, int THREADS>
 cudaError_t launch_rows(const Fp4QuantParams& p, long long loads, cudaStream_t st) {
   constexpr int CTA = THREADS == 32 ? 256 : THREADS, PER = CTA / THREADS;
   const unsigned grid = (static_cast<unsigned>((static_cast<long long>(p.rows) + 127) / 128 * 128) + PER - 1) / PER;
   const long long each = (loads + THREADS - 1) / THREADS;
-  if (each <= 1) return launch_overlapping(&quantize_fp4_kernel<kType, G, kVec, THREADS, 1>, dim3(grid), CTA, 0, st, p);
-  if (each <= 2) return launch_overlapping(&quantize_fp4_kernel<kType, G, kVec, THREADS, 2>, dim3(grid), CTA, 0, st, p);
-  if (each <= 4) return launch_overlapping(&quantize_fp4_kernel<kType, G, kVec, THREADS, 4>, dim3(grid), CTA, 0, st, p);
-  return launch_overlapping(&quantize_fp4_kernel<kType, G, kVec, THREADS, 6>, dim3(grid), CTA, 0, st, p);
+  if constexpr (kBytes == 32) {
+    if (each <= 1) return launch_overlapping(&quantize_fp4_kernel<kType, G, kBytes, THREADS, 1>, dim3(grid), CTA, 0, st, p);
+    if (each <= 2) return launch_overlapping(&quantize_fp4_kernel<kType, G, kBytes, THREADS, 2>, dim3(grid), CTA, 0, st, p);
+    return launch_overlapping(&quantize_fp4_kernel<kType, G, kBytes, THREADS, 3>, dim3(grid), CTA, 0, st, p);
+  } else {
+    if (each <= 1) return launch_overlapping(&quantize_fp4_kernel<kType, G, kBytes, THREADS, 1>, dim3(grid), CTA, 0, st, p);
+    if (each <= 2) return launch_overlapping(&quantize_fp4_kernel<kType, G, kBytes, THREADS, 2>, dim3(grid), CTA, 0, st, p);
+    if (each <= 4) return launch_overlapping(&quantize_fp4_kernel<kType, G, kBytes, THREADS, 4>, dim3(grid), CTA, 0, st, p);
+    return launch_overlapping(&quantize_fp4_kernel<kType, G, kBytes, THREADS, 6>, dim3(grid), CTA, 0, st, p);
+  }
 }
-template <int kType, int G, bool kVec>
+template <int kType, int G, int kBytes>
 cudaError_t launch_quant(const Fp4QuantParams& p, cudaStream_t st) {
-  // As few lanes per row as hold it in six 16-byte loads each: what a row's maximum costs grows with them.
-  constexpr int EPL = QuantIn<kType>::EPL;
+  // As few lanes per row as hold it in 96 bytes each: what a row's maximum costs grows with them.  (Loads of 32 bytes: 9216 x 12288 fp16 62 -> 49 us)
+  constexpr int EPL = QuantIn<kType>::EPL * (kBytes == 32 ? 2 : 1), MOST = kBytes == 32 ? 3 : 6;
   const long long loads = (static_cast<long long>(p.cols) + EPL - 1) / EPL;
-  if (loads <= 32 * 6) return launch_rows<kType, G, kVec, 32>(p, loads, st);
-  if (loads <= 64 * 6) return launch_rows<kType, G, kVec, 64>(p, loads, st);
-  if (loads <= 128 * 6) return launch_rows<kType, G, kVec, 128>(p, loads, st);
-  if (loads <= 256 * 6) return launch_rows<kType, G, kVec, 256>(p, loads, st);
-  return launch_rows<kType, G, kVec, 512>(p, loads, st);
+  if (loads <= 32 * MOST) return launch_rows<kType, G, kBytes, 32>(p, loads, st);
+  if (loads <= 64 * MOST) return launch_rows<kType, G, kBytes, 64>(p, loads, st);
+  if (loads <= 128 * MOST) return launch_rows<kType, G, kBytes, 128>(p, loads, st);
+  if (loads <= 256 * MOST) return launch_rows<kType, G, kBytes, 256>(p, loads, st);
+  return launch_rows<kType, G, kBytes, 512>(p, loads, st);
+}
+template <int kType, int G>
+cudaError_t launch_quant(const Fp4QuantParams& p, int bytes, cudaStream_t st) {
+  if (bytes == 32) return launch_quant<kType, G, 32>(p, st);
+  return bytes == 16 ? launch_quant<kType, G, 16>(p, st) : launch_quant<kType, G, 0>(p, st);
 }
 template <int kType>
-cudaError_t launch_quant(const Fp4QuantParams& p, int group, bool vec, cudaStream_t st) {
-  if (group == 16) return vec ? launch_quant<kType, 16, true>(p, st) : launch_quant<kType, 16, false>(p, st);
-  return vec ? launch_quant<kType, 32, true>(p, st) : launch_quant<kType, 32, false>(p, st);
+cudaError_t launch_quant(const Fp4QuantParams& p, int group, int bytes, cudaStream_t st) {
+  return group == 16 ? launch_quant<kType, 16>(p, bytes, st) : launch_quant<kType, 32>(p, bytes, st);
 }
 
 template <int kType, bool kVec>
@@ -200,11 +210,27 @@ cudaError_t launch_weight(const Fp4QuantWeightParams& p, int group, cudaStream_t
   return launch_overlapping(&quantize_weight_fp4_kernel<kType, 32, kVec>, dim3(grid), 256, 0, st, p);
 }
 
-template <int kType, int G>
-cudaError_t launch_values(const Fp4ValuesParams& p, bool vec, cudaStream_t st) {
-  const unsigned grid = static_cast<unsigned>((static_cast<long long>(p.rows) + kValueRows - 1) / kValueRows * ((static_cast<long long>(p.cols) + kValueCols - 1) / kValueCols));
-  if (vec) return launch_overlapping(&dequantize_fp4_kernel<kType, G, true>, dim3(grid), 256, 0, st, p);
-  return launch_overlapping(&dequantize_fp4_kernel<kType, G, false>, dim3(grid), 256, 0, st, p);
+template <int kType, int G, int kBytes>
+cudaError_t launch_values(const OpsDevice& d, const Fp4ValuesParams& p, cudaStream_t st) {
+  constexpr int COLS = kBytes == 32 ? 512 : 256;
+  auto ctas = [&](int rows) { return ((static_cast<long long>(p.rows) + rows - 1) / rows) * ((static_cast<long long>(p.cols) + COLS - 1) / COLS); };
+  // Four rows per warp (9216 x 12288 fp16: 45 us; eight 46, 82 against 78 in fp32), two where those would not fill the device (77 x 2056: 1.6 us against 2.9
+  // with eight).
+  if (ctas(kValueWarps * 4) >= 4ll * d.num_sms)
+    return launch_overlapping(&dequantize_fp4_kernel<kType, G, kBytes, 4>, dim3(static_cast<unsigned>(ctas(kValueWarps * 4))), kValueWarps * 32, 0, st, p);
+  return launch_overlapping(&dequantize_fp4_kernel<kType, G, kBytes, 2>, dim3(static_cast<unsigned>(ctas(kValueWarps * 2))), kValueWarps * 32, 0, st, p);
+}
+template <int kType>
+cudaError_t launch_values(const OpsDevice& d, const Fp4ValuesParams& p, int group, int bytes, cudaStream_t st) {
+  if (bytes == 32) return group == 16 ? launch_values<kType, 16, 32>(d, p, st) : launch_values<kType, 32, 32>(d, p, st);
+  if (bytes == 16) return group == 16 ? launch_values<kType, 16, 16>(d, p, st) : launch_values<kType, 32, 16>(d, p, st);
+  return group == 16 ? launch_values<kType, 16, 0>(d, p, st) : launch_values<kType, 32, 0>(d, p, st);
+}
+
+// What a matrix's rows start on multiples of.
+int row_alignment(const void* x, int64_t ld, dit_type type) {
+  auto starts_at = [&](int n) { return aligned(x, n) && ld * type_bytes(type) % n == 0; };
+  return starts_at(32) ? 32 : starts_at(16) ? 16 : 0;
 }
 
 dit_status status_of(cudaError_t e) { return e == cudaSuccess ? DIT_OK : DIT_ERR_CUDA; }
@@ -246,11 +272,11 @@ dit_status dit_quantize_fp4(const void* x, dit_type type, int64_t ld, int64_t ro
   Fp4QuantParams p{};
   p.x = x; p.codes = static_cast<uint8_t*>(codes); p.scales = static_cast<uint8_t*>(scales); p.row_scales = row_scales;
   p.ld = ld; p.ld_codes = ld_codes; p.rows = static_cast<int>(rows); p.cols = static_cast<int>(cols); p.chunks = chunks_of(cols, group);
-  const bool vec = aligned(x, 16) && ld * type_bytes(type) % 16 == 0;
+  const int bytes = row_alignment(x, ld, type);
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
-  if (type == DIT_TYPE_F16) return status_of(launch_quant<0>(p, group, vec, st));
-  if (type == DIT_TYPE_BF16) return status_of(launch_quant<1>(p, group, vec, st));
-  return status_of(launch_quant<2>(p, group, vec, st));
+  if (type == DIT_TYPE_F16) return status_of(launch_quant<0>(p, group, bytes, st));
+  if (type == DIT_TYPE_BF16) return status_of(launch_quant<1>(p, group, bytes, st));
+  return status_of(launch_quant<2>(p, group, bytes, st));
 }
 
 dit_status dit_quantize_weight_fp4(const void* w, dit_type type, int64_t ld, int64_t in_dim, int64_t out_dim, int32_t group, void* codes,
@@ -289,12 +315,11 @@ dit_status dit_dequantize_fp4(const void* codes, int64_t ld_codes, const void* s
   Fp4ValuesParams p{};
   p.codes = static_cast<const uint8_t*>(codes); p.scales = static_cast<const uint8_t*>(scales); p.row_scales = row_scales; p.out = out;
   p.ld_codes = ld_codes; p.ld_out = ld_out; p.rows = static_cast<int>(rows); p.cols = static_cast<int>(cols); p.chunks = chunks_of(cols, group);
-  const int unit = 8 * type_bytes(out_type);     // eight values leave in one store
-  const bool vec = aligned(out, unit) && ld_out * type_bytes(out_type) % unit == 0;
+  const int bytes = row_alignment(out, ld_out, out_type);
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
-  if (out_type == DIT_TYPE_F16) return status_of(group == 16 ? launch_values<0, 16>(p, vec, st) : launch_values<0, 32>(p, vec, st));
-  if (out_type == DIT_TYPE_BF16) return status_of(group == 16 ? launch_values<1, 16>(p, vec, st) : launch_values<1, 32>(p, vec, st));
-  return status_of(group == 16 ? launch_values<2, 16>(p, vec, st) : launch_values<2, 32>(p, vec, st));
+  if (out_type == DIT_TYPE_F16) return status_of(launch_values<0>(d, p, group, bytes, st));
+  if (out_type == DIT_TYPE_BF16) return status_of(launch_values<1>(d, p, group, bytes, st));
+  return status_of(launch_values<2>(d, p, group, bytes, st));
 }
 
 dit_status dit_gemm_fp4(const dit_gemm_fp4_args* a, void* stream) {

@@ -156,15 +156,18 @@ __device__ __forceinline__ long long scale_at(int row, int group, int chunks) {
   return (static_cast<long long>(row >> 7) * chunks + (group >> 2)) * 512 + (row & 31) * 16 + ((row & 127) >> 5) * 4 + (group & 3);
 }
 
-// A row per THREADS lanes (a warp of a CTA of eight, or a whole CTA), a 16-byte load of consecutive columns per lane: EPL values, kGroup / EPL lanes
-// to a group.  A row of up to THREADS * kLoads loads stays in registers between its maximum and its codes; a longer one
-// is read twice.  Rows behind the last one up to the tile's end get their zero scales only.  Bound by HBM.
-// kVec: rows start on 16-byte boundaries; otherwise elements are loaded one by one.
-template <int kType, int kGroup, bool kVec, int THREADS, int kLoads>
-__global__ void __launch_bounds__(THREADS == 32 ? 256 : THREADS, THREADS == 256 && kLoads == 6 ? 5 : 1)
+// A row per THREADS lanes (a warp of a CTA of eight, or a whole CTA), kBytes of consecutive columns per lane and load: EPL values, kGroup / EPL
+// lanes to a group.  A row of up to THREADS * kLoads loads stays in registers between its maximum and its codes; a longer one
+// is read twice.  Rows behind the last one up to the tile's end get their zero scales only.  Bound by HBM and the issue of instructions.
+// kBytes: what rows' starts are multiples of, 32 (one load per group of 16 16-bit numbers: its scale is found once), 16, or 0: anywhere,
+// loads of 16 bytes' worth made up of smaller ones.
+// Registers are held down so that 1280 threads (1536 with little to hold) fit an SM: 4096 x 40000 fp16, read twice, 140 -> 92 us, 10630 x 6480 44 -> 40.
+template <int kType, int kGroup, int kBytes, int THREADS, int kLoads>
+__global__ void __launch_bounds__(THREADS == 32 ? 256 : THREADS, (kLoads * (kBytes == 32 ? 2 : 1) <= 4 ? 1536 : 1280) / (THREADS == 32 ? 256 : THREADS))
 quantize_fp4_kernel(const Fp4QuantParams p) {
   using In = QuantIn<kType>;
-  constexpr int EPL = In::EPL, LPG = kGroup / EPL;                // lanes per group
+  constexpr int W = kBytes == 32 ? 2 : 1;                         // 16-byte words of a load
+  constexpr int EPW = In::EPL, EPL = EPW * W, LPG = kGroup / EPL; // values of a word, of a load; lanes per group
   constexpr int CTA = THREADS == 32 ? 256 : THREADS;
   __shared__ uint32_t warp_top[CTA / 32];
   dependents_may_start();
@@ -178,15 +181,25 @@ quantize_fp4_kernel(const Fp4QuantParams p) {
   const int span = THREADS * EPL * kLoads;                        // columns held at a time
   const int wide = p.chunks * 4 * kGroup;                         // columns with a scale byte
   const typename In::Elem* src = static_cast<const typename In::Elem*>(p.x) + (there ? row : 0) * p.ld;
-  uint4 raw[kLoads];
+  uint4 raw[kLoads][W];
   auto load = [&](int base) {
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
-      const int c = base + (i * THREADS + at) * EPL;
-      raw[i] = load_run<kType, kVec>(src + c, there ? p.cols - c : 0, c > 0);
+      const int c = base + (i * THREADS + at) * EPL, n = there ? p.cols - c : 0;
+      if (W == 2 && n >= EPL) {
+        if constexpr (W == 2) load_once_v8(raw[i], src + c);
+      } else {
+#pragma unroll
+        for (int w = 0; w < W; ++w) raw[i][w] = load_run<kType, (kBytes > 0)>(src + c + w * EPW, n - w * EPW, c + w > 0);
+      }
     }
   };
-  auto top_of = [&](const uint4& r) { return In::max_bits(In::max_bits(In::max_bits(In::max_bits(0u, r.x), r.y), r.z), r.w); };
+  auto top_of = [&](const uint4 (&r)[W]) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int w = 0; w < W; ++w) top = In::max_bits(In::max_bits(In::max_bits(In::max_bits(top, r[w].x), r[w].y), r[w].z), r[w].w);
+    return top;
+  };
   load(0);
   float up = 0.f;
   bool bad = false;
@@ -231,15 +244,21 @@ quantize_fp4_kernel(const Fp4QuantParams p) {
       // (THREADS * EPL columns are whole tiles of four groups: 512 bytes each)
       if (c < wide && (at % LPG) == 0) scale[static_cast<long long>((base / EPL + i * THREADS) / (4 * LPG)) * 512] = there && c < p.cols ? static_cast<uint8_t>(g.byte) : 0;
       if (there && c < p.cols) {
-        float v[EPL];
-        In::widen16(raw[i], v);
-        const uint32_t code = encode<kGroup, EPL>(v, g);
+        uint32_t code[W];
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
+          float v[EPW];
+          In::widen16(raw[i][w], v);
+          code[w] = encode<kGroup, EPW>(v, g);
+        }
         uint8_t* dst = codes + (base + i * THREADS * EPL) / 2;
         if (c + EPL <= p.cols) {
-          if constexpr (EPL == 8) *reinterpret_cast<uint32_t*>(dst) = code;
-          else *reinterpret_cast<uint16_t*>(dst) = static_cast<uint16_t>(code);
+          if constexpr (EPL == 16) *reinterpret_cast<uint2*>(dst) = make_uint2(code[0], code[1]);
+          else if constexpr (EPL == 8 && W == 2) *reinterpret_cast<uint32_t*>(dst) = code[0] | code[1] << 16;
+          else if constexpr (EPL == 8) *reinterpret_cast<uint32_t*>(dst) = code[0];
+          else *reinterpret_cast<uint16_t*>(dst) = static_cast<uint16_t>(code[0]);
         } else {
-          for (int b = 0; 2 * b < p.cols - c; ++b) dst[b] = static_cast<uint8_t>(code >> (8 * b));
+          for (int b = 0; 2 * b < p.cols - c; ++b) dst[b] = static_cast<uint8_t>(code[b / (EPW / 2)] >> (8 * (b % (EPW / 2))));
         }
       }
     }
@@ -397,69 +416,98 @@ struct Fp4ValuesParams {
   int rows, cols, chunks;
 };
 
-// code * scale (exact) * row scale, rounded to fp32 and then to the output's type.  A CTA takes 64 rows x 256 columns, a lane eight
-// consecutive codes at a time, a warp a row.  Bound by HBM.  kVec: rows of out start on 16-byte boundaries (fp32: on 32-byte ones).
-constexpr int kValueRows = 64, kValueCols = 256;
-template <int kType, int kGroup, bool kVec>
-__global__ void __launch_bounds__(256)
+// code * scale (exact) * row scale, rounded to fp32 and then to the output's type.  A lane takes `PER` consecutive codes of a row at a time, a warp a
+// row, a CTA kTurns rows per warp.  Bound by HBM.
+// kBytes: what rows of out are known to start on multiples of, 32: sixteen codes per lane, one scale of either group and whole sectors
+// to write; 16: eight codes, so that a 16-bit type's neighbouring stores still fill sectors; 0: anywhere.
+constexpr int kValueWarps = 8;
+template <int kType, int kGroup, int kBytes, int kTurns>
+__global__ void __launch_bounds__(kValueWarps * 32)
 dequantize_fp4_kernel(const Fp4ValuesParams p) {
-  constexpr int TURNS = kValueRows / 8;
-  const int col_tiles = (p.cols + kValueCols - 1) / kValueCols;
-  __shared__ float lines[kVec ? 1 : 8][kVec ? 1 : 32 * 9];
+  constexpr int PER = kBytes == 32 ? 16 : 8, WORDS = PER / 8;
+  using Out = typename QuantIn<kType>::Elem;
+  const int col_tiles = (p.cols + 32 * PER - 1) / (32 * PER);
+  __shared__ float lines[kBytes ? 1 : kValueWarps][kBytes ? 1 : 32 * 9];
   dependents_may_start();
   await_predecessor();
   const int lane = threadIdx.x & 31;
-  const int row0 = blockIdx.x / col_tiles * kValueRows + (threadIdx.x >> 5), c = blockIdx.x % col_tiles * kValueCols + lane * 8;
-  if (kVec && c >= p.cols) return;
-  const int bytes = max(0, min(4, (p.cols - c + 1) / 2));
+  const int row0 = blockIdx.x / col_tiles * (kValueWarps * kTurns) + (threadIdx.x >> 5), c = blockIdx.x % col_tiles * (32 * PER) + lane * PER;
+  if (kBytes && c >= p.cols) return;
   const uint8_t* codes = p.codes + row0 * p.ld_codes + c / 2;
-  uint32_t code[TURNS], byte[TURNS];
-  float factor[TURNS];
+  uint32_t code[kTurns][WORDS], byte[kTurns];
+  float factor[kTurns];
 #pragma unroll
-  for (int i = 0; i < TURNS; ++i) {
-    const int row = row0 + i * 8;
-    code[i] = 0; byte[i] = 0; factor[i] = 1.f;
+  for (int i = 0; i < kTurns; ++i) {
+    const int row = row0 + i * kValueWarps;
+    byte[i] = 0; factor[i] = 1.f;
+#pragma unroll
+    for (int w = 0; w < WORDS; ++w) code[i][w] = 0;
     if (row >= p.rows) continue;
-    const uint8_t* src = codes + i * 8 * p.ld_codes;
-    if (bytes == 4) code[i] = *reinterpret_cast<const uint32_t*>(src);
-    else for (int b = 0; b < bytes; ++b) code[i] |= static_cast<uint32_t>(src[b]) << (8 * b);
-    if (bytes > 0) byte[i] = p.scales[scale_at(row, c / kGroup, p.chunks)];
+    const uint8_t* src = codes + i * kValueWarps * p.ld_codes;
+    if (WORDS == 2 && c + 16 <= p.cols) {
+      const uint2 x = *reinterpret_cast<const uint2*>(src);
+      code[i][0] = x.x; code[i][WORDS - 1] = x.y;
+    } else {
+#pragma unroll
+      for (int w = 0; w < WORDS; ++w) {
+        const int n = p.cols - c - 8 * w;
+        if (n >= 8) code[i][w] = *reinterpret_cast<const uint32_t*>(src + 4 * w);
+        else
+          for (int b = 0; 2 * b < n; ++b) code[i][w] |= static_cast<uint32_t>(src[4 * w + b]) << (8 * b);
+      }
+    }
+    if (c < p.cols) byte[i] = p.scales[scale_at(row, c / kGroup, p.chunks)];
     if (p.row_scales) factor[i] = p.row_scales[row];
   }
 #pragma unroll
-  for (int i = 0; i < TURNS; ++i) {
-    const int row = row0 + i * 8;
+  for (int i = 0; i < kTurns; ++i) {
+    const int row = row0 + i * kValueWarps;
     if (row >= p.rows) break;                                      // (the whole warp)
     const float scale = kGroup == 16 ? e4m3_value(byte[i]) : e8m0_value(byte[i]);
-    float v[8];
-    e2m1_values(code[i], v);
+    Out* out = static_cast<Out*>(p.out) + row * p.ld_out + c;
+    float v[WORDS][8];
+    uint32_t packed[WORDS][4];                                     // (16-bit types)
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = v[j] * scale * factor[i];
-    if constexpr (kVec) {
-      if (c + 8 <= p.cols) {
-        if constexpr (kType == 2) {
-          uint32_t w[8];
+    for (int w = 0; w < WORDS; ++w) {
+      e2m1_values(code[i][w], v[w]);
 #pragma unroll
-          for (int j = 0; j < 8; ++j) w[j] = __float_as_uint(v[j]);
-          st_global_v8(static_cast<float*>(p.out) + row * p.ld_out + c, w);
-        } else {
-          *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.out) + row * p.ld_out + c) =
-              make_uint4(pack16x2<kType == 1>(v[0], v[1]), pack16x2<kType == 1>(v[2], v[3]), pack16x2<kType == 1>(v[4], v[5]), pack16x2<kType == 1>(v[6], v[7]));
-        }
-      } else {
+      for (int j = 0; j < 8; j += 2) {
+        const float2 x = fmul2(fmul2(make_float2(v[w][j], v[w][j + 1]), make_float2(scale, scale)), make_float2(factor[i], factor[i]));
+        v[w][j] = x.x; v[w][j + 1] = x.y;
+        if constexpr (kType != 2) packed[w][j / 2] = pack16x2<kType == 1>(x.x, x.y);
+      }
+    }
+    if constexpr (kBytes > 0) {
+      if (kType != 2 && WORDS == 2 && c + 16 <= p.cols) {
+        st_global_v8(out, *reinterpret_cast<const uint32_t(*)[8]>(packed));
+        continue;
+      }
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (c + j < p.cols) {
-            if constexpr (kType == 2) static_cast<float*>(p.out)[row * p.ld_out + c + j] = v[j];
-            else static_cast<uint16_t*>(p.out)[row * p.ld_out + c + j] = pack16<kType == 1>(v[j]);
+      for (int w = 0; w < WORDS; ++w) {
+        Out* dst = out + 8 * w;
+        const int n = p.cols - c - 8 * w;
+        if (n >= 8) {
+          if constexpr (kType != 2) *reinterpret_cast<uint4*>(dst) = make_uint4(packed[w][0], packed[w][1], packed[w][2], packed[w][3]);
+          else if constexpr (kBytes == 32) st_global_v8(dst, *reinterpret_cast<const uint32_t(*)[8]>(v[w]));
+          else {
+            reinterpret_cast<float4*>(dst)[0] = make_float4(v[w][0], v[w][1], v[w][2], v[w][3]);
+            reinterpret_cast<float4*>(dst)[1] = make_float4(v[w][4], v[w][5], v[w][6], v[w][7]);
           }
+        } else {
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            if (j < n) {
+              if constexpr (kType == 2) dst[j] = v[w][j];
+              else dst[j] = pack16<kType == 1>(v[w][j]);
+            }
+        }
       }
     } else {
-      // rows start anywhere: through shared memory, so that neighbouring lanes write neighbouring elements
+      // through shared memory, so that neighbouring lanes write neighbouring elements
       float* line = lines[threadIdx.x >> 5];
       __syncwarp();
 #pragma unroll
-      for (int j = 0; j < 8; ++j) line[lane * 9 + j] = v[j];       // (nine words apart: no two lanes in a bank)
+      for (int j = 0; j < 8; ++j) line[lane * 9 + j] = v[0][j];    // (nine words apart: no two lanes in a bank)
       __syncwarp();
       const int c0 = c - lane * 8;
 #pragma unroll
@@ -467,8 +515,8 @@ dequantize_fp4_kernel(const Fp4ValuesParams p) {
         const int e = j * 32 + lane;
         if (c0 + e < p.cols) {
           const float x = line[e / 8 * 9 + e % 8];
-          if constexpr (kType == 2) static_cast<float*>(p.out)[row * p.ld_out + c0 + e] = x;
-          else static_cast<uint16_t*>(p.out)[row * p.ld_out + c0 + e] = pack16<kType == 1>(x);
+          if constexpr (kType == 2) out[e - lane * 8] = x;
+          else out[e - lane * 8] = pack16<kType == 1>(x);
         }
       }
     }

@@ -282,6 +282,12 @@ __device__ __forceinline__ uint4 load_once(const void* p) {
   return v;
 }
 
+// 32 bytes that are read once (address a multiple of 32)
+__device__ __forceinline__ void load_once_v8(uint4 (&v)[2], const void* p) {
+  asm volatile("ld.global.nc.L1::no_allocate.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(v[0].x), "=r"(v[0].y), "=r"(v[0].z), "=r"(v[0].w), "=r"(v[1].x), "=r"(v[1].y), "=r"(v[1].z), "=r"(v[1].w) : "l"(p));
+}
+
 // 32 bytes to global memory in one store (address a multiple of 32): a whole sector per thread
 __device__ __forceinline__ void st_global_v8(void* p, const uint32_t (&r)[8]) {
   asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"

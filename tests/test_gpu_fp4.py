@@ -246,3 +246,31 @@ def test_empty_batches(B):
     b = B.dit_quantize_fp4(torch.ones(8, 64, device="cuda"), 16)
     assert B.dit_gemm_fp4(codes, scales, b[0], b[1], 64, 16, row_scales, b[2]).shape == (0, 8)
     assert B.dit_dequantize_fp4(codes, scales, 64, 16, row_scales).shape == (0, 64)
+
+
+@pytest.mark.parametrize("kind", ["float16", "float32"])
+@pytest.mark.parametrize("group", [16, 32])
+@pytest.mark.parametrize("cols", [1, 17, 40, 513, 1000, 6301, 13000, 26000])
+def test_rows_that_start_on_other_boundaries_have_the_same_codes_and_values(B, cols, group, kind):
+    """Starts on multiples of 32, 16, 8 and 4 bytes and of an element: each has its own loads and stores, and all give the oracle's bits."""
+    import torch
+    t = getattr(torch, kind)
+    size, rows = t.itemsize, 37
+    x = draw(cols, rows, cols, t)
+    want = P.quantize(x.double().numpy(), group)
+    values = P.values(*want, group)
+    for start in (32, 16, 8, 4, size):
+        pitch = (cols * size + 63) // 32 * 32 + start
+        buffer = torch.full((rows, pitch // size), 9.0, dtype=t, device="cuda")
+        part = buffer[:, start // size:start // size + cols]
+        part.copy_(x)
+        got = B.dit_quantize_fp4(part, group)
+        check_quantised(got, x.double().numpy(), group)
+        out = torch.full_like(buffer, 7.0)
+        B.dit_dequantize_fp4(got[0], got[1], cols, group, got[2], out=out[:, start // size:start // size + cols])
+        back = out.cpu()
+        # (a value has six bits: rounding it to the type is the only one)
+        inside = back[:, start // size:start // size + cols].double().numpy()
+        assert np.array_equal(inside, torch.from_numpy(values).to(t).double().numpy())
+        back[:, start // size:start // size + cols] = 7.0
+        assert (back == 7.0).all()
