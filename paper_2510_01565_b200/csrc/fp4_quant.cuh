@@ -158,7 +158,8 @@ __device__ __forceinline__ long long scale_at(int row, int group, int chunks) {
 
 // A row per THREADS lanes (a warp of a CTA of eight, or a whole CTA), kBytes of consecutive columns per lane and load: EPL values, kGroup / EPL
 // lanes to a group.  A row of up to THREADS * kLoads loads stays in registers between its maximum and its codes; a longer one
-// is read twice.  Rows behind the last one up to the tile's end get their zero scales only.  Bound by HBM and the issue of instructions.
+// is read twice.  Rows behind the last one up to the tile's end get their zero scales only.  Bound by HBM and the issue of instructions:
+// 9216 x 12288 fp16 49 us, 5.9 TB/s (groups of 32, without the meeting of the CTA, 43).
 // kBytes: what rows' starts are multiples of, 32 (one load per group of 16 16-bit numbers: its scale is found once), 16, or 0: anywhere,
 // loads of 16 bytes' worth made up of smaller ones.
 // Registers are held down so that 1280 threads (1536 with little to hold) fit an SM: 4096 x 40000 fp16, read twice, 140 -> 92 us, 10630 x 6480 44 -> 40.
@@ -417,7 +418,7 @@ struct Fp4ValuesParams {
 };
 
 // code * scale (exact) * row scale, rounded to fp32 and then to the output's type.  A lane takes `PER` consecutive codes of a row at a time, a warp a
-// row, a CTA kTurns rows per warp.  Bound by HBM.
+// row, a CTA kTurns rows per warp.  Bound by HBM: 9216 x 12288 to fp16 45 us, 6.4 TB/s.
 // kBytes: what rows of out are known to start on multiples of, 32: sixteen codes per lane, one scale of either group and whole sectors
 // to write; 16: eight codes, so that a 16-bit type's neighbouring stores still fill sectors; 0: anywhere.
 constexpr int kValueWarps = 8;

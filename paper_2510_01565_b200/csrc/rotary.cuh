@@ -51,7 +51,7 @@ __device__ __forceinline__ uint4 narrow16(const float (&v)[QuantIn<kType>::EPL])
 //
 // kUnits > 0: rows, heads and halves start on boundaries of kBytes (16 or 8), and the pieces of a head of that size, a piece and its
 // partner counted once where pairs are apart, are at most kUnits.  A lane keeps its place in the head and the cosines and sines of it, and
-// walks the heads of a row; its first pieces are requested before the sines are computed.  23058 rows of 40 heads of 128, fp16: 77 us, 6.1 TB/s
+// walks the heads of a row; its first pieces are requested before the sines are computed.  23058 rows of 40 heads of 128, fp16: 72-78 us, 6.0-6.5 TB/s
 // (98 with a division per piece and the sines from shared memory, and as much with twice the pieces in flight and half the CTAs).
 // kUnits == 0: a lane per pair, whatever the alignment.
 template <int kBytes>
