@@ -437,11 +437,11 @@ gemm_fp4_split_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_cons
     await_predecessor();
     for (int s = 0; s < min(C::STAGES, g1 - g0); ++s) load(g0 + s, s);
   }
-  dependents_may_start();
   if (warp == 1) { tmem_alloc(smem_u32(tmem_slot), C::COLS); tmem_relinquish(); }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
+  dependents_may_start();                      // not before: a CTA of the next kernel that took the SM's tensor memory first would wait for this one's end
   const uint32_t tmem_base = *tmem_slot;
   const int quarter = warp & 3;                                        // warps 2..5 -> quarters 2, 3, 0, 1
   const int col = n0 + quarter * 32 + lane;                            // this lane's output column (warps 2..5)

@@ -393,6 +393,7 @@ __device__ __forceinline__ void umma_commit_pair(uint32_t bar, uint16_t cta_mask
 // ----------------------------------------------------------------------------------- launches that overlap
 // A kernel launched with programmatic stream serialization may start while the one in front of it ends: it sets itself up and waits here, until
 // that one is complete and its writes are visible, before it touches memory.  dependents_may_start: the next one may do the same from now on.
+// A kernel that uses tensor memory calls it after its allocation: the next one's CTAs would keep what they took until this one ends.
 __device__ __forceinline__ void await_predecessor() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void dependents_may_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 

@@ -322,3 +322,45 @@ def test_calls_on_the_heels_of_one_another_wait_for_one_another(B, lens, context
         torch.cuda.synchronize()
         for i, (a, b) in enumerate(zip(want, results)):
             assert torch.equal(a.view(torch.int16), b.view(torch.int16)), i
+
+
+def test_calls_on_two_streams_captured_into_one_graph(B):
+    """Fork and join: a product on one stream, a rotation and mixed attention on another, and a product of both results; replayed on new inputs."""
+    import torch
+    layer = Layer(B, 384, 6, 2, 64, 32, 7)
+    lens, gen = [260, 1, 33], torch.Generator().manual_seed(8)
+    rows = sum(lens)
+    x, qkv = torch.empty(rows, 384, dtype=torch.float16, device="cuda"), torch.empty(rows, 640, dtype=torch.float16, device="cuda")
+
+    def work(other):
+        main = torch.cuda.current_stream()
+        turned = torch.empty_like(qkv)
+        mixed = torch.empty_like(x)
+        if other is not None:
+            other.wait_stream(main)
+        with torch.cuda.stream(other or main):
+            turned.copy_(qkv)
+            B.dit_rotary(turned[:, :512], 8, lens, out=turned[:, :512])
+            B.dit_prompt_attention(turned[:, :384], turned[:, 384:512], turned[:, 512:], lens, lens, 6, 2, out=mixed)
+        y = layer.product(x, layer.out_codes, 384, None, torch.float16)
+        if other is not None:
+            main.wait_stream(other)
+        return layer.product(mixed + y, layer.out_codes, 384, None, torch.float32), turned, mixed
+
+    def fill():
+        x.copy_(torch.randn(rows, 384, generator=gen).half())
+        qkv.copy_(torch.randn(rows, 640, generator=gen).half())
+
+    fill()
+    work(None)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured = work(torch.cuda.Stream())
+    for _ in range(3):
+        fill()
+        want = [t.clone() for t in work(None)]
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(captured, want):
+            assert torch.equal(a, b)
+    B.dit_ops_poll_status()
