@@ -174,7 +174,8 @@ dit_status dit_dequantize_fp4(const void *codes, int64_t ld_codes, const void *s
 /* Product of two such operands of the same group, both with k along a row:
  *   out[m, n] = a_rows[m] * b_rows[n] * sum_k (a's code * scale)[m, k] * (b's code * scale)[n, k] + bias[n]
  * The sum is the tensor cores', in fp32; the row scales (each NULL for 1) and the bias follow in fp32; rounded once into out, 16-bit outputs
- * clamp to the largest finite value.  Products of two scales have to lie inside fp32's range.
+ * clamp to the largest finite value.  Sums and products of two groups' scales have to lie inside fp32's range; row scales may have any size, the
+ * result leaves the range only where the whole product does.
  *   a, a_scales, a_rows   [m, k] as above, lda in bytes;  b, b_scales, b_rows  [n, k] likewise;  bias  device fp32 [n] or NULL
  *   out  device [m, ld_out] of out_type, element-aligned, ld_out >= n; must not overlap the operands
  * m == 0 is a no-op. */

@@ -59,6 +59,19 @@ __device__ __forceinline__ void tma_load_3d_pair(uint32_t dst, const void* tmap,
       : "memory");
 }
 
+// A finished sum with its row's and its column's factor and the bias.  A caller's factors may be of any size (a quantiser's row factors span 2^-111 to
+// 2^117): the result leaves fp32's range where the whole product does.  Of a factor above 1 and one that is not, the product of the two comes
+// first, whose size lies between theirs; two on the same side of 1 are taken one after the other, and the sum moves one way only.
+// fp4_far: the sum times the row's factor alone may leave the range.  Sums under e4m3 scales are 0 or 2^-20 .. 2^53 in size; under powers of two they may
+// be anything.
+template <int kGroup>
+__device__ __forceinline__ bool fp4_far(float fr) { return kGroup == 32 ? fr != 1.f : fabsf(fr) < 0x1p-100f || fabsf(fr) > 0x1p73f; }
+template <int kGroup>
+__device__ __forceinline__ float fp4_finish(float sum, float fr, float fc, float bias) {
+  if (fp4_far<kGroup>(fr) && (fabsf(fr) > 1.f) != (fabsf(fc) > 1.f)) return fmaf(sum, fr * fc, bias);
+  return fmaf(sum * fr, fc, bias);
+}
+
 // Scale tiles per stage of 256 k, and how a step of 64 k finds its scales in them.
 template <int kGroup>
 struct Fp4Scales {
@@ -305,12 +318,28 @@ gemm_fp4_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
       __syncwarp();
       if (lane == 0) mbar_arrive_cluster_light(tempty_leader + 8u * buf);
       if (!mine) continue;                     // (its warps of the next tile wait at its column factors)
+      if (!__any_sync(0xffffffffu, fp4_far<kGroup>(fr))) {
 #pragma unroll
-      for (int i = 0; i < 64; i += 2) {                                // (row factor * sum) * column factor + bias
-        const float4 f = *reinterpret_cast<const float4*>(col_of + 2 * i), b = *reinterpret_cast<const float4*>(col_of + 128 + 2 * i);
-        const float2 r = make_float2(fr, fr);
-        acc[i] = ffma2(fmul2(acc[i], r), make_float2(f.x, f.y), make_float2(b.x, b.y));
-        acc[i + 1] = ffma2(fmul2(acc[i + 1], r), make_float2(f.z, f.w), make_float2(b.z, b.w));
+        for (int i = 0; i < 64; i += 2) {                              // (row factor * sum) * column factor + bias
+          const float4 f = *reinterpret_cast<const float4*>(col_of + 2 * i), b = *reinterpret_cast<const float4*>(col_of + 128 + 2 * i);
+          const float2 r = make_float2(fr, fr);
+          acc[i] = ffma2(fmul2(acc[i], r), make_float2(f.x, f.y), make_float2(b.x, b.y));
+          acc[i + 1] = ffma2(fmul2(acc[i + 1], r), make_float2(f.z, f.w), make_float2(b.z, b.w));
+        }
+      } else {                                                         // by way of the box, 32 columns at a time: in registers alone it would spill
+        if (lane == 0) bulk_store_read_done();
+        __syncwarp();
+        volatile float* line = reinterpret_cast<volatile float*>(box) + lane;                // the lane's own words
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+#pragma unroll
+          for (int i = 0; i < 32; ++i) line[i * 32] = __uint_as_float(words[c * 32 + i]);
+#pragma unroll 1
+          for (int i = 0; i < 32; ++i) line[i * 32] = fp4_finish<kGroup>(line[i * 32], fr, col_of[c * 32 + i], col_of[128 + c * 32 + i]);
+#pragma unroll
+          for (int i = 0; i < 32; ++i) words[c * 32 + i] = __float_as_uint(line[i * 32]);
+        }
+        __syncwarp();
       }
       // through shared memory, and out by TMA where rows start on 16-byte boundaries
       constexpr bool kWide = EPI == kBlkF32;
@@ -513,7 +542,7 @@ gemm_fp4_split_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_cons
           if (splits > 1) {
             part[row * 128 + quarter * 32 + lane] = __uint_as_float(r[i]);
           } else if (col < p.N && m0 + row < p.M) {
-            fp4_store_one<EPI>(p, m0 + row, col, fmaf(__uint_as_float(r[i]) * row_of[row], fc, bias));
+            fp4_store_one<EPI>(p, m0 + row, col, fp4_finish<kGroup>(__uint_as_float(r[i]), row_of[row], fc, bias));
           }
         }
       }
@@ -538,7 +567,7 @@ gemm_fp4_split_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_cons
 #pragma unroll
           for (int r = 0; r < 8; ++r) sum += v[k][r];
           const int row = m0 + i0 + k * splits;
-          if (i0 + k * splits < rows) fp4_store_one<EPI>(p, row, col, fmaf(sum * row_of[row - m0], fc, bias));
+          if (i0 + k * splits < rows) fp4_store_one<EPI>(p, row, col, fp4_finish<kGroup>(sum, row_of[row - m0], fc, bias));
         }
       }
     }
