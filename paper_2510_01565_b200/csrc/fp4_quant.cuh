@@ -464,7 +464,9 @@ dequantize_fp4_kernel(const Fp4ValuesParams p) {
   for (int i = 0; i < kTurns; ++i) {
     const int row = row0 + i * kValueWarps;
     if (row >= p.rows) break;                                      // (the whole warp)
-    const float scale = kGroup == 16 ? e4m3_value(byte[i]) : e8m0_value(byte[i]);
+    float scale = kGroup == 16 ? e4m3_value(byte[i]) : e8m0_value(byte[i]), times = factor[i];
+    // 6 * 2^126 is no fp32 number, but may be one under a row factor below 1: a part of the scale goes there (exactly, both are far from their limits)
+    if (kGroup == 32 && byte[i] >= 253 && fabsf(times) < 1.f) { scale *= 0.125f; times *= 8.f; }
     Out* out = static_cast<Out*>(p.out) + row * p.ld_out + c;
     float v[WORDS][8];
     uint32_t packed[WORDS][4];                                     // (16-bit types)
@@ -473,7 +475,7 @@ dequantize_fp4_kernel(const Fp4ValuesParams p) {
       e2m1_values(code[i][w], v[w]);
 #pragma unroll
       for (int j = 0; j < 8; j += 2) {
-        const float2 x = fmul2(fmul2(make_float2(v[w][j], v[w][j + 1]), make_float2(scale, scale)), make_float2(factor[i], factor[i]));
+        const float2 x = fmul2(fmul2(make_float2(v[w][j], v[w][j + 1]), make_float2(scale, scale)), make_float2(times, times));
         v[w][j] = x.x; v[w][j + 1] = x.y;
         if constexpr (kType != 2) packed[w][j / 2] = pack16x2<kType == 1>(x.x, x.y);
       }

@@ -1,4 +1,4 @@
-"""Row factors of the 4-bit product over all of fp32's range.
+"""Row factors of the 4-bit product and of the values, over all of fp32's range.
 
 A factor that is a power of two changes no bit of a sum, so the product with factors is the product without them times both factors, rounded
 once into the output's type: compared bit for bit, whatever the factors' sizes.  The result leaves the type's range where the whole product does, and not where a
@@ -86,6 +86,35 @@ def test_factors_that_are_no_powers_of_two_and_a_bias(B, m, n, k):
     room = 2 * 2.0 ** -24 * part.abs() * (1 + 2.0 ** -20) + 2.0 ** -24 * want.abs() * (1 + 2.0 ** -20) + 2.0 ** -148
     assert bool(((got - want).abs() <= room)[fits].all()) and int(fits.sum()) * 4 > m * n
     assert bool((got[~fits].abs() >= 2.0 ** 126).all())
+
+
+@pytest.mark.parametrize("cols", [256, 250])
+@pytest.mark.parametrize("kind", ["float16", "bfloat16", "float32"])
+@pytest.mark.parametrize("group", [16, 32])
+def test_values_of_large_scales_under_small_row_factors(B, group, kind, cols):
+    import torch
+    out_dtype = getattr(torch, kind)
+    rows = 140
+    codes = torch.randint(0, 256, (rows, 128), generator=torch.Generator().manual_seed(1), dtype=torch.uint8).cuda()[:, :(cols + 1) // 2]
+    shape = (2, -(-cols // (4 * group)), 512)
+    byte = torch.arange(512) % 128 if group == 16 else torch.arange(512) % 255
+    byte = torch.where(byte == 127, 126, byte) if group == 16 else byte
+    scales = byte.to(torch.uint8).expand(shape).contiguous().cuda()
+    # (of the very large and the very small scales, a value under each factor lies inside fp32)
+    factors = torch.tensor([1.0, 2.0 ** -100, 2.0 ** 100, 2.0 ** -20, -2.0 ** -126, 1.5, 2.0 ** 127], device="cuda")[torch.arange(rows, device="cuda") % 7]
+    got = B.dit_dequantize_fp4(codes, scales, cols, group, factors, out_dtype=out_dtype)
+    levels = torch.tensor([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0], dtype=torch.float64, device="cuda")
+    col, row = torch.arange(cols, device="cuda"), torch.arange(rows, device="cuda")[:, None]
+    code = ((codes.int()[:, col // 2] >> (4 * (col % 2))) & 15).long()
+    value = torch.where(code >= 8, -levels[code & 7], levels[code & 7])
+    at = col // group
+    byte = scales[row // 128, at // 4, row % 32 * 16 + row % 128 // 32 * 4 + at % 4]
+    scale = byte.view(torch.float8_e4m3fn).double() if group == 16 else torch.exp2(byte.double() - 127.0)
+    want = (value * scale * factors.double()[:, None]).float()
+    if out_dtype != torch.float32:
+        limit = torch.finfo(out_dtype).max
+        want = want.clamp(-limit, limit).to(out_dtype)
+    assert torch.equal(got, want)
 
 
 def test_a_row_in_batches_of_other_sizes(B):
