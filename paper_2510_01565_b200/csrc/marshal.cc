@@ -14,6 +14,7 @@
 #include <vector>
 
 #include "../../include/dit_ops.h"
+#include "prompt_call.h"
 
 namespace {
 
@@ -553,15 +554,22 @@ PyObject* prompt_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const OnStream on(a[11], q.device());
     const at::Tensor out = given(a[9]) ? tensor(a[9], "out") : empty({rows, width}, q.scalar_type(), q);
     if (!shaped(out, rows, width) || out.scalar_type() != q.scalar_type()) refuse("out must be shaped and typed like q");
-    at::Tensor workspace = optional(a[10], "workspace");
-    const size_t need = dit_prompt_attention_workspace(&p);
-    if (!workspace.defined() && need > 0) workspace = empty({static_cast<int64_t>(need)}, at::kByte, q);
+    const at::Tensor workspace = optional(a[10], "workspace");
     if (workspace.defined() && (!workspace.is_cuda() || !workspace.is_contiguous())) refuse("workspace must be a contiguous CUDA tensor");
     same_device(q, {&k, &v, &out, &workspace});
     p.ld_out = matrix(out, "out");
     p.q = q.data_ptr(); p.k = k.data_ptr(); p.v = v.data_ptr(); p.out = out.data_ptr();
-    if (workspace.defined()) { p.workspace = workspace.data_ptr(); p.workspace_bytes = workspace.nbytes(); }
-    check(dit_prompt_attention(&p, on.raw));
+    if (workspace.defined()) {
+      p.workspace = workspace.data_ptr(); p.workspace_bytes = workspace.nbytes();
+      check(dit_prompt_attention(&p, on.raw));
+    } else {
+      struct Room { const at::Tensor& like; at::Tensor memory; } room{q, {}};
+      check(dit::prompt_attention_in(p, [](void* context, size_t bytes) {
+        Room& r = *static_cast<Room*>(context);
+        r.memory = empty({static_cast<int64_t>(bytes)}, at::kByte, r.like);
+        return r.memory.data_ptr();
+      }, &room, on.raw));
+    }
     return THPVariable_Wrap(out);
   });
 }

@@ -1,11 +1,13 @@
 // Rotary positions and attention over packed prompts (include/dit_ops.h): argument checks, tensor maps, launch rules.
 #include <algorithm>
 #include <cmath>
+#include <functional>
 #include <mutex>
 
 #include "common.cuh"
 #include "ops_launch.h"
 #include "prompt_attention.cuh"
+#include "prompt_call.h"
 #include "rotary.cuh"
 
 using namespace dit;
@@ -96,23 +98,6 @@ struct PromptPlan {
 };
 constexpr int kSms = 148;                        // (plans, and with them workspaces, depend on the sizes of a call alone)
 
-int64_t few_row_ctas(const PromptPlan& p, const dit_prompt_attention_args& a, int chunk) {
-  int64_t n = 0;
-  for (int i = 0; i < p.few.n; ++i) {
-    const int r = p.few.order[i];
-    n += static_cast<int64_t>(a.n_kv_heads) * prompt_row_tiles(a.q_lens[r], a.n_heads / a.n_kv_heads) * prompt_parts(a.kv_lens[r], chunk);
-  }
-  return n;
-}
-int64_t pairs_with(const PromptPlan& p, const dit_prompt_attention_args& a, int blocks) {
-  int64_t n = 0;
-  for (int i = 0; i < p.tiled.n; ++i) {
-    const int r = p.tiled.order[i];
-    n += pairs_of(a.q_lens[r], a.kv_lens[r], a.n_heads / a.n_kv_heads, a.causal != 0, blocks);
-  }
-  return n * a.n_kv_heads;
-}
-
 // Estimates in us, from measurements.  The tiled kernel takes 7 us for anything, 1.7 for a key block of a pair of tiles (pairs side by side on the
 // SMs) and 2.6 per pair; the few-row kernel 4 us, 0.45 for 64 keys of a part, and altogether the time to read the keys once for every 16
 // rows, from L2 behind the first time, at 7 TB/s.
@@ -141,37 +126,84 @@ int few_of(const dit_prompt_attention_args& a, RequestCost* c, int n) {
   return best;
 }
 
-// Key blocks of an item at most, 0 for whole pairs: cut where the longest pair would outlast the work of all by far, so that few pairs are dealt
-// out to many SMs.  The time of a cut is that of the fullest CTA, as the items will be dealt out, and what the parts cost: their results through
+// Key blocks of the pairs of the tiled kernel, most first; returns their number.
+int pair_lengths(const PromptPlan& p, const dit_prompt_attention_args& a, int* length) {
+  const int group = a.n_heads / a.n_kv_heads;
+  int n = 0;
+  for (int i = 0; i < p.tiled.n; ++i) {
+    const int r = p.tiled.order[i], q_len = a.q_lens[r], kv_len = a.kv_lens[r], row_blocks = (q_len + 127) / 128;
+    const int pairs = static_cast<int>((static_cast<int64_t>(row_blocks) * group + 1) / 2);
+    for (int pair = 0; pair < pairs; ++pair) {     // (a request's own come most first)
+      const int64_t rows = static_cast<int64_t>(row_blocks - 2 * pair / group) * 128;      // up to the end of the pair's first row block
+      const int64_t keys = a.causal ? std::max<int64_t>(0, kv_len - q_len + std::min<int64_t>(q_len, rows)) : kv_len;
+      length[n++] = static_cast<int>((keys + 127) / 128);
+    }
+  }
+  if (p.tiled.n > 1) std::sort(length, length + n, std::greater<int>());
+  for (int i = n - 1; i >= 0; --i)                 // every key head's
+    for (int h = 0; h < a.n_kv_heads; ++h) length[i * a.n_kv_heads + h] = length[i];
+  return n * a.n_kv_heads;
+}
+// Time of the fullest CTA when items of up to `part` key blocks are dealt out, first parts, second parts ..., forwards and backwards in turn; *items counts
+// them.  Whole parts cost the same, so they are added round by round.
+double deal_out(const int* length, int n, int part, int* items) {
+  double load[kSms] = {};
+  int at = 0, round = 0, count = 0;              // CTAs of the round that have their item
+  const double whole = kPairBlock * part + kPair;
+  for (int t = 0, m = n; m > 0; ++t) {
+    int next = m;                                // pairs with a further part: their t-th is a whole one
+    while (next > 0 && length[next - 1] <= (t + 1) * part) --next;
+    for (int left = next; left > 0;) {
+      const int here = std::min(left, kSms - at), low = (round & 1) ? kSms - at - here : at;
+      for (int i = low; i < low + here; ++i) load[i] += whole;
+      left -= here; at += here;
+      if (at == kSms) { at = 0; ++round; }
+    }
+    for (int i = next; i < m; ++i) {
+      load[(round & 1) ? kSms - 1 - at : at] += kPairBlock * std::min(part, length[i] - t * part) + kPair;
+      if (++at == kSms) { at = 0; ++round; }
+    }
+    count += m;
+    m = next;
+  }
+  *items = count;
+  return *std::max_element(load, load + kSms);
+}
+
+// Key blocks of an item at most, into p->part_blocks, 0 for whole pairs: cut where the longest pair would outlast the work of all by far, so that few pairs
+// are dealt out to many SMs.  The time of a cut is that of the fullest CTA, as the items will be dealt out, and what the parts cost: their results through
 // memory and a joining kernel.  us whole, and for the cut that is chosen: 8 heads of 64, 3240 rows 45, 33; 4 heads of 128, 8192 rows
 // 101, 77; one head, 16384 rows 190, 78; 128 rows of 32 heads over 8 key heads against 32768 keys 369, 79.
-int choose_parts(const PromptPlan& p, const dit_prompt_attention_args& a, double blocks) {
-  constexpr int kMost = 512;
-  const double chain = kPairBlock * p.most_blocks + kPair, work = (kPairBlock * blocks + kPair * p.pairs) / kSms;
-  if (p.pairs > kMost || chain < 1.3 * work + 8.0) return 0;
-  int length[kMost], n = 0;                      // key blocks of the pairs, most first
-  for (int c = p.most_blocks, before = 0; c >= 0; --c) {
-    const int now = static_cast<int>(pairs_with(p, a, c));
-    for (; before < now; ++before) length[n++] = c;
+// The host's time is part of a call's: cuts are tried in the order of a bound below their time, until no bound promises less than the best found.
+void choose_parts(PromptPlan* p, const dit_prompt_attention_args& a, double blocks) {
+  constexpr int kMost = 512, kTries = 64;
+  const double chain = kPairBlock * p->most_blocks + kPair, work = (kPairBlock * blocks + kPair * p->pairs) / kSms;
+  if (p->pairs > kMost || chain < 1.3 * work + 8.0) return;
+  int length[kMost];
+  const int n = pair_lengths(*p, a, length);
+  double total = 0;
+  for (int i = 0; i < n; ++i) total += length[i];
+  struct Try { double bound; int part; } tries[kTries];
+  int count = 0, longer = n;                     // pairs with more than `part` key blocks, `blocks_of` in all
+  double blocks_of = total;
+  for (int part = std::max(4, (p->most_blocks + kTileParts - 1) / kTileParts); 3 * part <= 2 * p->most_blocks && count < kTries; part += std::max(1, part / 4)) {
+    while (longer > 0 && length[longer - 1] <= part) blocks_of -= length[--longer];
+    const double items = n - longer + std::max(2.0 * longer, blocks_of / part);
+    const double most = std::max(kPairBlock * part + kPair, (kPairBlock * total + kPair * items) / kSms);
+    tries[count++] = Try{most + 6.0 + 0.06 * items, part};
   }
+  std::sort(tries, tries + count, [](const Try& x, const Try& y) { return x.bound != y.bound ? x.bound < y.bound : x.part < y.part; });
   double least = 0.95 * chain;
-  int best = 0;
-  for (int part = std::max(4, (p.most_blocks + kTileParts - 1) / kTileParts); 3 * part <= 2 * p.most_blocks; part += std::max(1, part / 4)) {
-    double load[kSms] = {}, most = 0;
+  int best = 0, best_items = 0;
+  for (int i = 0; i < count && tries[i].bound * (1.0 - 1e-9) <= least; ++i) {
     int items = 0;
-    for (int t = 0, m = n; m > 0 && most < least; ++t) {
-      for (int i = 0; i < m; ++i, ++items) {
-        const int round = items / kSms, at = items - round * kSms;
-        double& mine = load[(round & 1) ? kSms - 1 - at : at];
-        mine += kPairBlock * std::min(part, length[i] - t * part) + kPair;
-        most = std::max(most, mine);
-      }
-      while (m > 0 && length[m - 1] <= (t + 1) * part) --m;
-    }
-    const double time = most + 6.0 + 0.06 * items;
-    if (time < least) { least = time; best = part; }
+    const double time = deal_out(length, n, tries[i].part, &items) + 6.0 + 0.06 * items;
+    if (time < least || (time == least && best > 0 && tries[i].part < best)) { least = time; best = tries[i].part; best_items = items; }
   }
-  return best;
+  if (best == 0) return;
+  p->part_blocks = best;
+  p->items = best_items;
+  for (p->cut = 0; p->cut < n && length[p->cut] > best; ++p->cut) {}
 }
 
 // Checks sizes and lays the batch out.
@@ -227,19 +259,28 @@ dit_status plan_prompts(const dit_prompt_attention_args& a, PromptPlan* p) {
   }
   if (p->pairs > INT32_MAX / 16) return DIT_ERR_SHAPE;
   p->items = p->pairs;
-  if (p->pairs > 0 && (p->part_blocks = choose_parts(*p, a, blocks)) > 0) {
-    p->cut = pairs_with(*p, a, p->part_blocks + 1);
-    for (int t = 1; t * p->part_blocks < p->most_blocks; ++t) p->items += pairs_with(*p, a, t * p->part_blocks + 1);
-  }
+  if (p->pairs > 0) choose_parts(p, a, blocks);
   if (p->few.n > 0) {
     // Parts of equal length, one for each SM: what a CTA costs before its first product and after its last one is several us, and one per SM
     // keeps enough loads in flight (one row of 32 heads against 32768 keys, parts of 256, 896, 1792 keys: 60, 34, 29 us).  Beyond 4096 keys
     // a part is only cut off: more CTAs than SMs are resident at once, and share the memory's bandwidth evenly.
     const int least = static_cast<int>(std::min(4096.0, std::max(256.0, std::ceil(keys / kSms / 64) * 64)));
+    int64_t tiles[DIT_MAX_REQUESTS], ctas;
+    int keys_of[DIT_MAX_REQUESTS];
+    for (int i = 0; i < p->few.n; ++i) {
+      const int r = p->few.order[i];
+      tiles[i] = static_cast<int64_t>(a.n_kv_heads) * prompt_row_tiles(a.q_lens[r], static_cast<int>(group));
+      keys_of[i] = a.kv_lens[r];
+    }
+    auto ctas_with = [&](int chunk) {
+      int64_t n = 0;
+      for (int i = 0; i < p->few.n; ++i) n += tiles[i] * prompt_parts(keys_of[i], chunk);
+      return n;
+    };
     int chunk = least;
-    while (few_row_ctas(*p, a, chunk) > kSms && chunk < 2 * least) chunk += std::max(64, least / 16 / 64 * 64);
+    while ((ctas = ctas_with(chunk)) > kSms && chunk < 2 * least) chunk += std::max(64, least / 16 / 64 * 64);
     p->chunk = std::min(chunk, 4096);
-    p->ctas = few_row_ctas(*p, a, p->chunk);
+    p->ctas = p->chunk == chunk ? ctas : ctas_with(p->chunk);
     if (p->ctas > INT32_MAX / 16) return DIT_ERR_SHAPE;
     p->join = p->ctas > p->row_tiles;
   }
@@ -250,7 +291,7 @@ size_t few_bytes(const PromptPlan& p, int head_dim) { return p.join ? static_cas
 size_t part_bytes(const PromptPlan& p, int head_dim) { return few_bytes(p, head_dim) + (p.part_blocks > 0 ? static_cast<size_t>(p.items) * 2 * 128 * (head_dim + 4) * sizeof(float) : 0); }
 
 template <int D, bool BF16>
-cudaError_t launch_attention(const OpsDevice& d, const dit_prompt_attention_args& a, const PromptPlan& plan, PromptAttnParams p, cudaStream_t st) {
+cudaError_t launch_attention(const OpsDevice& d, const dit_prompt_attention_args& a, const PromptPlan& plan, PromptAttnParams p, void* workspace, cudaStream_t st) {
   const uint64_t width = static_cast<uint64_t>(a.n_heads) * D, kv_width = static_cast<uint64_t>(a.n_kv_heads) * D;
   const int q_rows = plan.tiled.cu_q[a.n_requests], kv_rows = plan.tiled.cu_kv[a.n_requests];
   // without keys nothing is loaded; the maps still have to describe some memory
@@ -265,7 +306,7 @@ cudaError_t launch_attention(const OpsDevice& d, const dit_prompt_attention_args
       return cudaErrorInvalidValue;
     p.items = static_cast<int>(plan.items); p.pairs = static_cast<int>(plan.pairs);
     p.most_blocks = plan.most_blocks; p.part_blocks = plan.part_blocks;
-    p.tile_parts = reinterpret_cast<float*>(static_cast<char*>(a.workspace) + few_bytes(plan, D));
+    p.tile_parts = reinterpret_cast<float*>(static_cast<char*>(workspace) + few_bytes(plan, D));
     const int grid = std::min(p.items, d.num_sms);
     auto kernel = p.part_blocks > 0 ? &prompt_attention_kernel<D, BF16, true> : &prompt_attention_kernel<D, BF16, false>;
     // (beside the few-row kernel, which starts under this one and does not wait for what is in front of both, the ordinary launch)
@@ -277,7 +318,7 @@ cudaError_t launch_attention(const OpsDevice& d, const dit_prompt_attention_args
     if (!half_map(d, &tmK, k, kv_width, std::max(kv_rows, 1), ld_k, kRowsTile) || !half_map(d, &tmV, v, kv_width, std::max(kv_rows, 1), ld_v, kRowsTile))
       return cudaErrorInvalidValue;
     p.chunk = plan.chunk;
-    p.parts = static_cast<float*>(a.workspace);
+    p.parts = static_cast<float*>(workspace);
     p.beside = plan.items > 0;
     if ((e = launch_overlapping(&prompt_rows_kernel<D, BF16>, dim3(static_cast<unsigned>(plan.ctas)), PromptRowsCfg<D>::THREADS, PromptRowsCfg<D>::SMEM_BYTES, st, tmK, tmV, p, plan.few)) != cudaSuccess)
       return e;
@@ -288,6 +329,38 @@ cudaError_t launch_attention(const OpsDevice& d, const dit_prompt_attention_args
   if (plan.part_blocks > 0)
     return launch_overlapping(&prompt_tile_join_kernel<D, BF16>, dim3(static_cast<unsigned>(plan.cut), 2 * D / 32), 256, 0, st, p, plan.tiled);
   return cudaSuccess;
+}
+
+// Checks what the plan did not look at and launches.  give(bytes, &workspace) is asked for memory where the plan needs some.
+template <class Give>
+dit_status attend(const dit_prompt_attention_args& a, const PromptPlan& plan, Give&& give, void* stream) {
+  const int64_t width = static_cast<int64_t>(a.n_heads) * a.head_dim, kv_width = static_cast<int64_t>(a.n_kv_heads) * a.head_dim;
+  auto matrix = [&](const void* p, int64_t ld, int64_t rows, int64_t cols) { return rows == 0 || (p && aligned(p, 16) && ld >= cols && ld % 8 == 0); };
+  const int q_rows = plan.tiled.cu_q[a.n_requests], kv_rows = plan.tiled.cu_kv[a.n_requests];
+  if (!matrix(a.q, a.ld_q, q_rows, width) || !matrix(a.out, a.ld_out, q_rows, width) || !matrix(a.k, a.ld_k, kv_rows, kv_width) ||
+      !matrix(a.v, a.ld_v, kv_rows, kv_width))
+    return DIT_ERR_INVALID_ARG;
+  if (!(a.scale >= 0.f) || !(a.scale <= 2.0e38f)) return DIT_ERR_INVALID_ARG;        // scale * log2(e) has to be finite
+  if (q_rows == 0) return DIT_OK;
+  void* workspace = nullptr;
+  dit_status s;
+  if (const size_t need = part_bytes(plan, a.head_dim); need > 0 && (s = give(need, &workspace)) != DIT_OK) return s;
+  OpsDevice d;
+  s = ops_device(&d);
+  if (s != DIT_OK) return s;
+  if (prepare(d) != cudaSuccess) return DIT_ERR_CUDA;
+  PromptAttnParams p{};
+  p.out = a.out; p.ld_out = a.ld_out; p.q = static_cast<const uint16_t*>(a.q); p.v = static_cast<const uint16_t*>(a.v);
+  p.ld_q = a.ld_q; p.ld_v = a.ld_v; p.n_heads = a.n_heads; p.kv_heads = a.n_kv_heads; p.group = a.n_heads / a.n_kv_heads;
+  p.causal = a.causal != 0;
+  p.scale_log2 = 1.4426950408889634f * (a.scale > 0.f ? a.scale : 1.0f / sqrtf(static_cast<float>(a.head_dim)));
+  p.wide_out = aligned(a.out, 32) && a.ld_out % 16 == 0;
+  p.status = d.status;
+  const cudaStream_t st = static_cast<cudaStream_t>(stream);
+  cudaError_t e;
+  if (a.head_dim == 128) e = a.type == DIT_TYPE_BF16 ? launch_attention<128, true>(d, a, plan, p, workspace, st) : launch_attention<128, false>(d, a, plan, p, workspace, st);
+  else e = a.type == DIT_TYPE_BF16 ? launch_attention<64, true>(d, a, plan, p, workspace, st) : launch_attention<64, false>(d, a, plan, p, workspace, st);
+  return e == cudaSuccess ? DIT_OK : DIT_ERR_CUDA;
 }
 
 }  // namespace
@@ -362,35 +435,23 @@ size_t dit_prompt_attention_workspace(const dit_prompt_attention_args* a) {
 dit_status dit_prompt_attention(const dit_prompt_attention_args* a, void* stream) {
   if (!a) return DIT_ERR_INVALID_ARG;
   PromptPlan plan;
-  dit_status s = plan_prompts(*a, &plan);
+  const dit_status s = plan_prompts(*a, &plan);
   if (s != DIT_OK) return s;
-  const int64_t width = static_cast<int64_t>(a->n_heads) * a->head_dim, kv_width = static_cast<int64_t>(a->n_kv_heads) * a->head_dim;
-  auto matrix = [&](const void* p, int64_t ld, int64_t rows, int64_t cols) { return rows == 0 || (p && aligned(p, 16) && ld >= cols && ld % 8 == 0); };
-  const int q_rows = plan.tiled.cu_q[a->n_requests], kv_rows = plan.tiled.cu_kv[a->n_requests];
-  if (!matrix(a->q, a->ld_q, q_rows, width) || !matrix(a->out, a->ld_out, q_rows, width) || !matrix(a->k, a->ld_k, kv_rows, kv_width) ||
-      !matrix(a->v, a->ld_v, kv_rows, kv_width))
-    return DIT_ERR_INVALID_ARG;
-  if (!(a->scale >= 0.f) || !(a->scale <= 2.0e38f)) return DIT_ERR_INVALID_ARG;      // scale * log2(e) has to be finite
-  if (q_rows == 0) return DIT_OK;
-  const size_t need = part_bytes(plan, a->head_dim);
-  if (need > 0 && (!a->workspace || !aligned(a->workspace, 16))) return DIT_ERR_INVALID_ARG;
-  if (a->workspace_bytes < need) return DIT_ERR_CAPACITY;
-  OpsDevice d;
-  s = ops_device(&d);
-  if (s != DIT_OK) return s;
-  if (prepare(d) != cudaSuccess) return DIT_ERR_CUDA;
-  PromptAttnParams p{};
-  p.out = a->out; p.ld_out = a->ld_out; p.q = static_cast<const uint16_t*>(a->q); p.v = static_cast<const uint16_t*>(a->v);
-  p.ld_q = a->ld_q; p.ld_v = a->ld_v; p.n_heads = a->n_heads; p.kv_heads = a->n_kv_heads; p.group = a->n_heads / a->n_kv_heads;
-  p.causal = a->causal != 0;
-  p.scale_log2 = 1.4426950408889634f * (a->scale > 0.f ? a->scale : 1.0f / sqrtf(static_cast<float>(a->head_dim)));
-  p.wide_out = aligned(a->out, 32) && a->ld_out % 16 == 0;
-  p.status = d.status;
-  const cudaStream_t st = static_cast<cudaStream_t>(stream);
-  cudaError_t e;
-  if (a->head_dim == 128) e = a->type == DIT_TYPE_BF16 ? launch_attention<128, true>(d, *a, plan, p, st) : launch_attention<128, false>(d, *a, plan, p, st);
-  else e = a->type == DIT_TYPE_BF16 ? launch_attention<64, true>(d, *a, plan, p, st) : launch_attention<64, false>(d, *a, plan, p, st);
-  return e == cudaSuccess ? DIT_OK : DIT_ERR_CUDA;
+  return attend(*a, plan, [&](size_t need, void** workspace) {
+    if (!a->workspace || !aligned(a->workspace, 16)) return DIT_ERR_INVALID_ARG;
+    *workspace = a->workspace;
+    return a->workspace_bytes < need ? DIT_ERR_CAPACITY : DIT_OK;
+  }, stream);
 }
 
 }  // extern "C"
+
+dit_status dit::prompt_attention_in(const dit_prompt_attention_args& a, void* (*room)(void*, size_t), void* context, void* stream) {
+  PromptPlan plan;
+  const dit_status s = plan_prompts(a, &plan);
+  if (s != DIT_OK) return s;
+  return attend(a, plan, [&](size_t need, void** workspace) {
+    *workspace = room(context, need);
+    return *workspace ? DIT_OK : DIT_ERR_CAPACITY;
+  }, stream);
+}
