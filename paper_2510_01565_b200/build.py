@@ -4,6 +4,7 @@ from __future__ import annotations
 
 import os
 import subprocess
+import time
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
@@ -22,12 +23,12 @@ def _newest_source_mtime() -> float:
     return t
 
 
-def _fresh(obj: str) -> bool:
-    """Whether an object is newer than every file that its dependency list names."""
+def _fresh(obj: str, made_by: str) -> bool:
+    """Whether an object was made by this compiler and command, to the end, from the files that its dependency list names as they are now."""
     try:
-        named = open(obj + ".d").read().replace("\\\n", " ").split()[1:]
-        return all(os.path.getmtime(p) < os.path.getmtime(obj) for p in named)
-    except OSError:
+        named = open(obj + ".d").read().replace("\\\n", " ").split(" : ", 1)[1].split()        # "object : source header ..."
+        return open(obj + ".by").read() == made_by and all(os.path.getmtime(p) < os.path.getmtime(obj) for p in named)
+    except (OSError, IndexError):
         return False
 
 
@@ -37,14 +38,26 @@ def build_library(force: bool = False, verbose: bool = False) -> str:
     if not force and all(os.path.exists(p) and os.path.getmtime(p) >= newest for p in (LIB, MARSHAL)):
         return LIB
     nvcc = os.environ.get("NVCC", "nvcc")
+    version = subprocess.run([nvcc, "--version"], capture_output=True, text=True).stdout
     os.makedirs(OBJECTS, exist_ok=True)
     objects = [os.path.join(OBJECTS, os.path.basename(src) + ".o") for src in SOURCES]
     jobs = []                                      # sources are compiled side by side, those whose object is older than what it was made of
     for src, obj in zip(SOURCES, objects):
-        if force or not _fresh(obj):
-            cmd = [nvcc] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + ["-MMD", "-MF", obj + ".d", "-c", src, "-o", obj]
-            jobs.append((src, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
-    done = [(src, job.communicate()[0], job.returncode) for src, job in jobs]
+        cmd = [nvcc] + NVCC_FLAGS + ["-MMD", "-MF", obj + ".d", "-c", src, "-o", obj]
+        made_by = "\n".join(cmd + [version])
+        if force or not _fresh(obj, made_by):
+            if os.path.exists(obj + ".by"):
+                os.remove(obj + ".by")
+            start = time.time()
+            jobs.append((src, obj, made_by, start, subprocess.Popen(cmd[:-4] + (["-Xptxas", "-v"] if verbose else []) + cmd[-4:], stdout=subprocess.PIPE,
+                                                                    stderr=subprocess.STDOUT, text=True)))
+    done = []
+    for src, obj, made_by, start, job in jobs:
+        done.append((src, job.communicate()[0], job.returncode))
+        if job.returncode == 0:
+            os.utime(obj, (start, start))          # (a file that changed meanwhile is newer)
+            with open(obj + ".by", "w") as f:
+                f.write(made_by)
     if verbose:
         print("".join(out for _, out, _ in done))
     for src, out, code in done:
