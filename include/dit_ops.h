@@ -206,9 +206,10 @@ dit_status dit_gemm_fp4(const dit_gemm_fp4_args *args, void *stream);
  *               q | k | v buffer may be turned in one call: n_heads = query heads + key heads
  *   positions   device int32 [rows], any values, or NULL: request r has lens[r] rows at positions first[r], first[r] + 1, ...
  *               (HOST arrays; first NULL: 0, otherwise >= 0; positions end before 2^31)
- * Angles are taken in 64 bits and reduced before they are narrowed: cosine and sine are off by at most 2^-21 up to position 2^24.  Results are
- * rounded once from fp32; infinities and NaN spread within their pair.  rotary_dim even, 2 .. min(head_dim, 256); head_dim <= 4096;
- * base > 0, factor >= 1, high > low where trained_len > 0, all finite.  rows == 0 is a no-op. */
+ * Angles are taken in 64 bits and reduced before they are narrowed: cosine and sine are off by at most 2^-21 up to position 2^24 where base >= 1
+ * (no pair turns faster than its position).  Results are rounded once from fp32; infinities and NaN spread within their pair.  rotary_dim even,
+ * 2 .. min(head_dim, 256); head_dim <= 4096; base > 0 with finite angles at every position, factor >= 1, high > low where trained_len > 0, all
+ * finite.  rows == 0 is a no-op. */
 typedef struct {
   const void *x;
   void *out;

@@ -378,6 +378,19 @@ dit_status dit_rotary(const dit_rotary_args* a, void* stream) {
     return DIT_ERR_INVALID_ARG;
   if (a->trained_len > 0.0 && (!std::isfinite(a->low) || !std::isfinite(a->high) || !(a->high > a->low))) return DIT_ERR_INVALID_ARG;
   RotaryParams p{};
+  p.pairs = a->rotary_dim / 2;
+  constexpr double kTurn = 6.283185307179586476925287;
+  for (int i = 0; i < p.pairs; ++i) {
+    double f = std::pow(a->base, -2.0 * i / a->rotary_dim);
+    if (a->trained_len > 0.0) {
+      const double keep = std::min(1.0, std::max(0.0, (a->trained_len * f / kTurn - a->low) / (a->high - a->low)));
+      f *= keep + (1.0 - keep) / a->factor;
+    } else {
+      f /= a->factor;
+    }
+    p.turns[i] = f / kTurn;
+    if (!std::isfinite(p.turns[i] * 2147483648.0)) return DIT_ERR_INVALID_ARG;       // (a base next to zero)
+  }
   if (!a->positions) {
     if (a->n_requests < 0 || (a->n_requests > 0 && !a->lens)) return DIT_ERR_INVALID_ARG;
     if (a->n_requests > DIT_MAX_REQUESTS) return DIT_ERR_CAPACITY;
@@ -403,19 +416,8 @@ dit_status dit_rotary(const dit_rotary_args* a, void* stream) {
   const dit_status s = ops_device(&d);
   if (s != DIT_OK) return s;
   p.x = a->x; p.out = a->out; p.ld_x = a->ld_x; p.ld_out = a->ld_out; p.rows = a->rows; p.positions = a->positions;
-  p.n_heads = a->n_heads; p.head_dim = a->head_dim; p.pairs = a->rotary_dim / 2; p.inverse = a->inverse != 0;
+  p.n_heads = a->n_heads; p.head_dim = a->head_dim; p.inverse = a->inverse != 0;
   p.magnitude = a->magnitude;
-  constexpr double kTurn = 6.283185307179586476925287;
-  for (int i = 0; i < p.pairs; ++i) {
-    double f = std::pow(a->base, -2.0 * i / a->rotary_dim);
-    if (a->trained_len > 0.0) {
-      const double keep = std::min(1.0, std::max(0.0, (a->trained_len * f / kTurn - a->low) / (a->high - a->low)));
-      f *= keep + (1.0 - keep) / a->factor;
-    } else {
-      f /= a->factor;
-    }
-    p.turns[i] = f / kTurn;
-  }
   // four rows per CTA once that leaves every SM one
   p.rows_per_cta = a->rows >= static_cast<int64_t>(kRotaryRows) * d.num_sms ? kRotaryRows : 1;
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
