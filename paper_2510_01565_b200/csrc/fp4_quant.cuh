@@ -162,7 +162,8 @@ __device__ __forceinline__ long long scale_at(int row, int group, int chunks) {
 // 9216 x 12288 fp16 49 us, 5.9 TB/s (groups of 32, without the meeting of the CTA, 43).
 // kBytes: what rows' starts are multiples of, 32 (one load per group of 16 16-bit numbers: its scale is found once), 16, or 0: anywhere,
 // loads of 16 bytes' worth made up of smaller ones.
-// Registers are held down so that 1280 threads (1536 with little to hold) fit an SM: 4096 x 40000 fp16, read twice, 140 -> 92 us, 10630 x 6480 44 -> 40.
+// Registers are held down to what lets as many whole CTAs as go into 1280 threads (1536 with little to hold) fit an SM: five of 256 threads, two of 512 (one
+// without the bound; 4096 x 40000 fp16, read twice, 140 -> 92 us, 10630 x 6480 44 -> 40).
 template <int kType, int kGroup, int kBytes, int THREADS, int kLoads>
 __global__ void __launch_bounds__(THREADS == 32 ? 256 : THREADS, (kLoads * (kBytes == 32 ? 2 : 1) <= 4 ? 1536 : 1280) / (THREADS == 32 ? 256 : THREADS))
 quantize_fp4_kernel(const Fp4QuantParams p) {
@@ -332,7 +333,7 @@ quantize_weight_fp4_kernel(const Fp4QuantWeightParams p) {
   // rows an odd number of words apart, and groups shifted against one another: lanes of several groups and rows meet in different banks
   constexpr int PITCH = kWeightOut + (kType == 2 ? 1 : 2), SHIFT = kGroup == 32 ? 8 : 4;
   auto place = [](int r) { return r * PITCH + r / kGroup * SHIFT; };
-  __shared__ Elem tile[kIn * PITCH + kIn / kGroup * SHIFT];
+  __shared__ __align__(16) Elem tile[kIn * PITCH + kIn / kGroup * SHIFT];          // (16-bit weights are written in pairs)
   dependents_may_start();
   await_predecessor();
   const int out_tiles = (p.out_dim + 127) / 128 * 2;               // whole scale tiles
