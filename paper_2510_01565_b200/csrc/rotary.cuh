@@ -19,7 +19,7 @@ struct RotaryParams {
   long long ld_x, ld_out;
   long long rows;
   const int* positions;      // [rows], or NULL: by the batch
-  int n_heads, head_dim, pairs, interleaved, inverse;
+  int n_heads, head_dim, pairs, inverse;
   int rows_per_cta;          // 1 or 4
   int pieces;                // of a head, kUnits at most
   float magnitude;
