@@ -60,16 +60,13 @@ __device__ __forceinline__ void tma_load_3d_pair(uint32_t dst, const void* tmap,
 }
 
 // A finished sum with its row's and its column's factor and the bias.  A caller's factors may be of any size (a quantiser's row factors span 2^-111 to
-// 2^117): the result leaves fp32's range where the whole product does.  Of a factor above 1 and one that is not, the product of the two comes
-// first, whose size lies between theirs; two on the same side of 1 are taken one after the other, and the sum moves one way only.
-// fp4_far: the sum times the row's factor alone may leave the range.  Sums under e4m3 scales are 0 or 2^-20 .. 2^53 in size; under powers of two they may
-// be anything.
-template <int kGroup>
-__device__ __forceinline__ bool fp4_far(float fr) { return kGroup == 32 ? fr != 1.f : fabsf(fr) < 0x1p-100f || fabsf(fr) > 0x1p73f; }
-template <int kGroup>
+// 2^117): the result leaves fp32's range where the whole product does.  Where the sum times the row's factor is already outside it, and the column's
+// factor leads back, the product of the two factors comes first, whose size lies between theirs.
 __device__ __forceinline__ float fp4_finish(float sum, float fr, float fc, float bias) {
-  if (fp4_far<kGroup>(fr) && (fabsf(fr) > 1.f) != (fabsf(fc) > 1.f)) return fmaf(sum, fr * fc, bias);
-  return fmaf(sum * fr, fc, bias);
+  const float t = sum * fr;
+  const bool outside = !(fabsf(t) < INFINITY) || (fabsf(t) < 0x1p-126f && sum != 0.f);
+  const bool across = outside && (fabsf(fr) > 1.f) != (fabsf(fc) > 1.f);
+  return fmaf(across ? sum : t, across ? fr * fc : fc, bias);
 }
 
 // Scale tiles per stage of 256 k, and how a step of 64 k finds its scales in them.
@@ -275,7 +272,6 @@ gemm_fp4_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
     const uint32_t tempty_leader = map_to_cta(tempty_bar(0), 0), shared_leader = map_to_cta(shared_bar, 0);
     uint8_t* box = aligned + C::OFF_OUT + (warp - 4) * BOX_BYTES;
     float* col_of = reinterpret_cast<float*>(aligned + C::OFF_COL + chalf * COL_BYTES);      // factors, then bias
-    const uint64_t policy = evict_first_policy();
     bool ok = true;                            // after a failed wait the warps still meet at their barriers, tile after tile
     int n = 0;
     for (int t = pair; t < num_tiles; t += num_pairs, ++n) {
@@ -318,15 +314,20 @@ gemm_fp4_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
       __syncwarp();
       if (lane == 0) mbar_arrive_cluster_light(tempty_leader + 8u * buf);
       if (!mine) continue;                     // (its warps of the next tile wait at its column factors)
-      if (!__any_sync(0xffffffffu, fp4_far<kGroup>(fr))) {
+      // Whether a sum times the row's factor may be outside fp32's range.  Sums under e4m3 scales are 0 or 2^-20 .. 2^53 in size; under powers of two they
+      // may be anything, and are looked through where there are factors.
+      bool far = __any_sync(0xffffffffu, kGroup == 16 ? fabsf(fr) < 0x1p-100f || fabsf(fr) > 0x1p73f : fr != 1.f);
+      if (kGroup == 32 && far) {
+        uint32_t most = 0, least = 0xffffffffu;                        // of the sums' magnitudes, of those that are not zero (less one)
 #pragma unroll
-        for (int i = 0; i < 64; i += 2) {                              // (row factor * sum) * column factor + bias
-          const float4 f = *reinterpret_cast<const float4*>(col_of + 2 * i), b = *reinterpret_cast<const float4*>(col_of + 128 + 2 * i);
-          const float2 r = make_float2(fr, fr);
-          acc[i] = ffma2(fmul2(acc[i], r), make_float2(f.x, f.y), make_float2(b.x, b.y));
-          acc[i + 1] = ffma2(fmul2(acc[i + 1], r), make_float2(f.z, f.w), make_float2(b.z, b.w));
+        for (int i = 0; i < 128; ++i) {
+          most = max(most, words[i] & 0x7FFFFFFFu);
+          least = min(least, (words[i] & 0x7FFFFFFFu) - 1);
         }
-      } else {                                                         // by way of the box, 32 columns at a time: in registers alone it would spill
+        const float size = fabsf(fr);
+        far = __any_sync(0xffffffffu, !(__uint_as_float(most) * size < INFINITY) || (least != 0xffffffffu && __uint_as_float(least + 1) * size < 0x1p-126f));
+      }
+      if (far) {                                                       // by way of the box, 32 columns at a time: in registers alone it would spill
         if (lane == 0) bulk_store_read_done();
         __syncwarp();
         volatile float* line = reinterpret_cast<volatile float*>(box) + lane;                // the lane's own words
@@ -335,7 +336,13 @@ gemm_fp4_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
 #pragma unroll
           for (int i = 0; i < 32; ++i) line[i * 32] = __uint_as_float(words[c * 32 + i]);
 #pragma unroll 1
-          for (int i = 0; i < 32; ++i) line[i * 32] = fp4_finish<kGroup>(line[i * 32], fr, col_of[c * 32 + i], col_of[128 + c * 32 + i]);
+          for (int i0 = 0; i0 < 32; i0 += 4) {
+            float x[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] = line[(i0 + i) * 32];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) line[(i0 + i) * 32] = fp4_finish(x[i], fr, col_of[c * 32 + i0 + i], col_of[128 + c * 32 + i0 + i]);
+          }
 #pragma unroll
           for (int i = 0; i < 32; ++i) words[c * 32 + i] = __float_as_uint(line[i * 32]);
         }
@@ -347,6 +354,15 @@ gemm_fp4_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
       constexpr int COLS = kWide ? 32 : 64;
 #pragma unroll
       for (int round = 0; round < 128 / COLS; ++round) {
+        if (!far) {                                                    // (row factor * sum) * column factor + bias
+#pragma unroll
+          for (int i = round * (COLS / 2); i < (round + 1) * (COLS / 2); i += 2) {
+            const float4 f = *reinterpret_cast<const float4*>(col_of + 2 * i), b = *reinterpret_cast<const float4*>(col_of + 128 + 2 * i);
+            const float2 r = make_float2(fr, fr);
+            acc[i] = ffma2(fmul2(acc[i], r), make_float2(f.x, f.y), make_float2(b.x, b.y));
+            acc[i + 1] = ffma2(fmul2(acc[i + 1], r), make_float2(f.z, f.w), make_float2(b.z, b.w));
+          }
+        }
         if (lane == 0) bulk_store_read_done();                         // the previous box has left
         __syncwarp();
 #pragma unroll
@@ -366,7 +382,7 @@ gemm_fp4_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
           fence_proxy_async_smem();
           __syncwarp();
           if (lane == 0 && x < p.N) {
-            tma_store_2d_hint(&tmOut, smem_u32(box), x, row0, policy);
+            tma_store_2d_hint(&tmOut, smem_u32(box), x, row0, evict_first_policy());
             bulk_store_commit();
           }
         } else {
@@ -542,7 +558,7 @@ gemm_fp4_split_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_cons
           if (splits > 1) {
             part[row * 128 + quarter * 32 + lane] = __uint_as_float(r[i]);
           } else if (col < p.N && m0 + row < p.M) {
-            fp4_store_one<EPI>(p, m0 + row, col, fp4_finish<kGroup>(__uint_as_float(r[i]), row_of[row], fc, bias));
+            fp4_store_one<EPI>(p, m0 + row, col, fp4_finish(__uint_as_float(r[i]), row_of[row], fc, bias));
           }
         }
       }
@@ -567,7 +583,7 @@ gemm_fp4_split_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_cons
 #pragma unroll
           for (int r = 0; r < 8; ++r) sum += v[k][r];
           const int row = m0 + i0 + k * splits;
-          if (i0 + k * splits < rows) fp4_store_one<EPI>(p, row, col, fp4_finish<kGroup>(sum, row_of[row - m0], fc, bias));
+          if (i0 + k * splits < rows) fp4_store_one<EPI>(p, row, col, fp4_finish(sum, row_of[row - m0], fc, bias));
         }
       }
     }

@@ -41,7 +41,7 @@ FACTORS = [2.0 ** 100, 2.0 ** -100, 1.0, 2.0 ** 120, 2.0 ** -120, 2.0 ** 60, 2.0
 
 
 @pytest.mark.parametrize("kind", ["float16", "bfloat16", "float32"])
-@pytest.mark.parametrize("group,scale", [(16, 0), (32, 0), (32, 50)])
+@pytest.mark.parametrize("group,scale", [(16, 0), (32, 0), (32, 50), (32, -50)])
 @pytest.mark.parametrize("m,n,k", SIZES)
 def test_factors_of_opposite_size(B, m, n, k, group, scale, kind):
     import torch
