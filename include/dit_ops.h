@@ -230,8 +230,8 @@ dit_status dit_rotary(const dit_rotary_args *args, void *stream);
  * over the keys j <= kv_len - q_len + i of row i's request where `causal` (the new rows are the last ones of their context: whole prompts have
  * equal lengths, a single new token has q_len 1), over all keys of the request otherwise.  A row that sees no key gets zeros, and so does
  * one all of whose scores are -infinity.  Keys and values that a row does not see are never part of its result, whatever they hold.
- * Scores, their differences, the softmax and the sums are held in fp32, probabilities are rounded to the inputs' type for the second product;
- * scores of any size and infinite or NaN values are treated as dit_block_attention treats them.  A request's results do not depend on the
+ * Scores, their differences, the softmax and the sums are held in fp32, probabilities are rounded to the inputs' type for the second product (which
+ * adds about as much to a result's error as its own rounding to that type does); scores of any size and infinite or NaN values are treated as dit_block_attention treats them.  A request's results do not depend on the
  * values of the others.  Which of two kernels serves a request, and into how many parts long keys are cut, depends on the lengths and heads of the
  * whole batch: results may differ in their last bits with the batch that a request comes in.  The same call gives the same bits.
  *   q, k, v, out  device, type f16 or bf16, 16-byte aligned, leading dimensions multiples of 8 and >= n_heads * head_dim (q, out) or

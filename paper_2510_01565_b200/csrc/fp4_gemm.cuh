@@ -106,7 +106,7 @@ struct Cfg {
 // row in 32-bit words; 16-bit rows that start in the middle of a word are shifted by one element on the way.  `cols` columns from c0 on exist
 // (may be <= 0).
 // Whole boxes take a loop of a few instructions per row, without bounds.  Sectors written in part are what is left (9472 x 8191 x 1024
-// fp16 141 us, 8190 columns 90, 8192 columns 49).
+// fp16 137 us, 8190 columns 90, 8192 columns 46).
 template <int EPI>
 __device__ __forceinline__ void fp4_store_box(const Fp4GemmParams& p, const uint8_t* box, int lane, int row0, int c0, int cols) {
   constexpr bool kWide = EPI == kBlkF32;

@@ -179,6 +179,9 @@ __device__ __forceinline__ PromptItem prompt_item(const PromptBatch& batch, cons
 // A causal tile masks its last block or two.  Scores that a row does not see are dropped before its maximum.  Values that it does not
 // see meet a probability of zero, which an infinity or NaN would turn into NaN: in the blocks that some rows see only in part such values are
 // replaced by zeros in shared memory, and if there was one, the rows that do see it add it to their results at the end.
+// Probabilities are rounded to the inputs' type, in which the tensor cores take both operands of the second product; their sum is of the unrounded ones.
+// It moves a result of many keys by 1.5e-3 of itself in bf16 and 1.5e-4 in fp16 (2-norms), where the rounding of the result alone moves it by 1.65e-3 and
+// 2.1e-4.  Keeping what is rounded off would take a third product of the same size beside the two.
 // What bounds it: the softmax chain of two tiles against the products of one S buffer, 1.7 us per key block and pair of tiles, 2.6 us more per pair.
 // 8192 rows, 32 heads of 128 over 8 key heads, causal: 396-430 us (1.28-1.39 PFLOP/s) under the power cap.
 // kParts: items may be parts of pairs.  (A kernel of its own: with it the ordinary one took 4 to 8 % longer, 8192 rows of 32 heads 452 us for 419.)
@@ -601,7 +604,7 @@ done:
 // Few rows.  The query rows of a request and the heads of a group make rows of one product with the group's keys (row i * group + h), 16 to
 // a CTA, so that a new token's heads read the keys once.  Reading the stored keys and values is the bound: a CTA takes p.chunk of them,
 // chosen so that one CTA per SM covers the batch, however uneven its requests are.  Inside it is block_rows_kernel: K and V by TMA in
-// tiles of 64 keys through one ring, four warps with 16 keys of every tile each, warp-level products, the warps' results joined in
+// tiles of 64 keys through one ring, four warps with 16 keys of every tile each, warp-level products (probabilities rounded as above), the warps' results joined in
 // shared memory.  A request with one chunk writes its rows; the parts of the others go to memory as (sums, maximum, sum of
 // probabilities) and prompt_join_kernel joins them in their order.
 // 32 heads of 128 over 8 key heads, us: one row against 32768 keys (134 MB) 28, of which 3 are the joining kernel; 64 rows of 64 requests against 4096 keys
