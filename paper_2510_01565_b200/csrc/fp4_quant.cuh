@@ -120,7 +120,7 @@ template <int kType, bool kVec>
 __device__ __forceinline__ uint4 load_run(const typename QuantIn<kType>::Elem* src, int n, bool before) {
   constexpr int EPL = QuantIn<kType>::EPL;
   if (n >= EPL) {
-    if constexpr (kVec) return load_once(src);
+    if constexpr (kVec) return load_passing(src);
     if constexpr (kType == 2) {
       return make_uint4(__float_as_uint(*src), __float_as_uint(src[1]), __float_as_uint(src[2]), __float_as_uint(src[3]));
     } else {
@@ -189,7 +189,7 @@ quantize_fp4_kernel(const Fp4QuantParams p) {
     for (int i = 0; i < kLoads; ++i) {
       const int c = base + (i * THREADS + at) * EPL, n = there ? p.cols - c : 0;
       if (W == 2 && n >= EPL) {
-        if constexpr (W == 2) load_once_v8(raw[i], src + c);
+        if constexpr (W == 2) load_passing_v8(raw[i], src + c);
       } else {
 #pragma unroll
         for (int w = 0; w < W; ++w) raw[i][w] = load_run<kType, (kBytes > 0)>(src + c + w * EPW, n - w * EPW, c + w > 0);

@@ -282,10 +282,17 @@ __device__ __forceinline__ uint4 load_once(const void* p) {
   return v;
 }
 
-// 32 bytes that are read once (address a multiple of 32)
-__device__ __forceinline__ void load_once_v8(uint4 (&v)[2], const void* p) {
-  asm volatile("ld.global.nc.L1::no_allocate.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-               : "=r"(v[0].x), "=r"(v[0].y), "=r"(v[0].z), "=r"(v[0].w), "=r"(v[1].x), "=r"(v[1].y), "=r"(v[1].z), "=r"(v[1].w) : "l"(p));
+// The same in a kernel that starts while the one in front of it still writes what is loaded here (await_predecessor): the non-coherent path is for memory
+// that nothing changes while the kernel runs.
+__device__ __forceinline__ uint4 load_passing(const void* p) {
+  uint4 v;
+  asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p) : "memory");
+  return v;
+}
+// 32 bytes (address a multiple of 32)
+__device__ __forceinline__ void load_passing_v8(uint4 (&v)[2], const void* p) {
+  asm volatile("ld.global.L1::no_allocate.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(v[0].x), "=r"(v[0].y), "=r"(v[0].z), "=r"(v[0].w), "=r"(v[1].x), "=r"(v[1].y), "=r"(v[1].z), "=r"(v[1].w) : "l"(p) : "memory");
 }
 
 // 32 bytes to global memory in one store (address a multiple of 32): a whole sector per thread
