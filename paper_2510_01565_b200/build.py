@@ -16,7 +16,7 @@ NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", 
 
 
 def _newest_source_mtime() -> float:
-    t = 0.0
+    t = os.path.getmtime(__file__)                 # (it holds the flags)
     for root in (CSRC, os.path.join(os.path.dirname(HERE), "include")):
         for name in os.listdir(root):
             t = max(t, os.path.getmtime(os.path.join(root, name)))

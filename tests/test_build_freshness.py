@@ -98,3 +98,12 @@ def test_a_source_that_changes_while_it_is_compiled_is_compiled_again(project, m
     assert project() == ["one.cu"]
     monkeypatch.setattr(build.subprocess, "Popen", popen)
     assert project() == ["one.cu"]
+
+
+def test_the_file_that_holds_the_flags_counts_as_a_source(tmp_path, monkeypatch):
+    later = tmp_path / "build.py"
+    later.write_text("")
+    at = build._newest_source_mtime() + 1000.0
+    os.utime(later, (at, at))
+    monkeypatch.setattr(build, "__file__", str(later))
+    assert build._newest_source_mtime() == at
